@@ -310,6 +310,147 @@ MULOCO_API muloco_status muloco_topk_sparsify(muloco_ctx* ctx, const float* x, i
  * without changing any state. */
 MULOCO_API muloco_status muloco_pseudogradient(muloco_ctx* ctx, int32_t tensor, float* psi_out);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators of the training step around the optimizer.  They take any context (one made with
+ * n_tensors == 0 will do), run on its stream and report as the calls above do: argument errors at
+ * once, conditions found on the device through muloco_sync_status.
+ * --------------------------------------------------------------------------------------------- */
+
+/* AdamW (Section 4.3) over many tensors in one launch, outside the MuLoCo state, with moments in 32 or
+ * in 8 bits.  Step t of a tensor with gradient g:
+ *     m <- beta1 m + (1 - beta1) g;   v <- beta2 v + (1 - beta2) g^2
+ *     theta <- theta - a ((m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps) + lambda wd_mult theta),
+ *     a = lr * lr_scale * lr_mult
+ * and, where `copy` is given, copy <- bf16(theta) (the working copy of a forward pass in bf16).
+ * state_bits == 32: state1 = m, state2 = v, float32 arrays of n elements; no scales.
+ * state_bits == 8: blocks of MULOCO_ADAMW_BLOCK consecutive elements of a tensor (the last one may be
+ *   short) share a float32 scale per moment:
+ *     m = c1 * scale1[block], c1 int8 in -127..127;    v = (c2 * scale2[block])^2, c2 uint8 in 0..255
+ *   state1 / state2 hold the codes, n rounded up to whole blocks; scale1 / scale2 one entry per block.
+ *   The second moment is linear in its ROOT, the quantity the update divides by: its relative error
+ *   is that of the root's code, and a code is at least 1 wherever v > 0, so that no denominator
+ *   vanishes.  After the float32 update (products and sums rounded one by one, no fused
+ *   multiply-add), scale = (largest |x| of the block) / top (x = m, top = 127; x = sqrt(v), top = 255) and
+ *     code = floor(x * (top / largest |x|) + u),   0 <= u < 1, clamped to the code's range
+ *   (a block whose largest |x| is at most 1e-36: codes as of x = 0).  Rounding with the dither u keeps
+ *   the averages unbiased: a step changes v by about (1 - beta2) v, often less than half a code, which
+ *   rounding to nearest would lose step after step.  u = 2^-16 times the low (first moment) or high
+ *   (second) half of hash((e + hash(hash(seed) + t)) mod 2^32), e = the element's index when the
+ *   tensors are laid out one after the other, each padded to whole blocks, and hash = Mueller's 32-bit
+ *   integer hash (twice: x ^= x >> 16, x *= 0x45d9f3b; then x ^= x >> 16).  Results do not depend on
+ *   the launch: the same call gives the same bits.
+ * A non-finite gradient raises MULOCO_ENONFINITE (the step is still applied).
+ * Gradients and parameters may have any alignment of their type (16 bytes is fastest); state1 and
+ * state2 must be 16-byte aligned, scales 4-byte aligned. */
+#define MULOCO_ADAMW_BLOCK 256
+typedef struct muloco_adamw muloco_adamw; /* opaque: a list of tensors and their device tables */
+typedef struct {
+  float lr, beta1, beta2, eps, weight_decay;
+  int32_t bias_correction; /* 0: the factors 1 / (1 - beta^t) are left out                     */
+  int32_t state_bits;      /* 32 or 8                                                          */
+  int32_t grad_dtype;      /* muloco_dtype                                                     */
+  uint32_t seed;           /* of the dither (8-bit states)                                     */
+} muloco_adamw_config;
+typedef struct {
+  int64_t n;              /* elements; 0 is allowed (the tensor is skipped)                    */
+  float* theta;           /* float32 parameters                                                */
+  void* copy;             /* bf16 copy of the parameters, or NULL                              */
+  const void* grad;       /* gradient used by steps that are given no table; may be NULL       */
+  void* state1;
+  void* state2;
+  float* scale1;          /* NULL with 32-bit states                                           */
+  float* scale2;
+  float wd_mult, lr_mult; /* as in muloco_tensor_desc (NaN lr_mult: 1)                         */
+} muloco_adamw_tensor;
+/* Records the tensors and builds the device tables; the states are the caller's to initialise (zeros
+ * at the start, 8-bit scales too).  The context must outlive the result. */
+MULOCO_API muloco_status muloco_adamw_create(muloco_ctx* ctx, const muloco_adamw_config* cfg,
+                                             const muloco_adamw_tensor* tensors, int32_t n_tensors,
+                                             muloco_adamw** out);
+/* Step number `step` (1, 2, ...; the caller counts) of all tensors.  `grads`: host table of device
+ * pointers [n_tensors], or NULL for the gradients named at create time. */
+MULOCO_API muloco_status muloco_adamw_step(muloco_adamw* opt, const void* const* grads, int64_t step,
+                                           float lr_scale);
+/* The moments of 8-bit states as the float32 values they stand for: m and v are device arrays of
+ * the padded layout (tensors one after the other, each padded to whole blocks). */
+MULOCO_API muloco_status muloco_adamw_moments(muloco_adamw* opt, float* m, float* v);
+/* Waits for the context's stream and releases the tables.  NULL is allowed. */
+MULOCO_API void muloco_adamw_destroy(muloco_adamw* opt);
+
+/* Root-mean-square norm of every query and key head and the position rotation, one pass over memory:
+ *     n = gain * x / sqrt(mean(x^2) + eps);     out = n turned pair by pair by the angles of its position
+ *     (a, b) -> (a cos - b sin, b cos + a sin)
+ * over the first rotary_dim entries of the head: pair i is (i, i + rotary_dim / 2), or (2i, 2i + 1) when
+ * `interleaved` is set; the other entries are only normed.  cos and sin are float32 tables
+ * [table_len][rotary_dim / 2]; a token's row is positions[token], or the token's index when
+ * positions is NULL.  A position outside the table raises MULOCO_EINVAL through muloco_sync_status,
+ * and the token's rows come out as NaN.
+ * q is [tokens][heads_q][head_dim] and k [tokens][heads_k][head_dim] of `dtype`, each with its own token and
+ * head strides (elements; the entries of a head are consecutive); either head count may be 0.  The
+ * statistics and the rotation are float32, the result is rounded once.  q_out may be q (and k_out k) with the same
+ * strides; otherwise results must not overlap inputs.
+ * Limits (MULOCO_ESHAPE): head_dim even, 2..512; rotary_dim even, 0..head_dim; tokens < 2^31. */
+typedef struct {
+  int64_t tokens;
+  int64_t table_len;
+  int32_t heads_q, heads_k, head_dim, rotary_dim;
+  int32_t dtype;        /* muloco_dtype of q, k and of what is made from them                  */
+  int32_t interleaved;
+  float eps;
+  int32_t pad;
+  const float* gain_q;  /* [head_dim] float32, NULL: ones                                      */
+  const float* gain_k;
+  const float* cos;
+  const float* sin;
+  const int64_t* positions;
+  const void* q;
+  const void* k;
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+} muloco_qk_norm;
+/* out strides: of q_out and k_out (forward) */
+MULOCO_API muloco_status muloco_qk_norm_rope(muloco_ctx* ctx, const muloco_qk_norm* a, void* q_out,
+                                             int64_t qo_token_stride, int64_t qo_head_stride, void* k_out,
+                                             int64_t ko_token_stride, int64_t ko_head_stride);
+/* Its backward pass: from the gradients dq_out, dk_out of the results, the gradients of the inputs (q and k are the
+ * forward pass's inputs; nothing else is kept from it) and of the gains, summed over all tokens and heads in a fixed
+ * order (float32 [head_dim], written, not added to; NULL: not wanted).  The gradients of the results have
+ * their own strides; dq and dk are dense, [tokens][heads][head_dim]. */
+MULOCO_API muloco_status muloco_qk_norm_rope_backward(muloco_ctx* ctx, const muloco_qk_norm* a, const void* dq_out,
+                                                      int64_t dqo_token_stride, int64_t dqo_head_stride,
+                                                      const void* dk_out, int64_t dko_token_stride,
+                                                      int64_t dko_head_stride, void* dq, void* dk,
+                                                      float* dgain_q, float* dgain_k);
+
+/* Gated feed-forward block on the matrices W1, W3 (d x F) and W2 (F x d) of a layer, all bf16 row-major:
+ *     G = X W1,  U = X W3,  H = act(G) * U,  Y = H W2
+ * G, U and the gated product come from one kernel (the two accumulators of a tile lie side by side in tensor memory),
+ * Y from a second.  act is g sigma(g) (MULOCO_ACT_SILU) or the tanh form of gelu (MULOCO_ACT_GELU).  X and Y are
+ * [tokens][d]; H is [tokens][F] and always written; G and U are [tokens][F], for the backward pass, or NULL.
+ * Sums are float32, every result is rounded once (Y from the rounded H).
+ * ld*: row strides in elements (G, U, H, Y dense).  d, F and the strides are multiples of 8 and the
+ * matrices 16-byte aligned (MULOCO_ESHAPE / MULOCO_EINVAL otherwise); tokens may be 0.
+ * The kernels are persistent but their thread blocks do not wait for one another. */
+enum { MULOCO_ACT_SILU = 0, MULOCO_ACT_GELU = 1 };
+typedef struct {
+  int64_t tokens, d, F;
+  int64_t ldx, ldw1, ldw3, ldw2;
+  const void* x;
+  const void* w1;
+  const void* w3;
+  const void* w2;
+  int32_t activation;
+  int32_t pad;
+} muloco_ffn;
+MULOCO_API muloco_status muloco_gated_ffn(muloco_ctx* ctx, const muloco_ffn* a, void* g, void* u, void* h, void* y);
+/* Backward pass, from dY [tokens][d] (row stride lddy) and the forward pass's G, U, H:
+ *     dH = dY W2^T,  dG = dH * U * act'(G),  dU = dH * act(G)       (one kernel; dH stays float32)
+ *     dX = dG W1^T + dU W3^T,  dW1 = X^T dG,  dW3 = X^T dU,  dW2 = H^T dY     (one kernel)
+ * dG and dU are bf16 [tokens][F] scratch that the caller provides (written; they are valid results too).  Any of dx,
+ * dw1, dw3, dw2 may be NULL (not wanted); they are dense bf16 and written, not added to. */
+MULOCO_API muloco_status muloco_gated_ffn_backward(muloco_ctx* ctx, const muloco_ffn* a, const void* dy, int64_t lddy,
+                                                   const void* g, const void* u, const void* h, void* dg, void* du,
+                                                   void* dx, void* dw1, void* dw3, void* dw2);
+
 /* Small host state for checkpoint/resume: inner step counters per worker and
  * sync counters per fragment.  Call with blob == NULL to get the size. */
 MULOCO_API muloco_status muloco_get_state(const muloco_ctx* ctx, void* host_blob, size_t* nbytes);

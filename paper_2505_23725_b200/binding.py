@@ -27,6 +27,8 @@ NS_BF16, NS_FP32 = 0, 1
 F32, BF16 = 0, 1
 DEBUG_WAIT_LIMIT_NS, DEBUG_WITHHOLD_COPY, DEBUG_CANARIES, DEBUG_CORRUPT_CANARY = 1, 2, 3, 4
 PHASES = ["prologue", "ns", "adamw", "sync", "copy"]
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+ADAMW_BLOCK = 256              # elements that share a scale in 8-bit AdamW states
 
 EXPORTS = [
     "muloco_create", "muloco_destroy", "muloco_inner_step", "muloco_inner_step_host",
@@ -35,6 +37,8 @@ EXPORTS = [
     "muloco_set_timing", "muloco_get_timings", "muloco_sync_status", "muloco_last_error",
     "muloco_newton_schulz_static", "muloco_debug_set", "muloco_check_workspace",
     "muloco_shard_layout", "muloco_shard_delta", "muloco_shard_step", "muloco_shard_broadcast",
+    "muloco_adamw_create", "muloco_adamw_step", "muloco_adamw_moments", "muloco_adamw_destroy",
+    "muloco_qk_norm_rope", "muloco_qk_norm_rope_backward", "muloco_gated_ffn", "muloco_gated_ffn_backward",
 ]
 
 
@@ -62,6 +66,35 @@ class Buffers(C.Structure):
     _fields_ = [("theta_k", C.POINTER(C.c_void_p)), ("theta_g", C.POINTER(C.c_void_p)),
                 ("outer_u", C.POINTER(C.c_void_p)), ("state1_k", C.POINTER(C.c_void_p)),
                 ("state2_k", C.POINTER(C.c_void_p)), ("ef_k", C.POINTER(C.c_void_p))]
+
+
+class AdamwConfig(C.Structure):
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
+                ("weight_decay", C.c_float), ("bias_correction", C.c_int32), ("state_bits", C.c_int32),
+                ("grad_dtype", C.c_int32), ("seed", C.c_uint32)]
+
+
+class AdamwTensor(C.Structure):
+    _fields_ = [("n", C.c_int64), ("theta", C.c_void_p), ("copy", C.c_void_p), ("grad", C.c_void_p),
+                ("state1", C.c_void_p), ("state2", C.c_void_p), ("scale1", C.c_void_p), ("scale2", C.c_void_p),
+                ("wd_mult", C.c_float), ("lr_mult", C.c_float)]
+
+
+class QkNorm(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("table_len", C.c_int64),
+                ("heads_q", C.c_int32), ("heads_k", C.c_int32), ("head_dim", C.c_int32), ("rotary_dim", C.c_int32),
+                ("dtype", C.c_int32), ("interleaved", C.c_int32), ("eps", C.c_float), ("pad", C.c_int32),
+                ("gain_q", C.c_void_p), ("gain_k", C.c_void_p), ("cos", C.c_void_p), ("sin", C.c_void_p),
+                ("positions", C.c_void_p), ("q", C.c_void_p), ("k", C.c_void_p),
+                ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64)]
+
+
+class Ffn(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("d", C.c_int64), ("F", C.c_int64),
+                ("ldx", C.c_int64), ("ldw1", C.c_int64), ("ldw3", C.c_int64), ("ldw2", C.c_int64),
+                ("x", C.c_void_p), ("w1", C.c_void_p), ("w3", C.c_void_p), ("w2", C.c_void_p),
+                ("activation", C.c_int32), ("pad", C.c_int32)]
 
 
 class MulocoError(RuntimeError):
@@ -110,9 +143,18 @@ def load_library():
     lib.muloco_shard_step.argtypes = [vp, i32, i32, i32, vp, vp]
     lib.muloco_shard_broadcast.argtypes = [vp, i32, i32, vp]
     lib.muloco_newton_schulz_static.argtypes = [vp, vp, i32, i64, i64, vp, C.c_char_p, C.c_size_t]
+    lib.muloco_adamw_create.argtypes = [vp, C.POINTER(AdamwConfig), C.POINTER(AdamwTensor), i32, C.POINTER(vp)]
+    lib.muloco_adamw_step.argtypes = [vp, C.POINTER(vp), i64, f32]
+    lib.muloco_adamw_moments.argtypes = [vp, vp, vp]
+    lib.muloco_adamw_destroy.argtypes = [vp]
+    lib.muloco_adamw_destroy.restype = None
+    lib.muloco_qk_norm_rope.argtypes = [vp, C.POINTER(QkNorm), vp, i64, i64, vp, i64, i64]
+    lib.muloco_qk_norm_rope_backward.argtypes = [vp, C.POINTER(QkNorm), vp, i64, i64, vp, i64, i64, vp, vp, vp, vp]
+    lib.muloco_gated_ffn.argtypes = [vp, C.POINTER(Ffn), vp, vp, vp, vp]
+    lib.muloco_gated_ffn_backward.argtypes = [vp, C.POINTER(Ffn), vp, i64] + [vp] * 9
     for name in EXPORTS:
         fn = getattr(lib, name)
-        if name not in ("muloco_destroy", "muloco_last_error"):
+        if name not in ("muloco_destroy", "muloco_last_error", "muloco_adamw_destroy"):
             fn.restype = i32
     _lib = lib
     return lib
@@ -223,7 +265,348 @@ def _ptr_table(ptrs: Sequence[int]):
     return arr
 
 
-class MuLoCo:
+class _Operators:
+    """The operators of the training step around the optimizer, as methods of whatever owns a library
+    context (self.ctx, self.lib, self.stream, self.device, self.torch, self._check).
+
+    Work runs on the context's stream.  When the caller's current stream is another one, the context's
+    stream first waits for it and it then waits for the context's, and the tensors are
+    recorded on the context's stream, so inputs, results and their memory may be used as usual."""
+
+    def _enter(self, tensors):
+        cur = self.torch.cuda.current_stream(self.device)
+        if cur.cuda_stream == self.stream.cuda_stream:
+            return None
+        self.stream.wait_stream(cur)
+        for t in tensors:
+            if t is not None:
+                t.record_stream(self.stream)
+        return cur
+
+    def _leave(self, cur, tensors):
+        if cur is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self.stream)
+            cur.wait_stream(self.stream)
+
+    def _need(self, name, t, dtype, shape):
+        """t is a tensor of this context's device with the given type and shape (None: any size)."""
+        if t.device != self.device:
+            raise ValueError(f"{name} must be on {self.device} (got {t.device})")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
+        if t.dim() != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
+            raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
+
+    # -- norm of queries and keys with the rotation -----------------------------------------------
+    def _qk(self, q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved):
+        torch = self.torch
+        some = q if q is not None else k
+        if some is None:
+            raise ValueError("q and k are both None")
+        if some.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"q and k must be float32 or bfloat16 (got {some.dtype})")
+        if some.dim() != 3:
+            raise ValueError(f"q and k must be [tokens, heads, head_dim] (got {tuple(some.shape)})")
+        T, _, D = some.shape
+        for name, t in (("q", q), ("k", k)):
+            if t is not None:
+                self._need(name, t, some.dtype, (T, None, D))
+                if D > 1 and t.stride(2) != 1:
+                    raise ValueError(f"{name}: the entries of a head must be consecutive")
+        self._need("cos", cos, torch.float32, (None, None))
+        self._need("sin", sin, torch.float32, tuple(cos.shape))
+        if not (cos.is_contiguous() and sin.is_contiguous()):
+            raise ValueError("cos and sin must be contiguous")
+        if positions is not None:
+            self._need("positions", positions, torch.int64, (T,))
+            if not positions.is_contiguous():
+                raise ValueError("positions must be contiguous")
+        for name, t in (("gain_q", gain_q), ("gain_k", gain_k)):
+            if t is not None:
+                self._need(name, t, torch.float32, (D,))
+                if not t.is_contiguous():
+                    raise ValueError(f"{name} must be contiguous")
+        ptr = lambda t: None if t is None else t.data_ptr()          # noqa: E731
+        a = QkNorm(T, cos.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], D,
+                   2 * cos.shape[1], BF16 if some.dtype == torch.bfloat16 else F32, int(interleaved), eps, 0,
+                   ptr(gain_q), ptr(gain_k), cos.data_ptr(), sin.data_ptr(), ptr(positions), ptr(q), ptr(k),
+                   *((0, 0) if q is None else q.stride()[:2]), *((0, 0) if k is None else k.stride()[:2]))
+        return a
+
+    def qk_norm_rope(self, q, k, cos, sin, positions=None, gain_q=None, gain_k=None, eps=1e-6, interleaved=False,
+                     out=None):
+        """muloco_qk_norm_rope: norm and rotation of the heads of q [tokens, heads, head_dim] and k (either may be
+        None).  cos and sin: float32 tables [length, rotary_dim / 2]; positions: int64 [tokens] or None
+        for 0, 1, ...  Returns (q_out, k_out), dense unless `out` = (q_out, k_out) gives them."""
+        torch = self.torch
+        a = self._qk(q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
+        if out is None:
+            out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+        else:
+            for name, o, t in (("q_out", out[0], q), ("k_out", out[1], k)):
+                if (o is None) != (t is None):
+                    raise ValueError(f"{name} is given without its input, or missing")
+                if o is not None:
+                    self._need(name, o, t.dtype, tuple(t.shape))
+                    if t.shape[2] > 1 and o.stride(2) != 1:
+                        raise ValueError(f"{name}: the entries of a head must be consecutive")
+        used = (q, k, cos, sin, positions, gain_q, gain_k) + tuple(out)
+        cur = self._enter(used)
+        args = []
+        for o in out:
+            args += [None, 0, 0] if o is None else [o.data_ptr(), o.stride(0), o.stride(1)]
+        self._check(self.lib.muloco_qk_norm_rope(self.ctx, C.byref(a), *args))
+        self._leave(cur, ())
+        return tuple(out)
+
+    def qk_norm_rope_backward(self, dq_out, dk_out, q, k, cos, sin, positions=None, gain_q=None, gain_k=None,
+                              eps=1e-6, interleaved=False):
+        """muloco_qk_norm_rope_backward: from the gradients of the results, (dq, dk, dgain_q, dgain_k)."""
+        torch = self.torch
+        a = self._qk(q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
+        grads, args, gains = [], [], []
+        for name, y, t in (("dq_out", dq_out, q), ("dk_out", dk_out, k)):
+            if (y is None) != (t is None):
+                raise ValueError(f"{name} is given without its input, or missing")
+            if t is None:
+                grads.append(None)
+                gains.append(None)
+                args += [None, 0, 0]
+                continue
+            self._need(name, y, t.dtype, tuple(t.shape))
+            if t.shape[2] > 1 and y.stride(2) != 1:
+                raise ValueError(f"{name}: the entries of a head must be consecutive")
+            grads.append(torch.empty(t.shape, dtype=t.dtype, device=t.device))
+            gains.append(torch.empty(t.shape[2], dtype=torch.float32, device=t.device))
+            args += [y.data_ptr(), y.stride(0), y.stride(1)]
+        cur = self._enter((q, k, cos, sin, positions, gain_q, gain_k, dq_out, dk_out, *grads, *gains))
+        ptr = lambda t: None if t is None else t.data_ptr()          # noqa: E731
+        self._check(self.lib.muloco_qk_norm_rope_backward(self.ctx, C.byref(a), *args, ptr(grads[0]), ptr(grads[1]),
+                                                          ptr(gains[0]), ptr(gains[1])))
+        self._leave(cur, ())
+        return grads[0], grads[1], gains[0], gains[1]
+
+    # -- gated feed-forward block -----------------------------------------------------------------
+    def _ffn(self, x, w1, w3, w2, activation):
+        bf16 = self.torch.bfloat16
+        if activation not in ACTIVATIONS:
+            raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)} (got {activation!r})")
+        self._need("x", x, bf16, (None, None))
+        T, d = x.shape
+        self._need("w1", w1, bf16, (d, None))
+        F = w1.shape[1]
+        self._need("w3", w3, bf16, (d, F))
+        self._need("w2", w2, bf16, (F, d))
+        for name, t in (("x", x), ("w1", w1), ("w3", w3), ("w2", w2)):
+            if t.stride(1) != 1:
+                raise ValueError(f"{name}: the entries of a row must be consecutive")
+        return Ffn(T, d, F, self._ld(x), w1.stride(0), w3.stride(0), w2.stride(0),
+                   x.data_ptr(), w1.data_ptr(), w3.data_ptr(), w2.data_ptr(), ACTIVATIONS[activation], 0), T, d, F
+
+    @staticmethod
+    def _ld(t):
+        """Row stride; that of a single row does not matter and is taken as its length."""
+        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+    def gated_ffn(self, x, w1, w3, w2, activation="silu", save=True):
+        """muloco_gated_ffn: y = (act(x w1) * (x w3)) w2, all bf16.  Returns (y, saved): saved = (g, u, h) is what
+        the backward pass needs (None with save=False, and g and u are then not written)."""
+        torch = self.torch
+        a, T, d, F = self._ffn(x, w1, w3, w2, activation)
+        y = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
+        h = torch.empty((T, F), dtype=torch.bfloat16, device=x.device)
+        g = u = None
+        if save:
+            g, u = torch.empty_like(h), torch.empty_like(h)
+        cur = self._enter((x, w1, w3, w2, y, h, g, u))
+        self._check(self.lib.muloco_gated_ffn(self.ctx, C.byref(a), g.data_ptr() if save else None,
+                                              u.data_ptr() if save else None, h.data_ptr(), y.data_ptr()))
+        self._leave(cur, ())
+        return y, ((g, u, h) if save else None)
+
+    def gated_ffn_backward(self, dy, x, w1, w3, w2, saved, activation="silu"):
+        """muloco_gated_ffn_backward: (dx, dw1, dw3, dw2), bf16, from dy and the forward pass's saved = (g, u, h)."""
+        torch = self.torch
+        bf16 = torch.bfloat16
+        a, T, d, F = self._ffn(x, w1, w3, w2, activation)
+        self._need("dy", dy, bf16, (T, d))
+        if dy.stride(1) != 1:
+            raise ValueError("dy: the entries of a row must be consecutive")
+        for name, t in zip(("g", "u", "h"), saved):
+            self._need(name, t, bf16, (T, F))
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        g, u, h = saved
+        dg, du = (torch.empty((T, F), dtype=bf16, device=x.device) for _ in range(2))
+        dx = torch.empty((T, d), dtype=bf16, device=x.device)
+        dw1, dw3 = (torch.empty((d, F), dtype=bf16, device=x.device) for _ in range(2))
+        dw2 = torch.empty((F, d), dtype=bf16, device=x.device)
+        cur = self._enter((dy, x, w1, w3, w2, g, u, h, dg, du, dx, dw1, dw3, dw2))
+        self._check(self.lib.muloco_gated_ffn_backward(
+            self.ctx, C.byref(a), dy.data_ptr(), self._ld(dy), g.data_ptr(), u.data_ptr(), h.data_ptr(), dg.data_ptr(),
+            du.data_ptr(), dx.data_ptr(), dw1.data_ptr(), dw3.data_ptr(), dw2.data_ptr()))
+        self._leave(cur, ())
+        return dx, dw1, dw3, dw2
+
+
+class Context(_Operators):
+    """A library context without optimizer state: for the operators of the training step around the
+    optimizer (and AdamW lists) on `device` and `stream` (default: the current one)."""
+
+    def __init__(self, device="cuda:0", stream=None):
+        import torch
+
+        self.torch = torch
+        self.ctx = None
+        self.lib = load_library()
+        if not torch.cuda.is_available():
+            raise RuntimeError("no CUDA device: libmuloco has no CPU path")
+        self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        torch.cuda.set_device(self.device)
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        cfg = make_config(_cfg.Workload("operators", K=1, H=1, J=1, tensors=[], muon_lr=0.0, muon_beta=0.0,
+                                        muon_wd=0.0, outer_lr=1.0, outer_momentum=0.0))
+        ctx = C.c_void_p()
+        st = self.lib.muloco_create(C.byref(cfg), None, 0, None, C.c_void_p(self.stream.cuda_stream), C.byref(ctx))
+        if st != OK:
+            raise MulocoError(st, self.lib.muloco_last_error(None).decode())
+        self.ctx = ctx
+
+    def _check(self, st):
+        if st != OK:
+            raise MulocoError(st, self.lib.muloco_last_error(self.ctx).decode())
+
+    def sync_status(self):
+        """Waits for the stream; raises what the device reported since the last call."""
+        self._check(self.lib.muloco_sync_status(self.ctx))
+
+    def close(self):
+        if getattr(self, "ctx", None):
+            self.lib.muloco_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdamW:
+    """muloco_adamw_*: AdamW over a list of float32 tensors, one launch per step, states in 32 or 8 bits.
+
+    `owner` is a Context or a MuLoCo.  params: contiguous float32 tensors, updated in place; grads: tensors of the
+    same shapes (float32 or bf16) used by step() without arguments; copies: bf16 tensors that receive the new
+    parameters in the same pass.  The states live in flat buffers, every tensor starting on a multiple
+    of 256 elements: state1, state2 (float32, or int8 / uint8 codes) and scale1, scale2 (one float32 per 256 codes).
+    `steps` counts the steps taken; with it, the states are all there is to save for a checkpoint."""
+
+    def __init__(self, owner, params, grads=None, lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.0,
+                 bias_correction=True, state_bits=32, wd_mult=None, lr_mult=None, copies=None, seed=0, grad_dtype=None):
+        torch = owner.torch
+        self.opt = None
+        self.owner, self.lib, self.params, self.grads, self.copies = owner, owner.lib, list(params), grads, copies
+        n = len(self.params)
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        for name, seq in (("grads", grads), ("copies", copies), ("wd_mult", wd_mult), ("lr_mult", lr_mult)):
+            if seq is not None and len(seq) != n:
+                raise ValueError(f"{name} must have one entry per parameter")
+        if grad_dtype is None:
+            grad_dtype = grads[0].dtype if grads else torch.float32
+        if grad_dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("gradients must be float32 or bfloat16")
+        self.state_bits, self.grad_dtype = state_bits, grad_dtype
+        self.numel = [p.numel() for p in self.params]
+        self.offsets, off = [], 0
+        for k in self.numel:
+            self.offsets.append(off)
+            off += -(-k // ADAMW_BLOCK) * ADAMW_BLOCK
+        self.padded = off
+        for i, p in enumerate(self.params):
+            self._same(f"params[{i}]", p, torch.float32, p)
+            if copies is not None:
+                self._same(f"copies[{i}]", copies[i], torch.bfloat16, p)
+        if grads is not None:
+            self._check_grads(grads)
+        dev = owner.device
+        q8 = state_bits == 8
+        self.state1 = torch.zeros(off, dtype=torch.int8 if q8 else torch.float32, device=dev)
+        self.state2 = torch.zeros(off, dtype=torch.uint8 if q8 else torch.float32, device=dev)
+        self.scale1 = torch.zeros(off // ADAMW_BLOCK, dtype=torch.float32, device=dev) if q8 else None
+        self.scale2 = torch.zeros(off // ADAMW_BLOCK, dtype=torch.float32, device=dev) if q8 else None
+        self.steps = 0
+        cfg = AdamwConfig(lr, beta1, beta2, eps, weight_decay, int(bias_correction), state_bits,
+                          BF16 if grad_dtype == torch.bfloat16 else F32, seed)
+        table = (AdamwTensor * max(1, n))()
+        for i, p in enumerate(self.params):
+            o, e = self.offsets[i], table[i]
+            e.n, e.theta = self.numel[i], p.data_ptr()
+            e.copy = copies[i].data_ptr() if copies is not None else None
+            e.grad = grads[i].data_ptr() if grads is not None else None
+            e.state1 = self.state1.data_ptr() + o * self.state1.element_size()
+            e.state2 = self.state2.data_ptr() + o * self.state2.element_size()
+            if q8:
+                e.scale1 = self.scale1.data_ptr() + o // ADAMW_BLOCK * 4
+                e.scale2 = self.scale2.data_ptr() + o // ADAMW_BLOCK * 4
+            e.wd_mult = 1.0 if wd_mult is None else wd_mult[i]
+            e.lr_mult = 1.0 if lr_mult is None else lr_mult[i]
+        opt = C.c_void_p()
+        owner._check(self.lib.muloco_adamw_create(owner.ctx, C.byref(cfg), table, n, C.byref(opt)))
+        self.opt = opt
+
+    def _same(self, name, t, dtype, like):
+        if t.device != self.owner.device or t.dtype != dtype or t.shape != like.shape or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(like.shape)} on {self.owner.device}")
+
+    def _check_grads(self, grads):
+        for i, (g, p) in enumerate(zip(grads, self.params)):
+            self._same(f"grads[{i}]", g, self.grad_dtype, p)
+
+    def step(self, grads=None, lr_scale: float = 1.0):
+        """One step of all tensors, with the gradients named at construction or those given."""
+        table = None
+        if grads is not None:
+            if len(grads) != len(self.params):
+                raise ValueError("grads must have one entry per parameter")
+            self._check_grads(grads)
+            table = _ptr_table([g.data_ptr() for g in grads])
+        used = (*(grads if grads is not None else self.grads or ()), *self.params, *(self.copies or ()))
+        cur = self.owner._enter(used)
+        self.owner._check(self.lib.muloco_adamw_step(self.opt, table, self.steps + 1, lr_scale))
+        self.owner._leave(cur, ())
+        self.steps += 1
+
+    def moments(self):
+        """(m, v) as flat float32 tensors in the layout of the states: what the codes stand for, or the
+        32-bit states themselves.  Padding entries are zero."""
+        if self.state_bits == 32:
+            return self.state1, self.state2
+        torch = self.owner.torch
+        m, v = (torch.empty(self.padded, dtype=torch.float32, device=self.owner.device) for _ in range(2))
+        cur = self.owner._enter((m, v))
+        self.owner._check(self.lib.muloco_adamw_moments(self.opt, m.data_ptr(), v.data_ptr()))
+        self.owner._leave(cur, ())
+        return m, v
+
+    def close(self):
+        if getattr(self, "opt", None):
+            if self.owner.ctx:
+                self.lib.muloco_adamw_destroy(self.opt)
+            self.opt = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class MuLoCo(_Operators):
     """Owns the device state of one MuLoCo problem and forwards to the C ABI.
 
     State lives in flat torch buffers (one per replica / state kind) so that the

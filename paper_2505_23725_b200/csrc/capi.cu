@@ -204,6 +204,9 @@ struct muloco_ctx {
   std::vector<TimedSpan> spans;
   std::vector<cudaEvent_t> ev_pool;
   int64_t launches = 0;
+
+  // operators around the optimizer (ops_capi.cu)
+  float* qk_scratch = nullptr;     // gain-gradient partials of qk_norm.cu, then its tickets; allocated on first use
 };
 
 namespace {
@@ -489,6 +492,38 @@ muloco_status release_ring(muloco_ctx* c, char* host) {
 }  // namespace
 
 // ===========================================================================
+// ---- what the entry points of ops_capi.cu see of a context ----
+namespace muloco {
+
+CtxView ctx_view(muloco_ctx* c) { return CtxView{c->st, c->d_status, c->n_sms, c->wait_limit_ns}; }
+
+muloco_status ctx_fail(muloco_ctx* c, muloco_status s, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(c, s, "%s", buf);
+}
+
+void ctx_count_launches(muloco_ctx* c, int n) { c->launches += n; }
+
+float* ctx_qk_scratch(muloco_ctx* c, int** tickets) {
+  if (!c->qk_scratch) {
+    const size_t bytes = QK_SCRATCH_FLOATS * sizeof(float) + 256;
+    if (cudaMalloc(&c->qk_scratch, bytes) != cudaSuccess) {
+      c->qk_scratch = nullptr;
+      cudaGetLastError();
+      return nullptr;
+    }
+    if (cudaMemsetAsync(c->qk_scratch + QK_SCRATCH_FLOATS, 0, 256, c->st) != cudaSuccess) return nullptr;
+  }
+  *tickets = reinterpret_cast<int*>(c->qk_scratch + QK_SCRATCH_FLOATS);
+  return c->qk_scratch;
+}
+
+}  // namespace muloco
+
 extern "C" {
 
 MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_tensor_desc* tensors, int32_t n_tensors,
@@ -672,6 +707,7 @@ MULOCO_API void muloco_destroy(muloco_ctx* c) {
   if (c->sa_ws) cudaFree(c->sa_ws);
   if (c->sa_d_mats) cudaFree(c->sa_d_mats);
   if (c->d_status) cudaFree(c->d_status);
+  if (c->qk_scratch) cudaFree(c->qk_scratch);
   if (c->d_replicas) cudaFree(c->d_replicas);
   if (c->d_ef) cudaFree(c->d_ef);
   if (c->topk.hist) cudaFree(c->topk.hist);
@@ -1251,6 +1287,7 @@ MULOCO_API muloco_status muloco_sync_status(muloco_ctx* c) {
   if (h) CK(cudaMemset(c->d_status, 0, sizeof(int)));
   if (h & ST_TIMEOUT) return fail(c, MULOCO_ETIMEOUT, "a bounded wait inside a kernel ran out");
   if (h & ST_BOUNDS) return fail(c, MULOCO_ECUDA, "a kernel rejected an out-of-range index");
+  if (h & ST_POSITION) return fail(c, MULOCO_EINVAL, "a position lies outside the rotation's table");
   if (h & ST_NONFINITE)
     return fail(c, MULOCO_ENONFINITE, "non-finite value: a pseudogradient, the Newton-Schulz input of a hidden matrix, or a gradient given to AdamW");
   return MULOCO_OK;

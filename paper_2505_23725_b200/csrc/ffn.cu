@@ -1,0 +1,566 @@
+// Gated feed-forward block on the 5th-generation tensor cores: tcgen05.mma with fp32 accumulators in
+// tensor memory, operands staged by TMA (128-byte swizzle), warp-specialised persistent thread blocks.
+//
+// One kernel body serves every product of the block; a launch works through the tiles of up to four
+// products whose tiles do not depend on one another:
+//   forward   G | U = X W1 | X W3, gated in the epilogue            then   Y = H W2
+//   backward  dH = dY W2^T, turned into dG and dU in the epilogue   then   dX, dW1, dW3, dW2 in one launch
+// An operand whose contraction index is its contiguous axis is staged K-major (64 x 128 boxes), one whose
+// other index is contiguous MN-major (two atoms of 64 columns by 64 contraction rows); so no matrix is ever transposed
+// in memory: X serves G = X W1 K-major and dW1 = X^T dG MN-major, and W1 likewise.
+//
+// Tile: a pair of CTAs on neighbouring SMs computes 256 x 256 with tcgen05.mma.cta_group::2 (each CTA stages
+// its 128 rows of the left operand and half of the right one and drains its own 128 accumulator rows).  For the
+// gated product the two halves of the right operand are 128 columns of W1 and the same 128 columns of W3: an accumulator
+// row then holds G in columns 0..127 and U in columns 128..255, and the activation and the product are
+// register arithmetic of the epilogue.
+//
+// Roles: warp 0 issues the copies, warp 1 the MMAs, warps 2..9 run the epilogue (two warps per 32 accumulator
+// lanes, half of the columns each).  Two accumulators alternate, so the epilogue of a tile runs beside the
+// products of the next.  Thread blocks never wait for one another across a pair, and every wait is bounded: when one
+// runs out the block raises ST_TIMEOUT, frees its tensor memory and returns.
+#include <string.h>
+
+#include "internal.h"
+#include "tc_ptx.cuh"
+
+namespace muloco {
+
+namespace {
+
+constexpr int BK = 64;                       // contraction slab: 64 bf16 = one 128-byte swizzle row
+constexpr int UMMA_K = 16;
+constexpr int CG = 2;                        // CTAs per tile
+constexpr int BM = 128;                      // rows per CTA
+constexpr int TM = 128 * CG, BN = 128 * CG;  // tile
+constexpr int EPI_WARPS = 8;
+constexpr int FFN_THREADS = 64 + 32 * EPI_WARPS;
+constexpr int STAGES = 6;
+constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = 128 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+constexpr uint32_t SMEM_BYTES = STAGES * STAGE_BYTES + 1024u;
+constexpr uint32_t TMEM_COLS = 2 * BN;
+constexpr int MAX_PROBS = 4, MAX_MAPS = 12;
+constexpr int GROUP_M = 8;                   // tile rows that are worked through together (L2 reuse)
+
+enum Epi : int { EPI_STORE = 0, EPI_GATE = 1, EPI_GATE_BACK = 2 };
+
+struct Maps { CUtensorMap m[MAX_MAPS]; };
+
+// One product: out [M][N] = sum over its (one or two) operand pairs.
+struct Prob {
+  int tile_begin, m_tiles, n_tiles;
+  int M, N;                 // result extents; EPI_GATE: N = F, a tile is 128 columns of it
+  int slabs0, slabs;        // contraction slabs of the first operand pair, of both
+  int a_mn, b_mn;           // operand is staged MN-major
+  int a_wide, b_wide;       // MN-major map delivers both atoms in one copy
+  int map_a[2], map_b[2];   // per operand pair (EPI_GATE: map_b = W1, W3)
+  void* out;                // EPI_GATE: H; EPI_GATE_BACK: dG
+  void* out2;               // EPI_GATE: G or NULL; EPI_GATE_BACK: dU
+  void* out3;               // EPI_GATE: U or NULL
+  const void* in1;          // EPI_GATE_BACK: G, U
+  const void* in2;
+};
+
+struct Params {
+  Prob prob[MAX_PROBS];
+  int n_probs, total_tiles, epi, act;
+  int* status;
+  unsigned long long wait_limit_ns;
+};
+
+struct Tile { int q, m, n; };
+
+__device__ __forceinline__ Tile decode(const Params& p, int tile) {
+  Tile t;
+  t.q = 0;
+#pragma unroll
+  for (int i = 1; i < MAX_PROBS; ++i)
+    if (i < p.n_probs && tile >= p.prob[i].tile_begin) t.q = i;
+  const Prob& b = p.prob[t.q];
+  const int local = tile - b.tile_begin;
+  const int per = GROUP_M * b.n_tiles;
+  const int g = local / per, rem = local - g * per;
+  const int left = b.m_tiles - g * GROUP_M;
+  const int size = left < GROUP_M ? left : GROUP_M;
+  t.n = rem / size;
+  t.m = g * GROUP_M + (rem - t.n * size);
+  return t;
+}
+
+// 16 bf16 values (32 bytes) per access where the row allows it, else 8.
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
+               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+               : "memory");
+}
+__device__ __forceinline__ void ld_global_32(const void* p, uint32_t* v) {
+  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+               : "l"(p));
+}
+// 32 consecutive values of a row of which the first `n` (a multiple of 8) exist.
+__device__ __forceinline__ void store_row32(__nv_bfloat16* row, const float (&f)[32], int n, bool wide) {
+  if (wide && n >= 32) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = pack_bf16x2(f[h * 16 + 2 * i], f[h * 16 + 2 * i + 1]);
+      st_global_32(row + h * 16, v);
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+      if (h * 8 < n)
+        *reinterpret_cast<uint4*>(row + h * 8) =
+            make_uint4(pack_bf16x2(f[h * 8], f[h * 8 + 1]), pack_bf16x2(f[h * 8 + 2], f[h * 8 + 3]),
+                       pack_bf16x2(f[h * 8 + 4], f[h * 8 + 5]), pack_bf16x2(f[h * 8 + 6], f[h * 8 + 7]));
+  }
+}
+__device__ __forceinline__ void load_row32(const __nv_bfloat16* row, uint32_t (&v)[16], int n, bool wide) {
+  if (wide && n >= 32) {
+    ld_global_32(row, v);
+    ld_global_32(row + 16, v + 8);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      uint4 u = make_uint4(0u, 0u, 0u, 0u);
+      if (h * 8 < n) u = *reinterpret_cast<const uint4*>(row + h * 8);
+      v[h * 4] = u.x; v[h * 4 + 1] = u.y; v[h * 4 + 2] = u.z; v[h * 4 + 3] = u.w;
+    }
+  }
+}
+
+// act(g) = g sigma and, for the backward pass, its slope.  sigma is the logistic function of g (silu) or of
+// 2 sqrt(2 / pi) (g + 0.044715 g^3), which makes g sigma the tanh form of gelu.  exp and the quotient are the fast ones (a few
+// units in the last place of float32): the results are rounded to 8 bits of mantissa.
+constexpr float GELU_K = 1.5957691216057308f, GELU_C = 0.044715f;
+__device__ __forceinline__ float sigma(float p) { return __fdividef(1.0f, 1.0f + __expf(-p)); }
+template <int ACT>
+__device__ __forceinline__ float act_value(float g) {
+  if (ACT == MULOCO_ACT_SILU) return g * sigma(g);
+  return g * sigma(GELU_K * fmaf(GELU_C * g * g, g, g));
+}
+template <int ACT>
+__device__ __forceinline__ void act_both(float g, float& value, float& slope) {
+  float s, k;
+  if (ACT == MULOCO_ACT_SILU) {
+    s = sigma(g);
+    k = g;
+  } else {
+    const float c = GELU_C * g * g;
+    s = sigma(GELU_K * fmaf(c, g, g));
+    k = GELU_K * fmaf(3.0f * c, g, g);
+  }
+  value = g * s;
+  slope = fmaf(s * (1.0f - s), k, s);
+}
+
+template <int EPI, int ACT>
+__global__ void __launch_bounds__(FFN_THREADS, 1)
+ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) {
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bar_full[STAGES];     // used in the CTA of rank 0
+  __shared__ __align__(8) uint64_t bar_empty[STAGES];
+  __shared__ __align__(8) uint64_t bar_tfull[2];
+  __shared__ __align__(8) uint64_t bar_tempty[2];        // used in the CTA of rank 0
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ volatile int abort_flag;
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint64_t limit = p.wait_limit_ns;
+  const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&bar_full[s]), 1);
+      mbar_init(smem_u32(&bar_empty[s]), 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(smem_u32(&bar_tfull[a]), 1);
+      mbar_init(smem_u32(&bar_tempty[a]), EPI_WARPS * CG);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc<CG>(smem_u32(&tmem_base_slot), TMEM_COLS);
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_base_slot;
+
+  if (warp == 0) {
+    // ------------------------------ TMA producer ------------------------------
+    if (lane == 0) {
+      const uint32_t empty0 = smem_u32(&bar_empty[0]);
+      const uint32_t full0 = smem_u32(&bar_full[0]);
+      const uint32_t full0_bar = map_to_rank(full0, 0);   // both CTAs' copies are counted on the barrier of rank 0
+      uint32_t stage = 0, phase = 0;
+      bool alive = true;
+      for (int tile = worker; alive && tile < p.total_tiles; tile += workers) {
+        const Tile t = decode(p, tile);
+        const Prob& b = p.prob[t.q];
+        const int row_a = t.m * TM + (int)rank * BM;
+        // gated product: this CTA's half of the right operand is W1 (rank 0) or W3 (rank 1), same columns
+        const int col_b = (EPI == EPI_GATE) ? t.n * 128 : t.n * BN + (int)rank * 128;
+        for (int kb = 0; kb < b.slabs; ++kb) {
+          if (!mbar_wait(empty0 + stage * 8u, phase ^ 1u, &abort_flag, limit)) { alive = false; break; }
+          const uint32_t sa = smem_base + stage * STAGE_BYTES;
+          const uint32_t sb = sa + A_BYTES;
+          const uint32_t bar = full0_bar + stage * 8u;
+          if (rank == 0) mbar_expect_tx(full0 + stage * 8u, CG * STAGE_BYTES);
+          const int second = kb >= b.slabs0;
+          const int k0 = (second ? kb - b.slabs0 : kb) * BK;
+          const CUtensorMap* ma = &maps.m[b.map_a[second]];
+          const CUtensorMap* mb = &maps.m[b.map_b[(EPI == EPI_GATE) ? (int)rank : second]];
+          if (!b.a_mn) {
+            tma_load_2d_pair(sa, ma, bar, k0, row_a);
+          } else if (b.a_wide) {
+            tma_load_3d_pair(sa, ma, bar, 0, k0, row_a >> 6);
+          } else {
+            tma_load_2d_pair(sa, ma, bar, row_a, k0);
+            tma_load_2d_pair(sa + BK * 128, ma, bar, row_a + 64, k0);
+          }
+          if (!b.b_mn) {
+            tma_load_2d_pair(sb, mb, bar, k0, col_b);
+          } else if (b.b_wide) {
+            tma_load_3d_pair(sb, mb, bar, 0, k0, col_b >> 6);
+          } else {
+            tma_load_2d_pair(sb, mb, bar, col_b, k0);
+            tma_load_2d_pair(sb + BK * 128, mb, bar, col_b + 64, k0);
+          }
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ------------------------------- MMA issuer -------------------------------
+    if (rank == 0 && lane == 0) {
+      // fp32 accumulate, bf16 x bf16; bit 15 / bit 16: left / right operand is MN-major
+      constexpr uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) |
+                                  ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(TM >> 4) << 24);
+      // descriptor halves: high = SBO 1024 B | version 1 | 128-byte swizzle; low = address/16 | LBO/16 << 16
+      constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+      constexpr uint32_t LBO_K = (16u >> 4) << 16, LBO_MN = ((uint32_t)(BK * 128) >> 4) << 16;
+      constexpr uint32_t STEP_K = (UMMA_K * 2) >> 4, STEP_MN = (UMMA_K * 128) >> 4;
+      const uint32_t full0 = smem_u32(&bar_full[0]);
+      const uint32_t empty0 = smem_u32(&bar_empty[0]);
+      const uint32_t empty0_peer = map_to_rank(empty0, 1);
+      const uint32_t tfull0 = smem_u32(&bar_tfull[0]);
+      const uint32_t tfull0_peer = map_to_rank(tfull0, 1);
+      uint32_t stage = 0, phase = 0;
+      int local_tile = 0;
+      bool alive = true;
+      for (int tile = worker; alive && tile < p.total_tiles; tile += workers, ++local_tile) {
+        const Tile t = decode(p, tile);
+        const Prob& b = p.prob[t.q];
+        const uint32_t acc = (uint32_t)local_tile & 1u;
+        const uint32_t acc_phase = (uint32_t)(local_tile >> 1) & 1u;
+        const uint32_t d_tmem = tmem_base + acc * (uint32_t)BN;
+        const bool a_mn = b.a_mn, b_mn = b.b_mn;
+        const uint32_t idesc = idesc0 | ((a_mn ? 1u : 0u) << 15) | ((b_mn ? 1u : 0u) << 16);
+        const uint32_t lbo_a = a_mn ? LBO_MN : LBO_K, astep = a_mn ? STEP_MN : STEP_K;
+        const uint32_t lbo_b = b_mn ? LBO_MN : LBO_K, bstep = b_mn ? STEP_MN : STEP_K;
+        const int slabs = b.slabs;
+        if (!mbar_wait(smem_u32(&bar_tempty[acc]), acc_phase ^ 1u, &abort_flag, limit)) break;
+        tc_fence_after();
+        for (int kb = 0; kb < slabs; ++kb) {
+          if (!mbar_wait(full0 + stage * 8u, phase, &abort_flag, limit)) { alive = false; break; }
+          tc_fence_after();
+          const uint32_t sa = smem_base + stage * STAGE_BYTES;
+          const uint32_t alo = (sa >> 4) | lbo_a, blo = ((sa + A_BYTES) >> 4) | lbo_b;
+#pragma unroll
+          for (int k = 0; k < BK / UMMA_K; ++k) {
+            const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(alo + (uint32_t)k * astep);
+            const uint64_t bdesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(blo + (uint32_t)k * bstep);
+            tc_mma_bf16<CG>(d_tmem, adesc, bdesc, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+          }
+          tc_commit<CG>(empty0 + stage * 8u);
+          tc_commit<CG>(empty0_peer + stage * 8u);
+          if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+        }
+        if (alive) {
+          tc_commit<CG>(tfull0 + acc * 8u);
+          tc_commit<CG>(tfull0_peer + acc * 8u);
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    // -------------------------------- epilogue --------------------------------
+    const int quarter = warp & 3;                    // tensor-memory lanes [32 * quarter, + 32)
+    const int side = (warp - 2) >> 2;                // half of the columns
+    int local_tile = 0;
+    bool alive = true;
+    for (int tile = worker; tile < p.total_tiles; tile += workers, ++local_tile) {
+      const Tile t = decode(p, tile);
+      const Prob& b = p.prob[t.q];
+      const int acc = local_tile & 1;
+      const uint32_t acc_phase = (uint32_t)(local_tile >> 1) & 1u;
+      const int row = t.m * TM + (int)rank * BM + quarter * 32 + lane;
+      const bool row_ok = row < b.M;
+      const int64_t row_off = (int64_t)(row_ok ? row : 0) * b.N;
+      const bool wide = (b.N & 15) == 0 && ((((uintptr_t)b.out | (uintptr_t)b.out2 | (uintptr_t)b.out3 |
+                                              (uintptr_t)b.in1 | (uintptr_t)b.in2) & 31) == 0);
+      const uint32_t t_row = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(acc * BN);
+      constexpr int CHUNKS = (EPI == EPI_GATE) ? 2 : 4;          // of 32 columns, per warp
+      const int c_first = (EPI == EPI_GATE) ? side * 64 : side * (BN / 2);
+      const int n_first = (EPI == EPI_GATE) ? t.n * 128 + c_first : t.n * BN + c_first;
+      uint32_t gv[16], uv[16];
+      if (EPI == EPI_GATE_BACK) {                    // the first chunk's G and U are under way before the accumulator is done
+        const int left = row_ok ? b.N - n_first : 0;
+        load_row32(reinterpret_cast<const __nv_bfloat16*>(b.in1) + row_off + n_first, gv, left, wide);
+        load_row32(reinterpret_cast<const __nv_bfloat16*>(b.in2) + row_off + n_first, uv, left, wide);
+      }
+      if (!mbar_wait(smem_u32(&bar_tfull[acc]), acc_phase, &abort_flag, limit)) alive = false;
+      alive = __all_sync(0xffffffffu, alive);
+      if (!alive) break;
+      tc_fence_after();
+#pragma unroll 1
+      for (int c = 0; c < CHUNKS; ++c) {
+        const int n0 = n_first + c * 32;
+        const int left = row_ok ? b.N - n0 : 0;      // columns of this chunk that exist (may be <= 0)
+        uint32_t v[32];
+        float f[32];
+        __syncwarp();                                // rows past the end leave the stores early
+        if (EPI == EPI_STORE) {
+          tc_ld32(t_row + (uint32_t)(c_first + c * 32), v);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]);
+          if (left > 0) store_row32(reinterpret_cast<__nv_bfloat16*>(b.out) + row_off + n0, f, left, wide);
+        } else if (EPI == EPI_GATE) {
+          uint32_t w[32];
+          tc_ld32(t_row + (uint32_t)(c_first + c * 32), v);
+          tc_ld32(t_row + (uint32_t)(128 + c_first + c * 32), w);
+          if (left > 0 && b.out2) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]);
+            store_row32(reinterpret_cast<__nv_bfloat16*>(b.out2) + row_off + n0, f, left, wide);
+          }
+          if (left > 0 && b.out3) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(w[e]);
+            store_row32(reinterpret_cast<__nv_bfloat16*>(b.out3) + row_off + n0, f, left, wide);
+          }
+#pragma unroll
+          for (int e = 0; e < 32; ++e) f[e] = act_value<ACT>(__uint_as_float(v[e])) * __uint_as_float(w[e]);
+          if (left > 0) store_row32(reinterpret_cast<__nv_bfloat16*>(b.out) + row_off + n0, f, left, wide);
+        } else {
+          tc_ld32(t_row + (uint32_t)(c_first + c * 32), v);
+          float f2[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            const float g = (e & 1) ? bf16_hi(gv[e >> 1]) : bf16_lo(gv[e >> 1]);
+            const float u = (e & 1) ? bf16_hi(uv[e >> 1]) : bf16_lo(uv[e >> 1]);
+            float value, slope;
+            act_both<ACT>(g, value, slope);
+            const float dh = __uint_as_float(v[e]);
+            f[e] = dh * u * slope;
+            f2[e] = dh * value;
+          }
+          if (c + 1 < CHUNKS) {
+            load_row32(reinterpret_cast<const __nv_bfloat16*>(b.in1) + row_off + n0 + 32, gv, left - 32, wide);
+            load_row32(reinterpret_cast<const __nv_bfloat16*>(b.in2) + row_off + n0 + 32, uv, left - 32, wide);
+          }
+          if (left > 0) {
+            store_row32(reinterpret_cast<__nv_bfloat16*>(b.out) + row_off + n0, f, left, wide);
+            store_row32(reinterpret_cast<__nv_bfloat16*>(b.out2) + row_off + n0, f2, left, wide);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_rank(smem_u32(&bar_tempty[acc]), 0));
+    }
+  }
+
+  // ------------------------------- teardown ----------------------------------
+  if (abort_flag) {
+    // give copies and MMAs still in flight time to land before memory is released
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
+    if (threadIdx.x == 0) atomicOr(p.status, ST_TIMEOUT);
+  }
+  tc_fence_before();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc<CG>(tmem_base, TMEM_COLS);
+  }
+}
+
+// ------------------------------ host side ----------------------------------
+// A row-major bf16 matrix as an operand: rows x cols with row pitch ld.
+struct Mat { const void* p; int64_t rows, cols, ld; };
+
+bool encode(CUtensorMap* out, const Mat& a, int box_cols, int box_rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[2] = {(cuuint64_t)a.cols, (cuuint64_t)a.rows};
+  cuuint64_t strides[1] = {(cuuint64_t)a.ld * 2};
+  cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
+  cuuint32_t estr[2] = {1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(a.p), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The same matrix as [cols / 64][rows][64]: both atoms of an MN-major slab in one copy.
+bool encode_wide(CUtensorMap* out, const Mat& a) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn || (a.cols & 63) != 0) return false;
+  cuuint64_t dims[3] = {64, (cuuint64_t)a.rows, (cuuint64_t)(a.cols / 64)};
+  cuuint64_t strides[2] = {(cuuint64_t)a.ld * 2, 128};
+  cuuint32_t box[3] = {64, (cuuint32_t)BK, 2};
+  cuuint32_t estr[3] = {1, 1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(a.p), dims, strides, box, estr,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct Builder {
+  Maps maps;
+  Params p;
+  int n_maps = 0;
+  bool ok = true;
+  Builder() { memset(&p, 0, sizeof p); }
+  int kmajor(const Mat& a) {
+    ok = ok && n_maps < MAX_MAPS && encode(&maps.m[n_maps], a, BK, 128);
+    return n_maps++;
+  }
+  int mnmajor(const Mat& a, int* wide) {
+    if (n_maps >= MAX_MAPS) { ok = false; return 0; }
+    *wide = encode_wide(&maps.m[n_maps], a);
+    if (!*wide) ok = ok && encode(&maps.m[n_maps], a, 64, BK);
+    return n_maps++;
+  }
+  // A product of M x N results; its tiles follow those of the products before it.
+  Prob& add(int64_t M, int64_t N, int tile_n, int64_t k0, int64_t k1) {
+    Prob& b = p.prob[p.n_probs++];
+    b.tile_begin = p.total_tiles;
+    b.m_tiles = (int)((M + TM - 1) / TM);
+    b.n_tiles = (int)((N + tile_n - 1) / tile_n);
+    b.M = (int)M; b.N = (int)N;
+    b.slabs0 = (int)((k0 + BK - 1) / BK);
+    b.slabs = b.slabs0 + (int)((k1 + BK - 1) / BK);
+    p.total_tiles += b.m_tiles * b.n_tiles;
+    return b;
+  }
+};
+
+template <int EPI, int ACT>
+cudaError_t launch_kernel(cudaStream_t st, const Builder& b, int n_sms) {
+  auto kernel = ffn_kernel<EPI, ACT>;
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  const int units = n_sms / CG;
+  const int workers = b.p.total_tiles < units ? b.p.total_tiles : units;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = dim3((unsigned)(workers * CG));
+  cfg.blockDim = dim3(FFN_THREADS);
+  cfg.dynamicSmemBytes = SMEM_BYTES;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = CG; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, b.maps, b.p);
+}
+
+cudaError_t launch_built(cudaStream_t st, Builder& b, const FfnArgs& a, int epi, const char** what) {
+  *what = "cuTensorMapEncodeTiled";
+  if (!b.ok) return cudaErrorInvalidValue;
+  *what = "launch of the feed-forward kernel";
+  b.p.epi = epi;
+  b.p.act = a.act;
+  b.p.status = a.status;
+  b.p.wait_limit_ns = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
+  const bool gelu = a.act == MULOCO_ACT_GELU;
+  if (epi == EPI_GATE)
+    return gelu ? launch_kernel<EPI_GATE, MULOCO_ACT_GELU>(st, b, a.n_sms) : launch_kernel<EPI_GATE, MULOCO_ACT_SILU>(st, b, a.n_sms);
+  if (epi == EPI_GATE_BACK)
+    return gelu ? launch_kernel<EPI_GATE_BACK, MULOCO_ACT_GELU>(st, b, a.n_sms)
+                : launch_kernel<EPI_GATE_BACK, MULOCO_ACT_SILU>(st, b, a.n_sms);
+  return launch_kernel<EPI_STORE, MULOCO_ACT_SILU>(st, b, a.n_sms);
+}
+
+}  // namespace
+
+cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
+  {
+    Builder b;
+    Prob& q = b.add(a.T, a.F, 128, a.d, 0);
+    q.map_a[0] = b.kmajor(Mat{a.x, a.T, a.d, a.ldx});
+    q.b_mn = 1;
+    q.map_b[0] = b.mnmajor(Mat{a.w1, a.d, a.F, a.ldw1}, &q.b_wide);
+    int wide3 = 0;
+    q.map_b[1] = b.mnmajor(Mat{a.w3, a.d, a.F, a.ldw3}, &wide3);
+    b.ok = b.ok && wide3 == q.b_wide;
+    q.out = a.h; q.out2 = a.g; q.out3 = a.u;
+    cudaError_t e = launch_built(st, b, a, EPI_GATE, what);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
+  Builder b;
+  Prob& q = b.add(a.T, a.d, BN, a.F, 0);
+  q.map_a[0] = b.kmajor(Mat{a.h, a.T, a.F, a.F});
+  q.b_mn = 1;
+  q.map_b[0] = b.mnmajor(Mat{a.w2, a.F, a.d, a.ldw2}, &q.b_wide);
+  q.out = a.y;
+  cudaError_t e = launch_built(st, b, a, EPI_STORE, what);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
+  if (a.dx || a.dw1 || a.dw3) {
+    Builder b;
+    Prob& q = b.add(a.T, a.F, BN, a.d, 0);
+    q.map_a[0] = b.kmajor(Mat{a.dy, a.T, a.d, a.lddy});
+    q.map_b[0] = b.kmajor(Mat{a.w2, a.F, a.d, a.ldw2});
+    q.in1 = a.g; q.in2 = a.u;
+    q.out = a.dg; q.out2 = a.du;
+    cudaError_t e = launch_built(st, b, a, EPI_GATE_BACK, what);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
+  Builder b;
+  const Mat dg{a.dg, a.T, a.F, a.F}, du{a.du, a.T, a.F, a.F};
+  if (a.dx) {
+    Prob& q = b.add(a.T, a.d, BN, a.F, a.F);
+    q.map_a[0] = b.kmajor(dg);
+    q.map_a[1] = b.kmajor(du);
+    q.map_b[0] = b.kmajor(Mat{a.w1, a.d, a.F, a.ldw1});
+    q.map_b[1] = b.kmajor(Mat{a.w3, a.d, a.F, a.ldw3});
+    q.out = a.dx;
+  }
+  const Mat x{a.x, a.T, a.d, a.ldx};
+  for (int w = 0; w < 2; ++w) {
+    void* out = w ? a.dw3 : a.dw1;
+    if (!out) continue;
+    Prob& q = b.add(a.d, a.F, BN, a.T, 0);
+    q.a_mn = q.b_mn = 1;
+    q.map_a[0] = b.mnmajor(x, &q.a_wide);
+    q.map_b[0] = b.mnmajor(w ? du : dg, &q.b_wide);
+    q.out = out;
+  }
+  if (a.dw2) {
+    Prob& q = b.add(a.F, a.d, BN, a.T, 0);
+    q.a_mn = q.b_mn = 1;
+    q.map_a[0] = b.mnmajor(Mat{a.h, a.T, a.F, a.F}, &q.a_wide);
+    q.map_b[0] = b.mnmajor(Mat{a.dy, a.T, a.d, a.lddy}, &q.b_wide);
+    q.out = a.dw2;
+  }
+  if (!b.p.n_probs) return cudaSuccess;
+  cudaError_t e = launch_built(st, b, a, EPI_STORE, what);
+  if (e == cudaSuccess) ++*launches;
+  return e;
+}
+
+}  // namespace muloco

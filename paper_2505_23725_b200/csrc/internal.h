@@ -9,7 +9,7 @@
 namespace muloco {
 
 // Device status word bits (OR-ed by kernels, read by muloco_sync_status).
-enum : int { ST_NONFINITE = 1, ST_TIMEOUT = 2, ST_BOUNDS = 4 };
+enum : int { ST_NONFINITE = 1, ST_TIMEOUT = 2, ST_BOUNDS = 4, ST_POSITION = 8 };
 
 // Debug build (-DMULOCO_DEBUG): kernels check the indices they derive (work-list cursors, matrix
 // slots, tile coordinates, segment and unit indices) before using them; a failed check raises
@@ -164,5 +164,96 @@ void launch_quantize(cudaStream_t st, const float* psi, int64_t rows, int64_t co
                      int bits, int8_t* codes, float* scales, float* dequant, int* status);
 void launch_broadcast_init(cudaStream_t st, const float* src, float* const* dst_table, int K,
                            int64_t n);
+
+// ---------------------------------------------------------------------------
+// Operators of the training step around the optimizer (adamw.cu, qk_norm.cu, ffn.cu), entered through
+// ops_capi.cu.
+// ---------------------------------------------------------------------------
+
+// What an entry point needs of its context.
+struct CtxView {
+  cudaStream_t st;
+  int* status;
+  int n_sms;
+  unsigned long long wait_limit_ns;   // 0: the default
+};
+CtxView ctx_view(muloco_ctx* c);
+muloco_status ctx_fail(muloco_ctx* c, muloco_status s, const char* fmt, ...);
+void ctx_count_launches(muloco_ctx* c, int n);
+// Scratch of the context that the reductions of qk_norm.cu use: QK_SCRATCH_FLOATS floats, then tickets
+// (zero between launches).  Allocated on first use; nullptr when that fails.
+float* ctx_qk_scratch(muloco_ctx* c, int** tickets);
+
+// AdamW over many tensors: one entry per tensor (include/muloco.h has the layout of the states).
+struct AdamwSeg {
+  float* theta;
+  void* copy;            // bf16 copy of the parameters, or NULL
+  void* s1;
+  void* s2;
+  float* scale1;
+  float* scale2;
+  int64_t n;
+  int64_t unit_begin;    // first work unit of this tensor
+  int64_t dither_base;   // its first element in the padded layout
+  float wd_mult, lr_mult;
+};
+struct AdamwStep {
+  float lr, lr_wd;       // alpha, alpha * lambda
+  float beta1, beta2, eps;
+  float inv_bc1, inv_sqrt_bc2;
+  uint32_t dither;
+};
+int64_t adamw_units(int64_t n);                       // work units of a tensor of n elements
+uint32_t adamw_dither(uint32_t seed, int64_t step);   // what step `step` adds to the element index before hashing
+// unit_seg[unit] = the entry that the unit belongs to; grads[entry] = its gradient
+void launch_adamw_multi(cudaStream_t st, const AdamwSeg* segs, const int* unit_seg, const void* const* grads,
+                        int n_segs, int64_t n_units, int state_bits, int g_is_bf16, const AdamwStep& a, int* status);
+void launch_adamw_moments(cudaStream_t st, const AdamwSeg* segs, const int* unit_seg, int n_segs, int64_t n_units,
+                          float* m, float* v, int* status);
+
+// Query / key norm with rotation.  One of the two tensors of a call:
+struct QkTensor {
+  const void* x;         // forward input (both passes)
+  const void* dy;        // backward: gradient of the result
+  void* out;             // forward: result; backward: gradient of x
+  const float* gain;     // NULL: ones
+  float* dgain;          // backward, or NULL
+  int64_t x_ts, x_hs, y_ts, y_hs, o_ts, o_hs;   // token and head strides (elements) of x, dy, out
+  int32_t heads, pad;
+};
+struct QkArgs {
+  QkTensor t[2];
+  int64_t tokens, table_len;
+  const float* cos;
+  const float* sin;
+  const int64_t* positions;
+  int32_t dim, rot, interleaved;
+  float eps;
+  int* status;
+  float* partials;       // backward: gain gradients of the thread blocks
+  int* tickets;          // backward: one per tensor, zero between launches
+};
+constexpr int QK_MAX_DIM = 512;
+constexpr int QK_MAX_CTAS = 148 * 8;
+constexpr size_t QK_SCRATCH_FLOATS = (size_t)QK_MAX_CTAS * QK_MAX_DIM;
+int launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_bf16, int n_sms);   // kernels launched
+
+// Gated feed-forward block.
+struct FfnArgs {
+  int64_t T, d, F;
+  const void* x; int64_t ldx;
+  const void* w1; int64_t ldw1;
+  const void* w3; int64_t ldw3;
+  const void* w2; int64_t ldw2;
+  int act;
+  void* g; void* u; void* h; void* y;          // forward results; backward inputs (g, u, h)
+  const void* dy; int64_t lddy;
+  void* dg; void* du; void* dx; void* dw1; void* dw3; void* dw2;
+  int* status;
+  unsigned long long wait_limit_ns;
+  int n_sms;
+};
+cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what);
+cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what);
 
 }  // namespace muloco
