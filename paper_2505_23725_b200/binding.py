@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import math
 import os
+import struct
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -97,6 +98,11 @@ class Ffn(C.Structure):
                 ("activation", C.c_int32), ("pad", C.c_int32)]
 
 
+# QkNorm and Ffn as bytes
+_QK_PACK = struct.Struct("qqiiiiiifiQQQQQQQqqqq").pack
+_FFN_PACK = struct.Struct("qqqqqqqQQQQii").pack
+
+
 class MulocoError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"muloco status {STATUS_NAMES[status] if 0 <= status < 8 else status}: {msg}")
@@ -148,10 +154,12 @@ def load_library():
     lib.muloco_adamw_moments.argtypes = [vp, vp, vp]
     lib.muloco_adamw_destroy.argtypes = [vp]
     lib.muloco_adamw_destroy.restype = None
-    lib.muloco_qk_norm_rope.argtypes = [vp, C.POINTER(QkNorm), vp, i64, i64, vp, i64, i64]
-    lib.muloco_qk_norm_rope_backward.argtypes = [vp, C.POINTER(QkNorm), vp, i64, i64, vp, i64, i64, vp, vp, vp, vp]
-    lib.muloco_gated_ffn.argtypes = [vp, C.POINTER(Ffn), vp, vp, vp, vp]
-    lib.muloco_gated_ffn_backward.argtypes = [vp, C.POINTER(Ffn), vp, i64] + [vp] * 9
+    # the argument structs of the operators are packed bytes (_QK_PACK, _FFN_PACK): a fifth of the time of a ctypes struct
+    packed = C.c_char_p
+    lib.muloco_qk_norm_rope.argtypes = [vp, packed, vp, i64, i64, vp, i64, i64]
+    lib.muloco_qk_norm_rope_backward.argtypes = [vp, packed, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp]
+    lib.muloco_gated_ffn.argtypes = [vp, packed, vp, vp, vp, vp]
+    lib.muloco_gated_ffn_backward.argtypes = [vp, packed, vp, i64] + [vp] * 9
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("muloco_destroy", "muloco_last_error", "muloco_adamw_destroy"):
@@ -273,34 +281,40 @@ class _Operators:
     stream first waits for it and it then waits for the context's, and the tensors are
     recorded on the context's stream, so inputs, results and their memory may be used as usual."""
 
-    def _enter(self, tensors):
-        cur = self.torch.cuda.current_stream(self.device)
-        if cur.cuda_stream == self.stream.cuda_stream:
+    @property
+    def _raw_stream(self):
+        # the handle of a device's current stream, without building a Stream object
+        return self.torch._C._cuda_getCurrentRawStream
+
+    def _other_stream(self):
+        """The caller's current stream when it is not the context's, else None."""
+        if self._raw_stream(self.device.index or 0) == self.stream.cuda_stream:
             return None
+        return self.torch.cuda.current_stream(self.device)
+
+    def _enter(self, cur, tensors):
         self.stream.wait_stream(cur)
         for t in tensors:
             if t is not None:
                 t.record_stream(self.stream)
-        return cur
 
-    def _leave(self, cur, tensors):
-        if cur is not None:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self.stream)
-            cur.wait_stream(self.stream)
-
-    def _need(self, name, t, dtype, shape):
-        """t is a tensor of this context's device with the given type and shape (None: any size)."""
-        if t.device != self.device:
+    def _need(self, name, t, dtype, shape, dense=False):
+        """Raises unless t is a tensor of this context's device with the given type and shape (None: any
+        size) whose last dimension is consecutive (dense: which is contiguous)."""
+        if t.get_device() != (self.device.index or 0):
             raise ValueError(f"{name} must be on {self.device} (got {t.device})")
-        if t.dtype != dtype:
+        if t.dtype is not dtype:
             raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
         if t.dim() != len(shape) or any(w is not None and w != h for w, h in zip(shape, t.shape)):
             raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
+        if dense and not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        if t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name}: the entries of its last dimension must be consecutive")
 
     # -- norm of queries and keys with the rotation -----------------------------------------------
-    def _qk(self, q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved):
+    def _check_qk(self, q, k, cos, sin, positions, gain_q, gain_k):
+        """The checks of _qk one by one, for the message."""
         torch = self.torch
         some = q if q is not None else k
         if some is None:
@@ -313,141 +327,191 @@ class _Operators:
         for name, t in (("q", q), ("k", k)):
             if t is not None:
                 self._need(name, t, some.dtype, (T, None, D))
-                if D > 1 and t.stride(2) != 1:
-                    raise ValueError(f"{name}: the entries of a head must be consecutive")
-        self._need("cos", cos, torch.float32, (None, None))
-        self._need("sin", sin, torch.float32, tuple(cos.shape))
-        if not (cos.is_contiguous() and sin.is_contiguous()):
-            raise ValueError("cos and sin must be contiguous")
+        self._need("cos", cos, torch.float32, (None, None), dense=True)
+        self._need("sin", sin, torch.float32, tuple(cos.shape), dense=True)
         if positions is not None:
-            self._need("positions", positions, torch.int64, (T,))
-            if not positions.is_contiguous():
-                raise ValueError("positions must be contiguous")
+            self._need("positions", positions, torch.int64, (T,), dense=True)
         for name, t in (("gain_q", gain_q), ("gain_k", gain_k)):
             if t is not None:
-                self._need(name, t, torch.float32, (D,))
-                if not t.is_contiguous():
-                    raise ValueError(f"{name} must be contiguous")
-        ptr = lambda t: None if t is None else t.data_ptr()          # noqa: E731
-        a = QkNorm(T, cos.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], D,
-                   2 * cos.shape[1], BF16 if some.dtype == torch.bfloat16 else F32, int(interleaved), eps, 0,
-                   ptr(gain_q), ptr(gain_k), cos.data_ptr(), sin.data_ptr(), ptr(positions), ptr(q), ptr(k),
-                   *((0, 0) if q is None else q.stride()[:2]), *((0, 0) if k is None else k.stride()[:2]))
-        return a
+                self._need(name, t, torch.float32, (D,), dense=True)
+
+    def _qk(self, q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved):
+        """The packed argument struct of a call.  The checks run every time, so they are written to be
+        quick; _check_qk repeats them with a message when one fails."""
+        torch, dev = self.torch, self.device.index or 0
+        f32 = torch.float32
+        some = q if q is not None else k
+        if some is None or some.dim() != 3 or cos.dim() != 2:
+            self._check_qk(q, k, cos, sin, positions, gain_q, gain_k)
+        dt = some.dtype
+        T, _, D = some.shape
+        ok = (dt is torch.bfloat16 or dt is f32) and cos.shape == sin.shape and cos.dtype is f32 and sin.dtype is f32 \
+            and cos.is_contiguous() and sin.is_contiguous() and cos.get_device() == dev and sin.get_device() == dev
+        hq = hk = pq = pk = qt = qh = kt = kh = pp = pgq = pgk = 0
+        if q is not None:
+            _, hq, d = q.shape
+            qt, qh, one = q.stride()
+            pq = q.data_ptr()
+            ok = ok and d == D and (one == 1 or D < 2) and q.get_device() == dev
+        if k is not None:
+            t, hk, d = k.shape if k.dim() == 3 else (-1, 0, 0)
+            kt, kh, one = k.stride() if k.dim() == 3 else (0, 0, 0)
+            pk = k.data_ptr()
+            ok = ok and t == T and d == D and (one == 1 or D < 2) and k.dtype is dt and k.get_device() == dev
+        if positions is not None:
+            pp = positions.data_ptr()
+            ok = ok and positions.dtype is torch.int64 and positions.shape == (T,) and positions.is_contiguous() \
+                and positions.get_device() == dev
+        if gain_q is not None:
+            pgq = gain_q.data_ptr()
+            ok = ok and gain_q.dtype is f32 and gain_q.shape == (D,) and gain_q.is_contiguous() and gain_q.get_device() == dev
+        if gain_k is not None:
+            pgk = gain_k.data_ptr()
+            ok = ok and gain_k.dtype is f32 and gain_k.shape == (D,) and gain_k.is_contiguous() and gain_k.get_device() == dev
+        if not ok:
+            self._check_qk(q, k, cos, sin, positions, gain_q, gain_k)
+        L, half = cos.shape
+        return _QK_PACK(T, L, hq, hk, D, 2 * half, BF16 if dt is torch.bfloat16 else F32, 1 if interleaved else 0, eps,
+                        0, pgq, pgk, cos.data_ptr(), sin.data_ptr(), pp, pq, pk, qt, qh, kt, kh)
 
     def qk_norm_rope(self, q, k, cos, sin, positions=None, gain_q=None, gain_k=None, eps=1e-6, interleaved=False,
                      out=None):
         """muloco_qk_norm_rope: norm and rotation of the heads of q [tokens, heads, head_dim] and k (either may be
         None).  cos and sin: float32 tables [length, rotary_dim / 2]; positions: int64 [tokens] or None
-        for 0, 1, ...  Returns (q_out, k_out), dense unless `out` = (q_out, k_out) gives them."""
-        torch = self.torch
+        for 0, 1, ...  Returns (q_out, k_out), new tensors in the inputs' order of dimensions unless
+        `out` = (q_out, k_out) gives them."""
+        empty_like = self.torch.empty_like
         a = self._qk(q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
         if out is None:
-            out = tuple(None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k))
+            qo = None if q is None else empty_like(q)
+            ko = None if k is None else empty_like(k)
         else:
-            for name, o, t in (("q_out", out[0], q), ("k_out", out[1], k)):
+            qo, ko = out
+            for name, o, t in (("q_out", qo, q), ("k_out", ko, k)):
                 if (o is None) != (t is None):
                     raise ValueError(f"{name} is given without its input, or missing")
                 if o is not None:
                     self._need(name, o, t.dtype, tuple(t.shape))
-                    if t.shape[2] > 1 and o.stride(2) != 1:
-                        raise ValueError(f"{name}: the entries of a head must be consecutive")
-        used = (q, k, cos, sin, positions, gain_q, gain_k) + tuple(out)
-        cur = self._enter(used)
-        args = []
-        for o in out:
-            args += [None, 0, 0] if o is None else [o.data_ptr(), o.stride(0), o.stride(1)]
-        self._check(self.lib.muloco_qk_norm_rope(self.ctx, C.byref(a), *args))
-        self._leave(cur, ())
-        return tuple(out)
+        p1 = t1 = h1 = p2 = t2 = h2 = 0
+        if qo is not None:
+            p1 = qo.data_ptr()
+            t1, h1, _ = qo.stride()
+        if ko is not None:
+            p2 = ko.data_ptr()
+            t2, h2, _ = ko.stride()
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (q, k, cos, sin, positions, gain_q, gain_k, qo, ko))
+        st = self.lib.muloco_qk_norm_rope(self.ctx, a, p1, t1, h1, p2, t2, h2)
+        if st:
+            self._check(st)
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        return qo, ko
 
     def qk_norm_rope_backward(self, dq_out, dk_out, q, k, cos, sin, positions=None, gain_q=None, gain_k=None,
                               eps=1e-6, interleaved=False):
         """muloco_qk_norm_rope_backward: from the gradients of the results, (dq, dk, dgain_q, dgain_k)."""
         torch = self.torch
         a = self._qk(q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
-        grads, args, gains = [], [], []
+        dev = self.device.index or 0
         for name, y, t in (("dq_out", dq_out, q), ("dk_out", dk_out, k)):
             if (y is None) != (t is None):
                 raise ValueError(f"{name} is given without its input, or missing")
-            if t is None:
-                grads.append(None)
-                gains.append(None)
-                args += [None, 0, 0]
-                continue
-            self._need(name, y, t.dtype, tuple(t.shape))
-            if t.shape[2] > 1 and y.stride(2) != 1:
-                raise ValueError(f"{name}: the entries of a head must be consecutive")
-            grads.append(torch.empty(t.shape, dtype=t.dtype, device=t.device))
-            gains.append(torch.empty(t.shape[2], dtype=torch.float32, device=t.device))
-            args += [y.data_ptr(), y.stride(0), y.stride(1)]
-        cur = self._enter((q, k, cos, sin, positions, gain_q, gain_k, dq_out, dk_out, *grads, *gains))
-        ptr = lambda t: None if t is None else t.data_ptr()          # noqa: E731
-        self._check(self.lib.muloco_qk_norm_rope_backward(self.ctx, C.byref(a), *args, ptr(grads[0]), ptr(grads[1]),
-                                                          ptr(gains[0]), ptr(gains[1])))
-        self._leave(cur, ())
-        return grads[0], grads[1], gains[0], gains[1]
+            if y is not None and (y.dtype is not t.dtype or y.shape != t.shape or y.get_device() != dev or y.stride(2) != 1):
+                self._need(name, y, t.dtype, tuple(t.shape))
+        dq = dk = gq = gk = None
+        p1 = t1 = h1 = p2 = t2 = h2 = o1 = o2 = g1 = g2 = 0
+        if q is not None:
+            dq, gq = q.new_empty(q.shape), cos.new_empty(q.shape[2])
+            p1, o1, g1 = dq_out.data_ptr(), dq.data_ptr(), gq.data_ptr()
+            t1, h1, _ = dq_out.stride()
+        if k is not None:
+            dk, gk = k.new_empty(k.shape), cos.new_empty(k.shape[2])
+            p2, o2, g2 = dk_out.data_ptr(), dk.data_ptr(), gk.data_ptr()
+            t2, h2, _ = dk_out.stride()
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (q, k, cos, sin, positions, gain_q, gain_k, dq_out, dk_out, dq, dk, gq, gk))
+        st = self.lib.muloco_qk_norm_rope_backward(self.ctx, a, p1, t1, h1, p2, t2, h2, o1, o2, g1, g2)
+        if st:
+            self._check(st)
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        return dq, dk, gq, gk
 
     # -- gated feed-forward block -----------------------------------------------------------------
-    def _ffn(self, x, w1, w3, w2, activation):
+    def _check_ffn(self, x, w1, w3, w2):
+        """The checks of _ffn one by one, for the message."""
         bf16 = self.torch.bfloat16
-        if activation not in ACTIVATIONS:
-            raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)} (got {activation!r})")
         self._need("x", x, bf16, (None, None))
-        T, d = x.shape
-        self._need("w1", w1, bf16, (d, None))
-        F = w1.shape[1]
-        self._need("w3", w3, bf16, (d, F))
-        self._need("w2", w2, bf16, (F, d))
-        for name, t in (("x", x), ("w1", w1), ("w3", w3), ("w2", w2)):
-            if t.stride(1) != 1:
-                raise ValueError(f"{name}: the entries of a row must be consecutive")
-        return Ffn(T, d, F, self._ld(x), w1.stride(0), w3.stride(0), w2.stride(0),
-                   x.data_ptr(), w1.data_ptr(), w3.data_ptr(), w2.data_ptr(), ACTIVATIONS[activation], 0), T, d, F
+        self._need("w1", w1, bf16, (x.shape[1], None))
+        self._need("w3", w3, bf16, tuple(w1.shape))
+        self._need("w2", w2, bf16, (w1.shape[1], w1.shape[0]))
 
-    @staticmethod
-    def _ld(t):
-        """Row stride; that of a single row does not matter and is taken as its length."""
-        return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    def _ffn(self, x, w1, w3, w2, activation):
+        """The packed argument struct of a call (its checks as in _qk)."""
+        bf16, dev = self.torch.bfloat16, self.device.index or 0
+        act = ACTIVATIONS.get(activation, -1)
+        if act < 0:
+            raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)} (got {activation!r})")
+        if x.dim() != 2 or w1.dim() != 2 or w3.dim() != 2 or w2.dim() != 2:
+            self._check_ffn(x, w1, w3, w2)
+        T, d = x.shape
+        d1, F = w1.shape
+        ldx, one = x.stride()
+        ld1, one1 = w1.stride()
+        ld3, one3 = w3.stride()
+        ld2, one2 = w2.stride()
+        if not (d1 == d and w3.shape == w1.shape and w2.shape == (F, d) and x.dtype is bf16 and w1.dtype is bf16
+                and w3.dtype is bf16 and w2.dtype is bf16 and one == 1 and one1 == 1 and one3 == 1 and one2 == 1
+                and x.get_device() == dev and w1.get_device() == dev and w3.get_device() == dev
+                and w2.get_device() == dev):
+            self._check_ffn(x, w1, w3, w2)
+        # the row stride of a single row does not matter
+        return _FFN_PACK(T, d, F, ldx if T > 1 else d, ld1, ld3, ld2, x.data_ptr(), w1.data_ptr(), w3.data_ptr(),
+                         w2.data_ptr(), act, 0), T, d, F
 
     def gated_ffn(self, x, w1, w3, w2, activation="silu", save=True):
         """muloco_gated_ffn: y = (act(x w1) * (x w3)) w2, all bf16.  Returns (y, saved): saved = (g, u, h) is what
         the backward pass needs (None with save=False, and g and u are then not written)."""
-        torch = self.torch
         a, T, d, F = self._ffn(x, w1, w3, w2, activation)
-        y = torch.empty((T, d), dtype=torch.bfloat16, device=x.device)
-        h = torch.empty((T, F), dtype=torch.bfloat16, device=x.device)
+        y, h = x.new_empty((T, d)), x.new_empty((T, F))
         g = u = None
+        pg = pu = 0
         if save:
-            g, u = torch.empty_like(h), torch.empty_like(h)
-        cur = self._enter((x, w1, w3, w2, y, h, g, u))
-        self._check(self.lib.muloco_gated_ffn(self.ctx, C.byref(a), g.data_ptr() if save else None,
-                                              u.data_ptr() if save else None, h.data_ptr(), y.data_ptr()))
-        self._leave(cur, ())
+            g, u = x.new_empty((T, F)), x.new_empty((T, F))
+            pg, pu = g.data_ptr(), u.data_ptr()
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (x, w1, w3, w2, y, h, g, u))
+        st = self.lib.muloco_gated_ffn(self.ctx, a, pg, pu, h.data_ptr(), y.data_ptr())
+        if st:
+            self._check(st)
+        if cur is not None:
+            cur.wait_stream(self.stream)
         return y, ((g, u, h) if save else None)
 
     def gated_ffn_backward(self, dy, x, w1, w3, w2, saved, activation="silu"):
         """muloco_gated_ffn_backward: (dx, dw1, dw3, dw2), bf16, from dy and the forward pass's saved = (g, u, h)."""
-        torch = self.torch
-        bf16 = torch.bfloat16
+        bf16 = self.torch.bfloat16
         a, T, d, F = self._ffn(x, w1, w3, w2, activation)
         self._need("dy", dy, bf16, (T, d))
-        if dy.stride(1) != 1:
-            raise ValueError("dy: the entries of a row must be consecutive")
-        for name, t in zip(("g", "u", "h"), saved):
-            self._need(name, t, bf16, (T, F))
-            if not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
         g, u, h = saved
-        dg, du = (torch.empty((T, F), dtype=bf16, device=x.device) for _ in range(2))
-        dx = torch.empty((T, d), dtype=bf16, device=x.device)
-        dw1, dw3 = (torch.empty((d, F), dtype=bf16, device=x.device) for _ in range(2))
-        dw2 = torch.empty((F, d), dtype=bf16, device=x.device)
-        cur = self._enter((dy, x, w1, w3, w2, g, u, h, dg, du, dx, dw1, dw3, dw2))
-        self._check(self.lib.muloco_gated_ffn_backward(
-            self.ctx, C.byref(a), dy.data_ptr(), self._ld(dy), g.data_ptr(), u.data_ptr(), h.data_ptr(), dg.data_ptr(),
-            du.data_ptr(), dx.data_ptr(), dw1.data_ptr(), dw3.data_ptr(), dw2.data_ptr()))
-        self._leave(cur, ())
+        for name, t in (("g", g), ("u", u), ("h", h)):
+            self._need(name, t, bf16, (T, F), dense=True)
+        dg, du = x.new_empty((T, F)), x.new_empty((T, F))
+        dx, dw1, dw3, dw2 = x.new_empty((T, d)), x.new_empty((d, F)), x.new_empty((d, F)), x.new_empty((F, d))
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (dy, x, w1, w3, w2, g, u, h, dg, du, dx, dw1, dw3, dw2))
+        st = self.lib.muloco_gated_ffn_backward(
+            self.ctx, a, dy.data_ptr(), dy.stride(0) if T > 1 else d, g.data_ptr(), u.data_ptr(), h.data_ptr(),
+            dg.data_ptr(), du.data_ptr(), dx.data_ptr(), dw1.data_ptr(), dw3.data_ptr(), dw2.data_ptr())
+        if st:
+            self._check(st)
+        if cur is not None:
+            cur.wait_stream(self.stream)
         return dx, dw1, dw3, dw2
 
 
@@ -575,10 +639,13 @@ class AdamW:
                 raise ValueError("grads must have one entry per parameter")
             self._check_grads(grads)
             table = _ptr_table([g.data_ptr() for g in grads])
-        used = (*(grads if grads is not None else self.grads or ()), *self.params, *(self.copies or ()))
-        cur = self.owner._enter(used)
+        cur = self.owner._other_stream()
+        if cur is not None:
+            self.owner._enter(cur, (*(grads if grads is not None else self.grads or ()), *self.params,
+                                    *(self.copies or ())))
         self.owner._check(self.lib.muloco_adamw_step(self.opt, table, self.steps + 1, lr_scale))
-        self.owner._leave(cur, ())
+        if cur is not None:
+            cur.wait_stream(self.owner.stream)
         self.steps += 1
 
     def moments(self):
@@ -588,9 +655,12 @@ class AdamW:
             return self.state1, self.state2
         torch = self.owner.torch
         m, v = (torch.empty(self.padded, dtype=torch.float32, device=self.owner.device) for _ in range(2))
-        cur = self.owner._enter((m, v))
+        cur = self.owner._other_stream()
+        if cur is not None:
+            self.owner._enter(cur, (m, v))
         self.owner._check(self.lib.muloco_adamw_moments(self.opt, m.data_ptr(), v.data_ptr()))
-        self.owner._leave(cur, ())
+        if cur is not None:
+            cur.wait_stream(self.owner.stream)
         return m, v
 
     def close(self):
