@@ -35,8 +35,13 @@ constexpr int BM = 128;                      // rows per CTA
 constexpr int TM = 128 * CG, BN = 128 * CG;  // tile
 constexpr int EPI_WARPS = 8;
 constexpr int FFN_THREADS = 64 + 32 * EPI_WARPS;
-constexpr int STAGES = 6;
-constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = 128 * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
+// Slabs per pipeline stage.  One per stage (7 stages) was measured slower (8192 x 2048 x 5632 backward 950 us against 886,
+// 16384 x 1024 x 2816 forward 244 against 234): the threads that issue copies and MMAs pay a wait
+// per stage; three per stage leave two stages, too few to cover a copy's latency (940, 256).
+constexpr int SPS = 2;
+constexpr int STAGES = 3;
+constexpr uint32_t A_BYTES = BM * BK * 2, B_BYTES = 128 * BK * 2, SLAB_BYTES = A_BYTES + B_BYTES;
+constexpr uint32_t STAGE_BYTES = SPS * SLAB_BYTES;
 constexpr uint32_t SMEM_BYTES = STAGES * STAGE_BYTES + 1024u;
 constexpr uint32_t TMEM_COLS = 2 * BN;
 constexpr int MAX_PROBS = 4, MAX_MAPS = 12;
@@ -207,31 +212,41 @@ ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) 
         const int row_a = t.m * TM + (int)rank * BM;
         // gated product: this CTA's half of the right operand is W1 (rank 0) or W3 (rank 1), same columns
         const int col_b = (EPI == EPI_GATE) ? t.n * 128 : t.n * BN + (int)rank * 128;
-        for (int kb = 0; kb < b.slabs; ++kb) {
+        const int slabs = b.slabs, slabs0 = b.slabs0;
+        const bool a_mn = b.a_mn, b_mn = b.b_mn, a_wide = b.a_wide, b_wide = b.b_wide;
+        const CUtensorMap* ma = &maps.m[b.map_a[0]];
+        const CUtensorMap* mb = &maps.m[b.map_b[(EPI == EPI_GATE) ? (int)rank : 0]];
+        const CUtensorMap* ma1 = &maps.m[b.map_a[1]];
+        const CUtensorMap* mb1 = &maps.m[b.map_b[1]];
+        int k0 = 0;
+        for (int kb0 = 0; kb0 < slabs; kb0 += SPS) {
           if (!mbar_wait(empty0 + stage * 8u, phase ^ 1u, &abort_flag, limit)) { alive = false; break; }
-          const uint32_t sa = smem_base + stage * STAGE_BYTES;
-          const uint32_t sb = sa + A_BYTES;
           const uint32_t bar = full0_bar + stage * 8u;
-          if (rank == 0) mbar_expect_tx(full0 + stage * 8u, CG * STAGE_BYTES);
-          const int second = kb >= b.slabs0;
-          const int k0 = (second ? kb - b.slabs0 : kb) * BK;
-          const CUtensorMap* ma = &maps.m[b.map_a[second]];
-          const CUtensorMap* mb = &maps.m[b.map_b[(EPI == EPI_GATE) ? (int)rank : second]];
-          if (!b.a_mn) {
-            tma_load_2d_pair(sa, ma, bar, k0, row_a);
-          } else if (b.a_wide) {
-            tma_load_3d_pair(sa, ma, bar, 0, k0, row_a >> 6);
-          } else {
-            tma_load_2d_pair(sa, ma, bar, row_a, k0);
-            tma_load_2d_pair(sa + BK * 128, ma, bar, row_a + 64, k0);
-          }
-          if (!b.b_mn) {
-            tma_load_2d_pair(sb, mb, bar, k0, col_b);
-          } else if (b.b_wide) {
-            tma_load_3d_pair(sb, mb, bar, 0, k0, col_b >> 6);
-          } else {
-            tma_load_2d_pair(sb, mb, bar, col_b, k0);
-            tma_load_2d_pair(sb + BK * 128, mb, bar, col_b + 64, k0);
+          const int here = slabs - kb0 < SPS ? slabs - kb0 : SPS;
+          if (rank == 0) mbar_expect_tx(full0 + stage * 8u, CG * SLAB_BYTES * (uint32_t)here);
+#pragma unroll
+          for (int j = 0; j < SPS; ++j) {
+            if (j >= here) break;
+            const uint32_t sa = smem_base + stage * STAGE_BYTES + (uint32_t)j * SLAB_BYTES;
+            const uint32_t sb = sa + A_BYTES;
+            if (kb0 + j == slabs0) { ma = ma1; mb = mb1; k0 = 0; }      // the second operand pair
+            if (!a_mn) {
+              tma_load_2d_pair(sa, ma, bar, k0, row_a);
+            } else if (a_wide) {
+              tma_load_3d_pair(sa, ma, bar, 0, k0, row_a >> 6);
+            } else {
+              tma_load_2d_pair(sa, ma, bar, row_a, k0);
+              tma_load_2d_pair(sa + BK * 128, ma, bar, row_a + 64, k0);
+            }
+            if (!b_mn) {
+              tma_load_2d_pair(sb, mb, bar, k0, col_b);
+            } else if (b_wide) {
+              tma_load_3d_pair(sb, mb, bar, 0, k0, col_b >> 6);
+            } else {
+              tma_load_2d_pair(sb, mb, bar, col_b, k0);
+              tma_load_2d_pair(sb + BK * 128, mb, bar, col_b + 64, k0);
+            }
+            k0 += BK;
           }
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
@@ -256,6 +271,10 @@ ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) 
       uint32_t stage = 0, phase = 0;
       int local_tile = 0;
       bool alive = true;
+      auto release = [&](uint32_t bar, uint32_t bar_peer) {
+        tc_commit<CG>(bar);
+        tc_commit<CG>(bar_peer);
+      };
       for (int tile = worker; alive && tile < p.total_tiles; tile += workers, ++local_tile) {
         const Tile t = decode(p, tile);
         const Prob& b = p.prob[t.q];
@@ -269,25 +288,26 @@ ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) 
         const int slabs = b.slabs;
         if (!mbar_wait(smem_u32(&bar_tempty[acc]), acc_phase ^ 1u, &abort_flag, limit)) break;
         tc_fence_after();
-        for (int kb = 0; kb < slabs; ++kb) {
+        for (int kb0 = 0; kb0 < slabs; kb0 += SPS) {
           if (!mbar_wait(full0 + stage * 8u, phase, &abort_flag, limit)) { alive = false; break; }
           tc_fence_after();
-          const uint32_t sa = smem_base + stage * STAGE_BYTES;
-          const uint32_t alo = (sa >> 4) | lbo_a, blo = ((sa + A_BYTES) >> 4) | lbo_b;
+          const int here = slabs - kb0 < SPS ? slabs - kb0 : SPS;
 #pragma unroll
-          for (int k = 0; k < BK / UMMA_K; ++k) {
-            const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(alo + (uint32_t)k * astep);
-            const uint64_t bdesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(blo + (uint32_t)k * bstep);
-            tc_mma_bf16<CG>(d_tmem, adesc, bdesc, idesc, (kb > 0 || k > 0) ? 1u : 0u);
+          for (int j = 0; j < SPS; ++j) {
+            if (j >= here) break;
+            const uint32_t sa = smem_base + stage * STAGE_BYTES + (uint32_t)j * SLAB_BYTES;
+            const uint32_t alo = (sa >> 4) | lbo_a, blo = ((sa + A_BYTES) >> 4) | lbo_b;
+#pragma unroll
+            for (int k = 0; k < BK / UMMA_K; ++k) {
+              const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(alo + (uint32_t)k * astep);
+              const uint64_t bdesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(blo + (uint32_t)k * bstep);
+              tc_mma_bf16<CG>(d_tmem, adesc, bdesc, idesc, (kb0 > 0 || j > 0 || k > 0) ? 1u : 0u);
+            }
           }
-          tc_commit<CG>(empty0 + stage * 8u);
-          tc_commit<CG>(empty0_peer + stage * 8u);
+          release(empty0 + stage * 8u, empty0_peer + stage * 8u);
           if (++stage == STAGES) { stage = 0; phase ^= 1u; }
         }
-        if (alive) {
-          tc_commit<CG>(tfull0 + acc * 8u);
-          tc_commit<CG>(tfull0_peer + acc * 8u);
-        }
+        if (alive) release(tfull0 + acc * 8u, tfull0_peer + acc * 8u);
       }
     }
     __syncwarp();
