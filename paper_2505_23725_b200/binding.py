@@ -281,14 +281,18 @@ class _Operators:
     stream first waits for it and it then waits for the context's, and the tensors are
     recorded on the context's stream, so inputs, results and their memory may be used as usual."""
 
-    @property
-    def _raw_stream(self):
-        # the handle of a device's current stream, without building a Stream object
-        return self.torch._C._cuda_getCurrentRawStream
+    def _init_operators(self):
+        """What every call looks up, once: device number, types, the stream's handle and the way to ask for the handle
+        of the current stream without building a Stream object."""
+        torch = self.torch
+        self._dev = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        self._bf16, self._f32, self._i64 = torch.bfloat16, torch.float32, torch.int64
+        self._raw_stream = torch._C._cuda_getCurrentRawStream
+        self._handle = self.stream.cuda_stream
 
     def _other_stream(self):
         """The caller's current stream when it is not the context's, else None."""
-        if self._raw_stream(self.device.index or 0) == self.stream.cuda_stream:
+        if self._raw_stream(self._dev) == self._handle:
             return None
         return self.torch.cuda.current_stream(self.device)
 
@@ -301,7 +305,7 @@ class _Operators:
     def _need(self, name, t, dtype, shape, dense=False):
         """Raises unless t is a tensor of this context's device with the given type and shape (None: any
         size) whose last dimension is consecutive (dense: which is contiguous)."""
-        if t.get_device() != (self.device.index or 0):
+        if t.get_device() != self._dev:
             raise ValueError(f"{name} must be on {self.device} (got {t.device})")
         if t.dtype is not dtype:
             raise ValueError(f"{name} must be {dtype} (got {t.dtype})")
@@ -338,14 +342,13 @@ class _Operators:
     def _qk(self, q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved):
         """The packed argument struct of a call.  The checks run every time, so they are written to be
         quick; _check_qk repeats them with a message when one fails."""
-        torch, dev = self.torch, self.device.index or 0
-        f32 = torch.float32
+        torch, dev, f32 = self.torch, self._dev, self._f32
         some = q if q is not None else k
         if some is None or some.dim() != 3 or cos.dim() != 2:
             self._check_qk(q, k, cos, sin, positions, gain_q, gain_k)
         dt = some.dtype
         T, _, D = some.shape
-        ok = (dt is torch.bfloat16 or dt is f32) and cos.shape == sin.shape and cos.dtype is f32 and sin.dtype is f32 \
+        ok = (dt is self._bf16 or dt is f32) and cos.shape == sin.shape and cos.dtype is f32 and sin.dtype is f32 \
             and cos.is_contiguous() and sin.is_contiguous() and cos.get_device() == dev and sin.get_device() == dev
         hq = hk = pq = pk = qt = qh = kt = kh = pp = pgq = pgk = 0
         if q is not None:
@@ -360,7 +363,7 @@ class _Operators:
             ok = ok and t == T and d == D and (one == 1 or D < 2) and k.dtype is dt and k.get_device() == dev
         if positions is not None:
             pp = positions.data_ptr()
-            ok = ok and positions.dtype is torch.int64 and positions.shape == (T,) and positions.is_contiguous() \
+            ok = ok and positions.dtype is self._i64 and positions.shape == (T,) and positions.is_contiguous() \
                 and positions.get_device() == dev
         if gain_q is not None:
             pgq = gain_q.data_ptr()
@@ -371,7 +374,7 @@ class _Operators:
         if not ok:
             self._check_qk(q, k, cos, sin, positions, gain_q, gain_k)
         L, half = cos.shape
-        return _QK_PACK(T, L, hq, hk, D, 2 * half, BF16 if dt is torch.bfloat16 else F32, 1 if interleaved else 0, eps,
+        return _QK_PACK(T, L, hq, hk, D, 2 * half, F32 if dt is f32 else BF16, 1 if interleaved else 0, eps,
                         0, pgq, pgk, cos.data_ptr(), sin.data_ptr(), pp, pq, pk, qt, qh, kt, kh)
 
     def qk_norm_rope(self, q, k, cos, sin, positions=None, gain_q=None, gain_k=None, eps=1e-6, interleaved=False,
@@ -412,9 +415,8 @@ class _Operators:
     def qk_norm_rope_backward(self, dq_out, dk_out, q, k, cos, sin, positions=None, gain_q=None, gain_k=None,
                               eps=1e-6, interleaved=False):
         """muloco_qk_norm_rope_backward: from the gradients of the results, (dq, dk, dgain_q, dgain_k)."""
-        torch = self.torch
         a = self._qk(q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
-        dev = self.device.index or 0
+        dev = self._dev
         for name, y, t in (("dq_out", dq_out, q), ("dk_out", dk_out, k)):
             if (y is None) != (t is None):
                 raise ValueError(f"{name} is given without its input, or missing")
@@ -451,7 +453,7 @@ class _Operators:
 
     def _ffn(self, x, w1, w3, w2, activation):
         """The packed argument struct of a call (its checks as in _qk)."""
-        bf16, dev = self.torch.bfloat16, self.device.index or 0
+        bf16, dev = self._bf16, self._dev
         act = ACTIVATIONS.get(activation, -1)
         if act < 0:
             raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)} (got {activation!r})")
@@ -528,10 +530,9 @@ class Context(_Operators):
         if not torch.cuda.is_available():
             raise RuntimeError("no CUDA device: libmuloco has no CPU path")
         self.device = torch.device(device)
-        if self.device.index is None:
-            self.device = torch.device("cuda", torch.cuda.current_device())
         torch.cuda.set_device(self.device)
         self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        self._init_operators()
         cfg = make_config(_cfg.Workload("operators", K=1, H=1, J=1, tensors=[], muon_lr=0.0, muon_beta=0.0,
                                         muon_wd=0.0, outer_lr=1.0, outer_momentum=0.0))
         ctx = C.c_void_p()
@@ -624,7 +625,7 @@ class AdamW:
         self.opt = opt
 
     def _same(self, name, t, dtype, like):
-        if t.device != self.owner.device or t.dtype != dtype or t.shape != like.shape or not t.is_contiguous():
+        if t.get_device() != self.owner._dev or t.dtype != dtype or t.shape != like.shape or not t.is_contiguous():
             raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(like.shape)} on {self.owner.device}")
 
     def _check_grads(self, grads):
@@ -768,6 +769,7 @@ class MuLoCo(_Operators):
             self._tables.append(_ptr_table([self.ef[k][i].data_ptr() for k in range(self.K) for i in range(self.n)]))
             bufs.ef_k = C.cast(self._tables[-1], C.POINTER(C.c_void_p))
         self.stream = stream if stream is not None else torch.cuda.current_stream(dev)
+        self._init_operators()
         self.ctx = C.c_void_p()
         st = self.lib.muloco_create(C.byref(self.cfg), descs, self.n, C.byref(bufs),
                                     C.c_void_p(self.stream.cuda_stream), C.byref(self.ctx))

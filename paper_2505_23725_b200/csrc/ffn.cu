@@ -136,6 +136,12 @@ __device__ __forceinline__ void load_row32(const __nv_bfloat16* row, uint32_t (&
   }
 }
 
+// Programmatic dependent launch: wait until the kernel before this one in the stream is complete and its results
+// can be seen; let the next kernel's blocks start (their own wait holds them before they touch memory).  A
+// kernel releases only after its wait, so whatever starts early knows everything before this kernel complete.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
 // act(g) = g sigma and, for the backward pass, its slope.  sigma is the logistic function of g (silu) or of
 // 2 sqrt(2 / pi) (g + 0.044715 g^3), which makes g sigma the tanh form of gelu.  exp and the quotient are the fast ones (a few
 // units in the last place of float32): the results are rounded to 8 bits of mantissa.
@@ -197,6 +203,9 @@ ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) 
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem_base = tmem_base_slot;
+  // Everything above may run beside the end of the kernel before this one; nothing below does.
+  grid_wait();
+  grid_release();
 
   if (warp == 0) {
     // ------------------------------ TMA producer ------------------------------
@@ -414,6 +423,261 @@ ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) 
   }
 }
 
+// ---------------------------------------------------------------------------
+// Few tokens.  The 256 x 256 tiles above leave most of the machine idle when there are few of them, and what counts then
+// is to pull the weights out of memory with every SM.  Here the product is turned round: 128 columns of
+// a weight matrix are the rows of a tile (the left operand), NT tokens its columns, and the contraction is split over the
+// S CTAs of a cluster.  Each CTA sums its share in tensor memory (gated product: two accumulators), the partial
+// sums cross the cluster through distributed shared memory, every CTA adds up those of NT / S tokens in the order of
+// the ranks and applies the epilogue to them.  The second kernel of a pass starts while the first still runs
+// (programmatic dependent launch) and has its weights under way by the time its activations are complete.
+// ---------------------------------------------------------------------------
+constexpr int FEW_EPI_THREADS = 256;
+constexpr int FEW_THREADS = 64 + FEW_EPI_THREADS;   // producer, MMA issuer, eight epilogue warps
+
+template <int EPI, int NT>
+struct FewShape {
+  static constexpr int ACCS = EPI == EPI_GATE ? 2 : 1;             // weight matrices per tile
+  static constexpr uint32_t B_BYTES = NT * BK * 2;
+  static constexpr uint32_t STAGE = ACCS * A_BYTES + B_BYTES;
+  static constexpr uint32_t REDUCE = ACCS * 128u * NT * 4u;        // partial sums, over the pipeline's space
+  static constexpr int STAGES = (int)(200u * 1024u / STAGE) < 8 ? (int)(200u * 1024u / STAGE) : 8;
+  static constexpr uint32_t SMEM = (STAGES * STAGE > REDUCE ? STAGES * STAGE : REDUCE) + 1024u;
+  static constexpr int COLS = ACCS * NT;                           // accumulator columns in use
+  static constexpr uint32_t TMEM = COLS < 32 ? 32u : (uint32_t)COLS;
+};
+
+struct FewParams {
+  int M, T;                  // rows of the transposed result (columns of the output), tokens
+  int slabs0, slabs;
+  int a_mn, a_wide;
+  void* out; void* out2; void* out3;
+  const void* in1; const void* in2;
+  int weights_early;         // the kernel before this one does not write the weights
+  int* status;
+  unsigned long long wait_limit_ns;
+};
+struct FewMaps { CUtensorMap a[2], b[2]; };  // EPI_GATE: a = W1, W3; else one per operand pair
+
+__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+
+template <int EPI, int ACT, int NT>
+__global__ void __launch_bounds__(FEW_THREADS, 1)
+ffn_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ FewParams p) {
+  using Sh = FewShape<EPI, NT>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bar_full[Sh::STAGES];
+  __shared__ __align__(8) uint64_t bar_empty[Sh::STAGES];
+  __shared__ __align__(8) uint64_t bar_done;
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ volatile int abort_flag;
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  const int S = gridDim.x;                   // CTAs of the cluster
+  const int share = blockIdx.x;              // rank in it
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint64_t limit = p.wait_limit_ns;
+  const int m0 = blockIdx.y * 128, t0 = blockIdx.z * NT;
+  const int kb_first = (int)((int64_t)p.slabs * share / S), kb_end = (int)((int64_t)p.slabs * (share + 1) / S);
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int s = 0; s < Sh::STAGES; ++s) {
+      mbar_init(smem_u32(&bar_full[s]), 1);
+      mbar_init(smem_u32(&bar_empty[s]), 1);
+    }
+    mbar_init(smem_u32(&bar_done), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) tmem_alloc<1>(smem_u32(&tmem_base_slot), Sh::TMEM);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = tmem_base_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      const bool a_mn = p.a_mn, a_wide = p.a_wide;
+      const int slabs0 = p.slabs0;
+      auto load_weights = [&](int kb, uint32_t stage) {
+        const uint32_t sa = smem_base + stage * Sh::STAGE;
+        const uint32_t bar = smem_u32(&bar_full[stage]);
+        mbar_expect_tx(bar, Sh::STAGE);
+        const bool second = kb >= slabs0;
+        const int k0 = (second ? kb - slabs0 : kb) * BK;
+#pragma unroll
+        for (int w = 0; w < Sh::ACCS; ++w) {
+          const CUtensorMap* ma = &maps.a[EPI == EPI_GATE ? w : (second ? 1 : 0)];
+          const uint32_t dst = sa + (uint32_t)w * A_BYTES;
+          if (!a_mn) {
+            tma_load_2d(dst, ma, bar, k0, m0);
+          } else if (a_wide) {
+            tma_load_3d(dst, ma, bar, 0, k0, m0 >> 6);
+          } else {
+            tma_load_2d(dst, ma, bar, m0, k0);
+            tma_load_2d(dst + BK * 128, ma, bar, m0 + 64, k0);
+          }
+        }
+      };
+      auto load_tokens = [&](int kb, uint32_t stage) {
+        const bool second = kb >= slabs0;
+        const int k0 = (second ? kb - slabs0 : kb) * BK;
+        tma_load_2d(smem_base + stage * Sh::STAGE + Sh::ACCS * A_BYTES, &maps.b[second ? 1 : 0],
+                    smem_u32(&bar_full[stage]), k0, t0);
+      };
+      // Second kernel of a pass: the weights of its first stages do not depend on the first kernel (which only lets this
+      // one start once everything before itself is complete), the activations do.
+      const int ahead = kb_end - kb_first < Sh::STAGES ? kb_end - kb_first : Sh::STAGES;
+      if (!p.weights_early) grid_wait();
+      for (int i = 0; i < ahead; ++i) load_weights(kb_first + i, (uint32_t)i);
+      if (p.weights_early) grid_wait();
+      grid_release();
+      for (int i = 0; i < ahead; ++i) load_tokens(kb_first + i, (uint32_t)i);
+      uint32_t stage = 0, phase = 0;
+      for (int kb = kb_first + ahead; kb < kb_end; ++kb) {
+        if (!mbar_wait(smem_u32(&bar_empty[stage]), phase, &abort_flag, limit)) break;
+        load_weights(kb, stage);
+        load_tokens(kb, stage);
+        if (++stage == (uint32_t)Sh::STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0) {
+      constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+      constexpr uint32_t LBO_K = (16u >> 4) << 16, LBO_MN = ((uint32_t)(BK * 128) >> 4) << 16;
+      constexpr uint32_t STEP_K = (UMMA_K * 2) >> 4, STEP_MN = (UMMA_K * 128) >> 4;
+      const bool a_mn = p.a_mn;
+      const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn ? 1u : 0u) << 15) |
+                             ((uint32_t)(NT >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+      const uint32_t lbo_a = a_mn ? LBO_MN : LBO_K, astep = a_mn ? STEP_MN : STEP_K;
+      uint32_t stage = 0, phase = 0;
+      bool alive = true;
+      for (int kb = kb_first; kb < kb_end; ++kb) {
+        if (!mbar_wait(smem_u32(&bar_full[stage]), phase, &abort_flag, limit)) { alive = false; break; }
+        tc_fence_after();
+        const uint32_t sa = smem_base + stage * Sh::STAGE;
+        // (the address field has 18 bits; above them a shared address carries the rank in the cluster)
+        const uint32_t blo = (((sa + Sh::ACCS * A_BYTES) & 0x3FFFFu) >> 4) | LBO_K;
+#pragma unroll
+        for (int w = 0; w < Sh::ACCS; ++w) {
+          const uint32_t alo = (((sa + (uint32_t)w * A_BYTES) & 0x3FFFFu) >> 4) | lbo_a;
+#pragma unroll
+          for (int k = 0; k < BK / UMMA_K; ++k) {
+            const uint64_t adesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(alo + (uint32_t)k * astep);
+            const uint64_t bdesc = ((uint64_t)DESC_HI << 32) | (uint64_t)(blo + (uint32_t)k * STEP_K);
+            tc_mma_bf16<1>(tmem_base + (uint32_t)(w * NT), adesc, bdesc, idesc, (kb > kb_first || k > 0) ? 1u : 0u);
+          }
+        }
+        tc_commit<1>(smem_u32(&bar_empty[stage]));
+        if (++stage == (uint32_t)Sh::STAGES) { stage = 0; phase ^= 1u; }
+      }
+      if (alive) tc_commit<1>(smem_u32(&bar_done));
+    }
+    __syncwarp();
+  } else {
+    grid_wait();
+    grid_release();
+    mbar_wait(smem_u32(&bar_done), 0, &abort_flag, limit);   // on a timeout the flag is set and the results do not count
+    __syncwarp();
+  }
+  // Every copy of this CTA has landed and been used; once that holds for the whole cluster the pipeline's space
+  // takes the partial sums: [accumulator][source rank][token of this CTA's share][128 rows].
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  const int per = NT / S;                            // tokens that each CTA finishes
+  if (warp >= 2) {
+    const int quarter = warp & 3, side = (warp - 2) >> 2;
+    const int r128 = quarter * 32 + lane;
+#pragma unroll 1
+    for (int c = side * 32; c < Sh::COLS; c += 64) {
+      uint32_t v[32];
+      tc_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        const int col = c + e;
+        if (col < Sh::COLS) {
+          const int w = col / NT, tok = col % NT;
+          const int dst = tok / per, tl = tok - dst * per;
+          const uint32_t off = (uint32_t)((((w * S + share) * per + tl) * 128 + r128) * 4);
+          st_cluster_f32(map_to_rank(smem_base + off, (uint32_t)dst), __uint_as_float(v[e]));
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  cluster_sync_all();
+  tc_fence_after();
+  if (warp >= 2) {
+    // two neighbouring columns per thread, the tokens over the thread groups, four tokens at a time
+    constexpr int GROUPS = FEW_EPI_THREADS / 64, BATCH = 4;
+    const float* sums = reinterpret_cast<const float*>(smem_raw + (smem_base - smem_u32(smem_raw)));
+    const int id = threadIdx.x - 64;
+    const int r = (id & 63) * 2, m = m0 + r;
+    const int left = p.T - (t0 + share * per);       // tokens of this CTA that exist
+    const int n_tok = left < per ? left : per;
+    auto total = [&](int w, int tl) {
+      float2 x = make_float2(0.f, 0.f);
+      for (int src = 0; src < S; ++src) {
+        const float2 y = *reinterpret_cast<const float2*>(sums + ((w * S + src) * per + tl) * 128 + r);
+        x.x += y.x; x.y += y.y;
+      }
+      return x;
+    };
+    auto put = [&](void* base, int64_t o, float a0, float a1) {
+      if (base) *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(base) + o) = pack_bf16x2(a0, a1);
+    };
+    if (m < p.M) {
+      for (int tl0 = id >> 6; tl0 < n_tok; tl0 += GROUPS * BATCH) {
+        uint32_t gv[BATCH], uv[BATCH];
+        if (EPI == EPI_GATE_BACK) {
+#pragma unroll
+          for (int j = 0; j < BATCH; ++j) {
+            const int tl = tl0 + j * GROUPS;
+            if (tl >= n_tok) break;
+            const int64_t o = (int64_t)(t0 + share * per + tl) * p.M + m;
+            gv[j] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(p.in1) + o);
+            uv[j] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(p.in2) + o);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < BATCH; ++j) {
+          const int tl = tl0 + j * GROUPS;
+          if (tl >= n_tok) break;
+          const int64_t o = (int64_t)(t0 + share * per + tl) * p.M + m;
+          const float2 x = total(0, tl);
+          if (EPI == EPI_STORE) {
+            put(p.out, o, x.x, x.y);
+          } else if (EPI == EPI_GATE) {
+            const float2 y = total(1, tl);
+            put(p.out2, o, x.x, x.y);
+            put(p.out3, o, y.x, y.y);
+            put(p.out, o, act_value<ACT>(x.x) * y.x, act_value<ACT>(x.y) * y.y);
+          } else {
+            float v0, s0, v1, s1;
+            act_both<ACT>(bf16_lo(gv[j]), v0, s0);
+            act_both<ACT>(bf16_hi(gv[j]), v1, s1);
+            put(p.out, o, x.x * bf16_lo(uv[j]) * s0, x.y * bf16_hi(uv[j]) * s1);
+            put(p.out2, o, x.x * v0, x.y * v1);
+          }
+        }
+      }
+    }
+  }
+  if (abort_flag) {
+    const uint64_t t1 = global_timer_ns();           // let copies and MMAs still in flight land
+    while (global_timer_ns() - t1 < 200000ull) __nanosleep(1000);
+    if (threadIdx.x == 0) atomicOr(p.status, ST_TIMEOUT);
+  }
+  __syncthreads();
+  if (warp == 1) tmem_dealloc<1>(tmem_base, Sh::TMEM);
+}
+
 // ------------------------------ host side ----------------------------------
 // A row-major bf16 matrix as an operand: rows x cols with row pitch ld.
 struct Mat { const void* p; int64_t rows, cols, ld; };
@@ -473,10 +737,22 @@ struct Builder {
   }
 };
 
+// Raises a kernel's shared-memory limit, once per device (`allowed`: the last device it was raised on).
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, int* allowed) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess || *allowed == dev) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) *allowed = dev;
+  return e;
+}
+
 template <int EPI, int ACT>
 cudaError_t launch_kernel(cudaStream_t st, const Builder& b, int n_sms) {
   auto kernel = ffn_kernel<EPI, ACT>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM_BYTES);
+  static int allowed = -1;
+  cudaError_t e = allow_smem(kernel, (int)SMEM_BYTES, &allowed);
   if (e != cudaSuccess) return e;
   const int units = n_sms / CG;
   const int workers = b.p.total_tiles < units ? b.p.total_tiles : units;
@@ -486,10 +762,12 @@ cudaError_t launch_kernel(cudaStream_t st, const Builder& b, int n_sms) {
   cfg.blockDim = dim3(FFN_THREADS);
   cfg.dynamicSmemBytes = SMEM_BYTES;
   cfg.stream = st;
-  cudaLaunchAttribute at[1];
+  cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = CG; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-  cfg.attrs = at; cfg.numAttrs = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, b.maps, b.p);
 }
 
@@ -510,9 +788,119 @@ cudaError_t launch_built(cudaStream_t st, Builder& b, const FfnArgs& a, int epi,
   return launch_kernel<EPI_STORE, MULOCO_ACT_SILU>(st, b, a.n_sms);
 }
 
+// ---- few tokens ----
+template <int EPI, int ACT, int NT>
+cudaError_t launch_few_kernel(cudaStream_t st, const FewMaps& m, const FewParams& p, int split) {
+  auto kernel = ffn_few_kernel<EPI, ACT, NT>;
+  using Sh = FewShape<EPI, NT>;
+  static int allowed = -1;                   // the device for which the kernel may use its shared memory
+  cudaError_t e = allow_smem(kernel, (int)Sh::SMEM, &allowed);
+  if (e != cudaSuccess) return e;
+  // only the stages that the CTA's slabs use, so that the next kernel's blocks may find room beside this one's
+  const int slabs = (p.slabs + split - 1) / split;
+  const uint32_t used = (uint32_t)(slabs < Sh::STAGES ? slabs : Sh::STAGES) * Sh::STAGE;
+  const size_t smem = (used > Sh::REDUCE ? used : Sh::REDUCE) + 1024u;
+  cudaLaunchConfig_t cfg;
+  memset(&cfg, 0, sizeof cfg);
+  cfg.gridDim = dim3((unsigned)split, (unsigned)((p.M + 127) / 128), (unsigned)((p.T + NT - 1) / NT));
+  cfg.blockDim = dim3(FEW_THREADS);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = split; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, m, p);
+}
+
+template <int EPI, int ACT>
+cudaError_t launch_few_nt(cudaStream_t st, int nt, const FewMaps& m, const FewParams& p, int split) {
+  if (nt == 16) return launch_few_kernel<EPI, ACT, 16>(st, m, p, split);
+  if (nt == 32) return launch_few_kernel<EPI, ACT, 32>(st, m, p, split);
+  if (nt == 64) return launch_few_kernel<EPI, ACT, 64>(st, m, p, split);
+  return launch_few_kernel<EPI, ACT, 128>(st, m, p, split);
+}
+
+// Tokens per tile.  Wider tiles read the weights fewer times and exchange more partial sums; 128 only where 64
+// would give more tiles than SMs.  Whole forward pass, us, tiles of 64 / 128: 128 tokens at 768 x 2048 21 / 32, at
+// 2048 x 5632 46 / 49; 256 tokens at 2048 x 5632 (176 tiles of 64) 81 / 60.
+int few_tile(int64_t T, int64_t M, int n_sms) {
+  if (T <= 32) return T <= 16 ? 16 : 32;
+  return (M + 127) / 128 * ((T + 63) / 64) <= n_sms ? 64 : 128;
+}
+
+struct FewOperand { Mat weight[2]; Mat tokens[2]; };   // per operand pair (gated product: weight = W1, W3)
+
+// One product of the few-token form.  `mn`: the weights are stored contraction index first (MN-major operand).
+cudaError_t launch_few(cudaStream_t st, const FfnArgs& a, int epi, const FewOperand& q, bool mn, int n_pairs,
+                       FewParams p, const char** what) {
+  const int nt = few_tile(a.T, p.M, a.n_sms);
+  FewMaps m;
+  bool ok = true;
+  const int n_weights = epi == EPI_GATE ? 2 : n_pairs;
+  p.a_mn = mn;
+  for (int w = 0; w < n_weights; ++w) {
+    if (mn) {
+      const bool wide = encode_wide(&m.a[w], q.weight[w]);
+      if (w && wide != (p.a_wide != 0)) ok = false;
+      p.a_wide = wide;
+      if (!wide) ok = ok && encode(&m.a[w], q.weight[w], 64, BK);
+    } else {
+      ok = ok && encode(&m.a[w], q.weight[w], BK, 128);
+    }
+  }
+  for (int w = 0; w < n_pairs; ++w) ok = ok && encode(&m.b[w], q.tokens[w], BK, nt);
+  *what = "cuTensorMapEncodeTiled";
+  if (!ok) return cudaErrorInvalidValue;
+  *what = "launch of the feed-forward kernel for few tokens";
+  p.T = (int)a.T;
+  p.status = a.status;
+  p.wait_limit_ns = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
+  // Split the contraction until every SM has a CTA.  Clusters of eight only while all of them find room at once
+  // (an SM cluster has place for two; 16 tiles of 2048 x 5632 at 8: 33 us for the pass, at 4: 29).
+  const int64_t tiles = (int64_t)((p.M + 127) / 128) * ((a.T + nt - 1) / nt);
+  int split = 1;
+  while (split < 4 && tiles * split * 2 <= a.n_sms && split * 2 <= p.slabs) split *= 2;
+  if (split == 4 && tiles * 8 <= 96 && p.slabs >= 8) split = 8;
+  const bool gelu = a.act == MULOCO_ACT_GELU;
+  if (epi == EPI_GATE)
+    return gelu ? launch_few_nt<EPI_GATE, MULOCO_ACT_GELU>(st, nt, m, p, split) : launch_few_nt<EPI_GATE, MULOCO_ACT_SILU>(st, nt, m, p, split);
+  if (epi == EPI_GATE_BACK)
+    return gelu ? launch_few_nt<EPI_GATE_BACK, MULOCO_ACT_GELU>(st, nt, m, p, split)
+                : launch_few_nt<EPI_GATE_BACK, MULOCO_ACT_SILU>(st, nt, m, p, split);
+  return launch_few_nt<EPI_STORE, MULOCO_ACT_SILU>(st, nt, m, p, split);
+}
+
+int slabs_of(int64_t k) { return (int)((k + BK - 1) / BK); }
+
+// Up to how many tokens a pass takes the few-token form, whole pass in us, few-token form / 256 x 256 tiles:
+// forward, 128 tokens: 21 / 25 (768 x 2048), 27 / 32 (1024 x 2816), 46 / 54 (2048 x 5632); 256: 26 / 25, 34 / 32, 60 / 54.
+// Backward, 256 tokens: 32 / 42, 44 / 53, 91 / 112; 384: 42 / 42, 49 / 53, 109 / 112.
+constexpr int64_t FEW_FORWARD = 128, FEW_BACKWARD = 256;
+
 }  // namespace
 
 cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
+  if (a.T <= FEW_FORWARD) {
+    FewParams p;
+    memset(&p, 0, sizeof p);
+    p.M = (int)a.F; p.slabs0 = p.slabs = slabs_of(a.d);
+    p.out = a.h; p.out2 = a.g; p.out3 = a.u;
+    FewOperand q{{Mat{a.w1, a.d, a.F, a.ldw1}, Mat{a.w3, a.d, a.F, a.ldw3}}, {Mat{a.x, a.T, a.d, a.ldx}, Mat{}}};
+    cudaError_t e = launch_few(st, a, EPI_GATE, q, true, 1, p, what);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+    memset(&p, 0, sizeof p);
+    p.M = (int)a.d; p.slabs0 = p.slabs = slabs_of(a.F);
+    p.out = a.y;
+    p.weights_early = 1;
+    FewOperand r{{Mat{a.w2, a.F, a.d, a.ldw2}, Mat{}}, {Mat{a.h, a.T, a.F, a.F}, Mat{}}};
+    e = launch_few(st, a, EPI_STORE, r, true, 1, p, what);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+  }
   {
     Builder b;
     Prob& q = b.add(a.T, a.F, 128, a.d, 0);
@@ -539,7 +927,18 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
 }
 
 cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
-  if (a.dx || a.dw1 || a.dw3) {
+  const bool few = a.T <= FEW_BACKWARD;
+  if ((a.dx || a.dw1 || a.dw3) && few) {
+    FewParams p;
+    memset(&p, 0, sizeof p);
+    p.M = (int)a.F; p.slabs0 = p.slabs = slabs_of(a.d);
+    p.in1 = a.g; p.in2 = a.u;
+    p.out = a.dg; p.out2 = a.du;
+    FewOperand q{{Mat{a.w2, a.F, a.d, a.ldw2}, Mat{}}, {Mat{a.dy, a.T, a.d, a.lddy}, Mat{}}};
+    cudaError_t e = launch_few(st, a, EPI_GATE_BACK, q, false, 1, p, what);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  } else if (a.dx || a.dw1 || a.dw3) {
     Builder b;
     Prob& q = b.add(a.T, a.F, BN, a.d, 0);
     q.map_a[0] = b.kmajor(Mat{a.dy, a.T, a.d, a.lddy});
@@ -550,9 +949,21 @@ cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches
     if (e != cudaSuccess) return e;
     ++*launches;
   }
+  if (a.dx && few) {
+    FewParams p;
+    memset(&p, 0, sizeof p);
+    p.M = (int)a.d; p.slabs0 = slabs_of(a.F); p.slabs = 2 * p.slabs0;
+    p.out = a.dx;
+    p.weights_early = 1;
+    FewOperand q{{Mat{a.w1, a.d, a.F, a.ldw1}, Mat{a.w3, a.d, a.F, a.ldw3}},
+                 {Mat{a.dg, a.T, a.F, a.F}, Mat{a.du, a.T, a.F, a.F}}};
+    cudaError_t e = launch_few(st, a, EPI_STORE, q, false, 2, p, what);
+    if (e != cudaSuccess) return e;
+    ++*launches;
+  }
   Builder b;
   const Mat dg{a.dg, a.T, a.F, a.F}, du{a.du, a.T, a.F, a.F};
-  if (a.dx) {
+  if (a.dx && !few) {
     Prob& q = b.add(a.T, a.d, BN, a.F, a.F);
     q.map_a[0] = b.kmajor(dg);
     q.map_a[1] = b.kmajor(du);
