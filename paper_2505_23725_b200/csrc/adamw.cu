@@ -12,7 +12,7 @@ namespace muloco {
 namespace {
 
 constexpr int AW_THREADS = 256;
-constexpr int AW_WARPS = AW_THREADS / 32;
+static_assert(ADAMW_UNIT == AW_THREADS / 32 * MULOCO_ADAMW_BLOCK, "one block of elements per warp");
 constexpr float AW_TINY = 1e-36f;       // blocks at or below this magnitude are encoded as zeros
 constexpr float AW_MAGIC = 12582912.0f; // 1.5 * 2^23: adding it leaves the integer part in the low bits
 
@@ -80,14 +80,30 @@ __device__ __forceinline__ void store_copy(void* c, int64_t i, const Four& v, bo
   }
 }
 
-// One block of 256 elements of tensor `s`, by one warp.  Returns whether a gradient was not finite.
-template <int BITS, bool GBF16>
-__device__ __forceinline__ bool adamw_block(const AdamwSeg& s, const void* g, int64_t blk, const AdamwStep& a) {
+// Byte e of w as a float, exactly: the byte becomes the low mantissa bits of 2^23.
+__device__ __forceinline__ float byte_f32(uint32_t w, int e) {
+  return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440u | (uint32_t)e)) - 8388608.0f;
+}
+// The low (h = 0) or high half of w as a float, exactly.
+__device__ __forceinline__ float half_f32(uint32_t w, int h) {
+  return __uint_as_float(__byte_perm(w, 0x4B000000u, h ? 0x7432u : 0x7410u)) - 8388608.0f;
+}
+// Byte 0 of a, b, c, d as the bytes of a word.
+__device__ __forceinline__ uint32_t pack_bytes(float a, float b, float c, float d) {
+  const uint32_t lo = __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040u);
+  const uint32_t hi = __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040u);
+  return __byte_perm(lo, hi, 0x5410u);
+}
+
+// One block of 256 elements by one warp.  FULL: all of them exist and every access is aligned.  Returns whether a
+// gradient was not finite.
+template <int BITS, bool GBF16, bool FULL>
+__device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, int blk, const AdamwStep& a) {
   const int lane = threadIdx.x & 31;
-  const bool vec_g = (((uintptr_t)g) & (GBF16 ? 7 : 15)) == 0;
-  const bool vec_t = (((uintptr_t)s.theta) & 15) == 0;
-  const bool vec_c = (((uintptr_t)s.copy) & 7) == 0;
-  const int64_t i0 = blk * MULOCO_ADAMW_BLOCK + lane * 4;
+  const bool vec_g = FULL || (((uintptr_t)g) & (GBF16 ? 7 : 15)) == 0;
+  const bool vec_t = FULL || (((uintptr_t)s.theta) & 15) == 0;
+  const bool vec_c = FULL || (((uintptr_t)s.copy) & 7) == 0;
+  const int i0 = blk * MULOCO_ADAMW_BLOCK + lane * 4;
   const float om1 = 1.0f - a.beta1, om2 = 1.0f - a.beta2;
   const float lr = a.lr * s.lr_mult, lr_wd = a.lr_wd * (s.lr_mult * s.wd_mult);
 
@@ -97,13 +113,13 @@ __device__ __forceinline__ bool adamw_block(const AdamwSeg& s, const void* g, in
   int cnt[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int64_t i = i0 + h * 128;
-    const int64_t left = s.n - i;
-    cnt[h] = left >= 4 ? 4 : (left > 0 ? (int)left : 0);
+    const int i = i0 + h * 128;
+    const int left = s.n - i;
+    cnt[h] = FULL || left >= 4 ? 4 : (left > 0 ? left : 0);
     gr[h] = load_grad<GBF16>(g, i, vec_g, cnt[h]);
     th[h] = load_f32(s.theta + i, vec_t, cnt[h]);
     if (BITS == 8) {
-      // the padding of the last block belongs to the state and is read and written with it
+      // the padding of the last block belongs to the state: it is read, counts as zero and is written
       c1[h] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(s.s1) + i);
       c2[h] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(s.s2) + i);
     } else {
@@ -114,44 +130,53 @@ __device__ __forceinline__ bool adamw_block(const AdamwSeg& s, const void* g, in
   float sc1 = 0.f, sc2 = 0.f;
   if (BITS == 8) { sc1 = s.scale1[blk]; sc2 = s.scale2[blk]; }
 
-  bool bad = false;
+  float finite = 0.f;                           // 0 * g summed: NaN as soon as one gradient is not finite
   float max1 = 0.f, max2 = 0.f;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < 2; ++h) {
+    if (BITS == 8) {
+      c1[h] ^= 0x80808080u;                     // two's complement codes plus 128
+      if (!FULL) {
+        const uint32_t keep = cnt[h] >= 4 ? 0xffffffffu : (1u << (8 * cnt[h])) - 1u;
+        c1[h] = (c1[h] & keep) | (0x80808080u & ~keep);
+        c2[h] &= keep;
+      }
+    }
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float ge = gr[h].x[e];
-      bad |= !(fabsf(ge) <= 3.402823466e38f);
+      finite = fmaf(ge, 0.f, finite);
       float root;
       if (BITS == 8) {
-        const bool there = e < cnt[h];
-        const float k1 = (float)(int)(int8_t)(c1[h] >> (8 * e)), k2 = (float)((c2[h] >> (8 * e)) & 0xffu);
-        const float mo = __fmul_rn(there ? k1 : 0.f, sc1);
-        const float ro = __fmul_rn(there ? k2 : 0.f, sc2);
+        const float mo = __fmul_rn(byte_f32(c1[h], e) - 128.0f, sc1);
+        const float ro = __fmul_rn(byte_f32(c2[h], e), sc2);
         const float mn = __fadd_rn(__fmul_rn(mo, a.beta1), __fmul_rn(ge, om1));
         const float vn = __fadd_rn(__fmul_rn(__fmul_rn(ro, ro), a.beta2), __fmul_rn(__fmul_rn(ge, ge), om2));
         root = __fsqrt_rn(vn);
         m[h].x[e] = mn;
         v[h].x[e] = root;                       // the root is what is encoded
-        // integer maxima: bits of non-negative floats order like integers, a NaN above all
-        max1 = __uint_as_float(max(__float_as_uint(max1), __float_as_uint(fabsf(mn))));
-        max2 = __uint_as_float(max(__float_as_uint(max2), __float_as_uint(root)));
+        max1 = fmaxf(max1, fabsf(mn));
+        max2 = fmaxf(max2, root);
       } else {
         m[h].x[e] = fmaf(a.beta1, m[h].x[e], om1 * ge);
         v[h].x[e] = fmaf(a.beta2, v[h].x[e], om2 * ge * ge);
         root = sqrtf(v[h].x[e]);
       }
+      // The quotient to two ulp: an update of about lr, far below theta's own rounding.  (It is zero for denominators
+      // above 2^126, where the true one is too small to change theta.)
       const float den = fmaf(root, a.inv_sqrt_bc2, a.eps);
-      // two ulp of the quotient, an update of about lr: far below theta's own rounding
       const float upd = __fdividef(m[h].x[e] * a.inv_bc1, den);
-      // (that quotient flushes to zero for denominators above 2^126, where the true one is below 2^-100)
       th[h].x[e] = th[h].x[e] - fmaf(lr, upd, lr_wd * th[h].x[e]);
     }
+  }
+  const bool bad = __any_sync(0xffffffffu, !(finite == 0.f));
 
   float inv1 = 0.f, inv2 = 0.f;
   if (BITS == 8) {
+    // bits of non-negative floats order like integers: one integer maximum per moment
     max1 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(max1)));
     max2 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(max2)));
+    if (bad) max1 = max2 = __int_as_float(0x7fffffff);      // such a block's moments are NaN from here on
     inv1 = max1 > AW_TINY ? __fdiv_rn(127.f, max1) : 0.f;
     inv2 = max2 > AW_TINY ? __fdiv_rn(255.f, max2) : 0.f;
     if (lane == 0) {
@@ -161,22 +186,21 @@ __device__ __forceinline__ bool adamw_block(const AdamwSeg& s, const void* g, in
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int64_t i = i0 + h * 128;
+    const int i = i0 + h * 128;
     if (BITS == 8) {
-      uint32_t o1 = 0, o2 = 0;
+      float t1[4], t2[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t r = hash32((uint32_t)(s.dither_base + i + e) + a.dither);
-        const float u1 = (float)(r & 0xffffu) * 1.52587890625e-5f, u2 = (float)(r >> 16) * 1.52587890625e-5f;
-        float t1 = __fadd_rn(__fmul_rn(m[h].x[e], inv1), u1);
-        float t2 = __fadd_rn(__fmul_rn(v[h].x[e], inv2), u2);
-        t1 = fminf(fmaxf(t1, -127.f), 127.f);
-        t2 = fminf(fmaxf(t2, v[h].x[e] > 0.f ? 1.f : 0.f), 255.f);
-        o1 |= (__float_as_uint(__fadd_rd(t1, AW_MAGIC)) & 0xffu) << (8 * e);
-        o2 |= (__float_as_uint(__fadd_rd(t2, AW_MAGIC)) & 0xffu) << (8 * e);
+        const uint32_t r = hash32((uint32_t)s.dither_base + a.dither + (uint32_t)(i + e));
+        // x * inv rounded, plus u rounded: u = k 2^-16 is exact, so the second step is one fused operation
+        t1[e] = fmaf(half_f32(r, 0), 1.52587890625e-5f, __fmul_rn(m[h].x[e], inv1));
+        t2[e] = fmaf(half_f32(r, 1), 1.52587890625e-5f, __fmul_rn(v[h].x[e], inv2));
+        t1[e] = __fadd_rd(fminf(fmaxf(t1[e], -127.f), 127.f), AW_MAGIC);
+        // at least 1 wherever v > 0: a root of a float32 is at least 2^-75, times 2^126 saturates to 1
+        t2[e] = __fadd_rd(fminf(fmaxf(t2[e], __saturatef(v[h].x[e] * 8.507059173023462e37f)), 255.f), AW_MAGIC);
       }
-      *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.s1) + i) = o1;
-      *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.s2) + i) = o2;
+      *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.s1) + i) = pack_bytes(t1[0], t1[1], t1[2], t1[3]);
+      *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.s2) + i) = pack_bytes(t2[0], t2[1], t2[2], t2[3]);
     } else {
       store_f32(reinterpret_cast<float*>(s.s1) + i, m[h], true, cnt[h]);
       store_f32(reinterpret_cast<float*>(s.s2) + i, v[h], true, cnt[h]);
@@ -188,74 +212,69 @@ __device__ __forceinline__ bool adamw_block(const AdamwSeg& s, const void* g, in
 }
 
 template <int BITS, bool GBF16>
-__global__ void __launch_bounds__(AW_THREADS)
-adamw_multi_kernel(const AdamwSeg* __restrict__ segs, const int* __restrict__ unit_seg,
-                   const void* const* __restrict__ grads, int n_segs, AdamwStep a, int* __restrict__ status) {
-  const int64_t unit = blockIdx.x;
-  const int si = unit_seg[unit];
-  if (!MULOCO_IN_BOUNDS(si >= 0 && si < n_segs, status)) return;
-  const AdamwSeg s = segs[si];
-  const int64_t blk = (unit - s.unit_begin) * AW_WARPS + (threadIdx.x >> 5);
+__global__ void __launch_bounds__(AW_THREADS, 4)
+adamw_multi_kernel(const AdamwUnit* __restrict__ units, const void* const* __restrict__ grads, AdamwStep a,
+                   int* __restrict__ status) {
+  const AdamwUnit s = units[blockIdx.x];
+  const int blk = threadIdx.x >> 5;
   if (blk * MULOCO_ADAMW_BLOCK >= s.n) return;
-  const bool bad = adamw_block<BITS, GBF16>(s, grads[si], blk, a);
-  if (__any_sync(0xffffffffu, bad) && (threadIdx.x & 31) == 0) atomicOr(status, ST_NONFINITE);
+  const void* g = s.grad;
+  if (grads)
+    g = reinterpret_cast<const uint8_t*>(grads[s.tensor]) + s.first * (GBF16 ? 2 : 4);
+  const bool full = (blk + 1) * MULOCO_ADAMW_BLOCK <= s.n &&
+                    ((((uintptr_t)s.theta) & 15) | (((uintptr_t)s.copy) & 7) | (((uintptr_t)g) & (GBF16 ? 7 : 15))) == 0;
+  const bool bad = full ? adamw_block<BITS, GBF16, true>(s, g, blk, a) : adamw_block<BITS, GBF16, false>(s, g, blk, a);
+  if (bad && (threadIdx.x & 31) == 0) atomicOr(status, ST_NONFINITE);
 }
 
 __global__ void __launch_bounds__(AW_THREADS)
-adamw_moments_kernel(const AdamwSeg* __restrict__ segs, const int* __restrict__ unit_seg, int n_segs,
-                     float* __restrict__ m, float* __restrict__ v, int* __restrict__ status) {
-  const int64_t unit = blockIdx.x;
-  const int si = unit_seg[unit];
-  if (!MULOCO_IN_BOUNDS(si >= 0 && si < n_segs, status)) return;
-  const AdamwSeg s = segs[si];
-  const int64_t blk = (unit - s.unit_begin) * AW_WARPS + (threadIdx.x >> 5);
+adamw_moments_kernel(const AdamwUnit* __restrict__ units, float* __restrict__ m, float* __restrict__ v) {
+  const AdamwUnit& s = units[blockIdx.x];
+  const int blk = threadIdx.x >> 5;
   if (blk * MULOCO_ADAMW_BLOCK >= s.n) return;
   const float sc1 = s.scale1[blk], sc2 = s.scale2[blk];
+  uint32_t c1[2], c2[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const int64_t i = blk * MULOCO_ADAMW_BLOCK + h * 128 + (threadIdx.x & 31) * 4;
-    const uint32_t c1 = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(s.s1) + i);
-    const uint32_t c2 = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(s.s2) + i);
-    float4 om, ov;
-    float* pm = &om.x;
-    float* pv = &ov.x;
+    const int i = blk * MULOCO_ADAMW_BLOCK + h * 128 + (threadIdx.x & 31) * 4;
+    c1[h] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(s.s1) + i) ^ 0x80808080u;
+    c2[h] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint8_t*>(s.s2) + i);
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = blk * MULOCO_ADAMW_BLOCK + h * 128 + (threadIdx.x & 31) * 4;
+    Four om, ov;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      pm[e] = __fmul_rn((float)(int)(int8_t)(c1 >> (8 * e)), sc1);
-      const float r = __fmul_rn((float)((c2 >> (8 * e)) & 0xffu), sc2);
-      pv[e] = __fmul_rn(r, r);
+      om.x[e] = __fmul_rn(byte_f32(c1[h], e) - 128.0f, sc1);
+      const float r = __fmul_rn(byte_f32(c2[h], e), sc2);
+      ov.x[e] = __fmul_rn(r, r);
     }
-    __stcs(reinterpret_cast<float4*>(m + s.dither_base + i), om);
-    __stcs(reinterpret_cast<float4*>(v + s.dither_base + i), ov);
+    __stcs(reinterpret_cast<float4*>(m + s.dither_base + i), make_float4(om.x[0], om.x[1], om.x[2], om.x[3]));
+    __stcs(reinterpret_cast<float4*>(v + s.dither_base + i), make_float4(ov.x[0], ov.x[1], ov.x[2], ov.x[3]));
   }
 }
 
 }  // namespace
 
-int64_t adamw_units(int64_t n) {
-  const int64_t per = (int64_t)AW_WARPS * MULOCO_ADAMW_BLOCK;
-  return (n + per - 1) / per;
-}
-
 uint32_t adamw_dither(uint32_t seed, int64_t step) { return hash32(hash32(seed) + (uint32_t)step); }
 
-void launch_adamw_multi(cudaStream_t st, const AdamwSeg* segs, const int* unit_seg, const void* const* grads,
-                        int n_segs, int64_t n_units, int state_bits, int g_is_bf16, const AdamwStep& a, int* status) {
+void launch_adamw_multi(cudaStream_t st, const AdamwUnit* units, const void* const* grads, int64_t n_units,
+                        int state_bits, int g_is_bf16, const AdamwStep& a, int* status) {
   if (n_units <= 0) return;
   const unsigned grid = (unsigned)n_units;   // one unit per block, in address order
   if (state_bits == 8) {
-    if (g_is_bf16) adamw_multi_kernel<8, true><<<grid, AW_THREADS, 0, st>>>(segs, unit_seg, grads, n_segs, a, status);
-    else adamw_multi_kernel<8, false><<<grid, AW_THREADS, 0, st>>>(segs, unit_seg, grads, n_segs, a, status);
+    if (g_is_bf16) adamw_multi_kernel<8, true><<<grid, AW_THREADS, 0, st>>>(units, grads, a, status);
+    else adamw_multi_kernel<8, false><<<grid, AW_THREADS, 0, st>>>(units, grads, a, status);
   } else {
-    if (g_is_bf16) adamw_multi_kernel<32, true><<<grid, AW_THREADS, 0, st>>>(segs, unit_seg, grads, n_segs, a, status);
-    else adamw_multi_kernel<32, false><<<grid, AW_THREADS, 0, st>>>(segs, unit_seg, grads, n_segs, a, status);
+    if (g_is_bf16) adamw_multi_kernel<32, true><<<grid, AW_THREADS, 0, st>>>(units, grads, a, status);
+    else adamw_multi_kernel<32, false><<<grid, AW_THREADS, 0, st>>>(units, grads, a, status);
   }
 }
 
-void launch_adamw_moments(cudaStream_t st, const AdamwSeg* segs, const int* unit_seg, int n_segs, int64_t n_units,
-                          float* m, float* v, int* status) {
+void launch_adamw_moments(cudaStream_t st, const AdamwUnit* units, int64_t n_units, float* m, float* v) {
   if (n_units <= 0) return;
-  adamw_moments_kernel<<<(unsigned)n_units, AW_THREADS, 0, st>>>(segs, unit_seg, n_segs, m, v, status);
+  adamw_moments_kernel<<<(unsigned)n_units, AW_THREADS, 0, st>>>(units, m, v);
 }
 
 }  // namespace muloco

@@ -184,17 +184,21 @@ void ctx_count_launches(muloco_ctx* c, int n);
 // (zero between launches).  Allocated on first use; nullptr when that fails.
 float* ctx_qk_scratch(muloco_ctx* c, int** tickets);
 
-// AdamW over many tensors: one entry per tensor (include/muloco.h has the layout of the states).
-struct AdamwSeg {
-  float* theta;
+// AdamW over many tensors (include/muloco.h has the layout of the states): one entry per work unit of ADAMW_UNIT
+// consecutive elements of a tensor, with everything a block needs, so that its first load names all the others.
+constexpr int ADAMW_UNIT = 8 * MULOCO_ADAMW_BLOCK;
+struct alignas(16) AdamwUnit {
+  float* theta;          // of the unit's first element, like all pointers here
   void* copy;            // bf16 copy of the parameters, or NULL
   void* s1;
   void* s2;
   float* scale1;
   float* scale2;
-  int64_t n;
-  int64_t unit_begin;    // first work unit of this tensor
-  int64_t dither_base;   // its first element in the padded layout
+  const void* grad;      // gradient named at create time, or NULL
+  int64_t first;         // the unit's first element inside its tensor
+  int64_t dither_base;   // ... and in the padded layout
+  int32_t n;             // elements of the unit
+  int32_t tensor;
   float wd_mult, lr_mult;
 };
 struct AdamwStep {
@@ -203,13 +207,11 @@ struct AdamwStep {
   float inv_bc1, inv_sqrt_bc2;
   uint32_t dither;
 };
-int64_t adamw_units(int64_t n);                       // work units of a tensor of n elements
 uint32_t adamw_dither(uint32_t seed, int64_t step);   // what step `step` adds to the element index before hashing
-// unit_seg[unit] = the entry that the unit belongs to; grads[entry] = its gradient
-void launch_adamw_multi(cudaStream_t st, const AdamwSeg* segs, const int* unit_seg, const void* const* grads,
-                        int n_segs, int64_t n_units, int state_bits, int g_is_bf16, const AdamwStep& a, int* status);
-void launch_adamw_moments(cudaStream_t st, const AdamwSeg* segs, const int* unit_seg, int n_segs, int64_t n_units,
-                          float* m, float* v, int* status);
+// grads[tensor]: the gradients of this step, or NULL for those in the units
+void launch_adamw_multi(cudaStream_t st, const AdamwUnit* units, const void* const* grads, int64_t n_units,
+                        int state_bits, int g_is_bf16, const AdamwStep& a, int* status);
+void launch_adamw_moments(cudaStream_t st, const AdamwUnit* units, int64_t n_units, float* m, float* v);
 
 // Query / key norm with rotation.  One of the two tensors of a call:
 struct QkTensor {

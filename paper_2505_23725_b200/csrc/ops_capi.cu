@@ -30,9 +30,7 @@ struct muloco_adamw {
   int64_t n_units = 0;
   bool has_default = true;               // every tensor named a gradient at create time
   std::vector<int64_t> numel;
-  AdamwSeg* d_segs = nullptr;
-  int* d_unit_seg = nullptr;
-  const void** d_default = nullptr;      // gradients named at create time
+  AdamwUnit* d_units = nullptr;
   const void** d_grads = nullptr;        // gradients of the current step
   const void** h_grads[GRAD_RING] = {nullptr, nullptr, nullptr};
   cudaEvent_t ev[GRAD_RING] = {nullptr, nullptr, nullptr};
@@ -45,9 +43,7 @@ extern "C" {
 MULOCO_API void muloco_adamw_destroy(muloco_adamw* o) {
   if (!o) return;
   cudaStreamSynchronize(ctx_view(o->ctx).st);
-  if (o->d_segs) cudaFree(o->d_segs);
-  if (o->d_unit_seg) cudaFree(o->d_unit_seg);
-  if (o->d_default) cudaFree(o->d_default);
+  if (o->d_units) cudaFree(o->d_units);
   if (o->d_grads) cudaFree(o->d_grads);
   for (int i = 0; i < GRAD_RING; ++i) {
     if (o->h_grads[i]) cudaFreeHost(o->h_grads[i]);
@@ -83,37 +79,44 @@ MULOCO_API muloco_status muloco_adamw_create(muloco_ctx* c, const muloco_adamw_c
     if (misaligned(d.theta, 4) || misaligned(d.copy, 2) || misaligned(d.grad, g_align) || misaligned(d.scale1, 4) ||
         misaligned(d.scale2, 4))
       return ctx_fail(c, MULOCO_EINVAL, "tensor %d: a pointer is not aligned to its type", i);
-    units += adamw_units(d.n);
+    units += (d.n + ADAMW_UNIT - 1) / ADAMW_UNIT;
   }
   if (units >= ((int64_t)1 << 31)) return ctx_fail(c, MULOCO_ESHAPE, "too many elements for one list");
 
   muloco_adamw* o = nullptr;
-  std::vector<AdamwSeg> segs;
-  std::vector<int> unit_seg;
-  std::vector<const void*> grads;
+  std::vector<AdamwUnit> table;
   try {
     o = new muloco_adamw();
     o->ctx = c;
     o->cfg = *cfg;
     o->n = n;
-    segs.resize(n);
-    grads.resize(n);
     o->numel.resize(n);
-    unit_seg.reserve((size_t)units);
+    table.resize((size_t)units);
+    size_t at = 0;
+    const size_t g_elt = cfg->grad_dtype == MULOCO_BF16 ? 2 : 4, s_elt = q8 ? 1 : 4;
     for (int i = 0; i < n; ++i) {
       const muloco_adamw_tensor& d = t[i];
-      AdamwSeg& s = segs[i];
-      memset(&s, 0, sizeof s);
-      s.theta = d.theta; s.copy = d.copy; s.s1 = d.state1; s.s2 = d.state2;
-      s.scale1 = d.scale1; s.scale2 = d.scale2;
-      s.n = d.n;
-      s.unit_begin = (int64_t)unit_seg.size();
-      s.dither_base = base;
-      s.wd_mult = d.wd_mult;
-      s.lr_mult = isnan(d.lr_mult) ? 1.f : d.lr_mult;
+      auto off = [](const void* p, size_t bytes) {
+        return p ? const_cast<char*>(reinterpret_cast<const char*>(p)) + bytes : nullptr;
+      };
+      for (int64_t e = 0; e < d.n; e += ADAMW_UNIT) {
+        AdamwUnit& u = table[at++];
+        memset(&u, 0, sizeof u);
+        u.theta = d.theta + e;
+        u.copy = off(d.copy, (size_t)e * 2);
+        u.grad = off(d.grad, (size_t)e * g_elt);
+        u.s1 = off(d.state1, (size_t)e * s_elt);
+        u.s2 = off(d.state2, (size_t)e * s_elt);
+        u.scale1 = q8 ? d.scale1 + e / MULOCO_ADAMW_BLOCK : nullptr;
+        u.scale2 = q8 ? d.scale2 + e / MULOCO_ADAMW_BLOCK : nullptr;
+        u.first = e;
+        u.dither_base = base + e;
+        u.n = (int32_t)(d.n - e < ADAMW_UNIT ? d.n - e : ADAMW_UNIT);
+        u.tensor = i;
+        u.wd_mult = d.wd_mult;
+        u.lr_mult = isnan(d.lr_mult) ? 1.f : d.lr_mult;
+      }
       base += (d.n + MULOCO_ADAMW_BLOCK - 1) / MULOCO_ADAMW_BLOCK * MULOCO_ADAMW_BLOCK;
-      unit_seg.insert(unit_seg.end(), (size_t)adamw_units(d.n), i);
-      grads[i] = d.grad;
       if (d.n > 0 && !d.grad) o->has_default = false;
       o->numel[i] = d.n;
     }
@@ -131,13 +134,9 @@ MULOCO_API muloco_status muloco_adamw_create(muloco_ctx* c, const muloco_adamw_c
   };
   if (units > 0) {
     cudaError_t e;
-    if ((e = cudaMalloc(&o->d_segs, n * sizeof(AdamwSeg))) != cudaSuccess) return bail(e, "tensor table");
-    if ((e = cudaMalloc(&o->d_unit_seg, unit_seg.size() * sizeof(int))) != cudaSuccess) return bail(e, "unit table");
-    if ((e = cudaMalloc(&o->d_default, n * sizeof(void*))) != cudaSuccess) return bail(e, "gradient table");
+    if ((e = cudaMalloc(&o->d_units, table.size() * sizeof(AdamwUnit))) != cudaSuccess) return bail(e, "unit table");
     if ((e = cudaMalloc(&o->d_grads, n * sizeof(void*))) != cudaSuccess) return bail(e, "gradient table");
-    if ((e = cudaMemcpy(o->d_segs, segs.data(), n * sizeof(AdamwSeg), cudaMemcpyHostToDevice)) != cudaSuccess) return bail(e, "tensor table");
-    if ((e = cudaMemcpy(o->d_unit_seg, unit_seg.data(), unit_seg.size() * sizeof(int), cudaMemcpyHostToDevice)) != cudaSuccess) return bail(e, "unit table");
-    if ((e = cudaMemcpy(o->d_default, grads.data(), n * sizeof(void*), cudaMemcpyHostToDevice)) != cudaSuccess) return bail(e, "gradient table");
+    if ((e = cudaMemcpy(o->d_units, table.data(), table.size() * sizeof(AdamwUnit), cudaMemcpyHostToDevice)) != cudaSuccess) return bail(e, "unit table");
     for (int i = 0; i < GRAD_RING; ++i) {
       if ((e = cudaMallocHost((void**)&o->h_grads[i], n * sizeof(void*))) != cudaSuccess) return bail(e, "pinned gradient table");
       if ((e = cudaEventCreateWithFlags(&o->ev[i], cudaEventDisableTiming)) != cudaSuccess) return bail(e, "event");
@@ -160,7 +159,7 @@ MULOCO_API muloco_status muloco_adamw_step(muloco_adamw* o, const void* const* g
       if (misaligned(grads[i], g_align)) return ctx_fail(c, MULOCO_EINVAL, "gradient of tensor %d is not aligned to its type", i);
     }
   if (o->n_units == 0) return MULOCO_OK;
-  const void* const* table = o->d_default;
+  const void* const* table = nullptr;    // the gradients that the units name
   if (grads) {
     // the pinned slot is free again once the copy that used it has run
     const int r = o->next;
@@ -182,8 +181,7 @@ MULOCO_API muloco_status muloco_adamw_step(muloco_adamw* o, const void* const* g
   a.inv_bc1 = (float)(1.0 / bc1);
   a.inv_sqrt_bc2 = (float)(1.0 / sqrt(bc2));
   a.dither = adamw_dither(f.seed, step);
-  launch_adamw_multi(v.st, o->d_segs, o->d_unit_seg, table, o->n, o->n_units, f.state_bits,
-                     f.grad_dtype == MULOCO_BF16, a, v.status);
+  launch_adamw_multi(v.st, o->d_units, table, o->n_units, f.state_bits, f.grad_dtype == MULOCO_BF16, a, v.status);
   OPS_CK(cudaGetLastError());
   ctx_count_launches(c, 1);
   return MULOCO_OK;
@@ -197,7 +195,7 @@ MULOCO_API muloco_status muloco_adamw_moments(muloco_adamw* o, float* m, float* 
   if (!m || !v) return ctx_fail(c, MULOCO_EINVAL, "m or v is NULL");
   if (misaligned(m, 16) || misaligned(v, 16)) return ctx_fail(c, MULOCO_EINVAL, "m and v must be 16-byte aligned");
   const CtxView w = ctx_view(c);
-  launch_adamw_moments(w.st, o->d_segs, o->d_unit_seg, o->n, o->n_units, m, v, w.status);
+  launch_adamw_moments(w.st, o->d_units, o->n_units, m, v);
   OPS_CK(cudaGetLastError());
   ctx_count_launches(c, 1);
   return MULOCO_OK;
