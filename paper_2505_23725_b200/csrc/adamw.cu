@@ -80,13 +80,54 @@ __device__ __forceinline__ void store_copy(void* c, int64_t i, const Four& v, bo
   }
 }
 
-// Byte e of w as a float, exactly: the byte becomes the low mantissa bits of 2^23.
-__device__ __forceinline__ float byte_f32(uint32_t w, int e) {
-  return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440u | (uint32_t)e)) - 8388608.0f;
+// Two float32 operations per instruction, each rounded as its scalar form.
+struct Pair { uint64_t v; };
+__device__ __forceinline__ Pair pair(float a, float b) {
+  Pair r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
 }
-// The low (h = 0) or high half of w as a float, exactly.
-__device__ __forceinline__ float half_f32(uint32_t w, int h) {
-  return __uint_as_float(__byte_perm(w, 0x4B000000u, h ? 0x7432u : 0x7410u)) - 8388608.0f;
+__device__ __forceinline__ Pair both(float a) { return pair(a, a); }
+__device__ __forceinline__ float2 parts(Pair p) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p.v));
+  return r;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+  Pair r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Pair add2(Pair a, Pair b) {
+  Pair r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Pair add2_down(Pair a, Pair b) {
+  Pair r;
+  asm("add.rm.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+  Pair r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+// A product that stays one: mul2 followed by add2 was measured to come out fused (other last bits than mul and add), a
+// fused operation with a zero addend is not fused again.  (-0 becomes +0.)
+__device__ __forceinline__ Pair mul2_alone(Pair a, Pair b) { return fma2(a, b, both(0.f)); }
+// Integers of a few bits as floats, exactly: they become the low mantissa bits of 2^23, which is taken off again.
+__device__ __forceinline__ float byte_bits(uint32_t w, int e) {      // byte e
+  return __uint_as_float(__byte_perm(w, 0x4B000000u, 0x7440u | (uint32_t)e));
+}
+__device__ __forceinline__ float half_bits(uint32_t w, int h) {      // low (h = 0) or high half
+  return __uint_as_float(__byte_perm(w, 0x4B000000u, h ? 0x7432u : 0x7410u));
+}
+constexpr float AW_2P23 = 8388608.0f;
+__device__ __forceinline__ float rcp_fast(float x) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
 }
 // Byte 0 of a, b, c, d as the bytes of a word.
 __device__ __forceinline__ uint32_t pack_bytes(float a, float b, float c, float d) {
@@ -105,7 +146,7 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
   const bool vec_c = FULL || (((uintptr_t)s.copy) & 7) == 0;
   const int i0 = blk * MULOCO_ADAMW_BLOCK + lane * 4;
   const float om1 = 1.0f - a.beta1, om2 = 1.0f - a.beta2;
-  const float lr = a.lr * s.lr_mult, lr_wd = a.lr_wd * (s.lr_mult * s.wd_mult);
+  const float lr = a.lr * a.inv_bc1 * s.lr_mult, lr_wd = a.lr_wd * (s.lr_mult * s.wd_mult);
 
   Four gr[2], th[2];
   uint32_t c1[2], c2[2];
@@ -130,7 +171,7 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
   float sc1 = 0.f, sc2 = 0.f;
   if (BITS == 8) { sc1 = s.scale1[blk]; sc2 = s.scale2[blk]; }
 
-  float finite = 0.f;                           // 0 * g summed: NaN as soon as one gradient is not finite
+  Pair finite = both(0.f);                      // 0 * g summed: NaN as soon as one gradient is not finite
   float max1 = 0.f, max2 = 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -143,33 +184,42 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
       }
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float ge = gr[h].x[e];
-      finite = fmaf(ge, 0.f, finite);
-      float root;
+    for (int e = 0; e < 4; e += 2) {
+      const Pair g2 = pair(gr[h].x[e], gr[h].x[e + 1]);
+      finite = fma2(g2, both(0.f), finite);
+      Pair mn;
+      float2 root;
       if (BITS == 8) {
-        const float mo = __fmul_rn(byte_f32(c1[h], e) - 128.0f, sc1);
-        const float ro = __fmul_rn(byte_f32(c2[h], e), sc2);
-        const float mn = __fadd_rn(__fmul_rn(mo, a.beta1), __fmul_rn(ge, om1));
-        const float vn = __fadd_rn(__fmul_rn(__fmul_rn(ro, ro), a.beta2), __fmul_rn(__fmul_rn(ge, ge), om2));
-        root = __fsqrt_rn(vn);
-        m[h].x[e] = mn;
-        v[h].x[e] = root;                       // the root is what is encoded
-        max1 = fmaxf(max1, fabsf(mn));
-        max2 = fmaxf(max2, root);
+        // products and sums rounded one by one
+        const Pair mo = mul2(add2(pair(byte_bits(c1[h], e), byte_bits(c1[h], e + 1)), both(-(AW_2P23 + 128.0f))), both(sc1));
+        const Pair ro = mul2(add2(pair(byte_bits(c2[h], e), byte_bits(c2[h], e + 1)), both(-AW_2P23)), both(sc2));
+        mn = add2(mul2_alone(mo, both(a.beta1)), mul2_alone(g2, both(om1)));
+        const float2 vn = parts(add2(mul2_alone(mul2(ro, ro), both(a.beta2)), mul2_alone(mul2(g2, g2), both(om2))));
+        root = make_float2(__fsqrt_rn(vn.x), __fsqrt_rn(vn.y));
+        const float2 mp = parts(mn);
+        m[h].x[e] = mp.x; m[h].x[e + 1] = mp.y;
+        v[h].x[e] = root.x; v[h].x[e + 1] = root.y;       // the root is what is encoded
+        max1 = fmaxf(max1, fmaxf(fabsf(mp.x), fabsf(mp.y)));
+        max2 = fmaxf(max2, fmaxf(root.x, root.y));
       } else {
-        m[h].x[e] = fmaf(a.beta1, m[h].x[e], om1 * ge);
-        v[h].x[e] = fmaf(a.beta2, v[h].x[e], om2 * ge * ge);
-        root = sqrtf(v[h].x[e]);
+        mn = fma2(pair(m[h].x[e], m[h].x[e + 1]), both(a.beta1), mul2(g2, both(om1)));
+        const float2 vn = parts(fma2(pair(v[h].x[e], v[h].x[e + 1]), both(a.beta2), mul2(mul2(g2, g2), both(om2))));
+        root = make_float2(sqrtf(vn.x), sqrtf(vn.y));
+        const float2 mp = parts(mn);
+        m[h].x[e] = mp.x; m[h].x[e + 1] = mp.y;
+        v[h].x[e] = vn.x; v[h].x[e + 1] = vn.y;
       }
-      // The quotient to two ulp: an update of about lr, far below theta's own rounding.  (It is zero for denominators
-      // above 2^126, where the true one is too small to change theta.)
-      const float den = fmaf(root, a.inv_sqrt_bc2, a.eps);
-      const float upd = __fdividef(m[h].x[e] * a.inv_bc1, den);
-      th[h].x[e] = th[h].x[e] - fmaf(lr, upd, lr_wd * th[h].x[e]);
+      // The fast reciprocal (one ulp): the update is about lr, far below theta's own rounding.  Its flush to zero does
+      // not matter: a root of a float32 is zero or at least 2^-75.
+      const float2 den = parts(fma2(pair(root.x, root.y), both(a.inv_sqrt_bc2), both(a.eps)));
+      const Pair upd = mul2(mn, pair(rcp_fast(den.x), rcp_fast(den.y)));
+      const Pair t2 = pair(th[h].x[e], th[h].x[e + 1]);
+      const float2 tn = parts(fma2(upd, both(-lr), fma2(t2, both(-lr_wd), t2)));
+      th[h].x[e] = tn.x; th[h].x[e + 1] = tn.y;
     }
   }
-  const bool bad = __any_sync(0xffffffffu, !(finite == 0.f));
+  const float2 fin = parts(finite);
+  const bool bad = __any_sync(0xffffffffu, !(fin.x + fin.y == 0.f));
 
   float inv1 = 0.f, inv2 = 0.f;
   if (BITS == 8) {
@@ -177,12 +227,13 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
     max1 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(max1)));
     max2 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(max2)));
     if (bad) max1 = max2 = __int_as_float(0x7fffffff);      // such a block's moments are NaN from here on
-    inv1 = max1 > AW_TINY ? __fdiv_rn(127.f, max1) : 0.f;
-    inv2 = max2 > AW_TINY ? __fdiv_rn(255.f, max2) : 0.f;
-    if (lane == 0) {
-      s.scale1[blk] = __fmul_rn(max1, 1.0f / 127.0f);
-      s.scale2[blk] = __fmul_rn(max2, 1.0f / 255.0f);
-    }
+    // even lanes deal with the first moment's scale, odd lanes with the second's: one division for both
+    const bool odd = lane & 1;
+    const float mx = odd ? max2 : max1;
+    const float inv = mx > AW_TINY ? __fdiv_rn(odd ? 255.f : 127.f, mx) : 0.f;
+    if (lane < 2) (odd ? s.scale2 : s.scale1)[blk] = __fmul_rn(mx, odd ? 1.0f / 255.0f : 1.0f / 127.0f);
+    inv1 = __shfl_sync(0xffffffffu, inv, 0);
+    inv2 = __shfl_sync(0xffffffffu, inv, 1);
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -190,14 +241,21 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
     if (BITS == 8) {
       float t1[4], t2[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t r = hash32((uint32_t)s.dither_base + a.dither + (uint32_t)(i + e));
+      for (int e = 0; e < 4; e += 2) {
+        const uint32_t r0 = hash32((uint32_t)s.dither_base + a.dither + (uint32_t)(i + e));
+        const uint32_t r1 = hash32((uint32_t)s.dither_base + a.dither + (uint32_t)(i + e + 1));
+        const Pair unit = both(1.52587890625e-5f), off = both(-AW_2P23);
+        const Pair k1 = add2(pair(half_bits(r0, 0), half_bits(r1, 0)), off), k2 = add2(pair(half_bits(r0, 1), half_bits(r1, 1)), off);
         // x * inv rounded, plus u rounded: u = k 2^-16 is exact, so the second step is one fused operation
-        t1[e] = fmaf(half_f32(r, 0), 1.52587890625e-5f, __fmul_rn(m[h].x[e], inv1));
-        t2[e] = fmaf(half_f32(r, 1), 1.52587890625e-5f, __fmul_rn(v[h].x[e], inv2));
-        t1[e] = __fadd_rd(fminf(fmaxf(t1[e], -127.f), 127.f), AW_MAGIC);
+        const float2 a1 = parts(fma2(k1, unit, mul2(pair(m[h].x[e], m[h].x[e + 1]), both(inv1))));
+        const float2 a2 = parts(fma2(k2, unit, mul2(pair(v[h].x[e], v[h].x[e + 1]), both(inv2))));
         // at least 1 wherever v > 0: a root of a float32 is at least 2^-75, times 2^126 saturates to 1
-        t2[e] = __fadd_rd(fminf(fmaxf(t2[e], __saturatef(v[h].x[e] * 8.507059173023462e37f)), 255.f), AW_MAGIC);
+        const float lo0 = __saturatef(v[h].x[e] * 8.507059173023462e37f), lo1 = __saturatef(v[h].x[e + 1] * 8.507059173023462e37f);
+        const Pair magic = both(AW_MAGIC);
+        const float2 b1 = parts(add2_down(pair(fminf(fmaxf(a1.x, -127.f), 127.f), fminf(fmaxf(a1.y, -127.f), 127.f)), magic));
+        const float2 b2 = parts(add2_down(pair(fminf(fmaxf(a2.x, lo0), 255.f), fminf(fmaxf(a2.y, lo1), 255.f)), magic));
+        t1[e] = b1.x; t1[e + 1] = b1.y;
+        t2[e] = b2.x; t2[e + 1] = b2.y;
       }
       *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.s1) + i) = pack_bytes(t1[0], t1[1], t1[2], t1[3]);
       *reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(s.s2) + i) = pack_bytes(t2[0], t2[1], t2[2], t2[3]);
@@ -216,14 +274,14 @@ __global__ void __launch_bounds__(AW_THREADS, 4)
 adamw_multi_kernel(const AdamwUnit* __restrict__ units, const void* const* __restrict__ grads, AdamwStep a,
                    int* __restrict__ status) {
   const AdamwUnit s = units[blockIdx.x];
+  const void* g = s.grad;
+  if (grads) g = reinterpret_cast<const uint8_t*>(grads[s.tensor]) + s.first * (GBF16 ? 2 : 4);
+  const bool aligned =
+      ((((uintptr_t)s.theta) & 15) | (((uintptr_t)s.copy) & 7) | (((uintptr_t)g) & (GBF16 ? 7 : 15))) == 0;
   const int blk = threadIdx.x >> 5;
   if (blk * MULOCO_ADAMW_BLOCK >= s.n) return;
-  const void* g = s.grad;
-  if (grads)
-    g = reinterpret_cast<const uint8_t*>(grads[s.tensor]) + s.first * (GBF16 ? 2 : 4);
-  const bool full = (blk + 1) * MULOCO_ADAMW_BLOCK <= s.n &&
-                    ((((uintptr_t)s.theta) & 15) | (((uintptr_t)s.copy) & 7) | (((uintptr_t)g) & (GBF16 ? 7 : 15))) == 0;
-  const bool bad = full ? adamw_block<BITS, GBF16, true>(s, g, blk, a) : adamw_block<BITS, GBF16, false>(s, g, blk, a);
+  const bool bad = aligned && (blk + 1) * MULOCO_ADAMW_BLOCK <= s.n ? adamw_block<BITS, GBF16, true>(s, g, blk, a)
+                                                                    : adamw_block<BITS, GBF16, false>(s, g, blk, a);
   if (bad && (threadIdx.x & 31) == 0) atomicOr(status, ST_NONFINITE);
 }
 
@@ -246,8 +304,8 @@ adamw_moments_kernel(const AdamwUnit* __restrict__ units, float* __restrict__ m,
     Four om, ov;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      om.x[e] = __fmul_rn(byte_f32(c1[h], e) - 128.0f, sc1);
-      const float r = __fmul_rn(byte_f32(c2[h], e), sc2);
+      om.x[e] = __fmul_rn(byte_bits(c1[h], e) - (AW_2P23 + 128.0f), sc1);
+      const float r = __fmul_rn(byte_bits(c2[h], e) - AW_2P23, sc2);
       ov.x[e] = __fmul_rn(r, r);
     }
     __stcs(reinterpret_cast<float4*>(m + s.dither_base + i), make_float4(om.x[0], om.x[1], om.x[2], om.x[3]));
