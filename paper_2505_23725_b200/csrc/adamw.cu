@@ -11,7 +11,7 @@ namespace muloco {
 
 namespace {
 
-constexpr int AW_THREADS = 256;
+constexpr int AW_THREADS = 128;
 static_assert(ADAMW_UNIT == AW_THREADS / 32 * MULOCO_ADAMW_BLOCK, "one block of elements per warp");
 constexpr float AW_TINY = 1e-36f;       // blocks at or below this magnitude are encoded as zeros
 constexpr float AW_MAGIC = 12582912.0f; // 1.5 * 2^23: adding it leaves the integer part in the low bits
@@ -269,8 +269,11 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
   return bad;
 }
 
+// Blocks of four warps: a block's warps start and end together, and small blocks stagger those that wait for memory against
+// those that compute.  8-bit states at ten blocks per SM (48 registers): 374M elements 992 us, with 256 threads and four per SM
+// 1070; 32-bit states want the registers (505 us for 134M elements, 531 at ten per SM).
 template <int BITS, bool GBF16>
-__global__ void __launch_bounds__(AW_THREADS, 4)
+__global__ void __launch_bounds__(AW_THREADS, BITS == 8 ? 10 : 8)
 adamw_multi_kernel(const AdamwUnit* __restrict__ units, const void* const* __restrict__ grads, AdamwStep a,
                    int* __restrict__ status) {
   const AdamwUnit s = units[blockIdx.x];

@@ -186,7 +186,7 @@ float* ctx_qk_scratch(muloco_ctx* c, int** tickets);
 
 // AdamW over many tensors (include/muloco.h has the layout of the states): one entry per work unit of ADAMW_UNIT
 // consecutive elements of a tensor, with everything a block needs, so that its first load names all the others.
-constexpr int ADAMW_UNIT = 8 * MULOCO_ADAMW_BLOCK;
+constexpr int ADAMW_UNIT = 4 * MULOCO_ADAMW_BLOCK;
 struct alignas(16) AdamwUnit {
   float* theta;          // of the unit's first element, like all pointers here
   void* copy;            // bf16 copy of the parameters, or NULL
@@ -231,14 +231,16 @@ struct QkArgs {
   const int64_t* positions;
   int32_t dim, rot, interleaved;
   float eps;
+  int32_t pad;
   int* status;
   float* partials;       // backward: gain gradients of the thread blocks
   int* tickets;          // backward: one per tensor, zero between launches
 };
 constexpr int QK_MAX_DIM = 512;
-constexpr int QK_MAX_CTAS = 148 * 8;
+constexpr int QK_MAX_CTAS = 148 * 16;
 constexpr size_t QK_SCRATCH_FLOATS = (size_t)QK_MAX_CTAS * QK_MAX_DIM;
-int launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_bf16, int n_sms);   // kernels launched
+// one launch, or none when there is no token or head
+cudaError_t launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_bf16, int n_sms);
 
 // Gated feed-forward block.
 struct FfnArgs {

@@ -294,9 +294,8 @@ MULOCO_API muloco_status muloco_qk_norm_rope(muloco_ctx* c, const muloco_qk_norm
   QkArgs k = qk_args(a, v);
   k.t[0].out = q_out; k.t[0].o_ts = qo_ts; k.t[0].o_hs = qo_hs;
   k.t[1].out = k_out; k.t[1].o_ts = ko_ts; k.t[1].o_hs = ko_hs;
-  const int n = launch_qk_norm(v.st, k, false, a->dtype == MULOCO_BF16, v.n_sms);
-  OPS_CK(cudaGetLastError());
-  ctx_count_launches(c, n);
+  OPS_CK(launch_qk_norm(v.st, k, false, a->dtype == MULOCO_BF16, v.n_sms));
+  ctx_count_launches(c, 1);
   return MULOCO_OK;
 }
 
@@ -324,9 +323,8 @@ MULOCO_API muloco_status muloco_qk_norm_rope_backward(muloco_ctx* c, const muloc
   for (QkTensor& t : k.t) { t.o_hs = a->head_dim; t.o_ts = (int64_t)t.heads * a->head_dim; }
   k.partials = ctx_qk_scratch(c, &k.tickets);
   if (!k.partials) return ctx_fail(c, MULOCO_ENOMEM, "scratch of the gain gradients");
-  const int n = launch_qk_norm(v.st, k, true, a->dtype == MULOCO_BF16, v.n_sms);
-  OPS_CK(cudaGetLastError());
-  ctx_count_launches(c, n);
+  OPS_CK(launch_qk_norm(v.st, k, true, a->dtype == MULOCO_BF16, v.n_sms));
+  ctx_count_launches(c, 1);
   return MULOCO_OK;
 }
 

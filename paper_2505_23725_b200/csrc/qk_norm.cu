@@ -11,59 +11,201 @@
 // so both members of a pair are in one lane and the rotation needs no exchange; a chunk is two vectors of V
 // elements.  32 / G heads of one token fit a warp at a time; the warp keeps the token's cosines and sines in
 // registers while it walks over the token's heads, and the gains while it walks over tokens.
+#include <string.h>
+
+#include <type_traits>
+
 #include "internal.h"
 
 namespace muloco {
 
 namespace {
 
-constexpr int QK_THREADS = 256;
+constexpr int QK_THREADS = 128;
 constexpr int QK_WARPS = QK_THREADS / 32;
 
-template <typename T, int V>
-__device__ __forceinline__ void load_vec(const T* p, float (&f)[V]);
-template <> __device__ __forceinline__ void load_vec<float, 4>(const float* p, float (&f)[4]) {
-  const float4 v = *reinterpret_cast<const float4*>(p);
-  f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+// V float32 values of a lane (V = 1, 4 or 8); products and sums of them two at a time where V allows it.
+template <int V> struct Vec { uint64_t p[V / 2]; };
+template <> struct Vec<1> { float f; };
+
+__device__ __forceinline__ uint64_t join(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
 }
-template <> __device__ __forceinline__ void load_vec<float, 1>(const float* p, float (&f)[1]) { f[0] = *p; }
-template <> __device__ __forceinline__ void load_vec<__nv_bfloat16, 8>(const __nv_bfloat16* p, float (&f)[8]) {
-  const uint4 v = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+__device__ __forceinline__ float2 split2(uint64_t p) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+template <int V> __device__ __forceinline__ Vec<V> mul(const Vec<V>& a, const Vec<V>& b) {
+  Vec<V> r;
+  if constexpr (V == 1) r.f = a.f * b.f;
+  else
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    for (int i = 0; i < V / 2; ++i) r.p[i] = mul2(a.p[i], b.p[i]);
+  return r;
+}
+template <int V> __device__ __forceinline__ Vec<V> mul(const Vec<V>& a, float b) {
+  Vec<V> r;
+  if constexpr (V == 1) r.f = a.f * b;
+  else {
+    const uint64_t bb = join(b, b);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) r.p[i] = mul2(a.p[i], bb);
+  }
+  return r;
+}
+template <int V> __device__ __forceinline__ Vec<V> fma(const Vec<V>& a, const Vec<V>& b, const Vec<V>& c) {
+  Vec<V> r;
+  if constexpr (V == 1) r.f = fmaf(a.f, b.f, c.f);
+  else
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) r.p[i] = fma2(a.p[i], b.p[i], c.p[i]);
+  return r;
+}
+template <int V> __device__ __forceinline__ Vec<V> fma(const Vec<V>& a, float b, const Vec<V>& c) {
+  Vec<V> r;
+  if constexpr (V == 1) r.f = fmaf(a.f, b, c.f);
+  else {
+    const uint64_t bb = join(b, b);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) r.p[i] = fma2(a.p[i], bb, c.p[i]);
+  }
+  return r;
+}
+template <int V> __device__ __forceinline__ Vec<V> of(const float (&f)[V]) {
+  Vec<V> r;
+  if constexpr (V == 1) r.f = f[0];
+  else
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) r.p[i] = join(f[2 * i], f[2 * i + 1]);
+  return r;
+}
+template <int V> __device__ __forceinline__ void to(const Vec<V>& a, float (&f)[V]) {
+  if constexpr (V == 1) f[0] = a.f;
+  else
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      const float2 x = split2(a.p[i]);
+      f[2 * i] = x.x;
+      f[2 * i + 1] = x.y;
+    }
+}
+template <int V> __device__ __forceinline__ Vec<V> filled(float x) {
+  float f[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) f[i] = x;
+  return of<V>(f);
+}
+template <int V> __device__ __forceinline__ Vec<V> from_shared(const float* p) {
+  float f[V];
+  if constexpr (V == 1) f[0] = *p;
+  else
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(p + i);
+      f[i] = x.x; f[i + 1] = x.y; f[i + 2] = x.z; f[i + 3] = x.w;
+    }
+  return of<V>(f);
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+template <int V> __device__ __forceinline__ float sum(const Vec<V>& a) {
+  if constexpr (V == 1) return a.f;
+  else {
+    uint64_t s = a.p[0];
+#pragma unroll
+    for (int i = 1; i < V / 2; ++i) s = add2(s, a.p[i]);
+    const float2 x = split2(s);
+    return x.x + x.y;
   }
 }
-template <> __device__ __forceinline__ void load_vec<__nv_bfloat16, 4>(const __nv_bfloat16* p, float (&f)[4]) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  f[0] = __uint_as_float(v.x << 16); f[1] = __uint_as_float(v.x & 0xFFFF0000u);
-  f[2] = __uint_as_float(v.y << 16); f[3] = __uint_as_float(v.y & 0xFFFF0000u);
+template <int V> __device__ __forceinline__ Vec<V> negated(const Vec<V>& a) {
+  float f[V];
+  to<V>(a, f);
+#pragma unroll
+  for (int i = 0; i < V; ++i) f[i] = -f[i];
+  return of<V>(f);
 }
-template <> __device__ __forceinline__ void load_vec<__nv_bfloat16, 1>(const __nv_bfloat16* p, float (&f)[1]) {
-  f[0] = __bfloat162float(*p);
+// Even and odd entries of the sequence (a, b): what neighbouring pairs are, and back.
+template <int V> __device__ __forceinline__ void pairs_apart(Vec<V>& a, Vec<V>& b) {
+  if constexpr (V > 1) {
+    float f[V], g[V], x[V], y[V];
+    to<V>(a, f); to<V>(b, g);
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      x[i] = 2 * i < V ? f[2 * i] : g[2 * i - V];
+      y[i] = 2 * i < V ? f[2 * i + 1] : g[2 * i + 1 - V];
+    }
+    a = of<V>(x); b = of<V>(y);
+  }
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b) {
-  __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+template <int V> __device__ __forceinline__ void pairs_together(Vec<V>& a, Vec<V>& b) {
+  if constexpr (V > 1) {
+    float f[V], g[V], x[V], y[V];
+    to<V>(a, f); to<V>(b, g);
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      x[2 * i] = f[i]; x[2 * i + 1] = g[i];
+      y[2 * i] = f[V / 2 + i]; y[2 * i + 1] = g[V / 2 + i];
+    }
+    a = of<V>(x); b = of<V>(y);
+  }
+}
+
+// V values as they lie in memory: one access.
+template <typename T, int V> struct Raw;
+template <> struct Raw<float, 4> { float4 v; };
+template <> struct Raw<float, 1> { float v; };
+template <> struct Raw<__nv_bfloat16, 8> { uint4 v; };
+template <> struct Raw<__nv_bfloat16, 4> { uint2 v; };
+template <> struct Raw<__nv_bfloat16, 1> { __nv_bfloat16 v; };
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> raw_zero() {
+  Raw<T, V> r;
+  memset(&r, 0, sizeof r);
+  return r;
+}
+__device__ __forceinline__ uint64_t from_bf16x2(uint32_t w) {
+  return join(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ Vec<4> unpack(const Raw<float, 4>& r) { return Vec<4>{{join(r.v.x, r.v.y), join(r.v.z, r.v.w)}}; }
+__device__ __forceinline__ Vec<1> unpack(const Raw<float, 1>& r) { return Vec<1>{r.v}; }
+__device__ __forceinline__ Vec<8> unpack(const Raw<__nv_bfloat16, 8>& r) {
+  return Vec<8>{{from_bf16x2(r.v.x), from_bf16x2(r.v.y), from_bf16x2(r.v.z), from_bf16x2(r.v.w)}};
+}
+__device__ __forceinline__ Vec<4> unpack(const Raw<__nv_bfloat16, 4>& r) { return Vec<4>{{from_bf16x2(r.v.x), from_bf16x2(r.v.y)}}; }
+__device__ __forceinline__ Vec<1> unpack(const Raw<__nv_bfloat16, 1>& r) { return Vec<1>{__bfloat162float(r.v)}; }
+__device__ __forceinline__ uint32_t to_bf16x2(uint64_t p) {
+  const float2 x = split2(p);
+  __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
   return *reinterpret_cast<uint32_t*>(&h);
 }
-template <typename T, int V>
-__device__ __forceinline__ void store_vec(T* p, const float (&f)[V]);
-template <> __device__ __forceinline__ void store_vec<float, 4>(float* p, const float (&f)[4]) {
-  *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+__device__ __forceinline__ void store(float* p, const Vec<4>& a) {
+  const float2 x = split2(a.p[0]), y = split2(a.p[1]);
+  *reinterpret_cast<float4*>(p) = make_float4(x.x, x.y, y.x, y.y);
 }
-template <> __device__ __forceinline__ void store_vec<float, 1>(float* p, const float (&f)[1]) { *p = f[0]; }
-template <> __device__ __forceinline__ void store_vec<__nv_bfloat16, 8>(__nv_bfloat16* p, const float (&f)[8]) {
-  *reinterpret_cast<uint4*>(p) =
-      make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
+__device__ __forceinline__ void store(float* p, const Vec<1>& a) { *p = a.f; }
+__device__ __forceinline__ void store(__nv_bfloat16* p, const Vec<8>& a) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(to_bf16x2(a.p[0]), to_bf16x2(a.p[1]), to_bf16x2(a.p[2]), to_bf16x2(a.p[3]));
 }
-template <> __device__ __forceinline__ void store_vec<__nv_bfloat16, 4>(__nv_bfloat16* p, const float (&f)[4]) {
-  *reinterpret_cast<uint2*>(p) = make_uint2(pack2(f[0], f[1]), pack2(f[2], f[3]));
+__device__ __forceinline__ void store(__nv_bfloat16* p, const Vec<4>& a) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(to_bf16x2(a.p[0]), to_bf16x2(a.p[1]));
 }
-template <> __device__ __forceinline__ void store_vec<__nv_bfloat16, 1>(__nv_bfloat16* p, const float (&f)[1]) {
-  *p = __float2bfloat16_rn(f[0]);
-}
+__device__ __forceinline__ void store(__nv_bfloat16* p, const Vec<1>& a) { *p = __float2bfloat16_rn(a.f); }
 
 // Elements of the two vectors of the chunk that starts at pair p.
 struct ChunkAt { int a, b; bool rot; };
@@ -75,40 +217,33 @@ __device__ __forceinline__ ChunkAt chunk_at(int p, int half, bool interleaved, i
   return c;
 }
 
-// Turns the V pairs of a chunk by (cos, sign * sin).
-template <int V, bool IL>
-__device__ __forceinline__ void turn(float (&a)[V], float (&b)[V], const float (&c)[V], const float (&s)[V], float sign) {
-  if (!IL) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float y = a[i] * c[i] - sign * b[i] * s[i], z = b[i] * c[i] + sign * a[i] * s[i];
-      a[i] = y; b[i] = z;
-    }
-  } else if (V == 1) {
-    const float y = a[0] * c[0] - sign * b[0] * s[0], z = b[0] * c[0] + sign * a[0] * s[0];
-    a[0] = y; b[0] = z;
-  } else {
-    // the 2 V elements lie in order: pair i is elements 2 i and 2 i + 1 of (a, b)
-#pragma unroll
-    for (int i = 0; i < V / 2; ++i) {
-      const float y = a[2 * i] * c[i] - sign * a[2 * i + 1] * s[i], z = a[2 * i + 1] * c[i] + sign * a[2 * i] * s[i];
-      a[2 * i] = y; a[2 * i + 1] = z;
-    }
-#pragma unroll
-    for (int i = 0; i < V / 2; ++i) {
-      const float y = b[2 * i] * c[V / 2 + i] - sign * b[2 * i + 1] * s[V / 2 + i];
-      const float z = b[2 * i + 1] * c[V / 2 + i] + sign * b[2 * i] * s[V / 2 + i];
-      b[2 * i] = y; b[2 * i + 1] = z;
-    }
-  }
+// Asynchronous copies from global to shared memory (8 or 16 bytes), in groups.
+template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Steps of a warp that are staged in shared memory: the bytes in flight do not take registers.  Two groups of heads a step, three
+// steps (backward two): 16384 tokens, 32 heads of 128, bf16: 47 us forward and 78 backward; with one group and 6 / 5 steps 51 and
+// 81, two groups and 5 / 4 steps 49 and 90 (fewer blocks fit an SM).
+template <typename T, int V, int NC, bool BACK> struct Stage {
+  static constexpr int U = 2;                                     // groups of heads in a step
+  static constexpr int DEPTH = BACK ? 2 : 3;
+  static constexpr int VEC = V * (int)sizeof(T);
+  static constexpr int GROUP = NC * (BACK ? 4 : 2) * 32 * VEC;       // bytes of a group of heads
+  static constexpr int DATA = U * GROUP;
+  static __host__ __device__ constexpr int bytes(int dim) { return DATA + dim * 4; }     // ... and of its token's cosines and sines
+};
 
 // Blocks [0, ctas0) serve the first tensor, the others the second.  A warp takes items in steps of the tensor's warps;
 // an item is one token and, of its heads, every `split`-th group of 32 / G (split > 1 when there are too few
-// tokens to fill the machine).
+// tokens to fill the machine).  A step is U groups of heads.  V > 1: the warp's next steps are on their way into shared memory
+// (and, with a token's first step, its cosines and sines) while it works on the current one.
 template <typename T, int V, int NC, bool IL, bool BACK>
-__global__ void __launch_bounds__(QK_THREADS)
-qk_norm_kernel(const QkArgs p, int ctas0, int G, int split0, int split1) {
+__global__ void __launch_bounds__(QK_THREADS, V == 1 ? 1 : BACK ? 3 : 4)
+qk_norm_kernel(const __grid_constant__ QkArgs p, int ctas0, int G, int split0, int split1) {
   const int which = blockIdx.x < (unsigned)ctas0 ? 0 : 1;
   const QkTensor& t = p.t[which];
   const int cta = which ? blockIdx.x - ctas0 : blockIdx.x;
@@ -118,105 +253,249 @@ qk_norm_kernel(const QkArgs p, int ctas0, int G, int split0, int split1) {
   const int sub = lane / G, gl = lane & (G - 1);
   const int rows = 32 / G;
   const int half = p.rot >> 1, pairs = p.dim >> 1;
+  const int heads = t.heads;
   const float inv_dim = 1.0f / (float)p.dim;
+
+  // the gains, in the order of the pairs' first and second entries per chunk (neighbouring pairs: apart)
+  __shared__ __align__(16) float gains[2][QK_MAX_DIM / 2];
+  for (int i = threadIdx.x; i < pairs; i += QK_THREADS) {
+    const int p0 = i / V * V;
+    const ChunkAt c = chunk_at(p0, half, IL, V);
+    const int e0 = IL ? 2 * i : c.a + (i - p0), e1 = IL ? 2 * i + 1 : c.b + (i - p0);
+    gains[0][i] = t.gain ? t.gain[e0] : 1.f;
+    gains[1][i] = t.gain ? t.gain[e1] : 1.f;
+  }
+  __syncthreads();
 
   bool on[NC];
   ChunkAt at[NC];
-  float ga[NC][V], gb[NC][V];                // gains of this lane's elements
-  float da[NC][V], db[NC][V];                // backward: sums of their gradients
+  Vec<V> da[NC], db[NC];                     // backward: sums of the gains' gradients
+  const float* g0[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const int pr = (gl + c * G) * V;
     on[c] = pr < pairs;
     at[c] = chunk_at(on[c] ? pr : 0, half, IL, V);
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      ga[c][i] = t.gain && on[c] ? t.gain[at[c].a + i] : 1.f;
-      gb[c][i] = t.gain && on[c] ? t.gain[at[c].b + i] : 1.f;
-      da[c][i] = db[c][i] = 0.f;
-    }
+    g0[c] = &gains[0][on[c] ? pr : 0];
+    da[c] = db[c] = filled<V>(0.f);
   }
 
   const int64_t items = p.tokens * split;
-  const int64_t step = (int64_t)ctas * QK_WARPS;
-  for (int64_t it = (int64_t)cta * QK_WARPS + warp; it < items; it += step) {
-    const int64_t tok = it / split;
-    const int first = (int)(it - tok * split);
-    const int64_t pos = p.positions ? p.positions[tok] : tok;
-    const bool pos_ok = half == 0 || (pos >= 0 && pos < p.table_len);
-    float cs[NC][V], sn[NC][V];
+  const int64_t stride = (int64_t)ctas * QK_WARPS;
+  const int64_t it0 = (int64_t)cta * QK_WARPS + warp;
+  auto token_of = [&](int64_t it) { return split == 1 ? it : it / split; };
+  auto first_of = [&](int64_t it) { return split == 1 ? 0 : (int)(it % split) * rows; };
+  const T* const xs = reinterpret_cast<const T*>(t.x);
+  const T* const ys = reinterpret_cast<const T*>(t.dy);
+  T* const os = reinterpret_cast<T*>(t.out);
+
+  // What a token's cosines and sines become for this lane's pairs (first, second entry), with g the gains:
+  //   forward   first' = r (k0 first + k1 second),  second' = r (k2 first + k3 second);  k = g0 c, -g1 s, g0 s, g1 c
+  //   backward  dn = R^T dy:  k0 = c, k1 = s, k2 = -s, k3 = c
+  Vec<V> k0[NC], k1[NC], k2[NC], k3[BACK ? 1 : NC];
+  auto coefficients = [&](int c, const Vec<V>& cs, const Vec<V>& sn) {
+    if (BACK) {
+      k0[c] = cs; k1[c] = sn; k2[c] = negated<V>(sn);
+    } else {
+      const Vec<V> ga = from_shared<V>(g0[c]), gb = from_shared<V>(g0[c] + QK_MAX_DIM / 2);
+      k0[c] = mul<V>(ga, cs); k1[c] = negated<V>(mul<V>(gb, sn));
+      k2[c] = mul<V>(ga, sn); k3[BACK ? 0 : c] = mul<V>(gb, cs);
+    }
+  };
+#pragma unroll
+  for (int c = 0; c < NC; ++c) coefficients(c, filled<V>(1.f), filled<V>(0.f));
+
+  // One group: norm and rotation (or their gradient) of the heads whose elements xa, xb (ya, yb) the lanes hold.
+  auto work = [&](Vec<V> (&xa)[NC], Vec<V> (&xb)[NC], Vec<V> (&ya)[NC], Vec<V> (&yb)[NC], T* out, bool there, bool pos_ok) {
+    Vec<V> sq, ex;
+    Vec<V> ea[NC], eb[NC];                   // gain dn
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) { cs[c][i] = 1.f; sn[c][i] = 0.f; }
-      if (on[c] && at[c].rot) {
-        if (pos_ok) {
-          const int64_t o = pos * half + (gl + c * G) * V;
-#pragma unroll
-          for (int i = 0; i < V; ++i) { cs[c][i] = __ldg(p.cos + o + i); sn[c][i] = __ldg(p.sin + o + i); }
-        }
+      if (IL) pairs_apart<V>(xa[c], xb[c]);
+      sq = c ? fma<V>(xa[c], xa[c], sq) : mul<V>(xa[c], xa[c]);
+      sq = fma<V>(xb[c], xb[c], sq);
+      if (BACK) {
+        if (IL) pairs_apart<V>(ya[c], yb[c]);
+        const Vec<V> a = ya[c], b = yb[c];
+        ya[c] = fma<V>(b, k1[c], mul<V>(a, k0[c]));
+        yb[c] = fma<V>(a, k2[c], mul<V>(b, k0[c]));
+        ea[c] = mul<V>(from_shared<V>(g0[c]), ya[c]);
+        eb[c] = mul<V>(from_shared<V>(g0[c] + QK_MAX_DIM / 2), yb[c]);
+        ex = c ? fma<V>(ea[c], xa[c], ex) : mul<V>(ea[c], xa[c]);
+        ex = fma<V>(eb[c], xb[c], ex);
       }
     }
-    if (!pos_ok && lane == 0) atomicOr(p.status, ST_POSITION);
-    for (int h0 = first * rows; h0 < t.heads; h0 += split * rows) {
-      const int h = h0 + sub;
-      const bool row_ok = h < t.heads;
-      const T* x = reinterpret_cast<const T*>(t.x) + tok * t.x_ts + (int64_t)(row_ok ? h : 0) * t.x_hs;
-      float xa[NC][V], xb[NC][V], ya[NC][V], yb[NC][V];
+    float ss = sum<V>(sq), es = BACK ? sum<V>(ex) : 0.f;
+    for (int o = G >> 1; o > 0; o >>= 1) {
+      ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      if (BACK) es += __shfl_xor_sync(0xffffffffu, es, o);
+    }
+    float r = rsqrtf(fmaf(ss, inv_dim, p.eps));
+    if (!pos_ok) r = __int_as_float(0x7fffffff);
+    const float k = BACK ? -(r * r * es * inv_dim) : 0.f;         // -mean(e x r) r
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
+    for (int c = 0; c < NC; ++c) {
+      if (!(there && on[c])) continue;
+      const Vec<V> ra = mul<V>(xa[c], r), rb = mul<V>(xb[c], r);
+      Vec<V> oa, ob;
+      if (!BACK) {
+        oa = fma<V>(rb, k1[c], mul<V>(ra, k0[c]));
+        ob = fma<V>(rb, k3[BACK ? 0 : c], mul<V>(ra, k2[c]));
+      } else {
+        da[c] = fma<V>(ya[c], ra, da[c]);
+        db[c] = fma<V>(yb[c], rb, db[c]);
+        oa = fma<V>(ra, k, mul<V>(ea[c], r));
+        ob = fma<V>(rb, k, mul<V>(eb[c], r));
+      }
+      if (IL) pairs_together<V>(oa, ob);
+      store(out + at[c].a, oa);
+      store(out + at[c].b, ob);
+    }
+  };
+
+  if constexpr (V > 1) {
+    using St = Stage<T, V, NC, BACK>;
+    constexpr int U = St::U;
+    extern __shared__ __align__(16) uint8_t staged[];
+    const int per = St::bytes(p.dim);
+    uint8_t* const mine = staged + (size_t)warp * St::DEPTH * per;
+    const uint32_t mine_s = (uint32_t)__cvta_generic_to_shared(mine);
+    const int group_step = split * rows, head_step = U * group_step;
+    auto position = [&](int64_t it) -> int64_t {
+      if (it >= items) return 0;
+      const int64_t tok = token_of(it);
+      return p.positions ? p.positions[tok] : tok;
+    };
+    // the step that is fetched next: item, head of this lane, its row of x (and dy), and the position of its
+    // token (read an item ahead)
+    int64_t f_it = it0;
+    int f_h = 0, f_first = 0;
+    const T* f_x = xs;
+    const T* f_y = ys;
+    auto start_item = [&]() {
+      if (f_it >= items) return;
+      const int64_t tok = token_of(f_it);
+      f_first = first_of(f_it) + sub;
+      f_h = f_first;
+      f_x = xs + tok * t.x_ts + (int64_t)f_h * t.x_hs;
+      if (BACK) f_y = ys + tok * t.y_ts + (int64_t)f_h * t.y_hs;
+    };
+    start_item();
+    int64_t f_pos = position(f_it), f_pos_next = position(f_it + stride);
+    int f_slot = 0;
+    auto fetch = [&]() {
+      if (f_it < items) {
+        const uint32_t dst = mine_s + f_slot * per;
+        if (f_h == f_first && half > 0 && f_pos >= 0 && f_pos < p.table_len)
+          for (int i = lane; i < half / 2; i += 32) {       // half cosines, then half sines, four at a time
+            const bool s = i >= half / 4;
+            const int e = (s ? i - half / 4 : i) * 4;
+            copy_async<16>(dst + St::DATA + ((s ? half : 0) + e) * 4, (s ? p.sin : p.cos) + f_pos * half + e);
+          }
 #pragma unroll
-        for (int i = 0; i < V; ++i) xa[c][i] = xb[c][i] = ya[c][i] = yb[c][i] = 0.f;
-        if (row_ok && on[c]) {
-          load_vec<T, V>(x + at[c].a, xa[c]);
-          load_vec<T, V>(x + at[c].b, xb[c]);
+        for (int u = 0; u < U; ++u) {
+          if (f_h < heads)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+              if (on[c]) {
+                const uint32_t d = dst + u * St::GROUP + ((c * (BACK ? 4 : 2)) * 32 + lane) * St::VEC;
+                copy_async<St::VEC>(d, f_x + at[c].a);
+                copy_async<St::VEC>(d + 32 * St::VEC, f_x + at[c].b);
+                if (BACK) {
+                  copy_async<St::VEC>(d + 64 * St::VEC, f_y + at[c].a);
+                  copy_async<St::VEC>(d + 96 * St::VEC, f_y + at[c].b);
+                }
+              }
+          f_h += group_step;
+          f_x += group_step * t.x_hs;
+          if (BACK) f_y += group_step * t.y_hs;
+        }
+        if (f_h - sub >= heads) {
+          f_it += stride;
+          start_item();
+          f_pos = f_pos_next;
+          f_pos_next = position(f_it + stride);
+        }
+      }
+      copy_commit();
+      f_slot = f_slot + 1 == St::DEPTH ? 0 : f_slot + 1;
+    };
+    for (int i = 0; i < St::DEPTH - 1; ++i) fetch();
+    int slot = 0;
+    int64_t pos = position(it0), pos_next = position(it0 + stride);
+    for (int64_t it = it0; it < items; it += stride) {
+      const bool pos_ok = half == 0 || (pos >= 0 && pos < p.table_len);
+      if (!pos_ok && lane == 0) atomicOr(p.status, ST_POSITION);
+      const int first = first_of(it);
+      T* out = os + token_of(it) * t.o_ts + (int64_t)(first + sub) * t.o_hs;
+      for (int h0 = first; h0 < heads; h0 += head_step) {
+        copy_wait<St::DEPTH - 2>();
+        __syncwarp();                          // every lane's copies of this step have landed; the slot before it is free
+        fetch();
+        const uint8_t* src = mine + slot * per;
+        if (h0 == first && pos_ok)
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+            if (on[c] && at[c].rot) {
+              const float* tab = reinterpret_cast<const float*>(src + St::DATA) + (gl + c * G) * V;
+              coefficients(c, from_shared<V>(tab), from_shared<V>(tab + half));
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (u > 0 && h0 + u * group_step >= heads) break;      // the whole warp
+          const bool there = h0 + u * group_step + sub < heads;
+          Vec<V> xa[NC], xb[NC], ya[NC], yb[NC];
+#pragma unroll
+          for (int c = 0; c < NC; ++c) {
+            Raw<T, V> a = raw_zero<T, V>(), b = a, d = a, e = a;
+            if (there && on[c]) {
+              const uint8_t* q = src + u * St::GROUP + ((c * (BACK ? 4 : 2)) * 32 + lane) * St::VEC;
+              a = *reinterpret_cast<const Raw<T, V>*>(q);
+              b = *reinterpret_cast<const Raw<T, V>*>(q + 32 * St::VEC);
+              if (BACK) {
+                d = *reinterpret_cast<const Raw<T, V>*>(q + 64 * St::VEC);
+                e = *reinterpret_cast<const Raw<T, V>*>(q + 96 * St::VEC);
+              }
+            }
+            xa[c] = unpack(a);
+            xb[c] = unpack(b);
+            if (BACK) { ya[c] = unpack(d); yb[c] = unpack(e); }
+          }
+          work(xa, xb, ya, yb, out, there, pos_ok);
+          out += group_step * t.o_hs;
+        }
+        slot = slot + 1 == St::DEPTH ? 0 : slot + 1;
+      }
+      pos = pos_next;
+      pos_next = position(it + 2 * stride);
+    }
+  } else {
+    // elements one by one: odd head sizes, strides and addresses
+    for (int64_t it = it0; it < items; it += stride) {
+      const int64_t tok = token_of(it);
+      const int64_t pos = p.positions ? p.positions[tok] : tok;
+      const bool pos_ok = half == 0 || (pos >= 0 && pos < p.table_len);
+      if (!pos_ok && lane == 0) atomicOr(p.status, ST_POSITION);
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (on[c] && at[c].rot && pos_ok)
+          coefficients(c, Vec<V>{__ldg(p.cos + pos * half + gl + c * G)}, Vec<V>{__ldg(p.sin + pos * half + gl + c * G)});
+      for (int h0 = first_of(it); h0 < heads; h0 += split * rows) {
+        const int h = h0 + sub;
+        const T* x = xs + tok * t.x_ts + (int64_t)h * t.x_hs;
+        const T* y = ys + (BACK ? tok * t.y_ts + (int64_t)h * t.y_hs : 0);
+        Vec<V> xa[NC], xb[NC], ya[NC], yb[NC];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const bool there = h < heads && on[c];
+          xa[c].f = there ? (float)x[at[c].a] : 0.f;
+          xb[c].f = there ? (float)x[at[c].b] : 0.f;
           if (BACK) {
-            const T* y = reinterpret_cast<const T*>(t.dy) + tok * t.y_ts + (int64_t)h * t.y_hs;
-            load_vec<T, V>(y + at[c].a, ya[c]);
-            load_vec<T, V>(y + at[c].b, yb[c]);
+            ya[c].f = there ? (float)y[at[c].a] : 0.f;
+            yb[c].f = there ? (float)y[at[c].b] : 0.f;
           }
         }
-      }
-      float ss = 0.f, es = 0.f;
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (BACK && at[c].rot) turn<V, IL>(ya[c], yb[c], cs[c], sn[c], -1.f);      // dn = R^T dy
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-          ss = fmaf(xa[c][i], xa[c][i], ss);
-          ss = fmaf(xb[c][i], xb[c][i], ss);
-          if (BACK) {
-            es = fmaf(ga[c][i] * ya[c][i], xa[c][i], es);
-            es = fmaf(gb[c][i] * yb[c][i], xb[c][i], es);
-          }
-        }
-      }
-      for (int o = G >> 1; o > 0; o >>= 1) {
-        ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        if (BACK) es += __shfl_xor_sync(0xffffffffu, es, o);
-      }
-      float r = rsqrtf(fmaf(ss, inv_dim, p.eps));
-      if (!pos_ok) r = __int_as_float(0x7fffffff);
-      const float k = BACK ? r * r * es * inv_dim : 0.f;      // mean(e x r) r
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        if (!(row_ok && on[c])) continue;
-        T* out = reinterpret_cast<T*>(t.out) + tok * t.o_ts + (int64_t)h * t.o_hs;
-        if (!BACK) {
-#pragma unroll
-          for (int i = 0; i < V; ++i) { xa[c][i] = xa[c][i] * r * ga[c][i]; xb[c][i] = xb[c][i] * r * gb[c][i]; }
-          if (at[c].rot) turn<V, IL>(xa[c], xb[c], cs[c], sn[c], 1.f);
-        } else {
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            da[c][i] = fmaf(ya[c][i], xa[c][i] * r, da[c][i]);
-            db[c][i] = fmaf(yb[c][i], xb[c][i] * r, db[c][i]);
-            xa[c][i] = r * (ga[c][i] * ya[c][i] - xa[c][i] * k);
-            xb[c][i] = r * (gb[c][i] * yb[c][i] - xb[c][i] * k);
-          }
-        }
-        store_vec<T, V>(out + at[c].a, xa[c]);
-        store_vec<T, V>(out + at[c].b, xb[c]);
+        work(xa, xb, ya, yb, os + tok * t.o_ts + (int64_t)h * t.o_hs, h < heads, pos_ok);
       }
     }
   }
@@ -225,13 +504,20 @@ qk_norm_kernel(const QkArgs p, int ctas0, int G, int split0, int split1) {
     // Sums in a fixed order: the heads side by side in the warp, the warps of the block, then the blocks.
     __shared__ float acc[QK_MAX_DIM];
     __shared__ int last;
+    float fa[NC][V], fb[NC][V];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      if (IL) pairs_together<V>(da[c], db[c]);
+      to<V>(da[c], fa[c]);
+      to<V>(db[c], fb[c]);
+    }
     for (int o = G; o < 32; o <<= 1)
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          da[c][i] += __shfl_xor_sync(0xffffffffu, da[c][i], o);
-          db[c][i] += __shfl_xor_sync(0xffffffffu, db[c][i], o);
+          fa[c][i] += __shfl_xor_sync(0xffffffffu, fa[c][i], o);
+          fb[c][i] += __shfl_xor_sync(0xffffffffu, fb[c][i], o);
         }
     for (int w = 0; w < QK_WARPS; ++w) {
       if (warp == w && sub == 0)
@@ -240,8 +526,8 @@ qk_norm_kernel(const QkArgs p, int ctas0, int G, int split0, int split1) {
           if (on[c])
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-              acc[at[c].a + i] = (w ? acc[at[c].a + i] : 0.f) + da[c][i];
-              acc[at[c].b + i] = (w ? acc[at[c].b + i] : 0.f) + db[c][i];
+              acc[at[c].a + i] = (w ? acc[at[c].a + i] : 0.f) + fa[c][i];
+              acc[at[c].b + i] = (w ? acc[at[c].b + i] : 0.f) + fb[c][i];
             }
       __syncthreads();
     }
@@ -252,32 +538,110 @@ qk_norm_kernel(const QkArgs p, int ctas0, int G, int split0, int split1) {
     if (threadIdx.x == 0) last = atomicAdd(p.tickets + which, 1) == ctas - 1;
     __syncthreads();
     if (last) {
+      // the blocks' sums: W entries per thread, the blocks dealt out to groups of threads, sixteen loads under way
       __threadfence();
       const float* all = p.partials + (size_t)(which ? ctas0 : 0) * p.dim;
-      for (int i = threadIdx.x; i < p.dim; i += QK_THREADS) {
-        float s = 0.f;
-        for (int b = 0; b < ctas; ++b) s += __ldcg(all + (size_t)b * p.dim + i);
-        t.dgain[i] = s;
-      }
+      auto add_up = [&](auto width) {
+        constexpr int W = decltype(width)::value;
+        const int cols = p.dim / W;
+        const int groups = cols < QK_THREADS ? QK_THREADS / cols : 1;
+        for (int c0 = 0; c0 < cols; c0 += QK_THREADS) {
+          const int col = c0 + threadIdx.x % (cols < QK_THREADS ? cols : QK_THREADS);
+          const int g = groups > 1 ? threadIdx.x / cols : 0;
+          float s[W];
+#pragma unroll
+          for (int i = 0; i < W; ++i) s[i] = 0.f;
+          if (col < cols && g < groups) {
+            for (int b0 = g; b0 < ctas; b0 += 16 * groups) {
+              float f[16][W];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                const int b = b0 + j * groups;
+                const float* q = all + (size_t)b * p.dim + col * W;
+                if constexpr (W == 4) {
+                  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                  if (b < ctas) x = __ldcg(reinterpret_cast<const float4*>(q));
+                  f[j][0] = x.x; f[j][1] = x.y; f[j][2] = x.z; f[j][3] = x.w;
+                } else {
+                  f[j][0] = b < ctas ? __ldcg(q) : 0.f;
+                }
+              }
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+#pragma unroll
+                for (int i = 0; i < W; ++i) s[i] += f[j][i];
+            }
+          }
+          for (int k = 0; k < groups; ++k) {
+            __syncthreads();
+            if (col < cols && g == k)
+#pragma unroll
+              for (int i = 0; i < W; ++i) acc[col * W + i] = (k ? acc[col * W + i] : 0.f) + s[i];
+          }
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < p.dim; i += QK_THREADS) t.dgain[i] = acc[i];
+      };
+      if (p.dim % 4 == 0) add_up(std::integral_constant<int, 4>());
+      else add_up(std::integral_constant<int, 1>());
       if (threadIdx.x == 0) p.tickets[which] = 0;      // for the next launch
     }
   }
 }
 
-template <typename T, int V, int NC>
-void launch_v(cudaStream_t st, const QkArgs& a, bool back, int grid, int ctas0, int G, int s0, int s1) {
-  if (a.interleaved) {
-    if (back) qk_norm_kernel<T, V, NC, true, true><<<grid, QK_THREADS, 0, st>>>(a, ctas0, G, s0, s1);
-    else qk_norm_kernel<T, V, NC, true, false><<<grid, QK_THREADS, 0, st>>>(a, ctas0, G, s0, s1);
-  } else {
-    if (back) qk_norm_kernel<T, V, NC, false, true><<<grid, QK_THREADS, 0, st>>>(a, ctas0, G, s0, s1);
-    else qk_norm_kernel<T, V, NC, false, false><<<grid, QK_THREADS, 0, st>>>(a, ctas0, G, s0, s1);
+template <typename T, int V, int NC, bool IL, bool BACK>
+cudaError_t launch_one(cudaStream_t st, const QkArgs& a, int n_sms, int G) {
+  auto kernel = qk_norm_kernel<T, V, NC, IL, BACK>;
+  size_t smem = 0;
+  int resident = BACK ? 8 : 16;              // blocks per SM: V == 1 has nothing staged and wants many
+  if constexpr (V > 1) {
+    using St = Stage<T, V, NC, BACK>;
+    smem = (size_t)QK_WARPS * St::DEPTH * St::bytes(a.dim);
+    // the resident blocks, asked for once per device and size (a second wave of blocks costs a third of the rate)
+    static int seen_dev = -1, seen_blocks = 0;
+    static size_t seen_smem = 0;
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && (seen_dev != dev || seen_smem != smem)) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                               (int)(QK_WARPS * St::DEPTH * St::bytes(QK_MAX_DIM)));
+      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&seen_blocks, kernel, QK_THREADS, smem);
+      if (e == cudaSuccess && seen_blocks < 1) e = cudaErrorLaunchOutOfResources;
+      if (e == cudaSuccess) { seen_dev = dev; seen_smem = smem; }
+    }
+    if (e != cudaSuccess) return e;
+    resident = seen_blocks;
   }
+  // The blocks are shared out by head counts; a token's heads go to several warps when there are fewer tokens than warps.
+  const int rows = 32 / G;
+  const int64_t heads = (int64_t)a.t[0].heads + a.t[1].heads;
+  const int64_t most = (int64_t)n_sms * resident < QK_MAX_CTAS - 1 ? (int64_t)n_sms * resident : QK_MAX_CTAS - 1;
+  int ctas[2] = {0, 0}, split[2] = {1, 1};
+  for (int w = 0; w < 2; ++w) {
+    if (!a.t[w].heads) continue;
+    const int groups = (a.t[w].heads + rows - 1) / rows;
+    int64_t share = w && ctas[0] ? most - most * a.t[0].heads / heads : most * a.t[w].heads / heads;
+    if (share < 1) share = 1;
+    while (split[w] < groups && a.tokens * split[w] < share * QK_WARPS) split[w] *= 2;
+    if (split[w] > groups) split[w] = groups;
+    const int64_t need = (a.tokens * split[w] + QK_WARPS - 1) / QK_WARPS;
+    ctas[w] = (int)(need < share ? need : share);
+  }
+  kernel<<<ctas[0] + ctas[1], QK_THREADS, smem, st>>>(a, ctas[0], G, split[0], split[1]);
+  return cudaGetLastError();
+}
+
+template <typename T, int V, int NC>
+cudaError_t launch_v(cudaStream_t st, const QkArgs& a, bool back, int n_sms, int G) {
+  if (a.interleaved)
+    return back ? launch_one<T, V, NC, true, true>(st, a, n_sms, G) : launch_one<T, V, NC, true, false>(st, a, n_sms, G);
+  return back ? launch_one<T, V, NC, false, true>(st, a, n_sms, G) : launch_one<T, V, NC, false, false>(st, a, n_sms, G);
 }
 
 // Whether every vector of V elements of `elt` bytes that the kernel touches is aligned.
 bool aligned(const QkArgs& a, bool back, int V, int elt) {
   if (a.dim % (2 * V) != 0 || a.rot % (2 * V) != 0) return false;
+  if (V > 1 && (a.rot % 8 != 0 || (((uintptr_t)a.cos | (uintptr_t)a.sin) & 15) != 0)) return false;   // table rows by 16 bytes
   for (const QkTensor& t : a.t) {
     if (!t.heads) continue;
     uintptr_t p = (uintptr_t)t.x | (uintptr_t)t.out;
@@ -290,33 +654,17 @@ bool aligned(const QkArgs& a, bool back, int V, int elt) {
 
 }  // namespace
 
-int launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_bf16, int n_sms) {
+cudaError_t launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_bf16, int n_sms) {
   const int64_t heads = (int64_t)a.t[0].heads + a.t[1].heads;
-  if (a.tokens <= 0 || heads <= 0) return 0;
+  if (a.tokens <= 0 || heads <= 0) return cudaSuccess;
   int V = 1;
-  if (is_bf16) V = aligned(a, back, 8, 2) ? 8 : aligned(a, back, 4, 2) ? 4 : 1;
+    if (is_bf16) V = aligned(a, back, 8, 2) ? 8 : aligned(a, back, 4, 2) ? 4 : 1;
   else V = aligned(a, back, 4, 4) ? 4 : 1;
   const int chunks = (a.dim / 2 + V - 1) / V;
   int G = 1;
   while (G < 32 && G < chunks) G <<= 1;
   const int NC = (chunks + G - 1) / G;
-  const int rows = 32 / G;
-  // Backward keeps one block's worth of gain sums per resident block: few blocks, many tokens each.
-  const int most = n_sms * (back ? 2 : 8) < QK_MAX_CTAS ? n_sms * (back ? 2 : 8) : QK_MAX_CTAS;
-  int ctas[2] = {0, 0}, split[2] = {1, 1};
-  for (int w = 0; w < 2; ++w) {
-    if (!a.t[w].heads) continue;
-    const int groups = (a.t[w].heads + rows - 1) / rows;
-    const int64_t share = most * (int64_t)a.t[w].heads / heads > 0 ? most * (int64_t)a.t[w].heads / heads : 1;
-    const int64_t warps = share * QK_WARPS;
-    // a token's heads go to several warps when there are fewer tokens than warps
-    while (split[w] < groups && a.tokens * split[w] < warps) split[w] *= 2;
-    if (split[w] > groups) split[w] = groups;
-    const int64_t need = (a.tokens * split[w] + QK_WARPS - 1) / QK_WARPS;
-    ctas[w] = (int)(need < share ? need : share);
-  }
-  const int grid = ctas[0] + ctas[1];
-#define QK_CASE(T, VV, N) launch_v<T, VV, N>(st, a, back, grid, ctas[0], G, split[0], split[1])
+#define QK_CASE(T, VV, N) return launch_v<T, VV, N>(st, a, back, n_sms, G)
   if (is_bf16) {
     if (V == 8) QK_CASE(__nv_bfloat16, 8, 1);
     else if (V == 4) { if (NC == 1) QK_CASE(__nv_bfloat16, 4, 1); else QK_CASE(__nv_bfloat16, 4, 2); }
@@ -328,7 +676,6 @@ int launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_bf16, int
     else QK_CASE(float, 1, 8);
   }
 #undef QK_CASE
-  return 1;
 }
 
 }  // namespace muloco
