@@ -313,7 +313,7 @@ class _Operators:
             raise ValueError(f"{name} must have shape {tuple(shape)} (got {tuple(t.shape)})")
         if dense and not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
+        if t.shape[-1] > 1 and t.stride(-1) != 1 and t.numel():
             raise ValueError(f"{name}: the entries of its last dimension must be consecutive")
 
     # -- norm of queries and keys with the rotation -----------------------------------------------
