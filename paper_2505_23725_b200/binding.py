@@ -112,6 +112,16 @@ class MulocoError(RuntimeError):
 _lib = None
 
 
+def _load_fastcall():
+    """The compiled call path of the operators (build.build_fastcall), or None where it was not built: the methods then
+    marshal their arguments in Python, in front of the same library."""
+    try:
+        from . import _fastcall
+        return _fastcall
+    except ImportError:
+        return None
+
+
 def load_library():
     """Load libmuloco.so from the package directory; raises if it is missing."""
     global _lib
@@ -289,6 +299,22 @@ class _Operators:
         self._bf16, self._f32, self._i64 = torch.bfloat16, torch.float32, torch.int64
         self._raw_stream = torch._C._cuda_getCurrentRawStream
         self._handle = self.stream.cuda_stream
+        fast = _load_fastcall()
+        self._fast = {}
+        if fast is not None:
+            for name in ("qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward"):
+                self._fast[name] = (getattr(fast, name), C.cast(getattr(self.lib, "muloco_" + name), C.c_void_p).value)
+
+    def _quick(self, name, *args):
+        """The compiled form of a call: its results, or None when this one has to go the long way (an argument is not as
+        it should be, or the caller is on another stream)."""
+        f = self._fast.get(name)
+        if f is None:
+            return None
+        r = f[0](self.ctx.value, f[1], self._dev, self._handle, *args)
+        if r.__class__ is int:
+            self._check(r)
+        return r
 
     def _other_stream(self):
         """The caller's current stream when it is not the context's, else None."""
@@ -383,6 +409,10 @@ class _Operators:
         None).  cos and sin: float32 tables [length, rotary_dim / 2]; positions: int64 [tokens] or None
         for 0, 1, ...  Returns (q_out, k_out), new tensors in the inputs' order of dimensions unless
         `out` = (q_out, k_out) gives them."""
+        if out is None:
+            r = self._quick("qk_norm_rope", q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
+            if r is not None:
+                return r
         empty_like = self.torch.empty_like
         a = self._qk(q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
         if out is None:
@@ -415,6 +445,9 @@ class _Operators:
     def qk_norm_rope_backward(self, dq_out, dk_out, q, k, cos, sin, positions=None, gain_q=None, gain_k=None,
                               eps=1e-6, interleaved=False):
         """muloco_qk_norm_rope_backward: from the gradients of the results, (dq, dk, dgain_q, dgain_k)."""
+        r = self._quick("qk_norm_rope_backward", dq_out, dk_out, q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
+        if r is not None:
+            return r
         a = self._qk(q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
         dev = self._dev
         for name, y, t in (("dq_out", dq_out, q), ("dk_out", dk_out, k)):
@@ -477,6 +510,9 @@ class _Operators:
     def gated_ffn(self, x, w1, w3, w2, activation="silu", save=True):
         """muloco_gated_ffn: y = (act(x w1) * (x w3)) w2, all bf16.  Returns (y, saved): saved = (g, u, h) is what
         the backward pass needs (None with save=False, and g and u are then not written)."""
+        r = self._quick("gated_ffn", x, w1, w3, w2, ACTIVATIONS.get(activation, -1), save)
+        if r is not None:
+            return r
         a, T, d, F = self._ffn(x, w1, w3, w2, activation)
         y, h = x.new_empty((T, d)), x.new_empty((T, F))
         g = u = None
@@ -496,10 +532,13 @@ class _Operators:
 
     def gated_ffn_backward(self, dy, x, w1, w3, w2, saved, activation="silu"):
         """muloco_gated_ffn_backward: (dx, dw1, dw3, dw2), bf16, from dy and the forward pass's saved = (g, u, h)."""
+        g, u, h = saved
+        r = self._quick("gated_ffn_backward", dy, x, w1, w3, w2, ACTIVATIONS.get(activation, -1), g, u, h)
+        if r is not None:
+            return r
         bf16 = self.torch.bfloat16
         a, T, d, F = self._ffn(x, w1, w3, w2, activation)
         self._need("dy", dy, bf16, (T, d))
-        g, u, h = saved
         for name, t in (("g", g), ("u", u), ("h", h)):
             self._need(name, t, bf16, (T, F), dense=True)
         dg, du = x.new_empty((T, F)), x.new_empty((T, F))
@@ -654,8 +693,7 @@ class AdamW:
         32-bit states themselves.  Padding entries are zero."""
         if self.state_bits == 32:
             return self.state1, self.state2
-        torch = self.owner.torch
-        m, v = (torch.empty(self.padded, dtype=torch.float32, device=self.owner.device) for _ in range(2))
+        m, v = self.scale1.new_empty(self.padded), self.scale1.new_empty(self.padded)
         cur = self.owner._other_stream()
         if cur is not None:
             self.owner._enter(cur, (m, v))

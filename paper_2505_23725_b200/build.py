@@ -25,7 +25,7 @@ def needs_build(lib_path: str = LIB) -> bool:
     if not os.path.exists(lib_path):
         return True
     t = os.path.getmtime(lib_path)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
+    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh", ".h"))]
     deps.append(os.path.join(os.path.dirname(HERE), "include", "muloco.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
@@ -36,6 +36,8 @@ def build_library(force: bool = False, verbose: bool = False, lib_path: str = No
     kernels' index checks compiled in (a failed check raises a status flag, nothing traps)."""
     if lib_path is None:
         lib_path = LIB_DEBUG if debug else LIB
+    if lib_path == LIB:
+        build_fastcall()
     if not force and lib_path in (LIB, LIB_DEBUG) and not needs_build(lib_path):
         return lib_path
     objs = []
@@ -65,5 +67,33 @@ def build_library(force: bool = False, verbose: bool = False, lib_path: str = No
     return lib_path
 
 
+FASTCALL = os.path.join(HERE, "_fastcall.so")
+
+
+def build_fastcall(force: bool = False) -> str:
+    """Compile the operators' call path (csrc/fastcall.cpp: a CPython module over torch's C++ interface, host code
+    only) next to the library."""
+    src = os.path.join(CSRC, "fastcall.cpp")
+    deps = [src, os.path.join(os.path.dirname(HERE), "include", "muloco.h")]
+    if not force and os.path.exists(FASTCALL) and all(os.path.getmtime(FASTCALL) >= os.path.getmtime(d) for d in deps):
+        return FASTCALL
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
+    lib = os.path.join(root, "lib")
+    cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", os.path.join(root, "include"), "-isystem", cuda, "-isystem", sysconfig.get_paths()["include"],
+           src, "-o", FASTCALL, "-L" + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath," + lib]
+    p = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if p.returncode != 0:
+        sys.stderr.write(p.stdout)
+        raise RuntimeError("g++ failed on fastcall.cpp")
+    return FASTCALL
+
+
 if __name__ == "__main__":
     print(build_library(force=True, verbose="-v" in sys.argv))
+    print(build_fastcall(force=True))

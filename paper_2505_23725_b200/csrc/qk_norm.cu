@@ -24,7 +24,7 @@ namespace {
 constexpr int QK_THREADS = 128;
 constexpr int QK_WARPS = QK_THREADS / 32;
 
-// V float32 values of a lane (V = 1, 4 or 8); products and sums of them two at a time where V allows it.
+// V float32 values of a lane (V = 1, 2, 4 or 8); products and sums of them two at a time where V allows it.
 template <int V> struct Vec { uint64_t p[V / 2]; };
 template <> struct Vec<1> { float f; };
 
@@ -111,7 +111,10 @@ template <int V> __device__ __forceinline__ Vec<V> filled(float x) {
 template <int V> __device__ __forceinline__ Vec<V> from_shared(const float* p) {
   float f[V];
   if constexpr (V == 1) f[0] = *p;
-  else
+  else if constexpr (V == 2) {
+    const float2 x = *reinterpret_cast<const float2*>(p);
+    f[0] = x.x; f[1] = x.y;
+  } else
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
       const float4 x = *reinterpret_cast<const float4*>(p + i);
@@ -170,9 +173,11 @@ template <int V> __device__ __forceinline__ void pairs_together(Vec<V>& a, Vec<V
 // V values as they lie in memory: one access.
 template <typename T, int V> struct Raw;
 template <> struct Raw<float, 4> { float4 v; };
+template <> struct Raw<float, 2> { float2 v; };
 template <> struct Raw<float, 1> { float v; };
 template <> struct Raw<__nv_bfloat16, 8> { uint4 v; };
 template <> struct Raw<__nv_bfloat16, 4> { uint2 v; };
+template <> struct Raw<__nv_bfloat16, 2> { uint32_t v; };
 template <> struct Raw<__nv_bfloat16, 1> { __nv_bfloat16 v; };
 template <typename T, int V> __device__ __forceinline__ Raw<T, V> raw_zero() {
   Raw<T, V> r;
@@ -183,6 +188,8 @@ __device__ __forceinline__ uint64_t from_bf16x2(uint32_t w) {
   return join(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
 }
 __device__ __forceinline__ Vec<4> unpack(const Raw<float, 4>& r) { return Vec<4>{{join(r.v.x, r.v.y), join(r.v.z, r.v.w)}}; }
+__device__ __forceinline__ Vec<2> unpack(const Raw<float, 2>& r) { return Vec<2>{{join(r.v.x, r.v.y)}}; }
+__device__ __forceinline__ Vec<2> unpack(const Raw<__nv_bfloat16, 2>& r) { return Vec<2>{{from_bf16x2(r.v)}}; }
 __device__ __forceinline__ Vec<1> unpack(const Raw<float, 1>& r) { return Vec<1>{r.v}; }
 __device__ __forceinline__ Vec<8> unpack(const Raw<__nv_bfloat16, 8>& r) {
   return Vec<8>{{from_bf16x2(r.v.x), from_bf16x2(r.v.y), from_bf16x2(r.v.z), from_bf16x2(r.v.w)}};
@@ -198,6 +205,7 @@ __device__ __forceinline__ void store(float* p, const Vec<4>& a) {
   const float2 x = split2(a.p[0]), y = split2(a.p[1]);
   *reinterpret_cast<float4*>(p) = make_float4(x.x, x.y, y.x, y.y);
 }
+__device__ __forceinline__ void store(float* p, const Vec<2>& a) { *reinterpret_cast<float2*>(p) = split2(a.p[0]); }
 __device__ __forceinline__ void store(float* p, const Vec<1>& a) { *p = a.f; }
 __device__ __forceinline__ void store(__nv_bfloat16* p, const Vec<8>& a) {
   *reinterpret_cast<uint4*>(p) = make_uint4(to_bf16x2(a.p[0]), to_bf16x2(a.p[1]), to_bf16x2(a.p[2]), to_bf16x2(a.p[3]));
@@ -205,6 +213,7 @@ __device__ __forceinline__ void store(__nv_bfloat16* p, const Vec<8>& a) {
 __device__ __forceinline__ void store(__nv_bfloat16* p, const Vec<4>& a) {
   *reinterpret_cast<uint2*>(p) = make_uint2(to_bf16x2(a.p[0]), to_bf16x2(a.p[1]));
 }
+__device__ __forceinline__ void store(__nv_bfloat16* p, const Vec<2>& a) { *reinterpret_cast<uint32_t*>(p) = to_bf16x2(a.p[0]); }
 __device__ __forceinline__ void store(__nv_bfloat16* p, const Vec<1>& a) { *p = __float2bfloat16_rn(a.f); }
 
 // Elements of the two vectors of the chunk that starts at pair p.
@@ -217,7 +226,7 @@ __device__ __forceinline__ ChunkAt chunk_at(int p, int half, bool interleaved, i
   return c;
 }
 
-// Asynchronous copies from global to shared memory (8 or 16 bytes), in groups.
+// Asynchronous copies from global to shared memory (4, 8 or 16 bytes), in groups.
 template <int BYTES> __device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
   if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
@@ -229,6 +238,7 @@ template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.
 // steps (backward two): 16384 tokens, 32 heads of 128, bf16: 47 us forward and 78 backward; with one group and 6 / 5 steps 51 and
 // 81, two groups and 5 / 4 steps 49 and 90 (fewer blocks fit an SM).
 template <typename T, int V, int NC, bool BACK> struct Stage {
+  static constexpr int TABLE = V == 2 ? 2 : 4;                       // table entries per copy
   static constexpr int U = 2;                                     // groups of heads in a step
   static constexpr int DEPTH = BACK ? 2 : 3;
   static constexpr int VEC = V * (int)sizeof(T);
@@ -387,10 +397,10 @@ qk_norm_kernel(const __grid_constant__ QkArgs p, int ctas0, int G, int split0, i
       if (f_it < items) {
         const uint32_t dst = mine_s + f_slot * per;
         if (f_h == f_first && half > 0 && f_pos >= 0 && f_pos < p.table_len)
-          for (int i = lane; i < half / 2; i += 32) {       // half cosines, then half sines, four at a time
-            const bool s = i >= half / 4;
-            const int e = (s ? i - half / 4 : i) * 4;
-            copy_async<16>(dst + St::DATA + ((s ? half : 0) + e) * 4, (s ? p.sin : p.cos) + f_pos * half + e);
+          for (int i = lane; i < 2 * half / St::TABLE; i += 32) {       // half cosines, then half sines
+            const bool s = i >= half / St::TABLE;
+            const int e = (s ? i - half / St::TABLE : i) * St::TABLE;
+            copy_async<4 * St::TABLE>(dst + St::DATA + ((s ? half : 0) + e) * 4, (s ? p.sin : p.cos) + f_pos * half + e);
           }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -641,7 +651,8 @@ cudaError_t launch_v(cudaStream_t st, const QkArgs& a, bool back, int n_sms, int
 // Whether every vector of V elements of `elt` bytes that the kernel touches is aligned.
 bool aligned(const QkArgs& a, bool back, int V, int elt) {
   if (a.dim % (2 * V) != 0 || a.rot % (2 * V) != 0) return false;
-  if (V > 1 && (a.rot % 8 != 0 || (((uintptr_t)a.cos | (uintptr_t)a.sin) & 15) != 0)) return false;   // table rows by 16 bytes
+  const int table = V == 2 ? 2 : 4;                                  // entries of a table row per copy
+  if (a.rot % (2 * table) != 0 || (((uintptr_t)a.cos | (uintptr_t)a.sin) & (4 * table - 1)) != 0) return false;
   for (const QkTensor& t : a.t) {
     if (!t.heads) continue;
     uintptr_t p = (uintptr_t)t.x | (uintptr_t)t.out;
@@ -658,8 +669,8 @@ cudaError_t launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_b
   const int64_t heads = (int64_t)a.t[0].heads + a.t[1].heads;
   if (a.tokens <= 0 || heads <= 0) return cudaSuccess;
   int V = 1;
-    if (is_bf16) V = aligned(a, back, 8, 2) ? 8 : aligned(a, back, 4, 2) ? 4 : 1;
-  else V = aligned(a, back, 4, 4) ? 4 : 1;
+  if (is_bf16) V = aligned(a, back, 8, 2) ? 8 : aligned(a, back, 4, 2) ? 4 : aligned(a, back, 2, 2) ? 2 : 1;
+  else V = aligned(a, back, 4, 4) ? 4 : aligned(a, back, 2, 4) ? 2 : 1;
   const int chunks = (a.dim / 2 + V - 1) / V;
   int G = 1;
   while (G < 32 && G < chunks) G <<= 1;
@@ -668,10 +679,12 @@ cudaError_t launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_b
   if (is_bf16) {
     if (V == 8) QK_CASE(__nv_bfloat16, 8, 1);
     else if (V == 4) { if (NC == 1) QK_CASE(__nv_bfloat16, 4, 1); else QK_CASE(__nv_bfloat16, 4, 2); }
+    else if (V == 2) { if (NC == 1) QK_CASE(__nv_bfloat16, 2, 1); else if (NC == 2) QK_CASE(__nv_bfloat16, 2, 2); else QK_CASE(__nv_bfloat16, 2, 4); }
     else if (NC <= 2) QK_CASE(__nv_bfloat16, 1, 2);
     else QK_CASE(__nv_bfloat16, 1, 8);
   } else {
     if (V == 4) { if (NC == 1) QK_CASE(float, 4, 1); else QK_CASE(float, 4, 2); }
+    else if (V == 2) { if (NC == 1) QK_CASE(float, 2, 1); else if (NC == 2) QK_CASE(float, 2, 2); else QK_CASE(float, 2, 4); }
     else if (NC <= 2) QK_CASE(float, 1, 2);
     else QK_CASE(float, 1, 8);
   }

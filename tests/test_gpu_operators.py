@@ -231,7 +231,8 @@ QK_CASES = [
     (1, 12, 12, 64, 64, False), (1, 3, 1, 128, 128, True), (5, 16, 4, 128, 64, False), (67, 5, 5, 80, 80, False),
     (33, 7, 2, 96, 32, True), (130, 2, 9, 256, 256, False), (19, 1, 1, 512, 512, False), (40, 6, 3, 90, 90, False),
     (40, 6, 3, 90, 44, True), (9, 4, 4, 2, 2, False), (300, 12, 3, 64, 0, False), (2000, 3, 2, 32, 32, True),
-    (31, 0, 4, 64, 64, False), (31, 4, 0, 510, 510, True),
+    (31, 0, 4, 64, 64, False), (31, 4, 0, 510, 510, True), (45, 5, 3, 236, 236, False), (45, 5, 3, 100, 52, True),
+    (600, 3, 2, 508, 508, False), (77, 9, 4, 36, 12, False),
 ]
 
 
@@ -537,6 +538,39 @@ def test_gated_ffn_refusals(ctx):
     with pytest.raises(binding.MulocoError) as e:
         ctx.gated_ffn(torch.zeros(4, 72, dtype=torch.bfloat16, device="cuda")[:, 4:68], w1, w3, w2)
     assert e.value.status == binding.EINVAL
+
+
+# ------------------------------------------------------------------------------------------------
+# the two ways of a call
+# ------------------------------------------------------------------------------------------------
+def test_compiled_and_python_call_paths_agree(ctx):
+    """A call marshalled by the compiled module and one marshalled in Python give the same tensors; the suite runs with
+    the compiled one (it has to be there), and what it does not take goes the other way."""
+    import torch
+    from paper_2505_23725_b200 import binding
+    plain = binding.Context("cuda:0")
+    plain._fast = {}
+    assert set(ctx._fast) == {"qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward"}
+    q, k, cos, sin, pos, gq, gk, dqo, dko = _qk_inputs((37, 6, 2, 64, 32, False), torch.bfloat16, layout="wide")
+    for args in ((q, k, cos, sin, pos, gq, gk, 1e-5, True), (q, None, cos, sin), (None, k, cos, sin, pos, None, gk)):
+        assert ctx._quick("qk_norm_rope", *(args + (None,) * (7 - len(args)) + (1e-6, False) if len(args) < 9 else args)) is not None
+        for a, b in zip(ctx.qk_norm_rope(*args), plain.qk_norm_rope(*args)):
+            assert (a is None and b is None) or (torch.equal(a, b) and a.stride() == b.stride())
+        dy = (dqo if args[0] is not None else None, dko if args[1] is not None else None)
+        for a, b in zip(ctx.qk_norm_rope_backward(*dy, *args), plain.qk_norm_rope_backward(*dy, *args)):
+            assert (a is None and b is None) or torch.equal(a, b)
+    x, w1, w3, w2, dy = _ffn_inputs(21, 72, 136)
+    y, saved = ctx.gated_ffn(x, w1, w3, w2, "gelu")
+    y2, saved2 = plain.gated_ffn(x, w1, w3, w2, "gelu")
+    assert torch.equal(y, y2) and all(torch.equal(a, b) for a, b in zip(saved, saved2))
+    for a, b in zip(ctx.gated_ffn_backward(dy, x, w1, w3, w2, saved, "gelu"), plain.gated_ffn_backward(dy, x, w1, w3, w2, saved, "gelu")):
+        assert torch.equal(a, b)
+    assert ctx._quick("gated_ffn", x.float(), w1, w3, w2, 0, True) is None
+    with torch.cuda.stream(torch.cuda.Stream()):
+        assert ctx._quick("gated_ffn", x, w1, w3, w2, 0, True) is None
+    ctx.sync_status()
+    plain.sync_status()
+    plain.close()
 
 
 # ------------------------------------------------------------------------------------------------
