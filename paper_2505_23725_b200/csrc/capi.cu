@@ -510,13 +510,13 @@ void ctx_count_launches(muloco_ctx* c, int n) { c->launches += n; }
 
 float* ctx_qk_scratch(muloco_ctx* c, int** tickets) {
   if (!c->qk_scratch) {
-    const size_t bytes = QK_SCRATCH_FLOATS * sizeof(float) + 256;
+    const size_t bytes = QK_SCRATCH_FLOATS * sizeof(float) + QK_TICKETS * sizeof(int);
     if (cudaMalloc(&c->qk_scratch, bytes) != cudaSuccess) {
       c->qk_scratch = nullptr;
       cudaGetLastError();
       return nullptr;
     }
-    if (cudaMemsetAsync(c->qk_scratch + QK_SCRATCH_FLOATS, 0, 256, c->st) != cudaSuccess) return nullptr;
+    if (cudaMemsetAsync(c->qk_scratch + QK_SCRATCH_FLOATS, 0, QK_TICKETS * sizeof(int), c->st) != cudaSuccess) return nullptr;
   }
   *tickets = reinterpret_cast<int*>(c->qk_scratch + QK_SCRATCH_FLOATS);
   return c->qk_scratch;

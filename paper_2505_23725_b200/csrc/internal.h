@@ -234,11 +234,14 @@ struct QkArgs {
   int32_t pad;
   int* status;
   float* partials;       // backward: gain gradients of the thread blocks
-  int* tickets;          // backward: one per tensor, zero between launches
+  int* tickets;          // backward: QK_TICKETS of them, zero between launches
 };
 constexpr int QK_MAX_DIM = 512;
 constexpr int QK_MAX_CTAS = 148 * 16;
-constexpr size_t QK_SCRATCH_FLOATS = (size_t)QK_MAX_CTAS * QK_MAX_DIM;
+constexpr int QK_JOIN = 16;                      // thread blocks whose gain sums are joined at a time
+constexpr size_t QK_SCRATCH_FLOATS = (size_t)(QK_MAX_CTAS + 2 * (QK_MAX_CTAS / QK_JOIN)) * QK_MAX_DIM;
+constexpr size_t QK_TICKETS = 2 * (QK_MAX_CTAS / QK_JOIN + 1);
+static_assert(QK_MAX_CTAS % QK_JOIN == 0, "whole groups of blocks");
 // one launch, or none when there is no token or head
 cudaError_t launch_qk_norm(cudaStream_t st, const QkArgs& a, bool back, int is_bf16, int n_sms);
 

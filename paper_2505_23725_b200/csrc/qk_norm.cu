@@ -541,61 +541,80 @@ qk_norm_kernel(const __grid_constant__ QkArgs p, int ctas0, int G, int split0, i
             }
       __syncthreads();
     }
-    float* mine = p.partials + (size_t)blockIdx.x * p.dim;
-    for (int i = threadIdx.x; i < p.dim; i += QK_THREADS) mine[i] = acc[i];
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) last = atomicAdd(p.tickets + which, 1) == ctas - 1;
-    __syncthreads();
-    if (last) {
-      // the blocks' sums: W entries per thread, the blocks dealt out to groups of threads, sixteen loads under way
+    // Blocks are joined sixteen at a time, by whichever of the sixteen comes last, and the sixteens by whichever of them comes last:
+    // one round of loads each, where a single block that added up all of them took 8 us.
+    const int n_groups = (ctas + QK_JOIN - 1) / QK_JOIN, group = cta / QK_JOIN;
+    const int in_group = group + 1 < n_groups ? QK_JOIN : ctas - group * QK_JOIN;
+    float* const rows1 = p.partials + (size_t)(which ? ctas0 : 0) * p.dim;                        // one row per block
+    float* const rows2 = p.partials + (size_t)(QK_MAX_CTAS + (which ? QK_MAX_CTAS / QK_JOIN : 0)) * p.dim;   // ... per group
+    int* const tickets = p.tickets + which * (QK_MAX_CTAS / QK_JOIN + 1);
+    // Writes acc to `row` and returns whether this block is the last of `of` to do so.
+    auto hand_in = [&](float* row, int* ticket, int of) {
+      for (int i = threadIdx.x; i < p.dim; i += QK_THREADS) row[i] = acc[i];
       __threadfence();
-      const float* all = p.partials + (size_t)(which ? ctas0 : 0) * p.dim;
-      auto add_up = [&](auto width) {
-        constexpr int W = decltype(width)::value;
-        const int cols = p.dim / W;
-        const int groups = cols < QK_THREADS ? QK_THREADS / cols : 1;
-        for (int c0 = 0; c0 < cols; c0 += QK_THREADS) {
-          const int col = c0 + threadIdx.x % (cols < QK_THREADS ? cols : QK_THREADS);
-          const int g = groups > 1 ? threadIdx.x / cols : 0;
-          float s[W];
+      __syncthreads();
+      if (threadIdx.x == 0) {
+        last = atomicAdd(ticket, 1) == of - 1;
+        if (last) *ticket = 0;                             // for the next launch
+      }
+      __syncthreads();
+      if (last) __threadfence();
+      return last != 0;
+    };
+    // acc <- the sum of n rows, in the order of the rows for every thread group and then of the groups
+    auto add_up = [&](const float* all, int n, auto width) {
+      constexpr int W = decltype(width)::value;
+      const int cols = p.dim / W;
+      const int groups = cols < QK_THREADS ? QK_THREADS / cols : 1;
+      for (int c0 = 0; c0 < cols; c0 += QK_THREADS) {
+        const int col = c0 + threadIdx.x % (cols < QK_THREADS ? cols : QK_THREADS);
+        const int g = groups > 1 ? threadIdx.x / cols : 0;
+        float s[W];
 #pragma unroll
-          for (int i = 0; i < W; ++i) s[i] = 0.f;
-          if (col < cols && g < groups) {
-            for (int b0 = g; b0 < ctas; b0 += 16 * groups) {
-              float f[16][W];
+        for (int i = 0; i < W; ++i) s[i] = 0.f;
+        if (col < cols && g < groups) {
+          for (int b0 = g; b0 < n; b0 += 8 * groups) {     // eight loads under way
+            float f[8][W];
 #pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                const int b = b0 + j * groups;
-                const float* q = all + (size_t)b * p.dim + col * W;
-                if constexpr (W == 4) {
-                  float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-                  if (b < ctas) x = __ldcg(reinterpret_cast<const float4*>(q));
-                  f[j][0] = x.x; f[j][1] = x.y; f[j][2] = x.z; f[j][3] = x.w;
-                } else {
-                  f[j][0] = b < ctas ? __ldcg(q) : 0.f;
-                }
+            for (int j = 0; j < 8; ++j) {
+              const int b = b0 + j * groups;
+              const float* q = all + (size_t)b * p.dim + col * W;
+              if constexpr (W == 4) {
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (b < n) x = __ldcg(reinterpret_cast<const float4*>(q));
+                f[j][0] = x.x; f[j][1] = x.y; f[j][2] = x.z; f[j][3] = x.w;
+              } else {
+                f[j][0] = b < n ? __ldcg(q) : 0.f;
               }
-#pragma unroll
-              for (int j = 0; j < 16; ++j)
-#pragma unroll
-                for (int i = 0; i < W; ++i) s[i] += f[j][i];
             }
-          }
-          for (int k = 0; k < groups; ++k) {
-            __syncthreads();
-            if (col < cols && g == k)
 #pragma unroll
-              for (int i = 0; i < W; ++i) acc[col * W + i] = (k ? acc[col * W + i] : 0.f) + s[i];
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+              for (int i = 0; i < W; ++i) s[i] += f[j][i];
           }
         }
-        __syncthreads();
-        for (int i = threadIdx.x; i < p.dim; i += QK_THREADS) t.dgain[i] = acc[i];
-      };
-      if (p.dim % 4 == 0) add_up(std::integral_constant<int, 4>());
-      else add_up(std::integral_constant<int, 1>());
-      if (threadIdx.x == 0) p.tickets[which] = 0;      // for the next launch
+        for (int k = 0; k < groups; ++k) {
+          __syncthreads();
+          if (col < cols && g == k)
+#pragma unroll
+            for (int i = 0; i < W; ++i) acc[col * W + i] = (k ? acc[col * W + i] : 0.f) + s[i];
+        }
+      }
+      __syncthreads();
+    };
+    auto join = [&](const float* all, int n) {
+      if (p.dim % 4 == 0) add_up(all, n, std::integral_constant<int, 4>());
+      else add_up(all, n, std::integral_constant<int, 1>());
+    };
+    if (ctas > 1) {
+      if (!hand_in(rows1 + (size_t)cta * p.dim, tickets + group, in_group)) return;
+      join(rows1 + (size_t)group * QK_JOIN * p.dim, in_group);
+      if (n_groups > 1) {
+        if (!hand_in(rows2 + (size_t)group * p.dim, tickets + QK_MAX_CTAS / QK_JOIN, n_groups)) return;
+        join(rows2, n_groups);
+      }
     }
+    for (int i = threadIdx.x; i < p.dim; i += QK_THREADS) t.dgain[i] = acc[i];
   }
 }
 
@@ -622,18 +641,23 @@ cudaError_t launch_one(cudaStream_t st, const QkArgs& a, int n_sms, int G) {
     if (e != cudaSuccess) return e;
     resident = seen_blocks;
   }
-  // The blocks are shared out by head counts; a token's heads go to several warps when there are fewer tokens than warps.
+  // The blocks are shared out by what a token costs in either tensor: its groups of heads, and about one more for what is done
+  // once per token (12 + 3 heads of 64, f32, 4099 tokens, backward: 27 us when shared out by heads).  A token's
+  // heads go to several warps when there are fewer tokens than warps.
   const int rows = 32 / G;
-  const int64_t heads = (int64_t)a.t[0].heads + a.t[1].heads;
   const int64_t most = (int64_t)n_sms * resident < QK_MAX_CTAS - 1 ? (int64_t)n_sms * resident : QK_MAX_CTAS - 1;
-  int ctas[2] = {0, 0}, split[2] = {1, 1};
+  int groups[2], ctas[2] = {0, 0}, split[2] = {1, 1};
+  int64_t cost[2];
   for (int w = 0; w < 2; ++w) {
-    if (!a.t[w].heads) continue;
-    const int groups = (a.t[w].heads + rows - 1) / rows;
-    int64_t share = w && ctas[0] ? most - most * a.t[0].heads / heads : most * a.t[w].heads / heads;
+    groups[w] = (a.t[w].heads + rows - 1) / rows;
+    cost[w] = groups[w] ? groups[w] + 1 : 0;
+  }
+  for (int w = 0; w < 2; ++w) {
+    if (!groups[w]) continue;
+    int64_t share = w ? most - most * cost[0] / (cost[0] + cost[1]) : most * cost[0] / (cost[0] + cost[1]);
     if (share < 1) share = 1;
-    while (split[w] < groups && a.tokens * split[w] < share * QK_WARPS) split[w] *= 2;
-    if (split[w] > groups) split[w] = groups;
+    while (split[w] < groups[w] && a.tokens * split[w] < share * QK_WARPS) split[w] *= 2;
+    if (split[w] > groups[w]) split[w] = groups[w];
     const int64_t need = (a.tokens * split[w] + QK_WARPS - 1) / QK_WARPS;
     ctas[w] = (int)(need < share ? need : share);
   }
