@@ -122,7 +122,18 @@ typedef struct {
                           pseudogradient, nothing is compressed after the mean.  Needs
                           quant == MULOCO_Q_NONE; error_feedback may be set with it.  Tensors
                           of 2^31 elements or more make muloco_create return MULOCO_ESHAPE.    */
+  int32_t adam_state_bits; /* 0 or 32: the moments of AdamW tensors are float32.  8: 8-bit codes (the format is
+                          given at muloco_adamw_create).  state1_k / state2_k of such a tensor of n
+                          elements then point to MULOCO_ADAMW_STATE8_BYTES(n) bytes, 16-byte aligned: the
+                          codes, padded to whole blocks, and behind them one float32 scale per block.
+                          Worker k's dither has the seed k, and its elements count from the first
+                          AdamW tensor on.                                                      */
 } muloco_config;
+
+/* Elements that share a scale in 8-bit AdamW states, and the bytes of such a state of n elements. */
+#define MULOCO_ADAMW_BLOCK 256
+#define MULOCO_ADAMW_STATE8_BYTES(n) \
+  (((n) + MULOCO_ADAMW_BLOCK - 1) / MULOCO_ADAMW_BLOCK * (MULOCO_ADAMW_BLOCK + sizeof(float)))
 
 /* State buffers.  Every field is a HOST array of DEVICE pointers.
  * Per-worker tables have K * n_tensors entries, entry [k * n_tensors + i]. */
@@ -130,7 +141,7 @@ typedef struct {
   float* const* theta_k;  /* [K][n]  worker replicas theta_k                            */
   float* const* theta_g;  /* [n]     global parameters theta                            */
   float* const* outer_u;  /* [n]     outer momentum u                                   */
-  float* const* state1_k; /* [K][n]  Muon momentum m, or Adam first moment              */
+  float* const* state1_k; /* [K][n]  Muon momentum m, or Adam first moment (see adam_state_bits) */
   float* const* state2_k; /* [K][n]  Adam second moment (ignored for Muon tensors)      */
   float* const* ef_k;     /* [K][n]  error-feedback accumulators E_i (Algorithm 2); the table
                              may be NULL unless cfg.error_feedback is set                */
@@ -342,7 +353,6 @@ MULOCO_API muloco_status muloco_pseudogradient(muloco_ctx* ctx, int32_t tensor, 
  * A non-finite gradient raises MULOCO_ENONFINITE (the step is still applied).
  * Gradients and parameters may have any alignment of their type (16 bytes is fastest); state1 and
  * state2 must be 16-byte aligned, scales 4-byte aligned. */
-#define MULOCO_ADAMW_BLOCK 256
 typedef struct muloco_adamw muloco_adamw; /* opaque: a list of tensors and their device tables */
 typedef struct {
   float lr, beta1, beta2, eps, weight_decay;

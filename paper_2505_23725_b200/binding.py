@@ -60,7 +60,7 @@ class Config(C.Structure):
                 ("quant", C.c_int32), ("quant_block", C.c_int32), ("grad_dtype", C.c_int32),
                 ("quant_stages", C.c_int32), ("workspace_bytes", C.c_uint64),
                 ("error_feedback", C.c_int32), ("ef_beta", C.c_float),
-                ("topk_fraction", C.c_float)]
+                ("topk_fraction", C.c_float), ("adam_state_bits", C.c_int32)]
 
 
 class Buffers(C.Structure):
@@ -269,6 +269,7 @@ def make_config(w: _cfg.Workload, workspace_bytes: int = 0, ns_mode: Optional[st
     c.error_feedback = int(w.error_feedback)
     c.ef_beta = w.ef_beta
     c.topk_fraction = w.topk_fraction
+    c.adam_state_bits = w.adam_state_bits
     c.grad_dtype = BF16 if w.grad_dtype == "bf16" else F32
     c.workspace_bytes = workspace_bytes
     for k, v in over.items():
@@ -720,7 +721,9 @@ class MuLoCo(_Operators):
 
     State lives in flat torch buffers (one per replica / state kind) so that the
     tensors of a replica are contiguous; each tensor starts on a 256-byte
-    boundary.  `self.theta_g[i]`, `self.theta_k[k][i]` ... are torch views.
+    boundary.  `self.theta_g[i]`, `self.theta_k[k][i]` ... are torch views.  With
+    adam_state_bits == 8 the states of AdamW tensors are byte tensors of their own
+    (2.03 bytes per element instead of 8): `self.adam_moments(k, i)` has their values.
     """
 
     ALIGN = 64  # elements
@@ -750,12 +753,18 @@ class MuLoCo(_Operators):
         self.flat_theta_g = torch.zeros(off, dtype=f32, device=dev)
         self.flat_u = torch.zeros(off, dtype=f32, device=dev)
         self.flat_theta_k = [torch.empty(off, dtype=f32, device=dev) for _ in range(self.K)]
-        self.flat_s1 = [torch.empty(off, dtype=f32, device=dev) for _ in range(self.K)]
+        # 8-bit AdamW states: bytes (codes, then scales; see the header) instead of places in flat_s1 and flat_s2
+        self.state8 = self.cfg.adam_state_bits == 8
+        off1, offsets1 = 0, []
+        for t in workload.tensors:
+            offsets1.append(off1)
+            off1 += 0 if self.state8 and t.kind == _cfg.ADAMW else (t.numel + self.ALIGN - 1) // self.ALIGN * self.ALIGN
+        self.flat_s1 = [torch.empty(off1, dtype=f32, device=dev) for _ in range(self.K)]
         # Adam's second moment exists for AdamW tensors only: its own compact buffer
         self.offsets2, off2 = [], 0
         for t in workload.tensors:
-            self.offsets2.append(off2 if t.kind == _cfg.ADAMW else None)
-            if t.kind == _cfg.ADAMW:
+            self.offsets2.append(off2 if t.kind == _cfg.ADAMW and not self.state8 else None)
+            if t.kind == _cfg.ADAMW and not self.state8:
                 off2 += (t.numel + self.ALIGN - 1) // self.ALIGN * self.ALIGN
         self.flat_s2 = [torch.empty(off2, dtype=f32, device=dev) if off2 else None for _ in range(self.K)]
         self.flat_ef = [torch.empty(off, dtype=f32, device=dev) for _ in range(self.K)] \
@@ -764,9 +773,16 @@ class MuLoCo(_Operators):
         self.theta_g = self._views(self.flat_theta_g)
         self.outer_u = self._views(self.flat_u)
         self.theta_k = [self._views(b) for b in self.flat_theta_k]
-        self.state1 = [self._views(b) for b in self.flat_s1]
+        self.state1 = [[b[o:o + t.numel].view(t.rows, t.cols) if not (self.state8 and t.kind == _cfg.ADAMW) else None
+                        for o, t in zip(offsets1, workload.tensors)] for b in self.flat_s1]
         self.state2 = [[b[o:o + t.numel].view(t.rows, t.cols) if (b is not None and o is not None) else None
                         for o, t in zip(self.offsets2, workload.tensors)] for b in self.flat_s2]
+        if self.state8:
+            for k in range(self.K):
+                for i, t in enumerate(workload.tensors):
+                    if t.kind == _cfg.ADAMW:
+                        n = -(-t.numel // ADAMW_BLOCK) * (ADAMW_BLOCK + 4)
+                        self.state1[k][i], self.state2[k][i] = (torch.empty(n, dtype=torch.uint8, device=dev) for _ in range(2))
         if init is not None:
             for i, a in enumerate(init):
                 self.theta_g[i].copy_(torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(dev))
@@ -972,6 +988,18 @@ class MuLoCo(_Operators):
         stream.  Returns the bytes this rank sent and received over the wire (the ring
         algorithm's 2 * 4 * stage_floats * (world - 1) / world)."""
         return sharded_outer_sync(self, fragment, dist, group)
+
+    def adam_moments(self, worker: int, tensor: int):
+        """(m, v) of an AdamW tensor as float32 of its shape: the states, or the values 8-bit states stand for."""
+        t = self.w.tensors[tensor]
+        a, b = self.state1[worker][tensor], self.state2[worker][tensor]
+        if not self.state8:
+            return a, b
+        torch, n = self.torch, -(-t.numel // ADAMW_BLOCK) * ADAMW_BLOCK
+        def values(s, dtype):
+            return s[:n].view(dtype).float().view(-1, ADAMW_BLOCK) * s[n:].view(torch.float32)[:, None]
+        m, r = values(a, torch.int8), values(b, torch.uint8)
+        return m.view(-1)[:t.numel].view(t.rows, t.cols), r.square().view(-1)[:t.numel].view(t.rows, t.cols)
 
     def check_workspace(self):
         """muloco_check_workspace: raises MulocoError(ESTATE) if a workspace canary was overwritten."""

@@ -205,6 +205,8 @@ struct muloco_ctx {
   std::vector<cudaEvent_t> ev_pool;
   int64_t launches = 0;
 
+  std::vector<muloco_adamw*> adam8;   // 8-bit AdamW states: one list per worker
+
   // operators around the optimizer (ops_capi.cu)
   float* qk_scratch = nullptr;     // gain-gradient partials of qk_norm.cu, then its tickets; allocated on first use
 };
@@ -291,6 +293,8 @@ muloco_status validate_config(const muloco_config* cfg) {
   if (cfg->grad_dtype != MULOCO_F32 && cfg->grad_dtype != MULOCO_BF16)
     return fail(c, MULOCO_EINVAL, "unknown grad_dtype %d", cfg->grad_dtype);
   if (!(cfg->ns_eps >= 0.f)) return fail(c, MULOCO_EINVAL, "ns_eps must be >= 0");
+  if (cfg->adam_state_bits != 0 && cfg->adam_state_bits != 32 && cfg->adam_state_bits != 8)
+    return fail(c, MULOCO_EINVAL, "adam_state_bits must be 0, 32 or 8");
   return MULOCO_OK;
 }
 
@@ -555,6 +559,9 @@ MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_te
       if (!bufs->theta_k[e] || !bufs->state1_k[e]) return fail(c, MULOCO_EINVAL, "tensor %d worker %d: NULL buffer", i, k);
       if (d.kind == MULOCO_ADAMW && !bufs->state2_k[e])
         return fail(c, MULOCO_EINVAL, "tensor %d worker %d: NULL second-moment buffer", i, k);
+      if (cfg->adam_state_bits == 8 && d.kind == MULOCO_ADAMW &&
+          ((((uintptr_t)bufs->state1_k[e]) | ((uintptr_t)bufs->state2_k[e])) & 15) != 0)
+        return fail(c, MULOCO_EINVAL, "tensor %d worker %d: 8-bit states must be 16-byte aligned", i, k);
       if (cfg->error_feedback != 0 && !bufs->ef_k[e])
         return fail(c, MULOCO_EINVAL, "tensor %d worker %d: NULL error-feedback buffer", i, k);
     }
@@ -681,14 +688,44 @@ MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_te
 
   { const muloco_status bs = build_sync_tables(c); if (bs != MULOCO_OK) return bail(bs); }
 
+  if (cfg->adam_state_bits == 8 && !c->adam_ids.empty()) {
+    muloco_adamw_config ac;
+    memset(&ac, 0, sizeof ac);
+    ac.lr = cfg->adam_lr; ac.beta1 = cfg->adam_beta1; ac.beta2 = cfg->adam_beta2; ac.eps = cfg->adam_eps;
+    ac.weight_decay = cfg->adam_wd; ac.bias_correction = cfg->adam_bias_correction;
+    ac.state_bits = 8; ac.grad_dtype = cfg->grad_dtype;
+    for (int k = 0; k < K; ++k) {
+      std::vector<muloco_adamw_tensor> list;
+      for (int i : c->adam_ids) {
+        const TensorInfo& t = c->T[i];
+        const size_t codes = (size_t)(t.numel() + MULOCO_ADAMW_BLOCK - 1) / MULOCO_ADAMW_BLOCK * MULOCO_ADAMW_BLOCK;
+        muloco_adamw_tensor a;
+        memset(&a, 0, sizeof a);
+        a.n = t.numel();
+        a.theta = t.theta_k[k];
+        a.state1 = t.s1[k]; a.state2 = t.s2[k];
+        a.scale1 = reinterpret_cast<float*>(reinterpret_cast<char*>(t.s1[k]) + codes);
+        a.scale2 = reinterpret_cast<float*>(reinterpret_cast<char*>(t.s2[k]) + codes);
+        a.wd_mult = t.wd_mult; a.lr_mult = t.lr_mult;
+        list.push_back(a);
+      }
+      ac.seed = (uint32_t)k;
+      muloco_adamw* o = nullptr;
+      const muloco_status as = muloco_adamw_create(c, &ac, list.data(), (int32_t)list.size(), &o);
+      if (as != MULOCO_OK) return bail(as);
+      c->adam8.push_back(o);
+    }
+  }
+
   // Algorithm 1, initialisation: u <- 0, inner state <- 0, theta_k <- theta_g
   for (int i = 0; i < n_tensors; ++i) {
     TensorInfo& t = c->T[i];
     const size_t bytes = (size_t)t.numel() * sizeof(float);
     CKC(cudaMemsetAsync(t.u, 0, bytes, c->st));
     for (int k = 0; k < K; ++k) {
-      CKC(cudaMemsetAsync(t.s1[k], 0, bytes, c->st));
-      if (t.s2[k]) CKC(cudaMemsetAsync(t.s2[k], 0, bytes, c->st));
+      const size_t state = t.kind == MULOCO_ADAMW && cfg->adam_state_bits == 8 ? MULOCO_ADAMW_STATE8_BYTES((size_t)t.numel()) : bytes;
+      CKC(cudaMemsetAsync(t.s1[k], 0, state, c->st));
+      if (t.s2[k]) CKC(cudaMemsetAsync(t.s2[k], 0, state, c->st));
       if (t.ef[k]) CKC(cudaMemsetAsync(t.ef[k], 0, bytes, c->st));     // Algorithm 2: E_i <- 0
       CKC(cudaMemcpyAsync(t.theta_k[k], t.theta_g, bytes, cudaMemcpyDeviceToDevice, c->st));
     }
@@ -701,6 +738,7 @@ MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_te
 MULOCO_API void muloco_destroy(muloco_ctx* c) {
   if (!c) return;
   cudaStreamSynchronize(c->st);
+  for (muloco_adamw* o : c->adam8) muloco_adamw_destroy(o);
   for (Group& g : c->groups) destroy_group(g);
   destroy_group(c->sa_group);
   if (c->ws) cudaFree(c->ws);
@@ -783,7 +821,8 @@ MULOCO_API muloco_status muloco_inner_step(muloco_ctx* c, int32_t worker, const 
   AdamSeg* ha = reinterpret_cast<AdamSeg*>(host + nm * sizeof(MatDesc));
   size_t na = 0;
   int64_t units = 0;
-  for (int k = k0; k < k1; ++k) {
+  const bool adam8 = !c->adam8.empty();
+  for (int k = k0; k < k1 && !adam8; ++k) {
     const double t_step = (double)(c->worker_step[k] + 1);
     const double bc1 = f.adam_bias_correction ? 1.0 - pow((double)f.adam_beta1, t_step) : 1.0;
     const double bc2 = f.adam_bias_correction ? 1.0 - pow((double)f.adam_beta2, t_step) : 1.0;
@@ -826,7 +865,7 @@ MULOCO_API muloco_status muloco_inner_step(muloco_ctx* c, int32_t worker, const 
       c->consumed_valid[gi] = 1;
     }
   }
-  if (na) {
+  if (na || adam8) {
     const size_t sec = c->groups.size();
     if (c->host_mode) {
       CK(cudaStreamWaitEvent(c->st, c->ev_copied[sec], 0));
@@ -834,8 +873,17 @@ MULOCO_API muloco_status muloco_inner_step(muloco_ctx* c, int32_t worker, const 
     }
     {
       PhaseTimer t(c, MULOCO_PH_ADAMW);
-      launch_adamw(c->st, c->d_adam, (int)na, units, g_is_bf16, f.adam_beta1, f.adam_beta2, f.adam_eps, c->d_status);
-      c->launches += 1;
+      if (adam8) {
+        std::vector<const void*> g(c->adam_ids.size());
+        for (int k = k0; k < k1; ++k) {
+          for (size_t j = 0; j < g.size(); ++j) g[j] = grads[(size_t)(k - k0) * n + c->adam_ids[j]];
+          rs = muloco_adamw_step(c->adam8[k], g.data(), c->worker_step[k] + 1, lr_scale);
+          if (rs != MULOCO_OK) return rs;
+        }
+      } else {
+        launch_adamw(c->st, c->d_adam, (int)na, units, g_is_bf16, f.adam_beta1, f.adam_beta2, f.adam_eps, c->d_status);
+        c->launches += 1;
+      }
     }
     if (c->host_mode) {
       CK(cudaEventRecord(c->ev_consumed[sec], c->st));

@@ -679,6 +679,15 @@ ffn_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ Few
 }
 
 // ------------------------------ host side ----------------------------------
+// Makes the current device's context this thread's: the descriptor encoder is a driver call, which fails in a
+// thread that has made no runtime call yet (a backward pass runs in a thread of its own).
+cudaError_t bind_context(const char** what) {
+  *what = "cudaSetDevice";
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  return e == cudaSuccess ? cudaSetDevice(dev) : e;
+}
+
 // A row-major bf16 matrix as an operand: rows x cols with row pitch ld.
 struct Mat { const void* p; int64_t rows, cols, ld; };
 
@@ -883,6 +892,8 @@ constexpr int64_t FEW_FORWARD = 128, FEW_BACKWARD = 256;
 }  // namespace
 
 cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
+  cudaError_t bound = bind_context(what);
+  if (bound != cudaSuccess) return bound;
   if (a.T <= FEW_FORWARD) {
     FewParams p;
     memset(&p, 0, sizeof p);
@@ -927,6 +938,8 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
 }
 
 cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
+  cudaError_t bound = bind_context(what);
+  if (bound != cudaSuccess) return bound;
   const bool few = a.T <= FEW_BACKWARD;
   if ((a.dx || a.dw1 || a.dw3) && few) {
     FewParams p;

@@ -1,0 +1,56 @@
+"""The operators of the training step as torch autograd functions.
+
+`owner` is a binding.Context or a binding.MuLoCo.  The backward passes are the library's own kernels; nothing
+is computed twice and nothing else is kept than what their docstrings in binding.py name."""
+from __future__ import annotations
+
+import torch
+
+
+class _GatedFFN(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, owner, activation, x, w1, w3, w2):
+        y, saved = owner.gated_ffn(x, w1, w3, w2, activation)
+        ctx.owner, ctx.activation = owner, activation
+        ctx.save_for_backward(x, w1, w3, w2, *saved)
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, w1, w3, w2, *saved = ctx.saved_tensors
+        dy = dy if dy.stride(1) == 1 else dy.contiguous()
+        return (None, None, *ctx.owner.gated_ffn_backward(dy, x, w1, w3, w2, tuple(saved), ctx.activation))
+
+
+def gated_ffn(owner, x, w1, w3, w2, activation: str = "silu"):
+    """(act(x w1) * (x w3)) w2 over the last dimension of x, differentiable in x and the weights (all bf16)."""
+    rows = x.reshape(-1, x.shape[-1])
+    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w3, w2)):
+        y = _GatedFFN.apply(owner, activation, rows, w1, w3, w2)
+    else:
+        y, _ = owner.gated_ffn(rows, w1, w3, w2, activation, save=False)
+    return y.view(*x.shape[:-1], w2.shape[1])
+
+
+class _QKNormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, owner, eps, interleaved, q, k, cos, sin, positions, gain_q, gain_k):
+        ctx.owner, ctx.eps, ctx.interleaved = owner, eps, interleaved
+        ctx.save_for_backward(q, k, cos, sin, positions, gain_q, gain_k)
+        return owner.qk_norm_rope(q, k, cos, sin, positions, gain_q, gain_k, eps, interleaved)
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        q, k, cos, sin, positions, gain_q, gain_k = ctx.saved_tensors
+        dq, dk = (d if d.stride(2) == 1 else d.contiguous() for d in (dq, dk))
+        dq, dk, dgq, dgk = ctx.owner.qk_norm_rope_backward(dq, dk, q, k, cos, sin, positions, gain_q, gain_k, ctx.eps,
+                                                           ctx.interleaved)
+        return (None, None, None, dq, dk, None, None, None, dgq if gain_q is not None else None,
+                dgk if gain_k is not None else None)
+
+
+def qk_norm_rope(owner, q, k, cos, sin, positions=None, gain_q=None, gain_k=None, eps: float = 1e-6,
+                 interleaved: bool = False):
+    """Norm and rotation of q [tokens, heads, head_dim] and k (binding.Context.qk_norm_rope), differentiable in q, k
+    and the gains."""
+    return _QKNormRope.apply(owner, eps, interleaved, q, k, cos, sin, positions, gain_q, gain_k)

@@ -20,12 +20,14 @@ def test_struct_layouts_match_the_header(tmp_path):
                    'int main(void){printf("%zu %zu %zu %zu %zu %zu %zu %d\\n", sizeof(muloco_adamw_config),'
                    ' sizeof(muloco_adamw_tensor), sizeof(muloco_qk_norm), sizeof(muloco_ffn),'
                    ' offsetof(muloco_adamw_tensor, wd_mult), offsetof(muloco_qk_norm, gain_q), offsetof(muloco_ffn, x),'
-                   ' MULOCO_ADAMW_BLOCK); return 0;}\n')
+                   ' MULOCO_ADAMW_BLOCK); printf("%zu %zu\\n", offsetof(muloco_config, adam_state_bits),'
+                   ' (size_t)MULOCO_ADAMW_STATE8_BYTES(257)); return 0;}\n')
     exe = tmp_path / "t"
     subprocess.check_call(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)])
     out = [int(x) for x in subprocess.check_output([str(exe)]).decode().split()]
     assert out == [C.sizeof(B.AdamwConfig), C.sizeof(B.AdamwTensor), C.sizeof(B.QkNorm), C.sizeof(B.Ffn),
-                   B.AdamwTensor.wd_mult.offset, B.QkNorm.gain_q.offset, B.Ffn.x.offset, B.ADAMW_BLOCK]
+                   B.AdamwTensor.wd_mult.offset, B.QkNorm.gain_q.offset, B.Ffn.x.offset, B.ADAMW_BLOCK,
+                   B.Config.adam_state_bits.offset, 2 * (256 + 4)]
     # the packed forms are the structs' bytes
     assert len(B._QK_PACK(*range(8), 0.5, *range(12))) == C.sizeof(B.QkNorm)
     assert len(B._FFN_PACK(*range(13))) == C.sizeof(B.Ffn)
