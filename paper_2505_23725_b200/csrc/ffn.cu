@@ -68,7 +68,7 @@ struct Prob {
 
 struct Params {
   Prob prob[MAX_PROBS];
-  int n_probs, total_tiles, epi, act;
+  int n_probs, total_tiles, n_maps, act;
   int* status;
   unsigned long long wait_limit_ns;
 };
@@ -185,6 +185,10 @@ ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) 
   const uint64_t limit = p.wait_limit_ns;
   const int worker = blockIdx.x / CG, workers = gridDim.x / CG;
 
+  if (threadIdx.x == 32 * 2) {
+#pragma unroll 1
+    for (int i = 0; i < p.n_maps; ++i) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.m[i]) : "memory");
+  }
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < STAGES; ++s) {
@@ -451,6 +455,7 @@ struct FewParams {
   int M, T;                  // rows of the transposed result (columns of the output), tokens
   int slabs0, slabs;
   int a_mn, a_wide;
+  int n_weights, n_pairs;    // descriptors in use
   void* out; void* out2; void* out3;
   const void* in1; const void* in2;
   int weights_early;         // the kernel before this one does not write the weights
@@ -459,8 +464,10 @@ struct FewParams {
 };
 struct FewMaps { CUtensorMap a[2], b[2]; };  // EPI_GATE: a = W1, W3; else one per operand pair
 
-__device__ __forceinline__ void st_cluster_f32(uint32_t addr, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+__device__ __forceinline__ float2 ld_cluster_f32x2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
+  return v;
 }
 
 template <int EPI, int ACT, int NT>
@@ -483,6 +490,12 @@ ffn_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ Few
   const int m0 = blockIdx.y * 128, t0 = blockIdx.z * NT;
   const int kb_first = (int)((int64_t)p.slabs * share / S), kb_end = (int)((int64_t)p.slabs * (share + 1) / S);
 
+  if (threadIdx.x == 64) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a[0]) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b[0]) : "memory");
+    if (p.n_weights > 1) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.a[1]) : "memory");
+    if (p.n_pairs > 1) asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.b[1]) : "memory");
+  }
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int s = 0; s < Sh::STAGES; ++s) {
@@ -585,10 +598,12 @@ ffn_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ Few
     mbar_wait(smem_u32(&bar_done), 0, &abort_flag, limit);   // on a timeout the flag is set and the results do not count
     __syncwarp();
   }
-  // Every copy of this CTA has landed and been used; once that holds for the whole cluster the pipeline's space
-  // takes the partial sums: [accumulator][source rank][token of this CTA's share][128 rows].
+  // Every copy of this CTA has landed and been used: the pipeline's space takes its partial sums,
+  // [accumulator][token][128 rows].  CTA r of the cluster finishes tokens r NT / S and on, and fetches the others' sums of
+  // them through distributed shared memory (fetching 8 bytes a lane: a 4-byte store per element to the CTA that
+  // wants it was measured twice as slow at 90 tokens).
   tc_fence_before();
-  cluster_sync_all();
+  __syncthreads();
   tc_fence_after();
   const int per = NT / S;                            // tokens that each CTA finishes
   if (warp >= 2) {
@@ -599,34 +614,31 @@ ffn_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ Few
       uint32_t v[32];
       tc_ld32(tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)c, v);
 #pragma unroll
-      for (int e = 0; e < 32; ++e) {
-        const int col = c + e;
-        if (col < Sh::COLS) {
-          const int w = col / NT, tok = col % NT;
-          const int dst = tok / per, tl = tok - dst * per;
-          const uint32_t off = (uint32_t)((((w * S + share) * per + tl) * 128 + r128) * 4);
-          st_cluster_f32(map_to_rank(smem_base + off, (uint32_t)dst), __uint_as_float(v[e]));
-        }
-      }
+      for (int e = 0; e < 32; ++e)
+        if (c + e < Sh::COLS) sts32(smem_base + (uint32_t)(((c + e) * 128 + r128) * 4), v[e]);
     }
   }
   tc_fence_before();
-  cluster_sync_all();
+  if (S > 1) cluster_sync_all(); else __syncthreads();
   tc_fence_after();
   if (warp >= 2) {
     // two neighbouring columns per thread, the tokens over the thread groups, four tokens at a time
     constexpr int GROUPS = FEW_EPI_THREADS / 64, BATCH = 4;
-    const float* sums = reinterpret_cast<const float*>(smem_raw + (smem_base - smem_u32(smem_raw)));
     const int id = threadIdx.x - 64;
     const int r = (id & 63) * 2, m = m0 + r;
     const int left = p.T - (t0 + share * per);       // tokens of this CTA that exist
     const int n_tok = left < per ? left : per;
-    auto total = [&](int w, int tl) {
-      float2 x = make_float2(0.f, 0.f);
-      for (int src = 0; src < S; ++src) {
-        const float2 y = *reinterpret_cast<const float2*>(sums + ((w * S + src) * per + tl) * 128 + r);
-        x.x += y.x; x.y += y.y;
-      }
+    auto total = [&](int w, int tl) {                // the CTAs' sums in the order of their ranks
+      const uint32_t at = smem_base + (uint32_t)(((w * NT + share * per + tl) * 128 + r) * 4);
+      if (S == 1) return ld_cluster_f32x2(at);
+      float2 y[8];
+#pragma unroll
+      for (int src = 0; src < 8; ++src)
+        if (src < S) y[src] = ld_cluster_f32x2(map_to_rank(at, (uint32_t)src));
+      float2 x = y[0];
+#pragma unroll
+      for (int src = 1; src < 8; ++src)
+        if (src < S) { x.x += y[src].x; x.y += y[src].y; }
       return x;
     };
     auto put = [&](void* base, int64_t o, float a0, float a1) {
@@ -674,7 +686,9 @@ ffn_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ Few
     while (global_timer_ns() - t1 < 200000ull) __nanosleep(1000);
     if (threadIdx.x == 0) atomicOr(p.status, ST_TIMEOUT);
   }
-  __syncthreads();
+  // (a CTA's sums stay until the others have fetched them)
+  __syncwarp();
+  if (S > 1) cluster_sync_all(); else __syncthreads();
   if (warp == 1) tmem_dealloc<1>(tmem_base, Sh::TMEM);
 }
 
@@ -784,7 +798,7 @@ cudaError_t launch_built(cudaStream_t st, Builder& b, const FfnArgs& a, int epi,
   *what = "cuTensorMapEncodeTiled";
   if (!b.ok) return cudaErrorInvalidValue;
   *what = "launch of the feed-forward kernel";
-  b.p.epi = epi;
+  b.p.n_maps = b.n_maps;
   b.p.act = a.act;
   b.p.status = a.status;
   b.p.wait_limit_ns = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
@@ -850,6 +864,8 @@ cudaError_t launch_few(cudaStream_t st, const FfnArgs& a, int epi, const FewOper
   bool ok = true;
   const int n_weights = epi == EPI_GATE ? 2 : n_pairs;
   p.a_mn = mn;
+  p.n_weights = n_weights;
+  p.n_pairs = n_pairs;
   for (int w = 0; w < n_weights; ++w) {
     if (mn) {
       const bool wide = encode_wide(&m.a[w], q.weight[w]);
