@@ -846,12 +846,12 @@ cudaError_t launch_few_nt(cudaStream_t st, int nt, const FewMaps& m, const FewPa
   return launch_few_kernel<EPI, ACT, 128>(st, m, p, split);
 }
 
-// Tokens per tile.  Wider tiles read the weights fewer times and exchange more partial sums; 128 only where 64
-// would give more tiles than SMs.  Whole forward pass, us, tiles of 64 / 128: 128 tokens at 768 x 2048 21 / 32, at
-// 2048 x 5632 46 / 49; 256 tokens at 2048 x 5632 (176 tiles of 64) 81 / 60.
+// Tokens per tile.  Wider tiles read the weights fewer times and give fewer CTAs more to do; above 64 tokens, tiles of
+// 64 only where they are few.  Whole forward pass, us, tiles of 64 / 128: 256 tokens at 2048 x 5632 (176 tiles of 64)
+// 44 / 38, 512 at 1024 x 2816 29 / 27; 64 tokens at 2048 x 5632 30 / 34.
 int few_tile(int64_t T, int64_t M, int n_sms) {
-  if (T <= 32) return T <= 16 ? 16 : 32;
-  return (M + 127) / 128 * ((T + 63) / 64) <= n_sms ? 64 : 128;
+  if (T <= 64) return T <= 16 ? 16 : T <= 32 ? 32 : 64;
+  return (M + 127) / 128 * ((T + 63) / 64) <= n_sms / 4 ? 64 : 128;
 }
 
 struct FewOperand { Mat weight[2]; Mat tokens[2]; };   // per operand pair (gated product: weight = W1, W3)
@@ -883,12 +883,14 @@ cudaError_t launch_few(cudaStream_t st, const FfnArgs& a, int epi, const FewOper
   p.T = (int)a.T;
   p.status = a.status;
   p.wait_limit_ns = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
-  // Split the contraction until every SM has a CTA.  Clusters of eight only while all of them find room at once
-  // (an SM cluster has place for two; 16 tiles of 2048 x 5632 at 8: 33 us for the pass, at 4: 29).
+  // Split the contraction until every SM has a CTA.  Clusters of four and eight only while all of them find room at once,
+  // which takes whole groups of neighbouring SMs: a second wave of clusters costs more than the split gains (36 tiles in clusters
+  // of four: 30 us for the pass, 24 tiles: 24).
   const int64_t tiles = (int64_t)((p.M + 127) / 128) * ((a.T + nt - 1) / nt);
   int split = 1;
-  while (split < 4 && tiles * split * 2 <= a.n_sms && split * 2 <= p.slabs) split *= 2;
-  if (split == 4 && tiles * 8 <= 96 && p.slabs >= 8) split = 8;
+  if (p.slabs >= 2 && tiles * 2 <= a.n_sms) split = 2;
+  if (p.slabs >= 4 && tiles * 4 <= a.n_sms * 7 / 8) split = 4;
+  if (p.slabs >= 8 && tiles * 8 <= a.n_sms * 2 / 3) split = 8;
   const bool gelu = a.act == MULOCO_ACT_GELU;
   if (epi == EPI_GATE)
     return gelu ? launch_few_nt<EPI_GATE, MULOCO_ACT_GELU>(st, nt, m, p, split) : launch_few_nt<EPI_GATE, MULOCO_ACT_SILU>(st, nt, m, p, split);
@@ -900,17 +902,23 @@ cudaError_t launch_few(cudaStream_t st, const FfnArgs& a, int epi, const FewOper
 
 int slabs_of(int64_t k) { return (int)((k + BK - 1) / BK); }
 
-// Up to how many tokens a pass takes the few-token form, whole pass in us, few-token form / 256 x 256 tiles:
-// forward, 128 tokens: 21 / 25 (768 x 2048), 27 / 32 (1024 x 2816), 46 / 54 (2048 x 5632); 256: 26 / 25, 34 / 32, 60 / 54.
-// Backward, 256 tokens: 32 / 42, 44 / 53, 91 / 112; 384: 42 / 42, 49 / 53, 109 / 112.
-constexpr int64_t FEW_FORWARD = 128, FEW_BACKWARD = 256;
+// Whether a pass takes the few-token form: while its widest product has at most a tile of 128 x 128 per SM, up to 512
+// tokens, or any number while that product is small.  Whole pass, us, few-token form / 256 x 256 tiles, forward and
+// backward: 256 tokens 19 / 25 and 27 / 42 (768 x 2048), 38 / 54 and 78 / 113 (2048 x 5632); 512 tokens 24 / 26
+// and 33 / 42, 27 / 32 and 45 / 53 (1024 x 2816), 69 / 66 and 123 / 116 (2048 x 5632, 176 tiles); 768 tokens
+// 31 / 26 and 49 / 45 (768 x 2048, 96 tiles).
+bool few_tokens(const FfnArgs& a) {
+  const int64_t N = a.F > a.d ? a.F : a.d;
+  const int64_t tiles = (N + 127) / 128 * ((a.T + 127) / 128);
+  return tiles <= a.n_sms && (a.T <= 512 || tiles <= 64);
+}
 
 }  // namespace
 
 cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
   cudaError_t bound = bind_context(what);
   if (bound != cudaSuccess) return bound;
-  if (a.T <= FEW_FORWARD) {
+  if (few_tokens(a)) {
     FewParams p;
     memset(&p, 0, sizeof p);
     p.M = (int)a.F; p.slabs0 = p.slabs = slabs_of(a.d);
@@ -956,7 +964,7 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
 cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
   cudaError_t bound = bind_context(what);
   if (bound != cudaSuccess) return bound;
-  const bool few = a.T <= FEW_BACKWARD;
+  const bool few = few_tokens(a);
   if ((a.dx || a.dw1 || a.dw3) && few) {
     FewParams p;
     memset(&p, 0, sizeof p);
