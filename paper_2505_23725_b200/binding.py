@@ -303,7 +303,8 @@ class _Operators:
         fast = _load_fastcall()
         self._fast = {}
         if fast is not None:
-            for name in ("qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward"):
+            for name in ("qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward", "adamw_step",
+                         "adamw_moments"):
                 self._fast[name] = (getattr(fast, name), C.cast(getattr(self.lib, "muloco_" + name), C.c_void_p).value)
 
     def _quick(self, name, *args):
@@ -674,6 +675,15 @@ class AdamW:
 
     def step(self, grads=None, lr_scale: float = 1.0):
         """One step of all tensors, with the gradients named at construction or those given."""
+        if grads is None:
+            f = self.owner._fast.get("adamw_step")
+            if f is not None:
+                st = f[0](self.opt.value, f[1], self.owner._dev, self.owner._handle, self.steps + 1, lr_scale)
+                if st is not None:
+                    if st:
+                        self.owner._check(st)
+                    self.steps += 1
+                    return
         table = None
         if grads is not None:
             if len(grads) != len(self.params):
@@ -694,6 +704,13 @@ class AdamW:
         32-bit states themselves.  Padding entries are zero."""
         if self.state_bits == 32:
             return self.state1, self.state2
+        f = self.owner._fast.get("adamw_moments")
+        if f is not None:
+            r = f[0](self.opt.value, f[1], self.owner._dev, self.owner._handle, self.scale1, self.padded)
+            if r.__class__ is int:
+                self.owner._check(r)
+            if r is not None:
+                return r
         m, v = self.scale1.new_empty(self.padded), self.scale1.new_empty(self.padded)
         cur = self.owner._other_stream()
         if cur is not None:

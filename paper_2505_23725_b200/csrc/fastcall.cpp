@@ -4,7 +4,7 @@
 // its own way, which says what is wrong or bridges the streams.  At one token the interpreter's part of a call
 // costs two to four times the kernel: norm with rotation 12 us a call without this file.
 //
-// A function gets (context, library function, device, stream) as integers, then the tensors; it returns the results, None,
+// A function gets (context or AdamW list, library function, device, stream) as integers, then its arguments; it returns the results, None,
 // or the library's status when that is an error.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -20,7 +20,7 @@
 namespace {
 
 struct Call {
-  muloco_ctx* ctx;
+  muloco_ctx* ctx;                 // (or the AdamW list)
   void* fn;
   int64_t dev;
   bool ok;
@@ -213,13 +213,40 @@ PyObject* ffn_backward(PyObject*, PyObject* const* o, Py_ssize_t n) {
       return none();
   }
   const auto opt = x->options();
-  at::Tensor dg = at::empty({a.tokens, a.F}, opt), du = at::empty({a.tokens, a.F}, opt), dx = at::empty({a.tokens, a.d}, opt),
+  // dG and dU are scratch: one allocation (each a multiple of 16 bytes)
+  at::Tensor scratch = at::empty({2, a.tokens, a.F}, opt), dx = at::empty({a.tokens, a.d}, opt),
              dw1 = at::empty({a.d, a.F}, opt), dw3 = at::empty({a.d, a.F}, opt), dw2 = at::empty({a.F, a.d}, opt);
   const auto fn = (decltype(&muloco_gated_ffn_backward))c.fn;
   const int st = fn(c.ctx, &a, dy->data_ptr(), a.tokens > 1 ? dy->stride(0) : a.d, s[0]->data_ptr(), s[1]->data_ptr(), s[2]->data_ptr(),
-                    dg.data_ptr(), du.data_ptr(), dx.data_ptr(), dw1.data_ptr(), dw3.data_ptr(), dw2.data_ptr());
+                    scratch.data_ptr(), static_cast<char*>(scratch.data_ptr()) + a.tokens * a.F * 2, dx.data_ptr(), dw1.data_ptr(), dw3.data_ptr(), dw2.data_ptr());
   if (st) return PyLong_FromLong(st);
   return Py_BuildValue("(NNNN)", wrap(dx), wrap(dw1), wrap(dw3), wrap(dw2));
+}
+
+// (list, library function, device, stream), step number, learning-rate scale: a step with the gradients named at construction
+PyObject* adamw_step(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  if (n != 6) return none();
+  const Call c = call_of(o);
+  const long long step = PyLong_AsLongLong(o[4]);
+  const double scale = PyFloat_AsDouble(o[5]);
+  if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
+  if (!c.ok) return none();
+  return PyLong_FromLong(((decltype(&muloco_adamw_step))c.fn)(reinterpret_cast<muloco_adamw*>(c.ctx), nullptr, step, (float)scale));
+}
+
+// (list, library function, device, stream), a float32 tensor to make the results like, their length
+PyObject* adamw_moments(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  if (n != 6) return none();
+  const Call c = call_of(o);
+  bool ok = c.ok;
+  const at::Tensor* like = tensor(o[4], &ok);
+  const long long len = PyLong_AsLongLong(o[5]);
+  if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
+  if (!ok || !like) return none();
+  at::Tensor m = at::empty({len}, like->options()), v = at::empty({len}, like->options());
+  const int st = ((decltype(&muloco_adamw_moments))c.fn)(reinterpret_cast<muloco_adamw*>(c.ctx), (float*)m.data_ptr(), (float*)v.data_ptr());
+  if (st) return PyLong_FromLong(st);
+  return Py_BuildValue("(NN)", wrap(m), wrap(v));
 }
 
 // No C++ exception (an allocation that fails, above all) leaves a function: it becomes a Python one.
@@ -246,6 +273,8 @@ PyMethodDef methods[] = {
     FAST("qk_norm_rope_backward", qk_backward, "muloco_qk_norm_rope_backward"),
     FAST("gated_ffn", ffn_forward, "muloco_gated_ffn"),
     FAST("gated_ffn_backward", ffn_backward, "muloco_gated_ffn_backward"),
+    FAST("adamw_step", adamw_step, "muloco_adamw_step"),
+    FAST("adamw_moments", adamw_moments, "muloco_adamw_moments"),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

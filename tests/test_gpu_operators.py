@@ -550,7 +550,19 @@ def test_compiled_and_python_call_paths_agree(ctx):
     from paper_2505_23725_b200 import binding
     plain = binding.Context("cuda:0")
     plain._fast = {}
-    assert set(ctx._fast) == {"qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward"}
+    assert set(ctx._fast) == {"qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward", "adamw_step",
+                              "adamw_moments"}
+    outs = []
+    for owner in (ctx, plain):
+        torch.manual_seed(3)
+        p, g = torch.randn(5000, device="cuda"), torch.randn(5000, device="cuda")
+        opt = binding.AdamW(owner, [p], grads=[g], state_bits=8, **HYPER)
+        opt.step()
+        opt.step(lr_scale=0.5)
+        outs.append((p, *opt.moments(), opt.state1))
+        assert opt.steps == 2
+        opt.close()
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
     q, k, cos, sin, pos, gq, gk, dqo, dko = _qk_inputs((37, 6, 2, 64, 32, False), torch.bfloat16, layout="wide")
     for args in ((q, k, cos, sin, pos, gq, gk, 1e-5, True), (q, None, cos, sin), (None, k, cos, sin, pos, None, gk)):
         assert ctx._quick("qk_norm_rope", *(args + (None,) * (7 - len(args)) + (1e-6, False) if len(args) < 9 else args)) is not None
