@@ -276,7 +276,9 @@ template <int BITS, bool GBF16>
 __global__ void __launch_bounds__(AW_THREADS, BITS == 8 ? 10 : 8)
 adamw_multi_kernel(const AdamwUnit* __restrict__ units, const void* const* __restrict__ grads, AdamwStep a,
                    int* __restrict__ status) {
-  const AdamwUnit s = units[blockIdx.x];
+  const AdamwUnit s = units[blockIdx.x];      // written before the first launch: needs no wait
+  grid_wait();
+  grid_release();
   const void* g = s.grad;
   if (grads) g = reinterpret_cast<const uint8_t*>(grads[s.tensor]) + s.first * (GBF16 ? 2 : 4);
   const bool aligned =
@@ -291,6 +293,8 @@ adamw_multi_kernel(const AdamwUnit* __restrict__ units, const void* const* __res
 __global__ void __launch_bounds__(AW_THREADS)
 adamw_moments_kernel(const AdamwUnit* __restrict__ units, float* __restrict__ m, float* __restrict__ v) {
   const AdamwUnit& s = units[blockIdx.x];
+  grid_wait();
+  grid_release();
   const int blk = threadIdx.x >> 5;
   if (blk * MULOCO_ADAMW_BLOCK >= s.n) return;
   const float sc1 = s.scale1[blk], sc2 = s.scale2[blk];
@@ -320,22 +324,18 @@ adamw_moments_kernel(const AdamwUnit* __restrict__ units, float* __restrict__ m,
 
 uint32_t adamw_dither(uint32_t seed, int64_t step) { return hash32(hash32(seed) + (uint32_t)step); }
 
-void launch_adamw_multi(cudaStream_t st, const AdamwUnit* units, const void* const* grads, int64_t n_units,
-                        int state_bits, int g_is_bf16, const AdamwStep& a, int* status) {
-  if (n_units <= 0) return;
-  const unsigned grid = (unsigned)n_units;   // one unit per block, in address order
-  if (state_bits == 8) {
-    if (g_is_bf16) adamw_multi_kernel<8, true><<<grid, AW_THREADS, 0, st>>>(units, grads, a, status);
-    else adamw_multi_kernel<8, false><<<grid, AW_THREADS, 0, st>>>(units, grads, a, status);
-  } else {
-    if (g_is_bf16) adamw_multi_kernel<32, true><<<grid, AW_THREADS, 0, st>>>(units, grads, a, status);
-    else adamw_multi_kernel<32, false><<<grid, AW_THREADS, 0, st>>>(units, grads, a, status);
-  }
+cudaError_t launch_adamw_multi(cudaStream_t st, const AdamwUnit* units, const void* const* grads, int64_t n_units,
+                               int state_bits, int g_is_bf16, const AdamwStep& a, int* status) {
+  if (n_units <= 0) return cudaSuccess;
+  const auto kernel = state_bits == 8 ? (g_is_bf16 ? adamw_multi_kernel<8, true> : adamw_multi_kernel<8, false>)
+                                      : (g_is_bf16 ? adamw_multi_kernel<32, true> : adamw_multi_kernel<32, false>);
+  // one unit per block, in address order
+  return launch_dependent(kernel, (unsigned)n_units, AW_THREADS, 0, st, units, grads, a, status);
 }
 
-void launch_adamw_moments(cudaStream_t st, const AdamwUnit* units, int64_t n_units, float* m, float* v) {
-  if (n_units <= 0) return;
-  adamw_moments_kernel<<<(unsigned)n_units, AW_THREADS, 0, st>>>(units, m, v);
+cudaError_t launch_adamw_moments(cudaStream_t st, const AdamwUnit* units, int64_t n_units, float* m, float* v) {
+  if (n_units <= 0) return cudaSuccess;
+  return launch_dependent(adamw_moments_kernel, (unsigned)n_units, AW_THREADS, 0, st, units, m, v);
 }
 
 }  // namespace muloco

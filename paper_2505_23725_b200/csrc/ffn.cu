@@ -136,12 +136,6 @@ __device__ __forceinline__ void load_row32(const __nv_bfloat16* row, uint32_t (&
   }
 }
 
-// Programmatic dependent launch: wait until the kernel before this one in the stream is complete and its results
-// can be seen; let the next kernel's blocks start (their own wait holds them before they touch memory).  A
-// kernel releases only after its wait, so whatever starts early knows everything before this kernel complete.
-__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-
 // act(g) = g sigma and, for the backward pass, its slope.  sigma is the logistic function of g (silu) or of
 // 2 sqrt(2 / pi) (g + 0.044715 g^3), which makes g sigma the tanh form of gelu.  exp and the quotient are the fast ones (a few
 // units in the last place of float32): the results are rounded to 8 bits of mantissa.

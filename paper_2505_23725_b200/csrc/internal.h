@@ -184,6 +184,30 @@ void ctx_count_launches(muloco_ctx* c, int n);
 // (zero between launches).  Allocated on first use; nullptr when that fails.
 float* ctx_qk_scratch(muloco_ctx* c, int** tickets);
 
+// Programmatic dependent launch: a kernel launched so may start while the one before it in the stream still
+// runs.  grid_wait: until that one is complete and its results can be seen.  grid_release: lets the next kernel start
+// (if it was launched so; its own grid_wait holds it back).  Every kernel releases only after its wait, so
+// whatever starts early knows everything before its predecessor complete.
+#ifdef __CUDACC__
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_dependent(void (*kernel)(P...), unsigned grid, unsigned threads, size_t smem, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+#endif
+
 // AdamW over many tensors (include/muloco.h has the layout of the states): one entry per work unit of ADAMW_UNIT
 // consecutive elements of a tensor, with everything a block needs, so that its first load names all the others.
 constexpr int ADAMW_UNIT = 4 * MULOCO_ADAMW_BLOCK;
@@ -209,9 +233,9 @@ struct AdamwStep {
 };
 uint32_t adamw_dither(uint32_t seed, int64_t step);   // what step `step` adds to the element index before hashing
 // grads[tensor]: the gradients of this step, or NULL for those in the units
-void launch_adamw_multi(cudaStream_t st, const AdamwUnit* units, const void* const* grads, int64_t n_units,
+cudaError_t launch_adamw_multi(cudaStream_t st, const AdamwUnit* units, const void* const* grads, int64_t n_units,
                         int state_bits, int g_is_bf16, const AdamwStep& a, int* status);
-void launch_adamw_moments(cudaStream_t st, const AdamwUnit* units, int64_t n_units, float* m, float* v);
+cudaError_t launch_adamw_moments(cudaStream_t st, const AdamwUnit* units, int64_t n_units, float* m, float* v);
 
 // Query / key norm with rotation.  One of the two tensors of a call:
 struct QkTensor {

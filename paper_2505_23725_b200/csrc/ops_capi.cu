@@ -137,6 +137,8 @@ MULOCO_API muloco_status muloco_adamw_create(muloco_ctx* c, const muloco_adamw_c
     if ((e = cudaMalloc(&o->d_units, table.size() * sizeof(AdamwUnit))) != cudaSuccess) return bail(e, "unit table");
     if ((e = cudaMalloc(&o->d_grads, n * sizeof(void*))) != cudaSuccess) return bail(e, "gradient table");
     if ((e = cudaMemcpy(o->d_units, table.data(), table.size() * sizeof(AdamwUnit), cudaMemcpyHostToDevice)) != cudaSuccess) return bail(e, "unit table");
+    // the copy above may still be on its way from a staging buffer: the kernels read the table without waiting for anything
+    if ((e = cudaStreamSynchronize(nullptr)) != cudaSuccess) return bail(e, "unit table");
     for (int i = 0; i < GRAD_RING; ++i) {
       if ((e = cudaMallocHost((void**)&o->h_grads[i], n * sizeof(void*))) != cudaSuccess) return bail(e, "pinned gradient table");
       if ((e = cudaEventCreateWithFlags(&o->ev[i], cudaEventDisableTiming)) != cudaSuccess) return bail(e, "event");
@@ -181,8 +183,7 @@ MULOCO_API muloco_status muloco_adamw_step(muloco_adamw* o, const void* const* g
   a.inv_bc1 = (float)(1.0 / bc1);
   a.inv_sqrt_bc2 = (float)(1.0 / sqrt(bc2));
   a.dither = adamw_dither(f.seed, step);
-  launch_adamw_multi(v.st, o->d_units, table, o->n_units, f.state_bits, f.grad_dtype == MULOCO_BF16, a, v.status);
-  OPS_CK(cudaGetLastError());
+  OPS_CK(launch_adamw_multi(v.st, o->d_units, table, o->n_units, f.state_bits, f.grad_dtype == MULOCO_BF16, a, v.status));
   ctx_count_launches(c, 1);
   return MULOCO_OK;
 }
@@ -195,8 +196,7 @@ MULOCO_API muloco_status muloco_adamw_moments(muloco_adamw* o, float* m, float* 
   if (!m || !v) return ctx_fail(c, MULOCO_EINVAL, "m or v is NULL");
   if (misaligned(m, 16) || misaligned(v, 16)) return ctx_fail(c, MULOCO_EINVAL, "m and v must be 16-byte aligned");
   const CtxView w = ctx_view(c);
-  launch_adamw_moments(w.st, o->d_units, o->n_units, m, v);
-  OPS_CK(cudaGetLastError());
+  OPS_CK(launch_adamw_moments(w.st, o->d_units, o->n_units, m, v));
   ctx_count_launches(c, 1);
   return MULOCO_OK;
 }

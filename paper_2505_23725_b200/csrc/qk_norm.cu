@@ -266,6 +266,8 @@ qk_norm_kernel(const __grid_constant__ QkArgs p, int ctas0, int G, int split0, i
   const int heads = t.heads;
   const float inv_dim = 1.0f / (float)p.dim;
 
+  grid_wait();
+  grid_release();
   // the gains, in the order of the pairs' first and second entries per chunk (neighbouring pairs: apart)
   __shared__ __align__(16) float gains[2][QK_MAX_DIM / 2];
   for (int i = threadIdx.x; i < pairs; i += QK_THREADS) {
@@ -661,8 +663,7 @@ cudaError_t launch_one(cudaStream_t st, const QkArgs& a, int n_sms, int G) {
     const int64_t need = (a.tokens * split[w] + QK_WARPS - 1) / QK_WARPS;
     ctas[w] = (int)(need < share ? need : share);
   }
-  kernel<<<ctas[0] + ctas[1], QK_THREADS, smem, st>>>(a, ctas[0], G, split[0], split[1]);
-  return cudaGetLastError();
+  return launch_dependent(kernel, (unsigned)(ctas[0] + ctas[1]), QK_THREADS, smem, st, a, ctas[0], G, split[0], split[1]);
 }
 
 template <typename T, int V, int NC>
