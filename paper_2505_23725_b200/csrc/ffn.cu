@@ -896,15 +896,18 @@ cudaError_t launch_few(cudaStream_t st, const FfnArgs& a, int epi, const FewOper
 
 int slabs_of(int64_t k) { return (int)((k + BK - 1) / BK); }
 
-// Whether a pass takes the few-token form: while its widest product has at most a tile of 128 x 128 per SM, up to 512
-// tokens, or any number while that product is small.  Whole pass, us, few-token form / 256 x 256 tiles, forward and
-// backward: 256 tokens 19 / 25 and 27 / 42 (768 x 2048), 38 / 54 and 78 / 113 (2048 x 5632); 512 tokens 24 / 26
-// and 33 / 42, 27 / 32 and 45 / 53 (1024 x 2816), 69 / 66 and 123 / 116 (2048 x 5632, 176 tiles); 768 tokens
-// 31 / 26 and 49 / 45 (768 x 2048, 96 tiles).
-bool few_tokens(const FfnArgs& a) {
-  const int64_t N = a.F > a.d ? a.F : a.d;
+// Whether a product of T x N results takes the few-token form: while it has at most a tile of 128 x 128 per SM, up to
+// `tokens` tokens, or any number of them while it has at most `tiles` tiles.  Whole pass in us, one side / the other:
+//   gated product, few-token form / 256 x 256 tiles: 100 tokens 14 / 25 (768 x 2048), 34 / 54 (2048 x 5632); 256 tokens
+//     19 / 17, 38 / 33; 512 tokens 24 / 19, 17 / 14 (360 x 848)
+//   Y = H W2: 600 tokens 19 / 26 (768 x 2048, 30 tiles), 1500 tokens 29 / 31 (72 tiles), 38 / 39 (1024 x 2816, 96 tiles)
+//   dG and dU: 2048 tokens at 744 x 424 (64 tiles) 33 / 48; 1500 at 360 x 848 (84 tiles) 40 / 41
+//   dX: 3000 tokens at 360 x 848 (72 tiles) 53 / 40; 1024 at 768 x 2048 (48 tiles) 47 / 47
+struct FewLimit { int64_t tokens, tiles; };
+constexpr FewLimit FEW_GATE = {128, 0}, FEW_DOWN = {512, 100}, FEW_GATE_BACK = {512, 64}, FEW_DX = {512, 64};
+bool few_tokens(const FfnArgs& a, int64_t N, FewLimit limit) {
   const int64_t tiles = (N + 127) / 128 * ((a.T + 127) / 128);
-  return tiles <= a.n_sms && (a.T <= 512 || tiles <= 64);
+  return tiles <= a.n_sms && (a.T <= limit.tokens || tiles <= limit.tiles);
 }
 
 }  // namespace
@@ -912,25 +915,15 @@ bool few_tokens(const FfnArgs& a) {
 cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
   cudaError_t bound = bind_context(what);
   if (bound != cudaSuccess) return bound;
-  if (few_tokens(a)) {
+  if (few_tokens(a, a.F, FEW_GATE)) {
     FewParams p;
     memset(&p, 0, sizeof p);
     p.M = (int)a.F; p.slabs0 = p.slabs = slabs_of(a.d);
     p.out = a.h; p.out2 = a.g; p.out3 = a.u;
     FewOperand q{{Mat{a.w1, a.d, a.F, a.ldw1}, Mat{a.w3, a.d, a.F, a.ldw3}}, {Mat{a.x, a.T, a.d, a.ldx}, Mat{}}};
-    cudaError_t e = launch_few(st, a, EPI_GATE, q, true, 1, p, what);
+    const cudaError_t e = launch_few(st, a, EPI_GATE, q, true, 1, p, what);
     if (e != cudaSuccess) return e;
-    ++*launches;
-    memset(&p, 0, sizeof p);
-    p.M = (int)a.d; p.slabs0 = p.slabs = slabs_of(a.F);
-    p.out = a.y;
-    p.weights_early = 1;
-    FewOperand r{{Mat{a.w2, a.F, a.d, a.ldw2}, Mat{}}, {Mat{a.h, a.T, a.F, a.F}, Mat{}}};
-    e = launch_few(st, a, EPI_STORE, r, true, 1, p, what);
-    if (e == cudaSuccess) ++*launches;
-    return e;
-  }
-  {
+  } else {
     Builder b;
     Prob& q = b.add(a.T, a.F, 128, a.d, 0);
     q.map_a[0] = b.kmajor(Mat{a.x, a.T, a.d, a.ldx});
@@ -940,17 +933,28 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
     q.map_b[1] = b.mnmajor(Mat{a.w3, a.d, a.F, a.ldw3}, &wide3);
     b.ok = b.ok && wide3 == q.b_wide;
     q.out = a.h; q.out2 = a.g; q.out3 = a.u;
-    cudaError_t e = launch_built(st, b, a, EPI_GATE, what);
+    const cudaError_t e = launch_built(st, b, a, EPI_GATE, what);
     if (e != cudaSuccess) return e;
-    ++*launches;
   }
-  Builder b;
-  Prob& q = b.add(a.T, a.d, BN, a.F, 0);
-  q.map_a[0] = b.kmajor(Mat{a.h, a.T, a.F, a.F});
-  q.b_mn = 1;
-  q.map_b[0] = b.mnmajor(Mat{a.w2, a.F, a.d, a.ldw2}, &q.b_wide);
-  q.out = a.y;
-  cudaError_t e = launch_built(st, b, a, EPI_STORE, what);
+  ++*launches;
+  cudaError_t e;
+  if (few_tokens(a, a.d, FEW_DOWN)) {
+    FewParams p;
+    memset(&p, 0, sizeof p);
+    p.M = (int)a.d; p.slabs0 = p.slabs = slabs_of(a.F);
+    p.out = a.y;
+    p.weights_early = 1;
+    FewOperand r{{Mat{a.w2, a.F, a.d, a.ldw2}, Mat{}}, {Mat{a.h, a.T, a.F, a.F}, Mat{}}};
+    e = launch_few(st, a, EPI_STORE, r, true, 1, p, what);
+  } else {
+    Builder b;
+    Prob& q = b.add(a.T, a.d, BN, a.F, 0);
+    q.map_a[0] = b.kmajor(Mat{a.h, a.T, a.F, a.F});
+    q.b_mn = 1;
+    q.map_b[0] = b.mnmajor(Mat{a.w2, a.F, a.d, a.ldw2}, &q.b_wide);
+    q.out = a.y;
+    e = launch_built(st, b, a, EPI_STORE, what);
+  }
   if (e == cudaSuccess) ++*launches;
   return e;
 }
@@ -958,8 +962,8 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
 cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
   cudaError_t bound = bind_context(what);
   if (bound != cudaSuccess) return bound;
-  const bool few = few_tokens(a);
-  if ((a.dx || a.dw1 || a.dw3) && few) {
+  const bool few = few_tokens(a, a.d, FEW_DX);
+  if ((a.dx || a.dw1 || a.dw3) && few_tokens(a, a.F, FEW_GATE_BACK)) {
     FewParams p;
     memset(&p, 0, sizeof p);
     p.M = (int)a.F; p.slabs0 = p.slabs = slabs_of(a.d);
