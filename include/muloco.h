@@ -439,7 +439,7 @@ MULOCO_API muloco_status muloco_qk_norm_rope_backward(muloco_ctx* ctx, const mul
  * Sums are float32, every result is rounded once (Y from the rounded H).
  * ld*: row strides in elements (G, U, H, Y dense).  d, F and the strides are multiples of 8 and the
  * matrices 16-byte aligned (MULOCO_ESHAPE / MULOCO_EINVAL otherwise); tokens may be 0.
- * The kernels are persistent but their thread blocks do not wait for one another. */
+ * Thread blocks wait for one another only inside a cluster (at most eight). */
 enum { MULOCO_ACT_SILU = 0, MULOCO_ACT_GELU = 1 };
 typedef struct {
   int64_t tokens, d, F;

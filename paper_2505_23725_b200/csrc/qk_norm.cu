@@ -9,8 +9,11 @@
 //   p < rot / 2, halves        : (p, p + rot / 2)
 //   otherwise                  : (2 p, 2 p + 1)      (interleaved pairs, and the entries that are not rotated)
 // so both members of a pair are in one lane and the rotation needs no exchange; a chunk is two vectors of V
-// elements.  32 / G heads of one token fit a warp at a time; the warp keeps the token's cosines and sines in
-// registers while it walks over the token's heads, and the gains while it walks over tokens.
+// elements.  32 / G heads of one token fit a warp at a time; the warp keeps what the token's cosines and sines (and, forward, the
+// gains) make of a pair in registers while it walks over the token's heads.
+//
+// Measured at 16384 tokens, 16 + 16 heads of 128, bf16: forward 45 us (6.2 TB/s, issue slots 62 % taken), backward 76 us (5.4 TB/s; 158
+// registers leave 12 warps per SM).
 #include <string.h>
 
 #include <type_traits>
