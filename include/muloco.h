@@ -350,7 +350,9 @@ MULOCO_API muloco_status muloco_pseudogradient(muloco_ctx* ctx, int32_t tensor, 
  *   tensors are laid out one after the other, each padded to whole blocks, and hash = Mueller's 32-bit
  *   integer hash (twice: x ^= x >> 16, x *= 0x45d9f3b; then x ^= x >> 16).  Results do not depend on
  *   the launch: the same call gives the same bits.
- * A non-finite gradient raises MULOCO_ENONFINITE (the step is still applied).
+ * A non-finite gradient raises MULOCO_ENONFINITE (the step is still applied).  With 8-bit states the
+ * block's scales are then NaN, and so are its moments from there on and its parameters from the next step on; the
+ * same holds where v overflows float32.  Every further step of such a block raises MULOCO_ENONFINITE again.
  * Gradients and parameters may have any alignment of their type (16 bytes is fastest); state1 and
  * state2 must be 16-byte aligned, scales 4-byte aligned. */
 typedef struct muloco_adamw muloco_adamw; /* opaque: a list of tensors and their device tables */

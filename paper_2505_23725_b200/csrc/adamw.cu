@@ -142,7 +142,7 @@ __device__ __forceinline__ uint32_t pack_bytes(float a, float b, float c, float 
 }
 
 // One block of 256 elements by one warp.  FULL: all of them exist and every access is aligned.  Returns whether a
-// gradient was not finite.
+// gradient was not finite, or (8-bit states) the block's new moments are not.
 template <int BITS, bool GBF16, bool FULL>
 __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, int blk, const AdamwStep& a) {
   const int lane = threadIdx.x & 31;
@@ -176,7 +176,9 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
   float sc1 = 0.f, sc2 = 0.f;
   if (BITS == 8) { sc1 = s.scale1[blk]; sc2 = s.scale2[blk]; }
 
-  Pair finite = both(0.f);                      // 0 * g summed: NaN as soon as one gradient is not finite
+  // 0 * x summed is NaN as soon as one x is not finite; x = g, and with 8-bit states m, which is not finite when g or the block's
+  // scale is not (the maxima below pass over NaN)
+  Pair finite = both(0.f);
   float max1 = 0.f, max2 = 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -191,7 +193,7 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
 #pragma unroll
     for (int e = 0; e < 4; e += 2) {
       const Pair g2 = pair(gr[h].x[e], gr[h].x[e + 1]);
-      finite = fma2(g2, both(0.f), finite);
+      if (BITS == 32) finite = fma2(g2, both(0.f), finite);
       Pair mn;
       float2 root;
       if (BITS == 8) {
@@ -199,6 +201,7 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
         const Pair mo = mul2(add2(pair(byte_bits(c1[h], e), byte_bits(c1[h], e + 1)), both(-(AW_2P23 + 128.0f))), both(sc1));
         const Pair ro = mul2(add2(pair(byte_bits(c2[h], e), byte_bits(c2[h], e + 1)), both(-AW_2P23)), both(sc2));
         mn = add2(mul2_alone(mo, both(a.beta1)), mul2_alone(g2, both(om1)));
+        finite = fma2(mn, both(0.f), finite);
         const float2 vn = parts(add2(mul2_alone(mul2(ro, ro), both(a.beta2)), mul2_alone(mul2(g2, g2), both(om2))));
         root = make_float2(__fsqrt_rn(vn.x), __fsqrt_rn(vn.y));
         const float2 mp = parts(mn);
@@ -224,14 +227,17 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
     }
   }
   const float2 fin = parts(finite);
-  const bool bad = __any_sync(0xffffffffu, !(fin.x + fin.y == 0.f));
+  bool bad = __any_sync(0xffffffffu, !(fin.x + fin.y + 0.f * sc2 == 0.f));
 
   float inv1 = 0.f, inv2 = 0.f;
   if (BITS == 8) {
     // bits of non-negative floats order like integers: one integer maximum per moment
     max1 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(max1)));
     max2 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(max2)));
-    if (bad) max1 = max2 = __int_as_float(0x7fffffff);      // such a block's moments are NaN from here on
+    bad = bad || max2 == __int_as_float(0x7f800000);        // a square beyond float32
+    // Such a block's scales are NaN, and so are its moments: this step's and, because a NaN scale makes m NaN, those of every
+    // step to come, each of which reports it again.
+    if (bad) max1 = max2 = __int_as_float(0x7fffffff);
     // even lanes deal with the first moment's scale, odd lanes with the second's: one division for both
     const bool odd = lane & 1;
     const float mx = odd ? max2 : max1;

@@ -1337,7 +1337,7 @@ MULOCO_API muloco_status muloco_sync_status(muloco_ctx* c) {
   if (h & ST_BOUNDS) return fail(c, MULOCO_ECUDA, "a kernel rejected an out-of-range index");
   if (h & ST_POSITION) return fail(c, MULOCO_EINVAL, "a position lies outside the rotation's table");
   if (h & ST_NONFINITE)
-    return fail(c, MULOCO_ENONFINITE, "non-finite value: a pseudogradient, the Newton-Schulz input of a hidden matrix, or a gradient given to AdamW");
+    return fail(c, MULOCO_ENONFINITE, "non-finite value: a pseudogradient, the Newton-Schulz input of a hidden matrix, a gradient given to AdamW, or a moment of its 8-bit states");
   return MULOCO_OK;
 }
 

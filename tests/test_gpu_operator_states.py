@@ -1,0 +1,57 @@
+"""AdamW lists: blocks of 8-bit states after a value that is not finite."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+HYPER = dict(lr=1e-2, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.1)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    from paper_2505_23725_b200 import binding
+    c = binding.Context("cuda:0")
+    yield c
+    c.close()
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -1e25])      # (the square of the last is beyond float32)
+@pytest.mark.parametrize("at", [700, 999])                                  # inside a whole block, and in the short last one
+def test_8_bit_block_stays_nan_and_is_reported_every_step(ctx, value, at, bf16):
+    """The scales that a block's elements share turn NaN, so by the formulas its moments are NaN at every later step and its
+    parameters from the next one on; each step says so, and the other blocks know nothing of it."""
+    import torch
+    from paper_2505_23725_b200 import binding
+    n, blk = 1000, at // 256
+    dt = torch.bfloat16 if bf16 else torch.float32
+    torch.manual_seed(0)
+    grads = [(torch.randn(n, device="cuda") * 1e-2).to(dt) for _ in range(4)]
+    hit = [g.clone() for g in grads]
+    hit[1][at] = value
+    p, q = torch.ones(n, device="cuda"), torch.ones(n, device="cuda")
+    good = binding.AdamW(ctx, [p], state_bits=8, seed=3, grad_dtype=dt, **HYPER)
+    bad = binding.AdamW(ctx, [q], state_bits=8, seed=3, grad_dtype=dt, **HYPER)
+    inside = torch.arange(n, device="cuda") // 256 == blk
+    for t in range(4):
+        good.step([grads[t]])
+        ctx.sync_status()
+        bad.step([hit[t]])
+        if t == 0:
+            ctx.sync_status()
+            assert torch.equal(p, q)
+            continue
+        with pytest.raises(binding.MulocoError) as e:
+            ctx.sync_status()
+        assert e.value.status == binding.ENONFINITE
+        assert torch.isnan(bad.scale1[blk]) and torch.isnan(bad.scale2[blk])
+        m, v = bad.moments()
+        assert torch.isnan(m[:n][inside]).all() and torch.isnan(v[:n][inside]).all()
+        if t > 1:
+            assert torch.isnan(q[inside]).all()
+        m0, v0 = good.moments()
+        assert torch.equal(q[~inside], p[~inside])
+        assert torch.equal(m[:n][~inside], m0[:n][~inside]) and torch.equal(v[:n][~inside], v0[:n][~inside])
+        others = torch.arange(4, device="cuda") != blk
+        assert torch.equal(bad.scale1[others], good.scale1[others]) and torch.equal(bad.scale2[others], good.scale2[others])
+    good.close()
+    bad.close()
