@@ -129,6 +129,12 @@ __device__ __forceinline__ float half_bits(uint32_t w, int h) {      // low (h =
   return __uint_as_float(__byte_perm(w, 0x4B000000u, h ? 0x7432u : 0x7410u));
 }
 constexpr float AW_2P23 = 8388608.0f;
+// The larger of two, NaN when one of them is NaN (its bits, 0x7fffffff, are above those of every number).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 __device__ __forceinline__ float rcp_fast(float x) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
@@ -176,9 +182,7 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
   float sc1 = 0.f, sc2 = 0.f;
   if (BITS == 8) { sc1 = s.scale1[blk]; sc2 = s.scale2[blk]; }
 
-  // 0 * x summed is NaN as soon as one x is not finite; x = g, and with 8-bit states m, which is not finite when g or the block's
-  // scale is not (the maxima below pass over NaN)
-  Pair finite = both(0.f);
+  Pair finite = both(0.f);                      // 32-bit states: 0 * g summed, NaN as soon as one gradient is not finite
   float max1 = 0.f, max2 = 0.f;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -201,14 +205,13 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
         const Pair mo = mul2(add2(pair(byte_bits(c1[h], e), byte_bits(c1[h], e + 1)), both(-(AW_2P23 + 128.0f))), both(sc1));
         const Pair ro = mul2(add2(pair(byte_bits(c2[h], e), byte_bits(c2[h], e + 1)), both(-AW_2P23)), both(sc2));
         mn = add2(mul2_alone(mo, both(a.beta1)), mul2_alone(g2, both(om1)));
-        finite = fma2(mn, both(0.f), finite);
         const float2 vn = parts(add2(mul2_alone(mul2(ro, ro), both(a.beta2)), mul2_alone(mul2(g2, g2), both(om2))));
         root = make_float2(__fsqrt_rn(vn.x), __fsqrt_rn(vn.y));
         const float2 mp = parts(mn);
         m[h].x[e] = mp.x; m[h].x[e + 1] = mp.y;
         v[h].x[e] = root.x; v[h].x[e + 1] = root.y;       // the root is what is encoded
-        max1 = fmaxf(max1, fmaxf(fabsf(mp.x), fabsf(mp.y)));
-        max2 = fmaxf(max2, fmaxf(root.x, root.y));
+        max1 = max_nan(max1, max_nan(fabsf(mp.x), fabsf(mp.y)));
+        max2 = max_nan(max2, max_nan(root.x, root.y));
       } else {
         mn = fma2(pair(m[h].x[e], m[h].x[e + 1]), both(a.beta1), mul2(g2, both(om1)));
         const float2 vn = parts(fma2(pair(v[h].x[e], v[h].x[e + 1]), both(a.beta2), mul2(mul2(g2, g2), both(om2))));
@@ -226,17 +229,20 @@ __device__ __forceinline__ bool adamw_block(const AdamwUnit& s, const void* g, i
       th[h].x[e] = tn.x; th[h].x[e + 1] = tn.y;
     }
   }
-  const float2 fin = parts(finite);
-  bool bad = __any_sync(0xffffffffu, !(fin.x + fin.y + 0.f * sc2 == 0.f));
+  bool bad = false;
+  if (BITS == 32) {
+    const float2 fin = parts(finite);
+    bad = __any_sync(0xffffffffu, !(fin.x + fin.y == 0.f));
+  }
 
   float inv1 = 0.f, inv2 = 0.f;
   if (BITS == 8) {
-    // bits of non-negative floats order like integers: one integer maximum per moment
+    // bits of non-negative floats order like integers, those of infinity and NaN above the rest: one integer maximum per moment
     max1 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(max1)));
     max2 = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(max2)));
-    bad = bad || max2 == __int_as_float(0x7f800000);        // a square beyond float32
-    // Such a block's scales are NaN, and so are its moments: this step's and, because a NaN scale makes m NaN, those of every
-    // step to come, each of which reports it again.
+    // A gradient that is not finite, a scale that was not, a square beyond float32: the block's scales are NaN, and so are its
+    // moments, this step's and those of every step to come, each of which reports it again.
+    bad = !(max1 < __int_as_float(0x7f800000) && max2 < __int_as_float(0x7f800000));
     if (bad) max1 = max2 = __int_as_float(0x7fffffff);
     // even lanes deal with the first moment's scale, odd lanes with the second's: one division for both
     const bool odd = lane & 1;
