@@ -1,10 +1,31 @@
 """The operators of the training step as torch autograd functions.
 
 `owner` is a binding.Context or a binding.MuLoCo.  The backward passes are the library's own kernels; nothing
-is computed twice and nothing else is kept than what their docstrings in binding.py name."""
+is computed twice and nothing else is kept than what their docstrings in binding.py name.  They are differentiable once,
+in reverse mode: what would need more raises."""
 from __future__ import annotations
 
 import torch
+
+
+class _Once(torch.autograd.Function):
+    """Hands results on; going back through them raises."""
+
+    @staticmethod
+    def forward(ctx, name, n, *tensors):
+        ctx.name = name
+        return tuple(None if t is None else t.view_as(t) for t in tensors[:n])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{ctx.name} is differentiable once: the gradients of its gradients are not implemented")
+
+
+def _once(name, results, inputs):
+    """The results of a backward pass, which are functions of `inputs` without a graph.  Where a graph is being recorded
+    (create_graph=True) they get one that raises, so that a loss made from them cannot lose their part silently.  (torch's
+    once_differentiable looks at the incoming gradients only: those of y.sum() need none.)"""
+    return _Once.apply(name, len(results), *results, *inputs) if torch.is_grad_enabled() else results
 
 
 class _GatedFFN(torch.autograd.Function):
@@ -19,7 +40,8 @@ class _GatedFFN(torch.autograd.Function):
     def backward(ctx, dy):
         x, w1, w3, w2, *saved = ctx.saved_tensors
         dy = dy if dy.stride(1) == 1 else dy.contiguous()
-        return (None, None, *ctx.owner.gated_ffn_backward(dy, x, w1, w3, w2, tuple(saved), ctx.activation))
+        grads = ctx.owner.gated_ffn_backward(dy, x, w1, w3, w2, tuple(saved), ctx.activation)
+        return (None, None, *_once("gated_ffn", grads, (dy, x, w1, w3, w2)))
 
 
 def gated_ffn(owner, x, w1, w3, w2, activation: str = "silu"):
@@ -43,8 +65,8 @@ class _QKNormRope(torch.autograd.Function):
     def backward(ctx, dq, dk):
         q, k, cos, sin, positions, gain_q, gain_k = ctx.saved_tensors
         dq, dk = (d if d.stride(2) == 1 else d.contiguous() for d in (dq, dk))
-        dq, dk, dgq, dgk = ctx.owner.qk_norm_rope_backward(dq, dk, q, k, cos, sin, positions, gain_q, gain_k, ctx.eps,
-                                                           ctx.interleaved)
+        grads = ctx.owner.qk_norm_rope_backward(dq, dk, q, k, cos, sin, positions, gain_q, gain_k, ctx.eps, ctx.interleaved)
+        dq, dk, dgq, dgk = _once("qk_norm_rope", grads, (dq, dk, q, k, cos, sin, gain_q, gain_k))
         return (None, None, None, dq, dk, None, None, None, dgq if gain_q is not None else None,
                 dgk if gain_k is not None else None)
 

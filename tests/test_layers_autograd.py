@@ -1,0 +1,112 @@
+"""layers.py without a GPU: what the autograd forms pass on, refuse and hand out, over a stand-in owner that computes the
+operators in plain torch and takes only the layouts that the library takes."""
+import pytest
+import torch
+from torch.autograd import forward_ad
+
+from paper_2505_23725_b200 import layers
+
+
+def _silu_parts(g):
+    s = torch.sigmoid(g)
+    return g * s, s * (1 + g * (1 - s))
+
+
+class Owner:
+    """float64 in place of bf16; a layout that the library would answer with an error raises."""
+
+    def _rows(self, t):
+        t_ok = t.stride(1) == 1 and t.data_ptr() % 16 == 0 and t.shape[1] % 8 == 0
+        if not t_ok or (t.shape[0] > 1 and (t.stride(0) < t.shape[1] or t.stride(0) % 8 != 0)):
+            raise RuntimeError(f"ESHAPE: strides {t.stride()}")
+
+    def gated_ffn(self, x, w1, w3, w2, activation="silu", save=True):
+        for t in (x, w1, w3, w2):
+            self._rows(t)
+        with torch.no_grad():
+            g, u = x.detach() @ w1.detach(), x.detach() @ w3.detach()
+            h = _silu_parts(g)[0] * u
+            return h @ w2.detach(), ((g, u, h) if save else None)
+
+    def gated_ffn_backward(self, dy, x, w1, w3, w2, saved, activation="silu"):
+        for t in (dy, x, w1, w3, w2):
+            self._rows(t)
+        with torch.no_grad():
+            dy, x, w1, w3, w2 = (t.detach() for t in (dy, x, w1, w3, w2))
+            g, u, h = saved
+            value, slope = _silu_parts(g)
+            dh = dy @ w2.T
+            dg, du = dh * u * slope, dh * value
+            return dg @ w1.T + du @ w3.T, x.T @ dg, x.T @ du, h.T @ dy
+
+    # the "norm" of the stand-in: x -> gain * x
+    def qk_norm_rope(self, q, k, cos, sin, positions=None, gain_q=None, gain_k=None, eps=1e-6, interleaved=False):
+        with torch.no_grad():
+            return tuple(None if x is None else x * (1 if g is None else g) for x, g in ((q, gain_q), (k, gain_k)))
+
+    def qk_norm_rope_backward(self, dq, dk, q, k, cos, sin, positions=None, gain_q=None, gain_k=None, eps=1e-6, interleaved=False):
+        out, gains = [], []
+        with torch.no_grad():
+            for d, x, g in ((dq, q, gain_q), (dk, k, gain_k)):
+                assert (d is None) == (x is None)
+                assert d is None or d.stride(2) == 1
+                out.append(None if x is None else d * (1 if g is None else g))
+                gains.append(None if x is None else (d * x).sum((0, 1)))
+        return (*out, *gains)
+
+
+def _tensors(T=3, d=8, F=16, grad=True):
+    torch.manual_seed(0)
+    return [(torch.randn(*s, dtype=torch.float64) / 2).requires_grad_(grad) for s in ((T, d), (d, F), (d, F), (F, d))]
+
+
+def _plain(x, w1, w3, w2):
+    return (_silu_parts(x @ w1)[0] * (x @ w3)) @ w2
+
+
+def _qk(T=3, h=2, D=4, grad=True):
+    torch.manual_seed(1)
+    q, k = (torch.randn(T, h, D, dtype=torch.float64, requires_grad=grad) for _ in range(2))
+    gq, gk = (torch.randn(D, dtype=torch.float64, requires_grad=grad) for _ in range(2))
+    return q, k, torch.ones(T, D // 2), torch.zeros(T, D // 2), None, gq, gk
+
+
+# -- second derivatives -------------------------------------------------------------------------
+@pytest.mark.parametrize("loss", [lambda y: y.sum(), lambda y: y.square().sum()], ids=["linear", "square"])
+def test_second_derivatives_are_refused_not_dropped(loss):
+    """The backward kernels have no graph of their own.  A gradient taken with create_graph=True can be used as a number,
+    but differentiating it says so instead of returning a gradient without that term."""
+    args = _tensors()
+    y = layers.gated_ffn(Owner(), *args)
+    grads = torch.autograd.grad(loss(y), args, create_graph=True)
+    want = torch.autograd.grad(loss(_plain(*args)), args)
+    assert all(torch.allclose(a, b) for a, b in zip(grads, want))
+    penalty = sum(g.square().sum() for g in grads)
+    assert penalty.requires_grad
+    with pytest.raises(RuntimeError, match="once"):
+        (args[0].square().sum() + penalty).backward()
+
+    q, k, cos, sin, _, gq, gk = _qk()
+    a, b = layers.qk_norm_rope(Owner(), q, k, cos, sin, None, gq, gk)
+    grads = torch.autograd.grad(loss(a) + loss(b), (q, k, gq, gk), create_graph=True)
+    for g in grads:
+        assert g.requires_grad
+        with pytest.raises(RuntimeError, match="once"):
+            (q.sum() + g.sum()).backward(retain_graph=True)
+
+
+def test_first_derivatives_with_create_graph_reach_the_rest_of_the_graph():
+    """create_graph=True with the block in the graph: derivatives that do not pass through its gradient still work."""
+    x, *ws = _tensors()
+    z = torch.randn(3, 8, dtype=torch.float64, requires_grad=True)
+    loss = layers.gated_ffn(Owner(), x, *ws).sum() + (z ** 3).sum()
+    gx, gz = torch.autograd.grad(loss, (x, z), create_graph=True)
+    gz.sum().backward()
+    assert torch.allclose(z.grad, 6 * z) and torch.allclose(gx, torch.autograd.grad(_plain(x, *ws).sum(), x)[0])
+
+
+def test_first_derivatives():
+    args = _tensors()
+    layers.gated_ffn(Owner(), *args).square().sum().backward()
+    want = torch.autograd.grad(_plain(*args).square().sum(), args)
+    assert all(torch.allclose(t.grad, g) and not t.grad.requires_grad for t, g in zip(args, want))
