@@ -6,6 +6,7 @@ in reverse mode: what would need more raises."""
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 
 
 class _Once(torch.autograd.Function):
@@ -24,16 +25,20 @@ class _Once(torch.autograd.Function):
 def _once(name, results, inputs):
     """The results of a backward pass, which are functions of `inputs` without a graph.  Where a graph is being recorded
     (create_graph=True) they get one that raises, so that a loss made from them cannot lose their part silently.  (torch's
-    once_differentiable looks at the incoming gradients only: those of y.sum() need none.)"""
-    return _Once.apply(name, len(results), *results, *inputs) if torch.is_grad_enabled() else results
+    once_differentiable looks at the incoming gradients only: those of y.sum() need none.)  An incoming gradient with a
+    forward-mode tangent raises here, as a custom function's dual input does."""
+    if torch.is_grad_enabled() or any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in inputs):
+        return _Once.apply(name, len(results), *results, *inputs)
+    return results
 
 
 class _GatedFFN(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, owner, activation, x, w1, w3, w2):
-        y, saved = owner.gated_ffn(x, w1, w3, w2, activation)
+    def forward(ctx, owner, activation, save, x, w1, w3, w2):
+        y, saved = owner.gated_ffn(x, w1, w3, w2, activation, save=save)
         ctx.owner, ctx.activation = owner, activation
-        ctx.save_for_backward(x, w1, w3, w2, *saved)
+        if save:
+            ctx.save_for_backward(x, w1, w3, w2, *saved)
         return y
 
     @staticmethod
@@ -41,16 +46,16 @@ class _GatedFFN(torch.autograd.Function):
         x, w1, w3, w2, *saved = ctx.saved_tensors
         dy = dy if dy.stride(1) == 1 else dy.contiguous()
         grads = ctx.owner.gated_ffn_backward(dy, x, w1, w3, w2, tuple(saved), ctx.activation)
-        return (None, None, *_once("gated_ffn", grads, (dy, x, w1, w3, w2)))
+        return (None, None, None, *_once("gated_ffn", grads, (dy, x, w1, w3, w2)))
 
 
 def gated_ffn(owner, x, w1, w3, w2, activation: str = "silu"):
     """(act(x w1) * (x w3)) w2 over the last dimension of x, differentiable in x and the weights (all bf16)."""
     rows = x.reshape(-1, x.shape[-1])
-    if torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w3, w2)):
-        y = _GatedFFN.apply(owner, activation, rows, w1, w3, w2)
-    else:
-        y, _ = owner.gated_ffn(rows, w1, w3, w2, activation, save=False)
+    # (G, U and H are kept only for a backward pass; without one the call still goes through the function, which refuses
+    # forward-mode inputs)
+    save = torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w3, w2))
+    y = _GatedFFN.apply(owner, activation, save, rows, w1, w3, w2)
     return y.view(*x.shape[:-1], w2.shape[1])
 
 

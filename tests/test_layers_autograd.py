@@ -110,3 +110,53 @@ def test_first_derivatives():
     layers.gated_ffn(Owner(), *args).square().sum().backward()
     want = torch.autograd.grad(_plain(*args).square().sum(), args)
     assert all(torch.allclose(t.grad, g) and not t.grad.requires_grad for t, g in zip(args, want))
+
+
+# -- forward mode -------------------------------------------------------------------------------
+@pytest.mark.parametrize("grad", [False, True], ids=["no_grad", "grad"])
+@pytest.mark.parametrize("which", range(4))
+def test_forward_mode_is_refused_not_dropped(grad, which):
+    args = _tensors(grad=False)
+    qk = _qk(grad=False)
+    at = (0, 1, 5, 6)[which]
+    with torch.set_grad_enabled(grad), forward_ad.dual_level():
+        duals = list(args)
+        duals[which] = forward_ad.make_dual(args[which], torch.ones_like(args[which]))
+        with pytest.raises(NotImplementedError, match="forward mode"):
+            layers.gated_ffn(Owner(), *duals)
+        duals = list(qk)
+        duals[at] = forward_ad.make_dual(qk[at], torch.ones_like(qk[at]))
+        with pytest.raises(NotImplementedError, match="forward mode"):
+            layers.qk_norm_rope(Owner(), *duals)
+
+
+def test_tangents_of_incoming_gradients_are_refused():
+    args = _tensors()
+    y = layers.gated_ffn(Owner(), *args)
+    q, k, *rest = _qk()
+    a, _ = layers.qk_norm_rope(Owner(), q, k, *rest)
+    with forward_ad.dual_level():
+        for out, at in ((y, args[0]), (a, q)):
+            dy = forward_ad.make_dual(torch.ones_like(out), torch.ones_like(out))
+            with pytest.raises(NotImplementedError, match="forward mode"):
+                torch.autograd.grad(out, at, dy, retain_graph=True)
+
+
+def test_nothing_is_kept_where_no_gradient_is_wanted():
+    class Watched(Owner):
+        saves = []
+
+        def gated_ffn(self, x, w1, w3, w2, activation="silu", save=True):
+            self.saves.append(save)
+            return super().gated_ffn(x, w1, w3, w2, activation, save)
+
+    args = _tensors()
+    o = Watched()
+    layers.gated_ffn(o, *args)
+    with torch.no_grad():
+        y = layers.gated_ffn(o, *args)
+    z = layers.gated_ffn(o, *(t.detach() for t in args))
+    with torch.inference_mode():
+        layers.gated_ffn(o, *(t.detach() for t in args))
+    assert o.saves == [True, False, False, False] and not y.requires_grad and not z.requires_grad
+    assert torch.allclose(y, _plain(*args)) and torch.equal(y, z)
