@@ -32,6 +32,15 @@ def _once(name, results, inputs):
     return results
 
 
+def _rows(t):
+    """t, or a copy of it where the library would refuse its layout: it takes rows of consecutive entries that start on 16 bytes
+    and do not overlap, a multiple of 8 entries apart.  Views and the gradients that autograd makes of sums, slices and
+    concatenations need not be laid out so."""
+    fits = t.dim() == 2 and t.stride(1) == 1 and t.data_ptr() % 16 == 0 and \
+        (t.shape[0] < 2 or (t.stride(0) >= t.shape[1] and t.stride(0) % 8 == 0))
+    return t if fits else t.clone(memory_format=torch.contiguous_format)
+
+
 class _GatedFFN(torch.autograd.Function):
     @staticmethod
     def forward(ctx, owner, activation, save, x, w1, w3, w2):
@@ -44,14 +53,13 @@ class _GatedFFN(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         x, w1, w3, w2, *saved = ctx.saved_tensors
-        dy = dy if dy.stride(1) == 1 else dy.contiguous()
-        grads = ctx.owner.gated_ffn_backward(dy, x, w1, w3, w2, tuple(saved), ctx.activation)
+        grads = ctx.owner.gated_ffn_backward(_rows(dy), x, w1, w3, w2, tuple(saved), ctx.activation)
         return (None, None, None, *_once("gated_ffn", grads, (dy, x, w1, w3, w2)))
 
 
 def gated_ffn(owner, x, w1, w3, w2, activation: str = "silu"):
     """(act(x w1) * (x w3)) w2 over the last dimension of x, differentiable in x and the weights (all bf16)."""
-    rows = x.reshape(-1, x.shape[-1])
+    rows, w1, w3, w2 = (_rows(t) for t in (x.reshape(-1, x.shape[-1]), w1, w3, w2))
     # (G, U and H are kept only for a backward pass; without one the call still goes through the function, which refuses
     # forward-mode inputs)
     save = torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w3, w2))

@@ -160,3 +160,57 @@ def test_nothing_is_kept_where_no_gradient_is_wanted():
         layers.gated_ffn(o, *(t.detach() for t in args))
     assert o.saves == [True, False, False, False] and not y.requires_grad and not z.requires_grad
     assert torch.allclose(y, _plain(*args)) and torch.equal(y, z)
+
+
+# -- layouts ------------------------------------------------------------------------------------
+LOSSES = {
+    "sum over tokens": lambda y: (y.sum(0) * torch.arange(8.0, dtype=torch.float64)).sum(),     # strides (0, 1)
+    "sum": lambda y: y.sum(),                                                                    # strides (0, 0)
+    "cat of an odd width": lambda y: (torch.cat([y, y.detach()[:, :3]], 1) ** 2).sum(),          # row stride 11
+    "cat behind an odd width": lambda y: (torch.cat([y.detach()[:, :3], y], 1) ** 2).sum(),      # ... and off 16 bytes
+    "transposed": lambda y: (y.t().contiguous() ** 2).sum(),
+}
+
+
+@pytest.mark.parametrize("loss", LOSSES)
+@pytest.mark.parametrize("T", [1, 3])
+def test_gradients_of_any_layout(loss, T):
+    args = _tensors(T)
+    got = torch.autograd.grad(LOSSES[loss](layers.gated_ffn(Owner(), *args)), args)
+    want = torch.autograd.grad(LOSSES[loss](_plain(*args)), args)
+    assert all(torch.allclose(a, b) for a, b in zip(got, want))
+
+
+def _views(t):
+    """t as parts of wider matrices, transposed, at an odd address, expanded from one row."""
+    n, m = t.shape
+    yield torch.cat([t, t[:, :3]], 1)[:, :m]
+    yield torch.cat([t[:, :1], t, t[:, :7]], 1)[:, 1:m + 1]
+    yield torch.cat([t, t], 1)[:, :m]
+    yield t.t().contiguous().t()
+    yield torch.cat([t.reshape(-1)[:1], t.reshape(-1)])[1:].view(n, m)
+    yield t[:1].expand(n, m)
+
+
+@pytest.mark.parametrize("which", range(4))
+@pytest.mark.parametrize("T", [1, 5])
+def test_inputs_of_any_layout(which, T):
+    args = _tensors(T, grad=False)
+    for i, v in enumerate(_views(args[which])):
+        a = [t.clone().requires_grad_() for t in args]
+        a[which] = v.detach().requires_grad_()
+        b = [t.detach().contiguous().requires_grad_() for t in a]
+        y, z = layers.gated_ffn(Owner(), *a), _plain(*b)
+        assert torch.allclose(y, z), i
+        got, want = torch.autograd.grad(y.square().sum(), a), torch.autograd.grad(z.square().sum(), b)
+        assert all(torch.allclose(g, w) for g, w in zip(got, want)), i
+        with torch.no_grad():
+            assert torch.equal(layers.gated_ffn(Owner(), *a), y)
+
+
+def test_more_dimensions_and_views_of_them():
+    args = _tensors(6)
+    x = args[0].detach().view(2, 3, 8)
+    for v in (x, x.transpose(0, 1), torch.cat([x, x[..., :2]], -1)[..., :8], x[:0], x[0, 0]):
+        y = layers.gated_ffn(Owner(), v, *args[1:])
+        assert y.shape == v.shape and torch.allclose(y, _plain(v.reshape(-1, 8), *args[1:]).view(v.shape))
