@@ -77,7 +77,8 @@ class _QKNormRope(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dq, dk):
         q, k, cos, sin, positions, gain_q, gain_k = ctx.saved_tensors
-        dq, dk = (d if d.stride(2) == 1 else d.contiguous() for d in (dq, dk))
+        # (a tensor that was not given has no gradient)
+        dq, dk = (d if d is None or d.stride(2) == 1 else d.contiguous() for d in (dq, dk))
         grads = ctx.owner.qk_norm_rope_backward(dq, dk, q, k, cos, sin, positions, gain_q, gain_k, ctx.eps, ctx.interleaved)
         dq, dk, dgq, dgk = _once("qk_norm_rope", grads, (dq, dk, q, k, cos, sin, gain_q, gain_k))
         return (None, None, None, dq, dk, None, None, None, dgq if gain_q is not None else None,
@@ -87,5 +88,5 @@ class _QKNormRope(torch.autograd.Function):
 def qk_norm_rope(owner, q, k, cos, sin, positions=None, gain_q=None, gain_k=None, eps: float = 1e-6,
                  interleaved: bool = False):
     """Norm and rotation of q [tokens, heads, head_dim] and k (binding.Context.qk_norm_rope), differentiable in q, k
-    and the gains."""
+    and the gains.  q or k may be None, and so is its result."""
     return _QKNormRope.apply(owner, eps, interleaved, q, k, cos, sin, positions, gain_q, gain_k)

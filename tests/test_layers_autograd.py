@@ -214,3 +214,32 @@ def test_more_dimensions_and_views_of_them():
     for v in (x, x.transpose(0, 1), torch.cat([x, x[..., :2]], -1)[..., :8], x[:0], x[0, 0]):
         y = layers.gated_ffn(Owner(), v, *args[1:])
         assert y.shape == v.shape and torch.allclose(y, _plain(v.reshape(-1, 8), *args[1:]).view(v.shape))
+
+
+# -- norm with rotation: one of the two tensors -------------------------------------------------
+@pytest.mark.parametrize("which", [0, 1])
+@pytest.mark.parametrize("gains", [False, True])
+def test_norm_of_queries_or_keys_alone(which, gains):
+    q, k, cos, sin, pos, gq, gk = _qk()
+    x, g = (q, gq) if which == 0 else (k, gk)
+    pair = [None, None]
+    pair[which] = x
+    gain = [None, None]
+    if gains:
+        gain[which] = g
+    out = layers.qk_norm_rope(Owner(), *pair, cos, sin, pos, *gain)
+    assert out[1 - which] is None
+    w = torch.randn_like(x)
+    leaves = (x, g) if gains else (x,)
+    got = torch.autograd.grad((out[which] * w).sum(), leaves)
+    want = torch.autograd.grad(((x * g if gains else x) * w).sum(), leaves)
+    assert all(torch.allclose(a, b) for a, b in zip(got, want))
+
+
+def test_norm_with_one_result_unused_and_transposed_gradients():
+    q, k, cos, sin, pos, gq, gk = _qk()
+    a, b = layers.qk_norm_rope(Owner(), q, k, cos, sin, pos, gq, gk)
+    got = torch.autograd.grad((a.transpose(1, 2).contiguous() ** 2).sum(), (q, k, gq, gk))
+    want = torch.autograd.grad(((q * gq) ** 2).sum(), (q, gq))
+    assert torch.allclose(got[0], want[0]) and torch.allclose(got[2], want[1])
+    assert not got[1].any() and not got[3].any()
