@@ -12,6 +12,7 @@ import ctypes as C
 import math
 import os
 import struct
+import weakref
 from typing import List, Optional, Sequence
 
 import numpy as np
@@ -296,6 +297,7 @@ class _Operators:
         """What every call looks up, once: device number, types, the stream's handle and the way to ask for the handle
         of the current stream without building a Stream object."""
         torch = self.torch
+        self._lists = weakref.WeakSet()          # AdamW lists, which the library's context must outlive
         self._dev = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._bf16, self._f32, self._i64 = torch.bfloat16, torch.float32, torch.int64
         self._raw_stream = torch._C._cuda_getCurrentRawStream
@@ -310,6 +312,8 @@ class _Operators:
     def _quick(self, name, *args):
         """The compiled form of a call: its results, or None when this one has to go the long way (an argument is not as
         it should be, or the caller is on another stream)."""
+        if self.ctx is None:
+            raise RuntimeError("the context is closed")
         f = self._fast.get(name)
         if f is None:
             return None
@@ -317,6 +321,14 @@ class _Operators:
         if r.__class__ is int:
             self._check(r)
         return r
+
+    def close(self):
+        """Releases the context, and before it the AdamW lists made with it."""
+        if getattr(self, "ctx", None):
+            for o in list(self._lists):
+                o.close()
+            self.lib.muloco_destroy(self.ctx)
+            self.ctx = None
 
     def _other_stream(self):
         """The caller's current stream when it is not the context's, else None."""
@@ -590,11 +602,6 @@ class Context(_Operators):
         """Waits for the stream; raises what the device reported since the last call."""
         self._check(self.lib.muloco_sync_status(self.ctx))
 
-    def close(self):
-        if getattr(self, "ctx", None):
-            self.lib.muloco_destroy(self.ctx)
-            self.ctx = None
-
     def __del__(self):
         try:
             self.close()
@@ -664,6 +671,12 @@ class AdamW:
         opt = C.c_void_p()
         owner._check(self.lib.muloco_adamw_create(owner.ctx, C.byref(cfg), table, n, C.byref(opt)))
         self.opt = opt
+        owner._lists.add(self)
+
+    def _open(self):
+        """Raises when the library's list is gone: its memory and, after the owner's close(), that of the context it names."""
+        if self.opt is None:
+            raise RuntimeError("the AdamW list is closed (by itself or with its context)")
 
     def _same(self, name, t, dtype, like):
         if t.get_device() != self.owner._dev or t.dtype != dtype or t.shape != like.shape or not t.is_contiguous():
@@ -675,6 +688,7 @@ class AdamW:
 
     def step(self, grads=None, lr_scale: float = 1.0):
         """One step of all tensors, with the gradients named at construction or those given."""
+        self._open()
         if grads is None:
             f = self.owner._fast.get("adamw_step")
             if f is not None:
@@ -704,6 +718,7 @@ class AdamW:
         32-bit states themselves.  Padding entries are zero."""
         if self.state_bits == 32:
             return self.state1, self.state2
+        self._open()
         f = self.owner._fast.get("adamw_moments")
         if f is not None:
             r = f[0](self.opt.value, f[1], self.owner._dev, self.owner._handle, self.scale1, self.padded)
@@ -870,11 +885,6 @@ class MuLoCo(_Operators):
     def _check(self, st):
         if st != OK:
             raise MulocoError(st, self.lib.muloco_last_error(self.ctx).decode())
-
-    def close(self):
-        if getattr(self, "ctx", None):
-            self.lib.muloco_destroy(self.ctx)
-            self.ctx = None
 
     def __del__(self):
         try:
