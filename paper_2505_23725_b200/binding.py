@@ -622,6 +622,8 @@ class AdamW:
                  bias_correction=True, state_bits=32, wd_mult=None, lr_mult=None, copies=None, seed=0, grad_dtype=None):
         torch = owner.torch
         self.opt = None
+        # own lists: the library's table holds the tensors' addresses
+        grads, copies = (None if l is None else list(l) for l in (grads, copies))
         self.owner, self.lib, self.params, self.grads, self.copies = owner, owner.lib, list(params), grads, copies
         n = len(self.params)
         if state_bits not in (8, 32):

@@ -97,3 +97,17 @@ def test_a_closed_context_refuses_operators():
         o.gated_ffn(x, x, x, x)
     with pytest.raises(RuntimeError, match="closed"):
         o.qk_norm_rope(torch.ones(1, 1, 8), None, torch.ones(1, 4), torch.zeros(1, 4))
+
+
+def test_tensors_named_at_construction_stay_alive():
+    """The library's table holds their addresses: what the caller does to its own lists afterwards must not free them."""
+    o = Owner()
+    params, grads, copies = [torch.ones(300)], [torch.ones(300)], [torch.ones(300, dtype=torch.bfloat16)]
+    opt = binding.AdamW(o, params, grads=grads, copies=copies)
+    refs = [weakref.ref(l[0]) for l in (params, grads, copies)]
+    for l in (params, grads, copies):
+        l[0] = None
+    gc.collect()
+    assert all(r() is not None for r in refs)
+    opt.step()
+    opt.close()
