@@ -654,6 +654,9 @@ class AdamW:
         self.state2 = torch.zeros(off, dtype=torch.uint8 if q8 else torch.float32, device=dev)
         self.scale1 = torch.zeros(off // ADAMW_BLOCK, dtype=torch.float32, device=dev) if q8 else None
         self.scale2 = torch.zeros(off // ADAMW_BLOCK, dtype=torch.float32, device=dev) if q8 else None
+        cur = owner._other_stream()
+        if cur is not None:                      # the zeros above are written there
+            owner._enter(cur, (self.state1, self.state2, self.scale1, self.scale2))
         self.steps = 0
         cfg = AdamwConfig(lr, beta1, beta2, eps, weight_decay, int(bias_correction), state_bits,
                           BF16 if grad_dtype == torch.bfloat16 else F32, seed)
@@ -858,6 +861,9 @@ class MuLoCo(_Operators):
             bufs.ef_k = C.cast(self._tables[-1], C.POINTER(C.c_void_p))
         self.stream = stream if stream is not None else torch.cuda.current_stream(dev)
         self._init_operators()
+        cur = self._other_stream()
+        if cur is not None:                      # the initial weights are written there
+            self.stream.wait_stream(cur)
         self.ctx = C.c_void_p()
         st = self.lib.muloco_create(C.byref(self.cfg), descs, self.n, C.byref(bufs),
                                     C.c_void_p(self.stream.cuda_stream), C.byref(self.ctx))

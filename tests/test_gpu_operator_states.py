@@ -1,4 +1,4 @@
-"""AdamW lists: blocks of 8-bit states after a value that is not finite."""
+"""AdamW states on the GPU: blocks of 8-bit states after a value that is not finite, states made on another stream."""
 import pytest
 
 pytestmark = pytest.mark.gpu
@@ -55,3 +55,59 @@ def test_8_bit_block_stays_nan_and_is_reported_every_step(ctx, value, at, bf16):
         assert torch.equal(bad.scale1[others], good.scale1[others]) and torch.equal(bad.scale2[others], good.scale2[others])
     good.close()
     bad.close()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_list_built_on_a_busy_stream(bits):
+    """States made on a stream that is still at work, first step on the context's: it finds them zero."""
+    import torch
+    from paper_2505_23725_b200 import binding
+    n = 1 << 20
+    torch.manual_seed(0)
+    g = torch.randn(n, device="cuda")
+    own, busy = torch.cuda.Stream(), torch.cuda.Stream()
+    ctx = binding.Context("cuda:0", stream=own)
+    torch.cuda.synchronize()
+    outs = []
+    for late in (False, True):
+        p = torch.ones(n, device="cuda")
+        torch.cuda.synchronize()
+        with torch.cuda.stream(busy if late else own):
+            # what the states' memory holds before
+            old = [torch.full((k * n,), 85, dtype=torch.uint8, device="cuda") for k in (1, 1, 4, 4)] + \
+                  [torch.full((n // 256,), 3.0, device="cuda") for _ in range(2)]
+            torch.cuda.synchronize()
+            del old
+            if late:
+                big = torch.randn(8192, 8192, device="cuda")
+                for _ in range(20):
+                    big = big @ big * 1e-2
+            opt = binding.AdamW(ctx, [p], state_bits=bits, seed=1, **HYPER)
+        with torch.cuda.stream(own):
+            opt.step([g])
+        torch.cuda.synchronize()
+        outs.append([p] + [t.clone() for t in (opt.state1, opt.state2, opt.scale1, opt.scale2) if t is not None])
+        opt.close()
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    ctx.sync_status()
+    ctx.close()
+
+
+def test_optimizer_built_on_a_busy_stream():
+    """The same for a MuLoCo with a stream of its own: its replicas start from the global parameters."""
+    import torch
+    from paper_2505_23725_b200 import binding, configs
+    w = configs.mini_workload(K=2, H=2, vocab=100, norms=True, adam_state_bits=8)
+    own, busy = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(busy):
+        big = torch.randn(8192, 8192, device="cuda")
+        torch.cuda.synchronize()
+        for _ in range(20):
+            big = big @ big * 1e-2
+        opt = binding.MuLoCo(w, "cuda:0", init_seed=3, stream=own)
+    torch.cuda.synchronize()
+    for i in range(len(w.tensors)):
+        assert torch.equal(opt.theta_k[0][i], opt.theta_g[i]) and torch.equal(opt.theta_k[1][i], opt.theta_g[i])
+        assert opt.theta_g[i].any()
+    opt.sync_status()
+    opt.close()

@@ -111,3 +111,15 @@ def test_tensors_named_at_construction_stay_alive():
     assert all(r() is not None for r in refs)
     opt.step()
     opt.close()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_states_made_on_another_stream_are_handed_over(bits):
+    """The zeros of the states are written on the caller's current stream: the context's has to wait for it."""
+    o, calls = Owner(), []
+    o._other_stream = lambda: "caller's"
+    o._enter = lambda cur, tensors: calls.append((cur, {t.data_ptr() for t in tensors if t is not None}))
+    opt = binding.AdamW(o, [torch.ones(300)], state_bits=bits)
+    states = [t for t in (opt.state1, opt.state2, opt.scale1, opt.scale2) if t is not None]
+    assert len(calls) == 1 and calls[0][0] == "caller's" and {t.data_ptr() for t in states} <= calls[0][1]
+    opt.close()
