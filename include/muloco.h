@@ -15,6 +15,8 @@
  *     host state; muloco_destroy releases them.
  *   - All matrices are row-major float32 unless stated; a vector is a 1 x n
  *     matrix.
+ *   - A context belongs to the device that was current when it was made; its calls make that
+ *     device current while they run and restore the caller's.
  *   - Every call enqueues its work on the CUDA stream given at create time and
  *     returns without waiting for the GPU.  Argument errors are reported by the
  *     return value at once.  Conditions found on the device (non-finite

@@ -149,6 +149,7 @@ struct muloco_ctx {
   int n = 0;
   std::vector<TensorInfo> T;
   cudaStream_t st = nullptr;
+  int device = 0;                  // that of the thread which made the context
   int n_sms = 148;
   std::string err;
   int* d_status = nullptr;
@@ -512,6 +513,8 @@ muloco_status ctx_fail(muloco_ctx* c, muloco_status s, const char* fmt, ...) {
 
 void ctx_count_launches(muloco_ctx* c, int n) { c->launches += n; }
 
+int ctx_device(const muloco_ctx* c) { return c->device; }
+
 float* ctx_qk_scratch(muloco_ctx* c, int** tickets) {
   if (!c->qk_scratch) {
     const size_t bytes = QK_SCRATCH_FLOATS * sizeof(float) + QK_TICKETS * sizeof(int);
@@ -613,6 +616,7 @@ MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_te
     (d.kind == MULOCO_MUON ? c->muon_ids : c->adam_ids).push_back(i);
   }
 
+  CKC(cudaGetDevice(&c->device));
   CKC(cudaMalloc(&c->d_status, sizeof(int)));
   CKC(cudaMemsetAsync(c->d_status, 0, sizeof(int), c->st));
 
@@ -737,6 +741,7 @@ MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_te
 
 MULOCO_API void muloco_destroy(muloco_ctx* c) {
   if (!c) return;
+  const DeviceScope scope(c->device);
   cudaStreamSynchronize(c->st);
   for (muloco_adamw* o : c->adam8) muloco_adamw_destroy(o);
   for (Group& g : c->groups) destroy_group(g);
@@ -777,6 +782,7 @@ MULOCO_API void muloco_destroy(muloco_ctx* c) {
 
 MULOCO_API muloco_status muloco_inner_step(muloco_ctx* c, int32_t worker, const void* const* grads, float lr_scale) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   const muloco_config& f = c->cfg;
   const int K = f.K, n = c->n;
   if (worker < -1 || worker >= K) return fail(c, MULOCO_EINVAL, "worker %d outside -1..%d", worker, K - 1);
@@ -898,6 +904,7 @@ MULOCO_API muloco_status muloco_inner_step(muloco_ctx* c, int32_t worker, const 
 MULOCO_API muloco_status muloco_inner_step_host(muloco_ctx* c, int32_t worker, const void* const* host_grads,
                                      float lr_scale) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   const int K = c->cfg.K, n = c->n;
   if (worker < -1 || worker >= K) return fail(c, MULOCO_EINVAL, "worker %d outside -1..%d", worker, K - 1);
   if (!host_grads && n > 0) return fail(c, MULOCO_EINVAL, "host_grads is NULL");
@@ -969,6 +976,7 @@ MULOCO_API muloco_status muloco_inner_step_host(muloco_ctx* c, int32_t worker, c
 
 MULOCO_API muloco_status muloco_outer_sync(muloco_ctx* c, int32_t fragment) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   const muloco_config& f = c->cfg;
   if (fragment < -1 || fragment >= f.J) return fail(c, MULOCO_EINVAL, "fragment %d outside -1..%d", fragment, f.J - 1);
   FragTable& ft = c->frags[fragment < 0 ? f.J : fragment];
@@ -1009,6 +1017,7 @@ MULOCO_API muloco_status muloco_outer_sync(muloco_ctx* c, int32_t fragment) {
 
 MULOCO_API muloco_status muloco_outer_sync_host(muloco_ctx* c, int32_t fragment, void* const* host_theta_g) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   if (!host_theta_g && c->n > 0) return fail(c, MULOCO_EINVAL, "host_theta_g is NULL");
   muloco_status s = muloco_outer_sync(c, fragment);
   if (s != MULOCO_OK) return s;
@@ -1053,6 +1062,7 @@ MULOCO_API muloco_status muloco_shard_delta(muloco_ctx* c, int32_t fragment, int
   FragTable* ft = nullptr;
   const muloco_status s = shard_check(c, fragment, world, 0, &ft);
   if (s != MULOCO_OK) return s;
+  ON_DEVICE(c);
   if (ft->n_segs == 0) return MULOCO_OK;
   if (!stage) return fail(c, MULOCO_EINVAL, "stage is NULL");
   const muloco_config& f = c->cfg;
@@ -1073,6 +1083,7 @@ MULOCO_API muloco_status muloco_shard_step(muloco_ctx* c, int32_t fragment, int3
   FragTable* ft = nullptr;
   const muloco_status s = shard_check(c, fragment, world, rank, &ft);
   if (s != MULOCO_OK) return s;
+  ON_DEVICE(c);
   if (ft->n_segs == 0) return MULOCO_OK;
   if (!reduced || !theta_shard) return fail(c, MULOCO_EINVAL, "reduced or theta_shard is NULL");
   const muloco_config& f = c->cfg;
@@ -1091,6 +1102,7 @@ MULOCO_API muloco_status muloco_shard_broadcast(muloco_ctx* c, int32_t fragment,
   FragTable* ft = nullptr;
   const muloco_status s = shard_check(c, fragment, world, 0, &ft);
   if (s != MULOCO_OK) return s;
+  ON_DEVICE(c);
   const muloco_config& f = c->cfg;
   if (fragment < 0) for (auto& n : c->frag_syncs) n += 1; else c->frag_syncs[fragment] += 1;
   if (ft->n_segs == 0) return MULOCO_OK;
@@ -1116,6 +1128,7 @@ MULOCO_API int32_t muloco_fragments_due(const muloco_ctx* c, int64_t step, int32
 MULOCO_API muloco_status muloco_newton_schulz(muloco_ctx* c, const void* X, int32_t x_dtype, void* O, int32_t o_dtype,
                                    int32_t batch, int64_t rows, int64_t cols, int32_t ns_mode) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   if (batch < 0 || rows < 1 || cols < 1) return fail(c, MULOCO_ESHAPE, "bad batch/shape");
   if (batch == 0) return MULOCO_OK;                  // an empty batch: nothing to read or write
   if (!X || !O) return fail(c, MULOCO_EINVAL, "X or O is NULL");
@@ -1186,6 +1199,7 @@ MULOCO_API muloco_status muloco_newton_schulz(muloco_ctx* c, const void* X, int3
 MULOCO_API muloco_status muloco_quantize(muloco_ctx* c, const float* psi, int64_t rows, int64_t cols, int32_t bits,
                               int8_t* codes, float* scales, float* dequant) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   if (bits != 8 && bits != 4 && bits != 2) return fail(c, MULOCO_EINVAL, "bits must be 8, 4 or 2");
   if (rows < 0 || cols < 0) return fail(c, MULOCO_ESHAPE, "negative shape");
   if (rows == 0 || cols == 0) return MULOCO_OK;      // empty input: nothing to read or write
@@ -1200,6 +1214,7 @@ MULOCO_API muloco_status muloco_quantize(muloco_ctx* c, const float* psi, int64_
 
 MULOCO_API muloco_status muloco_topk_sparsify(muloco_ctx* c, const float* x, int64_t n, float fraction, float* out) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   if (!(fraction > 0.f && fraction <= 1.f)) return fail(c, MULOCO_EINVAL, "fraction must be in (0, 1]");
   if (n < 0 || n >= ((int64_t)1 << 31)) return fail(c, MULOCO_ESHAPE, "n must be in 0..2^31-1");
   if (n == 0) return MULOCO_OK;                      // empty input: nothing to read or write
@@ -1234,6 +1249,7 @@ MULOCO_API muloco_status muloco_topk_sparsify(muloco_ctx* c, const float* x, int
 
 MULOCO_API muloco_status muloco_pseudogradient(muloco_ctx* c, int32_t tensor, float* psi_out) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   if (tensor < 0 || tensor >= c->n) return fail(c, MULOCO_EINVAL, "tensor %d outside 0..%d", tensor, c->n - 1);
   if (!psi_out) return fail(c, MULOCO_EINVAL, "psi_out is NULL");
   const TensorInfo& t = c->T[tensor];
@@ -1281,6 +1297,7 @@ MULOCO_API muloco_status muloco_set_timing(muloco_ctx* c, int32_t enabled) {
 
 MULOCO_API muloco_status muloco_get_timings(muloco_ctx* c, float* ms, int64_t* launches) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   CK(cudaStreamSynchronize(c->st));
   float acc[MULOCO_N_PHASES] = {0, 0, 0, 0, 0};
   for (TimedSpan& s : c->spans) {
@@ -1328,6 +1345,7 @@ MULOCO_API muloco_status muloco_check_workspace(muloco_ctx* c) {
 
 MULOCO_API muloco_status muloco_sync_status(muloco_ctx* c) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   cudaError_t e = cudaStreamSynchronize(c->st);
   if (e != cudaSuccess) return fail(c, MULOCO_ECUDA, "stream synchronize: %s", cudaGetErrorString(e));
   int h = 0;

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "../../include/muloco.h"
+#include "device_scope.h"
 
 namespace muloco {
 
@@ -180,6 +181,12 @@ struct CtxView {
 CtxView ctx_view(muloco_ctx* c);
 muloco_status ctx_fail(muloco_ctx* c, muloco_status s, const char* fmt, ...);
 void ctx_count_launches(muloco_ctx* c, int n);
+int ctx_device(const muloco_ctx* c);
+// First thing of every entry point that touches the device: the context's device is current until it returns.
+#define ON_DEVICE(c)                                                                                          \
+  const muloco::DeviceScope device_scope_(muloco::ctx_device(c));                                             \
+  if (device_scope_.error() != cudaSuccess)                                                                   \
+  return muloco::ctx_fail(c, MULOCO_ECUDA, "device %d: %s", muloco::ctx_device(c), cudaGetErrorString(device_scope_.error()))
 // Scratch of the context that the reductions of qk_norm.cu use: QK_SCRATCH_FLOATS floats, then tickets
 // (zero between launches).  Allocated on first use; nullptr when that fails.
 float* ctx_qk_scratch(muloco_ctx* c, int** tickets);

@@ -42,6 +42,7 @@ extern "C" {
 
 MULOCO_API void muloco_adamw_destroy(muloco_adamw* o) {
   if (!o) return;
+  const DeviceScope scope(ctx_device(o->ctx));
   cudaStreamSynchronize(ctx_view(o->ctx).st);
   if (o->d_units) cudaFree(o->d_units);
   if (o->d_grads) cudaFree(o->d_grads);
@@ -55,6 +56,7 @@ MULOCO_API void muloco_adamw_destroy(muloco_adamw* o) {
 MULOCO_API muloco_status muloco_adamw_create(muloco_ctx* c, const muloco_adamw_config* cfg,
                                              const muloco_adamw_tensor* t, int32_t n, muloco_adamw** out) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   if (!out) return ctx_fail(c, MULOCO_EINVAL, "out is NULL");
   *out = nullptr;
   if (!cfg) return ctx_fail(c, MULOCO_EINVAL, "config is NULL");
@@ -151,6 +153,7 @@ MULOCO_API muloco_status muloco_adamw_create(muloco_ctx* c, const muloco_adamw_c
 MULOCO_API muloco_status muloco_adamw_step(muloco_adamw* o, const void* const* grads, int64_t step, float lr_scale) {
   if (!o) return MULOCO_EINVAL;
   muloco_ctx* c = o->ctx;
+  ON_DEVICE(c);
   const CtxView v = ctx_view(c);
   if (step < 1) return ctx_fail(c, MULOCO_EINVAL, "step counts from 1 (got %lld)", (long long)step);
   if (!grads && !o->has_default) return ctx_fail(c, MULOCO_EINVAL, "no gradients given, and none named at create time");
@@ -191,6 +194,7 @@ MULOCO_API muloco_status muloco_adamw_step(muloco_adamw* o, const void* const* g
 MULOCO_API muloco_status muloco_adamw_moments(muloco_adamw* o, float* m, float* v) {
   if (!o) return MULOCO_EINVAL;
   muloco_ctx* c = o->ctx;
+  ON_DEVICE(c);
   if (o->cfg.state_bits != 8) return ctx_fail(c, MULOCO_EINVAL, "32-bit states are their own values");
   if (o->n_units == 0) return MULOCO_OK;
   if (!m || !v) return ctx_fail(c, MULOCO_EINVAL, "m or v is NULL");
@@ -281,6 +285,7 @@ extern "C" {
 MULOCO_API muloco_status muloco_qk_norm_rope(muloco_ctx* c, const muloco_qk_norm* a, void* q_out, int64_t qo_ts,
                                              int64_t qo_hs, void* k_out, int64_t ko_ts, int64_t ko_hs) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   const muloco_status s = check_qk(c, a);
   if (s != MULOCO_OK) return s;
   if (a->tokens == 0 || a->heads_q + a->heads_k == 0) return MULOCO_OK;
@@ -304,6 +309,7 @@ MULOCO_API muloco_status muloco_qk_norm_rope_backward(muloco_ctx* c, const muloc
                                                       int64_t dko_ts, int64_t dko_hs, void* dq, void* dk,
                                                       float* dgain_q, float* dgain_k) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   const muloco_status s = check_qk(c, a);
   if (s != MULOCO_OK) return s;
   const CtxView v = ctx_view(c);
@@ -330,6 +336,7 @@ MULOCO_API muloco_status muloco_qk_norm_rope_backward(muloco_ctx* c, const muloc
 
 MULOCO_API muloco_status muloco_gated_ffn(muloco_ctx* c, const muloco_ffn* a, void* g, void* u, void* h, void* y) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   const muloco_status s = check_ffn(c, a);
   if (s != MULOCO_OK) return s;
   if (a->tokens == 0) return MULOCO_OK;
@@ -351,6 +358,7 @@ MULOCO_API muloco_status muloco_gated_ffn_backward(muloco_ctx* c, const muloco_f
                                                    const void* g, const void* u, const void* h, void* dg, void* du,
                                                    void* dx, void* dw1, void* dw3, void* dw2) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   const muloco_status s = check_ffn(c, a);
   if (s != MULOCO_OK) return s;
   if (misaligned(dx, 16) || misaligned(dw1, 16) || misaligned(dw3, 16) || misaligned(dw2, 16))
