@@ -209,7 +209,7 @@ struct muloco_ctx {
   std::vector<muloco_adamw*> adam8;   // 8-bit AdamW states: one list per worker
 
   // operators around the optimizer (ops_capi.cu)
-  float* qk_scratch = nullptr;     // gain-gradient partials of qk_norm.cu, then its tickets; allocated on first use
+  float* qk_scratch = nullptr;     // gain-gradient partials of qk_norm.cu, then its tickets
 };
 
 namespace {
@@ -516,15 +516,6 @@ void ctx_count_launches(muloco_ctx* c, int n) { c->launches += n; }
 int ctx_device(const muloco_ctx* c) { return c->device; }
 
 float* ctx_qk_scratch(muloco_ctx* c, int** tickets) {
-  if (!c->qk_scratch) {
-    const size_t bytes = QK_SCRATCH_FLOATS * sizeof(float) + QK_TICKETS * sizeof(int);
-    if (cudaMalloc(&c->qk_scratch, bytes) != cudaSuccess) {
-      c->qk_scratch = nullptr;
-      cudaGetLastError();
-      return nullptr;
-    }
-    if (cudaMemsetAsync(c->qk_scratch + QK_SCRATCH_FLOATS, 0, QK_TICKETS * sizeof(int), c->st) != cudaSuccess) return nullptr;
-  }
   *tickets = reinterpret_cast<int*>(c->qk_scratch + QK_SCRATCH_FLOATS);
   return c->qk_scratch;
 }
@@ -619,6 +610,9 @@ MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_te
   CKC(cudaGetDevice(&c->device));
   CKC(cudaMalloc(&c->d_status, sizeof(int)));
   CKC(cudaMemsetAsync(c->d_status, 0, sizeof(int), c->st));
+  // 5 MB, here so that no call of the operators allocates
+  CKC(cudaMalloc(&c->qk_scratch, QK_SCRATCH_FLOATS * sizeof(float) + QK_TICKETS * sizeof(int)));
+  CKC(cudaMemsetAsync(c->qk_scratch + QK_SCRATCH_FLOATS, 0, QK_TICKETS * sizeof(int), c->st));
 
   // shape groups of the hidden matrices (same s x l after orienting to s <= l)
   std::map<std::pair<int64_t, int64_t>, int> gidx;

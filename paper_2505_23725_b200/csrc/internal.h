@@ -188,7 +188,7 @@ int ctx_device(const muloco_ctx* c);
   if (device_scope_.error() != cudaSuccess)                                                                   \
   return muloco::ctx_fail(c, MULOCO_ECUDA, "device %d: %s", muloco::ctx_device(c), cudaGetErrorString(device_scope_.error()))
 // Scratch of the context that the reductions of qk_norm.cu use: QK_SCRATCH_FLOATS floats, then tickets
-// (zero between launches).  Allocated on first use; nullptr when that fails.
+// (zero between launches).
 float* ctx_qk_scratch(muloco_ctx* c, int** tickets);
 
 // Programmatic dependent launch: a kernel launched so may start while the one before it in the stream still

@@ -328,7 +328,6 @@ MULOCO_API muloco_status muloco_qk_norm_rope_backward(muloco_ctx* c, const muloc
   k.t[1].dy = dk_out; k.t[1].y_ts = dko_ts; k.t[1].y_hs = dko_hs; k.t[1].out = dk; k.t[1].dgain = dgain_k;
   for (QkTensor& t : k.t) { t.o_hs = a->head_dim; t.o_ts = (int64_t)t.heads * a->head_dim; }
   k.partials = ctx_qk_scratch(c, &k.tickets);
-  if (!k.partials) return ctx_fail(c, MULOCO_ENOMEM, "scratch of the gain gradients");
   OPS_CK(launch_qk_norm(v.st, k, true, a->dtype == MULOCO_BF16, v.n_sms));
   ctx_count_launches(c, 1);
   return MULOCO_OK;

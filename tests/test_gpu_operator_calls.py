@@ -1,0 +1,69 @@
+"""Calls of the operators on a B200: what they allocate, calls inside a captured graph, calls from several threads."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def _qk(D=64, T=300, seed=0):
+    import torch
+    torch.manual_seed(seed)
+    q, k, dq, dk = (torch.randn(T, h, D, device="cuda") for h in (4, 2, 4, 2))
+    cos, sin = torch.randn(T, D // 2, device="cuda"), torch.randn(T, D // 2, device="cuda")
+    gq, gk = torch.randn(D, device="cuda"), torch.randn(D, device="cuda")
+    return (dq, dk, q, k, cos, sin, None, gq, gk), (q, k, cos, sin, None, gq, gk)
+
+
+def test_first_norm_backward_of_a_context_allocates_nothing():
+    import torch
+    from paper_2505_23725_b200 import binding
+    back, fwd = _qk()
+    warm = binding.Context("cuda:0")               # kernels loaded, torch's blocks cached
+    want = warm.qk_norm_rope_backward(*back)
+    del want
+    ctx = binding.Context("cuda:0")
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    got = ctx.qk_norm_rope_backward(*back)
+    torch.cuda.synchronize()
+    assert torch.cuda.mem_get_info()[0] == free
+    want = warm.qk_norm_rope_backward(*back)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    for c in (ctx, warm):
+        c.sync_status()
+        c.close()
+
+
+def test_operators_inside_a_captured_graph():
+    """A fresh context's calls, captured and replayed on other values, give what they give outside a graph."""
+    import torch
+    from paper_2505_23725_b200 import binding
+    plain = binding.Context("cuda:0")
+    back, fwd = _qk()
+    T, d, F = 200, 64, 136
+    x, dy = (torch.randn(T, d, device="cuda").to(torch.bfloat16) for _ in range(2))
+    w1, w3 = (torch.randn(d, F, device="cuda").to(torch.bfloat16) / 8 for _ in range(2))
+    w2 = torch.randn(F, d, device="cuda").to(torch.bfloat16) / 8
+
+    def calls(c):
+        y, saved = c.gated_ffn(x, w1, w3, w2)
+        return [*c.qk_norm_rope(*fwd), *c.qk_norm_rope_backward(*back), y, *c.gated_ffn_backward(dy, x, w1, w3, w2, saved)]
+
+    calls(plain)
+    side = torch.cuda.Stream()
+    ctx = binding.Context("cuda:0", stream=side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        got = calls(ctx)
+    for seed in (1, 2):
+        torch.manual_seed(seed)
+        for t in (*back[:4], x, dy):
+            t.copy_(torch.randn(t.shape, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, calls(plain)))
+    plain.sync_status()
+    ctx.sync_status()
+    del graph
+    ctx.close()
+    plain.close()
