@@ -25,6 +25,8 @@
 // alone take 239 and 886.  Unlimited, a slab takes 334 ns, about 635 cycles, where its MMAs need 512.
 #include <string.h>
 
+#include <atomic>
+
 #include "internal.h"
 #include "tc_ptx.cuh"
 
@@ -805,21 +807,23 @@ struct Builder {
   }
 };
 
-// Raises a kernel's shared-memory limit, once per device (`allowed`: the last device it was raised on).
+// Raises a kernel's shared-memory limit, once per device (`allowed`: a bit for each of the first 64 that it was raised on; calls
+// may come from several threads).
 template <typename K>
-cudaError_t allow_smem(K kernel, int bytes, int* allowed) {
+cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* allowed) {
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess || *allowed == dev) return e;
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (e != cudaSuccess || (allowed->load(std::memory_order_relaxed) & bit)) return e;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) *allowed = dev;
+  if (e == cudaSuccess) allowed->fetch_or(bit, std::memory_order_relaxed);
   return e;
 }
 
 template <int EPI, int ACT>
 cudaError_t launch_kernel(cudaStream_t st, const Builder& b, int n_sms) {
   auto kernel = ffn_kernel<EPI, ACT>;
-  static int allowed = -1;
+  static std::atomic<uint64_t> allowed{0};
   cudaError_t e = allow_smem(kernel, (int)SMEM_BYTES, &allowed);
   if (e != cudaSuccess) return e;
   const int units = n_sms / CG;
@@ -861,7 +865,7 @@ template <int EPI, int ACT, int NT>
 cudaError_t launch_few_kernel(cudaStream_t st, const FewMaps& m, const FewParams& p, int split) {
   auto kernel = ffn_few_kernel<EPI, ACT, NT>;
   using Sh = FewShape<EPI, NT>;
-  static int allowed = -1;                   // the device for which the kernel may use its shared memory
+  static std::atomic<uint64_t> allowed{0};
   cudaError_t e = allow_smem(kernel, (int)Sh::SMEM, &allowed);
   if (e != cudaSuccess) return e;
   // only the stages that the CTA's slabs use, so that the next kernel's blocks may find room beside this one's

@@ -16,6 +16,7 @@
 // registers leave 12 warps per SM).
 #include <string.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "internal.h"
@@ -631,20 +632,21 @@ cudaError_t launch_one(cudaStream_t st, const QkArgs& a, int n_sms, int G) {
   if constexpr (V > 1) {
     using St = Stage<T, V, NC, BACK>;
     smem = (size_t)QK_WARPS * St::DEPTH * St::bytes(a.dim);
-    // the resident blocks, asked for once per device and size (a second wave of blocks costs a third of the rate)
-    static int seen_dev = -1, seen_blocks = 0;
-    static size_t seen_smem = 0;
-    int dev = 0;
+    // the resident blocks (a second wave of blocks costs a third of the rate), asked for once per device and head size: one byte
+    // each, 0 while not known, so that calls from several threads find the answer for their own size or ask themselves
+    static std::atomic<uint8_t> known[8][QK_MAX_DIM / 2 + 1];
+    int dev = 0, blocks = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess && (seen_dev != dev || seen_smem != smem)) {
+    if (e == cudaSuccess && dev < 8) blocks = known[dev][a.dim / 2].load(std::memory_order_relaxed);
+    if (e == cudaSuccess && blocks == 0) {
       e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                (int)(QK_WARPS * St::DEPTH * St::bytes(QK_MAX_DIM)));
-      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&seen_blocks, kernel, QK_THREADS, smem);
-      if (e == cudaSuccess && seen_blocks < 1) e = cudaErrorLaunchOutOfResources;
-      if (e == cudaSuccess) { seen_dev = dev; seen_smem = smem; }
+      if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, QK_THREADS, smem);
+      if (e == cudaSuccess && blocks < 1) e = cudaErrorLaunchOutOfResources;
+      if (e == cudaSuccess && dev < 8) known[dev][a.dim / 2].store((uint8_t)blocks, std::memory_order_relaxed);
     }
     if (e != cudaSuccess) return e;
-    resident = seen_blocks;
+    resident = blocks;
   }
   // The blocks are shared out by what a token costs in either tensor: its groups of heads, and about one more for what is done
   // once per token (12 + 3 heads of 64, f32, 4099 tokens, backward: 27 us when shared out by heads).  A token's

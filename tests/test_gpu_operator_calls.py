@@ -67,3 +67,42 @@ def test_operators_inside_a_captured_graph():
     del graph
     ctx.close()
     plain.close()
+
+
+def test_calls_from_several_threads_with_sizes_in_turn():
+    """Gain gradients are summed in an order that the grid fixes: with other head sizes on their way in other threads it has to
+    be the same grid, hence the same bits."""
+    import threading
+    import torch
+    from paper_2505_23725_b200 import binding
+    sizes = (64, 128, 96, 32)
+    inputs = {D: _qk(D, 3000, seed=D)[0] for D in sizes}
+    ctx = binding.Context("cuda:0")
+    want = {D: ctx.qk_norm_rope_backward(*inputs[D]) for D in sizes}
+    x = torch.randn(40, 64, device="cuda").to(torch.bfloat16)
+    w = torch.randn(64, 64, device="cuda").to(torch.bfloat16) / 8
+    y = ctx.gated_ffn(x, w, w, w)[0]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            mine = binding.Context("cuda:0", stream=stream)
+            for n in range(60):
+                D = sizes[(i + n) % len(sizes)]
+                got = mine.qk_norm_rope_backward(*inputs[D])
+                if not all(torch.equal(a, b) for a, b in zip(got, want[D])):
+                    wrong.append((i, n, D))
+                if not torch.equal(mine.gated_ffn(x, w, w, w)[0], y):
+                    wrong.append((i, n, "ffn"))
+            mine.sync_status()
+            mine.close()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+    ctx.close()
