@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <map>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -207,6 +208,7 @@ struct muloco_ctx {
   int64_t launches = 0;
 
   std::vector<muloco_adamw*> adam8;   // 8-bit AdamW states: one list per worker
+  std::vector<const void*> adam8_grads;   // a worker's gradients on their way to its list
 
   // operators around the optimizer (ops_capi.cu)
   float* qk_scratch = nullptr;     // gain-gradient partials of qk_norm.cu, then its tickets
@@ -692,8 +694,17 @@ MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_te
     ac.lr = cfg->adam_lr; ac.beta1 = cfg->adam_beta1; ac.beta2 = cfg->adam_beta2; ac.eps = cfg->adam_eps;
     ac.weight_decay = cfg->adam_wd; ac.bias_correction = cfg->adam_bias_correction;
     ac.state_bits = 8; ac.grad_dtype = cfg->grad_dtype;
+    std::vector<muloco_adamw_tensor> list;
+    try {
+      list.reserve(c->adam_ids.size());
+      c->adam8.reserve(K);
+      c->adam8_grads.resize(c->adam_ids.size());
+    } catch (const std::bad_alloc&) {
+      fail(c, MULOCO_ENOMEM, "host tables of the 8-bit AdamW states");
+      return bail(MULOCO_ENOMEM);
+    }
     for (int k = 0; k < K; ++k) {
-      std::vector<muloco_adamw_tensor> list;
+      list.clear();
       for (int i : c->adam_ids) {
         const TensorInfo& t = c->T[i];
         const size_t codes = (size_t)(t.numel() + MULOCO_ADAMW_BLOCK - 1) / MULOCO_ADAMW_BLOCK * MULOCO_ADAMW_BLOCK;
@@ -783,9 +794,15 @@ MULOCO_API muloco_status muloco_inner_step(muloco_ctx* c, int32_t worker, const 
   if (!grads && n > 0) return fail(c, MULOCO_EINVAL, "grads is NULL");
   const int k0 = worker < 0 ? 0 : worker, k1 = worker < 0 ? K : worker + 1;
   const int nw = k1 - k0;
+  // every pointer before the first launch: a refused step has changed nothing
+  const uintptr_t off_type = f.grad_dtype == MULOCO_BF16 ? 1 : 3;
   for (int k = k0; k < k1; ++k)
-    for (int i = 0; i < n; ++i)
-      if (!grads[(size_t)(k - k0) * n + i]) return fail(c, MULOCO_EINVAL, "gradient of tensor %d (worker %d) is NULL", i, k);
+    for (int i = 0; i < n; ++i) {
+      const void* g = grads[(size_t)(k - k0) * n + i];
+      if (!g) return fail(c, MULOCO_EINVAL, "gradient of tensor %d (worker %d) is NULL", i, k);
+      if (((uintptr_t)g) & off_type)
+        return fail(c, MULOCO_EINVAL, "gradient of tensor %d (worker %d) is not aligned to its type", i, k);
+    }
   if (n == 0) return MULOCO_OK;
   // the step counters advance only once the whole step has been enqueued (a call that fails on the
   // way leaves them, and with them AdamW's bias correction and the state blob, where they were)
@@ -874,7 +891,7 @@ MULOCO_API muloco_status muloco_inner_step(muloco_ctx* c, int32_t worker, const 
     {
       PhaseTimer t(c, MULOCO_PH_ADAMW);
       if (adam8) {
-        std::vector<const void*> g(c->adam_ids.size());
+        std::vector<const void*>& g = c->adam8_grads;
         for (int k = k0; k < k1; ++k) {
           for (size_t j = 0; j < g.size(); ++j) g[j] = grads[(size_t)(k - k0) * n + c->adam_ids[j]];
           rs = muloco_adamw_step(c->adam8[k], g.data(), c->worker_step[k] + 1, lr_scale);

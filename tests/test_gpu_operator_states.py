@@ -111,3 +111,33 @@ def test_optimizer_built_on_a_busy_stream():
         assert opt.theta_g[i].any()
     opt.sync_status()
     opt.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bits", [8, 32])
+def test_inner_step_refuses_a_misaligned_gradient_before_it_changes_anything(bits, dtype):
+    import ctypes as C
+    import torch
+    from paper_2505_23725_b200 import binding, configs
+    w = configs.mini_workload(K=2, H=2, vocab=100, norms=True, adam_state_bits=bits, grad_dtype=dtype)
+    opt = binding.MuLoCo(w, "cuda:0", init_seed=1, alloc_grads=True)
+    for g in opt.flat_grads:
+        g.normal_()
+    opt.inner_step()
+    opt.sync_status()
+
+    def state():
+        return [t.clone() for per in (opt.theta_k, opt.state1, opt.state2) for k in range(w.K) for t in per[k] if t is not None]
+
+    before, blob = state(), opt.get_state()
+    last = max(i for i, t in enumerate(w.tensors) if t.kind == configs.ADAMW)
+    ptrs = [opt.grads[k][i].data_ptr() for k in range(w.K) for i in range(opt.n)]
+    ptrs[opt.n + last] += 1 if dtype == "bf16" else 2
+    table = (C.c_void_p * len(ptrs))(*ptrs)
+    assert opt.lib.muloco_inner_step(opt.ctx, -1, table, 1.0) == binding.EINVAL
+    assert b"aligned" in opt.lib.muloco_last_error(opt.ctx)
+    opt.sync_status()
+    assert all(torch.equal(a, b) for a, b in zip(before, state())) and opt.get_state() == blob
+    opt.inner_step()
+    opt.sync_status()
+    opt.close()
