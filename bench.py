@@ -305,7 +305,8 @@ def main():
         import dataclasses
         if w.K % world != 0:
             raise SystemExit(f"--shard-workers: K={w.K} is not a multiple of {world} ranks")
-        w = dataclasses.replace(w, K=w.K // world)       # this rank's share of the workers
+        # this rank's share of the workers (adam_seed: 8-bit states round by the worker's number in the whole run)
+        w = dataclasses.replace(w, K=w.K // world, adam_seed=rank * (w.K // world))
         seed_init = rank_seeds(w.seed, 0)[0]             # every rank starts from the same global parameters
         if not distributed:                              # one rank: a communicator of its own
             os.environ.setdefault("MASTER_ADDR", "127.0.0.1"); os.environ.setdefault("MASTER_PORT", "29533")

@@ -128,8 +128,12 @@ typedef struct {
                           given at muloco_adamw_create).  state1_k / state2_k of such a tensor of n
                           elements then point to MULOCO_ADAMW_STATE8_BYTES(n) bytes, 16-byte aligned: the
                           codes, padded to whole blocks, and behind them one float32 scale per block.
-                          Worker k's dither has the seed k, and its elements count from the first
-                          AdamW tensor on.                                                      */
+                          Worker k's dither has the seed adam_seed + k, and its elements count from
+                          the first AdamW tensor on.                                            */
+  uint32_t adam_seed;  /* of the first worker's dither (8-bit AdamW states).  Where the workers of one run
+                          are spread over several contexts: the number of workers before this one's, so
+                          that no two workers share a dither and the run's results do not depend on how
+                          they are spread.                                                      */
 } muloco_config;
 
 /* Elements that share a scale in 8-bit AdamW states, and the bytes of such a state of n elements. */

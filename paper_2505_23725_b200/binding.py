@@ -61,7 +61,7 @@ class Config(C.Structure):
                 ("quant", C.c_int32), ("quant_block", C.c_int32), ("grad_dtype", C.c_int32),
                 ("quant_stages", C.c_int32), ("workspace_bytes", C.c_uint64),
                 ("error_feedback", C.c_int32), ("ef_beta", C.c_float),
-                ("topk_fraction", C.c_float), ("adam_state_bits", C.c_int32)]
+                ("topk_fraction", C.c_float), ("adam_state_bits", C.c_int32), ("adam_seed", C.c_uint32)]
 
 
 class Buffers(C.Structure):
@@ -270,7 +270,7 @@ def make_config(w: _cfg.Workload, workspace_bytes: int = 0, ns_mode: Optional[st
     c.error_feedback = int(w.error_feedback)
     c.ef_beta = w.ef_beta
     c.topk_fraction = w.topk_fraction
-    c.adam_state_bits = w.adam_state_bits
+    c.adam_state_bits, c.adam_seed = w.adam_state_bits, w.adam_seed
     c.grad_dtype = BF16 if w.grad_dtype == "bf16" else F32
     c.workspace_bytes = workspace_bytes
     for k, v in over.items():

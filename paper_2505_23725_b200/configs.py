@@ -54,6 +54,7 @@ class Workload:
     adam_beta2: float = 0.99
     adam_eps: float = 1e-8
     adam_state_bits: int = 32           # 8: AdamW moments as 8-bit codes with a scale per 256 elements
+    adam_seed: int = 0                  # ... of the first worker's dither; in a sharded run, the workers before this rank's
     seed: int = 0
     grad_dtype: str = "f32"
     notes: str = ""

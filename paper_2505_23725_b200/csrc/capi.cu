@@ -718,7 +718,7 @@ MULOCO_API muloco_status muloco_create(const muloco_config* cfg, const muloco_te
         a.wd_mult = t.wd_mult; a.lr_mult = t.lr_mult;
         list.push_back(a);
       }
-      ac.seed = (uint32_t)k;
+      ac.seed = cfg->adam_seed + (uint32_t)k;
       muloco_adamw* o = nullptr;
       const muloco_status as = muloco_adamw_create(c, &ac, list.data(), (int32_t)list.size(), &o);
       if (as != MULOCO_OK) return bail(as);

@@ -141,3 +141,33 @@ def test_inner_step_refuses_a_misaligned_gradient_before_it_changes_anything(bit
     opt.inner_step()
     opt.sync_status()
     opt.close()
+
+
+def test_workers_spread_over_contexts_round_as_in_one():
+    """8-bit states: the dither goes by the worker's number in the whole run, so two contexts of one worker each give what
+    one context of two gives; with the same number they would round alike."""
+    import dataclasses
+    import torch
+    from paper_2505_23725_b200 import binding, configs
+    w = configs.mini_workload(K=2, H=2, vocab=100, norms=True, adam_state_bits=8)
+    both = binding.MuLoCo(w, "cuda:0", init_seed=1, alloc_grads=True)
+    one = [binding.MuLoCo(dataclasses.replace(w, K=1, adam_seed=s), "cuda:0", init_seed=1, alloc_grads=True) for s in (0, 1)]
+    for step in range(3):
+        torch.manual_seed(step)
+        both.flat_grads[0].normal_()
+        both.flat_grads[1].copy_(both.flat_grads[0])              # the same gradients: only the dither differs
+        for o in one:
+            o.flat_grads[0].copy_(both.flat_grads[0])
+            o.inner_step()
+        both.inner_step()
+    for i, t in enumerate(w.tensors):
+        for k in range(2):
+            assert torch.equal(both.theta_k[k][i], one[k].theta_k[0][i])
+            assert torch.equal(both.state1[k][i], one[k].state1[0][i])
+            if t.kind == configs.ADAMW:
+                assert torch.equal(both.state2[k][i], one[k].state2[0][i])
+        if t.kind == configs.ADAMW:
+            assert not torch.equal(both.state1[0][i], both.state1[1][i])
+    for o in (both, *one):
+        o.sync_status()
+        o.close()
