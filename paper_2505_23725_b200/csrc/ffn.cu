@@ -206,7 +206,12 @@ __device__ __forceinline__ void act_both(Pair g, Pair& value, Pair& slope) {
   value = mul2(g, s);
   const Pair t = mul2(s, fma2(s, both(-1.0f), both(1.0f)));          // sigma (1 - sigma)
   if (ACT == MULOCO_ACT_SILU) slope = fma2(t, g, s);
-  else slope = fma2(t, fma2(cube, both(3.0f * GELU_K), mul2(g, both(GELU_K))), s);
+  else {
+    // the exponent's slope times g is beyond float32 from |g| = 2e13 on, where sigma (1 - sigma) has long been 0: kept finite, so
+    // that their product is 0 and not NaN
+    const float2 q = parts(fma2(cube, both(3.0f * GELU_K), mul2(g, both(GELU_K))));
+    slope = fma2(t, pair(fminf(fmaxf(q.x, -1e38f), 1e38f), fminf(fmaxf(q.y, -1e38f), 1e38f)), s);
+  }
 }
 
 template <int EPI, int ACT>
