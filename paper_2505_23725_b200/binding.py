@@ -114,13 +114,14 @@ _lib = None
 
 
 def _load_fastcall():
-    """The compiled call path of the operators (build.build_fastcall), or None where it was not built: the methods then
-    marshal their arguments in Python, in front of the same library."""
+    """The compiled call path of the operators (build.build_fastcall), or None where it was not built, or was for another
+    torch: the methods then marshal their arguments in Python, in front of the same library."""
+    import torch
     try:
         from . import _fastcall
-        return _fastcall
     except ImportError:
         return None
+    return _fastcall if getattr(_fastcall, "TORCH", None) == torch.__version__ else None
 
 
 def load_library():

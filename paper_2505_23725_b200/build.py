@@ -37,7 +37,13 @@ def build_library(force: bool = False, verbose: bool = False, lib_path: str = No
     if lib_path is None:
         lib_path = LIB_DEBUG if debug else LIB
     if lib_path == LIB:
-        build_fastcall()
+        # the library needs neither g++ nor torch's headers, and the binding does without the call path
+        try:
+            build_fastcall()
+        except Exception as e:                   # noqa: BLE001 - whatever keeps it from being built
+            if os.path.exists(FASTCALL):
+                os.remove(FASTCALL)              # made for other sources or another torch
+            sys.stderr.write(f"_fastcall.so was not built ({e}): the operators' calls are marshalled in Python\n")
     if not force and lib_path in (LIB, LIB_DEBUG) and not needs_build(lib_path):
         return lib_path
     objs = []
@@ -68,6 +74,7 @@ def build_library(force: bool = False, verbose: bool = False, lib_path: str = No
 
 
 FASTCALL = os.path.join(HERE, "_fastcall.so")
+FASTCALL_TORCH = os.path.join(HERE, "_build", "fastcall.torch")    # the torch version that it was made for
 
 
 def build_fastcall(force: bool = False) -> str:
@@ -75,7 +82,10 @@ def build_fastcall(force: bool = False) -> str:
     only) next to the library."""
     src = os.path.join(CSRC, "fastcall.cpp")
     deps = [src, os.path.join(os.path.dirname(HERE), "include", "muloco.h")]
-    if not force and os.path.exists(FASTCALL) and all(os.path.getmtime(FASTCALL) >= os.path.getmtime(d) for d in deps):
+    from importlib.metadata import version
+    made_for = open(FASTCALL_TORCH).read() if os.path.exists(FASTCALL_TORCH) else None
+    if not force and os.path.exists(FASTCALL) and made_for == version("torch") and \
+            all(os.path.getmtime(FASTCALL) >= os.path.getmtime(d) for d in deps):
         return FASTCALL
     import sysconfig
 
@@ -84,13 +94,16 @@ def build_fastcall(force: bool = False) -> str:
     cuda = os.path.join(os.path.dirname(os.path.dirname(_nvcc())), "include")
     lib = os.path.join(root, "lib")
     cmd = [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DMULOCO_TORCH="{torch.__version__}"',
            "-isystem", os.path.join(root, "include"), "-isystem", cuda, "-isystem", sysconfig.get_paths()["include"],
            src, "-o", FASTCALL, "-L" + lib, "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python", "-Wl,-rpath," + lib]
     p = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if p.returncode != 0:
         sys.stderr.write(p.stdout)
         raise RuntimeError("g++ failed on fastcall.cpp")
+    os.makedirs(os.path.dirname(FASTCALL_TORCH), exist_ok=True)
+    with open(FASTCALL_TORCH, "w") as f:
+        f.write(version("torch"))
     return FASTCALL
 
 

@@ -281,4 +281,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, 
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__fastcall(void) { return PyModule_Create(&module); }
+// TORCH: the version whose headers this file was compiled with; binding.py uses the module with no other.
+PyMODINIT_FUNC PyInit__fastcall(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "TORCH", MULOCO_TORCH) < 0) { Py_DECREF(m); return nullptr; }
+  return m;
+}
