@@ -519,6 +519,12 @@ MULOCO_API muloco_status muloco_get_timings(muloco_ctx* ctx, float* ms, int64_t*
  * muloco_sync_status reports as MULOCO_ECUDA ("out-of-range index"), and the access is skipped. */
 enum { MULOCO_DEBUG_WAIT_LIMIT_NS = 1, MULOCO_DEBUG_WITHHOLD_COPY = 2, MULOCO_DEBUG_CANARIES = 3,
        MULOCO_DEBUG_CORRUPT_CANARY = 4 };
+/* Test hook, host only: the form that each product of a feed-forward call of this size takes on a device of n_sms
+ * multiprocessors.  Returns the OR of MULOCO_FFN_* for those on 256 x 256 tiles (the others take the form for few tokens, or,
+ * like the weight gradients, have only the first); tiles[4], if not NULL: the 256 x 256 tiles of the launch of G | U, of Y, of
+ * dG and dU, and of the last one (the weight gradients, and dX where it is on such tiles), 0 where there is no such launch. */
+enum { MULOCO_FFN_GATE = 1, MULOCO_FFN_Y = 2, MULOCO_FFN_GATE_BACK = 4, MULOCO_FFN_DX = 8 };
+MULOCO_API int32_t muloco_debug_ffn_forms(int64_t tokens, int64_t d, int64_t F, int32_t n_sms, int64_t* tiles);
 MULOCO_API muloco_status muloco_debug_set(muloco_ctx* ctx, int32_t what, int64_t value);
 MULOCO_API muloco_status muloco_check_workspace(muloco_ctx* ctx);
 

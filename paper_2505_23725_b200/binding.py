@@ -41,6 +41,7 @@ EXPORTS = [
     "muloco_shard_layout", "muloco_shard_delta", "muloco_shard_step", "muloco_shard_broadcast",
     "muloco_adamw_create", "muloco_adamw_step", "muloco_adamw_moments", "muloco_adamw_destroy",
     "muloco_qk_norm_rope", "muloco_qk_norm_rope_backward", "muloco_gated_ffn", "muloco_gated_ffn_backward",
+    "muloco_debug_ffn_forms",
 ]
 
 
@@ -172,6 +173,7 @@ def load_library():
     lib.muloco_qk_norm_rope_backward.argtypes = [vp, packed, vp, i64, i64, vp, i64, i64, vp, vp, vp, vp]
     lib.muloco_gated_ffn.argtypes = [vp, packed, vp, vp, vp, vp]
     lib.muloco_gated_ffn_backward.argtypes = [vp, packed, vp, i64] + [vp] * 9
+    lib.muloco_debug_ffn_forms.argtypes = [i64, i64, i64, i32, C.POINTER(i64)]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("muloco_destroy", "muloco_last_error", "muloco_adamw_destroy"):
@@ -277,6 +279,14 @@ def make_config(w: _cfg.Workload, workspace_bytes: int = 0, ns_mode: Optional[st
     for k, v in over.items():
         setattr(c, k, v)
     return c
+
+
+def ffn_forms(tokens: int, d: int, F: int, n_sms: int = 148):
+    """muloco_debug_ffn_forms: the products of a feed-forward call of this size that run on 256 x 256 tiles, and the tiles of its
+    launches on them."""
+    tiles = (C.c_int64 * 4)()
+    forms = load_library().muloco_debug_ffn_forms(tokens, d, F, n_sms, tiles)
+    return {n for i, n in enumerate(("gate", "y", "gate_back", "dx")) if forms >> i & 1}, list(tiles)
 
 
 def _ptr_table(ptrs: Sequence[int]):

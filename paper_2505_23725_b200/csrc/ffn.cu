@@ -965,12 +965,27 @@ int slabs_of(int64_t k) { return (int)((k + BK - 1) / BK); }
 //   dX: 3000 tokens at 360 x 848 (72 tiles) 53 / 40; 1024 at 768 x 2048 (48 tiles) 47 / 47
 struct FewLimit { int64_t tokens, tiles; };
 constexpr FewLimit FEW_GATE = {128, 0}, FEW_DOWN = {512, 100}, FEW_GATE_BACK = {512, 64}, FEW_DX = {512, 64};
-bool few_tokens(const FfnArgs& a, int64_t N, FewLimit limit) {
-  const int64_t tiles = (N + 127) / 128 * ((a.T + 127) / 128);
-  return tiles <= a.n_sms && (a.T <= limit.tokens || tiles <= limit.tiles);
+bool few_tokens(int64_t T, int64_t N, int n_sms, FewLimit limit) {
+  const int64_t tiles = (N + 127) / 128 * ((T + 127) / 128);
+  return tiles <= n_sms && (T <= limit.tokens || tiles <= limit.tiles);
 }
+bool few_tokens(const FfnArgs& a, int64_t N, FewLimit limit) { return few_tokens(a.T, N, a.n_sms, limit); }
 
 }  // namespace
+
+int ffn_forms(int64_t T, int64_t d, int64_t F, int n_sms, int64_t* tiles) {
+  const int forms = (few_tokens(T, F, n_sms, FEW_GATE) ? 0 : MULOCO_FFN_GATE) | (few_tokens(T, d, n_sms, FEW_DOWN) ? 0 : MULOCO_FFN_Y) |
+                    (few_tokens(T, F, n_sms, FEW_GATE_BACK) ? 0 : MULOCO_FFN_GATE_BACK) |
+                    (few_tokens(T, d, n_sms, FEW_DX) ? 0 : MULOCO_FFN_DX);
+  if (tiles) {
+    auto of = [](int64_t m, int64_t n, int64_t width) { return (m + TM - 1) / TM * ((n + width - 1) / width); };
+    tiles[0] = forms & MULOCO_FFN_GATE ? of(T, F, 128) : 0;
+    tiles[1] = forms & MULOCO_FFN_Y ? of(T, d, BN) : 0;
+    tiles[2] = forms & MULOCO_FFN_GATE_BACK ? of(T, F, BN) : 0;
+    tiles[3] = 2 * of(d, F, BN) + of(F, d, BN) + (forms & MULOCO_FFN_DX ? of(T, d, BN) : 0);
+  }
+  return forms;
+}
 
 cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what) {
   cudaError_t bound = bind_context(what);

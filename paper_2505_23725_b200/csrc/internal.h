@@ -293,5 +293,6 @@ struct FfnArgs {
 };
 cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what);
 cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what);
+int ffn_forms(int64_t T, int64_t d, int64_t F, int n_sms, int64_t* tiles);   // muloco_debug_ffn_forms
 
 }  // namespace muloco

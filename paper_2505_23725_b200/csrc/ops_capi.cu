@@ -353,6 +353,10 @@ MULOCO_API muloco_status muloco_gated_ffn(muloco_ctx* c, const muloco_ffn* a, vo
   return MULOCO_OK;
 }
 
+MULOCO_API int32_t muloco_debug_ffn_forms(int64_t tokens, int64_t d, int64_t F, int32_t n_sms, int64_t* tiles) {
+  return ffn_forms(tokens, d, F, n_sms, tiles);
+}
+
 MULOCO_API muloco_status muloco_gated_ffn_backward(muloco_ctx* c, const muloco_ffn* a, const void* dy, int64_t lddy,
                                                    const void* g, const void* u, const void* h, void* dg, void* du,
                                                    void* dx, void* dw1, void* dw3, void* dw2) {

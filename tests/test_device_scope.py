@@ -42,7 +42,7 @@ def test_scope_sets_and_restores(tmp_path):
 
 # calls that only read or write the context's host memory
 HOST_ONLY = {"muloco_fragments_due", "muloco_get_state", "muloco_set_state", "muloco_set_timing", "muloco_last_error",
-             "muloco_debug_set", "muloco_check_workspace", "muloco_shard_layout"}
+             "muloco_debug_set", "muloco_check_workspace", "muloco_shard_layout", "muloco_debug_ffn_forms"}
 # these have no context: the device that is current is the caller's choice (and becomes that of the context made)
 NO_CONTEXT = {"muloco_create", "muloco_newton_schulz_static"}
 
