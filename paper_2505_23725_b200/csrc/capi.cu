@@ -517,6 +517,12 @@ void ctx_count_launches(muloco_ctx* c, int n) { c->launches += n; }
 
 int ctx_device(const muloco_ctx* c) { return c->device; }
 
+int ctx_take_withhold(muloco_ctx* c) {
+  const int w = c->debug_withhold;
+  c->debug_withhold = 0;
+  return w;
+}
+
 float* ctx_qk_scratch(muloco_ctx* c, int** tickets) {
   *tickets = reinterpret_cast<int*>(c->qk_scratch + QK_SCRATCH_FLOATS);
   return c->qk_scratch;

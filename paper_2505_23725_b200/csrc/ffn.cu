@@ -75,6 +75,7 @@ struct Prob {
 struct Params {
   Prob prob[MAX_PROBS];
   int n_probs, total_tiles, n_maps, act;
+  int withhold;             // test hook: the first thread block issues no copies
   int* status;
   unsigned long long wait_limit_ns;
 };
@@ -260,7 +261,7 @@ ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) 
 
   if (warp == 0) {
     // ------------------------------ TMA producer ------------------------------
-    if (lane == 0) {
+    if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
       const uint32_t empty0 = smem_u32(&bar_empty[0]);
       const uint32_t full0 = smem_u32(&bar_full[0]);
       const uint32_t full0_bar = map_to_rank(full0, 0);   // both CTAs' copies are counted on the barrier of rank 0
@@ -467,10 +468,12 @@ ffn_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Params p) 
     // give copies and MMAs still in flight time to land before memory is released
     const uint64_t t0 = global_timer_ns();
     while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);
-    if (threadIdx.x == 0) atomicOr(p.status, ST_TIMEOUT);
   }
+  __syncwarp();
   tc_fence_before();
   cluster_sync_all();
+  // (only here does every thread know of a wait that ran out: the one that copies may have been done before)
+  if (threadIdx.x == 0 && abort_flag) atomicOr(p.status, ST_TIMEOUT);
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc<CG>(tmem_base, TMEM_COLS);
@@ -509,6 +512,7 @@ struct FewParams {
   void* out; void* out2; void* out3;
   const void* in1; const void* in2;
   int weights_early;         // the kernel before this one does not write the weights
+  int withhold;              // test hook: the first thread block issues no copies
   int* status;
   unsigned long long wait_limit_ns;
 };
@@ -563,7 +567,7 @@ ffn_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ Few
   const uint32_t tmem_base = tmem_base_slot;
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (lane == 0 && !(p.withhold && (blockIdx.x | blockIdx.y | blockIdx.z) == 0)) {
       const bool a_mn = p.a_mn, a_wide = p.a_wide;
       const int slabs0 = p.slabs0;
       auto load_weights = [&](int kb, uint32_t stage) {
@@ -848,12 +852,13 @@ cudaError_t launch_kernel(cudaStream_t st, const Builder& b, int n_sms) {
   return cudaLaunchKernelEx(&cfg, kernel, b.maps, b.p);
 }
 
-cudaError_t launch_built(cudaStream_t st, Builder& b, const FfnArgs& a, int epi, const char** what) {
+cudaError_t launch_built(cudaStream_t st, Builder& b, const FfnArgs& a, int epi, const int* launches, const char** what) {
   *what = "cuTensorMapEncodeTiled";
   if (!b.ok) return cudaErrorInvalidValue;
   *what = "launch of the feed-forward kernel";
   b.p.n_maps = b.n_maps;
   b.p.act = a.act;
+  b.p.withhold = a.withhold && *launches == 0;
   b.p.status = a.status;
   b.p.wait_limit_ns = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
   const bool gelu = a.act == MULOCO_ACT_GELU;
@@ -912,7 +917,7 @@ struct FewOperand { Mat weight[2]; Mat tokens[2]; };   // per operand pair (gate
 
 // One product of the few-token form.  `mn`: the weights are stored contraction index first (MN-major operand).
 cudaError_t launch_few(cudaStream_t st, const FfnArgs& a, int epi, const FewOperand& q, bool mn, int n_pairs,
-                       FewParams p, const char** what) {
+                       FewParams p, const int* launches, const char** what) {
   const int nt = few_tile(a.T, p.M, a.n_sms);
   FewMaps m;
   bool ok = true;
@@ -935,6 +940,7 @@ cudaError_t launch_few(cudaStream_t st, const FfnArgs& a, int epi, const FewOper
   if (!ok) return cudaErrorInvalidValue;
   *what = "launch of the feed-forward kernel for few tokens";
   p.T = (int)a.T;
+  p.withhold = a.withhold && *launches == 0;
   p.status = a.status;
   p.wait_limit_ns = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
   // Split the contraction until every SM has a CTA.  Clusters of four and eight only while all of them find room at once,
@@ -996,7 +1002,7 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
     p.M = (int)a.F; p.slabs0 = p.slabs = slabs_of(a.d);
     p.out = a.h; p.out2 = a.g; p.out3 = a.u;
     FewOperand q{{Mat{a.w1, a.d, a.F, a.ldw1}, Mat{a.w3, a.d, a.F, a.ldw3}}, {Mat{a.x, a.T, a.d, a.ldx}, Mat{}}};
-    const cudaError_t e = launch_few(st, a, EPI_GATE, q, true, 1, p, what);
+    const cudaError_t e = launch_few(st, a, EPI_GATE, q, true, 1, p, launches, what);
     if (e != cudaSuccess) return e;
   } else {
     Builder b;
@@ -1008,7 +1014,7 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
     q.map_b[1] = b.mnmajor(Mat{a.w3, a.d, a.F, a.ldw3}, &wide3);
     b.ok = b.ok && wide3 == q.b_wide;
     q.out = a.h; q.out2 = a.g; q.out3 = a.u;
-    const cudaError_t e = launch_built(st, b, a, EPI_GATE, what);
+    const cudaError_t e = launch_built(st, b, a, EPI_GATE, launches, what);
     if (e != cudaSuccess) return e;
   }
   ++*launches;
@@ -1020,7 +1026,7 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
     p.out = a.y;
     p.weights_early = 1;
     FewOperand r{{Mat{a.w2, a.F, a.d, a.ldw2}, Mat{}}, {Mat{a.h, a.T, a.F, a.F}, Mat{}}};
-    e = launch_few(st, a, EPI_STORE, r, true, 1, p, what);
+    e = launch_few(st, a, EPI_STORE, r, true, 1, p, launches, what);
   } else {
     Builder b;
     Prob& q = b.add(a.T, a.d, BN, a.F, 0);
@@ -1028,7 +1034,7 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
     q.b_mn = 1;
     q.map_b[0] = b.mnmajor(Mat{a.w2, a.F, a.d, a.ldw2}, &q.b_wide);
     q.out = a.y;
-    e = launch_built(st, b, a, EPI_STORE, what);
+    e = launch_built(st, b, a, EPI_STORE, launches, what);
   }
   if (e == cudaSuccess) ++*launches;
   return e;
@@ -1045,7 +1051,7 @@ cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches
     p.in1 = a.g; p.in2 = a.u;
     p.out = a.dg; p.out2 = a.du;
     FewOperand q{{Mat{a.w2, a.F, a.d, a.ldw2}, Mat{}}, {Mat{a.dy, a.T, a.d, a.lddy}, Mat{}}};
-    cudaError_t e = launch_few(st, a, EPI_GATE_BACK, q, false, 1, p, what);
+    cudaError_t e = launch_few(st, a, EPI_GATE_BACK, q, false, 1, p, launches, what);
     if (e != cudaSuccess) return e;
     ++*launches;
   } else if (a.dx || a.dw1 || a.dw3) {
@@ -1055,7 +1061,7 @@ cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches
     q.map_b[0] = b.kmajor(Mat{a.w2, a.F, a.d, a.ldw2});
     q.in1 = a.g; q.in2 = a.u;
     q.out = a.dg; q.out2 = a.du;
-    cudaError_t e = launch_built(st, b, a, EPI_GATE_BACK, what);
+    cudaError_t e = launch_built(st, b, a, EPI_GATE_BACK, launches, what);
     if (e != cudaSuccess) return e;
     ++*launches;
   }
@@ -1067,7 +1073,7 @@ cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches
     p.weights_early = 1;
     FewOperand q{{Mat{a.w1, a.d, a.F, a.ldw1}, Mat{a.w3, a.d, a.F, a.ldw3}},
                  {Mat{a.dg, a.T, a.F, a.F}, Mat{a.du, a.T, a.F, a.F}}};
-    cudaError_t e = launch_few(st, a, EPI_STORE, q, false, 2, p, what);
+    cudaError_t e = launch_few(st, a, EPI_STORE, q, false, 2, p, launches, what);
     if (e != cudaSuccess) return e;
     ++*launches;
   }
@@ -1099,7 +1105,7 @@ cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches
     q.out = a.dw2;
   }
   if (!b.p.n_probs) return cudaSuccess;
-  cudaError_t e = launch_built(st, b, a, EPI_STORE, what);
+  cudaError_t e = launch_built(st, b, a, EPI_STORE, launches, what);
   if (e == cudaSuccess) ++*launches;
   return e;
 }

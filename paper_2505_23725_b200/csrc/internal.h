@@ -182,6 +182,7 @@ CtxView ctx_view(muloco_ctx* c);
 muloco_status ctx_fail(muloco_ctx* c, muloco_status s, const char* fmt, ...);
 void ctx_count_launches(muloco_ctx* c, int n);
 int ctx_device(const muloco_ctx* c);
+int ctx_take_withhold(muloco_ctx* c);               // MULOCO_DEBUG_WITHHOLD_COPY, which it clears
 // First thing of every entry point that touches the device: the context's device is current until it returns.
 #define ON_DEVICE(c)                                                                                          \
   const muloco::DeviceScope device_scope_(muloco::ctx_device(c));                                             \
@@ -290,6 +291,7 @@ struct FfnArgs {
   int* status;
   unsigned long long wait_limit_ns;
   int n_sms;
+  int withhold;                                // test hook, of the call's first launch
 };
 cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const char** what);
 cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what);

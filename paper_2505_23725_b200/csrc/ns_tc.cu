@@ -836,6 +836,8 @@ ns_tc_kernel(const __grid_constant__ TcMaps maps, const TcParams p) {
   }
   tc_fence_before();
   if (CG == 2) cluster_sync_all(); else __syncthreads();
+  // (the thread that raised the flag above may have been done before another's wait ran out; here every thread knows)
+  if (threadIdx.x == 0 && abort_flag) atomicOr(p.status, abort_flag == 2 ? ST_BOUNDS : ST_TIMEOUT);
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc<CG>(tmem_base, TMEM_COLS);

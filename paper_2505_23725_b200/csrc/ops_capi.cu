@@ -345,6 +345,7 @@ MULOCO_API muloco_status muloco_gated_ffn(muloco_ctx* c, const muloco_ffn* a, vo
   const CtxView v = ctx_view(c);
   FfnArgs f = ffn_args(a, v);
   f.g = g; f.u = u; f.h = h; f.y = y;
+  f.withhold = ctx_take_withhold(c);
   int n = 0;
   const char* what = "";
   const cudaError_t e = launch_ffn(v.st, f, &n, &what);
@@ -383,6 +384,7 @@ MULOCO_API muloco_status muloco_gated_ffn_backward(muloco_ctx* c, const muloco_f
   f.dy = dy; f.lddy = lddy;
   f.g = const_cast<void*>(g); f.u = const_cast<void*>(u); f.h = const_cast<void*>(h);
   f.dg = dg; f.du = du; f.dx = dx; f.dw1 = dw1; f.dw3 = dw3; f.dw2 = dw2;
+  f.withhold = ctx_take_withhold(c);
   int n = 0;
   const char* what = "";
   const cudaError_t e = launch_ffn_backward(v.st, f, &n, &what);

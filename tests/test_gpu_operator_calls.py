@@ -106,3 +106,45 @@ def test_calls_from_several_threads_with_sizes_in_turn():
         t.join()
     assert not wrong
     ctx.close()
+
+
+@pytest.mark.parametrize("shape", [(5, 64, 136), (100, 264, 520), (300, 128, 264), (900, 1024, 1160), (4100, 1032, 1160)], ids=str)
+@pytest.mark.parametrize("back", [False, True])
+def test_a_wait_that_runs_out_is_reported_and_the_context_stays_usable(shape, back):
+    """One thread block issues no copies: the waits for them run out after the 2 ms that the test sets, the kernel returns, the timeout is
+    reported once, and the next call is right.  Few-token and 256 x 256 forms; with 128 or fewer columns of X the other CTA of the
+    pair has issued all its copies, and its copying thread is done, long before a wait runs out."""
+    import time
+    import torch
+    from paper_2505_23725_b200 import binding
+    T, d, F = shape
+    torch.manual_seed(T)
+    bf = torch.bfloat16
+    x, dy = (torch.randn(T, d, device="cuda").to(bf) for _ in range(2))
+    w1, w3 = ((torch.randn(d, F, device="cuda") * d ** -0.5).to(bf) for _ in range(2))
+    w2 = (torch.randn(F, d, device="cuda") * F ** -0.5).to(bf)
+    ctx = binding.Context("cuda:0")
+    _, saved = ctx.gated_ffn(x, w1, w3, w2)
+
+    def call():
+        if back:
+            return ctx.gated_ffn_backward(dy, x, w1, w3, w2, saved)
+        out, kept = ctx.gated_ffn(x, w1, w3, w2)
+        return (out, *kept)
+    want = call()
+    ctx.sync_status()
+    def hook(what, value):
+        assert ctx.lib.muloco_debug_set(ctx.ctx, what, value) == binding.OK
+    hook(binding.DEBUG_WAIT_LIMIT_NS, 2_000_000)
+    hook(binding.DEBUG_WITHHOLD_COPY, 1)
+    t0 = time.perf_counter()
+    call()
+    with pytest.raises(binding.MulocoError) as e:
+        ctx.sync_status()
+    assert e.value.status == binding.ETIMEOUT
+    assert time.perf_counter() - t0 < 5.0
+    ctx.sync_status()                                   # read once
+    hook(binding.DEBUG_WAIT_LIMIT_NS, 0)
+    assert all(torch.equal(a, b) for a, b in zip(call(), want))
+    ctx.sync_status()
+    ctx.close()
