@@ -148,3 +148,40 @@ def test_a_wait_that_runs_out_is_reported_and_the_context_stays_usable(shape, ba
     assert all(torch.equal(a, b) for a, b in zip(call(), want))
     ctx.sync_status()
     ctx.close()
+
+
+def test_autograd_forms_take_any_layout():
+    """layers.py in front of the library itself: inputs and gradients whose layout it refuses give the bits of contiguous ones."""
+    import torch
+    from paper_2505_23725_b200 import binding, layers
+    ctx = binding.Context("cuda:0")
+    torch.manual_seed(0)
+    T, d, F, bf = 70, 64, 136, torch.bfloat16
+    x, other = (torch.randn(T, d, device="cuda").to(bf) for _ in range(2))
+    ws = [(torch.randn(*s, device="cuda") / 8).to(bf) for s in ((d, F), (d, F), (F, d))]
+    wide = torch.cat([other[:, :1], x, other[:, :2]], 1)
+    row = torch.randn(d, device="cuda").to(bf)
+    losses = (lambda y: (y.sum(0) * row).sum(), lambda y: (torch.cat([y, other[:, :3]], 1) * wide).float().sum(),
+              lambda y: (torch.cat([other[:, :3], y], 1) * wide).float().sum(), lambda y: (y * other).float().sum())
+    # the gradients that reach the block, contiguous
+    for loss in losses:
+        y0 = torch.zeros(T, d, dtype=bf, device="cuda", requires_grad=True)
+        dy = torch.autograd.grad(loss(y0), y0)[0].contiguous()
+        want = ctx.gated_ffn_backward(dy, x, *ws, ctx.gated_ffn(x, *ws)[1])
+        for view in (x, wide[:, 1:d + 1], x.t().contiguous().t()):
+            leaves = [t.detach().requires_grad_() for t in (view, *ws)]
+            loss(layers.gated_ffn(ctx, *leaves)).backward()
+            assert all(torch.equal(t.grad, g) for t, g in zip(leaves, want))
+    q = torch.randn(9, 3, 16, device="cuda", requires_grad=True)
+    gain, ang = torch.randn(16, device="cuda", requires_grad=True), torch.randn(9, 8, device="cuda")
+    dq = torch.randn(9, 16, 3, device="cuda").transpose(1, 2)
+    want = ctx.qk_norm_rope_backward(dq.contiguous(), None, q.detach(), None, ang.cos(), ang.sin(), None, gain.detach())
+    for alone in (0, 1):
+        pair, gains = [None, None], [None, None]
+        pair[alone], gains[alone] = q, gain
+        out = layers.qk_norm_rope(ctx, *pair, ang.cos(), ang.sin(), None, *gains)
+        assert out[1 - alone] is None
+        got = torch.autograd.grad(out[alone], (q, gain), dq)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[2])
+    ctx.sync_status()
+    ctx.close()
