@@ -22,12 +22,17 @@ class _Once(torch.autograd.Function):
         raise RuntimeError(f"{ctx.name} is differentiable once: the gradients of its gradients are not implemented")
 
 
+def _dual(t):
+    """Whether t carries a forward-mode tangent."""
+    return forward_ad.unpack_dual(t).tangent is not None
+
+
 def _once(name, results, inputs):
     """The results of a backward pass, which are functions of `inputs` without a graph.  Where a graph is being recorded
     (create_graph=True) they get one that raises, so that a loss made from them cannot lose their part silently.  (torch's
     once_differentiable looks at the incoming gradients only: those of y.sum() need none.)  An incoming gradient with a
     forward-mode tangent raises here, as a custom function's dual input does."""
-    if torch.is_grad_enabled() or any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in inputs):
+    if torch.is_grad_enabled() or any(t is not None and _dual(t) for t in inputs):
         return _Once.apply(name, len(results), *results, *inputs)
     return results
 
@@ -36,9 +41,13 @@ def _rows(t):
     """t, or a copy of it where the library would refuse its layout: it takes rows of consecutive entries that start on 16 bytes
     and do not overlap, a multiple of 8 entries apart.  Views and the gradients that autograd makes of sums, slices and
     concatenations need not be laid out so."""
-    fits = t.dim() == 2 and t.stride(1) == 1 and t.data_ptr() % 16 == 0 and \
-        (t.shape[0] < 2 or (t.stride(0) >= t.shape[1] and t.stride(0) % 8 == 0))
-    return t if fits else t.clone(memory_format=torch.contiguous_format)
+    if t.data_ptr() % 16 == 0:
+        if t.is_contiguous():
+            return t
+        if t.dim() == 2 and t.stride(1) == 1 and \
+                (t.shape[0] < 2 or (t.stride(0) >= t.shape[1] and t.stride(0) % 8 == 0)):
+            return t
+    return t.clone(memory_format=torch.contiguous_format)
 
 
 class _GatedFFN(torch.autograd.Function):
@@ -59,12 +68,14 @@ class _GatedFFN(torch.autograd.Function):
 
 def gated_ffn(owner, x, w1, w3, w2, activation: str = "silu"):
     """(act(x w1) * (x w3)) w2 over the last dimension of x, differentiable in x and the weights (all bf16)."""
-    rows, w1, w3, w2 = (_rows(t) for t in (x.reshape(-1, x.shape[-1]), w1, w3, w2))
-    # (G, U and H are kept only for a backward pass; without one the call still goes through the function, which refuses
-    # forward-mode inputs)
-    save = torch.is_grad_enabled() and any(t.requires_grad for t in (x, w1, w3, w2))
-    y = _GatedFFN.apply(owner, activation, save, rows, w1, w3, w2)
-    return y.view(*x.shape[:-1], w2.shape[1])
+    rows, w1, w3, w2 = _rows(x if x.dim() == 2 else x.reshape(-1, x.shape[-1])), _rows(w1), _rows(w3), _rows(w2)
+    # G, U and H are kept only for a backward pass; forward-mode inputs go through the function, which refuses them
+    save = torch.is_grad_enabled() and (rows.requires_grad or w1.requires_grad or w3.requires_grad or w2.requires_grad)
+    if save or _dual(rows) or _dual(w1) or _dual(w3) or _dual(w2):
+        y = _GatedFFN.apply(owner, activation, save, rows, w1, w3, w2)
+    else:
+        y, _ = owner.gated_ffn(rows, w1, w3, w2, activation, save=False)
+    return y if x.dim() == 2 else y.view(*x.shape[:-1], w2.shape[1])
 
 
 class _QKNormRope(torch.autograd.Function):
