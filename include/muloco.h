@@ -516,7 +516,7 @@ MULOCO_API muloco_status muloco_get_timings(muloco_ctx* ctx, float* ms, int64_t*
  *       the host overwrites (one byte, by a memset on the stream) in the next chunk, so that
  *       the check has something to find.  One-shot.
  * A debug build of the library (-DMULOCO_DEBUG, build.build_library(debug=True)) adds
- * device-side checks of the indices the kernels derive; a failed check raises a flag that
+ * device-side checks of the indices that the Newton-Schulz, sync and inner-step AdamW kernels derive; a failed check raises a flag that
  * muloco_sync_status reports as MULOCO_ECUDA ("out-of-range index"), and the access is skipped. */
 enum { MULOCO_DEBUG_WAIT_LIMIT_NS = 1, MULOCO_DEBUG_WITHHOLD_COPY = 2, MULOCO_DEBUG_CANARIES = 3,
        MULOCO_DEBUG_CORRUPT_CANARY = 4 };

@@ -9,7 +9,7 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmuloco.so")
-LIB_DEBUG = os.path.join(HERE, "libmuloco_debug.so")   # the same sources with -DMULOCO_DEBUG (index checks in the kernels)
+LIB_DEBUG = os.path.join(HERE, "libmuloco_debug.so")   # the same sources with -DMULOCO_DEBUG (index checks of the optimizer's kernels)
 SOURCES = ["capi.cu", "elementwise.cu", "outer_sync.cu", "topk.cu", "ns_fp32.cu", "ns_tc.cu", "ns_static.cu",
            "adamw.cu", "qk_norm.cu", "ffn.cu", "ops_capi.cu"]
 
@@ -33,7 +33,7 @@ def needs_build(lib_path: str = LIB) -> bool:
 def build_library(force: bool = False, verbose: bool = False, lib_path: str = None, debug: bool = False) -> str:
     """Compile every CUDA source of the package for sm_100a into one shared library.
     debug=True builds libmuloco_debug.so: the same sources with -DMULOCO_DEBUG, i.e. with the
-    kernels' index checks compiled in (a failed check raises a status flag, nothing traps)."""
+    index checks of the Newton-Schulz, sync and inner-step AdamW kernels compiled in (a failed check raises a status flag, nothing traps)."""
     if lib_path is None:
         lib_path = LIB_DEBUG if debug else LIB
     if lib_path == LIB:

@@ -7,9 +7,9 @@
 // integers) and encodes again, all in registers: one read and one write of everything.
 //
 // 32-bit states are bound by memory (134M elements, bf16 gradients: 505 us, 6.9 TB/s).  8-bit states move 14 to 16
-// bytes an element, and at the memory's rate there are about 77 issue slots for the 14: the 65 that it takes (two conversions, the
+// bytes an element, and at the memory's rate there are about 77 issue slots for the 14: the 68 that it takes (two conversions, the
 // moments, a correctly rounded root, a hash of two dithers, two encodings) are what the paired operations and byte moves below
-// save for.  49M elements with bf16 gradients and a bf16 copy: 139 us, 5.7 TB/s; 374M with f32 gradients 980 us, 6.1 TB/s.
+// save for.  49M elements with bf16 gradients and a bf16 copy: 140 us, 5.6 TB/s; 374M with f32 gradients 971-1013 us, 5.9-6.2 TB/s.
 #include "internal.h"
 
 namespace muloco {

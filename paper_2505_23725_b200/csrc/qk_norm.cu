@@ -12,8 +12,8 @@
 // elements.  32 / G heads of one token fit a warp at a time; the warp keeps what the token's cosines and sines (and, forward, the
 // gains) make of a pair in registers while it walks over the token's heads.
 //
-// Measured at 16384 tokens, 16 + 16 heads of 128, bf16: forward 45 us (6.2 TB/s, issue slots 62 % taken), backward 76 us (5.4 TB/s; 158
-// registers leave 12 warps per SM).
+// Measured at 16384 tokens, 16 + 16 heads of 128, bf16, in a short burst: forward 45 us (6.2 TB/s, issue slots 62 % taken), backward 76 us
+// (5.4 TB/s; 158 registers leave 12 warps per SM); among other work 48 and 85 us.
 #include <string.h>
 
 #include <atomic>
