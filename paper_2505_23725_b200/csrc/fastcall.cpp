@@ -53,6 +53,15 @@ bool dense_vector(const at::Tensor& t, const Call& c, at::ScalarType type, int64
 }
 void* ptr(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
 
+// Calls the library without the interpreter's lock: a launch waits when the queue is full, for a GPU that may be waiting for a Python
+// callback.
+template <typename F> int unlocked(F call) {
+  PyThreadState* const state = PyEval_SaveThread();
+  const int status = call();
+  PyEval_RestoreThread(state);
+  return status;
+}
+
 PyObject* none() { Py_RETURN_NONE; }
 PyObject* wrap(const at::Tensor& t) { return THPVariable_Wrap(t); }
 PyObject* wrap_or_none(const at::Tensor& t) { return t.defined() ? THPVariable_Wrap(t) : none(); }
@@ -119,7 +128,7 @@ PyObject* qk_forward(PyObject*, PyObject* const* o, Py_ssize_t n) {
   if (r.q) { qo = at::empty_like(*r.q); s[0][0] = qo.stride(0); s[0][1] = qo.stride(1); }
   if (r.k) { ko = at::empty_like(*r.k); s[1][0] = ko.stride(0); s[1][1] = ko.stride(1); }
   const auto fn = (decltype(&muloco_qk_norm_rope))c.fn;
-  const int st = fn(c.ctx, &r.a, r.q ? qo.data_ptr() : nullptr, s[0][0], s[0][1], r.k ? ko.data_ptr() : nullptr, s[1][0], s[1][1]);
+  const int st = unlocked([&] { return fn(c.ctx, &r.a, r.q ? qo.data_ptr() : nullptr, s[0][0], s[0][1], r.k ? ko.data_ptr() : nullptr, s[1][0], s[1][1]); });
   if (st) return PyLong_FromLong(st);
   return Py_BuildValue("(NN)", wrap_or_none(qo), wrap_or_none(ko));
 }
@@ -147,8 +156,8 @@ PyObject* qk_backward(PyObject*, PyObject* const* o, Py_ssize_t n) {
   }
   auto p = [](const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
   const auto fn = (decltype(&muloco_qk_norm_rope_backward))c.fn;
-  const int st = fn(c.ctx, &r.a, ptr(dy[0]), s[0][0], s[0][1], ptr(dy[1]), s[1][0], s[1][1], p(dx[0]), p(dx[1]),
-                    (float*)p(dg[0]), (float*)p(dg[1]));
+  const int st = unlocked([&] { return fn(c.ctx, &r.a, ptr(dy[0]), s[0][0], s[0][1], ptr(dy[1]), s[1][0], s[1][1], p(dx[0]), p(dx[1]),
+                    (float*)p(dg[0]), (float*)p(dg[1])); });
   if (st) return PyLong_FromLong(st);
   return Py_BuildValue("(NNNN)", wrap_or_none(dx[0]), wrap_or_none(dx[1]), wrap_or_none(dg[0]), wrap_or_none(dg[1]));
 }
@@ -190,7 +199,7 @@ PyObject* ffn_forward(PyObject*, PyObject* const* o, Py_ssize_t n) {
     u = at::empty({a.tokens, a.F}, x->options());
   }
   const auto fn = (decltype(&muloco_gated_ffn))c.fn;
-  const int st = fn(c.ctx, &a, save ? g.data_ptr() : nullptr, save ? u.data_ptr() : nullptr, h.data_ptr(), y.data_ptr());
+  const int st = unlocked([&] { return fn(c.ctx, &a, save ? g.data_ptr() : nullptr, save ? u.data_ptr() : nullptr, h.data_ptr(), y.data_ptr()); });
   if (st) return PyLong_FromLong(st);
   if (!save) return Py_BuildValue("(NO)", wrap(y), Py_None);
   return Py_BuildValue("(N(NNN))", wrap(y), wrap(g), wrap(u), wrap(h));
@@ -217,8 +226,8 @@ PyObject* ffn_backward(PyObject*, PyObject* const* o, Py_ssize_t n) {
   at::Tensor scratch = at::empty({2, a.tokens, a.F}, opt), dx = at::empty({a.tokens, a.d}, opt),
              dw1 = at::empty({a.d, a.F}, opt), dw3 = at::empty({a.d, a.F}, opt), dw2 = at::empty({a.F, a.d}, opt);
   const auto fn = (decltype(&muloco_gated_ffn_backward))c.fn;
-  const int st = fn(c.ctx, &a, dy->data_ptr(), a.tokens > 1 ? dy->stride(0) : a.d, s[0]->data_ptr(), s[1]->data_ptr(), s[2]->data_ptr(),
-                    scratch.data_ptr(), static_cast<char*>(scratch.data_ptr()) + a.tokens * a.F * 2, dx.data_ptr(), dw1.data_ptr(), dw3.data_ptr(), dw2.data_ptr());
+  const int st = unlocked([&] { return fn(c.ctx, &a, dy->data_ptr(), a.tokens > 1 ? dy->stride(0) : a.d, s[0]->data_ptr(), s[1]->data_ptr(), s[2]->data_ptr(),
+                    scratch.data_ptr(), static_cast<char*>(scratch.data_ptr()) + a.tokens * a.F * 2, dx.data_ptr(), dw1.data_ptr(), dw3.data_ptr(), dw2.data_ptr()); });
   if (st) return PyLong_FromLong(st);
   return Py_BuildValue("(NNNN)", wrap(dx), wrap(dw1), wrap(dw3), wrap(dw2));
 }
@@ -231,7 +240,9 @@ PyObject* adamw_step(PyObject*, PyObject* const* o, Py_ssize_t n) {
   const double scale = PyFloat_AsDouble(o[5]);
   if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
   if (!c.ok) return none();
-  return PyLong_FromLong(((decltype(&muloco_adamw_step))c.fn)(reinterpret_cast<muloco_adamw*>(c.ctx), nullptr, step, (float)scale));
+  return PyLong_FromLong(unlocked([&] {
+    return ((decltype(&muloco_adamw_step))c.fn)(reinterpret_cast<muloco_adamw*>(c.ctx), nullptr, step, (float)scale);
+  }));
 }
 
 // (list, library function, device, stream), a float32 tensor to make the results like, their length
@@ -244,7 +255,7 @@ PyObject* adamw_moments(PyObject*, PyObject* const* o, Py_ssize_t n) {
   if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
   if (!ok || !like) return none();
   at::Tensor m = at::empty({len}, like->options()), v = at::empty({len}, like->options());
-  const int st = ((decltype(&muloco_adamw_moments))c.fn)(reinterpret_cast<muloco_adamw*>(c.ctx), (float*)m.data_ptr(), (float*)v.data_ptr());
+  const int st = unlocked([&] { return ((decltype(&muloco_adamw_moments))c.fn)(reinterpret_cast<muloco_adamw*>(c.ctx), (float*)m.data_ptr(), (float*)v.data_ptr()); });
   if (st) return PyLong_FromLong(st);
   return Py_BuildValue("(NN)", wrap(m), wrap(v));
 }

@@ -185,3 +185,35 @@ def test_autograd_forms_take_any_layout():
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[2])
     ctx.sync_status()
     ctx.close()
+
+
+def test_other_threads_run_while_a_call_waits():
+    """A launch into a full queue waits for the GPU, which may itself wait for a Python callback: the compiled call path does not hold
+    the interpreter meanwhile.  A C function that sleeps for as many microseconds as its first argument says stands in for the library's."""
+    import ctypes
+    import threading
+    import time
+    import torch
+    from paper_2505_23725_b200 import _fastcall
+    libc = ctypes.CDLL(None)
+    sleep = ctypes.cast(libc.usleep, ctypes.c_void_p).value
+    stream = torch.cuda.current_stream(0).cuda_stream
+    _fastcall.adamw_step(1, sleep, 0, stream, 1, 1.0)
+    ticks, stop = [0], threading.Event()
+
+    def tick():
+        while not stop.is_set():
+            ticks[0] += 1
+            time.sleep(0.001)
+
+    t = threading.Thread(target=tick)
+    t.start()
+    time.sleep(0.05)
+    before = ticks[0]
+    t0 = time.perf_counter()
+    r = _fastcall.adamw_step(400_000, sleep, 0, stream, 1, 1.0)
+    took, during = time.perf_counter() - t0, ticks[0] - before
+    stop.set()
+    t.join()
+    assert r == 0 and took > 0.3
+    assert during > 20, during
