@@ -171,7 +171,8 @@ MULOCO_API void muloco_destroy(muloco_ctx* ctx);
  * step for worker `worker` (0..K-1), or for all K workers batched when
  * worker == -1.  `grads` is a host table of device pointers: [n_tensors] for one
  * worker, [K][n_tensors] for all; each gradient has its tensor's shape and the
- * dtype named by cfg.grad_dtype.  Gradients are read only.
+ * dtype named by cfg.grad_dtype.  Gradients are read only.  Every pointer is checked (NULL, alignment
+ * to the dtype: MULOCO_EINVAL) before anything is launched.
  * Hidden matrices (Section 2 "Muon", Section 5 "MuLoCo"):
  *     m <- beta m + g;  U = g + beta m (Nesterov) or m;  O = NS_5(U / (||U||_F + eps));
  *     W <- W - eta' O - eta' lambda W,  eta' = muon_lr * lr_scale * sqrt(cols/rows).
