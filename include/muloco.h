@@ -470,6 +470,49 @@ MULOCO_API muloco_status muloco_gated_ffn_backward(muloco_ctx* ctx, const muloco
                                                    const void* g, const void* u, const void* h, void* dg, void* du,
                                                    void* dx, void* dw1, void* dw3, void* dw2);
 
+/* Causal attention over a batch of sequences packed one behind the other, with shared key heads:
+ *     s_ij = scale q_i . k_j  for the keys j <= i of query i's own sequence,  p = softmax over j,  o_i = sum_j p_ij v_j,
+ *     lse_i = ln sum_j exp s_ij
+ * bf16 in and out; scores, their statistics and all sums are float32 (the weights p are rounded to bf16 as an operand of
+ * the last product, as are the score gradients in the backward pass), every result is rounded once.
+ *
+ * muloco_sequences: the packing of a batch, made from the lengths of its sequences (host array; zeros are allowed) and
+ * the batch's count of tokens, which may be more than their sum: the tokens behind the last sequence belong to none.
+ * muloco_sequences_bytes says how much device memory its table takes; _create fills it (`table`, 16-byte aligned, the
+ * caller's, who keeps it until the last call with it has run; a copy of a few bytes per 128 tokens on the context's stream).
+ * It serves any number of calls with that context, forward and backward, captured into graphs as well; _create itself
+ * cannot be captured (MULOCO_ESTATE). */
+typedef struct muloco_sequences muloco_sequences;
+MULOCO_API muloco_status muloco_sequences_bytes(muloco_ctx* ctx, const int64_t* lengths, int64_t n, int64_t tokens,
+                                                size_t* bytes);
+MULOCO_API muloco_status muloco_sequences_create(muloco_ctx* ctx, const int64_t* lengths, int64_t n, int64_t tokens,
+                                                 void* table, size_t bytes, muloco_sequences** out);
+MULOCO_API void muloco_sequences_destroy(muloco_sequences* s);      /* host memory only; NULL is allowed */
+
+/* q [tokens][heads_q][head_dim], k and v [tokens][heads_k][head_dim], bf16, each with its own token and head strides
+ * (elements; multiples of 8, the entries of a head consecutive, 16-byte aligned); query head h reads key head
+ * h / (heads_q / heads_k).  scale > 0.  Results are dense.  o [tokens][heads_q][head_dim] and lse [heads_q][tokens]
+ * (float32) of tokens that belong to no sequence are zero, and so are their gradients.  What such tokens
+ * and other sequences hold does not matter, infinities and NaN included; a value that is not finite reaches
+ * rows of its own sequence only (also earlier ones, in the tile of 128 tokens that it is in).
+ * Limits (MULOCO_ESHAPE): head_dim a multiple of 8, 8..128; heads_q a multiple of heads_k; tokens < 2^31 - 256. */
+typedef struct {
+  int32_t heads_q, heads_k, head_dim;
+  float scale;
+  const void* q;
+  const void* k;
+  const void* v;
+  int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+} muloco_attention;
+MULOCO_API muloco_status muloco_causal_attention(muloco_ctx* ctx, const muloco_attention* a, const muloco_sequences* s,
+                                                 void* o, float* lse);
+/* Backward pass, from the gradient d_o of o (own strides) and the forward pass's o and lse: dq, dk and dv, bf16, summed over
+ * a group's query heads in a fixed order.  delta: float32 scratch [heads_q][tokens] that the caller provides. */
+MULOCO_API muloco_status muloco_causal_attention_backward(muloco_ctx* ctx, const muloco_attention* a,
+                                                          const muloco_sequences* s, const void* d_o,
+                                                          int64_t do_token_stride, int64_t do_head_stride, const void* o,
+                                                          const float* lse, float* delta, void* dq, void* dk, void* dv);
+
 /* Small host state for checkpoint/resume: inner step counters per worker and
  * sync counters per fragment.  Call with blob == NULL to get the size. */
 MULOCO_API muloco_status muloco_get_state(const muloco_ctx* ctx, void* host_blob, size_t* nbytes);

@@ -42,6 +42,8 @@ EXPORTS = [
     "muloco_adamw_create", "muloco_adamw_step", "muloco_adamw_moments", "muloco_adamw_destroy",
     "muloco_qk_norm_rope", "muloco_qk_norm_rope_backward", "muloco_gated_ffn", "muloco_gated_ffn_backward",
     "muloco_debug_ffn_forms",
+    "muloco_sequences_bytes", "muloco_sequences_create", "muloco_sequences_destroy",
+    "muloco_causal_attention", "muloco_causal_attention_backward",
 ]
 
 
@@ -100,9 +102,17 @@ class Ffn(C.Structure):
                 ("activation", C.c_int32), ("pad", C.c_int32)]
 
 
-# QkNorm and Ffn as bytes
+class Attention(C.Structure):
+    _fields_ = [("heads_q", C.c_int32), ("heads_k", C.c_int32), ("head_dim", C.c_int32), ("scale", C.c_float),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64), ("k_token_stride", C.c_int64),
+                ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64)]
+
+
+# the argument structs as bytes
 _QK_PACK = struct.Struct("qqiiiiiifiQQQQQQQqqqq").pack
 _FFN_PACK = struct.Struct("qqqqqqqQQQQii").pack
+_ATTENTION_PACK = struct.Struct("iiifQQQqqqqqq").pack
 
 
 class MulocoError(RuntimeError):
@@ -174,9 +184,15 @@ def load_library():
     lib.muloco_gated_ffn.argtypes = [vp, packed, vp, vp, vp, vp]
     lib.muloco_gated_ffn_backward.argtypes = [vp, packed, vp, i64] + [vp] * 9
     lib.muloco_debug_ffn_forms.argtypes = [i64, i64, i64, i32, C.POINTER(i64)]
+    lib.muloco_sequences_bytes.argtypes = [vp, C.POINTER(i64), i64, i64, C.POINTER(C.c_size_t)]
+    lib.muloco_sequences_create.argtypes = [vp, C.POINTER(i64), i64, i64, vp, C.c_size_t, C.POINTER(vp)]
+    lib.muloco_sequences_destroy.argtypes = [vp]
+    lib.muloco_sequences_destroy.restype = None
+    lib.muloco_causal_attention.argtypes = [vp, packed, vp, vp, vp]
+    lib.muloco_causal_attention_backward.argtypes = [vp, packed, vp, vp, i64, i64] + [vp] * 6
     for name in EXPORTS:
         fn = getattr(lib, name)
-        if name not in ("muloco_destroy", "muloco_last_error", "muloco_adamw_destroy"):
+        if name not in ("muloco_destroy", "muloco_last_error", "muloco_adamw_destroy", "muloco_sequences_destroy"):
             fn.restype = i32
     _lib = lib
     return lib
@@ -308,7 +324,7 @@ class _Operators:
         """What every call looks up, once: device number, types, the stream's handle and the way to ask for the handle
         of the current stream without building a Stream object."""
         torch = self.torch
-        self._lists = weakref.WeakSet()          # AdamW lists, which the library's context must outlive
+        self._lists = weakref.WeakSet()          # AdamW lists and sequences, which the library's context must outlive
         self._dev = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self._bf16, self._f32, self._i64 = torch.bfloat16, torch.float32, torch.int64
         self._raw_stream = torch._C._cuda_getCurrentRawStream
@@ -334,7 +350,7 @@ class _Operators:
         return r
 
     def close(self):
-        """Releases the context, and before it the AdamW lists made with it."""
+        """Releases the context, and before it the AdamW lists and sequences made with it."""
         if getattr(self, "ctx", None):
             for o in list(self._lists):
                 o.close()
@@ -579,6 +595,110 @@ class _Operators:
         if cur is not None:
             cur.wait_stream(self.stream)
         return dx, dw1, dw3, dw2
+
+    # -- causal attention ---------------------------------------------------------------------------
+    def _attention(self, q, k, v, sequences, scale):
+        """The packed argument struct of a call (scale None: head_dim ** -0.5)."""
+        bf16 = self._bf16
+        sequences._open(self)
+        T = sequences.tokens
+        self._need("q", q, bf16, (T, None, None))
+        D = q.shape[2]
+        self._need("k", k, bf16, (T, None, D))
+        self._need("v", v, bf16, tuple(k.shape))
+        return _ATTENTION_PACK(q.shape[1], k.shape[1], D, D ** -0.5 if scale is None else scale, q.data_ptr(), k.data_ptr(),
+                               v.data_ptr(), *q.stride()[:2], *k.stride()[:2], *v.stride()[:2])
+
+    def causal_attention(self, q, k, v, sequences, scale=None):
+        """muloco_causal_attention: attention of q [tokens, query heads, head_dim] over k and v [tokens, key heads, head_dim]
+        (bf16), every token over those up to it of its own sequence (`sequences`: a Sequences of this context).  Returns (o, lse): o
+        like q, lse float32 [query heads, tokens], which the backward pass needs."""
+        a = self._attention(q, k, v, sequences, scale)
+        o = q.new_empty(q.shape)
+        lse = q.new_empty((q.shape[1], q.shape[0]), dtype=self._f32)
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (q, k, v, o, lse, sequences.table))
+        self._check(self.lib.muloco_causal_attention(self.ctx, a, sequences.handle, o.data_ptr(), lse.data_ptr()))
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        return o, lse
+
+    def causal_attention_backward(self, do, q, k, v, o, lse, sequences, scale=None):
+        """muloco_causal_attention_backward: (dq, dk, dv), bf16, from do and the forward pass's o and lse."""
+        a = self._attention(q, k, v, sequences, scale)
+        self._need("do", do, self._bf16, tuple(q.shape))
+        self._need("o", o, self._bf16, tuple(q.shape), dense=True)
+        self._need("lse", lse, self._f32, (q.shape[1], q.shape[0]), dense=True)
+        delta, dq, dk, dv = lse.new_empty(lse.shape), q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (do, q, k, v, o, lse, delta, dq, dk, dv, sequences.table))
+        self._check(self.lib.muloco_causal_attention_backward(
+            self.ctx, a, sequences.handle, do.data_ptr(), *do.stride()[:2], o.data_ptr(), lse.data_ptr(), delta.data_ptr(),
+            dq.data_ptr(), dk.data_ptr(), dv.data_ptr()))
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        return dq, dk, dv
+
+
+class Sequences:
+    """muloco_sequences: the sequences of a packed batch, by their lengths, one behind the other.  `tokens` (default: their
+    sum) is the batch's count of tokens; those behind the last sequence belong to none.
+
+    Made once per batch and used by every attention call on it with `owner` (a Context or a MuLoCo), forward and backward.  Graphs
+    that captured such calls read its table: keep it as long as they are replayed."""
+
+    def __init__(self, owner, lengths, tokens=None):
+        self.handle, self.owner, lib = None, owner, owner.lib
+        if owner.ctx is None:
+            raise RuntimeError("the context is closed")
+        self.lengths = [int(n) for n in lengths]
+        self.tokens = sum(self.lengths) if tokens is None else int(tokens)
+        table = (C.c_int64 * max(1, len(self.lengths)))(*self.lengths)
+        size, handle = C.c_size_t(), C.c_void_p()
+        owner._check(lib.muloco_sequences_bytes(owner.ctx, table, len(self.lengths), self.tokens, C.byref(size)))
+        self.table = owner.torch.empty(size.value, dtype=owner.torch.uint8, device=owner.device)
+        cur = owner._other_stream()
+        if cur is not None:
+            owner._enter(cur, (self.table,))
+        owner._check(lib.muloco_sequences_create(owner.ctx, table, len(self.lengths), self.tokens, self.table.data_ptr(),
+                                                 size.value, C.byref(handle)))
+        if cur is not None:
+            cur.wait_stream(owner.stream)
+        self.lib, self.handle, self._positions = lib, handle, None
+        owner._lists.add(self)
+
+    def _open(self, owner):
+        """Raises unless calls of `owner` can use it."""
+        if self.handle is None:
+            raise RuntimeError("the sequences are closed (by themselves or with their context)")
+        if self.owner is not owner:
+            raise ValueError("the sequences were made with another context")
+
+    @property
+    def positions(self):
+        """int64 [tokens]: every token's place in its sequence, 0 behind the last one (for the position rotation)."""
+        if self._positions is None:
+            torch = self.owner.torch
+            p = torch.zeros(self.tokens, dtype=torch.int64)
+            at = 0
+            for n in self.lengths:
+                p[at:at + n] = torch.arange(n)
+                at += n
+            self._positions = p.to(self.owner.device)
+        return self._positions
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.muloco_sequences_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Context(_Operators):

@@ -1,0 +1,937 @@
+// Causal attention over packed sequences with shared key heads, forward and backward, on the 5th-generation tensor cores.
+//
+//   s_ij = scale q_i . k_j  for j <= i of the same sequence,   p = softmax_j s,   o_i = sum_j p_ij v_j,   lse_i = ln sum_j e^s_ij
+//   backward, from do:  dv_j = sum_i p_ij do_i,   dp_ij = do_i . v_j,   delta_i = do_i . o_i,   ds = p (dp - delta),
+//                       dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i     (dk, dv summed over the group's query heads)
+//
+// Tiles are 128 tokens of one sequence and one head; the host lays the tiles of a batch out once, heaviest first
+// (AttnTile).  Scores never reach memory: a tile of 128 x 128 lies in tensor memory, one thread per row reads it,
+// and what it makes of it (p or ds, rounded to bf16 as the operand of the next product) goes back over the scores' columns, from
+// where the next product takes it as its left operand.  Rows that several products contract over (v, and in the
+// backward pass k, q, do) are zeroed past the end of their sequence in shared memory: there the tile holds
+// the next sequence's tokens, whose weight is zero but which may be anything, infinities and NaN too.
+//
+// Forward: two tiles of 128 queries per thread block take turns, so that the exponentials of one run beside the
+// products of the other.  The running maximum is only moved (and the sums rescaled) when it would grow by more than
+// 2^8: sums stay below 2^8 times the count of keys, far inside float32, and the quotient does not depend on it.
+//
+// Backward: two kernels, without atomics, so results do not depend on the order of thread blocks.  The first goes over the keys of a
+// query tile (delta, dq), the second over the queries of a key tile with the scores transposed (dk, dv):
+// seven products instead of the five that one kernel with sums in global memory would take, and no float32 copy of dq.
+#include <string.h>
+
+#include "internal.h"
+#include "rows.cuh"
+#include "tc_ptx.cuh"
+
+namespace muloco {
+
+namespace {
+
+constexpr int TILE = 128;                     // tokens per tile
+constexpr int ATTN_THREADS = 320;             // eight warps for the rows, one for copies, one for products
+constexpr int COPY_WARP = 8, MMA_WARP = 9;
+constexpr uint32_t SLAB = TILE * 128;         // 128 rows of 64 bf16, swizzled
+constexpr float LN2 = 0.6931471805599453f, LOG2_E = 1.4426950408889634f;
+constexpr float MOVE = 8.0f;                  // growth of a row's maximum (in powers of two) that makes it move
+
+struct Maps4 { CUtensorMap q, k, v, g; };     // g: do
+
+struct AttnParams {
+  const AttnTile* tiles;
+  int64_t tokens;
+  int heads, group;                           // query heads; of them per key head
+  int dim;
+  float scale;
+  void* out; void* out2;                      // o | dq | dk, dv
+  float* lse;                                 // [heads][tokens]
+  float* delta;                               // [heads][tokens]
+  const void* o; const void* g;               // backward: o (dense), do
+  int64_t g_ts, g_hs;                         // strides of do
+  int* status;
+  unsigned long long wait_limit_ns;
+  int withhold;                               // test hook: the first thread block issues no copies
+};
+
+// ----------------------------- tensor memory --------------------------------
+__device__ __forceinline__ void tm_load32(uint32_t taddr, uint32_t* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]),
+        "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]),
+        "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]),
+        "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
+      : "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_store32(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(v[0]),
+      "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
+      "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]),
+      "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]),
+      "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Waits for the loads before it; nothing that uses v is moved in front of it.
+__device__ __forceinline__ void tm_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void after_load(uint32_t* v) {
+  asm volatile(""
+               : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                 "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]),
+                 "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]),
+                 "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]),
+                 "+r"(v[30]), "+r"(v[31]));
+}
+
+// D (tensor memory) = or += A B^T, A and B in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  tc_mma_bf16<1>(d, a, b, idesc, accumulate);
+}
+// ... with A (bf16, two to a column) in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Operands in shared memory: DP / 64 slabs of 128 rows of 64 entries.  As K-major operand its rows are the 128 rows or columns of the
+// result and the contraction runs over the entries; as MN-major operand (right side only) the contraction runs over the
+// 128 rows and the entries are the result's columns.
+constexpr uint32_t DESC_HI = (1024u >> 4) | (1u << 14) | (2u << 29);
+constexpr uint32_t LBO_K = (16u >> 4) << 16, LBO_MN = (SLAB >> 4) << 16;
+__device__ __forceinline__ uint64_t desc(uint32_t lo) { return ((uint64_t)DESC_HI << 32) | lo; }
+constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE >> 4) << 24);
+__host__ __device__ constexpr uint32_t idesc_k(int n) { return IDESC | ((uint32_t)(n >> 3) << 17); }
+__host__ __device__ constexpr uint32_t idesc_mn(int n) { return idesc_k(n) | (1u << 16); }
+
+// d[128][128] = a b^T over DP entries
+template <int DP>
+__device__ __forceinline__ void scores(uint32_t d, uint32_t a, uint32_t b) {
+#pragma unroll
+  for (int k = 0; k < DP / 16; ++k) {
+    const uint32_t off = (uint32_t)(k >> 2) * (SLAB >> 4) + (uint32_t)(k & 3) * 2u;
+    mma_ss(d, desc(((a >> 4) | LBO_K) + off), desc(((b >> 4) | LBO_K) + off), idesc_k(TILE), k > 0);
+  }
+}
+// d[128][DP] += p b over the 128 rows of b; the second half of p's columns starts `half` columns after the first
+template <int DP>
+__device__ __forceinline__ void weigh(uint32_t d, uint32_t p, uint32_t half, uint32_t b, bool accumulate) {
+#pragma unroll
+  for (int k = 0; k < TILE / 16; ++k)
+    mma_ts(d, p + (uint32_t)(k >> 2) * half + (uint32_t)(k & 3) * 8u, desc(((b >> 4) | LBO_MN) + (uint32_t)k * 128u),
+           idesc_mn(DP), accumulate || k > 0);
+}
+
+// Rows `first` .. 127 of an operand become zero (one warp); the products that follow see it.
+template <int DP>
+__device__ __forceinline__ void zero_rows(uint32_t b, int first, int lane) {
+  const int n = (TILE - first) * 8;
+#pragma unroll 1
+  for (int s = 0; s < DP / 64; ++s)
+#pragma unroll 1
+    for (int i = lane; i < n; i += 32) sts128(b + (uint32_t)s * SLAB + (uint32_t)(first * 128 + i * 16), make_uint4(0u, 0u, 0u, 0u));
+  fence_async_smem();
+  __syncwarp();
+}
+
+template <int DP>
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap* map, uint32_t bar, int head, int row) {
+#pragma unroll
+  for (int s = 0; s < DP / 64; ++s) tma_load_3d(dst + (uint32_t)s * SLAB, map, bar, s * 64, head, row);
+}
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float log2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// Accumulator columns [c0, c0 + n) of this thread's row, times `by`, as bf16 to columns c0 .. of `row` (first `dim` columns exist).
+__device__ __forceinline__ void store_columns(uint32_t t_row, __nv_bfloat16* row, int c0, int n, int dim, float by, bool row_ok,
+                                              bool wide) {
+#pragma unroll 1
+  for (int c = c0; c < c0 + n; c += 32) {
+    uint32_t v[32];
+    float f[32];
+    __syncwarp();
+    tm_load32(t_row + (uint32_t)c, v);
+    tm_load_wait();
+    after_load(v);
+#pragma unroll
+    for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]) * by;
+    const int left = row_ok ? dim - c : 0;
+    if (left > 0) store_row32(row + c, f, left, wide);
+  }
+}
+
+struct Pipe {                                 // position in a ring of N stages
+  uint32_t stage = 0, phase = 0;
+  template <int N> __device__ __forceinline__ void next() { if (++stage == (uint32_t)N) { stage = 0; phase ^= 1u; } }
+};
+
+// Start and end of every kernel: barriers, tensor memory, and the dependent launch.
+#define ATTN_BEGIN(cols)                                                                     \
+  if (threadIdx.x == 0) {                                                                    \
+    abort_flag = 0;                                                                          \
+    init_barriers();                                                                         \
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");                       \
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");                             \
+  }                                                                                          \
+  if (warp == MMA_WARP) tmem_alloc<1>(smem_u32(&tmem_base_slot), cols);                      \
+  tc_fence_before();                                                                         \
+  __syncthreads();                                                                           \
+  tc_fence_after();                                                                          \
+  const uint32_t tm = tmem_base_slot;                                                        \
+  grid_wait();                                                                               \
+  grid_release();
+
+#define ATTN_END(cols)                                                                       \
+  __syncwarp();                                                                              \
+  if (abort_flag) { /* copies and products still in flight land before memory is released */ \
+    const uint64_t t0 = global_timer_ns();                                                   \
+    while (global_timer_ns() - t0 < 200000ull) __nanosleep(1000);                            \
+  }                                                                                          \
+  __syncwarp();                                                                              \
+  tc_fence_before();                                                                         \
+  __syncthreads();                                                                           \
+  if (threadIdx.x == 0 && abort_flag) atomicOr(p.status, ST_TIMEOUT);                        \
+  if (warp == MMA_WARP) {                                                                    \
+    tc_fence_after();                                                                        \
+    tmem_dealloc<1>(tm, cols);                                                               \
+  }
+
+// ---------------------------------------------------------------------------
+// forward
+// ---------------------------------------------------------------------------
+template <int DP>
+struct FwdShape {
+  static constexpr uint32_t OPERAND = DP * TILE * 2;
+  static constexpr int STAGES = DP == 64 ? 8 : 4;              // k and v tiles in turn
+  static constexpr uint32_t SMEM = (2 + STAGES) * OPERAND + 1024u;
+};
+
+template <int DP>
+__global__ void __launch_bounds__(ATTN_THREADS, 1)
+attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnParams p) {
+  using Sh = FwdShape<DP>;
+  constexpr int STAGES = Sh::STAGES;
+  constexpr uint32_t OPERAND = Sh::OPERAND;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bar_q, bar_full[STAGES], bar_empty[STAGES], bar_s[2], bar_p[2], bar_o[2];
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ volatile int abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t ring = smem_base + 2 * OPERAND;
+  const uint64_t limit = p.wait_limit_ns;
+  auto init_barriers = [&] {
+    mbar_init(smem_u32(&bar_q), 1);
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&bar_full[s]), 1);
+      mbar_init(smem_u32(&bar_empty[s]), 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(smem_u32(&bar_s[t]), 1);
+      mbar_init(smem_u32(&bar_p[t]), 4);
+      mbar_init(smem_u32(&bar_o[t]), 1);
+    }
+  };
+  ATTN_BEGIN(512)
+  constexpr uint32_t TM_O = 256;              // columns: scores of the two tiles, their sums
+
+  const AttnTile tile = p.tiles[blockIdx.x / p.heads];
+  const int head = blockIdx.x % p.heads, kv_head = head / p.group;
+  // key tiles of the two query tiles (the second may be past the end of the sequence)
+  const int first = tile.offset / TILE;
+  const int n_a = first + 1, n_b = tile.offset + TILE < tile.length ? first + 2 : 0;
+  const int n = n_b ? n_b : n_a;
+  const int tail = tile.length - (n - 1) * TILE;               // rows of the last key tile that exist, when below 128
+
+  if (warp == COPY_WARP) {
+    if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
+      mbar_expect_tx(smem_u32(&bar_q), (n_b ? 2u : 1u) * OPERAND);
+      load_tile<DP>(smem_base, &maps.q, smem_u32(&bar_q), head, tile.start + tile.offset);
+      if (n_b) load_tile<DP>(smem_base + OPERAND, &maps.q, smem_u32(&bar_q), head, tile.start + tile.offset + TILE);
+      Pipe at;
+      for (int i = 0; i < 2 * n; ++i) {
+        if (!mbar_wait(smem_u32(&bar_empty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        const uint32_t bar = smem_u32(&bar_full[at.stage]);
+        mbar_expect_tx(bar, OPERAND);
+        load_tile<DP>(ring + at.stage * OPERAND, (i & 1) ? &maps.v : &maps.k, bar, kv_head, tile.start + (i >> 1) * TILE);
+        at.next<STAGES>();
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    // Order: scores of key tile 0 for both query tiles; then per key tile j and query tile: p v of j, scores of j + 1.  Products
+    // of one thread complete in order, so scores of j + 1 may overwrite the p of j that the product before them reads.
+    Pipe at;                                  // of the tile that is waited for next
+    auto arrived = [&]() { return mbar_wait(smem_u32(&bar_full[at.stage]), at.phase, &abort_flag, limit); };
+    bool alive = mbar_wait(smem_u32(&bar_q), 0, &abort_flag, limit) && arrived();
+    alive = __all_sync(0xffffffffu, alive);
+    if (alive) {
+      tc_fence_after();
+      uint32_t k_stage = at.stage;
+      at.next<STAGES>();
+      if (lane == 0) {
+        for (int t = 0; t < 2; ++t) {
+          if (t == 1 && !n_b) break;
+          scores<DP>(tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
+          tc_commit<1>(smem_u32(&bar_s[t]));
+        }
+        tc_commit<1>(smem_u32(&bar_empty[k_stage]));
+      }
+      __syncwarp();
+      for (int j = 0; alive && j < n; ++j) {
+        alive = __all_sync(0xffffffffu, arrived());
+        if (!alive) break;
+        const uint32_t v_stage = at.stage;
+        at.next<STAGES>();
+        if (j == n - 1 && tail < TILE) zero_rows<DP>(ring + v_stage * OPERAND, tail, lane);
+        if (j + 1 < n) {
+          alive = __all_sync(0xffffffffu, arrived());
+          if (!alive) break;
+          k_stage = at.stage;
+          at.next<STAGES>();
+        }
+        for (int t = 0; t < 2; ++t) {
+          const int n_t = t ? n_b : n_a;
+          if (j >= n_t) continue;
+          alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_p[t]), (uint32_t)j & 1u, &abort_flag, limit));
+          if (!alive) break;
+          tc_fence_after();
+          if (lane == 0) {
+            weigh<DP>(tm + TM_O + t * DP, tm + t * 128, 32, ring + v_stage * OPERAND, j > 0);
+            if (j + 1 < n_t) {
+              scores<DP>(tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
+              tc_commit<1>(smem_u32(&bar_s[t]));
+            } else {
+              tc_commit<1>(smem_u32(&bar_o[t]));
+            }
+          }
+          __syncwarp();
+        }
+        if (alive && lane == 0) {
+          tc_commit<1>(smem_u32(&bar_empty[v_stage]));
+          if (j + 1 < n) tc_commit<1>(smem_u32(&bar_empty[k_stage]));
+        }
+        __syncwarp();
+      }
+    }
+  } else {
+    const int t = warp >> 2, quarter = warp & 3;
+    const int row = quarter * 32 + lane;                       // of the tile; key columns up to `row` of the last key tile count
+    const int n_t = t ? n_b : n_a;
+    const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t t_s = t_lane + t * 128, t_o = t_lane + TM_O + t * DP;
+    const float c = p.scale * LOG2_E;
+    float top = -INFINITY, total = 0.f;                        // largest score (unscaled) that the sums refer to; sum of weights
+    bool alive = true;
+    for (int j = 0; j < n_t; ++j) {
+      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_s[t]), (uint32_t)j & 1u, &abort_flag, limit));
+      if (!alive) break;
+      tc_fence_after();
+      uint32_t s[128];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) tm_load32(t_s + i * 32, s + i * 32);
+      tm_load_wait();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) after_load(s + i * 32);
+      if (j == n_t - 1) {
+#pragma unroll
+        for (int e = 0; e < 128; ++e) s[e] = e > row ? 0xff800000u : s[e];
+      }
+      float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+      for (int e = 0; e < 128; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(s[e]));
+      const float m = fmaxf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), top);
+      if (j == 0) {
+        top = m;
+      } else if (__any_sync(0xffffffffu, (m - top) * c > MOVE)) {
+        // the scores of j are there, so the product of j - 1 before them is complete
+        const float by = exp2_approx((top - m) * c);
+        total *= by;
+        top = m;
+#pragma unroll 1
+        for (int i = 0; i < DP; i += 32) {
+          uint32_t v[32];
+          tm_load32(t_o + i, v);
+          tm_load_wait();
+          after_load(v);
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * by);
+          tm_store32(t_o + i, v);
+        }
+      }
+      const Pair c2 = both(c), shift = both(-top * c);
+      Pair sum[2] = {both(0.f), both(0.f)};
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t w[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+          const float2 x = parts(fma2(pair(__uint_as_float(s[h * 64 + 2 * e]), __uint_as_float(s[h * 64 + 2 * e + 1])), c2, shift));
+          const float a = exp2_approx(x.x), b = exp2_approx(x.y);
+          sum[e & 1] = add2(sum[e & 1], pair(a, b));
+          w[e] = pack_bf16x2(a, b);
+        }
+        tm_store32(t_s + h * 32, w);
+      }
+      const float2 both_sums = parts(add2(sum[0], sum[1]));
+      total += both_sums.x + both_sums.y;
+      tm_store_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(smem_u32(&bar_p[t]));
+    }
+    if (alive && n_t) {
+      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_o[t]), 0, &abort_flag, limit));
+      if (alive) {
+        tc_fence_after();
+        const int pos = tile.offset + t * TILE + row;
+        const bool ok = pos < tile.length;
+        const int64_t token = (int64_t)tile.start + pos;
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + ((ok ? token : 0) * p.heads + head) * p.dim;
+        const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
+        store_columns(t_o, out, 0, DP, p.dim, 1.0f / total, ok, wide);
+        if (ok) p.lse[(int64_t)head * p.tokens + token] = (top * c + log2_approx(total)) * LN2;
+      }
+    }
+  }
+  ATTN_END(512)
+}
+
+// ---------------------------------------------------------------------------
+// backward over the keys of a query tile: delta and dq
+// ---------------------------------------------------------------------------
+template <int DP>
+struct BackShape {
+  static constexpr uint32_t OPERAND = DP * TILE * 2;
+  static constexpr int STAGES = 2;
+  static constexpr uint32_t SMEM = (2 + 2 * STAGES) * OPERAND + 1024u;
+};
+
+// The two halves of a tile's columns belong to the first and the last four row warps; each writes its bf16 operand at the
+// start of its own 64 columns, so neither overwrites scores that the other has yet to read.
+constexpr uint32_t HALF = 64;
+
+template <int DP>
+__global__ void __launch_bounds__(ATTN_THREADS, 1)
+attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnParams p) {
+  using Sh = BackShape<DP>;
+  constexpr int STAGES = Sh::STAGES;
+  constexpr uint32_t OPERAND = Sh::OPERAND;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bar_q, bar_kfull[STAGES], bar_kempty[STAGES], bar_vfull[STAGES], bar_vempty[STAGES], bar_s[2], bar_dp,
+      bar_ds, bar_done;
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ volatile int abort_flag;
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t s_q = smem_base, s_g = smem_base + OPERAND, s_k = smem_base + 2 * OPERAND, s_v = s_k + STAGES * OPERAND;
+  const uint64_t limit = p.wait_limit_ns;
+  auto init_barriers = [&] {
+    mbar_init(smem_u32(&bar_q), 1);
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&bar_kfull[s]), 1);
+      mbar_init(smem_u32(&bar_kempty[s]), 1);
+      mbar_init(smem_u32(&bar_vfull[s]), 1);
+      mbar_init(smem_u32(&bar_vempty[s]), 1);
+    }
+    mbar_init(smem_u32(&bar_s[0]), 1);
+    mbar_init(smem_u32(&bar_s[1]), 1);
+    mbar_init(smem_u32(&bar_dp), 1);
+    mbar_init(smem_u32(&bar_ds), 8);
+    mbar_init(smem_u32(&bar_done), 1);
+  };
+  ATTN_BEGIN(512)
+  constexpr uint32_t TM_DP = 256, TM_DQ = 384;                 // columns: two tiles of scores, dp, dq
+
+  const AttnTile tile = p.tiles[blockIdx.x / p.heads];
+  const int head = blockIdx.x % p.heads, kv_head = head / p.group;
+  const int n = tile.offset / TILE + 1;                        // key tiles
+  const int tail = tile.length - (n - 1) * TILE;               // rows of the last one that exist, when below 128
+
+  if (warp == COPY_WARP) {
+    if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
+      mbar_expect_tx(smem_u32(&bar_q), 2 * OPERAND);
+      load_tile<DP>(s_q, &maps.q, smem_u32(&bar_q), head, tile.start + tile.offset);
+      load_tile<DP>(s_g, &maps.g, smem_u32(&bar_q), head, tile.start + tile.offset);
+      Pipe at;
+      for (int j = 0; j < n; ++j) {
+        if (!mbar_wait(smem_u32(&bar_kempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        mbar_expect_tx(smem_u32(&bar_kfull[at.stage]), OPERAND);
+        load_tile<DP>(s_k + at.stage * OPERAND, &maps.k, smem_u32(&bar_kfull[at.stage]), kv_head, tile.start + j * TILE);
+        if (!mbar_wait(smem_u32(&bar_vempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        mbar_expect_tx(smem_u32(&bar_vfull[at.stage]), OPERAND);
+        load_tile<DP>(s_v + at.stage * OPERAND, &maps.v, smem_u32(&bar_vfull[at.stage]), kv_head, tile.start + j * TILE);
+        at.next<STAGES>();
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    // Order: scores of 0; then per key tile j: dp of j, scores of j + 1 (into the other columns), dq += ds k of j.  (The scores of
+    // j + 1 may be complete before the row warps have looked for those of j: a barrier for each of the two places.)
+    Pipe at;                                  // key tile j
+    auto keys = [&](const Pipe& q, int j) {   // waits for key tile j and readies it
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_kfull[q.stage]), q.phase, &abort_flag, limit))) return false;
+      if (j == n - 1 && tail < TILE) zero_rows<DP>(s_k + q.stage * OPERAND, tail, lane);
+      return true;
+    };
+    bool alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_q), 0, &abort_flag, limit));
+    alive = alive && keys(at, 0);
+    if (alive) {
+      tc_fence_after();
+      if (lane == 0) {
+        scores<DP>(tm, s_q, s_k);
+        tc_commit<1>(smem_u32(&bar_s[0]));
+      }
+      __syncwarp();
+      for (int j = 0; j < n; ++j) {
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_vfull[at.stage]), at.phase, &abort_flag, limit))) break;
+        tc_fence_after();
+        if (lane == 0) {
+          scores<DP>(tm + TM_DP, s_g, s_v + at.stage * OPERAND);
+          tc_commit<1>(smem_u32(&bar_dp));
+          tc_commit<1>(smem_u32(&bar_vempty[at.stage]));
+        }
+        __syncwarp();
+        Pipe ahead = at;
+        ahead.next<STAGES>();
+        if (j + 1 < n) {
+          if (!keys(ahead, j + 1)) break;
+          tc_fence_after();
+          if (lane == 0) {
+            scores<DP>(tm + ((j + 1) & 1) * 128, s_q, s_k + ahead.stage * OPERAND);
+            tc_commit<1>(smem_u32(&bar_s[(j + 1) & 1]));
+          }
+          __syncwarp();
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_ds), (uint32_t)j & 1u, &abort_flag, limit))) break;
+        tc_fence_after();
+        if (lane == 0) {
+          weigh<DP>(tm + TM_DQ, tm + (j & 1) * 128, HALF, s_k + at.stage * OPERAND, j > 0);
+          tc_commit<1>(j + 1 < n ? smem_u32(&bar_kempty[at.stage]) : smem_u32(&bar_done));
+        }
+        __syncwarp();
+        at = ahead;
+      }
+    }
+  } else {
+    const int half = warp >> 2, quarter = warp & 3;
+    const int row = quarter * 32 + lane;
+    const int pos = tile.offset + row;
+    const bool ok = pos < tile.length;
+    const int64_t token = (int64_t)tile.start + (ok ? pos : 0);
+    const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
+    const float c = p.scale * LOG2_E;
+    const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(p.o) + (token * p.heads + head) * p.dim;
+    const __nv_bfloat16* g = reinterpret_cast<const __nv_bfloat16*>(p.g) + token * p.g_ts + head * p.g_hs;
+    // delta = do . o of the row, with o as it was rounded
+    Pair acc = both(0.f);
+#pragma unroll 4
+    for (int e = 0; e < p.dim; e += 8) {
+      const uint4 a = *reinterpret_cast<const uint4*>(o + e), b = *reinterpret_cast<const uint4*>(g + e);
+      acc = fma2(pair_bf16(a.x), pair_bf16(b.x), acc);
+      acc = fma2(pair_bf16(a.y), pair_bf16(b.y), acc);
+      acc = fma2(pair_bf16(a.z), pair_bf16(b.z), acc);
+      acc = fma2(pair_bf16(a.w), pair_bf16(b.w), acc);
+    }
+    const float2 halves = parts(acc);
+    const float delta = halves.x + halves.y;
+    const float lse2 = p.lse[(int64_t)head * p.tokens + token] * LOG2_E;
+    if (half == 0 && ok) p.delta[(int64_t)head * p.tokens + token] = delta;
+    const Pair c2 = both(c), shift = both(-lse2), minus = both(-delta);
+    bool alive = true;
+    for (int j = 0; j < n; ++j) {
+      const uint32_t t_s = t_lane + (j & 1) * 128 + half * HALF;
+      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_s[j & 1]), (uint32_t)(j >> 1) & 1u, &abort_flag, limit));
+      if (!alive) break;
+      tc_fence_after();
+      uint32_t s[64], d[64];
+      tm_load32(t_s, s);
+      tm_load32(t_s + 32, s + 32);
+      tm_load_wait();
+      after_load(s);
+      after_load(s + 32);
+#pragma unroll
+      for (int e = 0; e < 64; e += 2) {
+        const float2 x = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, shift));
+        s[e] = __float_as_uint(exp2_approx(x.x));
+        s[e + 1] = __float_as_uint(exp2_approx(x.y));
+      }
+      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_dp), (uint32_t)j & 1u, &abort_flag, limit));
+      if (!alive) break;
+      tc_fence_after();
+      tm_load32(t_lane + TM_DP + half * HALF, d);
+      tm_load32(t_lane + TM_DP + half * HALF + 32, d + 32);
+      tm_load_wait();
+      after_load(d);
+      after_load(d + 32);
+      uint32_t w[32];
+      if (j == n - 1) {                       // where the key comes after the query: no weight, whatever the products hold
+#pragma unroll
+        for (int e = 0; e < 64; e += 2) {
+          const float a = __uint_as_float(s[e]) * (__uint_as_float(d[e]) - delta);
+          const float b = __uint_as_float(s[e + 1]) * (__uint_as_float(d[e + 1]) - delta);
+          w[e >> 1] = pack_bf16x2(half * 64 + e > row ? 0.f : a, half * 64 + e + 1 > row ? 0.f : b);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 64; e += 2) {
+          const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
+                                      add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), minus)));
+          w[e >> 1] = pack_bf16x2(x.x, x.y);
+        }
+      }
+      tm_store32(t_s, w);
+      tm_store_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(smem_u32(&bar_ds));
+    }
+    if (alive) {
+      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_done), 0, &abort_flag, limit));
+      if (alive) {
+        tc_fence_after();
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (token * p.heads + head) * p.dim;
+        const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
+        store_columns(t_lane + TM_DQ, out, half * (DP / 2), DP / 2, p.dim, p.scale, ok, wide);
+      }
+    }
+  }
+  ATTN_END(512)
+}
+
+// ---------------------------------------------------------------------------
+// backward over the queries of a key tile, for all query heads of its group: dk and dv
+// ---------------------------------------------------------------------------
+template <int DP>
+__global__ void __launch_bounds__(ATTN_THREADS, 1)
+attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnParams p) {
+  using Sh = BackShape<DP>;
+  constexpr int STAGES = Sh::STAGES;
+  constexpr uint32_t OPERAND = Sh::OPERAND;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t bar_kv, bar_qfull[STAGES], bar_qempty[STAGES], bar_gfull[STAGES], bar_gempty[STAGES], bar_s, bar_dp,
+      bar_p, bar_ds, bar_done;
+  __shared__ uint32_t tmem_base_slot;
+  __shared__ volatile int abort_flag;
+  __shared__ __align__(16) float row_values[8][2][64];         // of each row warp: log-sum-exp and delta of its 64 queries, negated
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t s_k = smem_base, s_v = smem_base + OPERAND, s_q = smem_base + 2 * OPERAND, s_g = s_q + STAGES * OPERAND;
+  const uint64_t limit = p.wait_limit_ns;
+  auto init_barriers = [&] {
+    mbar_init(smem_u32(&bar_kv), 1);
+    for (int s = 0; s < STAGES; ++s) {
+      mbar_init(smem_u32(&bar_qfull[s]), 1);
+      mbar_init(smem_u32(&bar_qempty[s]), 1);
+      mbar_init(smem_u32(&bar_gfull[s]), 1);
+      mbar_init(smem_u32(&bar_gempty[s]), 1);
+    }
+    mbar_init(smem_u32(&bar_s), 1);
+    mbar_init(smem_u32(&bar_dp), 1);
+    mbar_init(smem_u32(&bar_p), 8);
+    mbar_init(smem_u32(&bar_ds), 8);
+    mbar_init(smem_u32(&bar_done), 1);
+  };
+  ATTN_BEGIN(512)
+  constexpr uint32_t TM_DP = 128, TM_DV = 256, TM_DK = 256 + DP;           // columns: scores, dp, dv, dk (rows are keys)
+
+  const int kv_heads = p.heads / p.group;
+  const AttnTile tile = p.tiles[blockIdx.x / kv_heads];
+  const int kv_head = blockIdx.x % kv_heads;
+  const int first = tile.offset / TILE, end = (tile.length + TILE - 1) / TILE;   // query tiles
+  const int per = end - first, n = per * p.group;
+  const int tail = tile.length - (end - 1) * TILE;             // rows of the last query tile that exist, when below 128
+
+  if (warp == COPY_WARP) {
+    if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
+      mbar_expect_tx(smem_u32(&bar_kv), 2 * OPERAND);
+      load_tile<DP>(s_k, &maps.k, smem_u32(&bar_kv), kv_head, tile.start + tile.offset);
+      load_tile<DP>(s_v, &maps.v, smem_u32(&bar_kv), kv_head, tile.start + tile.offset);
+      Pipe at;
+      int head = kv_head * p.group, i = first;
+      for (int it = 0; it < n; ++it) {
+        if (!mbar_wait(smem_u32(&bar_qempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        mbar_expect_tx(smem_u32(&bar_qfull[at.stage]), OPERAND);
+        load_tile<DP>(s_q + at.stage * OPERAND, &maps.q, smem_u32(&bar_qfull[at.stage]), head, tile.start + i * TILE);
+        if (!mbar_wait(smem_u32(&bar_gempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        mbar_expect_tx(smem_u32(&bar_gfull[at.stage]), OPERAND);
+        load_tile<DP>(s_g + at.stage * OPERAND, &maps.g, smem_u32(&bar_gfull[at.stage]), head, tile.start + i * TILE);
+        at.next<STAGES>();
+        if (++i == end) { i = first; ++head; }
+      }
+    }
+  } else if (warp == MMA_WARP) {
+    // Order: scores of 0; then per step: dp, dv += p do, scores of the next, dk += ds q.
+    Pipe at;
+    int i = first;                            // query tile of the step
+    auto queries = [&](const Pipe& q, int i) {
+      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_qfull[q.stage]), q.phase, &abort_flag, limit))) return false;
+      if (i == end - 1 && tail < TILE) zero_rows<DP>(s_q + q.stage * OPERAND, tail, lane);
+      return true;
+    };
+    bool alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_kv), 0, &abort_flag, limit));
+    alive = alive && queries(at, i);
+    if (alive) {
+      tc_fence_after();
+      if (lane == 0) {
+        scores<DP>(tm, s_k, s_q);
+        tc_commit<1>(smem_u32(&bar_s));
+      }
+      __syncwarp();
+      for (int it = 0; it < n; ++it) {
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_gfull[at.stage]), at.phase, &abort_flag, limit))) break;
+        if (i == end - 1 && tail < TILE) zero_rows<DP>(s_g + at.stage * OPERAND, tail, lane);
+        tc_fence_after();
+        if (lane == 0) {
+          scores<DP>(tm + TM_DP, s_v, s_g + at.stage * OPERAND);
+          tc_commit<1>(smem_u32(&bar_dp));
+        }
+        __syncwarp();
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_p), (uint32_t)it & 1u, &abort_flag, limit))) break;
+        tc_fence_after();
+        if (lane == 0) {
+          weigh<DP>(tm + TM_DV, tm, HALF, s_g + at.stage * OPERAND, it > 0);
+          tc_commit<1>(smem_u32(&bar_gempty[at.stage]));
+        }
+        __syncwarp();
+        Pipe ahead = at;
+        ahead.next<STAGES>();
+        const int i_next = i + 1 == end ? first : i + 1;
+        if (it + 1 < n) {
+          if (!queries(ahead, i_next)) break;
+          tc_fence_after();
+          if (lane == 0) {
+            scores<DP>(tm, s_k, s_q + ahead.stage * OPERAND);
+            tc_commit<1>(smem_u32(&bar_s));
+          }
+          __syncwarp();
+        }
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_ds), (uint32_t)it & 1u, &abort_flag, limit))) break;
+        tc_fence_after();
+        if (lane == 0) {
+          weigh<DP>(tm + TM_DK, tm + TM_DP, HALF, s_q + at.stage * OPERAND, it > 0);
+          tc_commit<1>(it + 1 < n ? smem_u32(&bar_qempty[at.stage]) : smem_u32(&bar_done));
+        }
+        __syncwarp();
+        at = ahead;
+        i = i_next;
+      }
+    }
+  } else {
+    const int half = warp >> 2, quarter = warp & 3;
+    const int row = quarter * 32 + lane;                       // key of the tile
+    const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t t_s = t_lane + half * HALF, t_dp = t_lane + TM_DP + half * HALF;
+    const float c = p.scale * LOG2_E;
+    const Pair c2 = both(c);
+    // each warp brings the log-sum-exp and the delta of its 64 queries into shared memory, fetched a step ahead
+    const int col0 = half * 64;
+    float* const lse = row_values[warp][0];
+    float* const delta = row_values[warp][1];
+    int head = kv_head * p.group, i = first;
+    float ahead[4];
+    auto fetch = [&] {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int pos = i * TILE + col0 + h * 32 + lane;
+        const int64_t at = (int64_t)head * p.tokens + tile.start + pos;
+        ahead[h] = pos < tile.length ? -LOG2_E * p.lse[at] : 0.f;
+        ahead[2 + h] = pos < tile.length ? -p.delta[at] : 0.f;
+      }
+    };
+    fetch();
+    bool alive = true;
+    for (int it = 0; it < n; ++it) {
+      const bool edge = i == first || (i == end - 1 && tail < TILE);       // some of the tile's pairs do not count
+      const int last = tile.length - i * TILE - 1;                         // columns from .. last count
+      const int from = i == first ? row : 0;
+      __syncwarp();
+      lse[lane] = ahead[0];
+      lse[32 + lane] = ahead[1];
+      delta[lane] = ahead[2];
+      delta[32 + lane] = ahead[3];
+      __syncwarp();
+      if (++i == end) { i = first; ++head; }
+      if (it + 1 < n) fetch();
+      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_s), (uint32_t)it & 1u, &abort_flag, limit));
+      if (!alive) break;
+      uint32_t s[64], w[32];
+      tc_fence_after();
+      tm_load32(t_s, s);
+      tm_load32(t_s + 32, s + 32);
+      tm_load_wait();
+      after_load(s);
+      after_load(s + 32);
+#pragma unroll
+      for (int e = 0; e < 64; e += 4) {
+        const float4 l = *reinterpret_cast<const float4*>(lse + e);
+        const float2 x = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, pair(l.x, l.y)));
+        const float2 y = parts(fma2(pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c2, pair(l.z, l.w)));
+        s[e] = __float_as_uint(exp2_approx(x.x));
+        s[e + 1] = __float_as_uint(exp2_approx(x.y));
+        s[e + 2] = __float_as_uint(exp2_approx(y.x));
+        s[e + 3] = __float_as_uint(exp2_approx(y.y));
+      }
+      if (edge) {
+#pragma unroll
+        for (int e = 0; e < 64; ++e) s[e] = col0 + e < from || col0 + e > last ? 0u : s[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 64; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+      tm_store32(t_s, w);
+      tm_store_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(smem_u32(&bar_p));
+      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_dp), (uint32_t)it & 1u, &abort_flag, limit));
+      if (!alive) break;
+      tc_fence_after();
+      uint32_t d[64];
+      tm_load32(t_dp, d);
+      tm_load32(t_dp + 32, d + 32);
+      tm_load_wait();
+      after_load(d);
+      after_load(d + 32);
+#pragma unroll
+      for (int e = 0; e < 64; e += 4) {
+        const float4 l = *reinterpret_cast<const float4*>(delta + e);
+        const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
+                                    add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pair(l.x, l.y))));
+        const float2 y = parts(mul2(pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])),
+                                    add2(pair(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])), pair(l.z, l.w))));
+        d[e] = __float_as_uint(x.x); d[e + 1] = __float_as_uint(x.y);
+        d[e + 2] = __float_as_uint(y.x); d[e + 3] = __float_as_uint(y.y);
+      }
+      if (edge) {                           // (zero times what the products hold there need not be zero)
+#pragma unroll
+        for (int e = 0; e < 64; ++e) d[e] = col0 + e < from || col0 + e > last ? 0u : d[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 64; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1]));
+      tm_store32(t_dp, w);
+      tm_store_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(smem_u32(&bar_ds));
+    }
+    if (alive) {
+      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_done), 0, &abort_flag, limit));
+      if (alive) {
+        tc_fence_after();
+        const int pos = tile.offset + row;
+        const bool ok = pos < tile.length;
+        const int64_t at = (((int64_t)tile.start + (ok ? pos : 0)) * kv_heads + kv_head) * p.dim;
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(half ? p.out : p.out2) + at;
+        const bool wide = (p.dim & 15) == 0 && (((uintptr_t)p.out | (uintptr_t)p.out2) & 31) == 0;
+        store_columns(t_lane + (half ? TM_DK : TM_DV), out, 0, DP, p.dim, half ? p.scale : 1.0f, ok, wide);
+      }
+    }
+  }
+  ATTN_END(512)
+}
+
+// ----------------------------- host ------------------------------------------
+
+// A tensor [tokens][heads][dim] in boxes of 64 entries of one head by 128 tokens; entries past dim and rows past the end read as zero.
+bool encode(CUtensorMap* map, const void* x, int64_t tokens, int64_t heads, int64_t dim, int64_t ts, int64_t hs) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  if (heads == 1) hs = dim;                   // the stride of a single head or token does not matter
+  if (tokens == 1) ts = heads * hs;
+  const cuuint64_t dims[3] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)tokens};
+  const cuuint64_t strides[2] = {(cuuint64_t)hs * 2, (cuuint64_t)ts * 2};
+  const cuuint32_t box[3] = {64, 1, TILE}, step[3] = {1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DP>
+cudaError_t run_forward(cudaStream_t st, const Maps4& m, const AttnParams& p, int64_t units) {
+  static std::atomic<uint64_t> allowed{0};
+  const cudaError_t e = allow_smem(attn_fwd_kernel<DP>, (int)FwdShape<DP>::SMEM, &allowed);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(attn_fwd_kernel<DP>, (unsigned)units, ATTN_THREADS, FwdShape<DP>::SMEM, st, m, p);
+}
+
+template <int DP>
+cudaError_t run_backward(cudaStream_t st, const Maps4& m, AttnParams p, const AttnArgs& a) {
+  static std::atomic<uint64_t> allowed{0}, allowed2{0};
+  cudaError_t e = allow_smem(attn_dq_kernel<DP>, (int)BackShape<DP>::SMEM, &allowed);
+  if (e == cudaSuccess) e = allow_smem(attn_dkv_kernel<DP>, (int)BackShape<DP>::SMEM, &allowed2);
+  if (e != cudaSuccess) return e;
+  p.tiles = a.query_tiles;
+  p.out = a.dq;
+  e = launch_dependent(attn_dq_kernel<DP>, (unsigned)(a.n_tiles * a.heads), ATTN_THREADS, BackShape<DP>::SMEM, st, m, p);
+  if (e != cudaSuccess) return e;
+  p.withhold = 0;
+  p.tiles = a.key_tiles;
+  p.out = a.dk;
+  p.out2 = a.dv;
+  return launch_dependent(attn_dkv_kernel<DP>, (unsigned)(a.n_tiles * a.kv_heads), ATTN_THREADS, BackShape<DP>::SMEM, st, m, p);
+}
+
+bool prepare(const AttnArgs& a, Maps4* m, AttnParams* p) {
+  memset(p, 0, sizeof *p);
+  p->tokens = a.tokens;
+  p->heads = a.heads; p->group = a.heads / a.kv_heads; p->dim = a.dim;
+  p->scale = a.scale;
+  p->lse = a.lse; p->delta = a.delta;
+  p->o = a.o; p->g = a.g; p->g_ts = a.g_ts; p->g_hs = a.g_hs;
+  p->status = a.status;
+  p->wait_limit_ns = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
+  p->withhold = a.withhold;
+  return encode(&m->q, a.q, a.tokens, a.heads, a.dim, a.q_ts, a.q_hs) && encode(&m->k, a.k, a.tokens, a.kv_heads, a.dim, a.k_ts, a.k_hs) &&
+         encode(&m->v, a.v, a.tokens, a.kv_heads, a.dim, a.v_ts, a.v_hs) &&
+         (!a.g || encode(&m->g, a.g, a.tokens, a.heads, a.dim, a.g_ts, a.g_hs));
+}
+
+}  // namespace
+
+cudaError_t launch_attention(cudaStream_t st, const AttnArgs& a, const char** what) {
+  const cudaError_t bound = bind_context(what);
+  if (bound != cudaSuccess) return bound;
+  Maps4 m;
+  AttnParams p;
+  memset(&m, 0, sizeof m);
+  *what = "cuTensorMapEncodeTiled";
+  if (!prepare(a, &m, &p)) return cudaErrorInvalidValue;
+  *what = "launch of the attention kernel";
+  p.tiles = a.pair_tiles;
+  p.out = a.o_out;
+  return a.dim <= 64 ? run_forward<64>(st, m, p, a.n_pairs * a.heads) : run_forward<128>(st, m, p, a.n_pairs * a.heads);
+}
+
+cudaError_t launch_attention_backward(cudaStream_t st, const AttnArgs& a, const char** what) {
+  const cudaError_t bound = bind_context(what);
+  if (bound != cudaSuccess) return bound;
+  Maps4 m;
+  AttnParams p;
+  memset(&m, 0, sizeof m);
+  *what = "cuTensorMapEncodeTiled";
+  if (!prepare(a, &m, &p)) return cudaErrorInvalidValue;
+  *what = "launch of the attention kernels of the backward pass";
+  return a.dim <= 64 ? run_backward<64>(st, m, p, a) : run_backward<128>(st, m, p, a);
+}
+
+}  // namespace muloco

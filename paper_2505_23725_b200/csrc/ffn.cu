@@ -25,9 +25,8 @@
 // alone take 239 and 886.  Unlimited, a slab takes 334 ns, about 635 cycles, where its MMAs need 512.
 #include <string.h>
 
-#include <atomic>
-
 #include "internal.h"
+#include "rows.cuh"
 #include "tc_ptx.cuh"
 
 namespace muloco {
@@ -97,80 +96,6 @@ __device__ __forceinline__ Tile decode(const Params& p, int tile) {
   t.n = rem / size;
   t.m = g * GROUP_M + (rem - t.n * size);
   return t;
-}
-
-// 16 bf16 values (32 bytes) per access where the row allows it, else 8.
-__device__ __forceinline__ void st_global_32(void* p, const uint32_t (&v)[8]) {
-  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]),
-               "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-               : "memory");
-}
-__device__ __forceinline__ void ld_global_32(const void* p, uint32_t* v) {
-  asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-               : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
-               : "l"(p));
-}
-// 32 consecutive values of a row of which the first `n` (a multiple of 8) exist.
-__device__ __forceinline__ void store_row32(__nv_bfloat16* row, const float (&f)[32], int n, bool wide) {
-  if (wide && n >= 32) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      uint32_t v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = pack_bf16x2(f[h * 16 + 2 * i], f[h * 16 + 2 * i + 1]);
-      st_global_32(row + h * 16, v);
-    }
-  } else {
-#pragma unroll
-    for (int h = 0; h < 4; ++h)
-      if (h * 8 < n)
-        *reinterpret_cast<uint4*>(row + h * 8) =
-            make_uint4(pack_bf16x2(f[h * 8], f[h * 8 + 1]), pack_bf16x2(f[h * 8 + 2], f[h * 8 + 3]),
-                       pack_bf16x2(f[h * 8 + 4], f[h * 8 + 5]), pack_bf16x2(f[h * 8 + 6], f[h * 8 + 7]));
-  }
-}
-__device__ __forceinline__ void load_row32(const __nv_bfloat16* row, uint32_t (&v)[16], int n, bool wide) {
-  if (wide && n >= 32) {
-    ld_global_32(row, v);
-    ld_global_32(row + 16, v + 8);
-  } else {
-#pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      uint4 u = make_uint4(0u, 0u, 0u, 0u);
-      if (h * 8 < n) u = *reinterpret_cast<const uint4*>(row + h * 8);
-      v[h * 4] = u.x; v[h * 4 + 1] = u.y; v[h * 4 + 2] = u.z; v[h * 4 + 3] = u.w;
-    }
-  }
-}
-
-// Two float32 operations per instruction.
-struct Pair { uint64_t v; };
-__device__ __forceinline__ Pair pair(float a, float b) {
-  Pair r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ Pair both(float a) { return pair(a, a); }
-__device__ __forceinline__ Pair pair_bf16(uint32_t w) { return pair(bf16_lo(w), bf16_hi(w)); }
-__device__ __forceinline__ float2 parts(Pair p) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(p.v));
-  return r;
-}
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
-  Pair r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Pair add2(Pair a, Pair b) {
-  Pair r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-  Pair r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
 }
 
 // act(g) = g sigma and, for the backward pass, its slope.  sigma is the logistic function of g (silu) or of
@@ -749,15 +674,6 @@ ffn_few_kernel(const __grid_constant__ FewMaps maps, const __grid_constant__ Few
 }
 
 // ------------------------------ host side ----------------------------------
-// Makes the current device's context this thread's: the descriptor encoder is a driver call, which fails in a
-// thread that has made no runtime call yet (a backward pass runs in a thread of its own).
-cudaError_t bind_context(const char** what) {
-  *what = "cudaSetDevice";
-  int dev = 0;
-  const cudaError_t e = cudaGetDevice(&dev);
-  return e == cudaSuccess ? cudaSetDevice(dev) : e;
-}
-
 // A row-major bf16 matrix as an operand: rows x cols with row pitch ld.
 struct Mat { const void* p; int64_t rows, cols, ld; };
 
@@ -815,19 +731,6 @@ struct Builder {
     return b;
   }
 };
-
-// Raises a kernel's shared-memory limit, once per device (`allowed`: a bit for each of the first 64 that it was raised on; calls
-// may come from several threads).
-template <typename K>
-cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* allowed) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-  if (e != cudaSuccess || (allowed->load(std::memory_order_relaxed) & bit)) return e;
-  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) allowed->fetch_or(bit, std::memory_order_relaxed);
-  return e;
-}
 
 template <int EPI, int ACT>
 cudaError_t launch_kernel(cudaStream_t st, const Builder& b, int n_sms) {

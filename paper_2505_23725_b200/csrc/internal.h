@@ -297,4 +297,36 @@ cudaError_t launch_ffn(cudaStream_t st, const FfnArgs& a, int* launches, const c
 cudaError_t launch_ffn_backward(cudaStream_t st, const FfnArgs& a, int* launches, const char** what);
 int ffn_forms(int64_t T, int64_t d, int64_t F, int n_sms, int64_t* tiles);   // muloco_debug_ffn_forms
 
+// Causal attention over packed sequences: the tiles of a batch, 128 tokens each (pair_tiles: up to 256), heaviest first.
+constexpr int ATTN_TILE = 128, ATTN_MAX_DIM = 128;
+struct alignas(16) AttnTile {
+  int32_t start;         // first token of the sequence
+  int32_t offset;        // first token of the tile in the sequence
+  int32_t length;        // of the sequence
+  int32_t pad;
+};
+struct AttnArgs {
+  const AttnTile* pair_tiles;                  // forward: query tiles of 256
+  const AttnTile* query_tiles;                 // backward: query tiles of 128, key tiles of 128
+  const AttnTile* key_tiles;
+  int64_t n_pairs, n_tiles;
+  int64_t tokens;
+  int32_t heads, kv_heads, dim;
+  float scale;
+  const void* q; int64_t q_ts, q_hs;           // token and head strides (elements)
+  const void* k; int64_t k_ts, k_hs;
+  const void* v; int64_t v_ts, v_hs;
+  void* o_out;                                 // forward: o, dense
+  float* lse;                                  // [heads][tokens]: written forward, read backward
+  const void* o;                               // backward
+  const void* g; int64_t g_ts, g_hs;           // do
+  float* delta;                                // scratch [heads][tokens]
+  void* dq; void* dk; void* dv;                // dense
+  int* status;
+  unsigned long long wait_limit_ns;
+  int withhold;
+};
+cudaError_t launch_attention(cudaStream_t st, const AttnArgs& a, const char** what);            // one launch
+cudaError_t launch_attention_backward(cudaStream_t st, const AttnArgs& a, const char** what);   // two
+
 }  // namespace muloco

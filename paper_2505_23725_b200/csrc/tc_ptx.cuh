@@ -7,6 +7,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 namespace muloco {
 
 namespace {
@@ -240,6 +242,28 @@ inline EncodeTiledFn get_encode_fn() {
     return nullptr;
   fn = reinterpret_cast<EncodeTiledFn>(ptr);
   return fn;
+}
+
+// Makes the current device's context this thread's: the descriptor encoder is a driver call, which fails in a
+// thread that has made no runtime call yet (a backward pass runs in a thread of its own).
+inline cudaError_t bind_context(const char** what) {
+  *what = "cudaSetDevice";
+  int dev = 0;
+  const cudaError_t e = cudaGetDevice(&dev);
+  return e == cudaSuccess ? cudaSetDevice(dev) : e;
+}
+
+// Raises a kernel's shared-memory limit, once per device (`allowed`: a bit for each of the first 64 that it was raised on; calls
+// may come from several threads).
+template <typename K>
+cudaError_t allow_smem(K kernel, int bytes, std::atomic<uint64_t>* allowed) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+  if (e != cudaSuccess || (allowed->load(std::memory_order_relaxed) & bit)) return e;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) allowed->fetch_or(bit, std::memory_order_relaxed);
+  return e;
 }
 
 }  // namespace
