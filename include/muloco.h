@@ -513,6 +513,52 @@ MULOCO_API muloco_status muloco_causal_attention_backward(muloco_ctx* ctx, const
                                                           int64_t do_token_stride, int64_t do_head_stride, const void* o,
                                                           const float* lse, float* delta, void* dq, void* dk, void* dv);
 
+/* Norm over the last dimension with the sum of the residual stream in front of it:
+ *     h = x + residual,  n = (h - m) / sqrt(mean (h - m)^2 + eps),  y = n * weight + bias
+ * with m = mean h when `center` is set (layer norm), else m = 0 (root mean square).  x, residual, h and y are [tokens][d] of
+ * `dtype`; without a residual h is x and not written.  weight and bias are float32 [d] or NULL (ones, zeros).  mean and rstd (float32
+ * [tokens]; mean only when centred) are for the backward pass.  Statistics are float32, the variance around the
+ * mean; y is made from the sum before it is rounded to h, and rounded once.
+ * ldx, ldr: row strides of x and residual in elements; h and y are dense.  y may be x (or residual), and h too, where that one is dense.
+ * Limits (MULOCO_ESHAPE): d in 1..32768, tokens < 2^31. */
+typedef struct {
+  int64_t tokens, d, ldx, ldr;
+  int32_t dtype, center;
+  float eps;
+  int32_t pad;
+  const void* x;
+  const void* residual;    /* or NULL */
+  const float* weight;
+  const float* bias;
+} muloco_norm;
+MULOCO_API muloco_status muloco_layer_norm(muloco_ctx* ctx, const muloco_norm* a, void* h, void* y, float* mean, float* rstd);
+/* Backward pass: x of `a` is the forward pass's h, residual its gradient dh from elsewhere (the stream's own) or NULL, bias is not
+ * read.  dx, dense, is the gradient of x and of the residual alike: that of h through y, and dh.  dweight and dbias (float32 [d],
+ * written, not added to; NULL: not wanted) are summed over the tokens in a fixed order, through scratch that the
+ * caller provides: float32 [MULOCO_NORM_PARTS][2][d]. */
+enum { MULOCO_NORM_PARTS = 296 };
+MULOCO_API muloco_status muloco_layer_norm_backward(muloco_ctx* ctx, const muloco_norm* a, const void* dy, int64_t lddy,
+                                                    const float* mean, const float* rstd, void* dx, float* dweight,
+                                                    float* dbias, float* scratch);
+
+/* Embedding lookup: out[t] = scale * table[ids[t]], table [rows][d] (row stride ld) and out [tokens][d] (dense) of `dtype`, ids
+ * int64.  A token outside the table raises MULOCO_EINVAL through muloco_sync_status and its row of out is NaN.
+ * Limits (MULOCO_ESHAPE): d in 1..2^20, tokens and rows < 2^31. */
+typedef struct {
+  int64_t tokens, rows, d, ld;
+  int32_t dtype;
+  float scale;
+  const int64_t* ids;
+} muloco_embedding;
+MULOCO_API muloco_status muloco_embedding_lookup(muloco_ctx* ctx, const muloco_embedding* a, const void* table, void* out);
+/* The table's gradient, dense [rows][d] of `dtable_dtype`, every row written: row v = scale * sum of the rows of dout (of a->dtype, row
+ * stride a->ld) whose token is v, added in float32 in the order of the tokens (runs of more than 64 in pieces, in a fixed
+ * order) and rounded once.  A token outside the table adds nothing and raises MULOCO_EINVAL through muloco_sync_status.
+ * scratch: device memory of muloco_embedding_scratch(tokens, d) bytes, 16-byte aligned, that the caller provides. */
+MULOCO_API size_t muloco_embedding_scratch(int64_t tokens, int64_t d);
+MULOCO_API muloco_status muloco_embedding_backward(muloco_ctx* ctx, const muloco_embedding* a, const void* dout,
+                                                   int32_t dtable_dtype, void* dtable, void* scratch);
+
 /* Small host state for checkpoint/resume: inner step counters per worker and
  * sync counters per fragment.  Call with blob == NULL to get the size. */
 MULOCO_API muloco_status muloco_get_state(const muloco_ctx* ctx, void* host_blob, size_t* nbytes);

@@ -31,6 +31,7 @@ DEBUG_WAIT_LIMIT_NS, DEBUG_WITHHOLD_COPY, DEBUG_CANARIES, DEBUG_CORRUPT_CANARY =
 PHASES = ["prologue", "ns", "adamw", "sync", "copy"]
 ACTIVATIONS = {"silu": 0, "gelu": 1}
 ADAMW_BLOCK = 256              # elements that share a scale in 8-bit AdamW states
+NORM_PARTS = 296               # partial sums of a norm's backward pass
 
 EXPORTS = [
     "muloco_create", "muloco_destroy", "muloco_inner_step", "muloco_inner_step_host",
@@ -44,6 +45,8 @@ EXPORTS = [
     "muloco_debug_ffn_forms",
     "muloco_sequences_bytes", "muloco_sequences_create", "muloco_sequences_destroy",
     "muloco_causal_attention", "muloco_causal_attention_backward",
+    "muloco_layer_norm", "muloco_layer_norm_backward",
+    "muloco_embedding_lookup", "muloco_embedding_scratch", "muloco_embedding_backward",
 ]
 
 
@@ -109,10 +112,23 @@ class Attention(C.Structure):
                 ("k_head_stride", C.c_int64), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64)]
 
 
+class Norm(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("d", C.c_int64), ("ldx", C.c_int64), ("ldr", C.c_int64), ("dtype", C.c_int32),
+                ("center", C.c_int32), ("eps", C.c_float), ("pad", C.c_int32), ("x", C.c_void_p),
+                ("residual", C.c_void_p), ("weight", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class Embedding(C.Structure):
+    _fields_ = [("tokens", C.c_int64), ("rows", C.c_int64), ("d", C.c_int64), ("ld", C.c_int64), ("dtype", C.c_int32),
+                ("scale", C.c_float), ("ids", C.c_void_p)]
+
+
 # the argument structs as bytes
 _QK_PACK = struct.Struct("qqiiiiiifiQQQQQQQqqqq").pack
 _FFN_PACK = struct.Struct("qqqqqqqQQQQii").pack
 _ATTENTION_PACK = struct.Struct("iiifQQQqqqqqq").pack
+_NORM_PACK = struct.Struct("qqqqiifiQQQQ").pack
+_EMBEDDING_PACK = struct.Struct("qqqqifQ").pack
 
 
 class MulocoError(RuntimeError):
@@ -190,10 +206,16 @@ def load_library():
     lib.muloco_sequences_destroy.restype = None
     lib.muloco_causal_attention.argtypes = [vp, packed, vp, vp, vp]
     lib.muloco_causal_attention_backward.argtypes = [vp, packed, vp, vp, i64, i64] + [vp] * 6
+    lib.muloco_layer_norm.argtypes = [vp, packed, vp, vp, vp, vp]
+    lib.muloco_layer_norm_backward.argtypes = [vp, packed, vp, i64, vp, vp, vp, vp, vp, vp]
+    lib.muloco_embedding_lookup.argtypes = [vp, packed, vp, vp]
+    lib.muloco_embedding_scratch.argtypes = [i64, i64]
+    lib.muloco_embedding_backward.argtypes = [vp, packed, vp, i32, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("muloco_destroy", "muloco_last_error", "muloco_adamw_destroy", "muloco_sequences_destroy"):
             fn.restype = i32
+    lib.muloco_embedding_scratch.restype = C.c_size_t
     _lib = lib
     return lib
 
@@ -640,6 +662,108 @@ class _Operators:
         if cur is not None:
             cur.wait_stream(self.stream)
         return dq, dk, dv
+
+    # -- norm over the last dimension ---------------------------------------------------------------
+    def _norm(self, x, weight, bias, other, other_name, eps, center):
+        """The packed argument struct of a call and the type (`other`: the residual, or its gradient)."""
+        if x.dtype not in (self._f32, self._bf16):
+            raise ValueError(f"x must be float32 or bfloat16 (got {x.dtype})")
+        self._need("x", x, x.dtype, (None, None))
+        T, d = x.shape
+        for name, t in (("weight", weight), ("bias", bias)):
+            if t is not None:
+                self._need(name, t, self._f32, (d,), dense=True)
+        if other is not None:
+            self._need(other_name, other, x.dtype, (T, d))
+        p = [0 if t is None else t.data_ptr() for t in (other, weight, bias)]
+        return _NORM_PACK(T, d, x.stride(0), 0 if other is None else other.stride(0), F32 if x.dtype is self._f32 else BF16,
+                          1 if center else 0, eps, 0, x.data_ptr(), *p)
+
+    def layer_norm(self, x, weight=None, bias=None, residual=None, eps=1e-6, center=True):
+        """muloco_layer_norm: with h = x + residual (x itself without one), y = (h - mean) / sqrt(var + eps) * weight + bias
+        over the last dimension of x [tokens, d] (float32 or bfloat16; weight and bias float32); with center=False the mean is left
+        where it is (root mean square norm).  Returns (y, h, rstd, mean), the last three for the backward pass; mean is
+        None with center=False."""
+        a = self._norm(x, weight, bias, residual, "residual", eps, center)
+        y = x.new_empty(x.shape)
+        h = x if residual is None else x.new_empty(x.shape)
+        rstd = x.new_empty(x.shape[:1], dtype=self._f32)
+        mean = x.new_empty(x.shape[:1], dtype=self._f32) if center else None
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (x, weight, bias, residual, y, h, rstd, mean))
+        self._check(self.lib.muloco_layer_norm(self.ctx, a, None if residual is None else h.data_ptr(), y.data_ptr(),
+                                               mean.data_ptr() if center else None, rstd.data_ptr()))
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        return y, h, rstd, mean
+
+    def layer_norm_backward(self, dy, h, rstd, mean=None, weight=None, dh=None, bias=False):
+        """muloco_layer_norm_backward: (dx, dweight, dbias) from dy, the forward pass's h, rstd and mean (None: not centred) and the
+        gradient dh that h has from elsewhere (or None).  dx is the gradient of x and of the residual.  dweight is None without a
+        weight, dbias unless `bias` is set."""
+        a = self._norm(h, weight, None, dh, "dh", 0.0, mean is not None)
+        T, d = h.shape
+        self._need("dy", dy, h.dtype, (T, d))
+        self._need("rstd", rstd, self._f32, (T,), dense=True)
+        if mean is not None:
+            self._need("mean", mean, self._f32, (T,), dense=True)
+        dx = h.new_empty(h.shape)
+        dw = rstd.new_empty(d) if weight is not None else None
+        db = rstd.new_empty(d) if bias else None
+        scratch = rstd.new_empty((NORM_PARTS, 2, d)) if weight is not None or bias else None
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (dy, h, rstd, mean, weight, dh, dx, dw, db, scratch))
+        p = [None if t is None else t.data_ptr() for t in (mean, rstd, dx, dw, db, scratch)]
+        self._check(self.lib.muloco_layer_norm_backward(self.ctx, a, dy.data_ptr(), dy.stride(0), *p))
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        return dx, dw, db
+
+    # -- embedding ------------------------------------------------------------------------------------
+    def embedding(self, ids, table, scale=1.0):
+        """muloco_embedding_lookup: scale * table[ids] for ids int64 [tokens] and a table [rows, d] in float32 or bfloat16; the
+        result has the table's type."""
+        if table.dtype not in (self._f32, self._bf16):
+            raise ValueError(f"table must be float32 or bfloat16 (got {table.dtype})")
+        self._need("table", table, table.dtype, (None, None))
+        self._need("ids", ids, self._i64, (None,), dense=True)
+        T, (V, d) = ids.shape[0], table.shape
+        out = table.new_empty((T, d))
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (ids, table, out))
+        self._check(self.lib.muloco_embedding_lookup(
+            self.ctx, _EMBEDDING_PACK(T, V, d, table.stride(0), F32 if table.dtype is self._f32 else BF16, scale, ids.data_ptr()),
+            table.data_ptr(), out.data_ptr()))
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        return out
+
+    def embedding_backward(self, dout, ids, rows, scale=1.0, dtype=None):
+        """muloco_embedding_backward: the gradient [rows, d] of the table, in `dtype` (float32, the default, or bfloat16), from dout
+        [tokens, d] in either type."""
+        dtype = self._f32 if dtype is None else dtype
+        if dtype not in (self._f32, self._bf16):
+            raise ValueError(f"dtype must be float32 or bfloat16 (got {dtype})")
+        if dout.dtype not in (self._f32, self._bf16):
+            raise ValueError(f"dout must be float32 or bfloat16 (got {dout.dtype})")
+        self._need("ids", ids, self._i64, (None,), dense=True)
+        T = ids.shape[0]
+        self._need("dout", dout, dout.dtype, (T, None))
+        d = dout.shape[1]
+        dtable = dout.new_empty((rows, d), dtype=dtype)
+        scratch = dout.new_empty(self.lib.muloco_embedding_scratch(T, d), dtype=self.torch.uint8)
+        cur = self._other_stream()
+        if cur is not None:
+            self._enter(cur, (dout, ids, dtable, scratch))
+        self._check(self.lib.muloco_embedding_backward(
+            self.ctx, _EMBEDDING_PACK(T, rows, d, dout.stride(0), F32 if dout.dtype is self._f32 else BF16, scale, ids.data_ptr()),
+            dout.data_ptr(), F32 if dtype is self._f32 else BF16, dtable.data_ptr(), scratch.data_ptr()))
+        if cur is not None:
+            cur.wait_stream(self.stream)
+        return dtable
 
 
 class Sequences:

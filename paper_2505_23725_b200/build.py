@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmuloco.so")
 LIB_DEBUG = os.path.join(HERE, "libmuloco_debug.so")   # the same sources with -DMULOCO_DEBUG (index checks of the optimizer's kernels)
 SOURCES = ["capi.cu", "elementwise.cu", "outer_sync.cu", "topk.cu", "ns_fp32.cu", "ns_tc.cu", "ns_static.cu",
-           "adamw.cu", "qk_norm.cu", "ffn.cu", "ops_capi.cu", "attention.cu", "block_capi.cu"]
+           "adamw.cu", "qk_norm.cu", "ffn.cu", "ops_capi.cu", "attention.cu", "layer_norm.cu", "embedding.cu", "block_capi.cu"]
 
 
 def _nvcc() -> str:

@@ -1,4 +1,5 @@
-// C entry points of the operators that complete a decoder block: causal attention over packed sequences.
+// C entry points of the operators that complete a decoder: causal attention over packed sequences, norm over the last dimension,
+// embedding lookup.
 #include <math.h>
 #include <string.h>
 
@@ -229,6 +230,160 @@ MULOCO_API muloco_status muloco_causal_attention_backward(muloco_ctx* c, const m
   const cudaError_t e = launch_attention_backward(v.st, k, &what);
   if (e != cudaSuccess) return ctx_fail(c, MULOCO_ECUDA, "%s: %s", what, cudaGetErrorString(e));
   ctx_count_launches(c, 2);
+  return MULOCO_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+muloco_status check_norm(muloco_ctx* c, const muloco_norm* a) {
+  if (!a) return ctx_fail(c, MULOCO_EINVAL, "arguments are NULL");
+  if (a->tokens < 0 || a->tokens > INT32_MAX) return ctx_fail(c, MULOCO_ESHAPE, "tokens must be in 0..2^31-1");
+  if (a->d < 1 || a->d > NORM_MAX_DIM) return ctx_fail(c, MULOCO_ESHAPE, "d must be in 1..%d (got %lld)", NORM_MAX_DIM, (long long)a->d);
+  if (a->dtype != MULOCO_F32 && a->dtype != MULOCO_BF16) return ctx_fail(c, MULOCO_EINVAL, "unknown dtype %d", a->dtype);
+  if (!(a->eps >= 0.f)) return ctx_fail(c, MULOCO_EINVAL, "eps must be >= 0");
+  if (a->tokens == 0) return MULOCO_OK;
+  if (a->tokens > 1 && (a->ldx < a->d || (a->residual && a->ldr < a->d))) return ctx_fail(c, MULOCO_ESHAPE, "row strides must be at least a row long");
+  const size_t al = a->dtype == MULOCO_BF16 ? 2 : 4;
+  if (!a->x || misaligned(a->x, al) || misaligned(a->residual, al) || misaligned(a->weight, 4) || misaligned(a->bias, 4))
+    return ctx_fail(c, MULOCO_EINVAL, "x is NULL, or a pointer is not aligned to its type");
+  return MULOCO_OK;
+}
+
+// (a single row's stride does not matter)
+int64_t stride_of(const muloco_norm* a, const void* p, int64_t ld) { return !p ? 0 : a->tokens > 1 ? ld : a->d; }
+
+NormArgs norm_args(const muloco_norm* a) {
+  NormArgs n;
+  memset(&n, 0, sizeof n);
+  n.tokens = a->tokens; n.d = (int32_t)a->d; n.center = a->center != 0;
+  n.ldx = stride_of(a, a->x, a->ldx); n.ldr = stride_of(a, a->residual, a->ldr);
+  n.x = a->x; n.weight = a->weight;
+  n.eps = a->eps;
+  n.inv_d = (float)(1.0 / (double)a->d);
+  return n;
+}
+
+muloco_status check_embedding(muloco_ctx* c, const muloco_embedding* a) {
+  if (!a) return ctx_fail(c, MULOCO_EINVAL, "arguments are NULL");
+  if (a->tokens < 0 || a->tokens > INT32_MAX || a->rows < 0 || a->rows > INT32_MAX)
+    return ctx_fail(c, MULOCO_ESHAPE, "tokens and rows must be in 0..2^31-1");
+  if (a->d < 1 || a->d > (1 << 20)) return ctx_fail(c, MULOCO_ESHAPE, "d must be in 1..2^20 (got %lld)", (long long)a->d);
+  if ((a->tokens + a->rows / 32 + 64) * ((a->d + 255) / 256) > ((int64_t)1 << 33)) return ctx_fail(c, MULOCO_ESHAPE, "too many rows for one call");
+  if (a->dtype != MULOCO_F32 && a->dtype != MULOCO_BF16) return ctx_fail(c, MULOCO_EINVAL, "unknown dtype %d", a->dtype);
+  if (!isfinite(a->scale)) return ctx_fail(c, MULOCO_EINVAL, "scale must be finite");
+  if (a->tokens > 0 && (!a->ids || misaligned(a->ids, 8))) return ctx_fail(c, MULOCO_EINVAL, "ids is NULL or not aligned to its type");
+  return MULOCO_OK;
+}
+
+EmbeddingArgs embedding_args(const muloco_embedding* a, const CtxView& v) {
+  EmbeddingArgs e;
+  memset(&e, 0, sizeof e);
+  e.tokens = a->tokens; e.rows = a->rows; e.ld = a->ld; e.d = (int32_t)a->d;
+  e.ids = a->ids; e.scale = a->scale;
+  e.status = v.status;
+  return e;
+}
+
+}  // namespace
+
+extern "C" {
+
+MULOCO_API muloco_status muloco_layer_norm(muloco_ctx* c, const muloco_norm* a, void* h, void* y, float* mean, float* rstd) {
+  if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
+  const muloco_status r = check_norm(c, a);
+  if (r != MULOCO_OK || a->tokens == 0) return r;
+  const size_t al = a->dtype == MULOCO_BF16 ? 2 : 4;
+  if (!y || !rstd || (a->center && !mean) || (a->residual && !h) || misaligned(y, al) || misaligned(h, al) || misaligned(mean, 4) ||
+      misaligned(rstd, 4))
+    return ctx_fail(c, MULOCO_EINVAL, "a result is NULL or not aligned to its type");
+  for (const void* in : {a->x, a->residual})
+    if (in && (in == y || in == h) && (in == a->x ? a->ldx : a->ldr) != a->d && a->tokens > 1)
+      return ctx_fail(c, MULOCO_EINVAL, "a result in place of an input needs that one dense");
+  if (a->residual && y == h) return ctx_fail(c, MULOCO_EINVAL, "y and h are the same");
+  const CtxView v = ctx_view(c);
+  NormArgs n = norm_args(a);
+  n.residual = a->residual; n.bias = a->bias;
+  n.h = h; n.y = y; n.mean = mean; n.rstd = rstd;
+  int launches = 0;
+  BLOCK_CK(launch_norm(v.st, n, false, a->dtype == MULOCO_BF16, v.n_sms, &launches));
+  ctx_count_launches(c, launches);
+  return MULOCO_OK;
+}
+
+MULOCO_API muloco_status muloco_layer_norm_backward(muloco_ctx* c, const muloco_norm* a, const void* dy, int64_t lddy, const float* mean,
+                                                    const float* rstd, void* dx, float* dweight, float* dbias, float* scratch) {
+  if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
+  const muloco_status r = check_norm(c, a);
+  if (r != MULOCO_OK) return r;
+  if (misaligned(dweight, 4) || misaligned(dbias, 4)) return ctx_fail(c, MULOCO_EINVAL, "a pointer is not aligned to its type");
+  const CtxView v = ctx_view(c);
+  if (a->tokens == 0) {                        // the sums over tokens are empty
+    if (dweight) BLOCK_CK(cudaMemsetAsync(dweight, 0, (size_t)a->d * 4, v.st));
+    if (dbias) BLOCK_CK(cudaMemsetAsync(dbias, 0, (size_t)a->d * 4, v.st));
+    return MULOCO_OK;
+  }
+  const size_t al = a->dtype == MULOCO_BF16 ? 2 : 4;
+  if (!dy || !dx || !rstd || (a->center && !mean) || misaligned(dy, al) || misaligned(dx, al) || misaligned(mean, 4) || misaligned(rstd, 4))
+    return ctx_fail(c, MULOCO_EINVAL, "a tensor is NULL or not aligned to its type");
+  if (a->tokens > 1 && lddy < a->d) return ctx_fail(c, MULOCO_ESHAPE, "row strides must be at least a row long");
+  if ((dweight || dbias) && (!scratch || misaligned(scratch, 16))) return ctx_fail(c, MULOCO_EINVAL, "scratch is NULL or not 16-byte aligned");
+  NormArgs n = norm_args(a);
+  n.dh = a->residual;
+  n.dy = dy; n.ldy = stride_of(a, dy, lddy);
+  n.mean = const_cast<float*>(mean); n.rstd = const_cast<float*>(rstd);
+  n.dx = dx; n.dweight = dweight; n.dbias = dbias;
+  n.partials = dweight || dbias ? scratch : nullptr;
+  int launches = 0;
+  BLOCK_CK(launch_norm(v.st, n, true, a->dtype == MULOCO_BF16, v.n_sms, &launches));
+  ctx_count_launches(c, launches);
+  return MULOCO_OK;
+}
+
+MULOCO_API muloco_status muloco_embedding_lookup(muloco_ctx* c, const muloco_embedding* a, const void* table, void* out) {
+  if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
+  const muloco_status r = check_embedding(c, a);
+  if (r != MULOCO_OK || a->tokens == 0) return r;
+  if (a->rows > 1 && a->ld < a->d) return ctx_fail(c, MULOCO_ESHAPE, "row strides must be at least a row long");
+  const size_t al = a->dtype == MULOCO_BF16 ? 2 : 4;
+  if ((a->rows > 0 && !table) || !out || misaligned(table, al) || misaligned(out, al))
+    return ctx_fail(c, MULOCO_EINVAL, "table or out is NULL or not aligned to its type");
+  const CtxView v = ctx_view(c);
+  EmbeddingArgs e = embedding_args(a, v);
+  e.table = table; e.out = out;
+  BLOCK_CK(launch_embedding(v.st, e, a->dtype == MULOCO_BF16));
+  ctx_count_launches(c, 1);
+  return MULOCO_OK;
+}
+
+MULOCO_API size_t muloco_embedding_scratch(int64_t tokens, int64_t d) { return tokens > 0 && d > 0 ? embedding_scratch(tokens, d) : 0; }
+
+MULOCO_API muloco_status muloco_embedding_backward(muloco_ctx* c, const muloco_embedding* a, const void* dout, int32_t dtable_dtype,
+                                                   void* dtable, void* scratch) {
+  if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
+  const muloco_status r = check_embedding(c, a);
+  if (r != MULOCO_OK) return r;
+  if (dtable_dtype != MULOCO_F32 && dtable_dtype != MULOCO_BF16) return ctx_fail(c, MULOCO_EINVAL, "unknown dtype %d", dtable_dtype);
+  const size_t al = a->dtype == MULOCO_BF16 ? 2 : 4, out_al = dtable_dtype == MULOCO_BF16 ? 2 : 4;
+  if (a->rows > 0 && (!dtable || misaligned(dtable, out_al))) return ctx_fail(c, MULOCO_EINVAL, "dtable is NULL or not aligned to its type");
+  const CtxView v = ctx_view(c);
+  if (a->tokens == 0) {
+    if (a->rows > 0) BLOCK_CK(cudaMemsetAsync(dtable, 0, (size_t)a->rows * (size_t)a->d * out_al, v.st));
+    return MULOCO_OK;
+  }
+  if (a->tokens > 1 && a->ld < a->d) return ctx_fail(c, MULOCO_ESHAPE, "row strides must be at least a row long");
+  if (!dout || misaligned(dout, al)) return ctx_fail(c, MULOCO_EINVAL, "dout is NULL or not aligned to its type");
+  if (!scratch || misaligned(scratch, 16)) return ctx_fail(c, MULOCO_EINVAL, "scratch is NULL or not 16-byte aligned");
+  EmbeddingArgs e = embedding_args(a, v);
+  e.dout = dout; e.dtable = dtable; e.scratch = scratch;
+  int launches = 0;
+  BLOCK_CK(launch_embedding_backward(v.st, e, a->dtype == MULOCO_BF16, dtable_dtype == MULOCO_BF16, &launches));
+  ctx_count_launches(c, launches);
   return MULOCO_OK;
 }
 

@@ -10,7 +10,7 @@
 namespace muloco {
 
 // Device status word bits (OR-ed by kernels, read by muloco_sync_status).
-enum : int { ST_NONFINITE = 1, ST_TIMEOUT = 2, ST_BOUNDS = 4, ST_POSITION = 8 };
+enum : int { ST_NONFINITE = 1, ST_TIMEOUT = 2, ST_BOUNDS = 4, ST_POSITION = 8, ST_TOKEN = 16 };
 
 // Debug build (-DMULOCO_DEBUG): kernels check the indices they derive (work-list cursors, matrix
 // slots, tile coordinates, segment and unit indices) before using them; a failed check raises
@@ -328,5 +328,43 @@ struct AttnArgs {
 };
 cudaError_t launch_attention(cudaStream_t st, const AttnArgs& a, const char** what);            // one launch
 cudaError_t launch_attention_backward(cudaStream_t st, const AttnArgs& a, const char** what);   // two
+
+// Norm over the last dimension.
+struct NormArgs {
+  int64_t tokens, ldx, ldr, ldy;               // row strides of x, of residual | dh, of dy (the other tensors are dense)
+  const void* x;                               // backward: h
+  const void* residual;                        // or NULL
+  void* h;                                     // forward, with a residual
+  void* y;
+  const float* weight;                         // NULL: ones
+  const float* bias;                           // NULL: zeros
+  float* mean;                                 // written forward, read backward (centred)
+  float* rstd;
+  const void* dy; const void* dh;              // backward; dh or NULL
+  void* dx;
+  float* dweight; float* dbias;                // or NULL
+  float* partials;                             // [NORM_PARTS][2][d], when dweight or dbias is wanted
+  int32_t d, center;
+  float eps, inv_d;
+};
+constexpr int NORM_PARTS = MULOCO_NORM_PARTS, NORM_MAX_DIM = 32768;
+cudaError_t launch_norm(cudaStream_t st, const NormArgs& a, bool back, int is_bf16, int n_sms, int* launches);
+
+// Embedding lookup.
+constexpr int EMB_SORT_BLOCK = 2048, EMB_MERGE = 8, EMB_CHUNK = 64;
+struct EmbeddingArgs {
+  int64_t tokens, rows, ld;                    // ld: row stride of the table (forward), of dout (backward)
+  const int64_t* ids;
+  const void* table; void* out;                // forward
+  const void* dout; void* dtable;              // backward
+  void* scratch;                               // embedding_scratch() bytes
+  float* partials;                             // in scratch: sums of the pieces of long runs, d_pad columns each
+  int32_t d, d_pad;
+  float scale;
+  int* status;
+};
+size_t embedding_scratch(int64_t tokens, int64_t d);
+cudaError_t launch_embedding(cudaStream_t st, const EmbeddingArgs& a, int is_bf16);             // one launch
+cudaError_t launch_embedding_backward(cudaStream_t st, const EmbeddingArgs& a, int in_bf16, int out_bf16, int* launches);
 
 }  // namespace muloco

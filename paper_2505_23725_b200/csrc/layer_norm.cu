@@ -1,0 +1,326 @@
+// Norm over the last dimension, centred (layer norm) or not (root mean square), with the residual sum in front of it, and its
+// backward pass.
+//
+//   h = x + residual,  m = mean h (0 if not centred),  r = 1 / sqrt(mean (h - m)^2 + eps),  n = (h - m) r,  y = n weight + bias
+//   backward:  e = dy weight,  dx = r (e - n mean(e n) - mean e) + dh   (mean e only if centred),
+//              dweight = sum over tokens of dy n,  dbias = sum over tokens of dy
+//
+// Bound by memory: every tensor crosses it once, so a row stays in registers between the statistics and the result.  A row is
+// held by WPR warps, E entries per lane; the variance is taken around the mean in a second pass over the registers.  The
+// sums over tokens: each block adds up its own rows in registers and leaves a partial sum, and a second kernel adds those in the
+// order of the blocks.
+#include <string.h>
+
+#include <type_traits>
+
+#include "internal.h"
+
+namespace muloco {
+
+namespace {
+
+template <typename T> __device__ __forceinline__ float to_f32(T x);
+template <> __device__ __forceinline__ float to_f32(float x) { return x; }
+template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <typename T> __device__ __forceinline__ T from_f32(float x);
+template <> __device__ __forceinline__ float from_f32(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16(x); }
+
+// E entries of a row in a lane: chunks of V neighbouring entries, chunk c of lane l starts at (c lanes + l) V.
+template <typename T, int V> struct alignas(sizeof(T) * V) Chunk { T v[V]; };
+
+template <typename T, int V, int E>
+struct Row {
+  Chunk<T, V> c[E / V];
+  __device__ __forceinline__ float at(int i) const { return to_f32(c[i / V].v[i % V]); }
+};
+
+template <int V>
+__device__ __forceinline__ int column(int chunk, int lane, int lanes) { return (chunk * lanes + lane) * V; }
+
+template <typename T, int V, int E>
+__device__ __forceinline__ void load_row(Row<T, V, E>& r, const T* p, int d, int lane, int lanes) {
+#pragma unroll
+  for (int c = 0; c < E / V; ++c) {
+    const int col = column<V>(c, lane, lanes);
+    if (col < d) {
+      r.c[c] = *reinterpret_cast<const Chunk<T, V>*>(p + col);
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) r.c[c].v[i] = from_f32<T>(0.f);
+    }
+  }
+}
+template <typename T, int V, int E>
+__device__ __forceinline__ void store_row(const float (&f)[E], T* p, int d, int lane, int lanes) {
+#pragma unroll
+  for (int c = 0; c < E / V; ++c) {
+    const int col = column<V>(c, lane, lanes);
+    Chunk<T, V> o;
+#pragma unroll
+    for (int i = 0; i < V; ++i) o.v[i] = from_f32<T>(f[c * V + i]);
+    if (col < d) *reinterpret_cast<Chunk<T, V>*>(p + col) = o;
+  }
+}
+// float32 vectors of the row's columns (weight, bias)
+template <int V>
+__device__ __forceinline__ void load_vector(float (&w)[V], const float* p, int col, int d, float otherwise) {
+  if (p && col < d) {
+    constexpr int W = V % 4 == 0 ? 4 : 1;      // (columns of a chunk of 8 are two accesses of 16 bytes)
+#pragma unroll
+    for (int i = 0; i < V; i += W) {
+      const Chunk<float, W> q = *reinterpret_cast<const Chunk<float, W>*>(p + col + i);
+#pragma unroll
+      for (int k = 0; k < W; ++k) w[i + k] = q.v[k];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) w[i] = otherwise;
+  }
+}
+
+// Sum over the lanes of a row's WPR warps, the same in all of them.  `slots`: WPR floats of this row group; a group's calls alternate
+// between two sets of them, so that one barrier is enough.
+template <int WPR, int N>
+__device__ __forceinline__ void row_sum(float (&x)[N], float* slots, int group, int warp_in_row) {
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+#pragma unroll
+    for (int o = 16; o; o >>= 1) x[n] += __shfl_xor_sync(0xffffffffu, x[n], o);
+  if (WPR > 1) {
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+      for (int n = 0; n < N; ++n) slots[n * WPR + warp_in_row] = x[n];
+    asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(WPR * 32) : "memory");
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      x[n] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WPR; ++w) x[n] += slots[n * WPR + w];
+    }
+  }
+}
+
+constexpr int BLOCK_WARPS = 8;
+template <int WPR> __host__ __device__ constexpr int block_warps() { return WPR > BLOCK_WARPS ? WPR : BLOCK_WARPS; }
+
+template <typename T, int V, int E, int WPR>
+__global__ void __launch_bounds__(block_warps<WPR>() * 32)
+norm_kernel(const NormArgs a) {
+  constexpr int GROUPS = block_warps<WPR>() / WPR;
+  __shared__ float slots[GROUPS][2][WPR];
+  const int warp = threadIdx.x >> 5, group = warp / WPR, in_row = warp % WPR;
+  const int lane = in_row * 32 + (threadIdx.x & 31), lanes = WPR * 32;
+  const int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  grid_wait();
+  grid_release();
+  if (row >= a.tokens) return;                 // (a whole row group)
+  const int d = a.d;
+  Row<T, V, E> x, r;
+  load_row(x, reinterpret_cast<const T*>(a.x) + row * a.ldx, d, lane, lanes);
+  if (a.residual) load_row(r, reinterpret_cast<const T*>(a.residual) + row * a.ldr, d, lane, lanes);
+  float f[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) f[i] = x.at(i);
+  if (a.residual) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) f[i] += r.at(i);
+    store_row<T, V, E>(f, reinterpret_cast<T*>(a.h) + row * d, d, lane, lanes);
+  }
+  float mean = 0.f;
+  if (a.center) {
+    float s[1] = {0.f};
+#pragma unroll
+    for (int i = 0; i < E; ++i) s[0] += f[i];  // (entries past the end are zero)
+    row_sum<WPR, 1>(s, slots[group][0], group, in_row);
+    mean = s[0] * a.inv_d;
+  }
+  float q[1] = {0.f};
+#pragma unroll
+  for (int c = 0; c < E / V; ++c) {
+    const bool in = column<V>(c, lane, lanes) < d;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      f[c * V + i] = in ? f[c * V + i] - mean : 0.f;
+      q[0] += f[c * V + i] * f[c * V + i];
+    }
+  }
+  row_sum<WPR, 1>(q, slots[group][1], group, in_row);
+  const float rstd = 1.0f / sqrtf(q[0] * a.inv_d + a.eps);
+#pragma unroll
+  for (int c = 0; c < E / V; ++c) {
+    const int col = column<V>(c, lane, lanes);
+    float w[V], b[V];
+    load_vector<V>(w, a.weight, col, d, 1.f);
+    load_vector<V>(b, a.bias, col, d, 0.f);
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[c * V + i] = f[c * V + i] * rstd * w[i] + b[i];
+  }
+  store_row<T, V, E>(f, reinterpret_cast<T*>(a.y) + row * d, d, lane, lanes);
+  if (lane == 0) {
+    a.rstd[row] = rstd;
+    if (a.center) a.mean[row] = mean;
+  }
+}
+
+template <typename T, int V, int E, int WPR>
+__global__ void __launch_bounds__(block_warps<WPR>() * 32)
+norm_back_kernel(const NormArgs a) {
+  constexpr int GROUPS = block_warps<WPR>() / WPR;
+  __shared__ float slots[GROUPS][2][2 * WPR];
+  extern __shared__ float sums[];              // [GROUPS][columns] of the block, when it has several row groups
+  const int warp = threadIdx.x >> 5, group = warp / WPR, in_row = warp % WPR;
+  const int lane = in_row * 32 + (threadIdx.x & 31), lanes = WPR * 32;
+  const int d = a.d;
+  grid_wait();
+  grid_release();
+  float dw[E], db[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) { dw[i] = 0.f; db[i] = 0.f; }
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < a.tokens; row += (int64_t)gridDim.x * GROUPS, turn ^= 1) {
+    Row<T, V, E> h, g, s;
+    load_row(g, reinterpret_cast<const T*>(a.dy) + row * a.ldy, d, lane, lanes);
+    load_row(h, reinterpret_cast<const T*>(a.x) + row * a.ldx, d, lane, lanes);
+    if (a.dh) load_row(s, reinterpret_cast<const T*>(a.dh) + row * a.ldr, d, lane, lanes);
+    const float rstd = a.rstd[row], mean = a.center ? a.mean[row] : 0.f;
+    float n[E], e[E], t[2] = {0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < E / V; ++c) {
+      const int col = column<V>(c, lane, lanes);
+      float w[V];
+      load_vector<V>(w, a.weight, col, d, 1.f);
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int k = c * V + i;
+        const float dy = g.at(k);              // zero past the end, which keeps such entries out of every sum
+        n[k] = (h.at(k) - mean) * rstd;
+        dw[k] += dy * n[k];
+        db[k] += dy;
+        e[k] = dy * w[i];
+        t[0] += e[k] * n[k];
+        t[1] += e[k];
+      }
+    }
+    row_sum<WPR, 2>(t, slots[group][turn], group, in_row);
+    const float along = t[0] * a.inv_d, common = a.center ? t[1] * a.inv_d : 0.f;
+#pragma unroll
+    for (int k = 0; k < E; ++k) e[k] = rstd * (e[k] - n[k] * along - common);
+    if (a.dh) {
+#pragma unroll
+      for (int k = 0; k < E; ++k) e[k] += s.at(k);
+    }
+    store_row<T, V, E>(e, reinterpret_cast<T*>(a.dx) + row * d, d, lane, lanes);
+  }
+  if (!a.partials) return;
+  // partial sums of the block: its row groups one after the other
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    if (which ? !a.dbias : !a.dweight) continue;
+    const float* mine = which ? db : dw;
+    float* out = a.partials + ((int64_t)blockIdx.x * 2 + which) * d;
+    if (GROUPS > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int c = 0; c < E / V; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const int col = column<V>(c, lane, lanes) + i;
+          if (col < d) sums[group * d + col] = mine[c * V + i];
+        }
+      __syncthreads();
+      for (int col = threadIdx.x; col < d; col += blockDim.x) {
+        float s = 0.f;
+#pragma unroll
+        for (int k = 0; k < GROUPS; ++k) s += sums[k * d + col];
+        out[col] = s;
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < E / V; ++c)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          const int col = column<V>(c, lane, lanes) + i;
+          if (col < d) out[col] = mine[c * V + i];
+        }
+    }
+  }
+}
+
+// dweight and dbias from the blocks' partial sums: 32 columns per block, 16 threads per column take every 16th block's.
+constexpr int JOIN = 16;
+__global__ void __launch_bounds__(32 * JOIN)
+norm_join_kernel(const float* partials, int parts, int d, float* dweight, float* dbias) {
+  __shared__ float sums[JOIN][32];
+  const int lane = threadIdx.x & 31, k = threadIdx.x >> 5;
+  const int which = blockIdx.y, col = blockIdx.x * 32 + lane;
+  float* out = which ? dbias : dweight;
+  grid_wait();
+  grid_release();
+  if (!out) return;
+  float s = 0.f;
+  if (col < d)
+#pragma unroll 4
+    for (int p = k; p < parts; p += JOIN) s += partials[((int64_t)p * 2 + which) * d + col];
+  sums[k][lane] = s;
+  __syncthreads();
+  if (k == 0 && col < d) {
+#pragma unroll
+    for (int i = 1; i < JOIN; ++i) s += sums[i][lane];
+    out[col] = s;
+  }
+}
+
+// ----------------------------- host ------------------------------------------
+template <typename T, int V, int E, int WPR>
+cudaError_t run(cudaStream_t st, const NormArgs& a, bool back, int n_sms, int* launches) {
+  constexpr int GROUPS = block_warps<WPR>() / WPR, THREADS = block_warps<WPR>() * 32;
+  const int64_t needed = (a.tokens + GROUPS - 1) / GROUPS;
+  if (!back) {
+    ++*launches;
+    return launch_dependent(norm_kernel<T, V, E, WPR>, (unsigned)needed, THREADS, 0, st, a);
+  }
+  const int most = n_sms * 2 < NORM_PARTS ? n_sms * 2 : NORM_PARTS;
+  const int blocks = (int)(needed < most ? needed : most);
+  const size_t smem = a.partials && GROUPS > 1 ? (size_t)GROUPS * a.d * 4 : 0;      // at most 8 x 1024 floats
+  cudaError_t e = launch_dependent(norm_back_kernel<T, V, E, WPR>, (unsigned)blocks, THREADS, smem, st, a);
+  ++*launches;
+  if (e != cudaSuccess || !a.partials) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((a.d + 31) / 32), 2);
+  cfg.blockDim = dim3(32 * JOIN);
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = 1;
+  ++*launches;
+  return cudaLaunchKernelEx(&cfg, norm_join_kernel, (const float*)a.partials, blocks, (int)a.d, a.dweight, a.dbias);
+}
+
+// Entries per lane and warps per row: short rows one warp with few entries, others as many warps as 32 entries a lane take.
+template <typename T, int V>
+cudaError_t choose(cudaStream_t st, const NormArgs& a, bool back, int n_sms, int* launches) {
+  if (a.d <= 256) return run<T, V, 8, 1>(st, a, back, n_sms, launches);
+  if (a.d <= 1024) return run<T, V, 32, 1>(st, a, back, n_sms, launches);
+  if (a.d <= 2048) return run<T, V, 32, 2>(st, a, back, n_sms, launches);
+  if (a.d <= 4096) return run<T, V, 32, 4>(st, a, back, n_sms, launches);
+  if (a.d <= 8192) return run<T, V, 32, 8>(st, a, back, n_sms, launches);
+  return run<T, V, 32, 32>(st, a, back, n_sms, launches);
+}
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+}  // namespace
+
+cudaError_t launch_norm(cudaStream_t st, const NormArgs& a, bool back, int is_bf16, int n_sms, int* launches) {
+  const int v = is_bf16 ? 8 : 4;               // entries in 16 bytes
+  const bool wide = a.d % v == 0 && a.ldx % v == 0 && a.ldr % v == 0 && a.ldy % v == 0 && aligned16(a.x) && aligned16(a.residual) &&
+                    aligned16(a.h) && aligned16(a.y) && aligned16(a.weight) && aligned16(a.bias) && aligned16(a.dy) && aligned16(a.dh) &&
+                    aligned16(a.dx);
+  if (is_bf16) return wide ? choose<__nv_bfloat16, 8>(st, a, back, n_sms, launches) : choose<__nv_bfloat16, 1>(st, a, back, n_sms, launches);
+  return wide ? choose<float, 4>(st, a, back, n_sms, launches) : choose<float, 1>(st, a, back, n_sms, launches);
+}
+
+}  // namespace muloco
