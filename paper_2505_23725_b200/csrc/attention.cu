@@ -271,7 +271,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       if (n_b) load_tile<DP>(smem_base + OPERAND, &maps.q, smem_u32(&bar_q), head, tile.start + tile.offset + TILE);
       Pipe at;
       for (int i = 0; i < 2 * n; ++i) {
-        if (!mbar_wait(smem_u32(&bar_empty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        if (!mbar_wait_cta(smem_u32(&bar_empty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
         const uint32_t bar = smem_u32(&bar_full[at.stage]);
         mbar_expect_tx(bar, OPERAND);
         load_tile<DP>(ring + at.stage * OPERAND, (i & 1) ? &maps.v : &maps.k, bar, kv_head, tile.start + (i >> 1) * TILE);
@@ -282,8 +282,8 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     // Order: scores of key tile 0 for both query tiles; then per key tile j and query tile: p v of j, scores of j + 1.  Products
     // of one thread complete in order, so scores of j + 1 may overwrite the p of j that the product before them reads.
     Pipe at;                                  // of the tile that is waited for next
-    auto arrived = [&]() { return mbar_wait(smem_u32(&bar_full[at.stage]), at.phase, &abort_flag, limit); };
-    bool alive = mbar_wait(smem_u32(&bar_q), 0, &abort_flag, limit) && arrived();
+    auto arrived = [&]() { return mbar_wait_cta(smem_u32(&bar_full[at.stage]), at.phase, &abort_flag, limit); };
+    bool alive = mbar_wait_cta(smem_u32(&bar_q), 0, &abort_flag, limit) && arrived();
     alive = __all_sync(0xffffffffu, alive);
     if (alive) {
       tc_fence_after();
@@ -313,7 +313,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         for (int t = 0; t < 2; ++t) {
           const int n_t = t ? n_b : n_a;
           if (j >= n_t) continue;
-          alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_p[t]), (uint32_t)j & 1u, &abort_flag, limit));
+          alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t]), (uint32_t)j & 1u, &abort_flag, limit));
           if (!alive) break;
           tc_fence_after();
           if (lane == 0) {
@@ -344,7 +344,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     float top = -INFINITY, total = 0.f;                        // largest score (unscaled) that the sums refer to; sum of weights
     bool alive = true;
     for (int j = 0; j < n_t; ++j) {
-      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_s[t]), (uint32_t)j & 1u, &abort_flag, limit));
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[t]), (uint32_t)j & 1u, &abort_flag, limit));
       if (!alive) break;
       tc_fence_after();
       uint32_t s[128];
@@ -398,10 +398,10 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       tm_store_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(smem_u32(&bar_p[t]));
+      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_p[t]));
     }
     if (alive && n_t) {
-      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_o[t]), 0, &abort_flag, limit));
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_o[t]), 0, &abort_flag, limit));
       if (alive) {
         tc_fence_after();
         const int pos = tile.offset + t * TILE + row;
@@ -476,10 +476,10 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
       load_tile<DP>(s_g, &maps.g, smem_u32(&bar_q), head, tile.start + tile.offset);
       Pipe at;
       for (int j = 0; j < n; ++j) {
-        if (!mbar_wait(smem_u32(&bar_kempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        if (!mbar_wait_cta(smem_u32(&bar_kempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
         mbar_expect_tx(smem_u32(&bar_kfull[at.stage]), OPERAND);
         load_tile<DP>(s_k + at.stage * OPERAND, &maps.k, smem_u32(&bar_kfull[at.stage]), kv_head, tile.start + j * TILE);
-        if (!mbar_wait(smem_u32(&bar_vempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        if (!mbar_wait_cta(smem_u32(&bar_vempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
         mbar_expect_tx(smem_u32(&bar_vfull[at.stage]), OPERAND);
         load_tile<DP>(s_v + at.stage * OPERAND, &maps.v, smem_u32(&bar_vfull[at.stage]), kv_head, tile.start + j * TILE);
         at.next<STAGES>();
@@ -490,11 +490,11 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
     // j + 1 may be complete before the row warps have looked for those of j: a barrier for each of the two places.)
     Pipe at;                                  // key tile j
     auto keys = [&](const Pipe& q, int j) {   // waits for key tile j and readies it
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_kfull[q.stage]), q.phase, &abort_flag, limit))) return false;
+      if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_kfull[q.stage]), q.phase, &abort_flag, limit))) return false;
       if (j == n - 1 && tail < TILE) zero_rows<DP>(s_k + q.stage * OPERAND, tail, lane);
       return true;
     };
-    bool alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_q), 0, &abort_flag, limit));
+    bool alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_q), 0, &abort_flag, limit));
     alive = alive && keys(at, 0);
     if (alive) {
       tc_fence_after();
@@ -504,7 +504,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
       }
       __syncwarp();
       for (int j = 0; j < n; ++j) {
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_vfull[at.stage]), at.phase, &abort_flag, limit))) break;
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_vfull[at.stage]), at.phase, &abort_flag, limit))) break;
         tc_fence_after();
         if (lane == 0) {
           scores<DP>(tm + TM_DP, s_g, s_v + at.stage * OPERAND);
@@ -523,7 +523,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
           }
           __syncwarp();
         }
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_ds), (uint32_t)j & 1u, &abort_flag, limit))) break;
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), (uint32_t)j & 1u, &abort_flag, limit))) break;
         tc_fence_after();
         if (lane == 0) {
           weigh<DP>(tm + TM_DQ, tm + (j & 1) * 128, HALF, s_k + at.stage * OPERAND, j > 0);
@@ -561,7 +561,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
     bool alive = true;
     for (int j = 0; j < n; ++j) {
       const uint32_t t_s = t_lane + (j & 1) * 128 + half * HALF;
-      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_s[j & 1]), (uint32_t)(j >> 1) & 1u, &abort_flag, limit));
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[j & 1]), (uint32_t)(j >> 1) & 1u, &abort_flag, limit));
       if (!alive) break;
       tc_fence_after();
       uint32_t s[64], d[64];
@@ -576,7 +576,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
         s[e] = __float_as_uint(exp2_approx(x.x));
         s[e + 1] = __float_as_uint(exp2_approx(x.y));
       }
-      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_dp), (uint32_t)j & 1u, &abort_flag, limit));
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), (uint32_t)j & 1u, &abort_flag, limit));
       if (!alive) break;
       tc_fence_after();
       tm_load32(t_lane + TM_DP + half * HALF, d);
@@ -604,10 +604,10 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
       tm_store_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(smem_u32(&bar_ds));
+      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_ds));
     }
     if (alive) {
-      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_done), 0, &abort_flag, limit));
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), 0, &abort_flag, limit));
       if (alive) {
         tc_fence_after();
         __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (token * p.heads + head) * p.dim;
@@ -671,10 +671,10 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       Pipe at;
       int head = kv_head * p.group, i = first;
       for (int it = 0; it < n; ++it) {
-        if (!mbar_wait(smem_u32(&bar_qempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        if (!mbar_wait_cta(smem_u32(&bar_qempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
         mbar_expect_tx(smem_u32(&bar_qfull[at.stage]), OPERAND);
         load_tile<DP>(s_q + at.stage * OPERAND, &maps.q, smem_u32(&bar_qfull[at.stage]), head, tile.start + i * TILE);
-        if (!mbar_wait(smem_u32(&bar_gempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
+        if (!mbar_wait_cta(smem_u32(&bar_gempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
         mbar_expect_tx(smem_u32(&bar_gfull[at.stage]), OPERAND);
         load_tile<DP>(s_g + at.stage * OPERAND, &maps.g, smem_u32(&bar_gfull[at.stage]), head, tile.start + i * TILE);
         at.next<STAGES>();
@@ -686,11 +686,11 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     Pipe at;
     int i = first;                            // query tile of the step
     auto queries = [&](const Pipe& q, int i) {
-      if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_qfull[q.stage]), q.phase, &abort_flag, limit))) return false;
+      if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_qfull[q.stage]), q.phase, &abort_flag, limit))) return false;
       if (i == end - 1 && tail < TILE) zero_rows<DP>(s_q + q.stage * OPERAND, tail, lane);
       return true;
     };
-    bool alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_kv), 0, &abort_flag, limit));
+    bool alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_kv), 0, &abort_flag, limit));
     alive = alive && queries(at, i);
     if (alive) {
       tc_fence_after();
@@ -700,7 +700,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       }
       __syncwarp();
       for (int it = 0; it < n; ++it) {
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_gfull[at.stage]), at.phase, &abort_flag, limit))) break;
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_gfull[at.stage]), at.phase, &abort_flag, limit))) break;
         if (i == end - 1 && tail < TILE) zero_rows<DP>(s_g + at.stage * OPERAND, tail, lane);
         tc_fence_after();
         if (lane == 0) {
@@ -708,7 +708,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
           tc_commit<1>(smem_u32(&bar_dp));
         }
         __syncwarp();
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_p), (uint32_t)it & 1u, &abort_flag, limit))) break;
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p), (uint32_t)it & 1u, &abort_flag, limit))) break;
         tc_fence_after();
         if (lane == 0) {
           weigh<DP>(tm + TM_DV, tm, HALF, s_g + at.stage * OPERAND, it > 0);
@@ -727,7 +727,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
           }
           __syncwarp();
         }
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_ds), (uint32_t)it & 1u, &abort_flag, limit))) break;
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), (uint32_t)it & 1u, &abort_flag, limit))) break;
         tc_fence_after();
         if (lane == 0) {
           weigh<DP>(tm + TM_DK, tm + TM_DP, HALF, s_q + at.stage * OPERAND, it > 0);
@@ -774,7 +774,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       __syncwarp();
       if (++i == end) { i = first; ++head; }
       if (it + 1 < n) fetch();
-      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_s), (uint32_t)it & 1u, &abort_flag, limit));
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s), (uint32_t)it & 1u, &abort_flag, limit));
       if (!alive) break;
       uint32_t s[64], w[32];
       tc_fence_after();
@@ -803,8 +803,8 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       tm_store_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(smem_u32(&bar_p));
-      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_dp), (uint32_t)it & 1u, &abort_flag, limit));
+      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_p));
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), (uint32_t)it & 1u, &abort_flag, limit));
       if (!alive) break;
       tc_fence_after();
       uint32_t d[64];
@@ -833,10 +833,10 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       tm_store_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(smem_u32(&bar_ds));
+      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_ds));
     }
     if (alive) {
-      alive = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_done), 0, &abort_flag, limit));
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), 0, &abort_flag, limit));
       if (alive) {
         tc_fence_after();
         const int pos = tile.offset + row;
