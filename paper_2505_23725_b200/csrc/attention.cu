@@ -29,11 +29,16 @@ namespace muloco {
 namespace {
 
 constexpr int TILE = 128;                     // tokens per tile
-constexpr int ATTN_THREADS = 320;             // eight warps for the rows, one for copies, one for products
+constexpr int ATTN_THREADS = 320;             // backward: eight warps for the rows, one for copies, one for products
+constexpr int FWD_THREADS = 576;              // forward: sixteen for the rows
 constexpr int COPY_WARP = 8, MMA_WARP = 9;
 constexpr uint32_t SLAB = TILE * 128;         // 128 rows of 64 bf16, swizzled
+// The two halves of a tile's columns belong to different row warps; each writes its bf16 operand at the start of its own 64 columns, so
+// neither overwrites scores that the other has yet to read.
+constexpr uint32_t HALF = 64;
 constexpr float LN2 = 0.6931471805599453f, LOG2_E = 1.4426950408889634f;
-constexpr float MOVE = 8.0f;                  // growth of a row's maximum (in powers of two) that makes it move
+constexpr int POLY_OF = 4;                    // forward: one in so many pairs of exponentials by polynomial
+constexpr float MOST = 65536.0f;              // sum of 64 weights that makes a row's reference move
 
 struct Maps4 { CUtensorMap q, k, v, g; };     // g: do
 
@@ -90,18 +95,49 @@ __device__ __forceinline__ void after_load(uint32_t* v) {
                  "+r"(v[30]), "+r"(v[31]));
 }
 
-// D (tensor memory) = or += A B^T, A and B in shared memory
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  tc_mma_bf16<1>(d, a, b, idesc, accumulate);
-}
-// ... with A (bf16, two to a column) in tensor memory
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// The products' warp runs as one: every lane goes through the same code and the instructions themselves are carried out by the lane that
+// `leader` is 1 in.  In code that only one lane enters, the descriptors are moved to the warp's registers one by one:
+// 86 cycles a product where the tensor cores need 32 to 64.
+__device__ __forceinline__ uint32_t elect_leader() {
+  uint32_t leader;
   asm volatile(
       "{\n"
       ".reg .pred p;\n"
+      "elect.sync _|p, 0xffffffff;\n"
+      "selp.u32 %0, 1, 0, p;\n"
+      "}\n"
+      : "=r"(leader));
+  return leader;
+}
+// D (tensor memory) = or += A B^T, A and B in shared memory
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
       "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
-      "}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "setp.ne.b32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+      "}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader)
+      : "memory");
+}
+// ... with A (bf16, two to a column) in tensor memory
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "setp.ne.b32 q, %5, 0;\n"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+      "}\n" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t leader, uint32_t bar) {
+  asm volatile(
+      "{\n"
+      ".reg .pred q;\n"
+      "setp.ne.b32 q, %1, 0;\n"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n"
+      "}\n" ::"r"(bar), "r"(leader)
       : "memory");
 }
 
@@ -117,20 +153,25 @@ __host__ __device__ constexpr uint32_t idesc_mn(int n) { return idesc_k(n) | (1u
 
 // d[128][128] = a b^T over DP entries
 template <int DP>
-__device__ __forceinline__ void scores(uint32_t d, uint32_t a, uint32_t b) {
+__device__ __forceinline__ void scores(uint32_t leader, uint32_t d, uint32_t a, uint32_t b) {
 #pragma unroll
   for (int k = 0; k < DP / 16; ++k) {
     const uint32_t off = (uint32_t)(k >> 2) * (SLAB >> 4) + (uint32_t)(k & 3) * 2u;
-    mma_ss(d, desc(((a >> 4) | LBO_K) + off), desc(((b >> 4) | LBO_K) + off), idesc_k(TILE), k > 0);
+    mma_ss(leader, d, desc(((a >> 4) | LBO_K) + off), desc(((b >> 4) | LBO_K) + off), idesc_k(TILE), k > 0);
   }
 }
-// d[128][DP] += p b over the 128 rows of b; the second half of p's columns starts `half` columns after the first
+// d[128][DP] += p b over rows 64 h .. 64 h + 63 of b; p: those 64 columns of the left operand
 template <int DP>
-__device__ __forceinline__ void weigh(uint32_t d, uint32_t p, uint32_t half, uint32_t b, bool accumulate) {
+__device__ __forceinline__ void weigh_half(uint32_t leader, uint32_t d, uint32_t p, uint32_t b, int h, bool accumulate) {
 #pragma unroll
-  for (int k = 0; k < TILE / 16; ++k)
-    mma_ts(d, p + (uint32_t)(k >> 2) * half + (uint32_t)(k & 3) * 8u, desc(((b >> 4) | LBO_MN) + (uint32_t)k * 128u),
-           idesc_mn(DP), accumulate || k > 0);
+  for (int k = 0; k < 4; ++k)
+    mma_ts(leader, d, p + (uint32_t)k * 8u, desc(((b >> 4) | LBO_MN) + (uint32_t)(4 * h + k) * 128u), idesc_mn(DP), accumulate || k > 0);
+}
+// ... over its 128 rows; the second half of p's columns starts `half` columns after the first
+template <int DP>
+__device__ __forceinline__ void weigh(uint32_t leader, uint32_t d, uint32_t p, uint32_t half, uint32_t b, bool accumulate) {
+  weigh_half<DP>(leader, d, p, b, 0, accumulate);
+  weigh_half<DP>(leader, d, p + half, b, 1, true);
 }
 
 // Rows `first` .. 127 of an operand become zero (one warp); the products that follow see it.
@@ -160,6 +201,46 @@ __device__ __forceinline__ float log2_approx(float x) {
   float y;
   asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// 2^x on the floating-point pipes instead of the special-function unit, which gives 16 results a cycle where a tile's products leave time for
+// 8 to 16: x = n + f with n the nearest integer, 2^f by the polynomial of degree 5 with the least largest relative error on
+// [-1/2, 1/2] (Remez exchange: 1.6e-7 with the coefficients in float32), n added to the exponent.  Below 2^-127 it gives
+// less than 2^-148, which is 0 in bf16; NaN does not pass.
+__device__ __forceinline__ float2 exp2_pair(Pair x) {
+  const float2 q = parts(x);
+  const Pair y = pair(fmaxf(q.x, -127.0f), fmaxf(q.y, -127.0f));
+  const Pair t = add2(y, both(12582912.0f));                     // 1.5 2^23: the integer ends up in the low bits
+  const Pair f = add2(y, mul2(add2(t, both(-12582912.0f)), both(-1.0f)));
+  Pair p = fma2(f, both(0.00132764725f), both(0.00967554096f));
+  p = fma2(p, f, both(0.0555071309f));
+  p = fma2(p, f, both(0.240221202f));
+  p = fma2(p, f, both(0.693146944f));
+  p = fma2(p, f, both(1.00000012f));
+  const float2 v = parts(p), n = parts(t);
+  return make_float2(__int_as_float(__float_as_int(v.x) + (__float_as_int(n.x) << 23)),
+                     __int_as_float(__float_as_int(v.y) + (__float_as_int(n.y) << 23)));
+}
+// Whether any thread of the two warps that share a tile's rows says so (barrier `id`; both take the same turns).
+__device__ __forceinline__ bool either(int id, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.b32 p, %1, 0;\n"
+      "barrier.cta.red.or.pred q, %2, 64, p;\n"
+      "selp.u32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(r)
+      : "r"((uint32_t)x), "r"(id)
+      : "memory");
+  return r != 0;
+}
+// The largest of three; NaN if one is.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 
 // Accumulator columns [c0, c0 + n) of this thread's row, times `by`, as bf16 to columns c0 .. of `row` (first `dim` columns exist).
@@ -227,15 +308,17 @@ struct FwdShape {
 };
 
 template <int DP>
-__global__ void __launch_bounds__(ATTN_THREADS, 1)
+__global__ void __launch_bounds__(FWD_THREADS, 1)
 attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnParams p) {
   using Sh = FwdShape<DP>;
+  constexpr int COPY_WARP = 16, MMA_WARP = 17;
   constexpr int STAGES = Sh::STAGES;
   constexpr uint32_t OPERAND = Sh::OPERAND;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_q, bar_full[STAGES], bar_empty[STAGES], bar_s[2], bar_p[2], bar_o[2];
+  __shared__ __align__(8) uint64_t bar_q, bar_full[STAGES], bar_empty[STAGES], bar_s[2], bar_p[2][2], bar_o[2];
   __shared__ uint32_t tmem_base_slot;
   __shared__ volatile int abort_flag;
+  __shared__ float row_share[2][2][TILE];       // what the two warps of a row tell one another: largest score, sum of weights
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -249,7 +332,8 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     }
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&bar_s[t]), 1);
-      mbar_init(smem_u32(&bar_p[t]), 4);
+      mbar_init(smem_u32(&bar_p[t][0]), 4);
+      mbar_init(smem_u32(&bar_p[t][1]), 4);
       mbar_init(smem_u32(&bar_o[t]), 1);
     }
   };
@@ -264,7 +348,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   const int n = n_b ? n_b : n_a;
   const int tail = tile.length - (n - 1) * TILE;               // rows of the last key tile that exist, when below 128
 
-  if (warp == COPY_WARP) {
+    if (warp == COPY_WARP) {
     if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
       mbar_expect_tx(smem_u32(&bar_q), (n_b ? 2u : 1u) * OPERAND);
       load_tile<DP>(smem_base, &maps.q, smem_u32(&bar_q), head, tile.start + tile.offset);
@@ -279,6 +363,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       }
     }
   } else if (warp == MMA_WARP) {
+    const uint32_t leader = elect_leader();
     // Order: scores of key tile 0 for both query tiles; then per key tile j and query tile: p v of j, scores of j + 1.  Products
     // of one thread complete in order, so scores of j + 1 may overwrite the p of j that the product before them reads.
     Pipe at;                                  // of the tile that is waited for next
@@ -289,14 +374,12 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       tc_fence_after();
       uint32_t k_stage = at.stage;
       at.next<STAGES>();
-      if (lane == 0) {
-        for (int t = 0; t < 2; ++t) {
-          if (t == 1 && !n_b) break;
-          scores<DP>(tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
-          tc_commit<1>(smem_u32(&bar_s[t]));
-        }
-        tc_commit<1>(smem_u32(&bar_empty[k_stage]));
+      for (int t = 0; t < 2; ++t) {
+        if (t == 1 && !n_b) break;
+        scores<DP>(leader, tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
+        mma_commit(leader, smem_u32(&bar_s[t]));
       }
+      mma_commit(leader, smem_u32(&bar_empty[k_stage]));
       __syncwarp();
       for (int j = 0; alive && j < n; ++j) {
         alive = __all_sync(0xffffffffu, arrived());
@@ -313,63 +396,70 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         for (int t = 0; t < 2; ++t) {
           const int n_t = t ? n_b : n_a;
           if (j >= n_t) continue;
-          alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t]), (uint32_t)j & 1u, &abort_flag, limit));
+          for (int h = 0; alive && h < 2; ++h) {
+            alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t][h]), (uint32_t)j & 1u, &abort_flag, limit));
+            if (!alive) break;
+            tc_fence_after();
+            weigh_half<DP>(leader, tm + TM_O + t * DP, tm + t * 128 + h * HALF, ring + v_stage * OPERAND, h, j > 0 || h > 0);
+          }
           if (!alive) break;
-          tc_fence_after();
-          if (lane == 0) {
-            weigh<DP>(tm + TM_O + t * DP, tm + t * 128, 32, ring + v_stage * OPERAND, j > 0);
-            if (j + 1 < n_t) {
-              scores<DP>(tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
-              tc_commit<1>(smem_u32(&bar_s[t]));
-            } else {
-              tc_commit<1>(smem_u32(&bar_o[t]));
-            }
+          if (j + 1 < n_t) {
+            scores<DP>(leader, tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
+            mma_commit(leader, smem_u32(&bar_s[t]));
+          } else {
+            mma_commit(leader, smem_u32(&bar_o[t]));
           }
           __syncwarp();
         }
-        if (alive && lane == 0) {
-          tc_commit<1>(smem_u32(&bar_empty[v_stage]));
-          if (j + 1 < n) tc_commit<1>(smem_u32(&bar_empty[k_stage]));
+        if (alive) {
+          mma_commit(leader, smem_u32(&bar_empty[v_stage]));
+          if (j + 1 < n) mma_commit(leader, smem_u32(&bar_empty[k_stage]));
         }
         __syncwarp();
       }
     }
   } else {
-    const int t = warp >> 2, quarter = warp & 3;
+    // A row belongs to two threads, each with half of its columns: warps 0-3 and 4-7 (first tile), 8-11 and 12-15 (second).
+    const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;
     const int row = quarter * 32 + lane;                       // of the tile; key columns up to `row` of the last key tile count
     const int n_t = t ? n_b : n_a;
+    const int col0 = half * 64, pair_id = 1 + t * 4 + quarter;
     const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t t_s = t_lane + t * 128, t_o = t_lane + TM_O + t * DP;
+    const uint32_t t_s = t_lane + t * 128 + half * HALF, t_o = t_lane + TM_O + t * DP + half * (DP / 2);
     const float c = p.scale * LOG2_E;
-    float top = -INFINITY, total = 0.f;                        // largest score (unscaled) that the sums refer to; sum of weights
-    bool alive = true;
-    for (int j = 0; j < n_t; ++j) {
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[t]), (uint32_t)j & 1u, &abort_flag, limit));
-      if (!alive) break;
-      tc_fence_after();
-      uint32_t s[128];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) tm_load32(t_s + i * 32, s + i * 32);
+    const Pair c2 = both(c);
+    float* const mine = &row_share[t][half][row];
+    const float* const other = &row_share[t][half ^ 1][row];
+    float top = 0.f, total = 0.f;                              // score that the weights refer to (the row's, unscaled); sum of the weights
+    Pair shift = both(0.f);
+    // 32 of this thread's 64 scores
+    auto load_scores = [&](uint32_t (&s)[32], int h, bool last) {
+      tm_load32(t_s + h * 32, s);
       tm_load_wait();
+      after_load(s);
+      if (last) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) after_load(s + i * 32);
-      if (j == n_t - 1) {
-#pragma unroll
-        for (int e = 0; e < 128; ++e) s[e] = e > row ? 0xff800000u : s[e];
+        for (int e = 0; e < 32; ++e) s[e] = col0 + h * 32 + e > row ? 0xff800000u : s[e];
       }
-      float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+    };
+    // The reference becomes the row's largest score so far; sums and weighted values so far (`some`: there are some) follow.
+    auto move_reference = [&](bool some, bool last) {
+      float m = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < 128; ++e) m4[e & 3] = fmaxf(m4[e & 3], __uint_as_float(s[e]));
-      const float m = fmaxf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), top);
-      if (j == 0) {
-        top = m;
-      } else if (__any_sync(0xffffffffu, (m - top) * c > MOVE)) {
-        // the scores of j are there, so the product of j - 1 before them is complete
+      for (int h = 0; h < 2; ++h) {
+        uint32_t s[32];
+        load_scores(s, h, last);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) m = max3(m, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+      }
+      *mine = m;
+      either(pair_id, false);
+      m = max3(m, *other, some ? top : m);
+      if (some) {                             // (the product before these scores is complete, as they are)
         const float by = exp2_approx((top - m) * c);
         total *= by;
-        top = m;
 #pragma unroll 1
-        for (int i = 0; i < DP; i += 32) {
+        for (int i = 0; i < DP / 2; i += 32) {
           uint32_t v[32];
           tm_load32(t_o + i, v);
           tm_load_wait();
@@ -379,38 +469,68 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
           tm_store32(t_o + i, v);
         }
       }
-      const Pair c2 = both(c), shift = both(-top * c);
+      top = m;
+      // (an infinite maximum makes every weight NaN, as the quotient of infinities is)
+      shift = both((top - top) - top * c);
+    };
+    auto weights = [&](uint32_t (&w)[32], bool last) {
       Pair sum[2] = {both(0.f), both(0.f)};
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        uint32_t w[32];
+        uint32_t s[32];
+        load_scores(s, h, last);
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-          const float2 x = parts(fma2(pair(__uint_as_float(s[h * 64 + 2 * e]), __uint_as_float(s[h * 64 + 2 * e + 1])), c2, shift));
-          const float a = exp2_approx(x.x), b = exp2_approx(x.y);
-          sum[e & 1] = add2(sum[e & 1], pair(a, b));
-          w[e] = pack_bf16x2(a, b);
+        for (int e = 0; e < 32; e += 2) {
+          const Pair x = fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, shift);
+          float2 y;
+          if ((e >> 1) % POLY_OF == POLY_OF - 1) {
+            y = exp2_pair(x);
+          } else {
+            y = parts(x);
+            y.x = exp2_approx(y.x);
+            y.y = exp2_approx(y.y);
+          }
+          sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pair(y.x, y.y));
+          w[h * 16 + (e >> 1)] = pack_bf16x2(y.x, y.y);
         }
-        tm_store32(t_s + h * 32, w);
       }
-      const float2 both_sums = parts(add2(sum[0], sum[1]));
-      total += both_sums.x + both_sums.y;
+      const float2 sums = parts(add2(sum[0], sum[1]));
+      return sums.x + sums.y;
+    };
+    bool alive = true;
+    for (int j = 0; j < n_t; ++j) {
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[t]), (uint32_t)j & 1u, &abort_flag, limit));
+      tc_fence_after();
+      const bool last = j == n_t - 1;
+      uint32_t w[32];
+      if (j == 0) move_reference(false, last);
+      float part = weights(w, last);
+      // Where the weights are too large by the reference as it was, or not numbers: once more by a new one.
+      if (either(pair_id, !alive || (j > 0 && !(part <= MOST)))) {
+        if (either(pair_id, !alive)) { alive = false; break; }
+        move_reference(true, last);
+        part = weights(w, last);
+      }
+      total += part;
+      tm_store32(t_s, w);
       tm_store_wait();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_p[t]));
+      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_p[t][half]));
     }
-    if (alive && n_t) {
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_o[t]), 0, &abort_flag, limit));
-      if (alive) {
+    if (n_t) {
+      if (alive) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_o[t]), 0, &abort_flag, limit));
+      *mine = total;
+      if (!either(pair_id, !alive)) {
         tc_fence_after();
+        total += *other;
         const int pos = tile.offset + t * TILE + row;
         const bool ok = pos < tile.length;
         const int64_t token = (int64_t)tile.start + pos;
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + ((ok ? token : 0) * p.heads + head) * p.dim;
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + ((ok ? token : 0) * p.heads + head) * p.dim + half * (DP / 2);
         const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
-        store_columns(t_o, out, 0, DP, p.dim, 1.0f / total, ok, wide);
-        if (ok) p.lse[(int64_t)head * p.tokens + token] = (top * c + log2_approx(total)) * LN2;
+        store_columns(t_o, out, 0, DP / 2, p.dim - half * (DP / 2), 1.0f / total, ok, wide);
+        if (ok && half == 0) p.lse[(int64_t)head * p.tokens + token] = (top * c + log2_approx(total)) * LN2;
       }
     }
   }
@@ -426,10 +546,6 @@ struct BackShape {
   static constexpr int STAGES = 2;
   static constexpr uint32_t SMEM = (2 + 2 * STAGES) * OPERAND + 1024u;
 };
-
-// The two halves of a tile's columns belong to the first and the last four row warps; each writes its bf16 operand at the
-// start of its own 64 columns, so neither overwrites scores that the other has yet to read.
-constexpr uint32_t HALF = 64;
 
 template <int DP>
 __global__ void __launch_bounds__(ATTN_THREADS, 1)
@@ -486,6 +602,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
       }
     }
   } else if (warp == MMA_WARP) {
+    const uint32_t leader = elect_leader();
     // Order: scores of 0; then per key tile j: dp of j, scores of j + 1 (into the other columns), dq += ds k of j.  (The scores of
     // j + 1 may be complete before the row warps have looked for those of j: a barrier for each of the two places.)
     Pipe at;                                  // key tile j
@@ -498,42 +615,34 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
     alive = alive && keys(at, 0);
     if (alive) {
       tc_fence_after();
-      if (lane == 0) {
-        scores<DP>(tm, s_q, s_k);
-        tc_commit<1>(smem_u32(&bar_s[0]));
-      }
+      scores<DP>(leader, tm, s_q, s_k);
+      mma_commit(leader, smem_u32(&bar_s[0]));
       __syncwarp();
       for (int j = 0; j < n; ++j) {
         if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_vfull[at.stage]), at.phase, &abort_flag, limit))) break;
         tc_fence_after();
-        if (lane == 0) {
-          scores<DP>(tm + TM_DP, s_g, s_v + at.stage * OPERAND);
-          tc_commit<1>(smem_u32(&bar_dp));
-          tc_commit<1>(smem_u32(&bar_vempty[at.stage]));
-        }
+        scores<DP>(leader, tm + TM_DP, s_g, s_v + at.stage * OPERAND);
+        mma_commit(leader, smem_u32(&bar_dp));
+        mma_commit(leader, smem_u32(&bar_vempty[at.stage]));
         __syncwarp();
         Pipe ahead = at;
         ahead.next<STAGES>();
         if (j + 1 < n) {
           if (!keys(ahead, j + 1)) break;
           tc_fence_after();
-          if (lane == 0) {
-            scores<DP>(tm + ((j + 1) & 1) * 128, s_q, s_k + ahead.stage * OPERAND);
-            tc_commit<1>(smem_u32(&bar_s[(j + 1) & 1]));
-          }
+          scores<DP>(leader, tm + ((j + 1) & 1) * 128, s_q, s_k + ahead.stage * OPERAND);
+          mma_commit(leader, smem_u32(&bar_s[(j + 1) & 1]));
           __syncwarp();
         }
         if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), (uint32_t)j & 1u, &abort_flag, limit))) break;
         tc_fence_after();
-        if (lane == 0) {
-          weigh<DP>(tm + TM_DQ, tm + (j & 1) * 128, HALF, s_k + at.stage * OPERAND, j > 0);
-          tc_commit<1>(j + 1 < n ? smem_u32(&bar_kempty[at.stage]) : smem_u32(&bar_done));
-        }
+        weigh<DP>(leader, tm + TM_DQ, tm + (j & 1) * 128, HALF, s_k + at.stage * OPERAND, j > 0);
+        mma_commit(leader, j + 1 < n ? smem_u32(&bar_kempty[at.stage]) : smem_u32(&bar_done));
         __syncwarp();
         at = ahead;
       }
     }
-  } else {
+  } else if (warp < COPY_WARP) {
     const int half = warp >> 2, quarter = warp & 3;
     const int row = quarter * 32 + lane;
     const int pos = tile.offset + row;
@@ -682,6 +791,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       }
     }
   } else if (warp == MMA_WARP) {
+    const uint32_t leader = elect_leader();
     // Order: scores of 0; then per step: dp, dv += p do, scores of the next, dk += ds q.
     Pipe at;
     int i = first;                            // query tile of the step
@@ -694,26 +804,20 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     alive = alive && queries(at, i);
     if (alive) {
       tc_fence_after();
-      if (lane == 0) {
-        scores<DP>(tm, s_k, s_q);
-        tc_commit<1>(smem_u32(&bar_s));
-      }
+      scores<DP>(leader, tm, s_k, s_q);
+      mma_commit(leader, smem_u32(&bar_s));
       __syncwarp();
       for (int it = 0; it < n; ++it) {
         if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_gfull[at.stage]), at.phase, &abort_flag, limit))) break;
         if (i == end - 1 && tail < TILE) zero_rows<DP>(s_g + at.stage * OPERAND, tail, lane);
         tc_fence_after();
-        if (lane == 0) {
-          scores<DP>(tm + TM_DP, s_v, s_g + at.stage * OPERAND);
-          tc_commit<1>(smem_u32(&bar_dp));
-        }
+        scores<DP>(leader, tm + TM_DP, s_v, s_g + at.stage * OPERAND);
+        mma_commit(leader, smem_u32(&bar_dp));
         __syncwarp();
         if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p), (uint32_t)it & 1u, &abort_flag, limit))) break;
         tc_fence_after();
-        if (lane == 0) {
-          weigh<DP>(tm + TM_DV, tm, HALF, s_g + at.stage * OPERAND, it > 0);
-          tc_commit<1>(smem_u32(&bar_gempty[at.stage]));
-        }
+        weigh<DP>(leader, tm + TM_DV, tm, HALF, s_g + at.stage * OPERAND, it > 0);
+        mma_commit(leader, smem_u32(&bar_gempty[at.stage]));
         __syncwarp();
         Pipe ahead = at;
         ahead.next<STAGES>();
@@ -721,24 +825,20 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         if (it + 1 < n) {
           if (!queries(ahead, i_next)) break;
           tc_fence_after();
-          if (lane == 0) {
-            scores<DP>(tm, s_k, s_q + ahead.stage * OPERAND);
-            tc_commit<1>(smem_u32(&bar_s));
-          }
+          scores<DP>(leader, tm, s_k, s_q + ahead.stage * OPERAND);
+          mma_commit(leader, smem_u32(&bar_s));
           __syncwarp();
         }
         if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), (uint32_t)it & 1u, &abort_flag, limit))) break;
         tc_fence_after();
-        if (lane == 0) {
-          weigh<DP>(tm + TM_DK, tm + TM_DP, HALF, s_q + at.stage * OPERAND, it > 0);
-          tc_commit<1>(it + 1 < n ? smem_u32(&bar_qempty[at.stage]) : smem_u32(&bar_done));
-        }
+        weigh<DP>(leader, tm + TM_DK, tm + TM_DP, HALF, s_q + at.stage * OPERAND, it > 0);
+        mma_commit(leader, it + 1 < n ? smem_u32(&bar_qempty[at.stage]) : smem_u32(&bar_done));
         __syncwarp();
         at = ahead;
         i = i_next;
       }
     }
-  } else {
+  } else if (warp < COPY_WARP) {
     const int half = warp >> 2, quarter = warp & 3;
     const int row = quarter * 32 + lane;                       // key of the tile
     const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
@@ -871,7 +971,7 @@ cudaError_t run_forward(cudaStream_t st, const Maps4& m, const AttnParams& p, in
   static std::atomic<uint64_t> allowed{0};
   const cudaError_t e = allow_smem(attn_fwd_kernel<DP>, (int)FwdShape<DP>::SMEM, &allowed);
   if (e != cudaSuccess) return e;
-  return launch_dependent(attn_fwd_kernel<DP>, (unsigned)units, ATTN_THREADS, FwdShape<DP>::SMEM, st, m, p);
+  return launch_dependent(attn_fwd_kernel<DP>, (unsigned)units, FWD_THREADS, FwdShape<DP>::SMEM, st, m, p);
 }
 
 template <int DP>
