@@ -31,19 +31,20 @@ namespace {
 constexpr int TILE = 128;                     // tokens per tile
 constexpr int ATTN_THREADS = 320;             // backward: eight warps for the rows, one for copies, one for products
 constexpr int FWD_THREADS = 576;              // forward: sixteen for the rows
-constexpr int COPY_WARP = 8, MMA_WARP = 9;
 constexpr uint32_t SLAB = TILE * 128;         // 128 rows of 64 bf16, swizzled
 // The two halves of a tile's columns belong to different row warps; each writes its bf16 operand at the start of its own 64 columns, so
 // neither overwrites scores that the other has yet to read.
 constexpr uint32_t HALF = 64;
+constexpr int64_t SECTION_BYTES = 32 << 20;   // of L2's 126 MB: what a section's units read again and again
 constexpr float LN2 = 0.6931471805599453f, LOG2_E = 1.4426950408889634f;
-constexpr int POLY_OF = 4;                    // forward: one in so many pairs of exponentials by polynomial
+constexpr int POLY_OF = 100;                    // forward: one in so many pairs of exponentials by polynomial
 constexpr float MOST = 65536.0f;              // sum of 64 weights that makes a row's reference move
 
 struct Maps4 { CUtensorMap q, k, v, g; };     // g: do
 
 struct AttnParams {
   const AttnTile* tiles;
+  int n_tiles, section;                       // section: heads whose units come together (query heads, or key heads for dk and dv)
   int64_t tokens;
   int heads, group;                           // query heads; of them per key head
   int dim;
@@ -261,6 +262,62 @@ __device__ __forceinline__ void store_columns(uint32_t t_row, __nv_bfloat16* row
   }
 }
 
+// Units of work: a tile (forward: a pair of tiles) and a head.  The grid has a block per unit; a block that is done with its own
+// takes over one that has not started yet (cluster launch control), so units start in the order of the grid as multiprocessors become free, and
+// copies and scores of the next unit run beside the end of this one.  The order: heads in sections whose keys and
+// values fit into L2 together, the tiles of a section heaviest first.
+struct Unit { AttnTile tile; int head; };
+__device__ __forceinline__ Unit unit_of(const AttnParams& p, int heads, int u) {
+  const int per = p.n_tiles * p.section, s = u / per, r = u - s * per;
+  const int left = heads - s * p.section, width = left < p.section ? left : p.section;
+  Unit x;
+  x.tile = p.tiles[r / width];
+  x.head = s * p.section + r % width;
+  return x;
+}
+
+// The next unit, asked for by the copying thread and read by every warp, through two places in turn.
+struct Next {
+  uint32_t full, empty, answer;               // barriers (8 bytes a place), answers (16)
+  uint32_t turn = 0;
+  __device__ __forceinline__ uint32_t place() const { return turn & 1u; }
+  __device__ __forceinline__ uint32_t parity() const { return (turn >> 1) & 1u; }
+};
+__device__ __forceinline__ bool ask(const Next& n, volatile int* abort_flag, uint64_t limit) {
+  if (!mbar_wait_cta(n.empty + n.place() * 8u, n.parity() ^ 1u, abort_flag, limit)) return false;
+  const uint32_t bar = n.full + n.place() * 8u;
+  mbar_expect_tx(bar, 16);
+  asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(n.answer + n.place() * 16u),
+               "r"(bar)
+               : "memory");
+  return true;
+}
+// A warp's (or the copying thread's) next unit: -1 when there is none, or the block is giving up.
+template <bool WARP>
+__device__ __forceinline__ int take(Next& n, volatile int* abort_flag, uint64_t limit) {
+  bool ok = mbar_wait_cta(n.full + n.place() * 8u, n.parity(), abort_flag, limit);
+  if (WARP) ok = __all_sync(0xffffffffu, ok);
+  if (!ok) return -1;
+  int u;
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      ".reg .b128 a;\n"
+      "ld.shared.b128 a, [%1];\n"
+      "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, a;\n"
+      "mov.b32 %0, -1;\n"
+      "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, a;\n"
+      "}\n"
+      : "=r"(u)
+      : "r"(n.answer + n.place() * 16u)
+      : "memory");
+  fence_async_smem();                         // the next answer to this place comes behind these reads
+  if (WARP) __syncwarp();
+  if (!WARP || (threadIdx.x & 31) == 0) mbar_arrive_cta(n.empty + n.place() * 8u);
+  ++n.turn;
+  return u;
+}
+
 struct Pipe {                                 // position in a ring of N stages
   uint32_t stage = 0, phase = 0;
   template <int N> __device__ __forceinline__ void next() { if (++stage == (uint32_t)N) { stage = 0; phase ^= 1u; } }
@@ -271,6 +328,10 @@ struct Pipe {                                 // position in a ring of N stages
   if (threadIdx.x == 0) {                                                                    \
     abort_flag = 0;                                                                          \
     init_barriers();                                                                         \
+    for (int i = 0; i < 2; ++i) {                                                            \
+      mbar_init(smem_u32(&bar_next[i]), 1);                                                  \
+      mbar_init(smem_u32(&bar_taken[i]), 2 + ROW_WARPS);                                     \
+    }                                                                                        \
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");                       \
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");                             \
   }                                                                                          \
@@ -280,7 +341,8 @@ struct Pipe {                                 // position in a ring of N stages
   tc_fence_after();                                                                          \
   const uint32_t tm = tmem_base_slot;                                                        \
   grid_wait();                                                                               \
-  grid_release();
+  grid_release();                                                                            \
+  Next next{smem_u32(&bar_next[0]), smem_u32(&bar_taken[0]), smem_u32(&next_answer[0])};
 
 #define ATTN_END(cols)                                                                       \
   __syncwarp();                                                                              \
@@ -311,14 +373,17 @@ template <int DP>
 __global__ void __launch_bounds__(FWD_THREADS, 1)
 attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnParams p) {
   using Sh = FwdShape<DP>;
-  constexpr int COPY_WARP = 16, MMA_WARP = 17;
+  constexpr int ROW_WARPS = 16, COPY_WARP = 16, MMA_WARP = 17;
   constexpr int STAGES = Sh::STAGES;
   constexpr uint32_t OPERAND = Sh::OPERAND;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_q, bar_full[STAGES], bar_empty[STAGES], bar_s[2], bar_p[2][2], bar_o[2];
+  __shared__ __align__(8) uint64_t bar_q, bar_qempty, bar_full[STAGES], bar_empty[STAGES], bar_s[2], bar_p[2][2], bar_o[2];
+  __shared__ __align__(16) uint4 next_answer[2];
+  __shared__ __align__(8) uint64_t bar_next[2], bar_taken[2];
   __shared__ uint32_t tmem_base_slot;
   __shared__ volatile int abort_flag;
-  __shared__ float row_share[2][2][TILE];       // what the two warps of a row tell one another: largest score, sum of weights
+  // what the two threads of a row tell one another (places of their own: the barriers between two uses of a place are those of a step)
+  __shared__ float row_largest[2][2][TILE], row_total[2][2][TILE];
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -326,6 +391,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   const uint64_t limit = p.wait_limit_ns;
   auto init_barriers = [&] {
     mbar_init(smem_u32(&bar_q), 1);
+    mbar_init(smem_u32(&bar_qempty), 1);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(&bar_full[s]), 1);
       mbar_init(smem_u32(&bar_empty[s]), 1);
@@ -340,26 +406,45 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   ATTN_BEGIN(512)
   constexpr uint32_t TM_O = 256;              // columns: scores of the two tiles, their sums
 
-  const AttnTile tile = p.tiles[blockIdx.x / p.heads];
-  const int head = blockIdx.x % p.heads, kv_head = head / p.group;
-  // key tiles of the two query tiles (the second may be past the end of the sequence)
-  const int first = tile.offset / TILE;
-  const int n_a = first + 1, n_b = tile.offset + TILE < tile.length ? first + 2 : 0;
-  const int n = n_b ? n_b : n_a;
-  const int tail = tile.length - (n - 1) * TILE;               // rows of the last key tile that exist, when below 128
+  // Of a pair of query tiles: their key tiles (the second may be past the end of the sequence, and has none then), rows of the last key
+  // tile that exist, when below 128.
+  struct Extent { int n_a, n_b, n, tail; };
+  auto extent_of = [](const AttnTile& x) {
+    Extent e;
+    e.n_a = x.offset / TILE + 1;
+    e.n_b = x.offset + TILE < x.length ? e.n_a + 1 : 0;
+    e.n = e.n_b ? e.n_b : e.n_a;
+    e.tail = x.length - (e.n - 1) * TILE;
+    return e;
+  };
 
-    if (warp == COPY_WARP) {
+  if (warp == COPY_WARP) {
     if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
-      mbar_expect_tx(smem_u32(&bar_q), (n_b ? 2u : 1u) * OPERAND);
-      load_tile<DP>(smem_base, &maps.q, smem_u32(&bar_q), head, tile.start + tile.offset);
-      if (n_b) load_tile<DP>(smem_base + OPERAND, &maps.q, smem_u32(&bar_q), head, tile.start + tile.offset + TILE);
       Pipe at;
-      for (int i = 0; i < 2 * n; ++i) {
-        if (!mbar_wait_cta(smem_u32(&bar_empty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
-        const uint32_t bar = smem_u32(&bar_full[at.stage]);
-        mbar_expect_tx(bar, OPERAND);
-        load_tile<DP>(ring + at.stage * OPERAND, (i & 1) ? &maps.v : &maps.k, bar, kv_head, tile.start + (i >> 1) * TILE);
-        at.next<STAGES>();
+      uint32_t turn = 0;
+      bool alive = true;
+      for (int u = blockIdx.x; u >= 0; u = alive ? take<false>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+        const Unit x = unit_of(p, p.heads, u);
+        const Extent e = extent_of(x.tile);
+        const int kv_head = x.head / p.group;
+        const int first_row = x.tile.start + x.tile.offset;
+        for (int k = 0; k < 2 * e.n; ++k) {
+          alive = mbar_wait_cta(smem_u32(&bar_empty[at.stage]), at.phase ^ 1u, &abort_flag, limit);
+          if (!alive) break;
+          const uint32_t bar = smem_u32(&bar_full[at.stage]);
+          mbar_expect_tx(bar, OPERAND);
+          load_tile<DP>(ring + at.stage * OPERAND, (k & 1) ? &maps.v : &maps.k, bar, kv_head, x.tile.start + (k >> 1) * TILE);
+          at.next<STAGES>();
+          if (k == 0) {                       // the queries' place is free once the last scores of the unit before are complete
+            alive = mbar_wait_cta(smem_u32(&bar_qempty), turn ^ 1u, &abort_flag, limit);
+            if (!alive) break;
+            mbar_expect_tx(smem_u32(&bar_q), (e.n_b ? 2u : 1u) * OPERAND);
+            load_tile<DP>(smem_base, &maps.q, smem_u32(&bar_q), x.head, first_row);
+            if (e.n_b) load_tile<DP>(smem_base + OPERAND, &maps.q, smem_u32(&bar_q), x.head, first_row + TILE);
+          }
+          if (k == 2 * e.n - 2) alive = ask(next, &abort_flag, limit);
+          if (!alive) break;
+        }
       }
     }
   } else if (warp == MMA_WARP) {
@@ -367,69 +452,74 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     // Order: scores of key tile 0 for both query tiles; then per key tile j and query tile: p v of j, scores of j + 1.  Products
     // of one thread complete in order, so scores of j + 1 may overwrite the p of j that the product before them reads.
     Pipe at;                                  // of the tile that is waited for next
-    auto arrived = [&]() { return mbar_wait_cta(smem_u32(&bar_full[at.stage]), at.phase, &abort_flag, limit); };
-    bool alive = mbar_wait_cta(smem_u32(&bar_q), 0, &abort_flag, limit) && arrived();
-    alive = __all_sync(0xffffffffu, alive);
-    if (alive) {
+    auto arrived = [&]() { return __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_full[at.stage]), at.phase, &abort_flag, limit)); };
+    uint32_t turn = 0, turn_p[2] = {0, 0};
+    bool alive = true;
+    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+      const Extent x = extent_of(unit_of(p, p.heads, u).tile);
+      const int n_t[2] = {x.n_a, x.n_b};
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_q), turn, &abort_flag, limit)) && arrived();
+      if (!alive) break;
       tc_fence_after();
       uint32_t k_stage = at.stage;
       at.next<STAGES>();
+#pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (t == 1 && !n_b) break;
+        if (!n_t[t]) continue;
         scores<DP>(leader, tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
         mma_commit(leader, smem_u32(&bar_s[t]));
       }
       mma_commit(leader, smem_u32(&bar_empty[k_stage]));
-      __syncwarp();
-      for (int j = 0; alive && j < n; ++j) {
-        alive = __all_sync(0xffffffffu, arrived());
+      if (x.n == 1) mma_commit(leader, smem_u32(&bar_qempty));
+      for (int j = 0; alive && j < x.n; ++j) {
+        alive = arrived();
         if (!alive) break;
         const uint32_t v_stage = at.stage;
         at.next<STAGES>();
-        if (j == n - 1 && tail < TILE) zero_rows<DP>(ring + v_stage * OPERAND, tail, lane);
-        if (j + 1 < n) {
-          alive = __all_sync(0xffffffffu, arrived());
+        if (j == x.n - 1 && x.tail < TILE) zero_rows<DP>(ring + v_stage * OPERAND, x.tail, lane);
+        if (j + 1 < x.n) {
+          alive = arrived();
           if (!alive) break;
           k_stage = at.stage;
           at.next<STAGES>();
         }
+#pragma unroll
         for (int t = 0; t < 2; ++t) {
-          const int n_t = t ? n_b : n_a;
-          if (j >= n_t) continue;
-          for (int h = 0; alive && h < 2; ++h) {
-            alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t][h]), (uint32_t)j & 1u, &abort_flag, limit));
-            if (!alive) break;
-            tc_fence_after();
-            weigh_half<DP>(leader, tm + TM_O + t * DP, tm + t * 128 + h * HALF, ring + v_stage * OPERAND, h, j > 0 || h > 0);
-          }
+          if (j >= n_t[t]) continue;
+          const uint32_t sums = tm + TM_O + t * DP, weights = tm + t * 128, values = ring + v_stage * OPERAND;
+          alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t][0]), turn_p[t], &abort_flag, limit));
+          // (at the unit's start both halves of the row warps: they have read the sums of the unit before)
+          if (alive && j == 0) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t][1]), turn_p[t], &abort_flag, limit));
           if (!alive) break;
-          if (j + 1 < n_t) {
+          tc_fence_after();
+          weigh_half<DP>(leader, sums, weights, values, 0, j > 0);
+          alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t][1]), turn_p[t], &abort_flag, limit));
+          if (!alive) break;
+          tc_fence_after();
+          weigh_half<DP>(leader, sums, weights + HALF, values, 1, true);
+          turn_p[t] ^= 1u;
+          if (j + 1 < n_t[t]) {
             scores<DP>(leader, tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
             mma_commit(leader, smem_u32(&bar_s[t]));
           } else {
             mma_commit(leader, smem_u32(&bar_o[t]));
           }
-          __syncwarp();
         }
-        if (alive) {
-          mma_commit(leader, smem_u32(&bar_empty[v_stage]));
-          if (j + 1 < n) mma_commit(leader, smem_u32(&bar_empty[k_stage]));
-        }
-        __syncwarp();
+        if (!alive) break;
+        mma_commit(leader, smem_u32(&bar_empty[v_stage]));
+        if (j + 1 < x.n) mma_commit(leader, smem_u32(&bar_empty[k_stage]));
+        if (j + 2 == x.n) mma_commit(leader, smem_u32(&bar_qempty));
       }
     }
   } else {
     // A row belongs to two threads, each with half of its columns: warps 0-3 and 4-7 (first tile), 8-11 and 12-15 (second).
     const int t = warp >> 3, half = (warp >> 2) & 1, quarter = warp & 3;
     const int row = quarter * 32 + lane;                       // of the tile; key columns up to `row` of the last key tile count
-    const int n_t = t ? n_b : n_a;
     const int col0 = half * 64, pair_id = 1 + t * 4 + quarter;
     const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
     const uint32_t t_s = t_lane + t * 128 + half * HALF, t_o = t_lane + TM_O + t * DP + half * (DP / 2);
     const float c = p.scale * LOG2_E;
     const Pair c2 = both(c);
-    float* const mine = &row_share[t][half][row];
-    const float* const other = &row_share[t][half ^ 1][row];
     float top = 0.f, total = 0.f;                              // score that the weights refer to (the row's, unscaled); sum of the weights
     Pair shift = both(0.f);
     // 32 of this thread's 64 scores
@@ -452,9 +542,9 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
 #pragma unroll
         for (int e = 0; e < 32; e += 2) m = max3(m, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
       }
-      *mine = m;
+      row_largest[t][half][row] = m;
       either(pair_id, false);
-      m = max3(m, *other, some ? top : m);
+      m = max3(m, row_largest[t][half ^ 1][row], some ? top : m);
       if (some) {                             // (the product before these scores is complete, as they are)
         const float by = exp2_approx((top - m) * c);
         total *= by;
@@ -497,41 +587,50 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       const float2 sums = parts(add2(sum[0], sum[1]));
       return sums.x + sums.y;
     };
+    uint32_t turn_s = 0, turn_o = 0;
     bool alive = true;
-    for (int j = 0; j < n_t; ++j) {
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[t]), (uint32_t)j & 1u, &abort_flag, limit));
-      tc_fence_after();
-      const bool last = j == n_t - 1;
-      uint32_t w[32];
-      if (j == 0) move_reference(false, last);
-      float part = weights(w, last);
-      // Where the weights are too large by the reference as it was, or not numbers: once more by a new one.
-      if (either(pair_id, !alive || (j > 0 && !(part <= MOST)))) {
-        if (either(pair_id, !alive)) { alive = false; break; }
-        move_reference(true, last);
-        part = weights(w, last);
-      }
-      total += part;
-      tm_store32(t_s, w);
-      tm_store_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_p[t][half]));
-    }
-    if (n_t) {
-      if (alive) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_o[t]), 0, &abort_flag, limit));
-      *mine = total;
-      if (!either(pair_id, !alive)) {
+    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1) {
+      const Unit x = unit_of(p, p.heads, u);
+      const Extent e = extent_of(x.tile);
+      const int n_t = t ? e.n_b : e.n_a;
+      if (!n_t) continue;
+      top = 0.f;
+      total = 0.f;
+      for (int j = 0; j < n_t; ++j) {
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[t]), turn_s, &abort_flag, limit));
         tc_fence_after();
-        total += *other;
-        const int pos = tile.offset + t * TILE + row;
-        const bool ok = pos < tile.length;
-        const int64_t token = (int64_t)tile.start + pos;
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + ((ok ? token : 0) * p.heads + head) * p.dim + half * (DP / 2);
-        const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
-        store_columns(t_o, out, 0, DP / 2, p.dim - half * (DP / 2), 1.0f / total, ok, wide);
-        if (ok && half == 0) p.lse[(int64_t)head * p.tokens + token] = (top * c + log2_approx(total)) * LN2;
+        const bool last = j == n_t - 1;
+        uint32_t w[32];
+        if (j == 0) move_reference(false, last);
+        float part = weights(w, last);
+        // Where the weights are too large by the reference as it was, or not numbers: once more by a new one.
+        if (either(pair_id, !alive || (j > 0 && !(part <= MOST)))) {
+          if (either(pair_id, !alive)) { alive = false; break; }
+          move_reference(true, last);
+          part = weights(w, last);
+        }
+        total += part;
+        tm_store32(t_s, w);
+        tm_store_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(smem_u32(&bar_p[t][half]));
+        turn_s ^= 1u;
       }
+      if (alive) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_o[t]), turn_o, &abort_flag, limit));
+      row_total[t][half][row] = total;
+      alive = !either(pair_id, !alive);
+      if (!alive) break;
+      turn_o ^= 1u;
+      tc_fence_after();
+      total += row_total[t][half ^ 1][row];
+      const int pos = x.tile.offset + t * TILE + row;
+      const bool ok = pos < x.tile.length;
+      const int64_t token = (int64_t)x.tile.start + pos;
+      __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + ((ok ? token : 0) * p.heads + x.head) * p.dim + half * (DP / 2);
+      const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
+      store_columns(t_o, out, 0, DP / 2, p.dim - half * (DP / 2), 1.0f / total, ok, wide);
+      if (ok && half == 0) p.lse[(int64_t)x.head * p.tokens + token] = (top * c + log2_approx(total)) * LN2;
     }
   }
   ATTN_END(512)
@@ -553,9 +652,12 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
   using Sh = BackShape<DP>;
   constexpr int STAGES = Sh::STAGES;
   constexpr uint32_t OPERAND = Sh::OPERAND;
+  constexpr int ROW_WARPS = 8, COPY_WARP = 8, MMA_WARP = 9;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_q, bar_kfull[STAGES], bar_kempty[STAGES], bar_vfull[STAGES], bar_vempty[STAGES], bar_s[2], bar_dp,
+  __shared__ __align__(8) uint64_t bar_q, bar_qempty, bar_kfull[STAGES], bar_kempty[STAGES], bar_vfull[STAGES], bar_vempty[STAGES], bar_s[2], bar_dp,
       bar_ds, bar_done;
+  __shared__ __align__(16) uint4 next_answer[2];
+  __shared__ __align__(8) uint64_t bar_next[2], bar_taken[2];
   __shared__ uint32_t tmem_base_slot;
   __shared__ volatile int abort_flag;
 
@@ -565,6 +667,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
   const uint64_t limit = p.wait_limit_ns;
   auto init_barriers = [&] {
     mbar_init(smem_u32(&bar_q), 1);
+    mbar_init(smem_u32(&bar_qempty), 1);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(&bar_kfull[s]), 1);
       mbar_init(smem_u32(&bar_kempty[s]), 1);
@@ -580,25 +683,34 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
   ATTN_BEGIN(512)
   constexpr uint32_t TM_DP = 256, TM_DQ = 384;                 // columns: two tiles of scores, dp, dq
 
-  const AttnTile tile = p.tiles[blockIdx.x / p.heads];
-  const int head = blockIdx.x % p.heads, kv_head = head / p.group;
-  const int n = tile.offset / TILE + 1;                        // key tiles
-  const int tail = tile.length - (n - 1) * TILE;               // rows of the last one that exist, when below 128
-
   if (warp == COPY_WARP) {
     if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
-      mbar_expect_tx(smem_u32(&bar_q), 2 * OPERAND);
-      load_tile<DP>(s_q, &maps.q, smem_u32(&bar_q), head, tile.start + tile.offset);
-      load_tile<DP>(s_g, &maps.g, smem_u32(&bar_q), head, tile.start + tile.offset);
       Pipe at;
-      for (int j = 0; j < n; ++j) {
-        if (!mbar_wait_cta(smem_u32(&bar_kempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
-        mbar_expect_tx(smem_u32(&bar_kfull[at.stage]), OPERAND);
-        load_tile<DP>(s_k + at.stage * OPERAND, &maps.k, smem_u32(&bar_kfull[at.stage]), kv_head, tile.start + j * TILE);
-        if (!mbar_wait_cta(smem_u32(&bar_vempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
-        mbar_expect_tx(smem_u32(&bar_vfull[at.stage]), OPERAND);
-        load_tile<DP>(s_v + at.stage * OPERAND, &maps.v, smem_u32(&bar_vfull[at.stage]), kv_head, tile.start + j * TILE);
-        at.next<STAGES>();
+      uint32_t turn = 0;
+      bool alive = true;
+      for (int u = blockIdx.x; u >= 0; u = alive ? take<false>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+        const Unit x = unit_of(p, p.heads, u);
+        const int n = x.tile.offset / TILE + 1, kv_head = x.head / p.group, first_row = x.tile.start + x.tile.offset;
+        for (int j = 0; j < n; ++j) {
+          alive = mbar_wait_cta(smem_u32(&bar_kempty[at.stage]), at.phase ^ 1u, &abort_flag, limit);
+          if (!alive) break;
+          mbar_expect_tx(smem_u32(&bar_kfull[at.stage]), OPERAND);
+          load_tile<DP>(s_k + at.stage * OPERAND, &maps.k, smem_u32(&bar_kfull[at.stage]), kv_head, x.tile.start + j * TILE);
+          if (j == 0) {                       // free once the last scores and dp of the unit before are complete
+            alive = mbar_wait_cta(smem_u32(&bar_qempty), turn ^ 1u, &abort_flag, limit);
+            if (!alive) break;
+            mbar_expect_tx(smem_u32(&bar_q), 2 * OPERAND);
+            load_tile<DP>(s_q, &maps.q, smem_u32(&bar_q), x.head, first_row);
+            load_tile<DP>(s_g, &maps.g, smem_u32(&bar_q), x.head, first_row);
+          }
+          alive = mbar_wait_cta(smem_u32(&bar_vempty[at.stage]), at.phase ^ 1u, &abort_flag, limit);
+          if (!alive) break;
+          mbar_expect_tx(smem_u32(&bar_vfull[at.stage]), OPERAND);
+          load_tile<DP>(s_v + at.stage * OPERAND, &maps.v, smem_u32(&bar_vfull[at.stage]), kv_head, x.tile.start + j * TILE);
+          at.next<STAGES>();
+          if (j == n - 1) alive = ask(next, &abort_flag, limit);
+          if (!alive) break;
+        }
       }
     }
   } else if (warp == MMA_WARP) {
@@ -606,122 +718,134 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
     // Order: scores of 0; then per key tile j: dp of j, scores of j + 1 (into the other columns), dq += ds k of j.  (The scores of
     // j + 1 may be complete before the row warps have looked for those of j: a barrier for each of the two places.)
     Pipe at;                                  // key tile j
-    auto keys = [&](const Pipe& q, int j) {   // waits for key tile j and readies it
-      if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_kfull[q.stage]), q.phase, &abort_flag, limit))) return false;
-      if (j == n - 1 && tail < TILE) zero_rows<DP>(s_k + q.stage * OPERAND, tail, lane);
-      return true;
-    };
-    bool alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_q), 0, &abort_flag, limit));
-    alive = alive && keys(at, 0);
-    if (alive) {
+    uint32_t turn = 0, step = 0;              // step: key tiles so far, over all units
+    bool alive = true;
+    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+      const AttnTile x = unit_of(p, p.heads, u).tile;
+      const int n = x.offset / TILE + 1;      // key tiles
+      const int tail = x.length - (n - 1) * TILE;              // rows of the last one that exist, when below 128
+      auto keys = [&](const Pipe& q, int j) {  // waits for key tile j and readies it
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_kfull[q.stage]), q.phase, &abort_flag, limit))) return false;
+        if (j == n - 1 && tail < TILE) zero_rows<DP>(s_k + q.stage * OPERAND, tail, lane);
+        return true;
+      };
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_q), turn, &abort_flag, limit)) && keys(at, 0);
+      if (!alive) break;
       tc_fence_after();
-      scores<DP>(leader, tm, s_q, s_k);
-      mma_commit(leader, smem_u32(&bar_s[0]));
-      __syncwarp();
-      for (int j = 0; j < n; ++j) {
-        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_vfull[at.stage]), at.phase, &abort_flag, limit))) break;
+      scores<DP>(leader, tm + (step & 1u) * 128, s_q, s_k + at.stage * OPERAND);
+      mma_commit(leader, smem_u32(&bar_s[step & 1u]));
+      for (int j = 0; j < n; ++j, ++step) {
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_vfull[at.stage]), at.phase, &abort_flag, limit));
+        if (!alive) break;
         tc_fence_after();
         scores<DP>(leader, tm + TM_DP, s_g, s_v + at.stage * OPERAND);
         mma_commit(leader, smem_u32(&bar_dp));
         mma_commit(leader, smem_u32(&bar_vempty[at.stage]));
-        __syncwarp();
         Pipe ahead = at;
         ahead.next<STAGES>();
         if (j + 1 < n) {
-          if (!keys(ahead, j + 1)) break;
+          alive = keys(ahead, j + 1);
+          if (!alive) break;
           tc_fence_after();
-          scores<DP>(leader, tm + ((j + 1) & 1) * 128, s_q, s_k + ahead.stage * OPERAND);
-          mma_commit(leader, smem_u32(&bar_s[(j + 1) & 1]));
-          __syncwarp();
+          scores<DP>(leader, tm + ((step + 1) & 1u) * 128, s_q, s_k + ahead.stage * OPERAND);
+          mma_commit(leader, smem_u32(&bar_s[(step + 1) & 1u]));
+        } else {
+          mma_commit(leader, smem_u32(&bar_qempty));
         }
-        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), (uint32_t)j & 1u, &abort_flag, limit))) break;
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), step & 1u, &abort_flag, limit));
+        if (!alive) break;
         tc_fence_after();
-        weigh<DP>(leader, tm + TM_DQ, tm + (j & 1) * 128, HALF, s_k + at.stage * OPERAND, j > 0);
-        mma_commit(leader, j + 1 < n ? smem_u32(&bar_kempty[at.stage]) : smem_u32(&bar_done));
-        __syncwarp();
+        weigh<DP>(leader, tm + TM_DQ, tm + (step & 1u) * 128, HALF, s_k + at.stage * OPERAND, j > 0);
+        mma_commit(leader, smem_u32(&bar_kempty[at.stage]));
+        if (j + 1 == n) mma_commit(leader, smem_u32(&bar_done));
         at = ahead;
       }
     }
   } else if (warp < COPY_WARP) {
     const int half = warp >> 2, quarter = warp & 3;
     const int row = quarter * 32 + lane;
-    const int pos = tile.offset + row;
-    const bool ok = pos < tile.length;
-    const int64_t token = (int64_t)tile.start + (ok ? pos : 0);
     const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
     const float c = p.scale * LOG2_E;
-    const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(p.o) + (token * p.heads + head) * p.dim;
-    const __nv_bfloat16* g = reinterpret_cast<const __nv_bfloat16*>(p.g) + token * p.g_ts + head * p.g_hs;
-    // delta = do . o of the row, with o as it was rounded
-    Pair acc = both(0.f);
-#pragma unroll 4
-    for (int e = 0; e < p.dim; e += 8) {
-      const uint4 a = *reinterpret_cast<const uint4*>(o + e), b = *reinterpret_cast<const uint4*>(g + e);
-      acc = fma2(pair_bf16(a.x), pair_bf16(b.x), acc);
-      acc = fma2(pair_bf16(a.y), pair_bf16(b.y), acc);
-      acc = fma2(pair_bf16(a.z), pair_bf16(b.z), acc);
-      acc = fma2(pair_bf16(a.w), pair_bf16(b.w), acc);
-    }
-    const float2 halves = parts(acc);
-    const float delta = halves.x + halves.y;
-    const float lse2 = p.lse[(int64_t)head * p.tokens + token] * LOG2_E;
-    if (half == 0 && ok) p.delta[(int64_t)head * p.tokens + token] = delta;
-    const Pair c2 = both(c), shift = both(-lse2), minus = both(-delta);
+    uint32_t turn = 0, step = 0;
     bool alive = true;
-    for (int j = 0; j < n; ++j) {
-      const uint32_t t_s = t_lane + (j & 1) * 128 + half * HALF;
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[j & 1]), (uint32_t)(j >> 1) & 1u, &abort_flag, limit));
-      if (!alive) break;
-      tc_fence_after();
-      uint32_t s[64], d[64];
-      tm_load32(t_s, s);
-      tm_load32(t_s + 32, s + 32);
-      tm_load_wait();
-      after_load(s);
-      after_load(s + 32);
-#pragma unroll
-      for (int e = 0; e < 64; e += 2) {
-        const float2 x = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, shift));
-        s[e] = __float_as_uint(exp2_approx(x.x));
-        s[e + 1] = __float_as_uint(exp2_approx(x.y));
+    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+      const Unit x = unit_of(p, p.heads, u);
+      const int pos = x.tile.offset + row;
+      const bool ok = pos < x.tile.length;
+      const int64_t token = (int64_t)x.tile.start + (ok ? pos : 0);
+      const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(p.o) + (token * p.heads + x.head) * p.dim;
+      const __nv_bfloat16* g = reinterpret_cast<const __nv_bfloat16*>(p.g) + token * p.g_ts + x.head * p.g_hs;
+      // delta = do . o of the row, with o as it was rounded
+      Pair acc = both(0.f);
+  #pragma unroll 4
+      for (int e = 0; e < p.dim; e += 8) {
+        const uint4 a = *reinterpret_cast<const uint4*>(o + e), b = *reinterpret_cast<const uint4*>(g + e);
+        acc = fma2(pair_bf16(a.x), pair_bf16(b.x), acc);
+        acc = fma2(pair_bf16(a.y), pair_bf16(b.y), acc);
+        acc = fma2(pair_bf16(a.z), pair_bf16(b.z), acc);
+        acc = fma2(pair_bf16(a.w), pair_bf16(b.w), acc);
       }
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), (uint32_t)j & 1u, &abort_flag, limit));
-      if (!alive) break;
-      tc_fence_after();
-      tm_load32(t_lane + TM_DP + half * HALF, d);
-      tm_load32(t_lane + TM_DP + half * HALF + 32, d + 32);
-      tm_load_wait();
-      after_load(d);
-      after_load(d + 32);
-      uint32_t w[32];
-      if (j == n - 1) {                       // where the key comes after the query: no weight, whatever the products hold
-#pragma unroll
-        for (int e = 0; e < 64; e += 2) {
-          const float a = __uint_as_float(s[e]) * (__uint_as_float(d[e]) - delta);
-          const float b = __uint_as_float(s[e + 1]) * (__uint_as_float(d[e + 1]) - delta);
-          w[e >> 1] = pack_bf16x2(half * 64 + e > row ? 0.f : a, half * 64 + e + 1 > row ? 0.f : b);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < 64; e += 2) {
-          const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
-                                      add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), minus)));
-          w[e >> 1] = pack_bf16x2(x.x, x.y);
-        }
-      }
-      tm_store32(t_s, w);
-      tm_store_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_ds));
-    }
-    if (alive) {
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), 0, &abort_flag, limit));
-      if (alive) {
+      const float2 halves = parts(acc);
+      const float delta = halves.x + halves.y;
+      const float lse2 = p.lse[(int64_t)x.head * p.tokens + token] * LOG2_E;
+      if (half == 0 && ok) p.delta[(int64_t)x.head * p.tokens + token] = delta;
+      const Pair c2 = both(c), shift = both(-lse2), minus = both(-delta);
+      const int n = x.tile.offset / TILE + 1;
+      for (int j = 0; j < n; ++j, ++step) {
+        const uint32_t t_s = t_lane + (step & 1u) * 128 + half * HALF;
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[step & 1u]), (step >> 1) & 1u, &abort_flag, limit));
+        if (!alive) break;
         tc_fence_after();
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (token * p.heads + head) * p.dim;
-        const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
-        store_columns(t_lane + TM_DQ, out, half * (DP / 2), DP / 2, p.dim, p.scale, ok, wide);
+        uint32_t s[64], d[64];
+        tm_load32(t_s, s);
+        tm_load32(t_s + 32, s + 32);
+        tm_load_wait();
+        after_load(s);
+        after_load(s + 32);
+  #pragma unroll
+        for (int e = 0; e < 64; e += 2) {
+          const float2 x = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, shift));
+          s[e] = __float_as_uint(exp2_approx(x.x));
+          s[e + 1] = __float_as_uint(exp2_approx(x.y));
+        }
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), step & 1u, &abort_flag, limit));
+        if (!alive) break;
+        tc_fence_after();
+        tm_load32(t_lane + TM_DP + half * HALF, d);
+        tm_load32(t_lane + TM_DP + half * HALF + 32, d + 32);
+        tm_load_wait();
+        after_load(d);
+        after_load(d + 32);
+        uint32_t w[32];
+        if (j == n - 1) {                       // where the key comes after the query: no weight, whatever the products hold
+  #pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            const float a = __uint_as_float(s[e]) * (__uint_as_float(d[e]) - delta);
+            const float b = __uint_as_float(s[e + 1]) * (__uint_as_float(d[e + 1]) - delta);
+            w[e >> 1] = pack_bf16x2(half * 64 + e > row ? 0.f : a, half * 64 + e + 1 > row ? 0.f : b);
+          }
+        } else {
+  #pragma unroll
+          for (int e = 0; e < 64; e += 2) {
+            const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
+                                        add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), minus)));
+            w[e >> 1] = pack_bf16x2(x.x, x.y);
+          }
+        }
+        tm_store32(t_s, w);
+        tm_store_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(smem_u32(&bar_ds));
+      }
+      if (alive) {
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), turn, &abort_flag, limit));
+        if (alive) {
+          tc_fence_after();
+          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (token * p.heads + x.head) * p.dim;
+          const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
+          store_columns(t_lane + TM_DQ, out, half * (DP / 2), DP / 2, p.dim, p.scale, ok, wide);
+        }
       }
     }
   }
@@ -737,9 +861,12 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   using Sh = BackShape<DP>;
   constexpr int STAGES = Sh::STAGES;
   constexpr uint32_t OPERAND = Sh::OPERAND;
+  constexpr int ROW_WARPS = 8, COPY_WARP = 8, MMA_WARP = 9;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_kv, bar_qfull[STAGES], bar_qempty[STAGES], bar_gfull[STAGES], bar_gempty[STAGES], bar_s, bar_dp,
+  __shared__ __align__(8) uint64_t bar_kv, bar_kvempty, bar_qfull[STAGES], bar_qempty[STAGES], bar_gfull[STAGES], bar_gempty[STAGES], bar_s, bar_dp,
       bar_p, bar_ds, bar_done;
+  __shared__ __align__(16) uint4 next_answer[2];
+  __shared__ __align__(8) uint64_t bar_next[2], bar_taken[2];
   __shared__ uint32_t tmem_base_slot;
   __shared__ volatile int abort_flag;
   __shared__ __align__(16) float row_values[8][2][64];         // of each row warp: log-sum-exp and delta of its 64 queries, negated
@@ -750,6 +877,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   const uint64_t limit = p.wait_limit_ns;
   auto init_barriers = [&] {
     mbar_init(smem_u32(&bar_kv), 1);
+    mbar_init(smem_u32(&bar_kvempty), 1);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(&bar_qfull[s]), 1);
       mbar_init(smem_u32(&bar_qempty[s]), 1);
@@ -766,74 +894,97 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   constexpr uint32_t TM_DP = 128, TM_DV = 256, TM_DK = 256 + DP;           // columns: scores, dp, dv, dk (rows are keys)
 
   const int kv_heads = p.heads / p.group;
-  const AttnTile tile = p.tiles[blockIdx.x / kv_heads];
-  const int kv_head = blockIdx.x % kv_heads;
-  const int first = tile.offset / TILE, end = (tile.length + TILE - 1) / TILE;   // query tiles
-  const int per = end - first, n = per * p.group;
-  const int tail = tile.length - (end - 1) * TILE;             // rows of the last query tile that exist, when below 128
+  // Of a key tile: its query tiles, first to end, of `group` heads; rows of the last one that exist, when below 128.
+  struct Extent { int first, end, n, tail; };
+  auto extent_of = [&](const AttnTile& x) {
+    Extent e;
+    e.first = x.offset / TILE;
+    e.end = (x.length + TILE - 1) / TILE;
+    e.n = (e.end - e.first) * p.group;
+    e.tail = x.length - (e.end - 1) * TILE;
+    return e;
+  };
 
   if (warp == COPY_WARP) {
     if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
-      mbar_expect_tx(smem_u32(&bar_kv), 2 * OPERAND);
-      load_tile<DP>(s_k, &maps.k, smem_u32(&bar_kv), kv_head, tile.start + tile.offset);
-      load_tile<DP>(s_v, &maps.v, smem_u32(&bar_kv), kv_head, tile.start + tile.offset);
       Pipe at;
-      int head = kv_head * p.group, i = first;
-      for (int it = 0; it < n; ++it) {
-        if (!mbar_wait_cta(smem_u32(&bar_qempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
-        mbar_expect_tx(smem_u32(&bar_qfull[at.stage]), OPERAND);
-        load_tile<DP>(s_q + at.stage * OPERAND, &maps.q, smem_u32(&bar_qfull[at.stage]), head, tile.start + i * TILE);
-        if (!mbar_wait_cta(smem_u32(&bar_gempty[at.stage]), at.phase ^ 1u, &abort_flag, limit)) break;
-        mbar_expect_tx(smem_u32(&bar_gfull[at.stage]), OPERAND);
-        load_tile<DP>(s_g + at.stage * OPERAND, &maps.g, smem_u32(&bar_gfull[at.stage]), head, tile.start + i * TILE);
-        at.next<STAGES>();
-        if (++i == end) { i = first; ++head; }
+      uint32_t turn = 0;
+      bool alive = true;
+      for (int u = blockIdx.x; u >= 0; u = alive ? take<false>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+        const Unit x = unit_of(p, kv_heads, u);
+        const Extent e = extent_of(x.tile);
+        int head = x.head * p.group, i = e.first;
+        for (int it = 0; it < e.n; ++it) {
+          alive = mbar_wait_cta(smem_u32(&bar_qempty[at.stage]), at.phase ^ 1u, &abort_flag, limit);
+          if (!alive) break;
+          mbar_expect_tx(smem_u32(&bar_qfull[at.stage]), OPERAND);
+          load_tile<DP>(s_q + at.stage * OPERAND, &maps.q, smem_u32(&bar_qfull[at.stage]), head, x.tile.start + i * TILE);
+          if (it == 0) {                      // free once the last scores and dp of the unit before are complete
+            alive = mbar_wait_cta(smem_u32(&bar_kvempty), turn ^ 1u, &abort_flag, limit);
+            if (!alive) break;
+            mbar_expect_tx(smem_u32(&bar_kv), 2 * OPERAND);
+            load_tile<DP>(s_k, &maps.k, smem_u32(&bar_kv), x.head, x.tile.start + x.tile.offset);
+            load_tile<DP>(s_v, &maps.v, smem_u32(&bar_kv), x.head, x.tile.start + x.tile.offset);
+          }
+          alive = mbar_wait_cta(smem_u32(&bar_gempty[at.stage]), at.phase ^ 1u, &abort_flag, limit);
+          if (!alive) break;
+          mbar_expect_tx(smem_u32(&bar_gfull[at.stage]), OPERAND);
+          load_tile<DP>(s_g + at.stage * OPERAND, &maps.g, smem_u32(&bar_gfull[at.stage]), head, x.tile.start + i * TILE);
+          at.next<STAGES>();
+          if (++i == e.end) { i = e.first; ++head; }
+          if (it == e.n - 1) alive = ask(next, &abort_flag, limit);
+          if (!alive) break;
+        }
       }
     }
   } else if (warp == MMA_WARP) {
     const uint32_t leader = elect_leader();
     // Order: scores of 0; then per step: dp, dv += p do, scores of the next, dk += ds q.
     Pipe at;
-    int i = first;                            // query tile of the step
-    auto queries = [&](const Pipe& q, int i) {
-      if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_qfull[q.stage]), q.phase, &abort_flag, limit))) return false;
-      if (i == end - 1 && tail < TILE) zero_rows<DP>(s_q + q.stage * OPERAND, tail, lane);
-      return true;
-    };
-    bool alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_kv), 0, &abort_flag, limit));
-    alive = alive && queries(at, i);
-    if (alive) {
+    uint32_t turn = 0, step = 0;              // step: query tiles so far, over all units
+    bool alive = true;
+    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+      const Extent x = extent_of(unit_of(p, kv_heads, u).tile);
+      int i = x.first;                        // query tile of the step
+      auto queries = [&](const Pipe& q, int i) {
+        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_qfull[q.stage]), q.phase, &abort_flag, limit))) return false;
+        if (i == x.end - 1 && x.tail < TILE) zero_rows<DP>(s_q + q.stage * OPERAND, x.tail, lane);
+        return true;
+      };
+      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_kv), turn, &abort_flag, limit)) && queries(at, i);
+      if (!alive) break;
       tc_fence_after();
-      scores<DP>(leader, tm, s_k, s_q);
+      scores<DP>(leader, tm, s_k, s_q + at.stage * OPERAND);
       mma_commit(leader, smem_u32(&bar_s));
-      __syncwarp();
-      for (int it = 0; it < n; ++it) {
-        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_gfull[at.stage]), at.phase, &abort_flag, limit))) break;
-        if (i == end - 1 && tail < TILE) zero_rows<DP>(s_g + at.stage * OPERAND, tail, lane);
+      for (int it = 0; it < x.n; ++it, ++step) {
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_gfull[at.stage]), at.phase, &abort_flag, limit));
+        if (!alive) break;
+        if (i == x.end - 1 && x.tail < TILE) zero_rows<DP>(s_g + at.stage * OPERAND, x.tail, lane);
         tc_fence_after();
         scores<DP>(leader, tm + TM_DP, s_v, s_g + at.stage * OPERAND);
         mma_commit(leader, smem_u32(&bar_dp));
-        __syncwarp();
-        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p), (uint32_t)it & 1u, &abort_flag, limit))) break;
+        if (it + 1 == x.n) mma_commit(leader, smem_u32(&bar_kvempty));
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p), step & 1u, &abort_flag, limit));
+        if (!alive) break;
         tc_fence_after();
         weigh<DP>(leader, tm + TM_DV, tm, HALF, s_g + at.stage * OPERAND, it > 0);
         mma_commit(leader, smem_u32(&bar_gempty[at.stage]));
-        __syncwarp();
         Pipe ahead = at;
         ahead.next<STAGES>();
-        const int i_next = i + 1 == end ? first : i + 1;
-        if (it + 1 < n) {
-          if (!queries(ahead, i_next)) break;
+        const int i_next = i + 1 == x.end ? x.first : i + 1;
+        if (it + 1 < x.n) {
+          alive = queries(ahead, i_next);
+          if (!alive) break;
           tc_fence_after();
           scores<DP>(leader, tm, s_k, s_q + ahead.stage * OPERAND);
           mma_commit(leader, smem_u32(&bar_s));
-          __syncwarp();
         }
-        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), (uint32_t)it & 1u, &abort_flag, limit))) break;
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), step & 1u, &abort_flag, limit));
+        if (!alive) break;
         tc_fence_after();
         weigh<DP>(leader, tm + TM_DK, tm + TM_DP, HALF, s_q + at.stage * OPERAND, it > 0);
-        mma_commit(leader, it + 1 < n ? smem_u32(&bar_qempty[at.stage]) : smem_u32(&bar_done));
-        __syncwarp();
+        mma_commit(leader, smem_u32(&bar_qempty[at.stage]));
+        if (it + 1 == x.n) mma_commit(leader, smem_u32(&bar_done));
         at = ahead;
         i = i_next;
       }
@@ -849,102 +1000,107 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     const int col0 = half * 64;
     float* const lse = row_values[warp][0];
     float* const delta = row_values[warp][1];
-    int head = kv_head * p.group, i = first;
-    float ahead[4];
-    auto fetch = [&] {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int pos = i * TILE + col0 + h * 32 + lane;
-        const int64_t at = (int64_t)head * p.tokens + tile.start + pos;
-        ahead[h] = pos < tile.length ? -LOG2_E * p.lse[at] : 0.f;
-        ahead[2 + h] = pos < tile.length ? -p.delta[at] : 0.f;
-      }
-    };
-    fetch();
+    uint32_t turn = 0, step = 0;
     bool alive = true;
-    for (int it = 0; it < n; ++it) {
-      const bool edge = i == first || (i == end - 1 && tail < TILE);       // some of the tile's pairs do not count
-      const int last = tile.length - i * TILE - 1;                         // columns from .. last count
-      const int from = i == first ? row : 0;
-      __syncwarp();
-      lse[lane] = ahead[0];
-      lse[32 + lane] = ahead[1];
-      delta[lane] = ahead[2];
-      delta[32 + lane] = ahead[3];
-      __syncwarp();
-      if (++i == end) { i = first; ++head; }
-      if (it + 1 < n) fetch();
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s), (uint32_t)it & 1u, &abort_flag, limit));
-      if (!alive) break;
-      uint32_t s[64], w[32];
-      tc_fence_after();
-      tm_load32(t_s, s);
-      tm_load32(t_s + 32, s + 32);
-      tm_load_wait();
-      after_load(s);
-      after_load(s + 32);
-#pragma unroll
-      for (int e = 0; e < 64; e += 4) {
-        const float4 l = *reinterpret_cast<const float4*>(lse + e);
-        const float2 x = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, pair(l.x, l.y)));
-        const float2 y = parts(fma2(pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c2, pair(l.z, l.w)));
-        s[e] = __float_as_uint(exp2_approx(x.x));
-        s[e + 1] = __float_as_uint(exp2_approx(x.y));
-        s[e + 2] = __float_as_uint(exp2_approx(y.x));
-        s[e + 3] = __float_as_uint(exp2_approx(y.y));
-      }
-      if (edge) {
-#pragma unroll
-        for (int e = 0; e < 64; ++e) s[e] = col0 + e < from || col0 + e > last ? 0u : s[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 64; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-      tm_store32(t_s, w);
-      tm_store_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_p));
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), (uint32_t)it & 1u, &abort_flag, limit));
-      if (!alive) break;
-      tc_fence_after();
-      uint32_t d[64];
-      tm_load32(t_dp, d);
-      tm_load32(t_dp + 32, d + 32);
-      tm_load_wait();
-      after_load(d);
-      after_load(d + 32);
-#pragma unroll
-      for (int e = 0; e < 64; e += 4) {
-        const float4 l = *reinterpret_cast<const float4*>(delta + e);
-        const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
-                                    add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pair(l.x, l.y))));
-        const float2 y = parts(mul2(pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])),
-                                    add2(pair(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])), pair(l.z, l.w))));
-        d[e] = __float_as_uint(x.x); d[e + 1] = __float_as_uint(x.y);
-        d[e + 2] = __float_as_uint(y.x); d[e + 3] = __float_as_uint(y.y);
-      }
-      if (edge) {                           // (zero times what the products hold there need not be zero)
-#pragma unroll
-        for (int e = 0; e < 64; ++e) d[e] = col0 + e < from || col0 + e > last ? 0u : d[e];
-      }
-#pragma unroll
-      for (int e = 0; e < 64; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1]));
-      tm_store32(t_dp, w);
-      tm_store_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cta(smem_u32(&bar_ds));
-    }
-    if (alive) {
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), 0, &abort_flag, limit));
-      if (alive) {
+    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+      const Unit x = unit_of(p, kv_heads, u);
+      const Extent ext = extent_of(x.tile);
+      int head = x.head * p.group, i = ext.first;
+      float ahead[4];
+      auto fetch = [&] {
+  #pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int pos = i * TILE + col0 + h * 32 + lane;
+          const int64_t at = (int64_t)head * p.tokens + x.tile.start + pos;
+          ahead[h] = pos < x.tile.length ? -LOG2_E * p.lse[at] : 0.f;
+          ahead[2 + h] = pos < x.tile.length ? -p.delta[at] : 0.f;
+        }
+      };
+      fetch();
+      for (int it = 0; it < ext.n; ++it, ++step) {
+        const bool edge = i == ext.first || (i == ext.end - 1 && ext.tail < TILE);       // some of the tile's pairs do not count
+        const int last = x.tile.length - i * TILE - 1;                         // columns from .. last count
+        const int from = i == ext.first ? row : 0;
+        __syncwarp();
+        lse[lane] = ahead[0];
+        lse[32 + lane] = ahead[1];
+        delta[lane] = ahead[2];
+        delta[32 + lane] = ahead[3];
+        __syncwarp();
+        if (++i == ext.end) { i = ext.first; ++head; }
+        if (it + 1 < ext.n) fetch();
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s), step & 1u, &abort_flag, limit));
+        if (!alive) break;
+        uint32_t s[64], w[32];
         tc_fence_after();
-        const int pos = tile.offset + row;
-        const bool ok = pos < tile.length;
-        const int64_t at = (((int64_t)tile.start + (ok ? pos : 0)) * kv_heads + kv_head) * p.dim;
-        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(half ? p.out : p.out2) + at;
-        const bool wide = (p.dim & 15) == 0 && (((uintptr_t)p.out | (uintptr_t)p.out2) & 31) == 0;
-        store_columns(t_lane + (half ? TM_DK : TM_DV), out, 0, DP, p.dim, half ? p.scale : 1.0f, ok, wide);
+        tm_load32(t_s, s);
+        tm_load32(t_s + 32, s + 32);
+        tm_load_wait();
+        after_load(s);
+        after_load(s + 32);
+  #pragma unroll
+        for (int e = 0; e < 64; e += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(lse + e);
+          const float2 x = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, pair(l.x, l.y)));
+          const float2 y = parts(fma2(pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c2, pair(l.z, l.w)));
+          s[e] = __float_as_uint(exp2_approx(x.x));
+          s[e + 1] = __float_as_uint(exp2_approx(x.y));
+          s[e + 2] = __float_as_uint(exp2_approx(y.x));
+          s[e + 3] = __float_as_uint(exp2_approx(y.y));
+        }
+        if (edge) {
+  #pragma unroll
+          for (int e = 0; e < 64; ++e) s[e] = col0 + e < from || col0 + e > last ? 0u : s[e];
+        }
+  #pragma unroll
+        for (int e = 0; e < 64; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+        tm_store32(t_s, w);
+        tm_store_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(smem_u32(&bar_p));
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), step & 1u, &abort_flag, limit));
+        if (!alive) break;
+        tc_fence_after();
+        uint32_t d[64];
+        tm_load32(t_dp, d);
+        tm_load32(t_dp + 32, d + 32);
+        tm_load_wait();
+        after_load(d);
+        after_load(d + 32);
+  #pragma unroll
+        for (int e = 0; e < 64; e += 4) {
+          const float4 l = *reinterpret_cast<const float4*>(delta + e);
+          const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
+                                      add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pair(l.x, l.y))));
+          const float2 y = parts(mul2(pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])),
+                                      add2(pair(__uint_as_float(d[e + 2]), __uint_as_float(d[e + 3])), pair(l.z, l.w))));
+          d[e] = __float_as_uint(x.x); d[e + 1] = __float_as_uint(x.y);
+          d[e + 2] = __float_as_uint(y.x); d[e + 3] = __float_as_uint(y.y);
+        }
+        if (edge) {                           // (zero times what the products hold there need not be zero)
+  #pragma unroll
+          for (int e = 0; e < 64; ++e) d[e] = col0 + e < from || col0 + e > last ? 0u : d[e];
+        }
+  #pragma unroll
+        for (int e = 0; e < 64; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1]));
+        tm_store32(t_dp, w);
+        tm_store_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(smem_u32(&bar_ds));
+      }
+      if (alive) {
+        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), turn, &abort_flag, limit));
+        if (alive) {
+          tc_fence_after();
+          const int pos = x.tile.offset + row;
+          const bool ok = pos < x.tile.length;
+          const int64_t at = (((int64_t)x.tile.start + (ok ? pos : 0)) * kv_heads + x.head) * p.dim;
+          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(half ? p.out : p.out2) + at;
+          const bool wide = (p.dim & 15) == 0 && (((uintptr_t)p.out | (uintptr_t)p.out2) & 31) == 0;
+          store_columns(t_lane + (half ? TM_DK : TM_DV), out, 0, DP, p.dim, half ? p.scale : 1.0f, ok, wide);
+        }
       }
     }
   }
@@ -967,11 +1123,11 @@ bool encode(CUtensorMap* map, const void* x, int64_t tokens, int64_t heads, int6
 }
 
 template <int DP>
-cudaError_t run_forward(cudaStream_t st, const Maps4& m, const AttnParams& p, int64_t units) {
+cudaError_t run_forward(cudaStream_t st, const Maps4& m, const AttnParams& p) {
   static std::atomic<uint64_t> allowed{0};
   const cudaError_t e = allow_smem(attn_fwd_kernel<DP>, (int)FwdShape<DP>::SMEM, &allowed);
   if (e != cudaSuccess) return e;
-  return launch_dependent(attn_fwd_kernel<DP>, (unsigned)units, FWD_THREADS, FwdShape<DP>::SMEM, st, m, p);
+  return launch_dependent(attn_fwd_kernel<DP>, (unsigned)(p.n_tiles * p.heads), FWD_THREADS, FwdShape<DP>::SMEM, st, m, p);
 }
 
 template <int DP>
@@ -980,12 +1136,14 @@ cudaError_t run_backward(cudaStream_t st, const Maps4& m, AttnParams p, const At
   cudaError_t e = allow_smem(attn_dq_kernel<DP>, (int)BackShape<DP>::SMEM, &allowed);
   if (e == cudaSuccess) e = allow_smem(attn_dkv_kernel<DP>, (int)BackShape<DP>::SMEM, &allowed2);
   if (e != cudaSuccess) return e;
+  p.n_tiles = (int)a.n_tiles;
   p.tiles = a.query_tiles;
   p.out = a.dq;
   e = launch_dependent(attn_dq_kernel<DP>, (unsigned)(a.n_tiles * a.heads), ATTN_THREADS, BackShape<DP>::SMEM, st, m, p);
   if (e != cudaSuccess) return e;
   p.withhold = 0;
   p.tiles = a.key_tiles;
+  p.section /= p.group;
   p.out = a.dk;
   p.out2 = a.dv;
   return launch_dependent(attn_dkv_kernel<DP>, (unsigned)(a.n_tiles * a.kv_heads), ATTN_THREADS, BackShape<DP>::SMEM, st, m, p);
@@ -1001,6 +1159,10 @@ bool prepare(const AttnArgs& a, Maps4* m, AttnParams* p) {
   p->status = a.status;
   p->wait_limit_ns = a.wait_limit_ns ? a.wait_limit_ns : 2000000000ull;
   p->withhold = a.withhold;
+  // key heads whose keys and values (backward: and queries and gradients, about as much again for each head of the group) stay in L2 together
+  const int64_t bytes = a.tokens * a.dim * 4 * (a.g ? 1 + p->group : 1);
+  const int64_t some = SECTION_BYTES / (bytes > 0 ? bytes : 1);
+  p->section = (int)(some < 1 ? 1 : some < a.kv_heads ? some : a.kv_heads) * p->group;
   return encode(&m->q, a.q, a.tokens, a.heads, a.dim, a.q_ts, a.q_hs) && encode(&m->k, a.k, a.tokens, a.kv_heads, a.dim, a.k_ts, a.k_hs) &&
          encode(&m->v, a.v, a.tokens, a.kv_heads, a.dim, a.v_ts, a.v_hs) &&
          (!a.g || encode(&m->g, a.g, a.tokens, a.heads, a.dim, a.g_ts, a.g_hs));
@@ -1019,7 +1181,8 @@ cudaError_t launch_attention(cudaStream_t st, const AttnArgs& a, const char** wh
   *what = "launch of the attention kernel";
   p.tiles = a.pair_tiles;
   p.out = a.o_out;
-  return a.dim <= 64 ? run_forward<64>(st, m, p, a.n_pairs * a.heads) : run_forward<128>(st, m, p, a.n_pairs * a.heads);
+  p.n_tiles = (int)a.n_pairs;
+  return a.dim <= 64 ? run_forward<64>(st, m, p) : run_forward<128>(st, m, p);
 }
 
 cudaError_t launch_attention_backward(cudaStream_t st, const AttnArgs& a, const char** what) {
