@@ -37,7 +37,7 @@ constexpr uint32_t SLAB = TILE * 128;         // 128 rows of 64 bf16, swizzled
 constexpr uint32_t HALF = 64;
 constexpr int64_t SECTION_BYTES = 32 << 20;   // of L2's 126 MB: what a section's units read again and again
 constexpr float LN2 = 0.6931471805599453f, LOG2_E = 1.4426950408889634f;
-constexpr int POLY_OF = 100;                    // forward: one in so many pairs of exponentials by polynomial
+constexpr int POLY_OF = 4;                    // forward: one in so many pairs of exponentials by polynomial
 constexpr float MOST = 65536.0f;              // sum of 64 weights that makes a row's reference move
 
 struct Maps4 { CUtensorMap q, k, v, g; };     // g: do
@@ -377,7 +377,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   constexpr int STAGES = Sh::STAGES;
   constexpr uint32_t OPERAND = Sh::OPERAND;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_q, bar_qempty, bar_full[STAGES], bar_empty[STAGES], bar_s[2], bar_p[2][2], bar_o[2];
+  __shared__ __align__(8) uint64_t bar_q[2], bar_qempty[2], bar_full[STAGES], bar_empty[STAGES], bar_s[2], bar_p[2][2], bar_o[2];
   __shared__ __align__(16) uint4 next_answer[2];
   __shared__ __align__(8) uint64_t bar_next[2], bar_taken[2];
   __shared__ uint32_t tmem_base_slot;
@@ -390,13 +390,13 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   const uint32_t ring = smem_base + 2 * OPERAND;
   const uint64_t limit = p.wait_limit_ns;
   auto init_barriers = [&] {
-    mbar_init(smem_u32(&bar_q), 1);
-    mbar_init(smem_u32(&bar_qempty), 1);
     for (int s = 0; s < STAGES; ++s) {
       mbar_init(smem_u32(&bar_full[s]), 1);
       mbar_init(smem_u32(&bar_empty[s]), 1);
     }
     for (int t = 0; t < 2; ++t) {
+      mbar_init(smem_u32(&bar_q[t]), 1);
+      mbar_init(smem_u32(&bar_qempty[t]), 1);
       mbar_init(smem_u32(&bar_s[t]), 1);
       mbar_init(smem_u32(&bar_p[t][0]), 4);
       mbar_init(smem_u32(&bar_p[t][1]), 4);
@@ -421,13 +421,12 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   if (warp == COPY_WARP) {
     if (lane == 0 && !(p.withhold && blockIdx.x == 0)) {
       Pipe at;
-      uint32_t turn = 0;
+      uint32_t turn[2] = {0, 0};
       bool alive = true;
-      for (int u = blockIdx.x; u >= 0; u = alive ? take<false>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+      for (int u = blockIdx.x; u >= 0; u = alive ? take<false>(next, &abort_flag, limit) : -1) {
         const Unit x = unit_of(p, p.heads, u);
         const Extent e = extent_of(x.tile);
         const int kv_head = x.head / p.group;
-        const int first_row = x.tile.start + x.tile.offset;
         for (int k = 0; k < 2 * e.n; ++k) {
           alive = mbar_wait_cta(smem_u32(&bar_empty[at.stage]), at.phase ^ 1u, &abort_flag, limit);
           if (!alive) break;
@@ -435,14 +434,16 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
           mbar_expect_tx(bar, OPERAND);
           load_tile<DP>(ring + at.stage * OPERAND, (k & 1) ? &maps.v : &maps.k, bar, kv_head, x.tile.start + (k >> 1) * TILE);
           at.next<STAGES>();
-          if (k == 0) {                       // the queries' place is free once the last scores of the unit before are complete
-            alive = mbar_wait_cta(smem_u32(&bar_qempty), turn ^ 1u, &abort_flag, limit);
-            if (!alive) break;
-            mbar_expect_tx(smem_u32(&bar_q), (e.n_b ? 2u : 1u) * OPERAND);
-            load_tile<DP>(smem_base, &maps.q, smem_u32(&bar_q), x.head, first_row);
-            if (e.n_b) load_tile<DP>(smem_base + OPERAND, &maps.q, smem_u32(&bar_q), x.head, first_row + TILE);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {       // the queries' places are free once the last scores of the unit before are complete
+            if (k > 0 || !alive || (t && !e.n_b)) continue;
+            alive = mbar_wait_cta(smem_u32(&bar_qempty[t]), turn[t] ^ 1u, &abort_flag, limit);
+            if (!alive) continue;
+            turn[t] ^= 1u;
+            mbar_expect_tx(smem_u32(&bar_q[t]), OPERAND);
+            load_tile<DP>(smem_base + t * OPERAND, &maps.q, smem_u32(&bar_q[t]), x.head, x.tile.start + x.tile.offset + t * TILE);
           }
-          if (k == 2 * e.n - 2) alive = ask(next, &abort_flag, limit);
+          if (alive && k == 2 * e.n - 2) alive = ask(next, &abort_flag, limit);
           if (!alive) break;
         }
       }
@@ -450,66 +451,89 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   } else if (warp == MMA_WARP) {
     const uint32_t leader = elect_leader();
     // Order: scores of key tile 0 for both query tiles; then per key tile j and query tile: p v of j, scores of j + 1.  Products
-    // of one thread complete in order, so scores of j + 1 may overwrite the p of j that the product before them reads.
+    // of one thread complete in order, so scores of j + 1 may overwrite the p of j that the product before them reads.  The first
+    // query tile has a key tile less than the second: while the last one's weights are made, it starts on the next unit.
     Pipe at;                                  // of the tile that is waited for next
-    auto arrived = [&]() { return __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_full[at.stage]), at.phase, &abort_flag, limit)); };
-    uint32_t turn = 0, turn_p[2] = {0, 0};
-    bool alive = true;
-    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1, turn ^= 1u) {
-      const Extent x = extent_of(unit_of(p, p.heads, u).tile);
-      const int n_t[2] = {x.n_a, x.n_b};
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_q), turn, &abort_flag, limit)) && arrived();
-      if (!alive) break;
-      tc_fence_after();
-      uint32_t k_stage = at.stage;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(bar), parity, &abort_flag, limit));
+    };
+    auto arrived = [&](uint32_t* stage) {
+      if (!wait(&bar_full[at.stage], at.phase)) return false;
+      *stage = at.stage;
       at.next<STAGES>();
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (!n_t[t]) continue;
-        scores<DP>(leader, tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
-        mma_commit(leader, smem_u32(&bar_s[t]));
-      }
+      return true;
+    };
+    uint32_t turn_q[2] = {0, 0}, turn_p[2] = {0, 0}, k_stage = 0, v_stage = 0;
+    // scores of a unit's key tile (the last one: the queries' place is free then)
+    auto score = [&](int t, bool last) {
+      scores<DP>(leader, tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
+      mma_commit(leader, smem_u32(&bar_s[t]));
+      if (last) mma_commit(leader, smem_u32(&bar_qempty[t]));
+    };
+    auto start = [&](int t, int n_t) {
+      if (!wait(&bar_q[t], turn_q[t])) return false;
+      turn_q[t] ^= 1u;
+      tc_fence_after();
+      score(t, n_t == 1);
+      return true;
+    };
+    bool alive = true, ahead = false;         // ahead: the unit's first scores are under way
+    int u = blockIdx.x;
+    Extent x = extent_of(unit_of(p, p.heads, u).tile);
+    while (u >= 0) {
+      if (!ahead) alive = arrived(&k_stage) && start(0, x.n_a);
+      ahead = false;
+      if (alive && x.n_b) alive = start(1, x.n_b);
+      if (!alive) break;
       mma_commit(leader, smem_u32(&bar_empty[k_stage]));
-      if (x.n == 1) mma_commit(leader, smem_u32(&bar_qempty));
-      for (int j = 0; alive && j < x.n; ++j) {
-        alive = arrived();
+      int u_next = -1;
+      Extent y = x;
+      bool known = false;
+      for (int j = 0; j < x.n; ++j) {
+        alive = arrived(&v_stage);
         if (!alive) break;
-        const uint32_t v_stage = at.stage;
-        at.next<STAGES>();
         if (j == x.n - 1 && x.tail < TILE) zero_rows<DP>(ring + v_stage * OPERAND, x.tail, lane);
-        if (j + 1 < x.n) {
-          alive = arrived();
-          if (!alive) break;
-          k_stage = at.stage;
-          at.next<STAGES>();
-        }
+        if (j + 1 < x.n) alive = arrived(&k_stage);
+        if (!alive) break;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if (j >= n_t[t]) continue;
+          const int n_t = t ? x.n_b : x.n_a;
+          if (j >= n_t || !alive) continue;
+          if (t == 1 && j + 1 == x.n) {
+            u_next = take<true>(next, &abort_flag, limit);
+            known = true;
+            if (u_next >= 0) {
+              y = extent_of(unit_of(p, p.heads, u_next).tile);
+              alive = arrived(&k_stage) && start(0, y.n_a);
+              ahead = alive;
+            }
+            if (!alive) continue;
+          }
           const uint32_t sums = tm + TM_O + t * DP, weights = tm + t * 128, values = ring + v_stage * OPERAND;
-          alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t][0]), turn_p[t], &abort_flag, limit));
           // (at the unit's start both halves of the row warps: they have read the sums of the unit before)
-          if (alive && j == 0) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t][1]), turn_p[t], &abort_flag, limit));
-          if (!alive) break;
+          alive = wait(&bar_p[t][0], turn_p[t]) && (j > 0 || wait(&bar_p[t][1], turn_p[t]));
+          if (!alive) continue;
           tc_fence_after();
           weigh_half<DP>(leader, sums, weights, values, 0, j > 0);
-          alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p[t][1]), turn_p[t], &abort_flag, limit));
-          if (!alive) break;
+          alive = wait(&bar_p[t][1], turn_p[t]);
+          if (!alive) continue;
           tc_fence_after();
           weigh_half<DP>(leader, sums, weights + HALF, values, 1, true);
           turn_p[t] ^= 1u;
-          if (j + 1 < n_t[t]) {
-            scores<DP>(leader, tm + t * 128, smem_base + t * OPERAND, ring + k_stage * OPERAND);
-            mma_commit(leader, smem_u32(&bar_s[t]));
-          } else {
-            mma_commit(leader, smem_u32(&bar_o[t]));
-          }
+          if (j + 1 < n_t) score(t, j + 2 == n_t);
+          else mma_commit(leader, smem_u32(&bar_o[t]));
         }
         if (!alive) break;
         mma_commit(leader, smem_u32(&bar_empty[v_stage]));
         if (j + 1 < x.n) mma_commit(leader, smem_u32(&bar_empty[k_stage]));
-        if (j + 2 == x.n) mma_commit(leader, smem_u32(&bar_qempty));
       }
+      if (!alive) break;
+      if (!known) {
+        u_next = take<true>(next, &abort_flag, limit);
+        if (u_next >= 0) y = extent_of(unit_of(p, p.heads, u_next).tile);
+      }
+      u = u_next;
+      x = y;
     }
   } else {
     // A row belongs to two threads, each with half of its columns: warps 0-3 and 4-7 (first tile), 8-11 and 12-15 (second).
