@@ -37,7 +37,7 @@ constexpr uint32_t SLAB = TILE * 128;         // 128 rows of 64 bf16, swizzled
 constexpr uint32_t HALF = 64;
 constexpr int64_t SECTION_BYTES = 32 << 20;   // of L2's 126 MB: what a section's units read again and again
 constexpr float LN2 = 0.6931471805599453f, LOG2_E = 1.4426950408889634f;
-constexpr int POLY_OF = 4;                    // forward: one in so many pairs of exponentials by polynomial
+constexpr int ASK_AHEAD = 3;                  // steps from its end at which a unit asks for the next
 constexpr float MOST = 65536.0f;              // sum of 64 weights that makes a row's reference move
 
 struct Maps4 { CUtensorMap q, k, v, g; };     // g: do
@@ -204,24 +204,6 @@ __device__ __forceinline__ float log2_approx(float x) {
   return y;
 }
 
-// 2^x on the floating-point pipes instead of the special-function unit, which gives 16 results a cycle where a tile's products leave time for
-// 8 to 16: x = n + f with n the nearest integer, 2^f by the polynomial of degree 5 with the least largest relative error on
-// [-1/2, 1/2] (Remez exchange: 1.6e-7 with the coefficients in float32), n added to the exponent.  Below 2^-127 it gives
-// less than 2^-148, which is 0 in bf16; NaN does not pass.
-__device__ __forceinline__ float2 exp2_pair(Pair x) {
-  const float2 q = parts(x);
-  const Pair y = pair(fmaxf(q.x, -127.0f), fmaxf(q.y, -127.0f));
-  const Pair t = add2(y, both(12582912.0f));                     // 1.5 2^23: the integer ends up in the low bits
-  const Pair f = add2(y, mul2(add2(t, both(-12582912.0f)), both(-1.0f)));
-  Pair p = fma2(f, both(0.00132764725f), both(0.00967554096f));
-  p = fma2(p, f, both(0.0555071309f));
-  p = fma2(p, f, both(0.240221202f));
-  p = fma2(p, f, both(0.693146944f));
-  p = fma2(p, f, both(1.00000012f));
-  const float2 v = parts(p), n = parts(t);
-  return make_float2(__int_as_float(__float_as_int(v.x) + (__float_as_int(n.x) << 23)),
-                     __int_as_float(__float_as_int(v.y) + (__float_as_int(n.y) << 23)));
-}
 // Whether any thread of the two warps that share a tile's rows says so (barrier `id`; both take the same turns).
 __device__ __forceinline__ bool either(int id, bool x) {
   uint32_t r;
@@ -443,7 +425,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
             mbar_expect_tx(smem_u32(&bar_q[t]), OPERAND);
             load_tile<DP>(smem_base + t * OPERAND, &maps.q, smem_u32(&bar_q[t]), x.head, x.tile.start + x.tile.offset + t * TILE);
           }
-          if (alive && k == 2 * e.n - 2) alive = ask(next, &abort_flag, limit);
+          if (alive && k == (e.n > ASK_AHEAD ? 2 * (e.n - ASK_AHEAD) : 0)) alive = ask(next, &abort_flag, limit);
           if (!alive) break;
         }
       }
@@ -596,14 +578,9 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
           const Pair x = fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, shift);
-          float2 y;
-          if ((e >> 1) % POLY_OF == POLY_OF - 1) {
-            y = exp2_pair(x);
-          } else {
-            y = parts(x);
-            y.x = exp2_approx(y.x);
-            y.y = exp2_approx(y.y);
-          }
+          float2 y = parts(x);
+          y.x = exp2_approx(y.x);
+          y.y = exp2_approx(y.y);
           sum[(e >> 1) & 1] = add2(sum[(e >> 1) & 1], pair(y.x, y.y));
           w[h * 16 + (e >> 1)] = pack_bf16x2(y.x, y.y);
         }
@@ -732,7 +709,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
           mbar_expect_tx(smem_u32(&bar_vfull[at.stage]), OPERAND);
           load_tile<DP>(s_v + at.stage * OPERAND, &maps.v, smem_u32(&bar_vfull[at.stage]), kv_head, x.tile.start + j * TILE);
           at.next<STAGES>();
-          if (j == n - 1) alive = ask(next, &abort_flag, limit);
+          if (j == (n > ASK_AHEAD ? n - ASK_AHEAD : 0)) alive = ask(next, &abort_flag, limit);
           if (!alive) break;
         }
       }
@@ -956,7 +933,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
           load_tile<DP>(s_g + at.stage * OPERAND, &maps.g, smem_u32(&bar_gfull[at.stage]), head, x.tile.start + i * TILE);
           at.next<STAGES>();
           if (++i == e.end) { i = e.first; ++head; }
-          if (it == e.n - 1) alive = ask(next, &abort_flag, limit);
+          if (it == (e.n > ASK_AHEAD ? e.n - ASK_AHEAD : 0)) alive = ask(next, &abort_flag, limit);
           if (!alive) break;
         }
       }

@@ -3,11 +3,12 @@
 //   out_t = scale table[id_t],      dtable[v] = scale sum over the tokens t with id_t = v of dout_t   (every row v, in 32 bits, in
 //   the order of the tokens)
 //
-// Both are bound by memory.  The gradient needs the tokens of a row together: (id, token) pairs are sorted, blocks of SORT_BLOCK
-// in shared memory, then merged by counting, for each pair, the smaller ones in the other sorted blocks.  A row's
-// sum is one warp's, 256 columns at a time, when it has up to HOT tokens.  Longer runs are cut at every HOT-th place of the
-// sorted order, each piece summed by a warp of its own into scratch, and a last kernel adds the pieces in order: so a token that
-// fills half of the batch does not hold up a single warp, and the sums do not depend on which warp runs first.
+// Both are bound by memory.  The gradient needs the tokens of a row together: (id, token) pairs are sorted, blocks of EMB_SORT_BLOCK in
+// shared memory (a warp sorts 64 in registers, then runs are merged two by two), then EMB_MERGE blocks at a time by counting,
+// for each pair, the smaller ones in the other sorted blocks.  The sorted order is cut into chunks of EMB_CHUNK pairs; a warp adds up a chunk, 256
+// columns at a time, and writes the rows whose tokens are all in it.  A row that goes on in the next chunk leaves a partial sum per
+// chunk, and a last kernel adds those in order: so a token that fills half of the batch does not hold up a single warp, and the
+// sums do not depend on which warp runs first.  Rows without a token are zeroed by warps of their own.
 #include "internal.h"
 
 namespace muloco {
@@ -23,45 +24,50 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return 
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int SLICE = 256;                     // columns that a warp works on at a time, 8 a lane
-constexpr int HOT = EMB_CHUNK;
+constexpr int CHUNK = EMB_CHUNK;
+static_assert(CHUNK == 32, "a pair per lane");
 
 // 8 entries of a slice in a lane: neighbours in 16-byte accesses (WIDE), or every 32nd.
 template <typename T> struct alignas(16) Vec16 { T v[16 / sizeof(T)]; };
-
-template <typename T, bool WIDE>
-__device__ __forceinline__ void load8(float (&f)[8], const T* p, int col, int d, int lane) {
-  if (WIDE) {
-    constexpr int V = 16 / sizeof(T);
+template <typename T, bool WIDE> struct Eight;
+template <typename T> struct Eight<T, true> {
+  static constexpr int V = 16 / sizeof(T);
+  Vec16<T> x[8 / V];
+  __device__ __forceinline__ void load(const T* p, int col, int d, int lane) {
 #pragma unroll
-    for (int i = 0; i < 8; i += V) {
-      Vec16<T> x;
-      if (col + lane * 8 < d) x = *reinterpret_cast<const Vec16<T>*>(p + col + lane * 8 + i);
+    for (int i = 0; i < 8 / V; ++i) {
+      if (col + lane * 8 < d) x[i] = *reinterpret_cast<const Vec16<T>*>(p + col + lane * 8 + i * V);
+      else {
 #pragma unroll
-      for (int k = 0; k < V; ++k) f[i + k] = col + lane * 8 < d ? to_f32(x.v[k]) : 0.f;
+        for (int k = 0; k < V; ++k) x[i].v[k] = from_f32<T>(0.f);
+      }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = col + i * 32 + lane < d ? to_f32(p[col + i * 32 + lane]) : 0.f;
   }
-}
-template <typename T, bool WIDE>
-__device__ __forceinline__ void store8(const float (&f)[8], T* p, int col, int d, int lane) {
-  if (WIDE) {
-    constexpr int V = 16 / sizeof(T);
+  __device__ __forceinline__ float at(int i) const { return to_f32(x[i / V].v[i % V]); }
+  __device__ __forceinline__ static void store(const float (&f)[8], T* p, int col, int d, int lane) {
     if (col + lane * 8 >= d) return;
 #pragma unroll
-    for (int i = 0; i < 8; i += V) {
-      Vec16<T> x;
+    for (int i = 0; i < 8 / V; ++i) {
+      Vec16<T> y;
 #pragma unroll
-      for (int k = 0; k < V; ++k) x.v[k] = from_f32<T>(f[i + k]);
-      *reinterpret_cast<Vec16<T>*>(p + col + lane * 8 + i) = x;
+      for (int k = 0; k < V; ++k) y.v[k] = from_f32<T>(f[i * V + k]);
+      *reinterpret_cast<Vec16<T>*>(p + col + lane * 8 + i * V) = y;
     }
-  } else {
+  }
+};
+template <typename T> struct Eight<T, false> {
+  T x[8];
+  __device__ __forceinline__ void load(const T* p, int col, int d, int lane) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = col + i * 32 + lane < d ? p[col + i * 32 + lane] : from_f32<T>(0.f);
+  }
+  __device__ __forceinline__ float at(int i) const { return to_f32(x[i]); }
+  __device__ __forceinline__ static void store(const float (&f)[8], T* p, int col, int d, int lane) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (col + i * 32 + lane < d) p[col + i * 32 + lane] = from_f32<T>(f[i]);
   }
-}
+};
 
 template <typename T, bool WIDE>
 __global__ void __launch_bounds__(THREADS)
@@ -78,15 +84,16 @@ embedding_kernel(const EmbeddingArgs a) {
   const bool ok = id >= 0 && id < a.rows;
   float f[8];
   if (ok) {
-    load8<T, WIDE>(f, reinterpret_cast<const T*>(a.table) + id * a.ld, col, a.d, lane);
+    Eight<T, WIDE> x;
+    x.load(reinterpret_cast<const T*>(a.table) + id * a.ld, col, a.d, lane);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] *= a.scale;
+    for (int i = 0; i < 8; ++i) f[i] = x.at(i) * a.scale;
   } else {
     if (lane == 0) atomicOr(a.status, ST_TOKEN);
 #pragma unroll
     for (int i = 0; i < 8; ++i) f[i] = __int_as_float(0x7fffffff);
   }
-  store8<T, WIDE>(f, reinterpret_cast<T*>(a.out) + token * a.d, col, a.d, lane);
+  Eight<T, WIDE>::store(f, reinterpret_cast<T*>(a.out) + token * a.d, col, a.d, lane);
 }
 
 // ----------------------------- sorted tokens ---------------------------------
@@ -98,31 +105,72 @@ __device__ __forceinline__ uint64_t pair_of(const EmbeddingArgs& a, int64_t t) {
   return ((uint64_t)(ok ? id : a.rows) << 32) | (uint64_t)t;
 }
 
-constexpr int SORT_THREADS = 1024;
+constexpr int SORT_THREADS = 1024, RUN = 64;   // RUN: pairs that a warp sorts in registers
 static_assert(EMB_SORT_BLOCK == 2 * SORT_THREADS, "two pairs per thread");
+
+// How many of the n pairs of a sorted run are below x (n at most `most`, a power of two).
+__device__ __forceinline__ int below_in_run(const uint64_t* p, int n, int most, uint64_t x) {
+  int k = 0;
+  for (int step = most; step; step >>= 1)
+    if (k + step <= n && p[k + step - 1] < x) k += step;
+  return k;
+}
 
 __global__ void __launch_bounds__(SORT_THREADS)
 sort_kernel(const EmbeddingArgs a, uint64_t* out) {
-  __shared__ uint64_t s[EMB_SORT_BLOCK];
+  __shared__ uint64_t s[2][EMB_SORT_BLOCK];
   grid_wait();
   grid_release();
   const int64_t first = (int64_t)blockIdx.x * EMB_SORT_BLOCK;
   const int n = (int)(a.tokens - first < EMB_SORT_BLOCK ? a.tokens - first : EMB_SORT_BLOCK);
-  int size = 64;                               // power of two that holds the block's pairs
-  while (size < n) size <<= 1;
-  for (int i = threadIdx.x; i < size; i += SORT_THREADS) s[i] = i < n ? pair_of(a, first + i) : ~0ull;
-  __syncthreads();
-  // bitonic sorting network
-  for (int k = 2; k <= size; k <<= 1)
+  const int lane = threadIdx.x & 31, run0 = (threadIdx.x >> 5) * RUN;
+  // bitonic network over 64 pairs: x[h] is pair 32 h + lane of the run
+  uint64_t x[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = run0 + 32 * h + lane;
+    x[h] = i < n ? pair_of(a, first + i) : ~0ull;
+  }
+#pragma unroll
+  for (int k = 2; k <= RUN; k <<= 1)
+#pragma unroll
     for (int j = k >> 1; j; j >>= 1) {
-      const int i = 2 * threadIdx.x - (threadIdx.x & (j - 1));
-      if (i < size) {
-        const uint64_t x = s[i], y = s[i + j];
-        if ((x > y) == ((i & k) == 0)) { s[i] = y; s[i + j] = x; }
+      if (j == 32) {                           // (k is RUN: ascending)
+        const uint64_t lo = x[0] < x[1] ? x[0] : x[1], hi = x[0] < x[1] ? x[1] : x[0];
+        x[0] = lo;
+        x[1] = hi;
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint64_t y = __shfl_xor_sync(0xffffffffu, x[h], j);
+          const bool up = ((32 * h + lane) & k) == 0, lower = (lane & j) == 0;
+          x[h] = (x[h] < y) == (up == lower) ? x[h] : y;
+        }
       }
-      __syncthreads();
     }
-  for (int i = threadIdx.x; i < n; i += SORT_THREADS) out[first + i] = s[i];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) s[0][run0 + 32 * h + lane] = x[h];
+  // merges of two runs each: a pair's place is its own in its run and the count of smaller ones in the other
+  int from = 0;
+  for (int run = RUN; run < EMB_SORT_BLOCK && run < n; run <<= 1, from ^= 1) {
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int i = threadIdx.x + h * SORT_THREADS;
+      if (i >= n) continue;                    // (only whole runs, and the last one, hold pairs)
+      const uint64_t v = s[from][i];
+      const int own = i & ~(run - 1), other = own ^ run;
+      int count = n - other;
+      count = count < 0 ? 0 : count < run ? count : run;
+      s[from ^ 1][(own & ~(2 * run - 1)) + (i - own) + below_in_run(&s[from][other], count, run, v)] = v;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int i = threadIdx.x + h * SORT_THREADS;
+    if (i < n) out[first + i] = s[from][i];
+  }
 }
 
 // How many of the n sorted pairs are below x.
@@ -135,7 +183,8 @@ __device__ __forceinline__ int64_t below(const uint64_t* p, int64_t n, uint64_t 
   return lo;
 }
 
-// Merges groups of EMB_MERGE sorted blocks of `block` pairs: a pair's place is the count of smaller ones (no two are equal).
+// Merges groups of EMB_MERGE sorted blocks of `block` pairs (a power of two): a pair's place is the count of smaller ones (no two are
+// equal).  The searches in the other blocks go step by step together, so that their loads overlap.
 __global__ void __launch_bounds__(THREADS)
 merge_kernel(const uint64_t* in, uint64_t* out, int64_t tokens, int64_t block) {
   grid_wait();
@@ -143,83 +192,119 @@ merge_kernel(const uint64_t* in, uint64_t* out, int64_t tokens, int64_t block) {
   const int64_t t = (int64_t)blockIdx.x * THREADS + threadIdx.x;
   if (t >= tokens) return;
   const uint64_t x = in[t];
-  const int64_t first = t / (block * EMB_MERGE) * (block * EMB_MERGE), own = (t - first) / block;
-  int64_t place = first + (t - first) % block;
-#pragma unroll 4
+  const int64_t first = t & ~(block * EMB_MERGE - 1), own = (t - first) / block;
+  int64_t k[EMB_MERGE], n[EMB_MERGE];
+#pragma unroll
   for (int b = 0; b < EMB_MERGE; ++b) {
-    const int64_t at = first + b * block;
-    if (b == own || at >= tokens) continue;
-    place += below(in + at, tokens - at < block ? tokens - at : block, x);
+    const int64_t left = tokens - (first + b * block);
+    n[b] = b == own || left < 0 ? 0 : left < block ? left : block;
+    k[b] = 0;
   }
+  for (int64_t step = block; step; step >>= 1) {
+    uint64_t y[EMB_MERGE];
+#pragma unroll
+    for (int b = 0; b < EMB_MERGE; ++b) y[b] = k[b] + step <= n[b] ? in[first + b * block + k[b] + step - 1] : ~0ull;
+#pragma unroll
+    for (int b = 0; b < EMB_MERGE; ++b)
+      if (y[b] < x) k[b] += step;
+  }
+  int64_t place = first + ((t - first) & (block - 1));
+#pragma unroll
+  for (int b = 0; b < EMB_MERGE; ++b) place += k[b];
   out[place] = x;
 }
 
 __device__ __forceinline__ uint32_t token_of(uint64_t x) { return (uint32_t)x; }
 __device__ __forceinline__ int64_t id_of(uint64_t x) { return (int64_t)(x >> 32); }
 
-// Sum of the gradients of pairs [from, to), 8 columns a lane.
-template <typename T, bool WIDE>
-__device__ __forceinline__ void sum_rows(float (&f)[8], const EmbeddingArgs& a, const uint64_t* pairs, int64_t from, int64_t to, int col,
-                                         int lane) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = 0.f;
-#pragma unroll 4
-  for (int64_t i = from; i < to; ++i) {
-    float g[8];
-    load8<T, WIDE>(g, reinterpret_cast<const T*>(a.dout) + (int64_t)token_of(pairs[i]) * a.ld, col, a.d, lane);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) f[k] += g[k];
-  }
+// What a chunk of the sorted order looks like from the warp that has it: a pair per lane.
+struct Piece {
+  int64_t begin;
+  int n;                                       // pairs of the chunk
+  int64_t id;                                  // of this lane's pair
+  uint32_t token;
+  int64_t first_id, last_id;
+  bool from_before, goes_on;                   // the first row's tokens began in an earlier chunk, the last one's end in a later one
+};
+__device__ __forceinline__ Piece piece_of(const EmbeddingArgs& a, const uint64_t* pairs, int64_t chunk, int lane) {
+  Piece c;
+  c.begin = chunk * CHUNK;
+  c.n = (int)(a.tokens - c.begin < CHUNK ? a.tokens - c.begin : CHUNK);
+  const uint64_t x = pairs[c.begin + (lane < c.n ? lane : c.n - 1)];
+  c.id = id_of(x);
+  c.token = token_of(x);
+  c.first_id = __shfl_sync(0xffffffffu, c.id, 0);
+  c.last_id = __shfl_sync(0xffffffffu, c.id, c.n - 1);
+  c.from_before = c.begin > 0 && id_of(pairs[c.begin - 1]) == c.first_id;
+  c.goes_on = c.begin + c.n < a.tokens && id_of(pairs[c.begin + c.n]) == c.last_id;
+  return c;
 }
 
-// Rows of the gradient (blocks 0 .. row_blocks - 1, a warp has 32 rows of a slice), pieces of long runs (the others).
+// Chunks of the sorted order (units 0 .. chunk_units - 1: a chunk and a slice each), then rows without tokens (a warp looks after 32 rows of up to
+// ZERO_COLS columns).
+constexpr int ZERO_COLS = 1024;
 template <typename T, typename O, bool WIDE>
 __global__ void __launch_bounds__(THREADS)
-gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t row_blocks) {
+gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t chunk_units, int64_t zero_units) {
   const int lane = threadIdx.x & 31;
-  const int slices = (a.d + SLICE - 1) / SLICE;
+  int64_t unit = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
   grid_wait();
   grid_release();
-  if (blockIdx.x < row_blocks) {
-    const int64_t unit = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
-    const int64_t first = unit / slices * 32;
-    if (first >= a.rows) return;
-    const int col = (int)(unit % slices) * SLICE;
-    const int64_t start = below(pairs, a.tokens, (uint64_t)(first + lane) << 32);
-    int64_t end = __shfl_down_sync(0xffffffffu, start, 1);
-    if (lane == 31) end = below(pairs, a.tokens, (uint64_t)(first + 32) << 32);
-    const int n = (int)(a.rows - first < 32 ? a.rows - first : 32);
-    for (int r = 0; r < n; ++r) {
-      const int64_t from = __shfl_sync(0xffffffffu, start, r), to = __shfl_sync(0xffffffffu, end, r);
-      if (to - from > HOT) continue;           // its pieces are summed below
-      float f[8];
-      sum_rows<T, WIDE>(f, a, pairs, from, to, col, lane);
+  if (unit < chunk_units) {
+    const int slices = (a.d + SLICE - 1) / SLICE;
+    const int64_t chunk = unit / slices;
+    const int col = (int)(unit - chunk * slices) * SLICE;
+    const Piece c = piece_of(a, pairs, chunk, lane);
+    float f[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] *= a.scale;
-      store8<O, WIDE>(f, reinterpret_cast<O*>(a.dtable) + (first + r) * a.d, col, a.d, lane);
+    for (int i = 0; i < 8; ++i) f[i] = 0.f;
+    bool open = c.from_before;                 // the row under way began in an earlier chunk
+    for (int e0 = 0; e0 < c.n; e0 += 8) {
+      Eight<T, WIDE> g[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)              // (behind the last pair: the last one's again, not used)
+        g[e].load(reinterpret_cast<const T*>(a.dout) + (int64_t)__shfl_sync(0xffffffffu, c.token, (e0 + e) & 31) * a.ld, col, a.d, lane);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (e0 + e >= c.n) break;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] += g[e].at(i);
+        const int64_t id = __shfl_sync(0xffffffffu, c.id, e0 + e);
+        const bool at_end = e0 + e + 1 == c.n;
+        if (!at_end && __shfl_sync(0xffffffffu, c.id, (e0 + e + 1) & 31) == id) continue;
+        // the row's last pair in this chunk
+        if (id < a.rows) {
+          if (open || (at_end && c.goes_on)) {
+            Eight<float, WIDE>::store(f, a.partials + (chunk * 2 + (open ? 0 : 1)) * a.d_pad, col, a.d, lane);
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= a.scale;
+            Eight<O, WIDE>::store(f, reinterpret_cast<O*>(a.dtable) + id * a.d, col, a.d, lane);
+          }
+        }
+        open = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 0.f;
+      }
     }
     return;
   }
-  const int64_t unit = (blockIdx.x - row_blocks) * WARPS + (threadIdx.x >> 5);
-  const int64_t chunk = unit / slices, begin = chunk * HOT;
-  if (begin >= a.tokens) return;
-  const int col = (int)(unit % slices) * SLICE;
-  const int64_t stop = begin + HOT < a.tokens ? begin + HOT : a.tokens;
-  const int64_t id0 = id_of(pairs[begin]), id1 = id_of(pairs[stop - 1]);
-  // lane 0, 1: start and end of the run of the first pair; lane 2, 3: of the last one's
-  const int64_t at = below(pairs, a.tokens, (uint64_t)((lane < 2 ? id0 : id1) + (lane & 1)) << 32);
-#pragma unroll
-  for (int w = 0; w < 2; ++w) {
-    const int64_t from = __shfl_sync(0xffffffffu, at, 2 * w), to = __shfl_sync(0xffffffffu, at, 2 * w + 1);
-    const int64_t id = w ? id1 : id0;
-    if (to - from <= HOT || id >= a.rows || (w && id1 == id0)) continue;
-    float f[8];
-    sum_rows<T, WIDE>(f, a, pairs, from > begin ? from : begin, to < stop ? to : stop, col, lane);
-    store8<float, WIDE>(f, a.partials + (chunk * 2 + w) * a.d_pad, col, a.d, lane);
+  unit -= chunk_units;
+  if (unit >= zero_units) return;
+  const int parts = (a.d + ZERO_COLS - 1) / ZERO_COLS;
+  const int64_t first = unit / parts * 32;
+  const int col0 = (int)(unit % parts) * ZERO_COLS, col1 = col0 + ZERO_COLS < a.d ? col0 + ZERO_COLS : a.d;
+  const int64_t start = below(pairs, a.tokens, (uint64_t)(first + lane) << 32);
+  const bool none = first + lane < a.rows && (start == a.tokens || id_of(pairs[start]) != first + lane);
+  const float zero[8] = {};
+  for (uint32_t rows = __ballot_sync(0xffffffffu, none); rows; rows &= rows - 1) {
+    O* row = reinterpret_cast<O*>(a.dtable) + (first + __ffs(rows) - 1) * a.d;
+    for (int col = col0; col < col1; col += SLICE) Eight<O, WIDE>::store(zero, row, col, a.d, lane);
   }
 }
 
-// Long runs: the block of the chunk in which one starts adds its pieces, each warp a share of them, then the warps' sums.
+// Rows whose tokens are in several chunks: the block of the chunk in which they begin adds the partial sums, each warp a share of
+// them, then the warps' sums.
 template <typename O, bool WIDE>
 __global__ void __launch_bounds__(THREADS)
 join_kernel(const EmbeddingArgs a, const uint64_t* pairs) {
@@ -228,49 +313,36 @@ join_kernel(const EmbeddingArgs a, const uint64_t* pairs) {
   const int slices = (a.d + SLICE - 1) / SLICE;
   grid_wait();
   grid_release();
-  const int64_t chunk = blockIdx.x / slices, begin = chunk * HOT;
+  const int64_t chunk = blockIdx.x / slices;
   const int col = (int)(blockIdx.x % slices) * SLICE;
-  const int64_t stop = begin + HOT < a.tokens ? begin + HOT : a.tokens;
-  // a long run that starts in this chunk is its first run or its last
-  const int64_t id0 = id_of(pairs[begin]), id1 = id_of(pairs[stop - 1]);
-#pragma unroll 1
-  for (int w = 0; w < 2; ++w) {
-    const int64_t id = w ? id1 : id0;
-    if ((w && id1 == id0) || id >= a.rows) continue;
-    if (!w && begin > 0 && id_of(pairs[begin - 1]) == id) continue;      // started before
-    // too short to be a long one: it ends in this chunk, or HOT places behind its start is another
-    if (!w && (id1 != id0 || stop == a.tokens)) continue;
-    if (w && (stop == a.tokens || id_of(pairs[stop]) != id)) continue;
-    const int64_t at = below(pairs, a.tokens, (uint64_t)(id + (lane & 1)) << 32);
-    const int64_t from = __shfl_sync(0xffffffffu, at, 0), to = __shfl_sync(0xffffffffu, at, 1);
-    if (to - from <= HOT) continue;
-    const int64_t last = (to - 1) / HOT, n = last - chunk + 1;           // pieces
-    const int64_t p0 = n * warp / WARPS, p1 = n * (warp + 1) / WARPS;
-    float f[8];
+  const Piece c = piece_of(a, pairs, chunk, lane);
+  const int64_t id = c.last_id;
+  if (!c.goes_on || id >= a.rows || (c.from_before && c.first_id == id)) return;      // (the whole block)
+  const int64_t end = below(pairs, a.tokens, (uint64_t)(id + 1) << 32);
+  const int64_t n = (end - 1) / CHUNK - chunk + 1;             // chunks of the row
+  const int64_t p0 = n * warp / WARPS, p1 = n * (warp + 1) / WARPS;
+  float f[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = 0.f;
+  for (int i = 0; i < 8; ++i) f[i] = 0.f;
 #pragma unroll 4
-    for (int64_t p = p0; p < p1; ++p) {
-      // the piece in the run's own first chunk is that chunk's first or last run, every other one its chunk's first
-      float g[8];
-      load8<float, WIDE>(g, a.partials + ((chunk + p) * 2 + (p == 0 ? w : 0)) * a.d_pad, col, a.d, lane);
+  for (int64_t p = p0; p < p1; ++p) {
+    Eight<float, WIDE> g;                      // (where it begins the row is the chunk's last, elsewhere its first)
+    g.load(a.partials + ((chunk + p) * 2 + (p == 0 ? 1 : 0)) * a.d_pad, col, a.d, lane);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] += g[i];
+    for (int i = 0; i < 8; ++i) f[i] += g.at(i);
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sums[warp][i * 32 + lane] = f[i];
+  __syncthreads();
+  if (warp == 0) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float s = 0.f;
+#pragma unroll
+      for (int k = 0; k < WARPS; ++k) s += sums[k][i * 32 + lane];
+      f[i] = s * a.scale;
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 8; ++i) sums[warp][i * 32 + lane] = f[i];
-    __syncthreads();
-    if (warp == 0) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float s = 0.f;
-#pragma unroll
-        for (int k = 0; k < WARPS; ++k) s += sums[k][i * 32 + lane];
-        f[i] = s * a.scale;
-      }
-      store8<O, WIDE>(f, reinterpret_cast<O*>(a.dtable) + id * a.d, col, a.d, lane);
-    }
+    Eight<O, WIDE>::store(f, reinterpret_cast<O*>(a.dtable) + id * a.d, col, a.d, lane);
   }
 }
 
@@ -279,15 +351,14 @@ bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 template <typename T, typename O, bool WIDE>
 cudaError_t gather(cudaStream_t st, const EmbeddingArgs& a, const uint64_t* pairs, int* launches) {
   const int64_t slices = (a.d + SLICE - 1) / SLICE;
-  const int64_t row_blocks = ((a.rows + 31) / 32 * slices + WARPS - 1) / WARPS;
-  // (up to HOT tokens no run is long)
-  const int64_t chunks = a.tokens > HOT ? (a.tokens + HOT - 1) / HOT : 0;
-  const int64_t piece_blocks = (chunks * slices + WARPS - 1) / WARPS;
+  const int64_t chunks = (a.tokens + CHUNK - 1) / CHUNK;
+  const int64_t zero_units = (a.rows + 31) / 32 * ((a.d + ZERO_COLS - 1) / ZERO_COLS);
   ++*launches;
-  cudaError_t e = launch_dependent(gather_kernel<T, O, WIDE>, (unsigned)(row_blocks + piece_blocks), THREADS, 0, st, a, pairs, row_blocks);
-  if (e != cudaSuccess || !chunks) return e;
+  cudaError_t e = launch_dependent(gather_kernel<T, O, WIDE>, (unsigned)((chunks * slices + zero_units + WARPS - 1) / WARPS), THREADS, 0, st, a, pairs,
+                                   chunks * slices, zero_units);
+  if (e != cudaSuccess || chunks < 2) return e;
   ++*launches;
-  return launch_dependent(join_kernel<O, WIDE>, (unsigned)(chunks * slices), THREADS, 0, st, a, pairs);
+  return launch_dependent(join_kernel<O, WIDE>, (unsigned)((chunks - 1) * slices), THREADS, 0, st, a, pairs);
 }
 
 template <typename T, typename O>
@@ -311,7 +382,7 @@ cudaError_t launch_embedding(cudaStream_t st, const EmbeddingArgs& a, int is_bf1
 
 size_t embedding_scratch(int64_t tokens, int64_t d) {
   const size_t pairs = (size_t)((tokens + 1) / 2 * 2) * 8;               // (a multiple of 16 bytes)
-  return 2 * pairs + (size_t)((tokens + HOT - 1) / HOT) * 2 * (size_t)((d + 3) / 4 * 4) * 4;
+  return 2 * pairs + (size_t)((tokens + CHUNK - 1) / CHUNK) * 2 * (size_t)((d + 3) / 4 * 4) * 4;
 }
 
 cudaError_t launch_embedding_backward(cudaStream_t st, const EmbeddingArgs& args, int in_bf16, int out_bf16, int* launches) {

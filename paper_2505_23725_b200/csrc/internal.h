@@ -352,14 +352,14 @@ constexpr int NORM_PARTS = MULOCO_NORM_PARTS, NORM_MAX_DIM = 32768;
 cudaError_t launch_norm(cudaStream_t st, const NormArgs& a, bool back, int is_bf16, int n_sms, int* launches);
 
 // Embedding lookup.
-constexpr int EMB_SORT_BLOCK = 2048, EMB_MERGE = 8, EMB_CHUNK = 64;
+constexpr int EMB_SORT_BLOCK = 2048, EMB_MERGE = 8, EMB_CHUNK = 32;
 struct EmbeddingArgs {
   int64_t tokens, rows, ld;                    // ld: row stride of the table (forward), of dout (backward)
   const int64_t* ids;
   const void* table; void* out;                // forward
   const void* dout; void* dtable;              // backward
   void* scratch;                               // embedding_scratch() bytes
-  float* partials;                             // in scratch: sums of the pieces of long runs, d_pad columns each
+  float* partials;                             // in scratch: two partial sums per chunk, d_pad columns each
   int32_t d, d_pad;
   float scale;
   int* status;

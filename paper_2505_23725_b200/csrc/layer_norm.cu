@@ -164,7 +164,7 @@ norm_kernel(const NormArgs a) {
 }
 
 template <typename T, int V, int E, int WPR>
-__global__ void __launch_bounds__(block_warps<WPR>() * 32)
+__global__ void __launch_bounds__(block_warps<WPR>() * 32, block_warps<WPR>() == 8 ? 2 : 1)
 norm_back_kernel(const NormArgs a) {
   constexpr int GROUPS = block_warps<WPR>() / WPR;
   __shared__ float slots[GROUPS][2][2 * WPR];
@@ -178,12 +178,26 @@ norm_back_kernel(const NormArgs a) {
 #pragma unroll
   for (int i = 0; i < E; ++i) { dw[i] = 0.f; db[i] = 0.f; }
   int turn = 0;
-  for (int64_t row = (int64_t)blockIdx.x * GROUPS + group; row < a.tokens; row += (int64_t)gridDim.x * GROUPS, turn ^= 1) {
-    Row<T, V, E> h, g, s;
+  const int64_t stride = (int64_t)gridDim.x * GROUPS;
+  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
+  // a row's tensors are on their way while the row before is joined and written
+  Row<T, V, E> h, g, s;
+  float rstd_next = 0.f, mean_next = 0.f;
+  auto fetch = [&](int64_t row) {
     load_row(g, reinterpret_cast<const T*>(a.dy) + row * a.ldy, d, lane, lanes);
     load_row(h, reinterpret_cast<const T*>(a.x) + row * a.ldx, d, lane, lanes);
+    rstd_next = a.rstd[row];
+    if (a.center) mean_next = a.mean[row];
+  };
+  auto fetch_stream = [&](int64_t row) {
     if (a.dh) load_row(s, reinterpret_cast<const T*>(a.dh) + row * a.ldr, d, lane, lanes);
-    const float rstd = a.rstd[row], mean = a.center ? a.mean[row] : 0.f;
+  };
+  if (row < a.tokens) {
+    fetch(row);
+    fetch_stream(row);
+  }
+  for (; row < a.tokens; row += stride, turn ^= 1) {
+    const float rstd = rstd_next, mean = mean_next;
     float n[E], e[E], t[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < E / V; ++c) {
@@ -202,6 +216,7 @@ norm_back_kernel(const NormArgs a) {
         t[1] += e[k];
       }
     }
+    if (row + stride < a.tokens) fetch(row + stride);
     row_sum<WPR, 2>(t, slots[group][turn], group, in_row);
     const float along = t[0] * a.inv_d, common = a.center ? t[1] * a.inv_d : 0.f;
 #pragma unroll
@@ -210,6 +225,7 @@ norm_back_kernel(const NormArgs a) {
 #pragma unroll
       for (int k = 0; k < E; ++k) e[k] += s.at(k);
     }
+    if (row + stride < a.tokens) fetch_stream(row + stride);
     store_row<T, V, E>(e, reinterpret_cast<T*>(a.dx) + row * d, d, lane, lanes);
   }
   if (!a.partials) return;
@@ -273,17 +289,20 @@ norm_join_kernel(const float* partials, int parts, int d, float* dweight, float*
 
 // ----------------------------- host ------------------------------------------
 template <typename T, int V, int E, int WPR>
-cudaError_t run(cudaStream_t st, const NormArgs& a, bool back, int n_sms, int* launches) {
-  constexpr int GROUPS = block_warps<WPR>() / WPR, THREADS = block_warps<WPR>() * 32;
+cudaError_t forward(cudaStream_t st, const NormArgs& a, int* launches) {
+  constexpr int GROUPS = block_warps<WPR>() / WPR;
+  ++*launches;
+  return launch_dependent(norm_kernel<T, V, E, WPR>, (unsigned)((a.tokens + GROUPS - 1) / GROUPS), block_warps<WPR>() * 32, 0, st, a);
+}
+
+template <typename T, int V, int E, int WPR>
+cudaError_t backward(cudaStream_t st, const NormArgs& a, int n_sms, int* launches) {
+  constexpr int GROUPS = block_warps<WPR>() / WPR;
   const int64_t needed = (a.tokens + GROUPS - 1) / GROUPS;
-  if (!back) {
-    ++*launches;
-    return launch_dependent(norm_kernel<T, V, E, WPR>, (unsigned)needed, THREADS, 0, st, a);
-  }
   const int most = n_sms * 2 < NORM_PARTS ? n_sms * 2 : NORM_PARTS;
   const int blocks = (int)(needed < most ? needed : most);
-  const size_t smem = a.partials && GROUPS > 1 ? (size_t)GROUPS * a.d * 4 : 0;      // at most 8 x 1024 floats
-  cudaError_t e = launch_dependent(norm_back_kernel<T, V, E, WPR>, (unsigned)blocks, THREADS, smem, st, a);
+  const size_t smem = a.partials && GROUPS > 1 ? (size_t)GROUPS * a.d * 4 : 0;      // at most 4096 floats
+  cudaError_t e = launch_dependent(norm_back_kernel<T, V, E, WPR>, (unsigned)blocks, block_warps<WPR>() * 32, smem, st, a);
   ++*launches;
   if (e != cudaSuccess || !a.partials) return e;
   cudaLaunchConfig_t cfg = {};
@@ -299,15 +318,25 @@ cudaError_t run(cudaStream_t st, const NormArgs& a, bool back, int n_sms, int* l
   return cudaLaunchKernelEx(&cfg, norm_join_kernel, (const float*)a.partials, blocks, (int)a.d, a.dweight, a.dbias);
 }
 
-// Entries per lane and warps per row: short rows one warp with few entries, others as many warps as 32 entries a lane take.
+// Entries per lane and warps per row.  Forward, up to 32 entries: a row's two tensors are all that a thread holds.  Backward, 16 while that
+// takes: with 32 the rows under way and the sums over tokens leave room for 8 warps on a multiprocessor.
 template <typename T, int V>
 cudaError_t choose(cudaStream_t st, const NormArgs& a, bool back, int n_sms, int* launches) {
-  if (a.d <= 256) return run<T, V, 8, 1>(st, a, back, n_sms, launches);
-  if (a.d <= 1024) return run<T, V, 32, 1>(st, a, back, n_sms, launches);
-  if (a.d <= 2048) return run<T, V, 32, 2>(st, a, back, n_sms, launches);
-  if (a.d <= 4096) return run<T, V, 32, 4>(st, a, back, n_sms, launches);
-  if (a.d <= 8192) return run<T, V, 32, 8>(st, a, back, n_sms, launches);
-  return run<T, V, 32, 32>(st, a, back, n_sms, launches);
+  if (a.d <= 256) return back ? backward<T, V, 8, 1>(st, a, n_sms, launches) : forward<T, V, 8, 1>(st, a, launches);
+  if (back) {
+    if (a.d <= 512) return backward<T, V, 16, 1>(st, a, n_sms, launches);
+    if (a.d <= 1024) return backward<T, V, 16, 2>(st, a, n_sms, launches);
+    if (a.d <= 2048) return backward<T, V, 16, 4>(st, a, n_sms, launches);
+    if (a.d <= 4096) return backward<T, V, 16, 8>(st, a, n_sms, launches);
+    if (a.d <= 8192) return backward<T, V, 16, 16>(st, a, n_sms, launches);
+    if (a.d <= 16384) return backward<T, V, 32, 16>(st, a, n_sms, launches);
+    return backward<T, V, 32, 32>(st, a, n_sms, launches);
+  }
+  if (a.d <= 1024) return forward<T, V, 32, 1>(st, a, launches);
+  if (a.d <= 2048) return forward<T, V, 32, 2>(st, a, launches);
+  if (a.d <= 4096) return forward<T, V, 32, 4>(st, a, launches);
+  if (a.d <= 8192) return forward<T, V, 32, 8>(st, a, launches);
+  return forward<T, V, 32, 32>(st, a, launches);
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
