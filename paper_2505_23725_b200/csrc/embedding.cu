@@ -27,31 +27,29 @@ constexpr int SLICE = 256;                     // columns that a warp works on a
 constexpr int CHUNK = EMB_CHUNK;
 static_assert(CHUNK == 32, "a pair per lane");
 
-// 8 entries of a slice in a lane: neighbours in 16-byte accesses (WIDE), or every 32nd.
-template <typename T> struct alignas(16) Vec16 { T v[16 / sizeof(T)]; };
+// 8 entries of a slice in a lane: twice 4 neighbours, 128 columns apart (WIDE: whole sectors are written whatever the type), or
+// every 32nd.
+template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
 template <typename T, bool WIDE> struct Eight;
 template <typename T> struct Eight<T, true> {
-  static constexpr int V = 16 / sizeof(T);
-  Vec16<T> x[8 / V];
+  Four<T> x[2];
   __device__ __forceinline__ void load(const T* p, int col, int d, int lane) {
 #pragma unroll
-    for (int i = 0; i < 8 / V; ++i) {
-      if (col + lane * 8 < d) x[i] = *reinterpret_cast<const Vec16<T>*>(p + col + lane * 8 + i * V);
-      else {
-#pragma unroll
-        for (int k = 0; k < V; ++k) x[i].v[k] = from_f32<T>(0.f);
-      }
+    for (int i = 0; i < 2; ++i) {
+      const int at = col + i * 128 + lane * 4;
+      if (at < d) x[i] = *reinterpret_cast<const Four<T>*>(p + at);
+      else x[i].v[0] = x[i].v[1] = x[i].v[2] = x[i].v[3] = from_f32<T>(0.f);
     }
   }
-  __device__ __forceinline__ float at(int i) const { return to_f32(x[i / V].v[i % V]); }
+  __device__ __forceinline__ float at(int i) const { return to_f32(x[i >> 2].v[i & 3]); }
   __device__ __forceinline__ static void store(const float (&f)[8], T* p, int col, int d, int lane) {
-    if (col + lane * 8 >= d) return;
 #pragma unroll
-    for (int i = 0; i < 8 / V; ++i) {
-      Vec16<T> y;
+    for (int i = 0; i < 2; ++i) {
+      const int at = col + i * 128 + lane * 4;
+      Four<T> y;
 #pragma unroll
-      for (int k = 0; k < V; ++k) y.v[k] = from_f32<T>(f[i * V + k]);
-      *reinterpret_cast<Vec16<T>*>(p + col + lane * 8 + i * V) = y;
+      for (int k = 0; k < 4; ++k) y.v[k] = from_f32<T>(f[i * 4 + k]);
+      if (at < d) *reinterpret_cast<Four<T>*>(p + at) = y;
     }
   }
 };
@@ -192,18 +190,19 @@ merge_kernel(const uint64_t* in, uint64_t* out, int64_t tokens, int64_t block) {
   const int64_t t = (int64_t)blockIdx.x * THREADS + threadIdx.x;
   if (t >= tokens) return;
   const uint64_t x = in[t];
-  const int64_t first = t & ~(block * EMB_MERGE - 1), own = (t - first) / block;
-  int64_t k[EMB_MERGE], n[EMB_MERGE];
+  const int64_t first = t & ~(block * EMB_MERGE - 1);
+  const int own = (int)((t - first) / block);
+  uint32_t k[EMB_MERGE], n[EMB_MERGE];
 #pragma unroll
   for (int b = 0; b < EMB_MERGE; ++b) {
     const int64_t left = tokens - (first + b * block);
-    n[b] = b == own || left < 0 ? 0 : left < block ? left : block;
+    n[b] = b == own || left < 0 ? 0 : (uint32_t)(left < block ? left : block);
     k[b] = 0;
   }
-  for (int64_t step = block; step; step >>= 1) {
+  for (uint32_t step = (uint32_t)block; step; step >>= 1) {
     uint64_t y[EMB_MERGE];
 #pragma unroll
-    for (int b = 0; b < EMB_MERGE; ++b) y[b] = k[b] + step <= n[b] ? in[first + b * block + k[b] + step - 1] : ~0ull;
+    for (int b = 0; b < EMB_MERGE; ++b) y[b] = k[b] + step <= n[b] ? in[first + b * block + (k[b] + step - 1)] : ~0ull;
 #pragma unroll
     for (int b = 0; b < EMB_MERGE; ++b)
       if (y[b] < x) k[b] += step;
@@ -240,17 +239,19 @@ __device__ __forceinline__ Piece piece_of(const EmbeddingArgs& a, const uint64_t
   return c;
 }
 
-// Chunks of the sorted order (units 0 .. chunk_units - 1: a chunk and a slice each), then rows without tokens (a warp looks after 32 rows of up to
-// ZERO_COLS columns).
+// Rows without tokens (units 0 .. zero_units - 1: a warp looks after 32 rows of up to ZERO_COLS columns), then chunks of the sorted order (a chunk and
+// a slice each).
 constexpr int ZERO_COLS = 1024;
 template <typename T, typename O, bool WIDE>
 __global__ void __launch_bounds__(THREADS)
-gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t chunk_units, int64_t zero_units) {
+gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t zero_units, int64_t chunk_units) {
   const int lane = threadIdx.x & 31;
   int64_t unit = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
   grid_wait();
   grid_release();
-  if (unit < chunk_units) {
+  if (unit >= zero_units) {
+    unit -= zero_units;
+    if (unit >= chunk_units) return;
     const int slices = (a.d + SLICE - 1) / SLICE;
     const int64_t chunk = unit / slices;
     const int col = (int)(unit - chunk * slices) * SLICE;
@@ -289,8 +290,6 @@ gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t chunk_units,
     }
     return;
   }
-  unit -= chunk_units;
-  if (unit >= zero_units) return;
   const int parts = (a.d + ZERO_COLS - 1) / ZERO_COLS;
   const int64_t first = unit / parts * 32;
   const int col0 = (int)(unit % parts) * ZERO_COLS, col1 = col0 + ZERO_COLS < a.d ? col0 + ZERO_COLS : a.d;
@@ -355,7 +354,7 @@ cudaError_t gather(cudaStream_t st, const EmbeddingArgs& a, const uint64_t* pair
   const int64_t zero_units = (a.rows + 31) / 32 * ((a.d + ZERO_COLS - 1) / ZERO_COLS);
   ++*launches;
   cudaError_t e = launch_dependent(gather_kernel<T, O, WIDE>, (unsigned)((chunks * slices + zero_units + WARPS - 1) / WARPS), THREADS, 0, st, a, pairs,
-                                   chunks * slices, zero_units);
+                                   zero_units, chunks * slices);
   if (e != cudaSuccess || chunks < 2) return e;
   ++*launches;
   return launch_dependent(join_kernel<O, WIDE>, (unsigned)((chunks - 1) * slices), THREADS, 0, st, a, pairs);
@@ -363,7 +362,7 @@ cudaError_t gather(cudaStream_t st, const EmbeddingArgs& a, const uint64_t* pair
 
 template <typename T, typename O>
 cudaError_t gather(cudaStream_t st, const EmbeddingArgs& a, const uint64_t* pairs, int* launches) {
-  const bool wide = a.d % 8 == 0 && a.ld % 8 == 0 && aligned16(a.dout) && aligned16(a.dtable);
+  const bool wide = a.d % 4 == 0 && a.ld % 4 == 0 && aligned16(a.dout) && aligned16(a.dtable);
   return wide ? gather<T, O, true>(st, a, pairs, launches) : gather<T, O, false>(st, a, pairs, launches);
 }
 
@@ -372,7 +371,7 @@ cudaError_t gather(cudaStream_t st, const EmbeddingArgs& a, const uint64_t* pair
 cudaError_t launch_embedding(cudaStream_t st, const EmbeddingArgs& a, int is_bf16) {
   const int64_t units = a.tokens * ((a.d + SLICE - 1) / SLICE);
   const unsigned blocks = (unsigned)((units + WARPS - 1) / WARPS);
-  const bool wide = a.d % 8 == 0 && a.ld % 8 == 0 && aligned16(a.table) && aligned16(a.out);
+  const bool wide = a.d % 4 == 0 && a.ld % 4 == 0 && aligned16(a.table) && aligned16(a.out);
   if (is_bf16)
     return wide ? launch_dependent(embedding_kernel<__nv_bfloat16, true>, blocks, THREADS, 0, st, a)
                 : launch_dependent(embedding_kernel<__nv_bfloat16, false>, blocks, THREADS, 0, st, a);
