@@ -11,9 +11,8 @@
 // order of the blocks.
 #include <string.h>
 
-#include <type_traits>
-
 #include "internal.h"
+#include "tc_ptx.cuh"
 
 namespace muloco {
 
@@ -163,12 +162,34 @@ norm_kernel(const NormArgs a) {
   }
 }
 
+// Rows under way in the backward pass: every lane copies the chunks that it will read itself into shared memory (cp.async), STAGES rows
+// ahead, which takes neither registers nor barriers.  Where 16 bytes are not one access, or a row is so long that two of them do not fit, rows
+// are loaded when they are needed.
+template <typename T, int V, int E, int WPR>
+struct BackShape {
+  static constexpr int THREADS = block_warps<WPR>() * 32, GROUPS = block_warps<WPR>() / WPR;
+  static constexpr int STAGES = sizeof(T) * V == 16 && WPR <= 8 ? (sizeof(T) == 2 ? 4 : 2) : 0;
+  static constexpr int STAGE = 3 * E * (int)sizeof(T) * THREADS;        // bytes: dy, h, dh
+  static size_t smem(int d, bool sums) {
+    const size_t a = (size_t)STAGES * STAGE, b = sums && GROUPS > 1 ? (size_t)GROUPS * d * 4 : 0;
+    return a > b ? a : b;
+  }
+};
+
+__device__ __forceinline__ void copy_async16(void* dst, const void* src, bool some) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(some ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 template <typename T, int V, int E, int WPR>
 __global__ void __launch_bounds__(block_warps<WPR>() * 32, block_warps<WPR>() == 8 ? 2 : 1)
 norm_back_kernel(const NormArgs a) {
-  constexpr int GROUPS = block_warps<WPR>() / WPR;
+  using Sh = BackShape<T, V, E, WPR>;
+  constexpr int GROUPS = Sh::GROUPS, STAGES = Sh::STAGES, CHUNKS = E / V;
   __shared__ float slots[GROUPS][2][2 * WPR];
-  extern __shared__ float sums[];              // [GROUPS][columns] of the block, when it has several row groups
+  extern __shared__ __align__(16) uint8_t staging[];           // rows under way, then the sums of the block's row groups
+  float* const sums = reinterpret_cast<float*>(staging);
   const int warp = threadIdx.x >> 5, group = warp / WPR, in_row = warp % WPR;
   const int lane = in_row * 32 + (threadIdx.x & 31), lanes = WPR * 32;
   const int d = a.d;
@@ -179,25 +200,49 @@ norm_back_kernel(const NormArgs a) {
   for (int i = 0; i < E; ++i) { dw[i] = 0.f; db[i] = 0.f; }
   int turn = 0;
   const int64_t stride = (int64_t)gridDim.x * GROUPS;
-  int64_t row = (int64_t)blockIdx.x * GROUPS + group;
-  // a row's tensors are on their way while the row before is joined and written
-  Row<T, V, E> h, g, s;
-  float rstd_next = 0.f, mean_next = 0.f;
-  auto fetch = [&](int64_t row) {
-    load_row(g, reinterpret_cast<const T*>(a.dy) + row * a.ldy, d, lane, lanes);
-    load_row(h, reinterpret_cast<const T*>(a.x) + row * a.ldx, d, lane, lanes);
-    rstd_next = a.rstd[row];
-    if (a.center) mean_next = a.mean[row];
+  const int64_t first = (int64_t)blockIdx.x * GROUPS + group;
+  const T* const gp = reinterpret_cast<const T*>(a.dy);
+  const T* const hp = reinterpret_cast<const T*>(a.x);
+  const T* const sp = reinterpret_cast<const T*>(a.dh);
+  using Ch = Chunk<T, V>;
+  // this thread's chunk c of tensor `which` in a stage
+  auto place = [&](int stage, int which, int c) {
+    return reinterpret_cast<Ch*>(staging + (size_t)stage * Sh::STAGE + ((size_t)(which * CHUNKS + c) * Sh::THREADS + threadIdx.x) * sizeof(Ch));
   };
-  auto fetch_stream = [&](int64_t row) {
-    if (a.dh) load_row(s, reinterpret_cast<const T*>(a.dh) + row * a.ldr, d, lane, lanes);
+  auto send = [&](int stage, int64_t row) {
+    if (row < a.tokens) {
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        const int col = column<V>(c, lane, lanes);
+        const bool in = col < d;
+        const int at = in ? col : 0;
+        copy_async16(place(stage, 0, c), gp + row * a.ldy + at, in);
+        copy_async16(place(stage, 1, c), hp + row * a.ldx + at, in);
+        if (sp) copy_async16(place(stage, 2, c), sp + row * a.ldr + at, in);
+      }
+    }
+    copy_commit();
   };
-  if (row < a.tokens) {
-    fetch(row);
-    fetch_stream(row);
+  int stage = 0;
+  if (STAGES) {
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k) send(k, first + k * stride);
   }
-  for (; row < a.tokens; row += stride, turn ^= 1) {
-    const float rstd = rstd_next, mean = mean_next;
+  for (int64_t row = first; row < a.tokens; row += stride, turn ^= 1) {
+    const float rstd = a.rstd[row], mean = a.center ? a.mean[row] : 0.f;
+    Row<T, V, E> g, h, s;
+    if (STAGES) {
+      copy_wait<STAGES ? STAGES - 1 : 0>();
+#pragma unroll
+      for (int c = 0; c < CHUNKS; ++c) {
+        g.c[c] = *place(stage, 0, c);
+        h.c[c] = *place(stage, 1, c);
+      }
+    } else {
+      load_row(g, gp + row * a.ldy, d, lane, lanes);
+      load_row(h, hp + row * a.ldx, d, lane, lanes);
+      if (sp) load_row(s, sp + row * a.ldr, d, lane, lanes);
+    }
     float n[E], e[E], t[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < E / V; ++c) {
@@ -216,18 +261,25 @@ norm_back_kernel(const NormArgs a) {
         t[1] += e[k];
       }
     }
-    if (row + stride < a.tokens) fetch(row + stride);
     row_sum<WPR, 2>(t, slots[group][turn], group, in_row);
     const float along = t[0] * a.inv_d, common = a.center ? t[1] * a.inv_d : 0.f;
 #pragma unroll
     for (int k = 0; k < E; ++k) e[k] = rstd * (e[k] - n[k] * along - common);
-    if (a.dh) {
+    if (sp) {
+      if (STAGES) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) s.c[c] = *place(stage, 2, c);
+      }
 #pragma unroll
       for (int k = 0; k < E; ++k) e[k] += s.at(k);
     }
-    if (row + stride < a.tokens) fetch_stream(row + stride);
+    if (STAGES) {                              // (this thread has read all that it copied there)
+      send(stage, row + STAGES * stride);
+      if (++stage == STAGES) stage = 0;
+    }
     store_row<T, V, E>(e, reinterpret_cast<T*>(a.dx) + row * d, d, lane, lanes);
   }
+  if (STAGES) copy_wait<0>();
   if (!a.partials) return;
   // partial sums of the block: its row groups one after the other
 #pragma unroll
@@ -297,12 +349,16 @@ cudaError_t forward(cudaStream_t st, const NormArgs& a, int* launches) {
 
 template <typename T, int V, int E, int WPR>
 cudaError_t backward(cudaStream_t st, const NormArgs& a, int n_sms, int* launches) {
-  constexpr int GROUPS = block_warps<WPR>() / WPR;
+  using Sh = BackShape<T, V, E, WPR>;
+  constexpr int GROUPS = Sh::GROUPS;
   const int64_t needed = (a.tokens + GROUPS - 1) / GROUPS;
   const int most = n_sms * 2 < NORM_PARTS ? n_sms * 2 : NORM_PARTS;
   const int blocks = (int)(needed < most ? needed : most);
-  const size_t smem = a.partials && GROUPS > 1 ? (size_t)GROUPS * a.d * 4 : 0;      // at most 4096 floats
-  cudaError_t e = launch_dependent(norm_back_kernel<T, V, E, WPR>, (unsigned)blocks, block_warps<WPR>() * 32, smem, st, a);
+  const size_t smem = Sh::smem(a.d, a.partials != nullptr);
+  static std::atomic<uint64_t> allowed{0};
+  cudaError_t e = allow_smem(norm_back_kernel<T, V, E, WPR>, 100 * 1024, &allowed);
+  if (e != cudaSuccess) return e;
+  e = launch_dependent(norm_back_kernel<T, V, E, WPR>, (unsigned)blocks, Sh::THREADS, smem, st, a);
   ++*launches;
   if (e != cudaSuccess || !a.partials) return e;
   cudaLaunchConfig_t cfg = {};
