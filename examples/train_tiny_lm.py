@@ -1,7 +1,7 @@
 """A small language model trained with MuLoCo, the whole step on the library's kernels:
 
-  forward / backward   norm of queries and keys with the rotation, gated feed-forward block (layers.py); attention, the
-                       other products and the loss are plain torch
+  forward / backward   embedding, norms with the residual sum, norm of queries and keys with the rotation, causal
+                       attention, gated feed-forward block (layers.py); the other products and the loss are plain torch
   inner step           Muon on the hidden matrices, AdamW with 8-bit states on embedding, head and gains
   outer step           every H steps, over K workers that draw their own batches
 
@@ -27,6 +27,7 @@ class Model:
         ang = torch.arange(length, device="cuda", dtype=torch.float64)[:, None] * \
             10000.0 ** (-torch.arange(self.dim // 2, device="cuda", dtype=torch.float64) * 2 / self.dim)
         self.cos, self.sin = ang.cos().float(), ang.sin().float()
+        self.batches = {}
 
     def leaves(self, theta):
         """Working copies that gather gradients: bf16 matrices, float32 gains."""
@@ -35,26 +36,24 @@ class Model:
     def loss(self, leaves, tokens):
         p = {n: leaves[i] for n, i in self.index.items()}
         B, S = tokens.shape[0], tokens.shape[1] - 1
-        pos = torch.arange(S, device="cuda").repeat(B)
+        if (B, S) not in self.batches:       # the batch's sequences, one behind the other
+            self.batches[B, S] = binding.Sequences(self.owner, [S] * B)
+        seq = self.batches[B, S]
 
-        def norm(x, gain):
-            f = x.float()
-            return (f * torch.rsqrt(f.square().mean(-1, keepdim=True) + 1e-6) * gain).to(torch.bfloat16)
+        def norm(x, gain, stream=None):
+            return layers.layer_norm(self.owner, x, p[gain].view(-1), residual=stream, center=False)
 
-        x = p["embed"][tokens[:, :-1].reshape(-1)]
-        causal = torch.ones(S, S, dtype=torch.bool, device="cuda").tril()
+        stream = layers.embedding(self.owner, tokens[:, :-1].reshape(-1), p["embed"])
+        n = norm(stream, "l0.attn_norm")
         for l in range(self.L):
-            n = norm(x, p[f"l{l}.attn_norm"])
-            q, k, v = (n @ p[f"l{l}.{w}"] for w in ("wq", "wk", "wv"))
-            q, k = layers.qk_norm_rope(self.owner, q.view(B * S, self.heads, self.dim), k.view(B * S, self.heads, self.dim),
-                                       self.cos, self.sin, pos, p[f"l{l}.q_norm"].view(-1), p[f"l{l}.k_norm"].view(-1))
-            q, k, v = (t.view(B, S, self.heads, self.dim).transpose(1, 2) for t in (q, k, v))
-            a = (q @ k.transpose(-1, -2)).float() * self.dim ** -0.5
-            a = a.masked_fill(~causal, float("-inf")).softmax(-1).to(torch.bfloat16) @ v
-            x = x + a.transpose(1, 2).reshape(B * S, self.d) @ p[f"l{l}.wo"]
-            n = norm(x, p[f"l{l}.ffn_norm"])
-            x = x + layers.gated_ffn(self.owner, n, p[f"l{l}.w1"], p[f"l{l}.w3"], p[f"l{l}.w2"])
-        logits = (norm(x, p["final_norm"]) @ p["head"]).float()
+            q, k, v = ((n @ p[f"l{l}.{w}"]).view(B * S, self.heads, self.dim) for w in ("wq", "wk", "wv"))
+            q, k = layers.qk_norm_rope(self.owner, q, k, self.cos, self.sin, seq.positions, p[f"l{l}.q_norm"].view(-1),
+                                       p[f"l{l}.k_norm"].view(-1))
+            a = layers.causal_attention(self.owner, q, k, v, seq)
+            n, stream = norm(a.view(B * S, self.d) @ p[f"l{l}.wo"], f"l{l}.ffn_norm", stream)
+            y = layers.gated_ffn(self.owner, n, p[f"l{l}.w1"], p[f"l{l}.w3"], p[f"l{l}.w2"])
+            n, stream = norm(y, f"l{l + 1}.attn_norm" if l + 1 < self.L else "final_norm", stream)
+        logits = (n @ p["head"]).float()
         return torch.nn.functional.cross_entropy(logits, tokens[:, 1:].reshape(-1))
 
 

@@ -355,8 +355,10 @@ class _Operators:
         self._fast = {}
         if fast is not None:
             for name in ("qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward", "adamw_step",
-                         "adamw_moments"):
+                         "adamw_moments", "causal_attention", "causal_attention_backward", "layer_norm",
+                         "layer_norm_backward", "embedding_lookup", "embedding_backward"):
                 self._fast[name] = (getattr(fast, name), C.cast(getattr(self.lib, "muloco_" + name), C.c_void_p).value)
+            self._scratch_size = C.cast(self.lib.muloco_embedding_scratch, C.c_void_p).value
 
     def _quick(self, name, *args):
         """The compiled form of a call: its results, or None when this one has to go the long way (an argument is not as
@@ -623,6 +625,8 @@ class _Operators:
         """The packed argument struct of a call (scale None: head_dim ** -0.5)."""
         bf16 = self._bf16
         sequences._open(self)
+        if self.ctx is None:
+            raise RuntimeError("the context is closed")
         T = sequences.tokens
         self._need("q", q, bf16, (T, None, None))
         D = q.shape[2]
@@ -635,6 +639,11 @@ class _Operators:
         """muloco_causal_attention: attention of q [tokens, query heads, head_dim] over k and v [tokens, key heads, head_dim]
         (bf16), every token over those up to it of its own sequence (`sequences`: a Sequences of this context).  Returns (o, lse): o
         like q, lse float32 [query heads, tokens], which the backward pass needs."""
+        if sequences.owner is self and sequences.handle is not None and q.dim() == 3:
+            r = self._quick("causal_attention", q, k, v, sequences.handle.value, sequences.tokens,
+                            q.shape[2] ** -0.5 if scale is None else scale)
+            if r is not None:
+                return r
         a = self._attention(q, k, v, sequences, scale)
         o = q.new_empty(q.shape)
         lse = q.new_empty((q.shape[1], q.shape[0]), dtype=self._f32)
@@ -648,6 +657,11 @@ class _Operators:
 
     def causal_attention_backward(self, do, q, k, v, o, lse, sequences, scale=None):
         """muloco_causal_attention_backward: (dq, dk, dv), bf16, from do and the forward pass's o and lse."""
+        if sequences.owner is self and sequences.handle is not None and q.dim() == 3:
+            r = self._quick("causal_attention_backward", do, q, k, v, o, lse, sequences.handle.value, sequences.tokens,
+                            q.shape[2] ** -0.5 if scale is None else scale)
+            if r is not None:
+                return r
         a = self._attention(q, k, v, sequences, scale)
         self._need("do", do, self._bf16, tuple(q.shape))
         self._need("o", o, self._bf16, tuple(q.shape), dense=True)
@@ -684,6 +698,9 @@ class _Operators:
         over the last dimension of x [tokens, d] (float32 or bfloat16; weight and bias float32); with center=False the mean is left
         where it is (root mean square norm).  Returns (y, h, rstd, mean), the last three for the backward pass; mean is
         None with center=False."""
+        r = self._quick("layer_norm", x, weight, bias, residual, eps, center)
+        if r is not None:
+            return r
         a = self._norm(x, weight, bias, residual, "residual", eps, center)
         y = x.new_empty(x.shape)
         h = x if residual is None else x.new_empty(x.shape)
@@ -702,6 +719,9 @@ class _Operators:
         """muloco_layer_norm_backward: (dx, dweight, dbias) from dy, the forward pass's h, rstd and mean (None: not centred) and the
         gradient dh that h has from elsewhere (or None).  dx is the gradient of x and of the residual.  dweight is None without a
         weight, dbias unless `bias` is set."""
+        r = self._quick("layer_norm_backward", dy, h, rstd, mean, weight, dh, bias)
+        if r is not None:
+            return r
         a = self._norm(h, weight, None, dh, "dh", 0.0, mean is not None)
         T, d = h.shape
         self._need("dy", dy, h.dtype, (T, d))
@@ -725,6 +745,9 @@ class _Operators:
     def embedding(self, ids, table, scale=1.0):
         """muloco_embedding_lookup: scale * table[ids] for ids int64 [tokens] and a table [rows, d] in float32 or bfloat16; the
         result has the table's type."""
+        r = self._quick("embedding_lookup", ids, table, scale)
+        if r is not None:
+            return r
         if table.dtype not in (self._f32, self._bf16):
             raise ValueError(f"table must be float32 or bfloat16 (got {table.dtype})")
         self._need("table", table, table.dtype, (None, None))
@@ -747,6 +770,10 @@ class _Operators:
         dtype = self._f32 if dtype is None else dtype
         if dtype not in (self._f32, self._bf16):
             raise ValueError(f"dtype must be float32 or bfloat16 (got {dtype})")
+        if self._fast:
+            r = self._quick("embedding_backward", dout, ids, rows, scale, dtype is self._bf16, self._scratch_size)
+            if r is not None:
+                return r
         if dout.dtype not in (self._f32, self._bf16):
             raise ValueError(f"dout must be float32 or bfloat16 (got {dout.dtype})")
         self._need("ids", ids, self._i64, (None,), dense=True)

@@ -260,6 +260,195 @@ PyObject* adamw_moments(PyObject*, PyObject* const* o, Py_ssize_t n) {
   return Py_BuildValue("(NN)", wrap(m), wrap(v));
 }
 
+// q, k, v; then, from index `rest`, sequences, their tokens, scale
+bool attention_of(PyObject* const* o, PyObject* const* rest, const Call& c, muloco_attention* a, const at::Tensor* (&t)[3], muloco_sequences** s) {
+  bool ok = true;
+  for (int i = 0; i < 3; ++i) {
+    t[i] = tensor(o[i], &ok);
+    if (!ok || !t[i] || !is(*t[i], c, at::kBFloat16, 3) || (t[i]->stride(2) != 1 && t[i]->size(2) > 1)) return false;
+  }
+  *s = reinterpret_cast<muloco_sequences*>(PyLong_AsVoidPtr(rest[0]));
+  const long long tokens = PyLong_AsLongLong(rest[1]);
+  const double scale = PyFloat_AsDouble(rest[2]);
+  if (PyErr_Occurred()) { PyErr_Clear(); return false; }
+  if (!*s || t[0]->size(0) != tokens || t[1]->size(0) != tokens || t[1]->size(2) != t[0]->size(2) || t[2]->sizes() != t[1]->sizes()) return false;
+  *a = muloco_attention();
+  a->heads_q = (int32_t)t[0]->size(1); a->heads_k = (int32_t)t[1]->size(1); a->head_dim = (int32_t)t[0]->size(2);
+  a->scale = (float)scale;
+  a->q = t[0]->data_ptr(); a->k = t[1]->data_ptr(); a->v = t[2]->data_ptr();
+  a->q_token_stride = t[0]->stride(0); a->q_head_stride = t[0]->stride(1);
+  a->k_token_stride = t[1]->stride(0); a->k_head_stride = t[1]->stride(1);
+  a->v_token_stride = t[2]->stride(0); a->v_head_stride = t[2]->stride(1);
+  return true;
+}
+
+PyObject* attention_forward(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  if (n != 10) return none();
+  const Call c = call_of(o);
+  muloco_attention a;
+  muloco_sequences* s;
+  const at::Tensor* t[3];
+  if (!c.ok || !attention_of(o + 4, o + 7, c, &a, t, &s)) return none();
+  at::Tensor out = at::empty(t[0]->sizes(), t[0]->options()), lse = at::empty({t[0]->size(1), t[0]->size(0)}, t[0]->options().dtype(at::kFloat));
+  const auto fn = (decltype(&muloco_causal_attention))c.fn;
+  const int st = unlocked([&] { return fn(c.ctx, &a, s, out.data_ptr(), (float*)lse.data_ptr()); });
+  if (st) return PyLong_FromLong(st);
+  return Py_BuildValue("(NN)", wrap(out), wrap(lse));
+}
+
+// do, q, k, v, o, lse, sequences, their tokens, scale
+PyObject* attention_backward(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  if (n != 13) return none();
+  const Call c = call_of(o);
+  muloco_attention a;
+  muloco_sequences* s;
+  const at::Tensor* t[3];
+  if (!c.ok || !attention_of(o + 5, o + 10, c, &a, t, &s)) return none();
+  bool ok = true;
+  const at::Tensor* g = tensor(o[4], &ok);
+  const at::Tensor* out = tensor(o[8], &ok);
+  const at::Tensor* lse = tensor(o[9], &ok);
+  if (!ok || !g || !out || !lse || !is(*g, c, at::kBFloat16, 3) || g->sizes() != t[0]->sizes() || (g->stride(2) != 1 && g->size(2) > 1) ||
+      !is(*out, c, at::kBFloat16, 3) || out->sizes() != t[0]->sizes() || !out->is_contiguous() || !is(*lse, c, at::kFloat, 2) ||
+      lse->size(0) != t[0]->size(1) || lse->size(1) != t[0]->size(0) || !lse->is_contiguous())
+    return none();
+  at::Tensor delta = at::empty(lse->sizes(), lse->options()), d[3];
+  for (int i = 0; i < 3; ++i) d[i] = at::empty(t[i]->sizes(), t[i]->options());
+  const auto fn = (decltype(&muloco_causal_attention_backward))c.fn;
+  const int st = unlocked([&] { return fn(c.ctx, &a, s, g->data_ptr(), g->stride(0), g->stride(1), out->data_ptr(), (const float*)lse->data_ptr(),
+                    (float*)delta.data_ptr(), d[0].data_ptr(), d[1].data_ptr(), d[2].data_ptr()); });
+  if (st) return PyLong_FromLong(st);
+  return Py_BuildValue("(NNN)", wrap(d[0]), wrap(d[1]), wrap(d[2]));
+}
+
+bool rows_of(const at::Tensor* t, const Call& c, at::ScalarType type, int64_t T, int64_t d) {
+  return t && is(*t, c, type, 2) && t->size(0) == T && t->size(1) == d && (d < 2 || t->stride(1) == 1);
+}
+
+// x, the residual (or its gradient), weight, bias
+bool norm_of(const at::Tensor* x, const at::Tensor* other, const at::Tensor* weight, const at::Tensor* bias, const Call& c, muloco_norm* a) {
+  if (!x || x->dim() != 2) return false;
+  const at::ScalarType type = x->scalar_type();
+  const int64_t T = x->size(0), d = x->size(1);
+  if ((type != at::kFloat && type != at::kBFloat16) || !rows_of(x, c, type, T, d) || (other && !rows_of(other, c, type, T, d)) ||
+      (weight && !dense_vector(*weight, c, at::kFloat, d)) || (bias && !dense_vector(*bias, c, at::kFloat, d)))
+    return false;
+  *a = muloco_norm();
+  a->tokens = T; a->d = d;
+  a->ldx = x->stride(0); a->ldr = other ? other->stride(0) : 0;
+  a->dtype = type == at::kFloat ? MULOCO_F32 : MULOCO_BF16;
+  a->x = x->data_ptr(); a->residual = ptr(other);
+  a->weight = (const float*)ptr(weight); a->bias = (const float*)ptr(bias);
+  return true;
+}
+
+// x, weight, bias, residual, eps, center
+PyObject* norm_forward(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  if (n != 10) return none();
+  const Call c = call_of(o);
+  bool ok = c.ok;
+  const at::Tensor* x = tensor(o[4], &ok);
+  const at::Tensor* weight = tensor(o[5], &ok);
+  const at::Tensor* bias = tensor(o[6], &ok);
+  const at::Tensor* residual = tensor(o[7], &ok);
+  const double eps = PyFloat_AsDouble(o[8]);
+  const int center = PyObject_IsTrue(o[9]);
+  if (PyErr_Occurred() || center < 0) { PyErr_Clear(); return none(); }
+  muloco_norm a;
+  if (!ok || !norm_of(x, residual, weight, bias, c, &a)) return none();
+  a.eps = (float)eps; a.center = center;
+  const auto f32 = x->options().dtype(at::kFloat);
+  at::Tensor y = at::empty(x->sizes(), x->options()), h, rstd = at::empty({a.tokens}, f32), mean;
+  if (residual) h = at::empty(x->sizes(), x->options());
+  if (center) mean = at::empty({a.tokens}, f32);
+  const auto fn = (decltype(&muloco_layer_norm))c.fn;
+  const int st = unlocked([&] { return fn(c.ctx, &a, residual ? h.data_ptr() : nullptr, y.data_ptr(), center ? (float*)mean.data_ptr() : nullptr, (float*)rstd.data_ptr()); });
+  if (st) return PyLong_FromLong(st);
+  PyObject* hh = residual ? wrap(h) : (Py_INCREF(o[4]), o[4]);
+  return Py_BuildValue("(NNNN)", wrap(y), hh, wrap(rstd), wrap_or_none(mean));
+}
+
+// dy, h, rstd, mean, weight, dh, whether the bias's gradient is wanted
+PyObject* norm_backward(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  if (n != 11) return none();
+  const Call c = call_of(o);
+  bool ok = c.ok;
+  const at::Tensor* dy = tensor(o[4], &ok);
+  const at::Tensor* h = tensor(o[5], &ok);
+  const at::Tensor* rstd = tensor(o[6], &ok);
+  const at::Tensor* mean = tensor(o[7], &ok);
+  const at::Tensor* weight = tensor(o[8], &ok);
+  const at::Tensor* dh = tensor(o[9], &ok);
+  const int bias = PyObject_IsTrue(o[10]);
+  if (bias < 0) { PyErr_Clear(); return none(); }
+  muloco_norm a;
+  if (!ok || !rstd || !norm_of(h, dh, weight, nullptr, c, &a) || !rows_of(dy, c, h->scalar_type(), a.tokens, a.d) ||
+      !dense_vector(*rstd, c, at::kFloat, a.tokens) || (mean && !dense_vector(*mean, c, at::kFloat, a.tokens)))
+    return none();
+  a.center = mean != nullptr;
+  at::Tensor dx = at::empty(h->sizes(), h->options()), dw, db, scratch;
+  if (weight) dw = at::empty({a.d}, rstd->options());
+  if (bias) db = at::empty({a.d}, rstd->options());
+  if (weight || bias) scratch = at::empty({MULOCO_NORM_PARTS, 2, a.d}, rstd->options());
+  auto p = [](const at::Tensor& t) { return t.defined() ? (float*)t.data_ptr() : nullptr; };
+  const auto fn = (decltype(&muloco_layer_norm_backward))c.fn;
+  const int st = unlocked([&] { return fn(c.ctx, &a, dy->data_ptr(), dy->stride(0), (const float*)ptr(mean), (const float*)rstd->data_ptr(), dx.data_ptr(), p(dw), p(db), p(scratch)); });
+  if (st) return PyLong_FromLong(st);
+  return Py_BuildValue("(NNN)", wrap(dx), wrap_or_none(dw), wrap_or_none(db));
+}
+
+// ids, table, scale
+PyObject* embedding_forward(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  if (n != 7) return none();
+  const Call c = call_of(o);
+  bool ok = c.ok;
+  const at::Tensor* ids = tensor(o[4], &ok);
+  const at::Tensor* table = tensor(o[5], &ok);
+  const double scale = PyFloat_AsDouble(o[6]);
+  if (PyErr_Occurred()) { PyErr_Clear(); return none(); }
+  if (!ok || !ids || !table || ids->dim() != 1 || table->dim() != 2 || !dense_vector(*ids, c, at::kLong, ids->size(0))) return none();
+  const at::ScalarType type = table->scalar_type();
+  if ((type != at::kFloat && type != at::kBFloat16) || !rows_of(table, c, type, table->size(0), table->size(1))) return none();
+  muloco_embedding a = muloco_embedding();
+  a.tokens = ids->size(0); a.rows = table->size(0); a.d = table->size(1); a.ld = table->stride(0);
+  a.dtype = type == at::kFloat ? MULOCO_F32 : MULOCO_BF16;
+  a.scale = (float)scale;
+  a.ids = (const int64_t*)ids->data_ptr();
+  at::Tensor out = at::empty({a.tokens, a.d}, table->options());
+  const auto fn = (decltype(&muloco_embedding_lookup))c.fn;
+  const int st = unlocked([&] { return fn(c.ctx, &a, table->data_ptr(), out.data_ptr()); });
+  if (st) return PyLong_FromLong(st);
+  return wrap(out);
+}
+
+// dout, ids, rows, scale, whether the result is bf16, muloco_embedding_scratch
+PyObject* embedding_backward(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  if (n != 10) return none();
+  const Call c = call_of(o);
+  bool ok = c.ok;
+  const at::Tensor* dout = tensor(o[4], &ok);
+  const at::Tensor* ids = tensor(o[5], &ok);
+  const long long rows = PyLong_AsLongLong(o[6]);
+  const double scale = PyFloat_AsDouble(o[7]);
+  const int bf16 = PyObject_IsTrue(o[8]);
+  const auto size = (decltype(&muloco_embedding_scratch))PyLong_AsVoidPtr(o[9]);
+  if (PyErr_Occurred() || bf16 < 0) { PyErr_Clear(); return none(); }
+  if (!ok || !dout || !ids || !size || rows < 0 || ids->dim() != 1 || dout->dim() != 2 || !dense_vector(*ids, c, at::kLong, ids->size(0))) return none();
+  const at::ScalarType type = dout->scalar_type();
+  if ((type != at::kFloat && type != at::kBFloat16) || !rows_of(dout, c, type, ids->size(0), dout->size(1))) return none();
+  muloco_embedding a = muloco_embedding();
+  a.tokens = ids->size(0); a.rows = rows; a.d = dout->size(1); a.ld = dout->stride(0);
+  a.dtype = type == at::kFloat ? MULOCO_F32 : MULOCO_BF16;
+  a.scale = (float)scale;
+  a.ids = (const int64_t*)ids->data_ptr();
+  at::Tensor dtable = at::empty({a.rows, a.d}, dout->options().dtype(bf16 ? at::kBFloat16 : at::kFloat)),
+             scratch = at::empty({(int64_t)size(a.tokens, a.d)}, dout->options().dtype(at::kByte));
+  const auto fn = (decltype(&muloco_embedding_backward))c.fn;
+  const int st = unlocked([&] { return fn(c.ctx, &a, dout->data_ptr(), bf16 ? MULOCO_BF16 : MULOCO_F32, dtable.data_ptr(), scratch.data_ptr()); });
+  if (st) return PyLong_FromLong(st);
+  return wrap(dtable);
+}
+
 // No C++ exception (an allocation that fails, above all) leaves a function: it becomes a Python one.
 template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
 PyObject* guarded(PyObject* self, PyObject* const* o, Py_ssize_t n) {
@@ -284,6 +473,12 @@ PyMethodDef methods[] = {
     FAST("qk_norm_rope_backward", qk_backward, "muloco_qk_norm_rope_backward"),
     FAST("gated_ffn", ffn_forward, "muloco_gated_ffn"),
     FAST("gated_ffn_backward", ffn_backward, "muloco_gated_ffn_backward"),
+    FAST("causal_attention", attention_forward, "muloco_causal_attention"),
+    FAST("causal_attention_backward", attention_backward, "muloco_causal_attention_backward"),
+    FAST("layer_norm", norm_forward, "muloco_layer_norm"),
+    FAST("layer_norm_backward", norm_backward, "muloco_layer_norm_backward"),
+    FAST("embedding_lookup", embedding_forward, "muloco_embedding_lookup"),
+    FAST("embedding_backward", embedding_backward, "muloco_embedding_backward"),
     FAST("adamw_step", adamw_step, "muloco_adamw_step"),
     FAST("adamw_moments", adamw_moments, "muloco_adamw_moments"),
     {nullptr, nullptr, 0, nullptr}};

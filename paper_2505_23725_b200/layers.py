@@ -101,3 +101,85 @@ def qk_norm_rope(owner, q, k, cos, sin, positions=None, gain_q=None, gain_k=None
     """Norm and rotation of q [tokens, heads, head_dim] and k (binding.Context.qk_norm_rope), differentiable in q, k
     and the gains.  q or k may be None, and so is its result."""
     return _QKNormRope.apply(owner, eps, interleaved, q, k, cos, sin, positions, gain_q, gain_k)
+
+
+def _heads(t):
+    """t [tokens, heads, head_dim], or a copy of it where the library would refuse its layout (as _rows)."""
+    if t.data_ptr() % 16 == 0 and (t.is_contiguous() or (
+            t.stride(2) == 1 and all(n < 2 or (s >= t.shape[2] and s % 8 == 0) for n, s in zip(t.shape[:2], t.stride()[:2])))):
+        return t
+    return t.clone(memory_format=torch.contiguous_format)
+
+
+class _CausalAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, owner, sequences, scale, q, k, v):
+        o, lse = owner.causal_attention(q, k, v, sequences, scale)
+        ctx.owner, ctx.sequences, ctx.scale = owner, sequences, scale
+        ctx.save_for_backward(q, k, v, o, lse)
+        return o
+
+    @staticmethod
+    def backward(ctx, do):
+        q, k, v, o, lse = ctx.saved_tensors
+        grads = ctx.owner.causal_attention_backward(_heads(do), q, k, v, o, lse, ctx.sequences, ctx.scale)
+        return (None, None, None, *_once("causal_attention", grads, (do, q, k, v)))
+
+
+def causal_attention(owner, q, k, v, sequences, scale=None):
+    """Attention of q [tokens, query heads, head_dim] over k and v [tokens, key heads, head_dim] (bf16), every token over those up to it
+    of its own sequence (binding.Sequences of the batch), differentiable in q, k and v."""
+    return _CausalAttention.apply(owner, sequences, scale, _heads(q), _heads(k), _heads(v))
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, owner, eps, center, x, weight, bias, residual):
+        y, h, rstd, mean = owner.layer_norm(x, weight, bias, residual, eps, center)
+        ctx.owner, ctx.bias, ctx.residual = owner, bias is not None, residual is not None
+        ctx.save_for_backward(h, rstd, mean, weight)
+        return (y, h) if residual is not None else y
+
+    @staticmethod
+    def backward(ctx, dy, dh=None):
+        h, rstd, mean, weight = ctx.saved_tensors
+        dx, dw, db = ctx.owner.layer_norm_backward(_last(dy), h, rstd, mean, weight, None if dh is None else _last(dh), ctx.bias)
+        dx, dr, dw, db = _once("layer_norm", (dx, dx if ctx.residual else None, dw, db), (dy, dh, h, weight))
+        return None, None, None, dx, dw, db, dr
+
+
+def _last(t):
+    """t [tokens, d], or a copy of it where the entries of a row are not consecutive or rows overlap."""
+    return t if t.stride(1) == 1 and (t.shape[0] < 2 or t.stride(0) >= t.shape[1]) else t.contiguous()
+
+
+def layer_norm(owner, x, weight=None, bias=None, residual=None, eps: float = 1e-6, center: bool = True):
+    """(h - mean) / sqrt(var + eps) * weight + bias over the last dimension of h = x + residual (center=False: without the mean, the
+    root mean square norm), differentiable in x, the residual, weight and bias.  With a residual the result is (y, h): h is
+    the stream that goes on."""
+    shape = x.shape
+    x2 = _last(x.reshape(-1, shape[-1]))
+    r2 = None if residual is None else _last(residual.reshape(-1, shape[-1]))
+    out = _LayerNorm.apply(owner, eps, center, x2, weight, bias, r2)
+    return out.view(shape) if residual is None else tuple(t.view(shape) for t in out)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, owner, scale, ids, table):
+        ctx.owner, ctx.scale, ctx.rows, ctx.dtype = owner, scale, table.shape[0], table.dtype
+        ctx.save_for_backward(ids)
+        return owner.embedding(ids, table, scale)
+
+    @staticmethod
+    def backward(ctx, dout):
+        ids, = ctx.saved_tensors
+        grad = ctx.owner.embedding_backward(_last(dout), ids, ctx.rows, ctx.scale, ctx.dtype)
+        grad, = _once("embedding", (grad,), (dout,))
+        return None, None, None, grad
+
+
+def embedding(owner, ids, table, scale: float = 1.0):
+    """scale * table[ids] for int64 ids of any shape, differentiable in the table (the gradient, of the table's type, has every row)."""
+    out = _Embedding.apply(owner, scale, ids.reshape(-1).contiguous(), _last(table))
+    return out.view(*ids.shape, table.shape[1])
