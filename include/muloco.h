@@ -554,8 +554,8 @@ MULOCO_API muloco_status muloco_embedding_lookup(muloco_ctx* ctx, const muloco_e
 /* The table's gradient, dense [rows][d] of `dtable_dtype`, every row written: row v = scale * sum of the rows of dout (of a->dtype, row
  * stride a->ld) whose token is v, added in float32 in the order of the tokens (in pieces where there are many, in a fixed
  * order) and rounded once.  A token outside the table adds nothing and raises MULOCO_EINVAL through muloco_sync_status.
- * scratch: device memory of muloco_embedding_scratch(tokens, d) bytes, 16-byte aligned, that the caller provides. */
-MULOCO_API size_t muloco_embedding_scratch(int64_t tokens, int64_t d);
+ * scratch: device memory, 16-byte aligned, that the caller provides; muloco_embedding_scratch says how many bytes. */
+MULOCO_API muloco_status muloco_embedding_scratch(muloco_ctx* ctx, int64_t tokens, int64_t d, size_t* bytes);
 MULOCO_API muloco_status muloco_embedding_backward(muloco_ctx* ctx, const muloco_embedding* a, const void* dout,
                                                    int32_t dtable_dtype, void* dtable, void* scratch);
 

@@ -209,13 +209,12 @@ def load_library():
     lib.muloco_layer_norm.argtypes = [vp, packed, vp, vp, vp, vp]
     lib.muloco_layer_norm_backward.argtypes = [vp, packed, vp, i64, vp, vp, vp, vp, vp, vp]
     lib.muloco_embedding_lookup.argtypes = [vp, packed, vp, vp]
-    lib.muloco_embedding_scratch.argtypes = [i64, i64]
+    lib.muloco_embedding_scratch.argtypes = [vp, i64, i64, C.POINTER(C.c_size_t)]
     lib.muloco_embedding_backward.argtypes = [vp, packed, vp, i32, vp, vp]
     for name in EXPORTS:
         fn = getattr(lib, name)
         if name not in ("muloco_destroy", "muloco_last_error", "muloco_adamw_destroy", "muloco_sequences_destroy"):
             fn.restype = i32
-    lib.muloco_embedding_scratch.restype = C.c_size_t
     _lib = lib
     return lib
 
@@ -342,6 +341,8 @@ class _Operators:
     stream first waits for it and it then waits for the context's, and the tensors are
     recorded on the context's stream, so inputs, results and their memory may be used as usual."""
 
+    _fast_decoder = {}                           # compiled calls of attention, layer norm and embedding
+
     def _init_operators(self):
         """What every call looks up, once: device number, types, the stream's handle and the way to ask for the handle
         of the current stream without building a Stream object."""
@@ -354,10 +355,12 @@ class _Operators:
         fast = _load_fastcall()
         self._fast = {}
         if fast is not None:
-            for name in ("qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward", "adamw_step",
-                         "adamw_moments", "causal_attention", "causal_attention_backward", "layer_norm",
-                         "layer_norm_backward", "embedding_lookup", "embedding_backward"):
-                self._fast[name] = (getattr(fast, name), C.cast(getattr(self.lib, "muloco_" + name), C.c_void_p).value)
+            def calls(*names):
+                return {n: (getattr(fast, n), C.cast(getattr(self.lib, "muloco_" + n), C.c_void_p).value) for n in names}
+            self._fast = calls("qk_norm_rope", "qk_norm_rope_backward", "gated_ffn", "gated_ffn_backward", "adamw_step",
+                               "adamw_moments")
+            self._fast_decoder = calls("causal_attention", "causal_attention_backward", "layer_norm", "layer_norm_backward",
+                                       "embedding_lookup", "embedding_backward")
             self._scratch_size = C.cast(self.lib.muloco_embedding_scratch, C.c_void_p).value
 
     def _quick(self, name, *args):
@@ -365,7 +368,7 @@ class _Operators:
         it should be, or the caller is on another stream)."""
         if self.ctx is None:
             raise RuntimeError("the context is closed")
-        f = self._fast.get(name)
+        f = self._fast.get(name) or self._fast_decoder.get(name)
         if f is None:
             return None
         r = f[0](self.ctx.value, f[1], self._dev, self._handle, *args)
@@ -770,7 +773,7 @@ class _Operators:
         dtype = self._f32 if dtype is None else dtype
         if dtype not in (self._f32, self._bf16):
             raise ValueError(f"dtype must be float32 or bfloat16 (got {dtype})")
-        if self._fast:
+        if self._fast_decoder:
             r = self._quick("embedding_backward", dout, ids, rows, scale, dtype is self._bf16, self._scratch_size)
             if r is not None:
                 return r
@@ -780,8 +783,10 @@ class _Operators:
         T = ids.shape[0]
         self._need("dout", dout, dout.dtype, (T, None))
         d = dout.shape[1]
+        size = C.c_size_t()
+        self._check(self.lib.muloco_embedding_scratch(self.ctx, T, d, C.byref(size)))
         dtable = dout.new_empty((rows, d), dtype=dtype)
-        scratch = dout.new_empty(self.lib.muloco_embedding_scratch(T, d), dtype=self.torch.uint8)
+        scratch = dout.new_empty(size.value, dtype=self.torch.uint8)
         cur = self._other_stream()
         if cur is not None:
             self._enter(cur, (dout, ids, dtable, scratch))

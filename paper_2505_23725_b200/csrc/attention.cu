@@ -538,8 +538,9 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         for (int e = 0; e < 32; ++e) s[e] = col0 + h * 32 + e > row ? 0xff800000u : s[e];
       }
     };
-    // The reference becomes the row's largest score so far; sums and weighted values so far (`some`: there are some) follow.
-    auto move_reference = [&](bool some, bool last) {
+    // The reference becomes the row's largest score so far; sums and weighted values so far (`some`: there are some) follow.  Only in rows whose
+    // own weights ask for it: what a row comes out as does not depend on the others.
+    auto move_reference = [&](bool some, bool last, float part) {
       float m = -INFINITY;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -549,8 +550,10 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         for (int e = 0; e < 32; e += 2) m = max3(m, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
       }
       row_largest[t][half][row] = m;
+      if (some) row_total[t][half][row] = part;   // (at a unit's start the other thread may not have read the last one's total)
       either(pair_id, false);
       m = max3(m, row_largest[t][half ^ 1][row], some ? top : m);
+      if (some && part <= MOST && row_total[t][half ^ 1][row] <= MOST) m = top;
       if (some) {                             // (the product before these scores is complete, as they are)
         const float by = exp2_approx((top - m) * c);
         total *= by;
@@ -595,6 +598,8 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       const Extent e = extent_of(x.tile);
       const int n_t = t ? e.n_b : e.n_a;
       if (!n_t) continue;
+      const int pos = x.tile.offset + t * TILE + row;
+      const bool ok = pos < x.tile.length;    // rows past the end hold another sequence's tokens: nothing goes by them
       top = 0.f;
       total = 0.f;
       for (int j = 0; j < n_t; ++j) {
@@ -602,12 +607,12 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         tc_fence_after();
         const bool last = j == n_t - 1;
         uint32_t w[32];
-        if (j == 0) move_reference(false, last);
+        if (j == 0) move_reference(false, last, 0.f);
         float part = weights(w, last);
         // Where the weights are too large by the reference as it was, or not numbers: once more by a new one.
-        if (either(pair_id, !alive || (j > 0 && !(part <= MOST)))) {
+        if (either(pair_id, !alive || (j > 0 && ok && !(part <= MOST)))) {
           if (either(pair_id, !alive)) { alive = false; break; }
-          move_reference(true, last);
+          move_reference(true, last, part);
           part = weights(w, last);
         }
         total += part;
@@ -625,8 +630,6 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       turn_o ^= 1u;
       tc_fence_after();
       total += row_total[t][half ^ 1][row];
-      const int pos = x.tile.offset + t * TILE + row;
-      const bool ok = pos < x.tile.length;
       const int64_t token = (int64_t)x.tile.start + pos;
       __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + ((ok ? token : 0) * p.heads + x.head) * p.dim + half * (DP / 2);
       const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;

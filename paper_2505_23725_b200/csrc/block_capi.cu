@@ -25,6 +25,7 @@ bool misaligned(const void* p, size_t a) { return (((uintptr_t)p) & (a - 1)) != 
 
 struct muloco_sequences {
   muloco_ctx* ctx = nullptr;
+  int device = 0;
   int64_t tokens = 0, used = 0;         // of the batch, of the sequences
   int64_t n_pairs = 0, n_tiles = 0;
   const AttnTile* table = nullptr;      // pair tiles, query tiles, key tiles
@@ -112,6 +113,7 @@ extern "C" {
 
 MULOCO_API muloco_status muloco_sequences_bytes(muloco_ctx* c, const int64_t* lengths, int64_t n, int64_t tokens, size_t* bytes) {
   if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
   if (!bytes) return ctx_fail(c, MULOCO_EINVAL, "bytes is NULL");
   muloco_sequences s;
   const muloco_status r = count_tiles(c, lengths, n, tokens, &s);
@@ -156,6 +158,7 @@ MULOCO_API muloco_status muloco_sequences_create(muloco_ctx* c, const int64_t* l
     std::stable_sort(keys, t.end(), [](const AttnTile& x, const AttnTile& y) { return x.length - x.offset > y.length - y.offset; });
     muloco_sequences* s = new muloco_sequences(made);
     s->ctx = c;
+    s->device = ctx_device(c);
     s->table = static_cast<const AttnTile*>(table);
     // (pageable memory: it is read before the call returns)
     const cudaError_t e = need ? cudaMemcpyAsync(table, t.data(), need, cudaMemcpyHostToDevice, v.st) : cudaSuccess;
@@ -170,7 +173,11 @@ MULOCO_API muloco_status muloco_sequences_create(muloco_ctx* c, const int64_t* l
   return MULOCO_OK;
 }
 
-MULOCO_API void muloco_sequences_destroy(muloco_sequences* s) { delete s; }
+MULOCO_API void muloco_sequences_destroy(muloco_sequences* s) {
+  if (!s) return;
+  const DeviceScope scope(s->device);
+  delete s;
+}
 
 MULOCO_API muloco_status muloco_causal_attention(muloco_ctx* c, const muloco_attention* a, const muloco_sequences* s, void* o, float* lse) {
   if (!c) return MULOCO_EINVAL;
@@ -360,7 +367,13 @@ MULOCO_API muloco_status muloco_embedding_lookup(muloco_ctx* c, const muloco_emb
   return MULOCO_OK;
 }
 
-MULOCO_API size_t muloco_embedding_scratch(int64_t tokens, int64_t d) { return tokens > 0 && d > 0 ? embedding_scratch(tokens, d) : 0; }
+MULOCO_API muloco_status muloco_embedding_scratch(muloco_ctx* c, int64_t tokens, int64_t d, size_t* bytes) {
+  if (!c) return MULOCO_EINVAL;
+  ON_DEVICE(c);
+  if (!bytes || tokens < 0 || tokens > INT32_MAX || d < 1 || d > (1 << 20)) return ctx_fail(c, MULOCO_EINVAL, "tokens or d out of range, or bytes NULL");
+  *bytes = tokens > 0 ? embedding_scratch(tokens, d) : 0;
+  return MULOCO_OK;
+}
 
 MULOCO_API muloco_status muloco_embedding_backward(muloco_ctx* c, const muloco_embedding* a, const void* dout, int32_t dtable_dtype,
                                                    void* dtable, void* scratch) {

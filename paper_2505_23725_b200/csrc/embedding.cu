@@ -25,7 +25,7 @@ template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int SLICE = 256;                     // columns that a warp works on at a time, 8 a lane
 constexpr int CHUNK = EMB_CHUNK;
-static_assert(CHUNK == 32, "a pair per lane");
+static_assert(CHUNK == 16, "a pair per lane, two batches of loads");
 
 // 8 entries of a slice in a lane: twice 4 neighbours, 128 columns apart (WIDE: whole sectors are written whatever the type), or
 // every 32nd.
@@ -103,8 +103,7 @@ __device__ __forceinline__ uint64_t pair_of(const EmbeddingArgs& a, int64_t t) {
   return ((uint64_t)(ok ? id : a.rows) << 32) | (uint64_t)t;
 }
 
-constexpr int SORT_THREADS = 1024, RUN = 64;   // RUN: pairs that a warp sorts in registers
-static_assert(EMB_SORT_BLOCK == 2 * SORT_THREADS, "two pairs per thread");
+constexpr int SORT_THREADS = EMB_SORT_BLOCK / 2, RUN = 64;   // RUN: pairs that a warp sorts in registers
 
 // How many of the n pairs of a sorted run are below x (n at most `most`, a power of two).
 __device__ __forceinline__ int below_in_run(const uint64_t* p, int n, int most, uint64_t x) {
@@ -183,11 +182,14 @@ __device__ __forceinline__ int64_t below(const uint64_t* p, int64_t n, uint64_t 
 
 // Merges groups of EMB_MERGE sorted blocks of `block` pairs (a power of two): a pair's place is the count of smaller ones (no two are
 // equal).  The searches in the other blocks go step by step together, so that their loads overlap.
-__global__ void __launch_bounds__(THREADS)
+// Both kernels are small blocks: their searches read scattered places, 32 to an instruction, which a multiprocessor serves one by one (blocks of 2048
+// pairs and 256 threads: 15 and 15 us for 16384 tokens).
+constexpr int MERGE_THREADS = 64;
+__global__ void __launch_bounds__(MERGE_THREADS)
 merge_kernel(const uint64_t* in, uint64_t* out, int64_t tokens, int64_t block) {
   grid_wait();
   grid_release();
-  const int64_t t = (int64_t)blockIdx.x * THREADS + threadIdx.x;
+  const int64_t t = (int64_t)blockIdx.x * MERGE_THREADS + threadIdx.x;
   if (t >= tokens) return;
   const uint64_t x = in[t];
   const int64_t first = t & ~(block * EMB_MERGE - 1);
@@ -242,11 +244,12 @@ __device__ __forceinline__ Piece piece_of(const EmbeddingArgs& a, const uint64_t
 // Rows without tokens (units 0 .. zero_units - 1: a warp looks after 32 rows of up to ZERO_COLS columns), then chunks of the sorted order (a chunk and
 // a slice each).
 constexpr int ZERO_COLS = 1024;
+constexpr int GATHER_WARPS = 4;
 template <typename T, typename O, bool WIDE>
-__global__ void __launch_bounds__(THREADS)
+__global__ void __launch_bounds__(32 * GATHER_WARPS)
 gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t zero_units, int64_t chunk_units) {
   const int lane = threadIdx.x & 31;
-  int64_t unit = (int64_t)blockIdx.x * WARPS + (threadIdx.x >> 5);
+  int64_t unit = (int64_t)blockIdx.x * GATHER_WARPS + (threadIdx.x >> 5);
   grid_wait();
   grid_release();
   if (unit >= zero_units) {
@@ -264,7 +267,7 @@ gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t zero_units, 
       Eight<T, WIDE> g[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e)              // (behind the last pair: the last one's again, not used)
-        g[e].load(reinterpret_cast<const T*>(a.dout) + (int64_t)__shfl_sync(0xffffffffu, c.token, (e0 + e) & 31) * a.ld, col, a.d, lane);
+        g[e].load(reinterpret_cast<const T*>(a.dout) + (int64_t)__shfl_sync(0xffffffffu, c.token, e0 + e) * a.ld, col, a.d, lane);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         if (e0 + e >= c.n) break;
@@ -272,7 +275,7 @@ gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t zero_units, 
         for (int i = 0; i < 8; ++i) f[i] += g[e].at(i);
         const int64_t id = __shfl_sync(0xffffffffu, c.id, e0 + e);
         const bool at_end = e0 + e + 1 == c.n;
-        if (!at_end && __shfl_sync(0xffffffffu, c.id, (e0 + e + 1) & 31) == id) continue;
+        if (!at_end && __shfl_sync(0xffffffffu, c.id, e0 + e + 1) == id) continue;
         // the row's last pair in this chunk
         if (id < a.rows) {
           if (open || (at_end && c.goes_on)) {
@@ -317,8 +320,14 @@ join_kernel(const EmbeddingArgs a, const uint64_t* pairs) {
   const Piece c = piece_of(a, pairs, chunk, lane);
   const int64_t id = c.last_id;
   if (!c.goes_on || id >= a.rows || (c.from_before && c.first_id == id)) return;      // (the whole block)
-  const int64_t end = below(pairs, a.tokens, (uint64_t)(id + 1) << 32);
-  const int64_t n = (end - 1) / CHUNK - chunk + 1;             // chunks of the row
+  // chunks of the row: this one and those behind it that begin with it, looked at 32 at a time
+  int64_t n = 1;
+  for (bool more = true; more;) {
+    const int64_t at = (chunk + n + lane) * CHUNK;
+    const uint32_t others = __ballot_sync(0xffffffffu, at >= a.tokens || id_of(pairs[at]) != id);
+    more = others == 0;
+    n += more ? 32 : __ffs(others) - 1;
+  }
   const int64_t p0 = n * warp / WARPS, p1 = n * (warp + 1) / WARPS;
   float f[8];
 #pragma unroll
@@ -353,7 +362,8 @@ cudaError_t gather(cudaStream_t st, const EmbeddingArgs& a, const uint64_t* pair
   const int64_t chunks = (a.tokens + CHUNK - 1) / CHUNK;
   const int64_t zero_units = (a.rows + 31) / 32 * ((a.d + ZERO_COLS - 1) / ZERO_COLS);
   ++*launches;
-  cudaError_t e = launch_dependent(gather_kernel<T, O, WIDE>, (unsigned)((chunks * slices + zero_units + WARPS - 1) / WARPS), THREADS, 0, st, a, pairs,
+  cudaError_t e = launch_dependent(gather_kernel<T, O, WIDE>, (unsigned)((chunks * slices + zero_units + GATHER_WARPS - 1) / GATHER_WARPS),
+                                   32 * GATHER_WARPS, 0, st, a, pairs,
                                    zero_units, chunks * slices);
   if (e != cudaSuccess || chunks < 2) return e;
   ++*launches;
@@ -394,7 +404,7 @@ cudaError_t launch_embedding_backward(cudaStream_t st, const EmbeddingArgs& args
   cudaError_t e = launch_dependent(sort_kernel, (unsigned)((a.tokens + EMB_SORT_BLOCK - 1) / EMB_SORT_BLOCK), SORT_THREADS, 0, st, a, pairs);
   ++*launches;
   for (int64_t block = EMB_SORT_BLOCK; e == cudaSuccess && block < a.tokens; block *= EMB_MERGE) {
-    e = launch_dependent(merge_kernel, (unsigned)((a.tokens + THREADS - 1) / THREADS), THREADS, 0, st, (const uint64_t*)pairs, other, a.tokens, block);
+    e = launch_dependent(merge_kernel, (unsigned)((a.tokens + MERGE_THREADS - 1) / MERGE_THREADS), MERGE_THREADS, 0, st, (const uint64_t*)pairs, other, a.tokens, block);
     ++*launches;
     uint64_t* t = pairs;
     pairs = other;

@@ -441,8 +441,10 @@ PyObject* embedding_backward(PyObject*, PyObject* const* o, Py_ssize_t n) {
   a.dtype = type == at::kFloat ? MULOCO_F32 : MULOCO_BF16;
   a.scale = (float)scale;
   a.ids = (const int64_t*)ids->data_ptr();
+  size_t bytes = 0;
+  if (const int st = size(c.ctx, a.tokens, a.d, &bytes)) return PyLong_FromLong(st);
   at::Tensor dtable = at::empty({a.rows, a.d}, dout->options().dtype(bf16 ? at::kBFloat16 : at::kFloat)),
-             scratch = at::empty({(int64_t)size(a.tokens, a.d)}, dout->options().dtype(at::kByte));
+             scratch = at::empty({(int64_t)bytes}, dout->options().dtype(at::kByte));
   const auto fn = (decltype(&muloco_embedding_backward))c.fn;
   const int st = unlocked([&] { return fn(c.ctx, &a, dout->data_ptr(), bf16 ? MULOCO_BF16 : MULOCO_F32, dtable.data_ptr(), scratch.data_ptr()); });
   if (st) return PyLong_FromLong(st);

@@ -352,7 +352,7 @@ constexpr int NORM_PARTS = MULOCO_NORM_PARTS, NORM_MAX_DIM = 32768;
 cudaError_t launch_norm(cudaStream_t st, const NormArgs& a, bool back, int is_bf16, int n_sms, int* launches);
 
 // Embedding lookup.
-constexpr int EMB_SORT_BLOCK = 2048, EMB_MERGE = 8, EMB_CHUNK = 32;
+constexpr int EMB_SORT_BLOCK = 512, EMB_MERGE = 8, EMB_CHUNK = 16;
 struct EmbeddingArgs {
   int64_t tokens, rows, ld;                    // ld: row stride of the table (forward), of dout (backward)
   const int64_t* ids;

@@ -45,7 +45,7 @@ def reference(q, k, v, do, lengths, scale):
     T, hq, D = q.shape
     hk = k.shape[1]
     group = hq // hk
-    z = lambda *s: torch.zeros(*s, dtype=torch.float64, device="cuda")          # noqa: E731
+    z = lambda *s: torch.zeros(*s, dtype=torch.float64, device=q.device)          # noqa: E731
     r = {"o": z(T, hq, D), "lse": z(hq, T), "dq": z(T, hq, D), "dk": z(T, hk, D), "dv": z(T, hk, D)}
     tol = {n: torch.zeros_like(t) for n, t in r.items()}
     a = 0
@@ -53,7 +53,7 @@ def reference(q, k, v, do, lengths, scale):
         b = a + n
         if n == 0:
             continue
-        later = torch.ones(n, n, dtype=torch.bool, device="cuda").triu(1)
+        later = torch.ones(n, n, dtype=torch.bool, device=q.device).triu(1)
         for h in range(hq):
             Q, K, V, G = q[a:b, h].double(), k[a:b, h // group].double(), v[a:b, h // group].double(), do[a:b, h].double()
             s = (Q @ K.T * scale).masked_fill(later, -torch.inf)
