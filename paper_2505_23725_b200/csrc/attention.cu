@@ -204,21 +204,6 @@ __device__ __forceinline__ float log2_approx(float x) {
   return y;
 }
 
-// Whether any thread of the two warps that share a tile's rows says so (barrier `id`; both take the same turns).
-__device__ __forceinline__ bool either(int id, bool x) {
-  uint32_t r;
-  asm volatile(
-      "{\n"
-      ".reg .pred p, q;\n"
-      "setp.ne.b32 p, %1, 0;\n"
-      "barrier.cta.red.or.pred q, %2, 64, p;\n"
-      "selp.u32 %0, 1, 0, q;\n"
-      "}\n"
-      : "=r"(r)
-      : "r"((uint32_t)x), "r"(id)
-      : "memory");
-  return r != 0;
-}
 // The largest of three; NaN if one is.
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
@@ -258,6 +243,21 @@ __device__ __forceinline__ Unit unit_of(const AttnParams& p, int heads, int u) {
   return x;
 }
 
+// Whether any thread of the two warps that share a tile's rows says so (barrier `id`; both take the same turns).
+__device__ __forceinline__ bool either(int id, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n"
+      ".reg .pred p, q;\n"
+      "setp.ne.b32 p, %1, 0;\n"
+      "barrier.cta.red.or.pred q, %2, 64, p;\n"
+      "selp.u32 %0, 1, 0, q;\n"
+      "}\n"
+      : "=r"(r)
+      : "r"((uint32_t)x), "r"(id)
+      : "memory");
+  return r != 0;
+}
 // The next unit, asked for by the copying thread and read by every warp, through two places in turn.
 struct Next {
   uint32_t full, empty, answer;               // barriers (8 bytes a place), answers (16)
@@ -274,12 +274,12 @@ __device__ __forceinline__ bool ask(const Next& n, volatile int* abort_flag, uin
                : "memory");
   return true;
 }
-// A warp's (or the copying thread's) next unit: -1 when there is none, or the block is giving up.
+// A warp's (or the copying thread's) next unit: -1 when there is none, -2 when the block is giving up.
 template <bool WARP>
 __device__ __forceinline__ int take(Next& n, volatile int* abort_flag, uint64_t limit) {
   bool ok = mbar_wait_cta(n.full + n.place() * 8u, n.parity(), abort_flag, limit);
   if (WARP) ok = __all_sync(0xffffffffu, ok);
-  if (!ok) return -1;
+  if (!ok) return -2;
   int u;
   asm volatile(
       "{\n"
@@ -298,6 +298,12 @@ __device__ __forceinline__ int take(Next& n, volatile int* abort_flag, uint64_t 
   if (!WARP || (threadIdx.x & 31) == 0) mbar_arrive_cta(n.empty + n.place() * 8u);
   ++n.turn;
   return u;
+}
+
+// The next unit of two warps that meet at barrier `id`: both go on or neither does.
+__device__ __forceinline__ int take_together(Next& n, int id, volatile int* abort_flag, uint64_t limit) {
+  const int u = take<true>(n, abort_flag, limit);
+  return either(id, u == -2) ? -2 : u;
 }
 
 struct Pipe {                                 // position in a ring of N stages
@@ -593,7 +599,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     };
     uint32_t turn_s = 0, turn_o = 0;
     bool alive = true;
-    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1) {
+    for (int u = blockIdx.x; u >= 0; u = alive ? take_together(next, pair_id, &abort_flag, limit) : -1) {
       const Unit x = unit_of(p, p.heads, u);
       const Extent e = extent_of(x.tile);
       const int n_t = t ? e.n_b : e.n_a;
@@ -658,12 +664,13 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
   constexpr uint32_t OPERAND = Sh::OPERAND;
   constexpr int ROW_WARPS = 8, COPY_WARP = 8, MMA_WARP = 9;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_q, bar_qempty, bar_kfull[STAGES], bar_kempty[STAGES], bar_vfull[STAGES], bar_vempty[STAGES], bar_s[2], bar_dp,
+  __shared__ __align__(8) uint64_t bar_q, bar_qempty, bar_kfull[STAGES], bar_kempty[STAGES], bar_vfull[STAGES], bar_vempty[STAGES], bar_s[2], bar_dp, bar_dpfree,
       bar_ds, bar_done;
   __shared__ __align__(16) uint4 next_answer[2];
   __shared__ __align__(8) uint64_t bar_next[2], bar_taken[2];
   __shared__ uint32_t tmem_base_slot;
   __shared__ volatile int abort_flag;
+  __shared__ float row_part[2][2][TILE];      // halves of a row's delta, two units in turn
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -681,6 +688,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
     mbar_init(smem_u32(&bar_s[0]), 1);
     mbar_init(smem_u32(&bar_s[1]), 1);
     mbar_init(smem_u32(&bar_dp), 1);
+    mbar_init(smem_u32(&bar_dpfree), 8);
     mbar_init(smem_u32(&bar_ds), 8);
     mbar_init(smem_u32(&bar_done), 1);
   };
@@ -719,44 +727,41 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
     }
   } else if (warp == MMA_WARP) {
     const uint32_t leader = elect_leader();
-    // Order: scores of 0; then per key tile j: dp of j, scores of j + 1 (into the other columns), dq += ds k of j.  (The scores of
-    // j + 1 may be complete before the row warps have looked for those of j: a barrier for each of the two places.)
-    Pipe at;                                  // key tile j
+    // Order: scores and dp of 0; then per key tile j: scores of j + 1 (into the other columns), dp of j + 1 (when the row warps have read
+    // that of j), dq += ds k of j.  (The scores of j + 1 may be complete before the row warps have looked for those of j: a barrier for
+    // each of the two places.)
+    Pipe at, at_v;                            // key tile j; value tile that is waited for next
     uint32_t turn = 0, step = 0;              // step: key tiles so far, over all units
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(bar), parity, &abort_flag, limit));
+    };
     bool alive = true;
     for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1, turn ^= 1u) {
       const AttnTile x = unit_of(p, p.heads, u).tile;
       const int n = x.offset / TILE + 1;      // key tiles
       const int tail = x.length - (n - 1) * TILE;              // rows of the last one that exist, when below 128
-      auto keys = [&](const Pipe& q, int j) {  // waits for key tile j and readies it
-        if (!__all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_kfull[q.stage]), q.phase, &abort_flag, limit))) return false;
+      // scores and dp of key tile j, which is step `k`
+      auto start = [&](const Pipe& q, int j, uint32_t k) {
+        if (!wait(&bar_kfull[q.stage], q.phase)) return false;
         if (j == n - 1 && tail < TILE) zero_rows<DP>(s_k + q.stage * OPERAND, tail, lane);
+        tc_fence_after();
+        scores<DP>(leader, tm + (k & 1u) * 128, s_q, s_k + q.stage * OPERAND);
+        mma_commit(leader, smem_u32(&bar_s[k & 1u]));
+        if (!wait(&bar_vfull[at_v.stage], at_v.phase) || !wait(&bar_dpfree, (k & 1u) ^ 1u)) return false;
+        tc_fence_after();
+        scores<DP>(leader, tm + TM_DP, s_g, s_v + at_v.stage * OPERAND);
+        mma_commit(leader, smem_u32(&bar_dp));
+        mma_commit(leader, smem_u32(&bar_vempty[at_v.stage]));
+        at_v.next<STAGES>();
+        if (j == n - 1) mma_commit(leader, smem_u32(&bar_qempty));
         return true;
       };
-      alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_q), turn, &abort_flag, limit)) && keys(at, 0);
-      if (!alive) break;
-      tc_fence_after();
-      scores<DP>(leader, tm + (step & 1u) * 128, s_q, s_k + at.stage * OPERAND);
-      mma_commit(leader, smem_u32(&bar_s[step & 1u]));
-      for (int j = 0; j < n; ++j, ++step) {
-        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_vfull[at.stage]), at.phase, &abort_flag, limit));
-        if (!alive) break;
-        tc_fence_after();
-        scores<DP>(leader, tm + TM_DP, s_g, s_v + at.stage * OPERAND);
-        mma_commit(leader, smem_u32(&bar_dp));
-        mma_commit(leader, smem_u32(&bar_vempty[at.stage]));
+      alive = wait(&bar_q, turn) && start(at, 0, step);
+      for (int j = 0; alive && j < n; ++j, ++step) {
         Pipe ahead = at;
         ahead.next<STAGES>();
-        if (j + 1 < n) {
-          alive = keys(ahead, j + 1);
-          if (!alive) break;
-          tc_fence_after();
-          scores<DP>(leader, tm + ((step + 1) & 1u) * 128, s_q, s_k + ahead.stage * OPERAND);
-          mma_commit(leader, smem_u32(&bar_s[(step + 1) & 1u]));
-        } else {
-          mma_commit(leader, smem_u32(&bar_qempty));
-        }
-        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), step & 1u, &abort_flag, limit));
+        if (j + 1 < n) alive = start(ahead, j + 1, step + 1);
+        alive = alive && wait(&bar_ds, step & 1u);
         if (!alive) break;
         tc_fence_after();
         weigh<DP>(leader, tm + TM_DQ, tm + (step & 1u) * 128, HALF, s_k + at.stage * OPERAND, j > 0);
@@ -770,35 +775,47 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
     const int row = quarter * 32 + lane;
     const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
     const float c = p.scale * LOG2_E;
+    const int pair_id = 1 + quarter;                           // barrier of the two warps that share these rows
     uint32_t turn = 0, step = 0;
+    const Pair c2 = both(c);
     bool alive = true;
-    for (int u = blockIdx.x; u >= 0; u = alive ? take<true>(next, &abort_flag, limit) : -1, turn ^= 1u) {
+    for (int u = blockIdx.x; u >= 0; u = alive ? take_together(next, pair_id, &abort_flag, limit) : -1, turn ^= 1u) {
       const Unit x = unit_of(p, p.heads, u);
+      const int n = x.tile.offset / TILE + 1;
       const int pos = x.tile.offset + row;
       const bool ok = pos < x.tile.length;
-      const int64_t token = (int64_t)x.tile.start + (ok ? pos : 0);
-      const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(p.o) + (token * p.heads + x.head) * p.dim;
-      const __nv_bfloat16* g = reinterpret_cast<const __nv_bfloat16*>(p.g) + token * p.g_ts + x.head * p.g_hs;
-      // delta = do . o of the row, with o as it was rounded
-      Pair acc = both(0.f);
-  #pragma unroll 4
-      for (int e = 0; e < p.dim; e += 8) {
-        const uint4 a = *reinterpret_cast<const uint4*>(o + e), b = *reinterpret_cast<const uint4*>(g + e);
-        acc = fma2(pair_bf16(a.x), pair_bf16(b.x), acc);
-        acc = fma2(pair_bf16(a.y), pair_bf16(b.y), acc);
-        acc = fma2(pair_bf16(a.z), pair_bf16(b.z), acc);
-        acc = fma2(pair_bf16(a.w), pair_bf16(b.w), acc);
+      const int64_t token = (int64_t)x.tile.start + (ok ? pos : 0), stat = (int64_t)x.head * p.tokens + token;
+      float* const mine = &row_part[turn][half][row];
+      const float* const other = &row_part[turn][half ^ 1][row];
+      const Pair shift = both(-p.lse[stat] * LOG2_E);
+      // delta = do . o, with o as it was rounded; each of the row's two threads has half of it.  A row with a single key tile takes the
+      // sum of p dp below instead: there o is nearly as large as v, and its rounding would show in dq.
+      float delta = 0.f;
+      if (n > 1) {
+        const int c0 = half * (DP / 2);
+        const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(p.o) + (token * p.heads + x.head) * p.dim + c0;
+        const __nv_bfloat16* g = reinterpret_cast<const __nv_bfloat16*>(p.g) + token * p.g_ts + x.head * p.g_hs + c0;
+        Pair acc = both(0.f);
+#pragma unroll
+        for (int e = 0; e < DP / 2; e += 8) {
+          if (c0 + e >= p.dim) break;
+          const uint4 a = *reinterpret_cast<const uint4*>(o + e), b = *reinterpret_cast<const uint4*>(g + e);
+          acc = fma2(pair_bf16(a.x), pair_bf16(b.x), acc);
+          acc = fma2(pair_bf16(a.y), pair_bf16(b.y), acc);
+          acc = fma2(pair_bf16(a.z), pair_bf16(b.z), acc);
+          acc = fma2(pair_bf16(a.w), pair_bf16(b.w), acc);
+        }
+        const float2 sums = parts(acc);
+        const float part = sums.x + sums.y;
+        *mine = part;
+        either(pair_id, false);
+        delta = half ? *other + part : part + *other;
+        if (half == 0 && ok) p.delta[stat] = delta;
       }
-      const float2 halves = parts(acc);
-      const float delta = halves.x + halves.y;
-      const float lse2 = p.lse[(int64_t)x.head * p.tokens + token] * LOG2_E;
-      if (half == 0 && ok) p.delta[(int64_t)x.head * p.tokens + token] = delta;
-      const Pair c2 = both(c), shift = both(-lse2), minus = both(-delta);
-      const int n = x.tile.offset / TILE + 1;
       for (int j = 0; j < n; ++j, ++step) {
         const uint32_t t_s = t_lane + (step & 1u) * 128 + half * HALF;
         alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[step & 1u]), (step >> 1) & 1u, &abort_flag, limit));
-        if (!alive) break;
+        if (!alive && n > 1) break;
         tc_fence_after();
         uint32_t s[64], d[64];
         tm_load32(t_s, s);
@@ -806,34 +823,47 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
         tm_load_wait();
         after_load(s);
         after_load(s + 32);
-  #pragma unroll
+#pragma unroll
         for (int e = 0; e < 64; e += 2) {
-          const float2 x = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, shift));
-          s[e] = __float_as_uint(exp2_approx(x.x));
-          s[e + 1] = __float_as_uint(exp2_approx(x.y));
+          const float2 y = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, shift));
+          s[e] = __float_as_uint(exp2_approx(y.x));
+          s[e + 1] = __float_as_uint(exp2_approx(y.y));
         }
-        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), step & 1u, &abort_flag, limit));
-        if (!alive) break;
+        if (alive) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), step & 1u, &abort_flag, limit));
+        if (!alive && n > 1) break;
         tc_fence_after();
         tm_load32(t_lane + TM_DP + half * HALF, d);
         tm_load32(t_lane + TM_DP + half * HALF + 32, d + 32);
         tm_load_wait();
         after_load(d);
         after_load(d + 32);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cta(smem_u32(&bar_dpfree));
         uint32_t w[32];
-        if (j == n - 1) {                       // where the key comes after the query: no weight, whatever the products hold
-  #pragma unroll
+        if (j == n - 1) {                     // where the key comes after the query: no weight, whatever the products hold
+          if (n == 1) {
+            float part = 0.f;
+#pragma unroll
+            for (int e = 0; e < 64; ++e) part += half * 64 + e > row ? 0.f : __uint_as_float(s[e]) * __uint_as_float(d[e]);
+            *mine = part;
+            if (either(pair_id, !alive)) { alive = false; break; }
+            delta = half ? *other + part : part + *other;
+            if (half == 0 && ok) p.delta[stat] = delta;
+          }
+#pragma unroll
           for (int e = 0; e < 64; e += 2) {
             const float a = __uint_as_float(s[e]) * (__uint_as_float(d[e]) - delta);
             const float b = __uint_as_float(s[e + 1]) * (__uint_as_float(d[e + 1]) - delta);
             w[e >> 1] = pack_bf16x2(half * 64 + e > row ? 0.f : a, half * 64 + e + 1 > row ? 0.f : b);
           }
         } else {
-  #pragma unroll
+          const Pair minus = both(-delta);
+#pragma unroll
           for (int e = 0; e < 64; e += 2) {
-            const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
+            const float2 y = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
                                         add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), minus)));
-            w[e >> 1] = pack_bf16x2(x.x, x.y);
+            w[e >> 1] = pack_bf16x2(y.x, y.y);
           }
         }
         tm_store32(t_s, w);
@@ -842,14 +872,13 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
         __syncwarp();
         if (lane == 0) mbar_arrive_cta(smem_u32(&bar_ds));
       }
+      if (alive) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), turn, &abort_flag, limit));
+      alive = !either(pair_id, !alive);
       if (alive) {
-        alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), turn, &abort_flag, limit));
-        if (alive) {
-          tc_fence_after();
-          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (token * p.heads + x.head) * p.dim;
-          const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
-          store_columns(t_lane + TM_DQ, out, half * (DP / 2), DP / 2, p.dim, p.scale, ok, wide);
-        }
+        tc_fence_after();
+        __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (token * p.heads + x.head) * p.dim;
+        const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
+        store_columns(t_lane + TM_DQ, out, half * (DP / 2), DP / 2, p.dim, p.scale, ok, wide);
       }
     }
   }
