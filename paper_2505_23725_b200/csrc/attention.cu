@@ -29,12 +29,12 @@ namespace muloco {
 namespace {
 
 constexpr int TILE = 128;                     // tokens per tile
-constexpr int ATTN_THREADS = 320;             // backward: eight warps for the rows, one for copies, one for products
-constexpr int FWD_THREADS = 576;              // forward: sixteen for the rows
+constexpr int ATTN_THREADS = 576;             // sixteen warps for the rows, one for copies, one for products
+constexpr int ROW_WARPS = 16, COPY_WARP = 16, MMA_WARP = 17;
 constexpr uint32_t SLAB = TILE * 128;         // 128 rows of 64 bf16, swizzled
-// The two halves of a tile's columns belong to different row warps; each writes its bf16 operand at the start of its own 64 columns, so
-// neither overwrites scores that the other has yet to read.
-constexpr uint32_t HALF = 64;
+// The columns of a tile are divided among row warps (forward in halves, backward in quarters); each writes its bf16 operand at the
+// start of its own columns, so none overwrites scores that another has yet to read.
+constexpr uint32_t HALF = 64, QUARTER = 32;
 constexpr int64_t SECTION_BYTES = 32 << 20;   // of L2's 126 MB: what a section's units read again and again
 constexpr float LN2 = 0.6931471805599453f, LOG2_E = 1.4426950408889634f;
 constexpr int ASK_AHEAD = 3;                  // steps from its end at which a unit asks for the next
@@ -82,6 +82,13 @@ __device__ __forceinline__ void tm_store32(uint32_t taddr, const uint32_t* v) {
       "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]),
       "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]),
       "r"(v[29]), "r"(v[30]), "r"(v[31]), "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tm_store16(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(v[0]),
+      "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]),
+      "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr)
       : "memory");
 }
 __device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -168,11 +175,13 @@ __device__ __forceinline__ void weigh_half(uint32_t leader, uint32_t d, uint32_t
   for (int k = 0; k < 4; ++k)
     mma_ts(leader, d, p + (uint32_t)k * 8u, desc(((b >> 4) | LBO_MN) + (uint32_t)(4 * h + k) * 128u), idesc_mn(DP), accumulate || k > 0);
 }
-// ... over its 128 rows; the second half of p's columns starts `half` columns after the first
+// ... over its 128 rows, p in quarters
 template <int DP>
-__device__ __forceinline__ void weigh(uint32_t leader, uint32_t d, uint32_t p, uint32_t half, uint32_t b, bool accumulate) {
-  weigh_half<DP>(leader, d, p, b, 0, accumulate);
-  weigh_half<DP>(leader, d, p + half, b, 1, true);
+__device__ __forceinline__ void weigh(uint32_t leader, uint32_t d, uint32_t p, uint32_t b, bool accumulate) {
+#pragma unroll
+  for (int k = 0; k < TILE / 16; ++k)
+    mma_ts(leader, d, p + (uint32_t)(k >> 1) * QUARTER + (uint32_t)(k & 1) * 8u, desc(((b >> 4) | LBO_MN) + (uint32_t)k * 128u), idesc_mn(DP),
+           accumulate || k > 0);
 }
 
 // Rows `first` .. 127 of an operand become zero (one warp); the products that follow see it.
@@ -243,21 +252,24 @@ __device__ __forceinline__ Unit unit_of(const AttnParams& p, int heads, int u) {
   return x;
 }
 
-// Whether any thread of the two warps that share a tile's rows says so (barrier `id`; both take the same turns).
-__device__ __forceinline__ bool either(int id, bool x) {
+// Whether any thread of the warps that share a tile's rows says so (barrier `id`, THREADS in all; they take the same turns).
+template <int THREADS>
+__device__ __forceinline__ bool any_of(int id, bool x) {
   uint32_t r;
   asm volatile(
       "{\n"
       ".reg .pred p, q;\n"
       "setp.ne.b32 p, %1, 0;\n"
-      "barrier.cta.red.or.pred q, %2, 64, p;\n"
+      "barrier.cta.red.or.pred q, %2, %3, p;\n"
       "selp.u32 %0, 1, 0, q;\n"
       "}\n"
       : "=r"(r)
-      : "r"((uint32_t)x), "r"(id)
+      : "r"((uint32_t)x), "r"(id), "n"(THREADS)
       : "memory");
   return r != 0;
 }
+__device__ __forceinline__ bool either(int id, bool x) { return any_of<64>(id, x); }
+
 // The next unit, asked for by the copying thread and read by every warp, through two places in turn.
 struct Next {
   uint32_t full, empty, answer;               // barriers (8 bytes a place), answers (16)
@@ -300,10 +312,11 @@ __device__ __forceinline__ int take(Next& n, volatile int* abort_flag, uint64_t 
   return u;
 }
 
-// The next unit of two warps that meet at barrier `id`: both go on or neither does.
+// The next unit of warps that meet at barrier `id`: all go on or none does.
+template <int THREADS>
 __device__ __forceinline__ int take_together(Next& n, int id, volatile int* abort_flag, uint64_t limit) {
   const int u = take<true>(n, abort_flag, limit);
-  return either(id, u == -2) ? -2 : u;
+  return any_of<THREADS>(id, u == -2) ? -2 : u;
 }
 
 struct Pipe {                                 // position in a ring of N stages
@@ -358,10 +371,9 @@ struct FwdShape {
 };
 
 template <int DP>
-__global__ void __launch_bounds__(FWD_THREADS, 1)
+__global__ void __launch_bounds__(ATTN_THREADS, 1)
 attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnParams p) {
   using Sh = FwdShape<DP>;
-  constexpr int ROW_WARPS = 16, COPY_WARP = 16, MMA_WARP = 17;
   constexpr int STAGES = Sh::STAGES;
   constexpr uint32_t OPERAND = Sh::OPERAND;
   extern __shared__ uint8_t smem_raw[];
@@ -599,7 +611,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     };
     uint32_t turn_s = 0, turn_o = 0;
     bool alive = true;
-    for (int u = blockIdx.x; u >= 0; u = alive ? take_together(next, pair_id, &abort_flag, limit) : -1) {
+    for (int u = blockIdx.x; u >= 0; u = alive ? take_together<64>(next, pair_id, &abort_flag, limit) : -1) {
       const Unit x = unit_of(p, p.heads, u);
       const Extent e = extent_of(x.tile);
       const int n_t = t ? e.n_b : e.n_a;
@@ -662,15 +674,14 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
   using Sh = BackShape<DP>;
   constexpr int STAGES = Sh::STAGES;
   constexpr uint32_t OPERAND = Sh::OPERAND;
-  constexpr int ROW_WARPS = 8, COPY_WARP = 8, MMA_WARP = 9;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bar_q, bar_qempty, bar_kfull[STAGES], bar_kempty[STAGES], bar_vfull[STAGES], bar_vempty[STAGES], bar_s[2], bar_dp, bar_dpfree,
+  __shared__ __align__(8) uint64_t bar_q, bar_qempty, bar_kfull[STAGES], bar_kempty[STAGES], bar_vfull[STAGES], bar_vempty[STAGES], bar_s[2], bar_dp,
       bar_ds, bar_done;
   __shared__ __align__(16) uint4 next_answer[2];
   __shared__ __align__(8) uint64_t bar_next[2], bar_taken[2];
   __shared__ uint32_t tmem_base_slot;
   __shared__ volatile int abort_flag;
-  __shared__ float row_part[2][2][TILE];      // halves of a row's delta, two units in turn
+  __shared__ float row_part[2][4][TILE];      // quarters of a row's delta, two units in turn
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -688,8 +699,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
     mbar_init(smem_u32(&bar_s[0]), 1);
     mbar_init(smem_u32(&bar_s[1]), 1);
     mbar_init(smem_u32(&bar_dp), 1);
-    mbar_init(smem_u32(&bar_dpfree), 8);
-    mbar_init(smem_u32(&bar_ds), 8);
+    mbar_init(smem_u32(&bar_ds), ROW_WARPS);
     mbar_init(smem_u32(&bar_done), 1);
   };
   ATTN_BEGIN(512)
@@ -740,14 +750,17 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
       const AttnTile x = unit_of(p, p.heads, u).tile;
       const int n = x.offset / TILE + 1;      // key tiles
       const int tail = x.length - (n - 1) * TILE;              // rows of the last one that exist, when below 128
-      // scores and dp of key tile j, which is step `k`
+      // scores of key tile j, which is step `k`, and dp
       auto start = [&](const Pipe& q, int j, uint32_t k) {
         if (!wait(&bar_kfull[q.stage], q.phase)) return false;
         if (j == n - 1 && tail < TILE) zero_rows<DP>(s_k + q.stage * OPERAND, tail, lane);
         tc_fence_after();
         scores<DP>(leader, tm + (k & 1u) * 128, s_q, s_k + q.stage * OPERAND);
         mma_commit(leader, smem_u32(&bar_s[k & 1u]));
-        if (!wait(&bar_vfull[at_v.stage], at_v.phase) || !wait(&bar_dpfree, (k & 1u) ^ 1u)) return false;
+        return true;
+      };
+      auto start_dp = [&](int j) {
+        if (!wait(&bar_vfull[at_v.stage], at_v.phase)) return false;
         tc_fence_after();
         scores<DP>(leader, tm + TM_DP, s_g, s_v + at_v.stage * OPERAND);
         mma_commit(leader, smem_u32(&bar_dp));
@@ -756,7 +769,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
         if (j == n - 1) mma_commit(leader, smem_u32(&bar_qempty));
         return true;
       };
-      alive = wait(&bar_q, turn) && start(at, 0, step);
+      alive = wait(&bar_q, turn) && start(at, 0, step) && start_dp(0);
       for (int j = 0; alive && j < n; ++j, ++step) {
         Pipe ahead = at;
         ahead.next<STAGES>();
@@ -764,40 +777,47 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
         alive = alive && wait(&bar_ds, step & 1u);
         if (!alive) break;
         tc_fence_after();
-        weigh<DP>(leader, tm + TM_DQ, tm + (step & 1u) * 128, HALF, s_k + at.stage * OPERAND, j > 0);
+        weigh<DP>(leader, tm + TM_DQ, tm + (step & 1u) * 128, s_k + at.stage * OPERAND, j > 0);
         mma_commit(leader, smem_u32(&bar_kempty[at.stage]));
         if (j + 1 == n) mma_commit(leader, smem_u32(&bar_done));
+        if (j + 1 < n) alive = start_dp(j + 1);
         at = ahead;
       }
     }
   } else if (warp < COPY_WARP) {
-    const int half = warp >> 2, quarter = warp & 3;
+    const int part = warp >> 2, quarter = warp & 3;            // columns 32 part .. of rows 32 quarter ..
     const int row = quarter * 32 + lane;
     const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
     const float c = p.scale * LOG2_E;
-    const int pair_id = 1 + quarter;                           // barrier of the two warps that share these rows
+    const int id = 1 + quarter;                                // barrier of the four warps that share these rows
     uint32_t turn = 0, step = 0;
     const Pair c2 = both(c);
     bool alive = true;
-    for (int u = blockIdx.x; u >= 0; u = alive ? take_together(next, pair_id, &abort_flag, limit) : -1, turn ^= 1u) {
+    for (int u = blockIdx.x; u >= 0; u = alive ? take_together<128>(next, id, &abort_flag, limit) : -1, turn ^= 1u) {
       const Unit x = unit_of(p, p.heads, u);
       const int n = x.tile.offset / TILE + 1;
       const int pos = x.tile.offset + row;
       const bool ok = pos < x.tile.length;
       const int64_t token = (int64_t)x.tile.start + (ok ? pos : 0), stat = (int64_t)x.head * p.tokens + token;
-      float* const mine = &row_part[turn][half][row];
-      const float* const other = &row_part[turn][half ^ 1][row];
+      // the row's sum of what its four threads have, in the same order in all of them
+      auto row_sum = [&](float x, bool failed, float* sum) {
+        row_part[turn][part][row] = x;
+        if (any_of<128>(id, failed)) return false;
+        const float* q = &row_part[turn][0][row];
+        *sum = (q[0] + q[TILE]) + (q[2 * TILE] + q[3 * TILE]);
+        return true;
+      };
       const Pair shift = both(-p.lse[stat] * LOG2_E);
-      // delta = do . o, with o as it was rounded; each of the row's two threads has half of it.  A row with a single key tile takes the
+      // delta = do . o, with o as it was rounded; each of the row's four threads has a quarter of it.  A row with a single key tile takes the
       // sum of p dp below instead: there o is nearly as large as v, and its rounding would show in dq.
       float delta = 0.f;
       if (n > 1) {
-        const int c0 = half * (DP / 2);
+        const int c0 = part * (DP / 4);
         const __nv_bfloat16* o = reinterpret_cast<const __nv_bfloat16*>(p.o) + (token * p.heads + x.head) * p.dim + c0;
         const __nv_bfloat16* g = reinterpret_cast<const __nv_bfloat16*>(p.g) + token * p.g_ts + x.head * p.g_hs + c0;
         Pair acc = both(0.f);
 #pragma unroll
-        for (int e = 0; e < DP / 2; e += 8) {
+        for (int e = 0; e < DP / 4; e += 8) {
           if (c0 + e >= p.dim) break;
           const uint4 a = *reinterpret_cast<const uint4*>(o + e), b = *reinterpret_cast<const uint4*>(g + e);
           acc = fma2(pair_bf16(a.x), pair_bf16(b.x), acc);
@@ -806,25 +826,20 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
           acc = fma2(pair_bf16(a.w), pair_bf16(b.w), acc);
         }
         const float2 sums = parts(acc);
-        const float part = sums.x + sums.y;
-        *mine = part;
-        either(pair_id, false);
-        delta = half ? *other + part : part + *other;
-        if (half == 0 && ok) p.delta[stat] = delta;
+        row_sum(sums.x + sums.y, false, &delta);
+        if (part == 0 && ok) p.delta[stat] = delta;
       }
       for (int j = 0; j < n; ++j, ++step) {
-        const uint32_t t_s = t_lane + (step & 1u) * 128 + half * HALF;
+        const uint32_t t_s = t_lane + (step & 1u) * 128 + part * QUARTER;
         alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s[step & 1u]), (step >> 1) & 1u, &abort_flag, limit));
         if (!alive && n > 1) break;
         tc_fence_after();
-        uint32_t s[64], d[64];
+        uint32_t s[32], d[32];
         tm_load32(t_s, s);
-        tm_load32(t_s + 32, s + 32);
         tm_load_wait();
         after_load(s);
-        after_load(s + 32);
 #pragma unroll
-        for (int e = 0; e < 64; e += 2) {
+        for (int e = 0; e < 32; e += 2) {
           const float2 y = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, shift));
           s[e] = __float_as_uint(exp2_approx(y.x));
           s[e + 1] = __float_as_uint(exp2_approx(y.y));
@@ -832,53 +847,46 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
         if (alive) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), step & 1u, &abort_flag, limit));
         if (!alive && n > 1) break;
         tc_fence_after();
-        tm_load32(t_lane + TM_DP + half * HALF, d);
-        tm_load32(t_lane + TM_DP + half * HALF + 32, d + 32);
+        tm_load32(t_lane + TM_DP + part * QUARTER, d);
         tm_load_wait();
         after_load(d);
-        after_load(d + 32);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cta(smem_u32(&bar_dpfree));
-        uint32_t w[32];
+        uint32_t w[16];
         if (j == n - 1) {                     // where the key comes after the query: no weight, whatever the products hold
           if (n == 1) {
-            float part = 0.f;
+            float sum = 0.f;
 #pragma unroll
-            for (int e = 0; e < 64; ++e) part += half * 64 + e > row ? 0.f : __uint_as_float(s[e]) * __uint_as_float(d[e]);
-            *mine = part;
-            if (either(pair_id, !alive)) { alive = false; break; }
-            delta = half ? *other + part : part + *other;
-            if (half == 0 && ok) p.delta[stat] = delta;
+            for (int e = 0; e < 32; ++e) sum += part * 32 + e > row ? 0.f : __uint_as_float(s[e]) * __uint_as_float(d[e]);
+            if (!row_sum(sum, !alive, &delta)) { alive = false; break; }
+            if (part == 0 && ok) p.delta[stat] = delta;
           }
 #pragma unroll
-          for (int e = 0; e < 64; e += 2) {
+          for (int e = 0; e < 32; e += 2) {
             const float a = __uint_as_float(s[e]) * (__uint_as_float(d[e]) - delta);
             const float b = __uint_as_float(s[e + 1]) * (__uint_as_float(d[e + 1]) - delta);
-            w[e >> 1] = pack_bf16x2(half * 64 + e > row ? 0.f : a, half * 64 + e + 1 > row ? 0.f : b);
+            w[e >> 1] = pack_bf16x2(part * 32 + e > row ? 0.f : a, part * 32 + e + 1 > row ? 0.f : b);
           }
         } else {
           const Pair minus = both(-delta);
 #pragma unroll
-          for (int e = 0; e < 64; e += 2) {
+          for (int e = 0; e < 32; e += 2) {
             const float2 y = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
                                         add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), minus)));
             w[e >> 1] = pack_bf16x2(y.x, y.y);
           }
         }
-        tm_store32(t_s, w);
+        tm_store16(t_s, w);
         tm_store_wait();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive_cta(smem_u32(&bar_ds));
       }
       if (alive) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_done), turn, &abort_flag, limit));
-      alive = !either(pair_id, !alive);
-      if (alive) {
+      alive = !any_of<128>(id, !alive);
+      if (alive && part < DP / 32) {
         tc_fence_after();
         __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(p.out) + (token * p.heads + x.head) * p.dim;
         const bool wide = (p.dim & 15) == 0 && ((uintptr_t)p.out & 31) == 0;
-        store_columns(t_lane + TM_DQ, out, half * (DP / 2), DP / 2, p.dim, p.scale, ok, wide);
+        store_columns(t_lane + TM_DQ, out, part * 32, 32, p.dim, p.scale, ok, wide);
       }
     }
   }
@@ -894,7 +902,6 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   using Sh = BackShape<DP>;
   constexpr int STAGES = Sh::STAGES;
   constexpr uint32_t OPERAND = Sh::OPERAND;
-  constexpr int ROW_WARPS = 8, COPY_WARP = 8, MMA_WARP = 9;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bar_kv, bar_kvempty, bar_qfull[STAGES], bar_qempty[STAGES], bar_gfull[STAGES], bar_gempty[STAGES], bar_s, bar_dp,
       bar_p, bar_ds, bar_done;
@@ -902,7 +909,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
   __shared__ __align__(8) uint64_t bar_next[2], bar_taken[2];
   __shared__ uint32_t tmem_base_slot;
   __shared__ volatile int abort_flag;
-  __shared__ __align__(16) float row_values[8][2][64];         // of each row warp: log-sum-exp and delta of its 64 queries, negated
+  __shared__ __align__(16) float row_values[ROW_WARPS][2][32]; // of each row warp: log-sum-exp and delta of its 32 queries, negated
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -919,8 +926,8 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     }
     mbar_init(smem_u32(&bar_s), 1);
     mbar_init(smem_u32(&bar_dp), 1);
-    mbar_init(smem_u32(&bar_p), 8);
-    mbar_init(smem_u32(&bar_ds), 8);
+    mbar_init(smem_u32(&bar_p), ROW_WARPS);
+    mbar_init(smem_u32(&bar_ds), ROW_WARPS);
     mbar_init(smem_u32(&bar_done), 1);
   };
   ATTN_BEGIN(512)
@@ -1000,7 +1007,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_p), step & 1u, &abort_flag, limit));
         if (!alive) break;
         tc_fence_after();
-        weigh<DP>(leader, tm + TM_DV, tm, HALF, s_g + at.stage * OPERAND, it > 0);
+        weigh<DP>(leader, tm + TM_DV, tm, s_g + at.stage * OPERAND, it > 0);
         mma_commit(leader, smem_u32(&bar_gempty[at.stage]));
         Pipe ahead = at;
         ahead.next<STAGES>();
@@ -1015,7 +1022,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_ds), step & 1u, &abort_flag, limit));
         if (!alive) break;
         tc_fence_after();
-        weigh<DP>(leader, tm + TM_DK, tm + TM_DP, HALF, s_q + at.stage * OPERAND, it > 0);
+        weigh<DP>(leader, tm + TM_DK, tm + TM_DP, s_q + at.stage * OPERAND, it > 0);
         mma_commit(leader, smem_u32(&bar_qempty[at.stage]));
         if (it + 1 == x.n) mma_commit(leader, smem_u32(&bar_done));
         at = ahead;
@@ -1023,14 +1030,14 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       }
     }
   } else if (warp < COPY_WARP) {
-    const int half = warp >> 2, quarter = warp & 3;
+    const int part = warp >> 2, quarter = warp & 3;            // columns 32 part .. (queries) of rows 32 quarter ..
     const int row = quarter * 32 + lane;                       // key of the tile
     const uint32_t t_lane = tm + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t t_s = t_lane + half * HALF, t_dp = t_lane + TM_DP + half * HALF;
+    const uint32_t t_s = t_lane + part * QUARTER, t_dp = t_lane + TM_DP + part * QUARTER;
     const float c = p.scale * LOG2_E;
     const Pair c2 = both(c);
-    // each warp brings the log-sum-exp and the delta of its 64 queries into shared memory, fetched a step ahead
-    const int col0 = half * 64;
+    // each warp brings the log-sum-exp and the delta of its 32 queries into shared memory, fetched a step ahead
+    const int col0 = part * 32;
     float* const lse = row_values[warp][0];
     float* const delta = row_values[warp][1];
     uint32_t turn = 0, step = 0;
@@ -1039,15 +1046,12 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
       const Unit x = unit_of(p, kv_heads, u);
       const Extent ext = extent_of(x.tile);
       int head = x.head * p.group, i = ext.first;
-      float ahead[4];
+      float ahead[2];
       auto fetch = [&] {
-  #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int pos = i * TILE + col0 + h * 32 + lane;
-          const int64_t at = (int64_t)head * p.tokens + x.tile.start + pos;
-          ahead[h] = pos < x.tile.length ? -LOG2_E * p.lse[at] : 0.f;
-          ahead[2 + h] = pos < x.tile.length ? -p.delta[at] : 0.f;
-        }
+        const int pos = i * TILE + col0 + lane;
+        const int64_t at = (int64_t)head * p.tokens + x.tile.start + pos;
+        ahead[0] = pos < x.tile.length ? -LOG2_E * p.lse[at] : 0.f;
+        ahead[1] = pos < x.tile.length ? -p.delta[at] : 0.f;
       };
       fetch();
       for (int it = 0; it < ext.n; ++it, ++step) {
@@ -1056,23 +1060,19 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         const int from = i == ext.first ? row : 0;
         __syncwarp();
         lse[lane] = ahead[0];
-        lse[32 + lane] = ahead[1];
-        delta[lane] = ahead[2];
-        delta[32 + lane] = ahead[3];
+        delta[lane] = ahead[1];
         __syncwarp();
         if (++i == ext.end) { i = ext.first; ++head; }
         if (it + 1 < ext.n) fetch();
         alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_s), step & 1u, &abort_flag, limit));
         if (!alive) break;
-        uint32_t s[64], w[32];
+        uint32_t s[32], w[16];
         tc_fence_after();
         tm_load32(t_s, s);
-        tm_load32(t_s + 32, s + 32);
         tm_load_wait();
         after_load(s);
-        after_load(s + 32);
   #pragma unroll
-        for (int e = 0; e < 64; e += 4) {
+        for (int e = 0; e < 32; e += 4) {
           const float4 l = *reinterpret_cast<const float4*>(lse + e);
           const float2 x = parts(fma2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), c2, pair(l.x, l.y)));
           const float2 y = parts(fma2(pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])), c2, pair(l.z, l.w)));
@@ -1083,11 +1083,11 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         }
         if (edge) {
   #pragma unroll
-          for (int e = 0; e < 64; ++e) s[e] = col0 + e < from || col0 + e > last ? 0u : s[e];
+          for (int e = 0; e < 32; ++e) s[e] = col0 + e < from || col0 + e > last ? 0u : s[e];
         }
   #pragma unroll
-        for (int e = 0; e < 64; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-        tm_store32(t_s, w);
+        for (int e = 0; e < 32; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+        tm_store16(t_s, w);
         tm_store_wait();
         tc_fence_before();
         __syncwarp();
@@ -1095,14 +1095,12 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), step & 1u, &abort_flag, limit));
         if (!alive) break;
         tc_fence_after();
-        uint32_t d[64];
+        uint32_t d[32];
         tm_load32(t_dp, d);
-        tm_load32(t_dp + 32, d + 32);
         tm_load_wait();
         after_load(d);
-        after_load(d + 32);
   #pragma unroll
-        for (int e = 0; e < 64; e += 4) {
+        for (int e = 0; e < 32; e += 4) {
           const float4 l = *reinterpret_cast<const float4*>(delta + e);
           const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
                                       add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pair(l.x, l.y))));
@@ -1113,11 +1111,11 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         }
         if (edge) {                           // (zero times what the products hold there need not be zero)
   #pragma unroll
-          for (int e = 0; e < 64; ++e) d[e] = col0 + e < from || col0 + e > last ? 0u : d[e];
+          for (int e = 0; e < 32; ++e) d[e] = col0 + e < from || col0 + e > last ? 0u : d[e];
         }
   #pragma unroll
-        for (int e = 0; e < 64; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1]));
-        tm_store32(t_dp, w);
+        for (int e = 0; e < 32; e += 2) w[e >> 1] = pack_bf16x2(__uint_as_float(d[e]), __uint_as_float(d[e + 1]));
+        tm_store16(t_dp, w);
         tm_store_wait();
         tc_fence_before();
         __syncwarp();
@@ -1130,9 +1128,10 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
           const int pos = x.tile.offset + row;
           const bool ok = pos < x.tile.length;
           const int64_t at = (((int64_t)x.tile.start + (ok ? pos : 0)) * kv_heads + x.head) * p.dim;
-          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(half ? p.out : p.out2) + at;
+          const bool keys = part >= 2;          // two warps have dv, two dk
+          __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(keys ? p.out : p.out2) + at;
           const bool wide = (p.dim & 15) == 0 && (((uintptr_t)p.out | (uintptr_t)p.out2) & 31) == 0;
-          store_columns(t_lane + (half ? TM_DK : TM_DV), out, 0, DP, p.dim, half ? p.scale : 1.0f, ok, wide);
+          store_columns(t_lane + (keys ? TM_DK : TM_DV), out, (part & 1) * (DP / 2), DP / 2, p.dim, keys ? p.scale : 1.0f, ok, wide);
         }
       }
     }
@@ -1160,7 +1159,7 @@ cudaError_t run_forward(cudaStream_t st, const Maps4& m, const AttnParams& p) {
   static std::atomic<uint64_t> allowed{0};
   const cudaError_t e = allow_smem(attn_fwd_kernel<DP>, (int)FwdShape<DP>::SMEM, &allowed);
   if (e != cudaSuccess) return e;
-  return launch_dependent(attn_fwd_kernel<DP>, (unsigned)(p.n_tiles * p.heads), FWD_THREADS, FwdShape<DP>::SMEM, st, m, p);
+  return launch_dependent(attn_fwd_kernel<DP>, (unsigned)(p.n_tiles * p.heads), ATTN_THREADS, FwdShape<DP>::SMEM, st, m, p);
 }
 
 template <int DP>
