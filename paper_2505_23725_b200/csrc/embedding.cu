@@ -181,18 +181,34 @@ __device__ __forceinline__ int64_t below(const uint64_t* p, int64_t n, uint64_t 
 }
 
 // Merges groups of EMB_MERGE sorted blocks of `block` pairs (a power of two): a pair's place is the count of smaller ones (no two are
-// equal).  The searches in the other blocks go step by step together, so that their loads overlap.
-// Both kernels are small blocks: their searches read scattered places, 32 to an instruction, which a multiprocessor serves one by one (blocks of 2048
-// pairs and 256 threads: 15 and 15 us for 16384 tokens).
-constexpr int MERGE_THREADS = 64;
-__global__ void __launch_bounds__(MERGE_THREADS)
+// equal).  The searches in the other blocks go step by step together, so that their loads overlap.  STAGED (the first merge, whose groups are
+// small enough): a group's pairs are brought into shared memory in one go, where a step of a search is a tenth of the time.
+// Both are small thread blocks: searches read scattered places, 32 to an instruction, which a multiprocessor serves one by one (sorted blocks of
+// 2048 pairs and 256 threads a merge: 15 and 15 us for 16384 tokens, 7 and 10 as it is).
+template <bool STAGED> __host__ __device__ constexpr int merge_threads() { return STAGED ? 128 : 64; }
+constexpr int GROUP = EMB_SORT_BLOCK * EMB_MERGE;
+template <bool STAGED>
+__global__ void __launch_bounds__(merge_threads<STAGED>())
 merge_kernel(const uint64_t* in, uint64_t* out, int64_t tokens, int64_t block) {
+  constexpr int THREADS_ = merge_threads<STAGED>();
+  __shared__ __align__(16) uint64_t staged[STAGED ? GROUP : 1];
   grid_wait();
   grid_release();
-  const int64_t t = (int64_t)blockIdx.x * MERGE_THREADS + threadIdx.x;
+  const int64_t t = (int64_t)blockIdx.x * THREADS_ + threadIdx.x;
+  const int64_t first = ((int64_t)blockIdx.x * THREADS_) & ~(block * EMB_MERGE - 1);    // (a thread block's pairs are of one group)
+  const uint64_t* from = in + first;
+  if (STAGED) {
+    const int n = (int)(tokens - first < GROUP ? tokens - first : GROUP);
+#pragma unroll 8
+    for (int i = threadIdx.x; 2 * i < n; i += THREADS_) {
+      // (the scratch that pairs lie in has room for an even count of them)
+      reinterpret_cast<ulonglong2*>(staged)[i] = reinterpret_cast<const ulonglong2*>(from)[i];
+    }
+    __syncthreads();
+    from = staged;
+  }
   if (t >= tokens) return;
-  const uint64_t x = in[t];
-  const int64_t first = t & ~(block * EMB_MERGE - 1);
+  const uint64_t x = from[t - first];
   const int own = (int)((t - first) / block);
   uint32_t k[EMB_MERGE], n[EMB_MERGE];
 #pragma unroll
@@ -204,7 +220,7 @@ merge_kernel(const uint64_t* in, uint64_t* out, int64_t tokens, int64_t block) {
   for (uint32_t step = (uint32_t)block; step; step >>= 1) {
     uint64_t y[EMB_MERGE];
 #pragma unroll
-    for (int b = 0; b < EMB_MERGE; ++b) y[b] = k[b] + step <= n[b] ? in[first + b * block + (k[b] + step - 1)] : ~0ull;
+    for (int b = 0; b < EMB_MERGE; ++b) y[b] = k[b] + step <= n[b] ? from[b * block + (k[b] + step - 1)] : ~0ull;
 #pragma unroll
     for (int b = 0; b < EMB_MERGE; ++b)
       if (y[b] < x) k[b] += step;
@@ -404,7 +420,10 @@ cudaError_t launch_embedding_backward(cudaStream_t st, const EmbeddingArgs& args
   cudaError_t e = launch_dependent(sort_kernel, (unsigned)((a.tokens + EMB_SORT_BLOCK - 1) / EMB_SORT_BLOCK), SORT_THREADS, 0, st, a, pairs);
   ++*launches;
   for (int64_t block = EMB_SORT_BLOCK; e == cudaSuccess && block < a.tokens; block *= EMB_MERGE) {
-    e = launch_dependent(merge_kernel, (unsigned)((a.tokens + MERGE_THREADS - 1) / MERGE_THREADS), MERGE_THREADS, 0, st, (const uint64_t*)pairs, other, a.tokens, block);
+    const bool staged = block == EMB_SORT_BLOCK;
+    const int threads = staged ? merge_threads<true>() : merge_threads<false>();
+    e = launch_dependent(staged ? merge_kernel<true> : merge_kernel<false>, (unsigned)((a.tokens + threads - 1) / threads), threads, 0, st,
+                         (const uint64_t*)pairs, other, a.tokens, block);
     ++*launches;
     uint64_t* t = pairs;
     pairs = other;
