@@ -494,7 +494,8 @@ MULOCO_API void muloco_sequences_destroy(muloco_sequences* s);      /* host memo
  * h / (heads_q / heads_k).  scale > 0.  Results are dense.  o [tokens][heads_q][head_dim] and lse [heads_q][tokens]
  * (float32) of tokens that belong to no sequence are zero, and so are their gradients.  What such tokens
  * and other sequences hold does not matter, infinities and NaN included; a value that is not finite reaches
- * rows of its own sequence only (also earlier ones, in the tile of 128 tokens that it is in).
+ * rows of its own sequence only (also earlier ones, in the tile of 128 tokens that it is in).  Sums of weights may reach 2^16 per
+ * 64 keys before they are scaled down, so entries of v beyond about 2^100 may overflow.
  * Limits (MULOCO_ESHAPE): head_dim a multiple of 8, 8..128; heads_q a multiple of heads_k; tokens < 2^31 - 256. */
 typedef struct {
   int32_t heads_q, heads_k, head_dim;
@@ -519,7 +520,8 @@ MULOCO_API muloco_status muloco_causal_attention_backward(muloco_ctx* ctx, const
  * `dtype`; without a residual h is x and not written.  weight and bias are float32 [d] or NULL (ones, zeros).  mean and rstd (float32
  * [tokens]; mean only when centred) are for the backward pass.  Statistics are float32, the variance around the
  * mean; y is made from the sum before it is rounded to h, and rounded once.
- * ldx, ldr: row strides of x and residual in elements; h and y are dense.  y may be x (or residual), and h too, where that one is dense.
+ * ldx, ldr: row strides of x and residual in elements; h and y are dense.  y or h may be x or the residual, where that one is dense;
+ * otherwise results must not overlap inputs.
  * Limits (MULOCO_ESHAPE): d in 1..32768, tokens < 2^31. */
 typedef struct {
   int64_t tokens, d, ldx, ldr;

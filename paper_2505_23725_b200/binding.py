@@ -834,7 +834,8 @@ class Sequences:
 
     @property
     def positions(self):
-        """int64 [tokens]: every token's place in its sequence, 0 behind the last one (for the position rotation)."""
+        """int64 [tokens]: every token's place in its sequence, 0 behind the last one (for the position rotation).  Copied to the
+        device when it is first asked for, which cannot be captured into a graph."""
         if self._positions is None:
             torch = self.owner.torch
             p = torch.zeros(self.tokens, dtype=torch.int64)

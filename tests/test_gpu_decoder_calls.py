@@ -313,6 +313,107 @@ def test_calls_allocate_nothing_of_their_own(ctx):
     assert torch.cuda.mem_get_info()[0] == free
 
 
+def test_many_sequences_of_one_token(ctx):
+    """More units than the grid has places for, each a row of its own: o is v, nothing flows into q and k."""
+    T = 3000
+    q, k, v, do = qkv(T, 4, 2, 64, seed=11)
+    lengths = [1, 0] * T
+    seq = binding.Sequences(ctx, lengths)
+    o, lse = ctx.causal_attention(q, k, v, seq)
+    assert torch.equal(o, v.repeat_interleave(2, 1))
+    dq, dk, dv = ctx.causal_attention_backward(do, q, k, v, o, lse, seq)
+    # ds = p (dp - p dp), p within 2^-18 of 1 (the scores' rounding): 2^-18 of the products' magnitudes
+    dp = (do.float().abs() * v.float().abs().repeat_interleave(2, 1)).sum(2, keepdim=True)
+    assert (dq.float().abs() <= 2.0 ** -18 * dp * k.float().abs().repeat_interleave(2, 1) + 1e-30).all()
+    want = do.double().view(T, 2, 2, 64).sum(2)
+    size = do.double().abs().view(T, 2, 2, 64).sum(2)
+    assert ((dv.double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -8 + 2.0 ** -16) * size).all()
+    ctx.sync_status()
+
+
+def test_results_in_place_of_inputs(ctx):
+    """What the header allows a C caller: y or h over x, or over the residual."""
+    x, r = rand(300, 1000, seed=1), rand(300, 1000, seed=2)
+    want, h, rstd, mean = ctx.layer_norm(x, residual=r)
+    for y_over, h_over in (("x", "r"), ("r", "x"), (None, "x"), ("x", None)):
+        t = dict(x=x.clone(), r=r.clone())
+        y, hh = (t[o] if o else torch.empty_like(x) for o in (y_over, h_over))
+        a = ctx._norm(t["x"], None, None, t["r"], "residual", 1e-6, True)
+        assert ctx.lib.muloco_layer_norm(ctx.ctx, a, hh.data_ptr(), y.data_ptr(), torch.empty_like(mean).data_ptr(),
+                                         torch.empty_like(rstd).data_ptr()) == binding.OK
+        assert torch.equal(y, want) and torch.equal(hh, h)
+    wide = rand(300, 1008)
+    a = ctx._norm(wide[:, :1000], None, None, None, "residual", 1e-6, False)
+    assert ctx.lib.muloco_layer_norm(ctx.ctx, a, None, wide.data_ptr(), None, rstd.data_ptr()) == binding.EINVAL
+
+
+def test_offsets_beyond_32_bits(ctx):
+    """Tensors of more than 2^31 entries: their last rows come out as on their own."""
+    heads, dim, last = 120, 128, 200
+    lengths = [128] * 1100 + [last]
+    T = sum(lengths)
+    assert T * heads * dim > 2 ** 31
+    q, k, v, do = (torch.zeros(T, heads, dim, dtype=BF16, device="cuda") for _ in range(4))
+    for i, t in enumerate((q, k, v, do)):
+        t[-last:] = rand(last, heads, dim, seed=i)
+    seq, own = binding.Sequences(ctx, lengths), binding.Sequences(ctx, [last])
+    o, lse = ctx.causal_attention(q, k, v, seq)
+    tails = [t[-last:].clone() for t in (q, k, v, do)]
+    o2, lse2 = ctx.causal_attention(*tails[:3], own)
+    assert torch.equal(o[-last:], o2) and torch.equal(lse[:, -last:], lse2)
+    got = ctx.causal_attention_backward(do, q, k, v, o, lse, seq)
+    for a, b in zip(got, ctx.causal_attention_backward(tails[3], *tails[:3], o2, lse2, own)):
+        assert torch.equal(a[-last:], b) and not a[:100].any()
+    del q, k, v, do, o, got
+    d = 2048
+    rows = 2 ** 31 // d + 300
+    x = torch.zeros(rows, d, dtype=BF16, device="cuda")
+    x[-50:] = rand(50, d, seed=5)
+    y, _, rstd, mean = ctx.layer_norm(x)
+    assert torch.equal(y[-50:], ctx.layer_norm(x[-50:].clone())[0])
+    w = torch.ones(d, device="cuda")
+    dx, _, _ = ctx.layer_norm_backward(x, x, rstd, mean, weight=w)
+    assert torch.equal(dx[-50:], ctx.layer_norm_backward(*(t[-50:].clone() for t in (x, x, rstd, mean)), weight=w)[0])
+    del y, dx
+    ids = torch.tensor([rows - 1, 3, rows - 30, rows - 1], device="cuda")
+    assert torch.equal(ctx.embedding(ids, x), x[ids])
+    g = rand(4, d, seed=6)
+    grad = ctx.embedding_backward(g, ids, rows, dtype=BF16)
+    assert torch.equal(grad[rows - 30], g[2]) and torch.equal(grad[rows - 1], (g[0].float() + g[3].float()).to(BF16))
+    assert not grad[rows - 29:rows - 1].any()
+    ctx.sync_status()
+
+
+def test_two_graphs_side_by_side():
+    """Graphs of two contexts replayed on two streams at once: no workspace is shared."""
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    owners = [binding.Context("cuda:0", stream=s) for s in streams]
+    sets = [inputs(seed=20 + i) for i in range(2)]
+    seqs = [binding.Sequences(o, LENGTHS, 333) for o in owners]
+    torch.cuda.synchronize()
+    graphs, outs, wants = [], [], []
+    for s, o, q, a in zip(streams, owners, seqs, sets):
+        with torch.cuda.stream(s):
+            wants.append([t.clone() for t in everything(o, q, *a)])
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            outs.append(everything(o, q, *a))
+        graphs.append(g)
+    for _ in range(30):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    for out, want in zip(outs, wants):
+        assert all(torch.equal(a, b) for a, b in zip(out, want))
+    for o in owners:
+        o.sync_status()
+    del graphs, g, outs, out
+    for o in owners:
+        o.close()
+
+
 def block(ops, p, ids, seq, cos, sin, heads):
     """A decoder block as they are used together: embedding, norm, rotation, attention, norm with the stream, feed-forward."""
     T, dim = ids.shape[0], cos.shape[1] * 2
