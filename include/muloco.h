@@ -582,7 +582,7 @@ MULOCO_API muloco_status muloco_set_timing(muloco_ctx* ctx, int32_t enabled);
  * last call to *launches (either may be NULL), then resets both. */
 MULOCO_API muloco_status muloco_get_timings(muloco_ctx* ctx, float* ms, int64_t* launches);
 
-/* Test hooks for the failure path of the tensor-core kernels (Newton-Schulz, feed-forward), whose every
+/* Test hooks for the failure path of the tensor-core kernels (Newton-Schulz, feed-forward, attention), whose every
  * device-side wait (on a copy, on the tensor cores, on another CTA's tiles) has a time limit.
  *   MULOCO_DEBUG_WAIT_LIMIT_NS : that limit in nanoseconds (0 restores the default of 2 s).
  *   MULOCO_DEBUG_WITHHOLD_COPY : value != 0 makes the NEXT tensor-core launch of this context

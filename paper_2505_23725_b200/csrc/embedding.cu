@@ -13,18 +13,12 @@
 // Measured: lookup of 16384 x 1024 in bf16 12.3 us (5.5 TB/s).  Gradient of a table of 32000 rows: 16384 tokens x 2048 in float32 94 us, of which
 // writing and reading everything once take 50 (the gathering kernel 61: 4.8 TB/s), sorting 20 and joining 12; 4001 x 768 in bf16
 // 25 us, five dependent kernels of about 5.
+#include "convert.cuh"
 #include "internal.h"
 
 namespace muloco {
 
 namespace {
-
-template <typename T> __device__ __forceinline__ float to_f32(T x);
-template <> __device__ __forceinline__ float to_f32(float x) { return x; }
-template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename T> __device__ __forceinline__ T from_f32(float x);
-template <> __device__ __forceinline__ float from_f32(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16(x); }
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 constexpr int SLICE = 256;                     // columns that a warp works on at a time, 8 a lane
@@ -373,8 +367,6 @@ join_kernel(const EmbeddingArgs a, const uint64_t* pairs) {
     Eight<O, WIDE>::store(f, reinterpret_cast<O*>(a.dtable) + id * a.d, col, a.d, lane);
   }
 }
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 template <typename T, typename O, bool WIDE>
 cudaError_t gather(cudaStream_t st, const EmbeddingArgs& a, const uint64_t* pairs, int* launches) {

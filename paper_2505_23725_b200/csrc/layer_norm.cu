@@ -15,19 +15,13 @@
 // per lane and the next row's loads early in registers, which the compiler moved back.
 #include <string.h>
 
+#include "convert.cuh"
 #include "internal.h"
 #include "tc_ptx.cuh"
 
 namespace muloco {
 
 namespace {
-
-template <typename T> __device__ __forceinline__ float to_f32(T x);
-template <> __device__ __forceinline__ float to_f32(float x) { return x; }
-template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename T> __device__ __forceinline__ T from_f32(float x);
-template <> __device__ __forceinline__ float from_f32(float x) { return x; }
-template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float x) { return __float2bfloat16(x); }
 
 // E entries of a row in a lane: chunks of V neighbouring entries, chunk c of lane l starts at (c lanes + l) V.
 template <typename T, int V> struct alignas(sizeof(T) * V) Chunk { T v[V]; };
@@ -398,8 +392,6 @@ cudaError_t choose(cudaStream_t st, const NormArgs& a, bool back, int n_sms, int
   if (a.d <= 8192) return forward<T, V, 32, 8>(st, a, launches);
   return forward<T, V, 32, 32>(st, a, launches);
 }
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 }  // namespace
 
