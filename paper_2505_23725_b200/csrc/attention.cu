@@ -601,6 +601,12 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
           for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * by);
           tm_store32(t_o + i, v);
         }
+        // The next product adds to all columns of the sums once the first half's weights are there: both threads of the row have
+        // rescaled theirs before either hands weights over.
+        tm_store_wait();
+        tc_fence_before();
+        either(pair_id, false);
+        tc_fence_after();
       }
       top = m;
       // (an infinite maximum makes every weight NaN, as the quotient of infinities is)
