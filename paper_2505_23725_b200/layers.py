@@ -134,9 +134,9 @@ def causal_attention(owner, q, k, v, sequences, scale=None):
 
 class _LayerNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, owner, eps, center, apart, x, weight, bias, residual):
+    def forward(ctx, owner, eps, center, x, weight, bias, residual):
         y, h, rstd, mean = owner.layer_norm(x, weight, bias, residual, eps, center)
-        ctx.owner, ctx.bias, ctx.residual, ctx.apart = owner, bias is not None, residual is not None, apart
+        ctx.owner, ctx.bias = owner, bias is not None
         ctx.save_for_backward(h, rstd, mean, weight)
         return (y, h) if residual is not None else y
 
@@ -144,9 +144,11 @@ class _LayerNorm(torch.autograd.Function):
     def backward(ctx, dy, dh=None):
         h, rstd, mean, weight = ctx.saved_tensors
         dx, dw, db = ctx.owner.layer_norm_backward(_last(dy), h, rstd, mean, weight, None if dh is None else _last(dh), ctx.bias)
-        dr = None if not ctx.residual else dx.clone() if ctx.apart else dx
+        # The same values for both addends, in a tensor each: whatever hands a gradient on unchanged (a view, a sum) lets a leaf keep
+        # it as its own, and in-place work on the one must not reach the other.
+        dr = None if not ctx.needs_input_grad[6] else dx.clone() if ctx.needs_input_grad[3] else dx
         dx, dr, dw, db = _once("layer_norm", (dx, dr, dw, db), (dy, dh, h, weight))
-        return None, None, None, None, dx, dw, db, dr
+        return None, None, None, dx, dw, db, dr
 
 
 def _last(t):
@@ -161,9 +163,7 @@ def layer_norm(owner, x, weight=None, bias=None, residual=None, eps: float = 1e-
     shape = x.shape
     x2 = _last(x.reshape(-1, shape[-1]))
     r2 = None if residual is None else _last(residual.reshape(-1, shape[-1]))
-    # one gradient serves x and the residual; where both would keep it as their own (leaves), each has one
-    apart = residual is not None and x.is_leaf and residual.is_leaf
-    out = _LayerNorm.apply(owner, eps, center, apart, x2, weight, bias, r2)
+    out = _LayerNorm.apply(owner, eps, center, x2, weight, bias, r2)
     return out.view(shape) if residual is None else tuple(t.view(shape) for t in out)
 
 
