@@ -878,6 +878,8 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 32; ++e) sum += part * 32 + e > row ? 0.f : __uint_as_float(s[e]) * __uint_as_float(d[e]);
+            // (a sequence's first query has one key, whose weight is 1, not the 1 +- 2^-18 that its rounded log-sum-exp gives: ds is zero)
+            if (part == 0 && row == 0) sum = __uint_as_float(d[0]);
             if (!row_sum(sum, !alive, &delta)) { alive = false; break; }
             if (part == 0 && ok) p.delta[stat] = delta;
           }
@@ -1080,6 +1082,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         const bool edge = i == ext.first || (i == ext.end - 1 && ext.tail < TILE);       // some of the tile's pairs do not count
         const int last = x.tile.length - i * TILE - 1;                         // columns from .. last count
         const int from = i == ext.first ? row : 0;
+        const bool single = x.tile.offset == 0 && i == ext.first && row == 0 && col0 == 0;     // the sequence's first query and key
         __syncwarp();
         lse[lane] = ahead[0];
         delta[lane] = ahead[1];
@@ -1123,7 +1126,8 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         after_load(d);
   #pragma unroll
         for (int e = 0; e < 32; e += 4) {
-          const float4 l = *reinterpret_cast<const float4*>(delta + e);
+          float4 l = *reinterpret_cast<const float4*>(delta + e);
+          if (e == 0 && single) l.x = -__uint_as_float(d[0]);  // (delta is its dp, from another kernel's product: here the same bits)
           const float2 x = parts(mul2(pair(__uint_as_float(s[e]), __uint_as_float(s[e + 1])),
                                       add2(pair(__uint_as_float(d[e]), __uint_as_float(d[e + 1])), pair(l.x, l.y))));
           const float2 y = parts(mul2(pair(__uint_as_float(s[e + 2]), __uint_as_float(s[e + 3])),
