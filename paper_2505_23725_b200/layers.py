@@ -161,6 +161,8 @@ def layer_norm(owner, x, weight=None, bias=None, residual=None, eps: float = 1e-
     root mean square norm), differentiable in x, the residual, weight and bias.  With a residual the result is (y, h): h is
     the stream that goes on."""
     shape = x.shape
+    if residual is not None and residual.shape != shape:
+        raise ValueError(f"residual must have the shape of x {tuple(shape)} (got {tuple(residual.shape)})")
     x2 = _last(x.reshape(-1, shape[-1]))
     r2 = None if residual is None else _last(residual.reshape(-1, shape[-1]))
     out = _LayerNorm.apply(owner, eps, center, x2, weight, bias, r2)
