@@ -179,46 +179,62 @@ __device__ __forceinline__ int64_t below(const uint64_t* p, int64_t n, uint64_t 
 }
 
 // Merges groups of EMB_MERGE sorted blocks of `block` pairs (a power of two): a pair's place is the count of smaller ones (no two are
-// equal).  The searches in the other blocks go step by step together, so that their loads overlap.  STAGED (the first merge, whose groups are
-// small enough): a group's pairs are brought into shared memory in one go, where a step of a search is a tenth of the time.
-// Both are small thread blocks: searches read scattered places, 32 to an instruction, which a multiprocessor serves one by one (sorted blocks of
-// 2048 pairs and 256 threads a merge: 15 and 15 us for 16384 tokens, 7 and 10 as it is).
-template <bool STAGED> __host__ __device__ constexpr int merge_threads() { return STAGED ? 128 : 64; }
-constexpr int GROUP = EMB_SORT_BLOCK * EMB_MERGE;
-template <bool STAGED>
-__global__ void __launch_bounds__(merge_threads<STAGED>())
+// equal).  The searches in the other blocks go step by step together, so that their loads overlap.  The first steps look at SAMPLES evenly
+// spaced pairs of a sorted block only: those are brought into shared memory in one go, where a step is a tenth of the time (in the first merge all pairs
+// are).  The rest is among neighbours.  Second merge of 16384 and of 70000 tokens, cold: 10.6 and 15.8 us with all steps in global memory,
+// 6.5 and 9.5 with 64 samples (32: as much; 512: 8.2 for 16384, and slower than without for 70000, as every thread block fetches its own).
+// Small thread blocks: searches read scattered places, 32 to an instruction, which a multiprocessor serves one by one.
+constexpr int MERGE_THREADS = 128, SAMPLES = 64;
+template <bool FIRST>                          // block is EMB_SORT_BLOCK
+__global__ void __launch_bounds__(MERGE_THREADS)
 merge_kernel(const uint64_t* in, uint64_t* out, int64_t tokens, int64_t block) {
-  constexpr int THREADS_ = merge_threads<STAGED>();
-  __shared__ __align__(16) uint64_t staged[STAGED ? GROUP : 1];
+  constexpr int EACH = FIRST ? EMB_SORT_BLOCK : SAMPLES, ALL = EACH * EMB_MERGE;
+  __shared__ __align__(16) uint64_t sample[ALL];               // pair (s + 1) apart - 1 of sorted block b at b EACH + s
   grid_wait();
   grid_release();
-  const int64_t t = (int64_t)blockIdx.x * THREADS_ + threadIdx.x;
-  const int64_t first = ((int64_t)blockIdx.x * THREADS_) & ~(block * EMB_MERGE - 1);    // (a thread block's pairs are of one group)
+  const int64_t t = (int64_t)blockIdx.x * MERGE_THREADS + threadIdx.x;
+  const int64_t first = ((int64_t)blockIdx.x * MERGE_THREADS) & ~(block * EMB_MERGE - 1);    // (a thread block's pairs are of one group)
   const uint64_t* from = in + first;
-  if (STAGED) {
-    const int n = (int)(tokens - first < GROUP ? tokens - first : GROUP);
+  const int64_t left = tokens - first;
+  const int64_t apart = FIRST ? 1 : block / EACH;
+  uint64_t x = 0;
+  if (FIRST) {
+    const int n = (int)(left < ALL ? left : ALL);
 #pragma unroll 8
-    for (int i = threadIdx.x; 2 * i < n; i += THREADS_) {
+    for (int i = threadIdx.x; 2 * i < n; i += MERGE_THREADS) {
       // (the scratch that pairs lie in has room for an even count of them)
-      reinterpret_cast<ulonglong2*>(staged)[i] = reinterpret_cast<const ulonglong2*>(from)[i];
+      reinterpret_cast<ulonglong2*>(sample)[i] = reinterpret_cast<const ulonglong2*>(from)[i];
     }
-    __syncthreads();
-    from = staged;
+  } else {
+    if (t < tokens) x = in[t];
+#pragma unroll 8
+    for (int i = threadIdx.x; i < ALL; i += MERGE_THREADS) {
+      const int64_t at = (i + 1) * apart - 1;                  // (whole blocks one after the other)
+      if (at < left) sample[i] = from[at];
+    }
   }
+  __syncthreads();
   if (t >= tokens) return;
-  const uint64_t x = from[t - first];
+  if (FIRST) x = sample[t - first];
   const int own = (int)((t - first) / block);
   uint32_t k[EMB_MERGE], n[EMB_MERGE];
 #pragma unroll
   for (int b = 0; b < EMB_MERGE; ++b) {
-    const int64_t left = tokens - (first + b * block);
-    n[b] = b == own || left < 0 ? 0 : (uint32_t)(left < block ? left : block);
+    const int64_t rest = left - b * block;
+    n[b] = b == own || rest < 0 ? 0 : (uint32_t)(rest < block ? rest : block);
     k[b] = 0;
   }
+  // (while step is a multiple of `apart`, so is k, and the pair that is looked at is a sample)
+  const int shift = FIRST ? 0 : 63 - __clzll(apart);
   for (uint32_t step = (uint32_t)block; step; step >>= 1) {
     uint64_t y[EMB_MERGE];
+    if (FIRST || step >> shift) {
 #pragma unroll
-    for (int b = 0; b < EMB_MERGE; ++b) y[b] = k[b] + step <= n[b] ? from[b * block + (k[b] + step - 1)] : ~0ull;
+      for (int b = 0; b < EMB_MERGE; ++b) y[b] = k[b] + step <= n[b] ? sample[b * EACH + ((k[b] + step) >> shift) - 1] : ~0ull;
+    } else {
+#pragma unroll
+      for (int b = 0; b < EMB_MERGE; ++b) y[b] = k[b] + step <= n[b] ? from[b * block + (k[b] + step - 1)] : ~0ull;
+    }
 #pragma unroll
     for (int b = 0; b < EMB_MERGE; ++b)
       if (y[b] < x) k[b] += step;
@@ -255,13 +271,12 @@ __device__ __forceinline__ Piece piece_of(const EmbeddingArgs& a, const uint64_t
   return c;
 }
 
-// Rows without tokens (units 0 .. zero_units - 1: a warp looks after 32 rows of up to ZERO_COLS columns), then chunks of the sorted order (a chunk and
+// Rows without tokens (units 0 .. zero_units - 1: a warp looks after 32 rows of up to zero_cols columns), then chunks of the sorted order (a chunk and
 // a slice each).
-constexpr int ZERO_COLS = 1024;
 constexpr int GATHER_WARPS = 4;
 template <typename T, typename O, bool WIDE>
 __global__ void __launch_bounds__(32 * GATHER_WARPS)
-gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t zero_units, int64_t chunk_units) {
+gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int zero_cols, int64_t zero_units, int64_t chunk_units) {
   const int lane = threadIdx.x & 31;
   int64_t unit = (int64_t)blockIdx.x * GATHER_WARPS + (threadIdx.x >> 5);
   grid_wait();
@@ -307,9 +322,9 @@ gather_kernel(const EmbeddingArgs a, const uint64_t* pairs, int64_t zero_units, 
     }
     return;
   }
-  const int parts = (a.d + ZERO_COLS - 1) / ZERO_COLS;
+  const int parts = (a.d + zero_cols - 1) / zero_cols;
   const int64_t first = unit / parts * 32;
-  const int col0 = (int)(unit % parts) * ZERO_COLS, col1 = col0 + ZERO_COLS < a.d ? col0 + ZERO_COLS : a.d;
+  const int col0 = (int)(unit % parts) * zero_cols, col1 = col0 + zero_cols < a.d ? col0 + zero_cols : a.d;
   const int64_t start = below(pairs, a.tokens, (uint64_t)(first + lane) << 32);
   const bool none = first + lane < a.rows && (start == a.tokens || id_of(pairs[start]) != first + lane);
   const float zero[8] = {};
@@ -372,11 +387,14 @@ template <typename T, typename O, bool WIDE>
 cudaError_t gather(cudaStream_t st, const EmbeddingArgs& a, const uint64_t* pairs, int* launches) {
   const int64_t slices = (a.d + SLICE - 1) / SLICE;
   const int64_t chunks = (a.tokens + CHUNK - 1) / CHUNK;
-  const int64_t zero_units = (a.rows + 31) / 32 * ((a.d + ZERO_COLS - 1) / ZERO_COLS);
+  // 1024 columns to a warp (each one searches for its rows' tokens), fewer where that leaves multiprocessors without work: 4 warps each of 148
+  // (4000 rows of 771 in float32, 1500 tokens: 28.1 us with 1024 columns, 20.4 with 256)
+  int zero_cols = 1024;
+  while (zero_cols > SLICE && (a.rows + 31) / 32 * ((a.d + zero_cols - 1) / zero_cols) < 148 * 4) zero_cols /= 2;
+  const int64_t zero_units = (a.rows + 31) / 32 * ((a.d + zero_cols - 1) / zero_cols);
   ++*launches;
   cudaError_t e = launch_dependent(gather_kernel<T, O, WIDE>, (unsigned)((chunks * slices + zero_units + GATHER_WARPS - 1) / GATHER_WARPS),
-                                   32 * GATHER_WARPS, 0, st, a, pairs,
-                                   zero_units, chunks * slices);
+                                   32 * GATHER_WARPS, 0, st, a, pairs, zero_cols, zero_units, chunks * slices);
   if (e != cudaSuccess || chunks < 2) return e;
   ++*launches;
   return launch_dependent(join_kernel<O, WIDE>, (unsigned)((chunks - 1) * slices), THREADS, 0, st, a, pairs);
@@ -416,10 +434,9 @@ cudaError_t launch_embedding_backward(cudaStream_t st, const EmbeddingArgs& args
   cudaError_t e = launch_dependent(sort_kernel, (unsigned)((a.tokens + EMB_SORT_BLOCK - 1) / EMB_SORT_BLOCK), SORT_THREADS, 0, st, a, pairs);
   ++*launches;
   for (int64_t block = EMB_SORT_BLOCK; e == cudaSuccess && block < a.tokens; block *= EMB_MERGE) {
-    const bool staged = block == EMB_SORT_BLOCK;
-    const int threads = staged ? merge_threads<true>() : merge_threads<false>();
-    e = launch_dependent(staged ? merge_kernel<true> : merge_kernel<false>, (unsigned)((a.tokens + threads - 1) / threads), threads, 0, st,
-                         (const uint64_t*)pairs, other, a.tokens, block);
+    e = launch_dependent(block == EMB_SORT_BLOCK ? merge_kernel<true> : merge_kernel<false>,
+                         (unsigned)((a.tokens + MERGE_THREADS - 1) / MERGE_THREADS), MERGE_THREADS, 0, st, (const uint64_t*)pairs, other,
+                         a.tokens, block);
     ++*launches;
     uint64_t* t = pairs;
     pairs = other;
