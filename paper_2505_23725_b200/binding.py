@@ -341,7 +341,9 @@ class _Operators:
     stream first waits for it and it then waits for the context's, and the tensors are
     recorded on the context's stream, so inputs, results and their memory may be used as usual."""
 
-    _fast_decoder = {}                           # compiled calls of attention, layer norm and embedding
+    # compiled calls of attention, layer norm and embedding (beside _fast, whose names are a list of their own: either can be emptied to take
+    # the way through Python)
+    _fast_decoder = {}
 
     def _init_operators(self):
         """What every call looks up, once: device number, types, the stream's handle and the way to ask for the handle

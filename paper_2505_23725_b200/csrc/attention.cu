@@ -76,19 +76,6 @@ struct AttnParams {
 };
 
 // ----------------------------- tensor memory --------------------------------
-__device__ __forceinline__ void tm_load32(uint32_t taddr, uint32_t* v) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-      : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
-        "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]),
-        "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]),
-        "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]),
-        "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
-      : "r"(taddr)
-      : "memory");
-}
 __device__ __forceinline__ void tm_store32(uint32_t taddr, const uint32_t* v) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
@@ -108,8 +95,7 @@ __device__ __forceinline__ void tm_store16(uint32_t taddr, const uint32_t* v) {
       : "memory");
 }
 __device__ __forceinline__ void tm_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// Waits for the loads before it; nothing that uses v is moved in front of it.
-__device__ __forceinline__ void tm_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+// Behind tc_ld32, which waits for its load: nothing that uses v is moved in front of this.
 __device__ __forceinline__ void after_load(uint32_t* v) {
   asm volatile(""
                : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
@@ -244,8 +230,7 @@ __device__ __forceinline__ void store_columns(uint32_t t_row, __nv_bfloat16* row
     uint32_t v[32];
     float f[32];
     __syncwarp();
-    tm_load32(t_row + (uint32_t)c, v);
-    tm_load_wait();
+    tc_ld32(t_row + (uint32_t)c, v);
     after_load(v);
 #pragma unroll
     for (int e = 0; e < 32; ++e) f[e] = __uint_as_float(v[e]) * by;
@@ -564,8 +549,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
     Pair shift = both(0.f);
     // 32 of this thread's 64 scores
     auto load_scores = [&](uint32_t (&s)[32], int h, bool last) {
-      tm_load32(t_s + h * 32, s);
-      tm_load_wait();
+      tc_ld32(t_s + h * 32, s);
       after_load(s);
       if (last) {
 #pragma unroll
@@ -594,8 +578,7 @@ attn_fwd_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
 #pragma unroll 1
         for (int i = 0; i < DP / 2; i += 32) {
           uint32_t v[32];
-          tm_load32(t_o + i, v);
-          tm_load_wait();
+          tc_ld32(t_o + i, v);
           after_load(v);
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * by);
@@ -857,8 +840,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
         if (!alive && n > 1) break;
         tc_fence_after();
         uint32_t s[32], d[32];
-        tm_load32(t_s, s);
-        tm_load_wait();
+        tc_ld32(t_s, s);
         after_load(s);
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
@@ -869,8 +851,7 @@ attn_dq_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ AttnP
         if (alive) alive = __all_sync(0xffffffffu, mbar_wait_cta(smem_u32(&bar_dp), step & 1u, &abort_flag, limit));
         if (!alive && n > 1) break;
         tc_fence_after();
-        tm_load32(t_lane + TM_DP + part * QUARTER, d);
-        tm_load_wait();
+        tc_ld32(t_lane + TM_DP + part * QUARTER, d);
         after_load(d);
         uint32_t w[16];
         if (j == n - 1) {                     // where the key comes after the query: no weight, whatever the products hold
@@ -1093,8 +1074,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         if (!alive) break;
         uint32_t s[32], w[16];
         tc_fence_after();
-        tm_load32(t_s, s);
-        tm_load_wait();
+        tc_ld32(t_s, s);
         after_load(s);
   #pragma unroll
         for (int e = 0; e < 32; e += 4) {
@@ -1121,8 +1101,7 @@ attn_dkv_kernel(const __grid_constant__ Maps4 maps, const __grid_constant__ Attn
         if (!alive) break;
         tc_fence_after();
         uint32_t d[32];
-        tm_load32(t_dp, d);
-        tm_load_wait();
+        tc_ld32(t_dp, d);
         after_load(d);
   #pragma unroll
         for (int e = 0; e < 32; e += 4) {

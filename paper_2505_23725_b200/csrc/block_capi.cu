@@ -97,7 +97,7 @@ AttnArgs attention_args(const muloco_attention* a, const muloco_sequences* s, co
   k.q = a->q; k.q_ts = a->q_token_stride; k.q_hs = a->q_head_stride;
   k.k = a->k; k.k_ts = a->k_token_stride; k.k_hs = a->k_head_stride;
   k.v = a->v; k.v_ts = a->v_token_stride; k.v_hs = a->v_head_stride;
-  k.status = v.status; k.wait_limit_ns = v.wait_limit_ns; k.n_sms = v.n_sms;
+  k.status = v.status; k.wait_limit_ns = v.wait_limit_ns;
   return k;
 }
 

@@ -324,7 +324,6 @@ struct AttnArgs {
   void* dq; void* dk; void* dv;                // dense
   int* status;
   unsigned long long wait_limit_ns;
-  int n_sms;
   int withhold;
 };
 cudaError_t launch_attention(cudaStream_t st, const AttnArgs& a, const char** what);            // one launch

@@ -1,7 +1,7 @@
 """The operators of the training step as torch autograd functions.
 
 `owner` is a binding.Context or a binding.MuLoCo.  The backward passes are the library's own kernels; nothing
-is computed twice and nothing else is kept than what their docstrings in binding.py name.  They are differentiable once,
+else is kept than what their docstrings in binding.py name (so attention's makes the scores again).  They are differentiable once,
 in reverse mode: what would need more raises."""
 from __future__ import annotations
 
