@@ -496,7 +496,8 @@ MULOCO_API void muloco_sequences_destroy(muloco_sequences* s);      /* host memo
  * and other sequences hold does not matter, infinities and NaN included; a value that is not finite reaches
  * rows of its own sequence only (also earlier ones, in the tile of 128 tokens that it is in).  Sums of weights may reach 2^16 per
  * 64 keys before they are scaled down, so entries of v beyond about 2^100 may overflow.
- * Limits (MULOCO_ESHAPE): head_dim a multiple of 8, 8..128; heads_q a multiple of heads_k; tokens < 2^31 - 256. */
+ * Limits (MULOCO_ESHAPE): head_dim a multiple of 8, 8..128; heads_q a multiple of heads_k, at most 65536; tokens < 2^31 - 256; the tiles
+ * of 128 tokens of all sequences times heads_q < 2^31. */
 typedef struct {
   int32_t heads_q, heads_k, head_dim;
   float scale;

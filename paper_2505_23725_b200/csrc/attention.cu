@@ -20,13 +20,17 @@
 // query tile (delta, dq), the second over the queries of a key tile with the scores transposed (dk, dv):
 // seven products instead of the five that one kernel with sums in global memory would take, and no float32 copy of dq.
 //
-// Measured (us, in bursts of one call; credited TFLOP/s: 4 and 10 operations per pair, head and entry):
-//   8 x 2048 tokens, 16 heads of 128    forward 168 (820)    backward 545 (630)
-//   1 x 16384, 16 + 4 heads of 128      forward 860 (1280)   backward 3290 (835; 1170 with the two products more)
-//   8 x 2048, 16 heads of 64            forward 138 (500)    backward 435 (395)
+// Measured (us, among other calls; in brackets in bursts of one call; credited TFLOP/s: 4 and 10 operations per pair, head and entry):
+//   8 x 2048 tokens, 16 heads of 128    forward 184 (157 to 175) 749    backward 625 (540 to 580) 550
+//   1 x 16384, 16 + 4 heads of 128      forward 1002 (860 to 980) 1098  backward (3290 to 3450)
+//   8 x 2048, 16 heads of 64            forward (122 to 143)            backward (435 to 460)
+// The moved reference costs the scores read twice more and the sums rewritten: where scores rise along the keys so that it moves at every
+// tile, in bursts 268 instead of 157, 1654 instead of 972, 222 instead of 143 (forward, the three lines above); one move in a row 3 %.
 // Long sequences with heads of 128 run near the power limit.  Elsewhere a step's chain binds: scores to tensor memory, row warps, weights
-// back, products: about 3200 cycles for two forward tiles whose products take 2048 and exponentials 2048 (57 % of either
-// pipe), and a unit's end (8000 cycles: last product, results to memory, first scores of the next).
+// back, products: about 3200 cycles for two forward tiles whose products take 2048 and exponentials 2048, and a unit's end (8000 cycles: last
+// product, results to memory, first scores of the next).  Counters, tensor pipe / exponentials: 57 / 57 % with one sequence of 8192 tokens, 44 / 45 %
+// with 8 x 2048 (products take 120 thousand of 295 thousand cycles), where units' ends weigh more.
+// 96 registers a thread, the most that 576 threads may have: attn_fwd_kernel<128> spills 108 bytes (348 of loads), <64> 28, the others up to 8.
 // Tried and dropped: half to all of the exponentials' load on the floating-point pipes (polynomial of degree 5: 5 to 20 % slower, the
 // pipe is not what is waited for); one thread per row with registers moved between warpgroups (904 against 857); in the backward
 // pass two groups of row warps on alternate steps (682 against 545: a step of a single warp takes twice as long), and dp of the

@@ -59,7 +59,7 @@ muloco_status check_attention(muloco_ctx* c, const muloco_attention* a, const mu
   if (a->head_dim < 8 || a->head_dim > ATTN_MAX_DIM || (a->head_dim & 7))
     return ctx_fail(c, MULOCO_ESHAPE, "head_dim must be a multiple of 8 in 8..%d (got %d)", ATTN_MAX_DIM, a->head_dim);
   if (a->heads_k < 1 || a->heads_q < 1 || a->heads_q > 65536 || a->heads_q % a->heads_k)
-    return ctx_fail(c, MULOCO_ESHAPE, "the count of query heads must be a multiple of that of key heads (got %d, %d)", a->heads_q, a->heads_k);
+    return ctx_fail(c, MULOCO_ESHAPE, "the count of query heads must be a multiple of that of key heads, at most 65536 (got %d, %d)", a->heads_q, a->heads_k);
   if (!(a->scale > 0.f) || !isfinite(a->scale)) return ctx_fail(c, MULOCO_EINVAL, "scale must be positive and finite");
   if (s->n_tiles * a->heads_q > INT32_MAX) return ctx_fail(c, MULOCO_ESHAPE, "too many tokens and heads for one call");
   if (s->tokens == 0) return MULOCO_OK;

@@ -10,9 +10,10 @@
 // chunk, and a last kernel adds those in order: so a token that fills half of the batch does not hold up a single warp, and the
 // sums do not depend on which warp runs first.  Rows without a token are zeroed by warps of their own.
 //
-// Measured: lookup of 16384 x 1024 in bf16 12.3 us (5.5 TB/s).  Gradient of a table of 32000 rows: 16384 tokens x 2048 in float32 94 us, of which
-// writing and reading everything once take 50 (the gathering kernel 61: 4.8 TB/s), sorting 20 and joining 12; 4001 x 768 in bf16
-// 25 us, five dependent kernels of about 5.
+// Measured: lookup of 16384 x 1024 in bf16 12.3 us (5.5 TB/s), in float32 20 (6.7).  Gradient of a table of 32000 rows: 16384 tokens x 2048 in float32
+// 91 us, of which writing and reading everything once take 50 (the gathering kernel 62: 4.7 TB/s; cold: sort 7, merges 5 and 7, join 17); 4001 x 768
+// in bf16 25 us, four dependent kernels (cold: sort 7, merge 7, gather 14, join 5).  A small gradient is five kernels' latency: 16384 x 24
+// takes 28 us whatever the table.
 #include "convert.cuh"
 #include "internal.h"
 
